@@ -454,6 +454,94 @@ int taurus_relabel_csr(int64_t V, int64_t E, const int64_t* row_ptr, const int32
 int taurus_permute_rows(int64_t V, int32_t width, const float* in_rows, int64_t ld_in, const int32_t* rank, float* out_rows,
                         int64_t ld_out, void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Operators on typed rows: what makes the rows that a layer takes and what stands between two layers (no counterpart in
+ * the paper, whose vertices all have features of one kind).  taurus_embed_rows looks rows up in a learned table,
+ * taurus_typed_project gives each vertex type a weight matrix of its own, taurus_norm_rows is a norm with an activation over
+ * a batch of graphs; each has its gradient, so that tables, weights and norms can be trained.
+ *
+ * Rules common to them.  They need no context.  Every pointer is DEVICE memory of the current device, aligned to its element
+ * (anything else: TAURUS_ERR_INVALID_ARG); a pitch ld is in elements, at least the row's width; rows need no alignment, but rows
+ * whose addresses and pitches are multiples of 16 bytes are the fast ones.  All work is enqueued on `cuda_stream` of the current
+ * device and the call returns without waiting; no call allocates or synchronises, so all may be captured into a graph.  A call reads
+ * nothing that an earlier one left in a workspace.  Calls that may run at the same time (two streams, two graphs) need
+ * workspaces of their own; calls in order may share one.  Outputs may not overlap inputs, the workspace or each other except where stated.
+ * Element types of rows are TAURUS_F32, TAURUS_BF16, TAURUS_F16; products, sums and statistics are formed in fp32 or wider and
+ * rounded to the output's type once.  Results do not depend on the launch: the same call gives the same bits.
+ * Widths are 1 .. TAURUS_MAX_ROW_WIDTH (else TAURUS_ERR_UNSUPPORTED), numbers of rows below 2^31; n = 0 is allowed.
+ * Where the argument checks need the device's memory contents (ids, offsets) the kernels check them: nothing outside the arrays is
+ * read or written, and the first error is stored in *status (device int32, may be NULL; a TAURUS_ERR_* code, never cleared by the
+ * library: a program clears it once and reads it when it likes).
+ * The *_workspace functions return bytes (0: none needed) or a negative TAURUS_ERR_* code; workspaces are 256-byte aligned.
+ */
+enum { TAURUS_F32 = 0, TAURUS_BF16 = 1, TAURUS_F16 = 2 };
+enum { TAURUS_ACT_NONE = 0, TAURUS_ACT_RELU = 1, TAURUS_ACT_SILU = 2 };
+#define TAURUS_MAX_ROW_WIDTH 1024
+#define TAURUS_MAX_TYPES 1024
+
+/*
+ * out_rows[i] = scale * table[ids[i]] for i in [0, n); id -1 stands for "no entry" and gives a row of zeros.  Any other id
+ * outside [0, table_rows) gives zeros too and TAURUS_ERR_INVALID_ARG in *status.  table_type and out_type are independent.
+ */
+int taurus_embed_rows(int64_t n, const int64_t* ids, const void* table, int32_t table_type, int64_t table_rows, int32_t width,
+                      int64_t ld_table, float scale, void* out_rows, int32_t out_type, int64_t ld_out, int32_t* status,
+                      void* cuda_stream);
+/*
+ * Gradient of the table: grad_table[v] = scale * (sum of grad_rows[i] over the i with ids[i] = v), every row of it written (zeros
+ * where no id names it).  The ids are sorted, and each sum is formed in the order of i.  Ids outside the table as above: they
+ * add to nothing.
+ */
+int64_t taurus_embed_grad_workspace(int64_t n, int64_t table_rows, int32_t width);
+int taurus_embed_grad(int64_t n, const int64_t* ids, const void* grad_rows, int32_t grad_type, int64_t ld_grad, int32_t width,
+                      float scale, void* grad_table, int32_t table_type, int64_t table_rows, int64_t ld_table, void* workspace,
+                      int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+
+/*
+ * Projection by vertex type: out[r] = x[r] W[g] + bias[g] for the rows r in [offsets[g], offsets[g + 1]) of type g, g in
+ * [0, types), types in 1 .. TAURUS_MAX_TYPES.  offsets: [types + 1], non-decreasing, inside [0, n]; a type may have no rows; rows of out in
+ * front of offsets[0] or behind offsets[types] are left as they are.  Offsets that break this give TAURUS_ERR_INVALID_ARG in *status (the
+ * rows written are then unspecified).  W: [types x d_in x d_out] row-major without gaps, of x's type; bias: [types x d_out] fp32 or
+ * NULL; out_type: x's type or TAURUS_F32.  With TAURUS_F32 operands the products are as exact as fp32 multiplications; the sums are fp32.
+ */
+int64_t taurus_typed_project_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type);
+int taurus_typed_project(int64_t n, int32_t types, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, const void* W,
+                         const float* bias, int32_t d_in, int32_t d_out, void* out, int32_t out_type, int64_t ld_out, void* workspace,
+                         int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+/*
+ * Gradients of taurus_typed_project from grad_out ([n x d_out], x's type).  Any of the three may be NULL:
+ *   grad_x[r]    = grad_out[r] W[g]^T                                          (x's type; rows outside the types' ranges are left as they are)
+ *   grad_W[g]    = sum over the rows of type g of x[r]^T grad_out[r]           (grad_W_type: x's type or TAURUS_F32; zeros for a type without rows)
+ *   grad_bias[g] = sum over the rows of type g of grad_out[r]                  (fp32)
+ */
+int64_t taurus_typed_project_grad_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type);
+int taurus_typed_project_grad(int64_t n, int32_t types, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, const void* W,
+                              const void* grad_out, int64_t ld_grad, int32_t d_in, int32_t d_out, void* grad_x, int64_t ld_grad_x, void* grad_W,
+                              int32_t grad_W_type, float* grad_bias, void* workspace, int64_t workspace_bytes, int32_t* status,
+                              void* cuda_stream);
+
+/*
+ * Group norm with an activation, channels last, over a batch of graphs: graph s owns rows [offsets[s], offsets[s + 1]) of x
+ * ([n x width]), its channels form `groups` groups of width / groups neighbours, and for each (graph, group)
+ *     out = act(gamma * (x - mean) / sqrt(var + eps) + beta)
+ * with the mean and the (biased) variance over the graph's rows and the group's channels.  groups = 1 normalises a graph as a whole, groups = width
+ * each channel by itself.  offsets: [graphs + 1] as in taurus_typed_project (rows outside are left as they are), or NULL for one graph of n rows (graphs = 1).
+ * gamma, beta: [width] fp32 or NULL (ones, zeros).  mean, rstd: [graphs x groups] fp32, NULL unless the gradient will be taken (zeros for a graph without
+ * rows).  out_rows may be x itself with the same pitch.
+ */
+int64_t taurus_norm_rows_workspace(int64_t n, int64_t graphs, int32_t width, int32_t groups);
+int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, int32_t width,
+                     int32_t groups, const float* gamma, const float* beta, float eps, int32_t act, void* out_rows, int64_t ld_out,
+                     float* mean, float* rstd, void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+/*
+ * Gradients of taurus_norm_rows from grad_out, with mean and rstd as the forward call left them.  All rows are of `type`; grad_x may be x or
+ * grad_out itself with the same pitch.  grad_gamma, grad_beta: [width] fp32, either may be NULL.  The slope of ReLU at 0 is 0.
+ */
+int64_t taurus_norm_rows_grad_workspace(int64_t n, int64_t graphs, int32_t width, int32_t groups);
+int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, int32_t width,
+                          int32_t groups, const float* gamma, const float* beta, int32_t act, const float* mean, const float* rstd,
+                          const void* grad_out, int64_t ld_grad, void* grad_x, int64_t ld_grad_x, float* grad_gamma, float* grad_beta,
+                          void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+
 /* Which order layer `layer` runs in: *out_aggregate_first = 1 when it aggregates (scaled) input rows and applies the
  * weights to the finished rows (see TAURUS_FLAG_PROJECT_FIRST), 0 when it projects every chunk first;
  * *out_row_floats = floats per accumulator row (and per evicted row) of that layer.  Either pointer may be NULL.

@@ -18,6 +18,9 @@ ERROR_CODES = {
     "CUDA": -6, "INTERNAL": -7, "NOMEM": -8, "UNSUPPORTED": -9, "RUN_STORE_FULL": -10, "RUNS_INCOMPLETE": -11,
 }
 RUNS_HOST, RUNS_DEVICE = 0, 1
+F32, BF16, F16 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+MAX_ROW_WIDTH, MAX_TYPES = 1024, 1024
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _lib = None
@@ -91,6 +94,9 @@ EXPORTS = [
     "taurus_runs_directory", "taurus_runs_get_run", "taurus_runs_reset", "taurus_runs_destroy",
     "taurus_layer_set_run_output", "taurus_push_chunk_from_runs", "taurus_gat_project_chunk", "taurus_gat_attention",
     "taurus_get_sample_digest", "taurus_gat_project_chunk_from_runs", "taurus_relabel_csr", "taurus_permute_rows",
+    "taurus_embed_rows", "taurus_embed_grad", "taurus_embed_grad_workspace", "taurus_typed_project", "taurus_typed_project_workspace",
+    "taurus_typed_project_grad", "taurus_typed_project_grad_workspace", "taurus_norm_rows", "taurus_norm_rows_workspace",
+    "taurus_norm_rows_grad", "taurus_norm_rows_grad_workspace",
 ]
 NOALLOC_MAX_VERTICES = 4 * 1024 * 1024
 
@@ -139,6 +145,18 @@ def load_library():
     lib.taurus_gat_project_chunk_from_runs.argtypes = [vp, i64, i64, vp, vp, i64, vp]
     lib.taurus_relabel_csr.argtypes = [i64, i64, vp, vp, vp, vp, vp, vp, vp]
     lib.taurus_permute_rows.argtypes = [i64, i32, vp, i64, vp, vp, i64, vp]
+    f32 = ctypes.c_float
+    lib.taurus_embed_rows.argtypes = [i64, vp, vp, i32, i64, i32, i64, f32, vp, i32, i64, vp, vp]
+    lib.taurus_embed_grad.argtypes = [i64, vp, vp, i32, i64, i32, f32, vp, i32, i64, i64, vp, i64, vp, vp]
+    lib.taurus_typed_project.argtypes = [i64, i32, vp, vp, i64, i32, vp, vp, i32, i32, vp, i32, i64, vp, i64, vp, vp]
+    lib.taurus_typed_project_grad.argtypes = [i64, i32, vp, vp, i64, i32, vp, vp, i64, i32, i32, vp, i64, vp, i32, vp, vp, i64, vp, vp]
+    lib.taurus_norm_rows.argtypes = [i64, i64, vp, vp, i64, i32, i32, i32, vp, vp, f32, i32, vp, i64, vp, vp, vp, i64, vp, vp]
+    lib.taurus_norm_rows_grad.argtypes = [i64, i64, vp, vp, i64, i32, i32, i32, vp, vp, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp]
+    lib.taurus_embed_grad_workspace.argtypes = [i64, i64, i32]
+    lib.taurus_typed_project_workspace.argtypes = lib.taurus_typed_project_grad_workspace.argtypes = [i64, i32, i32, i32, i32]
+    lib.taurus_norm_rows_workspace.argtypes = lib.taurus_norm_rows_grad_workspace.argtypes = [i64, i64, i32, i32]
+    for name in ("embed_grad", "typed_project", "typed_project_grad", "norm_rows", "norm_rows_grad"):
+        getattr(lib, "taurus_%s_workspace" % name).restype = i64
     lib.taurus_get_layer_plan.argtypes = [vp, ctypes.c_int32, vp, vp]
     lib.taurus_launch_count.argtypes = [vp]
     lib.taurus_launch_count.restype = i64
@@ -215,6 +233,139 @@ def permute_rows(V: int, width: int, in_rows, ld_in: int, rank, out_rows, ld_out
     rc = load_library().taurus_permute_rows(V, width, _ptr(in_rows), ld_in, _ptr(rank), _ptr(out_rows), ld_out, _stream(stream))
     if rc != 0:
         raise TaurusError(rc, "taurus_permute_rows")
+
+
+def _row_type(t) -> int:
+    """F32, BF16 or F16 of a torch or numpy dtype, of a tensor or array, or as it is given (F32, ...)."""
+    if isinstance(t, int):
+        return t
+    name = str(getattr(t, "dtype", t)).replace("torch.", "")
+    if name not in ("float32", "bfloat16", "float16"):
+        raise TypeError("rows are float32, bfloat16 or float16, got %s" % name)
+    return {"float32": F32, "bfloat16": BF16, "float16": F16}[name]
+
+
+def _rows(x, n: int, width: int, ld: int) -> Optional[int]:
+    """Address of n rows: a 2-D tensor of at least n x width whose rows are contiguous and ld elements apart, or an address."""
+    if x is None or isinstance(x, int):
+        return x
+    if x.dim() != 2 or x.shape[0] < n or x.shape[1] < width or (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) != ld):
+        raise ValueError("expected at least %d contiguous rows of %d elements, %d elements apart" % (n, width, ld))
+    return x.data_ptr()
+
+
+def _array(x, dtype: Optional[str], count: int) -> Optional[int]:
+    """Address of a contiguous tensor of at least count elements of that dtype, or an address."""
+    if hasattr(x, "numel"):
+        if dtype and str(x.dtype).replace("torch.", "") != dtype:
+            raise TypeError("expected %s, got %s" % (dtype, x.dtype))
+        if x.numel() < count:
+            raise ValueError("expected at least %d elements, got %d" % (count, x.numel()))
+    return _ptr(x)
+
+
+def _space(workspace):
+    """Address and bytes of a workspace tensor."""
+    return (None, 0) if workspace is None else (_ptr(workspace), workspace.numel() * workspace.element_size())
+
+
+def _checked(rc: int, where: str) -> int:
+    if rc < 0:
+        raise TaurusError(rc, where, load_library().taurus_last_cuda_error().decode() if rc == ERROR_CODES["CUDA"] else "")
+    return rc
+
+
+def embed_rows(n: int, ids, table, table_rows: int, width: int, ld_table: int, out_rows, ld_out: int, scale: float = 1.0, status=None, stream=None,
+               table_type=None, out_type=None):
+    """taurus_embed_rows: out_rows[i] = scale * table[ids[i]] (id -1: zeros).  Device tensors; ids int64.  Types are those of the
+    tensors; with addresses in their place table_type and out_type say them."""
+    _checked(load_library().taurus_embed_rows(
+        n, _array(ids, "int64", n), _rows(table, table_rows, width, ld_table), _row_type(table if table_type is None else table_type), table_rows, width, ld_table, scale,
+        _rows(out_rows, n, width, ld_out), _row_type(out_rows if out_type is None else out_type), ld_out, _array(status, "int32", 1), _stream(stream)),
+        "taurus_embed_rows")
+
+
+def embed_grad_workspace(n: int, table_rows: int, width: int) -> int:
+    """Bytes of embed_grad's workspace."""
+    return _checked(load_library().taurus_embed_grad_workspace(n, table_rows, width), "taurus_embed_grad_workspace")
+
+
+def embed_grad(n: int, ids, grad_rows, ld_grad: int, width: int, grad_table, table_rows: int, ld_table: int, workspace, scale: float = 1.0, status=None,
+               stream=None, grad_type=None, table_type=None):
+    """taurus_embed_grad: grad_table[v] = scale * sum of the grad_rows[i] with ids[i] = v; every row is written."""
+    _checked(load_library().taurus_embed_grad(
+        n, _array(ids, "int64", n), _rows(grad_rows, n, width, ld_grad), _row_type(grad_rows if grad_type is None else grad_type), ld_grad, width, scale,
+        _rows(grad_table, table_rows, width, ld_table), _row_type(grad_table if table_type is None else table_type), table_rows, ld_table, *_space(workspace),
+        _array(status, "int32", 1), _stream(stream)), "taurus_embed_grad")
+
+
+def typed_project_workspace(n: int, types: int, d_in: int, d_out: int, type) -> int:
+    """Bytes of typed_project's workspace; type: dtype of x and W."""
+    return _checked(load_library().taurus_typed_project_workspace(n, types, d_in, d_out, _row_type(type)), "taurus_typed_project_workspace")
+
+
+def typed_project(n: int, types: int, offsets, x, ld_x: int, W, bias, d_in: int, d_out: int, out, ld_out: int, workspace=None, status=None, stream=None,
+                  type=None, out_type=None):
+    """taurus_typed_project: out[r] = x[r] W[g] + bias[g] for the rows r in [offsets[g], offsets[g + 1])."""
+    t = _row_type(x if type is None else type)
+    if hasattr(W, "dtype") and _row_type(W) != t:
+        raise TypeError("x and W are of one type")
+    _checked(load_library().taurus_typed_project(
+        n, types, _array(offsets, "int64", types + 1), _rows(x, n, d_in, ld_x), ld_x, t, _array(W, None, types * d_in * d_out), _array(bias, "float32", types * d_out), d_in, d_out, _rows(out, n, d_out, ld_out),
+        _row_type(out if out_type is None else out_type), ld_out, *_space(workspace), _array(status, "int32", 1), _stream(stream)), "taurus_typed_project")
+
+
+def typed_project_grad_workspace(n: int, types: int, d_in: int, d_out: int, type) -> int:
+    """Bytes of typed_project_grad's workspace; type: dtype of x, W and grad_out."""
+    return _checked(load_library().taurus_typed_project_grad_workspace(n, types, d_in, d_out, _row_type(type)), "taurus_typed_project_grad_workspace")
+
+
+def typed_project_grad(n: int, types: int, offsets, x, ld_x: int, W, grad_out, ld_grad: int, d_in: int, d_out: int, grad_x=None, ld_grad_x: int = 0, grad_W=None,
+                       grad_bias=None, workspace=None, status=None, stream=None, type=None, grad_W_type=None):
+    """taurus_typed_project_grad: the gradients asked for (grad_x, grad_W, grad_bias) from grad_out."""
+    t = _row_type(grad_out if type is None else type)
+    for other in (x, W, grad_out, grad_x):
+        if hasattr(other, "dtype") and _row_type(other) != t:
+            raise TypeError("x, W, grad_out and grad_x are of one type")
+    _checked(load_library().taurus_typed_project_grad(
+        n, types, _array(offsets, "int64", types + 1), _rows(x, n, d_in, ld_x), ld_x, t, _array(W, None, types * d_in * d_out), _rows(grad_out, n, d_out, ld_grad), ld_grad, d_in, d_out, _rows(grad_x, n, d_in, ld_grad_x or d_in),
+        ld_grad_x or d_in, _array(grad_W, None, types * d_in * d_out), t if grad_W is None else _row_type(grad_W if grad_W_type is None else grad_W_type), _array(grad_bias, "float32", types * d_out),
+        *_space(workspace), _array(status, "int32", 1), _stream(stream)), "taurus_typed_project_grad")
+
+
+def norm_rows_workspace(n: int, graphs: int, width: int, groups: int) -> int:
+    """Bytes of norm_rows' workspace."""
+    return _checked(load_library().taurus_norm_rows_workspace(n, graphs, width, groups), "taurus_norm_rows_workspace")
+
+
+def norm_rows(n: int, graphs: int, offsets, x, ld_x: int, width: int, groups: int, gamma, beta, eps: float, act: int, out_rows, ld_out: int, mean=None, rstd=None,
+              workspace=None, status=None, stream=None, type=None):
+    """taurus_norm_rows: group norm with an activation (ACT_NONE, ACT_RELU, ACT_SILU) over the rows of each graph."""
+    t = _row_type(x if type is None else type)
+    if hasattr(out_rows, "dtype") and _row_type(out_rows) != t:
+        raise TypeError("x and out_rows are of one type")
+    _checked(load_library().taurus_norm_rows(
+        n, graphs, _array(offsets, "int64", graphs + 1), _rows(x, n, width, ld_x), ld_x, t, width, groups, _array(gamma, "float32", width), _array(beta, "float32", width), eps, act,
+        _rows(out_rows, n, width, ld_out), ld_out, _array(mean, "float32", graphs * groups), _array(rstd, "float32", graphs * groups), *_space(workspace), _array(status, "int32", 1), _stream(stream)),
+        "taurus_norm_rows")
+
+
+def norm_rows_grad_workspace(n: int, graphs: int, width: int, groups: int) -> int:
+    """Bytes of norm_rows_grad's workspace."""
+    return _checked(load_library().taurus_norm_rows_grad_workspace(n, graphs, width, groups), "taurus_norm_rows_grad_workspace")
+
+
+def norm_rows_grad(n: int, graphs: int, offsets, x, ld_x: int, width: int, groups: int, gamma, beta, act: int, mean, rstd, grad_out, ld_grad: int, grad_x,
+                   ld_grad_x: int, grad_gamma=None, grad_beta=None, workspace=None, status=None, stream=None, type=None):
+    """taurus_norm_rows_grad: gradients of norm_rows, with mean and rstd as the forward call left them."""
+    t = _row_type(x if type is None else type)
+    for other in (grad_out, grad_x):
+        if hasattr(other, "dtype") and _row_type(other) != t:
+            raise TypeError("x, grad_out and grad_x are of one type")
+    _checked(load_library().taurus_norm_rows_grad(
+        n, graphs, _array(offsets, "int64", graphs + 1), _rows(x, n, width, ld_x), ld_x, t, width, groups, _array(gamma, "float32", width), _array(beta, "float32", width), act, _array(mean, "float32", graphs * groups),
+        _array(rstd, "float32", graphs * groups), _rows(grad_out, n, width, ld_grad), ld_grad, _rows(grad_x, n, width, ld_grad_x), ld_grad_x, _array(grad_gamma, "float32", width), _array(grad_beta, "float32", width),
+        *_space(workspace), _array(status, "int32", 1), _stream(stream)), "taurus_norm_rows_grad")
 
 
 class Runs:

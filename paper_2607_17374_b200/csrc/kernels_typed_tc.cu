@@ -1,0 +1,794 @@
+// Products by vertex type on the 5th-generation tensor cores.  One kernel, three products:
+//   PROJECT   out[r]    = x[r] W[g] + bias[g]        rows of x are K-major A tiles, W is an MN-major B tile
+//   GRAD_X    grad_x[r] = grad_out[r] W[g]^T         rows of grad_out are K-major A tiles, W is a K-major B tile
+//   GRAD_W    grad_W[g] = x_g^T grad_out_g           both are MN-major: the rows are what is summed over
+//
+// Persistent: one CTA per SM walks units, a unit is a 128-row tile of the output of one type and a block of up to BN columns (GRAD_W: 128 rows of
+// grad_W[g] and a block of columns, over one chunk of the type's rows; a type of several chunks leaves one partial product a chunk, which
+// typed_join_kernel adds up in their order).  Which units there are follows from the offsets in device memory: every CTA works it out for itself.
+// Roles:  warp 0       TMA: operands that stand in memory as the tensor core takes them
+//         warp 1       tcgen05.mma, accumulators in TMEM, two slots of 256 columns: the epilogue of a unit runs beside the products of the next
+//         warps 2..5   epilogue: TMEM -> registers -> transposed through shared memory -> rows
+//         warps 6..13  loaders (LOADED): operands that have to be split, or whose rows TMA cannot address
+//
+// fp32 operands: x = hi + mid + lo, three bf16 values that hold its 24 bits (hi by truncation, so that nothing overflows), and six of the nine
+// products: hi hi into one accumulator, hi mid + mid hi + mid mid + hi lo + lo hi into another.  What is left out is below 2^-24 of a product.
+// Each element keeps an exponent of its own, whatever stands beside it.  Two accumulators: where hi hi is not finite the sum is what it says
+// (an infinity times a mid or lo of zero would make it NaN).  W is split by a kernel in front (it is read once per tile), rows by the loaders.
+//
+// Every wait is bounded, as in the projection of the layers: a CTA that gives up records TAURUS_ERR_INTERNAL, waits (bounded) for its copies and
+// products in flight, frees its TMEM and returns.  Every TMA load is a plain load of the issuing CTA alone.
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "stage_waits.h"
+#include "typed.cuh"
+
+namespace {
+
+enum { PROJECT = 0, GRAD_X = 1, GRAD_W = 2 };
+
+constexpr int BM = 128, STAGES = 4, MAX_G = TAURUS_MAX_TYPES;
+constexpr int STAGE_BYTES = 48 * 1024;
+constexpr int OPERAND_BYTES = STAGES * STAGE_BYTES;
+constexpr int EPI_WARPS = 4, LOAD_WARPS = 8, LOADERS = 32 * LOAD_WARPS;
+constexpr int EPI_TILE_BYTES = 32 * 128;              // 32 rows x 32 fp32
+constexpr unsigned WAIT_LIMIT = 1u << 24;
+
+template <class T> constexpr int planes_of() { return sizeof(T) == 4 ? 3 : 1; }
+template <class T> constexpr int block_k() { return sizeof(T) == 4 ? 32 : 64; }                   // columns (rows) of a stage
+template <class T, bool LOADED> constexpr int block_n() { return LOADED ? 128 : 256; }
+
+struct Shared {
+  unsigned long long full[STAGES], empty[STAGES], acc_full[2], acc_empty[2];
+  unsigned tmem_base;
+  int abort_flag, loads, mmas;
+  int begin[MAX_G + 1];       // rows of type g: [begin[g], begin[g + 1]) (the types' rows follow one another)
+  int prefix[MAX_G + 1];      // units (row tiles, chunks) in front of type g
+  int slot[MAX_G + 1];        // GRAD_W: partial products in front of type g
+};
+constexpr int SHARED_BYTES = OPERAND_BYTES + EPI_WARPS * EPI_TILE_BYTES + (int)sizeof(Shared);
+static_assert(SHARED_BYTES <= 227 * 1024, "shared memory of a block");
+
+struct TcArgs {
+  long long n;
+  const long long* offsets;
+  int types;
+  int M, N, Kc;               // GRAD_W: rows of grad_W (M), columns (N); else columns of the output (N), length of the sums (Kc)
+  int bn, n_blocks, m_blocks; // columns of a block; blocks of columns; GRAD_W: blocks of rows
+  int chunk;                  // GRAD_W: rows of a chunk
+  const void *a, *b;          // LOADED: rows of A; GRAD_W: rows of B too
+  long long lda, ldb;
+  int a_vec, b_vec;           // four elements at a time
+  void* out;
+  long long ld_out;           // PROJECT, GRAD_X
+  int out_f32;                // the output is fp32, else of the operands' type
+  int out_vec;                // four columns at a time
+  const float* bias;
+  float* part;                // GRAD_W: [slots x (M + 1) x N]
+  int32_t* status;
+};
+
+// ---------------------------------------------------------------------------------------------------------------- PTX
+__device__ __forceinline__ unsigned smem_u32(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(unsigned long long* bar, unsigned count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
+}
+__device__ __forceinline__ void mbar_arrive(unsigned long long* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx(unsigned long long* bar, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(unsigned long long* bar, unsigned parity) {
+  unsigned ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait(unsigned long long* bar, unsigned parity, volatile int* abort_flag) {
+  for (unsigned i = 0; i < WAIT_LIMIT; ++i) {
+    if (mbar_try(bar, parity)) return true;
+    if ((i & 63u) == 63u && *abort_flag) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+__device__ __forceinline__ bool mbar_wait_warp(unsigned long long* bar, unsigned parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+__device__ __forceinline__ void tma_2d(unsigned dst, const CUtensorMap* map, int x, int y, unsigned long long* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tma_3d(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned long long* bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
+}
+// K-major operand: rows of ROW bytes (128- or 64-byte swizzle), groups of 8 rows behind one another.
+template <int ROW>
+__device__ __forceinline__ unsigned long long desc_k(unsigned addr) {
+  static_assert(ROW == 128 || ROW == 64, "operand rows of 128 or 64 bytes");
+  return (unsigned long long)((addr & 0x3FFFFu) >> 4) | 1ull << 16 | (unsigned long long)((8 * ROW) >> 4) << 32 | 1ull << 46 | (ROW == 128 ? 2ull : 4ull) << 61;
+}
+// MN-major operand: rows of 64 elements (128 bytes, 128-byte swizzle), one for each index that is summed over, in groups of 8; the next 64
+// elements of the other index `block` bytes on.
+__device__ __forceinline__ unsigned long long desc_mn(unsigned addr, unsigned block) {
+  return (unsigned long long)((addr & 0x3FFFFu) >> 4) | (unsigned long long)(block >> 4) << 16 | (unsigned long long)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+__device__ __forceinline__ void umma(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_commit(unsigned long long* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// 32 columns of an accumulator, one row per lane.
+__device__ __forceinline__ void tmem_ld32(unsigned (&v)[32], unsigned taddr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+        "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+        "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// ---------------------------------------------------------------------------------------------------------------- units
+// Fills begin, prefix and slot; false (for every thread of every CTA) when the offsets are not what they have to be.
+template <int KIND>
+__device__ __forceinline__ bool plan(const TcArgs& a, Shared* s) {
+  bool bad = false;
+  for (int g = threadIdx.x; g <= a.types; g += blockDim.x) {
+    const long long b = a.offsets[g], e = g < a.types ? a.offsets[g + 1] : a.n;
+    bad |= b < 0 || b > a.n || e > a.n || e < b;
+    s->begin[g] = (int)b;
+  }
+  if (__syncthreads_or(bad)) return false;
+  if (threadIdx.x < 32) {
+    int units = 0, slots = 0;
+    for (int g0 = 0; g0 <= a.types; g0 += 32) {
+      const int g = g0 + threadIdx.x, len = g < a.types ? s->begin[g + 1] - s->begin[g] : 0;
+      int u = 0, p = 0;
+      if (g < a.types) {
+        if (KIND == GRAD_W) { u = len > 0 ? (len + a.chunk - 1) / a.chunk : 1; p = u > 1 ? u : 0; }
+        else u = (len + BM - 1) / BM;
+      }
+      int iu = u, ip = p;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, iu, o), y = __shfl_up_sync(0xffffffffu, ip, o);
+        if ((int)threadIdx.x >= o) { iu += x; ip += y; }
+      }
+      if (g <= a.types) { s->prefix[g] = units + iu - u; s->slot[g] = slots + ip - p; }
+      units += __shfl_sync(0xffffffffu, iu, 31);
+      slots += __shfl_sync(0xffffffffu, ip, 31);
+    }
+  }
+  __syncthreads();
+  return true;
+}
+
+struct Unit {
+  int g, row0, rows;     // type; first row of the tile (of the chunk), rows
+  int m0, n0, bw;        // GRAD_W: first row of grad_W; first column of the block, columns (a multiple of 16)
+  int steps;             // stages
+  int slot;              // GRAD_W: partial product, -1: the result itself
+};
+template <int KIND, int BK>
+__device__ __forceinline__ Unit unit_at(const TcArgs& a, const Shared* s, int w) {
+  Unit u;
+  const int per = KIND == GRAD_W ? a.m_blocks * a.n_blocks : a.n_blocks;
+  const int t = w / per, b = w % per;
+  int lo = 0, hi = a.types;                       // the type g with prefix[g] <= t < prefix[g + 1]
+  while (hi - lo > 1) { const int m = (lo + hi) >> 1; if (s->prefix[m] <= t) lo = m; else hi = m; }
+  u.g = lo;
+  const int nth = t - s->prefix[lo], height = KIND == GRAD_W ? a.chunk : BM;
+  u.row0 = s->begin[lo] + nth * height;
+  u.rows = min(height, s->begin[lo + 1] - u.row0);
+  u.m0 = KIND == GRAD_W ? b / a.n_blocks * BM : 0;
+  u.n0 = (KIND == GRAD_W ? b % a.n_blocks : b) * a.bn;
+  u.bw = min(a.bn, (a.N - u.n0 + 15) / 16 * 16);
+  u.steps = KIND == GRAD_W ? (u.rows + BK - 1) / BK : (a.Kc + BK - 1) / BK;
+  u.slot = KIND == GRAD_W && s->prefix[lo + 1] - s->prefix[lo] > 1 ? s->slot[lo] + nth : -1;
+  return u;
+}
+
+// ---------------------------------------------------------------------------------------------------------------- loaders
+// Four neighbouring elements of a row as bf16 planes (fp32) or as they are (16 bits), 8 bytes a plane.
+template <class T> struct Quad { T v[4]; };
+
+template <class T>
+__device__ __forceinline__ Quad<T> load_quad(const T* row, int c, int limit, bool vec) {     // row null: zeros
+  Quad<T> q;
+  if (row && vec && c + 4 <= limit) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(&q) = __ldg(reinterpret_cast<const float4*>(row + c));
+    else *reinterpret_cast<uint2*>(&q) = __ldg(reinterpret_cast<const uint2*>(row + c));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q.v[i] = row && c + i < limit ? row[c + i] : from_f32<T>(0.f);
+  }
+  return q;
+}
+__device__ __forceinline__ unsigned pack2(float a, float b) {
+  const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const unsigned*>(&r);
+}
+template <class T>
+__device__ __forceinline__ void store_quad(unsigned addr, unsigned plane_bytes, const Quad<T>& q) {
+  if constexpr (sizeof(T) == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(&q);
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
+  } else {
+    unsigned h[2], m[2], l[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const Split3 s0 = split3(q.v[2 * i]), s1 = split3(q.v[2 * i + 1]);
+      h[i] = pack2(s0.hi, s1.hi); m[i] = pack2(s0.mid, s1.mid); l[i] = pack2(s0.lo, s1.lo);
+    }
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(h[0]), "r"(h[1]) : "memory");
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr + plane_bytes), "r"(m[0]), "r"(m[1]) : "memory");
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr + 2 * plane_bytes), "r"(l[0]), "r"(l[1]) : "memory");
+  }
+}
+
+// What a loader thread brings of one stage.
+template <class T, int KIND>
+struct Loader {
+  static constexpr int BK = block_k<T>(), QUADS_A = BM * BK / 4 / LOADERS, QUADS_B = KIND == GRAD_W ? QUADS_A : 0;
+  Quad<T> q[QUADS_A + QUADS_B];
+
+  __device__ __forceinline__ void load(const TcArgs& a, const Unit& u, int step, int t) {
+    if constexpr (KIND != GRAD_W) {          // rows of 128-row tile, BK columns
+#pragma unroll
+      for (int i = 0; i < QUADS_A; ++i) {
+        const int at = t + i * LOADERS, r = at / (BK / 4), c = step * BK + at % (BK / 4) * 4;
+        const T* const row = r < u.rows ? static_cast<const T*>(a.a) + (u.row0 + (long long)r) * a.lda : nullptr;
+        q[i] = load_quad(row, c, a.Kc, a.a_vec);
+      }
+    } else {                                 // BK rows, 128 columns of either operand
+#pragma unroll
+      for (int i = 0; i < QUADS_A; ++i) {
+        const int at = t + i * LOADERS, r = at / 32, c = at % 32 * 4;
+        const bool in = step * BK + r < u.rows;
+        const long long row = u.row0 + (long long)step * BK + r;
+        q[i] = load_quad(in ? static_cast<const T*>(a.a) + row * a.lda : nullptr, u.m0 + c, a.M, a.a_vec);
+        q[QUADS_A + i] = load_quad(in && c < u.bw ? static_cast<const T*>(a.b) + row * a.ldb : nullptr, u.n0 + c, a.N, a.b_vec);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(unsigned stage, int t) const {
+    constexpr unsigned PLANE = BM * BK * 2;  // bytes of a plane of either operand (blocks of 128 columns)
+    if constexpr (KIND != GRAD_W) {
+#pragma unroll
+      for (int i = 0; i < QUADS_A; ++i) {
+        const int at = t + i * LOADERS, r = at / (BK / 4), c = at % (BK / 4);
+        const int chunk = BK == 64 ? (c >> 1) ^ (r & 7) : (c >> 1) ^ ((r >> 1) & 3);
+        store_quad<T>(stage + r * (BK * 2) + chunk * 16 + (c & 1) * 8, PLANE, q[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < QUADS_A; ++i) {
+        const int at = t + i * LOADERS, r = at / 32, c = at % 32;      // quad c: block of 64 columns c / 16
+        const unsigned off = (c >> 4) * (BK * 128) + r * 128 + ((((c & 15) >> 1) ^ (r & 7)) << 4) + (c & 1) * 8;
+        store_quad<T>(stage + off, PLANE, q[i]);
+        store_quad<T>(stage + planes_of<T>() * PLANE + off, PLANE, q[QUADS_A + i]);
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------------------------------------------- kernel
+template <class T, int KIND, bool LOADED>
+__global__ void __launch_bounds__(32 * (2 + EPI_WARPS + (LOADED ? LOAD_WARPS : 0)), 1)
+typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ TcArgs a) {
+  static_assert(LOADED || sizeof(T) == 2, "fp32 operands are split by the loaders");
+  constexpr int NP = planes_of<T>(), BK = block_k<T>(), BN = block_n<T, LOADED>(), ROW = BK * 2;
+  constexpr unsigned PLANE_A = BM * BK * 2, PLANE_B = BN * BK * 2;
+  static_assert(NP * (PLANE_A + PLANE_B) <= (unsigned)STAGE_BYTES, "a stage's operands");
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* const staging = smem + OPERAND_BYTES;
+  Shared* const sh = reinterpret_cast<Shared*>(staging + EPI_WARPS * EPI_TILE_BYTES);
+  volatile int* const abort_flag = &sh->abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if ((smem_u32(smem) & 1023u) != 0) {                     // the swizzled tiles want it
+    if (threadIdx.x == 0) rows_status(a.status, TAURUS_ERR_INTERNAL);
+    return;
+  }
+  if (!plan<KIND>(a, sh)) {
+    if (threadIdx.x == 0) rows_status(a.status, TAURUS_ERR_INVALID_ARG);
+    return;
+  }
+  const int units = sh->prefix[a.types] * (KIND == GRAD_W ? a.m_blocks * a.n_blocks : a.n_blocks);
+  if ((int)blockIdx.x >= units) return;
+  constexpr bool TMA_A = !LOADED, TMA_B = !LOADED || KIND != GRAD_W;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) { mbar_init(&sh->full[s], (TMA_A || TMA_B ? 1 : 0) + (LOADED ? LOAD_WARPS : 0)); mbar_init(&sh->empty[s], 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(&sh->acc_full[b], 1); mbar_init(&sh->acc_empty[b], EPI_WARPS); }
+    sh->abort_flag = 0; sh->loads = 0; sh->mmas = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const unsigned tmem_base = sh->tmem_base;
+  const unsigned operands = smem_u32(smem);
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA
+    if ((TMA_A || TMA_B) && lane == 0) {
+      int it = 0;
+      for (int w = blockIdx.x; w < units && !*abort_flag; w += gridDim.x) {
+        const Unit u = unit_at<KIND, BK>(a, sh, w);
+        const int boxes_n = (u.bw + 63) / 64;
+        bool ok = true;
+        for (int k = 0; k < u.steps; ++k, ++it) {
+          const int s = it % STAGES;
+          if (it >= STAGES && !mbar_wait(&sh->empty[s], (it / STAGES & 1) ^ 1, abort_flag)) { ok = false; break; }
+          const unsigned st = operands + s * STAGE_BYTES, sb = st + NP * PLANE_A;
+          unsigned long long* const bar = &sh->full[s];
+          const unsigned bytes_a = TMA_A ? PLANE_A : 0;
+          const unsigned bytes_b = KIND == GRAD_X ? NP * a.bn * ROW : NP * boxes_n * (BK * 128);
+          mbar_expect_tx(bar, bytes_a + bytes_b);
+          if (TMA_A) {
+            if (KIND == GRAD_W) {
+              tma_2d(st, &map_a, u.m0, u.row0 + k * BK, bar);
+              tma_2d(st + BK * 128, &map_a, u.m0 + 64, u.row0 + k * BK, bar);      // (behind the last column: zeros)
+            } else {
+              tma_2d(st, &map_a, k * BK, u.row0, bar);
+            }
+          }
+          if (KIND == GRAD_W) {
+            for (int j = 0; j < boxes_n; ++j) tma_2d(sb + j * (BK * 128), &map_b, u.n0 + j * 64, u.row0 + k * BK, bar);
+          } else if (KIND == PROJECT) {
+            for (int p = 0; p < NP; ++p)
+              for (int j = 0; j < boxes_n; ++j) tma_3d(sb + p * PLANE_B + j * (BK * 128), &map_b, u.n0 + j * 64, k * BK, u.g * NP + p, bar);
+          } else {
+            for (int p = 0; p < NP; ++p) tma_3d(sb + p * PLANE_B, &map_b, k * BK, u.n0, u.g * NP + p, bar);
+          }
+        }
+        if (!ok) break;
+      }
+      sh->loads = it;
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ products
+    int it = 0, nth = 0;
+    for (int w = blockIdx.x; w < units; w += gridDim.x) {
+      const Unit u = unit_at<KIND, BK>(a, sh, w);
+      if (u.steps == 0) continue;
+      const int buf = nth & 1;
+      if (nth >= 2 && !mbar_wait_warp(&sh->acc_empty[buf], (nth >> 1 & 1) ^ 1, abort_flag)) break;
+      ++nth;
+      tc_fence_after();
+      const unsigned d1 = tmem_base + buf * 256, d2 = d1 + 128;
+      constexpr bool A_MN = KIND == GRAD_W, B_MN = KIND != GRAD_X;
+      constexpr unsigned FORMAT = std::is_same<T, __half>::value ? 0u : 1u;
+      const unsigned idesc = 1u << 4 | FORMAT << 7 | FORMAT << 10 | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | (unsigned)(u.bw >> 3) << 17 | (unsigned)(BM >> 4) << 24;
+      bool ok = true;
+      for (int k = 0; k < u.steps; ++k, ++it) {
+        const int s = it % STAGES;
+        if (!mbar_wait_warp(&sh->full[s], it / STAGES & 1, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const unsigned st = operands + s * STAGE_BYTES, sb = st + NP * PLANE_A;
+        if (KIND == GRAD_W && !LOADED && u.rows - k * BK < BK) {
+          // the rows behind the chunk are another type's, or no one's: zeros in both operands, whatever they hold
+          const int first = u.rows - k * BK, count = (BK - first) * 8;
+          const int blocks = 2 + (u.bw + 63) / 64;
+          for (int i = lane; i < count * blocks; i += 32) {
+            const int j = i / count, c = i % count;
+            const unsigned at = (j < 2 ? st + j * (BK * 128) : sb + (j - 2) * (BK * 128)) + first * 128 + c * 16;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+          }
+          async_fence();
+          __syncwarp();
+        }
+        if (lane == 0) {
+#pragma unroll
+          for (int kk = 0; kk < BK / 16; ++kk) {
+            unsigned long long da[NP], db[NP];
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+              da[p] = A_MN ? desc_mn(st + p * PLANE_A + kk * 2048, BK * 128) : desc_k<ROW>(st + p * PLANE_A + kk * 32);
+              db[p] = B_MN ? desc_mn(sb + p * PLANE_B + kk * 2048, BK * 128) : desc_k<ROW>(sb + p * PLANE_B + kk * 32);
+            }
+            const unsigned more = (k | kk) != 0;
+            if constexpr (NP == 1) {
+              umma(d1, da[0], db[0], idesc, more);
+            } else {
+              umma(d2, da[2], db[0], idesc, more);
+              umma(d2, da[0], db[2], idesc, 1u);
+              umma(d2, da[1], db[1], idesc, 1u);
+              umma(d2, da[1], db[0], idesc, 1u);
+              umma(d2, da[0], db[1], idesc, 1u);
+              umma(d1, da[0], db[0], idesc, more);
+            }
+          }
+          umma_commit(&sh->empty[s]);
+        }
+        __syncwarp();
+      }
+      if (!ok) break;
+      if (lane == 0) umma_commit(&sh->acc_full[buf]);
+      __syncwarp();
+    }
+    if (lane == 0) sh->mmas = it;
+  } else if (warp < 2 + EPI_WARPS) {
+    // ------------------------------------------------------------ epilogue: TMEM lanes 32 (warp % 4) ..
+    const int q = warp & 3;
+    unsigned char* const tile = staging + (warp - 2) * EPI_TILE_BYTES;      // 16-byte chunk c of row r at chunk c ^ (r & 7)
+    int nth = 0;
+    for (int w = blockIdx.x; w < units; w += gridDim.x) {
+      const Unit u = unit_at<KIND, BK>(a, sh, w);
+      const int buf = nth & 1;
+      if (u.steps > 0) {
+        if (!mbar_wait_warp(&sh->acc_full[buf], nth >> 1 & 1, abort_flag)) break;
+        ++nth;
+        tc_fence_after();
+      }
+      const int rows = KIND == GRAD_W ? min(BM, a.M - u.m0) : u.rows, columns = min(u.bw, a.N - u.n0);
+      const int row_of_warp = q * 32;
+      const bool part = KIND == GRAD_W && u.slot >= 0;
+      const bool f32 = part || a.out_f32;
+      const long long ld = KIND == GRAD_W ? a.N : a.ld_out;
+      const long long first = KIND == GRAD_W ? ((long long)(part ? u.slot : u.g) * (part ? a.M + 1 : a.M) + u.m0) * a.N + u.n0 : u.row0 * ld + u.n0;
+      for (int c0 = 0; c0 < columns; c0 += 32) {
+        float o[32];
+        if (u.steps > 0) {
+          const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + buf * 256 + c0;
+          unsigned v[32];
+          tmem_ld32(v, at);
+          if constexpr (NP == 3) {
+            unsigned v2[32];
+            tmem_ld32(v2, at + 128);
+            tmem_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const float x = __uint_as_float(v[j]), y = x + __uint_as_float(v2[j]);
+              o[j] = (v[j] & 0x7F800000u) == 0x7F800000u ? x : y;
+            }
+          } else {
+            tmem_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = __uint_as_float(v[j]);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) o[j] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 32; j += 4)
+          *reinterpret_cast<float4*>(tile + lane * 128 + (((j >> 2) ^ (lane & 7)) << 4)) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+        __syncwarp();
+        const int ch = lane & 7, c = c0 + ch * 4;
+        float4 add = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (KIND == PROJECT && a.bias) {
+          const float* const b = a.bias + (long long)u.g * a.N + u.n0;
+          if (c < columns) add.x = b[c];
+          if (c + 1 < columns) add.y = b[c + 1];
+          if (c + 2 < columns) add.z = b[c + 2];
+          if (c + 3 < columns) add.w = b[c + 3];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int rr = i * 4 + (lane >> 3), row = row_of_warp + rr;
+          float4 y = *reinterpret_cast<const float4*>(tile + rr * 128 + ((ch ^ (rr & 7)) << 4));
+          if (row >= rows || c >= columns) continue;
+          if (KIND == PROJECT) { y.x += add.x; y.y += add.y; y.z += add.z; y.w += add.w; }
+          const long long at = first + row * ld + c;
+          const float e[4] = {y.x, y.y, y.z, y.w};
+          if (f32) {
+            float* const p = (part ? a.part : static_cast<float*>(a.out)) + at;
+            if (a.out_vec && c + 4 <= columns) *reinterpret_cast<float4*>(p) = y;
+            else
+#pragma unroll
+              for (int j = 0; j < 4; ++j) if (c + j < columns) p[j] = e[j];
+          } else {
+            T* const p = static_cast<T*>(a.out) + at;
+            if (a.out_vec && c + 4 <= columns) store_f32<T, 4>(p, e);
+            else
+#pragma unroll
+              for (int j = 0; j < 4; ++j) if (c + j < columns) p[j] = from_f32<T>(e[j]);
+          }
+        }
+        __syncwarp();
+      }
+      if (u.steps > 0) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh->acc_empty[buf]);
+      }
+    }
+  } else if constexpr (LOADED) {
+    // ------------------------------------------------------------ loaders: the rows of the next stage are on their way while one is stored
+    const int t = threadIdx.x - 32 * (2 + EPI_WARPS);
+    Loader<T, KIND> cur, next;
+    int it = 0, w = blockIdx.x, k = 0;
+    Unit u = {};
+    auto skip_empty = [&] { while (w < units) { u = unit_at<KIND, BK>(a, sh, w); if (u.steps > 0) break; w += gridDim.x; } };
+    skip_empty();
+    if (w < units) cur.load(a, u, 0, t);
+    while (w < units) {
+      if (++k == u.steps) { k = 0; w += gridDim.x; skip_empty(); }
+      if (w < units) next.load(a, u, k, t);
+      const int s = it % STAGES;
+      if (it >= STAGES && !mbar_wait_warp(&sh->empty[s], (it / STAGES & 1) ^ 1, abort_flag)) break;
+      cur.store(operands + s * STAGE_BYTES, t);
+      async_fence();                                    // for the tensor core to see
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh->full[s]);
+      cur = next;
+      ++it;
+    }
+    if (t == 0 && !TMA_B) sh->loads = it;
+  }
+
+  // -------------------------------------------------------------- teardown
+  __syncthreads();
+  if (*abort_flag) {
+    if (threadIdx.x == 0) {
+      rows_status(a.status, TAURUS_ERR_INTERNAL);
+      wait_last_phases(sh->loads, STAGES, 1u << 16, [&](int s, unsigned parity) { return mbar_try(&sh->full[s], parity); });
+      wait_last_phases(sh->mmas, STAGES, 1u << 16, [&](int s, unsigned parity) { return mbar_try(&sh->empty[s], parity); });
+    }
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+  }
+}
+
+// W as planes of bf16 (fp32) or with rows that TMA can address (16 bits): [types * planes x K x pitch].
+template <class T>
+__global__ void __launch_bounds__(256) typed_pack_kernel(const T* __restrict__ W, long long types, int K, int N, int pitch, void* __restrict__ out) {
+  const long long rows = types * K;
+  const int quads = (N + 3) / 4;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * quads; i += (long long)gridDim.x * 256) {
+    const long long r = i / quads, g = r / K, k = r % K;
+    const int c = (int)(i % quads) * 4;                // (the pitch is a multiple of 8: a quad stays inside its row)
+    const Quad<T> q = load_quad(W + r * N, c, N, false);
+    if constexpr (sizeof(T) == 2) {
+      reinterpret_cast<uint2*>(static_cast<T*>(out) + r * pitch + c)[0] = *reinterpret_cast<const uint2*>(&q);
+    } else {
+      __nv_bfloat16* const o = static_cast<__nv_bfloat16*>(out) + (g * 3 * K + k) * pitch + c;
+      const long long plane = (long long)K * pitch;
+      Split3 s[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] = split3(q.v[j]);
+      reinterpret_cast<uint2*>(o)[0] = make_uint2(pack2(s[0].hi, s[1].hi), pack2(s[2].hi, s[3].hi));
+      reinterpret_cast<uint2*>(o + plane)[0] = make_uint2(pack2(s[0].mid, s[1].mid), pack2(s[2].mid, s[3].mid));
+      reinterpret_cast<uint2*>(o + 2 * plane)[0] = make_uint2(pack2(s[0].lo, s[1].lo), pack2(s[2].lo, s[3].lo));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- gradient of the bias, joins
+struct JoinArgs {
+  long long n;
+  const long long* offsets;
+  int types, K, N, chunk, out_f32;
+  const float* part;
+  void* dW;
+  float* db;
+};
+// Chunks of type g and its first partial result (by a block).
+__device__ __forceinline__ int chunks_of(const JoinArgs& a, int g, int* first) {
+  int mine = 0;
+  for (int j = threadIdx.x; j < g; j += blockDim.x) {
+    const int c = (int)((a.offsets[j + 1] - a.offsets[j] + a.chunk - 1) / a.chunk);
+    mine += c > 1 ? c : 0;
+  }
+  __shared__ int sum;
+  if (threadIdx.x == 0) sum = 0;
+  __syncthreads();
+  mine = __reduce_add_sync(0xffffffffu, mine);
+  if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&sum, mine);      // (whole numbers: any order)
+  __syncthreads();
+  *first = sum;
+  return (int)((a.offsets[g + 1] - a.offsets[g] + a.chunk - 1) / a.chunk);
+}
+__device__ __forceinline__ bool offsets_bad(const long long* offsets, int types, long long n) {      // by a block
+  bool bad = false;
+  for (int g = threadIdx.x; g < types; g += blockDim.x) { const long long b = offsets[g], e = offsets[g + 1]; bad |= b < 0 || e > n || e < b; }
+  return __syncthreads_or(bad);
+}
+
+// Column sums of grad_out over a chunk: a block to a chunk and 32 columns.  Grid (blocks of columns, chunks at most, by stride).
+template <class T>
+__global__ void __launch_bounds__(256) typed_bias_kernel(const JoinArgs a, const T* __restrict__ dy, long long ld, float* __restrict__ part, int32_t* status) {
+  __shared__ float red[8][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  if (offsets_bad(a.offsets, a.types, a.n)) { if (threadIdx.x == 0) rows_status(status, TAURUS_ERR_INVALID_ARG); return; }
+  int unit = 0, slots = 0;                                  // of the types so far
+  for (int g = 0; g < a.types; ++g) {
+    const long long b = a.offsets[g], e = a.offsets[g + 1];
+    const int chunks = max(1, (int)((e - b + a.chunk - 1) / a.chunk));
+    // the chunks of this type that are this block's: unit + i = blockIdx.y modulo gridDim.y
+    int i = (int)blockIdx.y - unit % (int)gridDim.y;
+    if (i < 0) i += gridDim.y;
+    for (; i < chunks; i += gridDim.y) {
+      const long long rb = b + (long long)i * a.chunk, re = min(rb + a.chunk, e);
+      float s = 0.f;
+      if (c < a.N)
+#pragma unroll 8
+        for (long long r = rb + warp; r < re; r += 8) s += to_f32<T>(dy[r * ld + c]);
+      red[warp][lane] = s;
+      __syncthreads();
+      if (warp == 0 && c < a.N) {
+        for (int w = 1; w < 8; ++w) s += red[w][lane];
+        if (chunks > 1) part[((long long)(slots + i) * (a.K + 1) + a.K) * a.N + c] = s;
+        else a.db[(long long)g * a.N + c] = s;
+      }
+      __syncthreads();
+    }
+    unit += chunks;
+    slots += chunks > 1 ? chunks : 0;
+  }
+}
+
+// The partial results of the types of several chunks, added in the chunks' order.  Grid (elements by stride, types).
+template <class O>
+__global__ void __launch_bounds__(256) typed_join_kernel(const JoinArgs a) {
+  if (offsets_bad(a.offsets, a.types, a.n)) return;
+  const int g = blockIdx.y;
+  int first;
+  const int chunks = chunks_of(a, g, &first);
+  if (chunks <= 1) return;
+  const long long size = (long long)(a.K + 1) * a.N;
+  const long long from = a.dW ? 0 : (long long)a.K * a.N, to = a.db ? size : (long long)a.K * a.N;
+  for (long long i = from + (long long)blockIdx.x * 256 + threadIdx.x; i < to; i += (long long)gridDim.x * 256) {
+    float s = 0.f;
+#pragma unroll 8
+    for (int c = 0; c < chunks; ++c) s += a.part[(long long)(first + c) * size + i];
+    if (i < (long long)a.K * a.N) static_cast<O*>(a.dW)[(long long)g * a.K * a.N + i] = from_f32<O>(s);
+    else a.db[(long long)g * a.N + (i - (long long)a.K * a.N)] = s;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- host
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn() {
+  static const EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) { cudaGetLastError(); p = nullptr; }
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+// Elements of 16 bits, box inner x rows (x 1), swizzle of the box's inner bytes (128 or 64).
+bool make_map(CUtensorMap* m, int32_t type, const void* base, long long cols, long long rows, long long depth, long long ld, int box_cols, int box_rows) {
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)depth};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
+  const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
+  return encode_fn()(m, type == TAURUS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, depth > 0 ? 3 : 2, const_cast<void*>(base), dims, strides, box,
+                     one, CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool tma_rows(const void* p, long long ld) { return ld % 8 == 0 && rows_aligned(p, 16); }      // of 16-bit elements
+
+// Blocks of nearly equal width, a multiple of 16.
+int block_columns(int N, int most) {
+  const int np = taurus_round_up(N, 16), blocks = (np + most - 1) / most;
+  return taurus_round_up((np + blocks - 1) / blocks, 16);
+}
+
+template <class T, int KIND, bool LOADED>
+int launch(const CUtensorMap& ma, const CUtensorMap& mb, TcArgs a, long long most_units, int sms, cudaStream_t st) {
+  const cudaError_t e = cudaFuncSetAttribute(typed_tc_kernel<T, KIND, LOADED>, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED_BYTES);
+  if (e != cudaSuccess) { taurus_note_cuda_error(e, "typed_project"); return TAURUS_ERR_CUDA; }
+  const int threads = 32 * (2 + EPI_WARPS + (LOADED ? LOAD_WARPS : 0));
+  typed_tc_kernel<T, KIND, LOADED><<<(int)std::max<long long>(1, std::min<long long>(most_units, sms)), threads, SHARED_BYTES, st>>>(ma, mb, a);
+  return TAURUS_OK;
+}
+template <int KIND, class F>
+int launch_type(int32_t type, bool loaded, F f) {     // f(launch function)
+  if (type == TAURUS_F32) return f(launch<float, KIND, true>);
+  if (type == TAURUS_BF16) return loaded ? f(launch<__nv_bfloat16, KIND, true>) : f(launch<__nv_bfloat16, KIND, false>);
+  return loaded ? f(launch<__half, KIND, true>) : f(launch<__half, KIND, false>);
+}
+
+int weight_pitch(int d_out) { return taurus_round_up(d_out, 8); }
+int bn_most(int32_t type, bool loaded) { return loaded || type == TAURUS_F32 ? 128 : 256; }
+
+}  // namespace
+
+bool typed_tc_usable() { return encode_fn() != nullptr; }
+// Does W have to be laid out anew?
+bool typed_tc_packs(int32_t type, int d_out) { return type == TAURUS_F32 || d_out % 8 != 0; }
+size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type) {
+  return typed_tc_packs(type, d_out) ? (size_t)types * (type == TAURUS_F32 ? 3 : 1) * d_in * weight_pitch(d_out) * 2 : 0;
+}
+// Rows of a chunk of grad_W: about two units to an SM, 512 rows at least, 4 096 at most.
+int typed_tc_chunk(int64_t n, int d_in, int d_out, int32_t type) {
+  const int most = bn_most(type, false);
+  const long long tiles = (long long)((d_in + BM - 1) / BM) * ((d_out + most - 1) / most);
+  return (int)std::min<long long>(4096, std::max<long long>(512, taurus_round_up((int)std::min<long long>(n * tiles / 296, 1 << 20), 64)));
+}
+// A type of more than one chunk has more than `chunk` rows and at most rows / chunk + 1 chunks.
+size_t typed_tc_part_bytes(int64_t n, int d_in, int d_out, int32_t type) {
+  const int chunk = typed_tc_chunk(n, d_in, d_out, type);
+  return (size_t)(2 * (n / chunk)) * (size_t)(d_in + 1) * d_out * 4;
+}
+
+int typed_tc_pack(int32_t type, const void* W, int32_t types, int d_in, int d_out, void* packed, int sms, cudaStream_t st) {
+  const long long quads = (long long)types * d_in * ((d_out + 3) / 4);
+  const int grid = (int)std::min<long long>((quads + 255) / 256, (long long)sms * 16);
+  with_row_type(type, [&](auto tt) {
+    using T = typename decltype(tt)::type;
+    typed_pack_kernel<T><<<grid, 256, 0, st>>>(static_cast<const T*>(W), types, d_in, d_out, weight_pitch(d_out), packed);
+    return 0;
+  });
+  return TAURUS_OK;
+}
+
+// out = x W + bias, or grad_x = grad_out W^T (transposed).  w: W itself, or what typed_tc_pack made of it.
+int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* w, const float* bias, int d_in, int d_out,
+                  void* out, int32_t out_type, int64_t ld_out, int32_t* status, int sms, cudaStream_t st) {
+  const int Kc = transposed ? d_out : d_in, N = transposed ? d_in : d_out, planes = type == TAURUS_F32 ? 3 : 1;
+  const bool loaded = type == TAURUS_F32 || !tma_rows(x, ld_x);
+  const int bk = type == TAURUS_F32 ? 32 : 64;
+  TcArgs a = {};
+  a.n = n; a.offsets = offsets; a.types = types; a.N = N; a.Kc = Kc;
+  a.bn = block_columns(N, bn_most(type, loaded)); a.n_blocks = (N + a.bn - 1) / a.bn;
+  a.a = x; a.lda = ld_x; a.a_vec = ld_x % 4 == 0 && rows_aligned(x, 4 * row_type_size(type));
+  a.out = out; a.ld_out = ld_out; a.out_f32 = out_type == TAURUS_F32; a.out_vec = ld_out % 4 == 0 && rows_aligned(out, 4 * row_type_size(out_type));
+  a.bias = bias; a.status = status;
+  const long long pitch = typed_tc_packs(type, d_out) ? weight_pitch(d_out) : d_out;
+  CUtensorMap ma = {}, mb = {};
+  if (!loaded && !make_map(&ma, type, x, Kc, n, 0, ld_x, bk, BM)) return TAURUS_ERR_CUDA;
+  if (!make_map(&mb, type, w, d_out, d_in, (long long)types * planes, pitch, transposed ? bk : 64, transposed ? a.bn : bk)) return TAURUS_ERR_CUDA;
+  const long long units = (n / BM + std::min<long long>(types, n)) * a.n_blocks;
+  auto go = [&](auto f) { return f(ma, mb, a, units, sms, st); };
+  return transposed ? launch_type<GRAD_X>(type, loaded, go) : launch_type<PROJECT>(type, loaded, go);
+}
+
+// grad_W and grad_bias (either may be null); part: typed_tc_part_bytes.
+int typed_tc_weights(int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* dy, int64_t ld_dy, int d_in, int d_out, void* dW,
+                     int32_t dW_type, float* db, float* part, int32_t* status, int sms, cudaStream_t st) {
+  const int chunk = typed_tc_chunk(n, d_in, d_out, type);
+  if (dW) {
+    const bool loaded = type == TAURUS_F32 || !tma_rows(x, ld_x) || !tma_rows(dy, ld_dy);
+    const int bk = type == TAURUS_F32 ? 32 : 64, size = row_type_size(type);
+    TcArgs a = {};
+    a.n = n; a.offsets = offsets; a.types = types; a.M = d_in; a.N = d_out; a.chunk = chunk;
+    a.bn = block_columns(d_out, bn_most(type, loaded)); a.n_blocks = (d_out + a.bn - 1) / a.bn; a.m_blocks = (d_in + BM - 1) / BM;
+    a.a = x; a.lda = ld_x; a.a_vec = ld_x % 4 == 0 && rows_aligned(x, 4 * size);
+    a.b = dy; a.ldb = ld_dy; a.b_vec = ld_dy % 4 == 0 && rows_aligned(dy, 4 * size);
+    a.out = dW; a.out_f32 = dW_type == TAURUS_F32; a.out_vec = d_out % 4 == 0 && rows_aligned(dW, 4 * row_type_size(dW_type)); a.part = part; a.status = status;
+    CUtensorMap ma = {}, mb = {};
+    if (!loaded && (!make_map(&ma, type, x, d_in, n, 0, ld_x, 64, bk) || !make_map(&mb, type, dy, d_out, n, 0, ld_dy, 64, bk))) return TAURUS_ERR_CUDA;
+    const long long units = (n / chunk + types) * a.m_blocks * a.n_blocks;
+    const int rc = launch_type<GRAD_W>(type, loaded, [&](auto f) { return f(ma, mb, a, units, sms, st); });
+    if (rc) return rc;
+  }
+  JoinArgs j = {};
+  j.n = n; j.offsets = offsets; j.types = types; j.K = d_in; j.N = d_out; j.chunk = chunk; j.part = part; j.dW = dW; j.db = db;
+  if (db)
+    with_row_type(type, [&](auto tt) {
+      using T = typename decltype(tt)::type;
+      const int cols = (d_out + 31) / 32;
+      const dim3 grid((unsigned)cols, (unsigned)std::min<long long>(n / chunk + types, std::max(1, sms * 8 / cols)));
+      typed_bias_kernel<T><<<grid, 256, 0, st>>>(j, static_cast<const T*>(dy), ld_dy, part, status);
+      return 0;
+    });
+  if (n > chunk)
+    with_row_type(dW ? dW_type : TAURUS_F32, [&](auto tt) {
+      using O = typename decltype(tt)::type;
+      const long long size = (long long)(d_in + 1) * d_out;
+      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 255) / 256, 256), (unsigned)types), 256, 0, st>>>(j);
+      return 0;
+    });
+  return TAURUS_OK;
+}

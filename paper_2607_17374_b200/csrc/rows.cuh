@@ -1,0 +1,117 @@
+// What the operators on typed rows share (embedding lookup, products by vertex type, norm): element types, vectors of elements, the
+// status word, and the host's checks of their arguments.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "taurus_internal.h"
+
+static inline int row_type_size(int32_t t) { return t == TAURUS_F32 ? 4 : t == TAURUS_BF16 || t == TAURUS_F16 ? 2 : 0; }   // 0: no such type
+
+// The device that is current; every operator's arguments have to live there.
+static inline bool rows_current_device(int* dev, int* sms) {
+  cudaError_t e = cudaGetDevice(dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev);
+  if (e != cudaSuccess) { taurus_note_cuda_error(e, "current device"); return false; }
+  return true;
+}
+static inline bool rows_on_device(const void* p, int dev) {
+  cudaPointerAttributes at;
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) { cudaGetLastError(); return false; }
+  return (at.type == cudaMemoryTypeDevice && at.device == dev) || at.type == cudaMemoryTypeManaged;
+}
+static inline bool rows_aligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+// Do [a, a + an) and [b, b + bn) share a byte?
+static inline bool rows_overlap(const void* a, size_t an, const void* b, size_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return an > 0 && bn > 0 && x < y + bn && y < x + an;
+}
+static inline size_t rows_bytes(int64_t n, int64_t ld, int64_t width, int size) { return n > 0 ? ((size_t)(n - 1) * (size_t)ld + (size_t)width) * (size_t)size : 0; }
+// n rows of ld elements of `size` bytes stay below 2^62 bytes, so that no product of sizes overflows.
+static inline bool rows_fit(int64_t n, int64_t ld, int size) { return n == 0 || ld <= (int64_t)((1ll << 62) / size) / n; }
+
+// A status word keeps the first error of the calls it was given to.
+static __device__ __forceinline__ void rows_status(int32_t* status, int code) { if (status) atomicCAS(status, 0, code); }
+
+template <class T> static __device__ __forceinline__ float to_f32(T v);
+template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
+template <class T> static __device__ __forceinline__ T from_f32(float v);     // rounded to nearest, once
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+// N elements that start at a multiple of their own size.
+template <class T, int N> struct __align__(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Vec { T v[N]; };
+
+enum { LOAD_PLAIN = 0, LOAD_ONCE = 1 };   // LOAD_ONCE: not expected to be read again soon
+
+template <class V, int HOW = LOAD_PLAIN>
+static __device__ __forceinline__ V load_vec(const void* p) {
+  V r;
+  if constexpr (sizeof(V) % 16 == 0) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(V) / 16; ++i)
+      reinterpret_cast<uint4*>(&r)[i] = HOW == LOAD_ONCE ? __ldcs(reinterpret_cast<const uint4*>(p) + i) : reinterpret_cast<const uint4*>(p)[i];
+  } else if constexpr (sizeof(V) == 8) {
+    *reinterpret_cast<uint2*>(&r) = HOW == LOAD_ONCE ? __ldcs(reinterpret_cast<const uint2*>(p)) : *reinterpret_cast<const uint2*>(p);
+  } else if constexpr (sizeof(V) == 4) {
+    *reinterpret_cast<uint32_t*>(&r) = HOW == LOAD_ONCE ? __ldcs(reinterpret_cast<const uint32_t*>(p)) : *reinterpret_cast<const uint32_t*>(p);
+  } else {
+    *reinterpret_cast<uint16_t*>(&r) = *reinterpret_cast<const uint16_t*>(p);
+  }
+  return r;
+}
+template <class V>
+static __device__ __forceinline__ void store_vec(void* p, const V& r) {
+  if constexpr (sizeof(V) % 16 == 0) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(V) / 16; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(&r)[i];
+  } else if constexpr (sizeof(V) == 8) {
+    *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(&r);
+  } else if constexpr (sizeof(V) == 4) {
+    *reinterpret_cast<uint32_t*>(p) = *reinterpret_cast<const uint32_t*>(&r);
+  } else {
+    *reinterpret_cast<uint16_t*>(p) = *reinterpret_cast<const uint16_t*>(&r);
+  }
+}
+template <class T, int N>
+static __device__ __forceinline__ void store_f32(T* p, const float (&x)[N]) {
+  Vec<T, N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) r.v[i] = from_f32<T>(x[i]);
+  store_vec(p, r);
+}
+template <class T, int N, int HOW = LOAD_PLAIN>
+static __device__ __forceinline__ void load_f32(const T* p, float (&x)[N]) {
+  const Vec<T, N> r = load_vec<Vec<T, N>, HOW>(p);
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = to_f32<T>(r.v[i]);
+}
+
+// Group g's rows by its two offsets, kept inside [0, n] whatever the offsets hold; a group that runs backwards or leaves [0, n] is reported.
+static __device__ __forceinline__ void group_rows(const long long* offsets, long long g, long long n, long long* begin, long long* end, int32_t* status) {
+  const long long a = offsets[g], b = offsets[g + 1];
+  if (a < 0 || b > n || b < a) rows_status(status, TAURUS_ERR_INVALID_ARG);
+  *begin = a < 0 ? 0 : a > n ? n : a;
+  *end = b < *begin ? *begin : b > n ? n : b;
+}
+
+// f(tag of T) for the element type `t`.
+template <class T> struct RowTag { using type = T; };
+template <class F> static inline int with_row_type(int32_t t, F f) {
+  if (t == TAURUS_F32) return f(RowTag<float>());
+  if (t == TAURUS_BF16) return f(RowTag<__nv_bfloat16>());
+  return f(RowTag<__half>());
+}
+// f(integral_constant of the vector length v).
+template <class F> static inline int with_vector(int v, F f) {
+  return v == 8 ? f(std::integral_constant<int, 8>()) : v == 4 ? f(std::integral_constant<int, 4>())
+         : v == 2 ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 1>());
+}

@@ -1,0 +1,266 @@
+"""Products by vertex type and their gradients against fp64: types, ragged and empty groups, odd widths, pitches, rows outside the groups."""
+import pytest
+import torch
+
+import paper_2607_17374_b200 as tb
+from rows_reference import U32, close, typed, typed_grad
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def strided(n, width, ld, dtype, shift=0):
+    store = torch.full((shift + max(n, 1) * ld + 8,), 7.0, dtype=dtype, device="cuda")
+    return torch.as_strided(store, (n, width), (ld, 1), shift), store
+
+
+def workspace(size):
+    return torch.full((size,), 255, dtype=torch.uint8, device="cuda") if size else None
+
+
+def sums(m):
+    """Bound on the relative error of a sum of m products: a step of a tensor core's sum may round toward zero, and there are no more
+    steps than terms."""
+    return (m + 4) * 2 * U32
+
+
+# sizes of the groups; a list that begins or ends with a negative number leaves that many rows in front or behind
+SHAPES = [
+    ([1], 1, 1), ([5], 100, 256), ([0, 3, 0], 37, 130), ([-2, 1, 0, 2, 1, -3], 64, 64), ([130, 1, 127, 128, 129], 128, 128), ([300, 0, 41, 7], 33, 47),
+    ([1000], 100, 256), ([257, 511], 512, 200), ([64] * 20, 16, 24), ([700, 90], 1000, 72), ([90, 333], 72, 1000), ([-5, 400, 200, -9], 96, 96), ([2] * 300, 40, 40),
+    ([2600], 48, 264), ([5000, 3], 24, 16),
+]
+
+
+def lay_out(sizes):
+    front = -sizes[0] if sizes[0] < 0 else 0
+    behind = -sizes[-1] if len(sizes) > 1 and sizes[-1] < 0 else 0
+    groups = [s for s in sizes if s >= 0]
+    off = [front]
+    for s in groups:
+        off.append(off[-1] + s)
+    return off, off[-1] + behind
+
+
+def make(sizes, K, N, t, seed=0, pad=0, shift=0):
+    off, n = lay_out(sizes)
+    g = torch.Generator("cuda").manual_seed(seed + K * 7 + N)
+    x, xs = strided(n, K, K + pad, t, shift)
+    x.copy_(torch.randn(n, K, generator=g, device="cuda"))
+    W = torch.randn(len(off) - 1, K, N, generator=g, device="cuda").to(t)
+    bias = torch.randn(len(off) - 1, N, generator=g, device="cuda")
+    dy, _ = strided(n, N, N + pad, t, shift)
+    dy.copy_(torch.randn(n, N, generator=g, device="cuda"))
+    return off, n, x, W, bias, dy
+
+
+def forward(off, n, x, W, bias, out, status=None, **kw):
+    G, K, N = W.shape
+    ws = workspace(tb.typed_project_workspace(n, G, K, N, x))
+    tb.typed_project(n, G, torch.tensor(off, device="cuda"), x, x.stride(0), W, bias, K, N, out, out.stride(0), ws, status, **kw)
+
+
+def backward(off, n, x, W, dy, dx, dW, db, status=None):
+    G, K, N = W.shape
+    ws = workspace(tb.typed_project_grad_workspace(n, G, K, N, dy))
+    tb.typed_project_grad(n, G, torch.tensor(off, device="cuda"), x, x.stride(0), W, dy, dy.stride(0), K, N, dx, dx.stride(0) if dx is not None else 0, dW, db, ws, status)
+
+
+@pytest.mark.parametrize("t,ot", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16), (F16, F32)])
+@pytest.mark.parametrize("sizes,K,N", SHAPES)
+@pytest.mark.parametrize("pad,shift", [(0, 0), (8, 0), (3, 1)])
+def test_project(t, ot, sizes, K, N, pad, shift):
+    off, n, x, W, bias, _ = make(sizes, K, N, t, pad=pad, shift=shift)
+    for b in (bias, None):
+        out, store = strided(n, N, N + pad, ot, shift)
+        before = store.clone()
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        forward(off, n, x, W, b, out, status)
+        ref, mag = typed(off, x, W, b)
+        lo, hi = off[0], off[-1]
+        close(out[lo:hi], ref[lo:hi], mag[lo:hi] * sums(K))
+        assert int(status) == 0
+        torch.as_strided(before, (n, N), (N + pad, 1), shift)[lo:hi] = out[lo:hi]
+        assert torch.equal(before, store)               # nothing else was written
+
+
+@pytest.mark.parametrize("t,wt", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16), (F16, F32)])
+@pytest.mark.parametrize("sizes,K,N", SHAPES)
+@pytest.mark.parametrize("pad,shift", [(0, 0), (8, 0), (3, 1)])
+def test_gradients(t, wt, sizes, K, N, pad, shift):
+    off, n, x, W, bias, dy = make(sizes, K, N, t, pad=pad, shift=shift)
+    G = W.shape[0]
+    dx, store = strided(n, K, K + pad, t, shift)
+    before = store.clone()
+    dW, db = torch.full((G, K, N), 9.0, dtype=wt, device="cuda"), torch.full((G, N), 9.0, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    backward(off, n, x, W, dy, dx, dW, db, status)
+    (rx, mx), (rw, mw), (rb, mb) = typed_grad(off, x, W, dy)
+    lo, hi = off[0], off[-1]
+    most = max(b - a for a, b in zip(off, off[1:]))
+    close(dx[lo:hi], rx[lo:hi], mx[lo:hi] * sums(N))
+    close(dW, rw, mw * sums(most))
+    close(db, rb, mb * sums(most))
+    assert int(status) == 0
+    torch.as_strided(before, (n, K), (K + pad, 1), shift)[lo:hi] = dx[lo:hi]
+    assert torch.equal(before, store)
+    again = [dx.clone(), dW.clone(), db.clone()]
+    backward(off, n, x, W, dy, dx, dW, db)
+    assert all(torch.equal(a, b) for a, b in zip(again, (dx, dW, db)))
+    for which in range(3):                              # one at a time: the same bits
+        alone = [torch.full_like(o, 5.0) if i == which else None for i, o in enumerate((dx, dW, db))]
+        if which == 0:
+            alone[0] = torch.as_strided(torch.zeros_like(store), (n, K), (K + pad, 1), shift)
+        backward(off, n, x, W, dy, *alone)
+        got, want = alone[which], again[which]
+        assert torch.equal(got[lo:hi], want[lo:hi]) if which == 0 else torch.equal(got, want)
+
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+def test_rows_outside_the_groups_may_hold_anything(t):
+    """NaN and infinity in rows of no group and in the rows of one group reach no other group's results."""
+    off, n = [3, 103, 103, 205, 400], 410
+    g = torch.Generator("cuda").manual_seed(3)
+    x = torch.randn(n, 72, generator=g, device="cuda").to(t)
+    dy = torch.randn(n, 56, generator=g, device="cuda").to(t)
+    W = torch.randn(4, 72, 56, generator=g, device="cuda").to(t)
+    rows = torch.ones(n, dtype=torch.bool, device="cuda")
+    rows[:3] = rows[400:] = rows[103:205] = False
+    xn, dyn, Wn = x.clone(), dy.clone(), W.clone()
+    xn[~rows], dyn[~rows] = float("nan"), float("inf")
+    Wn[1], Wn[2] = float("nan"), float("inf")
+
+    def results(x, dy, W):
+        out, dx = torch.zeros(n, 56, dtype=t, device="cuda"), torch.zeros(n, 72, dtype=t, device="cuda")
+        dW, db = torch.empty(4, 72, 56, device="cuda"), torch.empty(4, 56, device="cuda")
+        forward(off, n, x, W, None, out)
+        backward(off, n, x, W, dy, dx, dW, db)
+        return out, dx, dW, db
+    clean, foul = results(x, dy, W), results(xn, dyn, Wn)
+    for a, b in zip(clean[:2], foul[:2]):
+        assert torch.equal(a[rows], b[rows])
+    for a, b in zip(clean[2:], foul[2:]):
+        assert torch.equal(a[[0, 1, 3]], b[[0, 1, 3]])
+
+
+@pytest.mark.parametrize("n", [3, 400])
+@pytest.mark.parametrize("t", [F32, BF16])
+def test_infinities_stay_infinities(t, n):
+    """A row with an infinity gives infinities of the weights' signs, as the formula does.  40 times 1e37 is above fp32's largest value (3.4e38) and
+    becomes infinity too; 40 times 8e36 is below it and stays finite."""
+    x = torch.ones(n, 40, dtype=t, device="cuda")
+    W = torch.ones(1, 40, 24, dtype=t, device="cuda")
+    W[0, 7, 3] = -1.0
+    x[1, 7] = float("inf")
+    x[2] = 1e37
+    out = torch.empty(n, 24, device="cuda")
+    forward([0, n], n, x, W, None, out)
+    want = x.double() @ W[0].double()
+    assert torch.equal(out[:3], want[:3].float())
+    x[2] = 8e36
+    forward([0, n], n, x, W, None, out)
+    want = x.double() @ W[0].double()
+    assert torch.isfinite(out[2]).all() and ((out[2].double() - want[2]).abs() <= 40 * x[2, 0].double() * sums(40)).all()
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("bad", [[0, 50, 40, 300], [-5, 50, 90, 300], [0, 50, 90, 301], [0, 1 << 40, 90, 300], [300, 200, 100, 0], [0, -(1 << 50), 90, 200]])
+def test_bad_offsets_give_a_status(bad, t):
+    """Offsets that run backwards or leave the rows: an error in the status word, nothing outside the arrays is touched."""
+    n, K, N = 300, 40, 48
+    x, dy, W = (torch.ones(s, dtype=t, device="cuda") for s in ((n, K), (n, N), (3, K, N)))
+    out, os = strided(n, N, N, t)
+    dx, xs = strided(n, K, K, t)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    forward(bad, n, x, W, None, out, status)
+    assert int(status) == tb.ERROR_CODES["INVALID_ARG"]
+    status.zero_()
+    backward(bad, n, x, W, dy, dx, torch.empty(3, K, N, device="cuda"), torch.empty(3, N, device="cuda"), status)
+    assert int(status) == tb.ERROR_CODES["INVALID_ARG"]
+    assert (os[n * N:] == 7).all() and (xs[n * K:] == 7).all()
+
+
+def test_gradients_against_differences():
+    """The product is linear in x and in W: central differences of <r, out> against the gradients, up to the rounding of the sums."""
+    sizes, K, N = [150, 0, 333], 60, 52
+    off, n, x, W, bias, r = make(sizes, K, N, F32)
+    g = torch.Generator("cuda").manual_seed(9)
+    dX, dWd = torch.randn(n, K, generator=g, device="cuda"), torch.randn(3, K, N, generator=g, device="cuda")
+    dx, dW, db = torch.empty(n, K, device="cuda"), torch.empty(3, K, N, device="cuda"), torch.empty(3, N, device="cuda")
+    backward(off, n, x, W, r, dx, dW, db)
+
+    def loss(x, W):
+        out = torch.empty(n, N, device="cuda")
+        forward(off, n, x, W, bias, out)
+        return float((out.double() * r.double()).sum()), float((typed(off, x, W, bias)[1] * r.double().abs()).sum())
+    for grad, d, plus, minus in ((dx, dX, (x + dX, W), (x - dX, W)), (dW, dWd, (x, W + dWd), (x, W - dWd))):
+        (a, ma), (b, mb) = loss(*plus), loss(*minus)
+        i = 0 if grad is dx else 1
+        step = plus[i].double() - minus[i].double()
+        assert abs((a - b) - float((grad.double() * step).sum())) <= (ma + mb) * (sums(K) + sums(N if grad is dx else 333))
+
+
+def test_without_rows():
+    W = torch.ones(2, 8, 16, device="cuda")
+    off = torch.zeros(3, dtype=torch.int64, device="cuda")
+    dW, db = torch.ones(2, 8, 16, device="cuda"), torch.ones(2, 16, device="cuda")
+    ws = workspace(tb.typed_project_grad_workspace(0, 2, 8, 16, torch.float32))
+    tb.typed_project_grad(0, 2, off, None, 8, W, None, 16, 8, 16, None, 0, dW, db, ws, type=tb.F32)
+    assert (dW == 0).all() and (db == 0).all()
+
+
+def test_most_types_and_wide_rows():
+    """1 024 types, most without rows; rows of 1 024 columns."""
+    n = 500
+    g = torch.Generator("cuda").manual_seed(1)
+    ends = torch.sort(torch.randint(0, n + 1, (1023,), generator=g, device="cuda")).values
+    off = [0] + ends.tolist() + [n]
+    x = torch.randn(n, 40, generator=g, device="cuda").bfloat16()
+    W = torch.randn(1024, 40, 24, generator=g, device="cuda").bfloat16()
+    out = torch.empty(n, 24, device="cuda")
+    forward(off, n, x, W, None, out)
+    ref, mag = typed(off, x, W, None)
+    close(out, ref, mag * sums(40))
+    for t in (F32, BF16):
+        off, n, x, W, bias, dy = make([400, 30], 1024, 1024, t)
+        out, dx = torch.empty(n, 1024, device="cuda"), torch.empty(n, 1024, dtype=t, device="cuda")
+        dW, db = torch.empty(2, 1024, 1024, device="cuda"), torch.empty(2, 1024, device="cuda")
+        forward(off, n, x, W, bias, out)
+        backward(off, n, x, W, dy, dx, dW, db)
+        ref, mag = typed(off, x, W, bias)
+        close(out, ref, mag * sums(1024))
+        (rx, mx), (rw, mw), (rb, mb) = typed_grad(off, x, W, dy)
+        close(dx, rx, mx * sums(1024)); close(dW, rw, mw * sums(400)); close(db, rb, mb * sums(400))
+
+
+def test_fp32_products_keep_their_bits():
+    """fp32 operands whose products cancel to their last bits: the error stays at fp32's own, also beside elements 1e6 times as large."""
+    n, K, N = 2000, 256, 128
+    g = torch.Generator("cuda").manual_seed(2)
+    x = torch.randn(n, K, generator=g, device="cuda")
+    x[:, 5] *= 1e6
+    W = torch.randn(1, K, N, generator=g, device="cuda")
+    W[0, 5] = 0
+    out = torch.empty(n, N, device="cuda")
+    forward([0, n], n, x, W, None, out)
+    ref, mag = typed([0, n], x, W, None)
+    assert float(((out.double() - ref).abs() / mag).max()) <= sums(K)
+    assert float(((out.double() - ref) / mag).pow(2).mean().sqrt()) <= 16 * U32      # as a mean: nowhere near the bound of the sum
+
+
+def test_refused_on_a_device():
+    x, W, out = torch.zeros(4, 8, device="cuda"), torch.zeros(2, 8, 8, device="cuda"), torch.zeros(4, 8, device="cuda")
+    off = torch.tensor([0, 2, 4], device="cuda")
+    for bad in (dict(x=x.cpu()), dict(W=W.cpu()), dict(off=off.cpu()), dict(out=x), dict(out=W[0, :4]), dict(bias=torch.zeros(16))):
+        a = dict(x=x, W=W, off=off, out=out, bias=None)
+        a.update(bad)
+        with pytest.raises(tb.TaurusError) as e:
+            tb.typed_project(4, 2, a["off"], a["x"], 8, a["W"], a["bias"], 8, 8, a["out"], 8, workspace(1 << 20))
+        assert e.value.code == tb.ERROR_CODES["INVALID_ARG"]
+    dW, db = torch.zeros_like(W), torch.zeros(2, 8, device="cuda")
+    for bad in (dict(dx=out), dict(dx=x), dict(dW=W), dict(db=out[:2]), dict(dW=dW.cpu())):
+        a = dict(dx=torch.zeros(4, 8, device="cuda"), dW=dW, db=db)
+        a.update(bad)
+        with pytest.raises(tb.TaurusError) as e:
+            tb.typed_project_grad(4, 2, off, x, 8, W, out, 8, 8, 8, a["dx"], 8, a["dW"], a["db"], workspace(1 << 20))
+        assert e.value.code == tb.ERROR_CODES["INVALID_ARG"]

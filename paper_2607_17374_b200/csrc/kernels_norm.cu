@@ -6,13 +6,13 @@
 //   dx = rstd (gamma dz - mean_g(gamma dz) - xh mean_g(gamma dz xh))
 //
 // Bytes bound it: x in, y out (dx: x and dy in, dx out).  Statistics need all of a graph before its first row can be written.  A short graph
-// is the work of one block, which reads its rows a second time from registers or the caches.  The rows of a long graph are spread over blocks
-// of R rows (stats), their partial statistics joined in a fixed order (combine), and the rows are read again and written (apply).  How long
-// a graph is stands in device memory: every launch decides for itself which graphs are its own.
+// is the work of one block, which has its rows in registers or finds them in the caches when it writes.  The rows of a long graph are spread over
+// blocks of R rows (stats), their partial statistics joined in a fixed order (combine), and the rows are read again and written (apply).  How long
+// a graph is stands in device memory: the kernel for short graphs leaves a word that says whether there are others.
 //
-// A thread keeps to one vector of channels and walks the rows.  Sums of x are taken of x - pivot (the channel's value in the part's first
-// row), so that an offset does not eat the variance, in fp32 over at most R rows; parts are joined by (count, mean, sum of squared
-// deviations) in fp64.
+// A thread keeps to one vector of channels and walks the rows.  Moments are taken of a batch of its rows in registers (mean first, then squares of
+// deviations) and joined as (count, mean, sum of squared deviations): neither an offset nor a single large value eats the variance, as they would with sums of squares.
+// All in fp32, the parts of a long graph in fp64.
 #include <algorithm>
 
 #include "rows.cuh"
@@ -20,39 +20,43 @@
 namespace {
 
 constexpr int MAX_C = TAURUS_MAX_ROW_WIDTH;
-constexpr int BATCH = 4;                 // row vectors of a thread in flight; a short graph's first ones stay in registers
 
 struct NormArgs {
   long long n, graphs;
   const long long* offsets;              // null: one graph of n rows
   long long ld_x, ld_y, ld_dy;           // ld_y: of the rows written
   int C, groups, cg, vpr, lanes;         // cg: channels of a group; vpr: vectors of a row; lanes: rows that a block walks at once
-  int act;
   float eps;
   const float *gamma, *beta;             // null: ones, zeros
   float *mean, *rstd;                    // [graphs x groups]
-  long long R, blocks, short_blocks;     // rows of a block of rows; their number; blocks of the kernel for short graphs
+  long long R, blocks;                   // rows of a block of rows; their number
+  int short_blocks, row_grid;            // blocks of the kernel for short graphs; blocks that share the blocks of rows
+  int* any_long;                         // is there a long graph?
   float2* part;                          // [blocks x 2 x groups]
-  float2* chan;                          // [(blocks + short_blocks) x C] (grad_gamma, grad_beta) of a block
+  float2* chan;                          // [(row_grid + short_blocks) x C] (grad_gamma, grad_beta) of a block
   float2* sums;                          // [graphs x groups] backward: the two means of a long graph
   float *grad_gamma, *grad_beta;
   int32_t* status;
 };
 
-__device__ __forceinline__ float act_f(int act, float z) {
-  if (act == TAURUS_ACT_RELU) return z < 0.f ? 0.f : z;
-  if (act == TAURUS_ACT_SILU) return z / (1.f + expf(-z));
+// 1 / (1 + e^-z): the division is the hardware's reciprocal (1 ulp); an overflow of e^-z gives 0.
+__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + expf(-z)); }
+template <int ACT>
+__device__ __forceinline__ float act_f(float z) {
+  if (ACT == TAURUS_ACT_RELU) return z < 0.f ? 0.f : z;
+  if (ACT == TAURUS_ACT_SILU) return z * sigmoid(z);
   return z;
 }
-__device__ __forceinline__ float act_slope(int act, float z) {
-  if (act == TAURUS_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (act == TAURUS_ACT_SILU) { const float s = 1.f / (1.f + expf(-z)); return s * (1.f + z * (1.f - s)); }
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+  if (ACT == TAURUS_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+  if (ACT == TAURUS_ACT_SILU) { const float s = sigmoid(z); return s * (1.f + z * (1.f - s)); }
   return 1.f;
 }
 
-__device__ __forceinline__ void graph_rows(const NormArgs& a, long long s, long long* b, long long* e) {
+__device__ __forceinline__ void graph_rows(const NormArgs& a, long long s, long long* b, long long* e, int32_t* status = nullptr) {
   if (!a.offsets) { *b = 0; *e = a.n; return; }
-  group_rows(a.offsets, s, a.n, b, e, nullptr);
+  group_rows(a.offsets, s, a.n, b, e, status);
 }
 
 // The graph that row r belongs to (-1: none): the last one whose offset is not above r.  By one warp, 32 offsets a step.
@@ -65,10 +69,9 @@ __device__ __forceinline__ long long graph_of(const NormArgs& a, long long r) {
     const long long i = lo + step * lane;   // offsets[i] <= r for a first run of lanes
     const unsigned yes = __ballot_sync(0xffffffffu, i < hi && a.offsets[i] <= r);
     const int k = __popc(yes);              // (any count: offsets out of order are refused, but read in bounds)
-    if (k == 0) { hi = lo; break; }
-    const long long first = lo + step * (k - 1);
+    if (k == 0) break;
     const long long next = lo + step * k;
-    lo = first + 1;
+    lo += step * (k - 1) + 1;
     if (next < hi) hi = next;
     if (step == 1) break;
   }
@@ -76,133 +79,181 @@ __device__ __forceinline__ long long graph_of(const NormArgs& a, long long r) {
   return s >= 0 && s < a.graphs ? s : -1;
 }
 
-// Sums over the row lanes of a block: red[c] holds channel c's afterwards, and the block is in step.
-__device__ __forceinline__ void sum_lanes(float2* red, int C, int lanes) {
-  __syncthreads();
-  while (lanes > 1) {
-    const int half = (lanes + 1) / 2;
-    for (int i = threadIdx.x; i < (lanes - half) * C; i += blockDim.x) {
-      const float2 o = red[i + half * C];
-      red[i].x += o.x; red[i].y += o.y;
-    }
-    __syncthreads();
-    lanes = half;
+// Shared memory: red [lanes x vpr x NG] | stat [groups].
+__device__ __forceinline__ float2* shared_red() { extern __shared__ __align__(16) float2 norm_shared[]; return norm_shared; }
+
+// SAME: the V channels of a vector are of one group, and a thread has one mean for them; else one for each (NG of them).
+template <int V, bool SAME> constexpr int ng() { return SAME ? 1 : V; }
+// Row vectors of a thread in flight, and of a short graph's in registers.
+template <int V> constexpr int batch() { return V == 8 ? 4 : 8; }
+template <int V> constexpr int grad_batch() { return V == 8 ? 2 : 4; }
+
+struct Moments { float n, mean, m2; };
+__device__ __forceinline__ void join(Moments& a, float nb, float mb, float m2b) {
+  if (nb > 0.f) {
+    const float d = mb - a.mean, n = a.n + nb, f = __fdividef(nb, n);
+    a.m2 += m2b + d * d * a.n * f;
+    a.mean += d * f;
+    a.n = n;
   }
 }
 
-// Lanes that share a group: a power of two of them, each with its channels; f(g, first channel of the lane, step) -> value to sum.
-__device__ __forceinline__ int team_of(int cg) { int t = 1; while (t < cg && t < 32) t *= 2; return t; }
-__device__ __forceinline__ float team_sum(float v, int team) {
-  for (int o = team / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
+// What a thread knows for the whole launch.
+template <class T, int V, bool SAME>
+struct Place {
+  int cv, r;
+  bool on;
+  int g[ng<V, SAME>()];
+  __device__ __forceinline__ explicit Place(const NormArgs& a) {
+    cv = threadIdx.x % a.vpr; r = threadIdx.x / a.vpr;
+    on = r < a.lanes;
+#pragma unroll
+    for (int k = 0; k < ng<V, SAME>(); ++k) g[k] = (cv * V + k) / a.cg;
+  }
+  // Rows of [b, e) that are this thread's.
+  __device__ __forceinline__ int rows(const NormArgs& a, long long b, long long e) const {
+    const int len = (int)(e - b);
+    return on && len > r ? (len - r + a.lanes - 1) / a.lanes : 0;
+  }
+  __device__ __forceinline__ const T* at(const T* x, long long ld, long long b) const { return x + (b + r) * ld + cv * V; }
+};
+
+template <class T, int V, int U>
+__device__ __forceinline__ void load_batch(Vec<T, V> (&v)[U], const T* p, long long step, int left) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) if (u < left) v[u] = load_vec<Vec<T, V>>(p + u * step);
+}
+// Keeps vectors as they were loaded: without it the compiler keeps the fp32 values it made of them, twice as many registers for 16-bit types.
+template <class T, int V, int U>
+__device__ __forceinline__ void as_loaded(Vec<T, V> (&v)[U]) {
+  if constexpr (sizeof(T) == 2 && V > 1) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) asm volatile("" : "+r"(reinterpret_cast<unsigned*>(&v[u])[i]));
+  }
+}
+// Joins the first min(left, U) vectors to m.
+template <class T, int V, int U, bool SAME>
+__device__ __forceinline__ void add_batch(Moments (&m)[ng<V, SAME>()], const Vec<T, V> (&v)[U], int left) {
+  const int count = left < U ? left : U;
+  if (SAME) {
+    float s = 0.f, q = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u < left)
+#pragma unroll
+        for (int k = 0; k < V; ++k) s += to_f32<T>(v[u].v[k]);
+    const float n = (float)(count * V), mean = __fdividef(s, n);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u < left)
+#pragma unroll
+        for (int k = 0; k < V; ++k) { const float d = to_f32<T>(v[u].v[k]) - mean; q += d * d; }
+    // (deviations from a mean that is off by its rounding: the square of that is far below the sum)
+    join(m[0], n, mean, q);
+  } else {
+    const float n = (float)count, inv = __fdividef(1.f, n);
+#pragma unroll
+    for (int k = 0; k < ng<V, SAME>(); ++k) {
+      float s = 0.f, q = 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) if (u < left) s += to_f32<T>(v[u].v[k]);
+      const float mean = s * inv;
+#pragma unroll
+      for (int u = 0; u < U; ++u) if (u < left) { const float d = to_f32<T>(v[u].v[k]) - mean; q += d * d; }
+      join(m[k], n, mean, q);
+    }
+  }
 }
 
-// (mean, sum of squared deviations) of every group of a part with `rows` rows from red[c] = sums of (x - pivot) and its square.
-__device__ __forceinline__ void group_moments(const NormArgs& a, const float2* red, const float* pivot, long long rows, float2* out) {
-  const int team = team_of(a.cg), per_warp = 32 / team, warps = blockDim.x >> 5;
-  const int lane = threadIdx.x & 31, t = lane % team;
-  const float inv = 1.f / (float)rows;
-  for (int g0 = (threadIdx.x >> 5) * per_warp; g0 < a.groups; g0 += warps * per_warp) {
-    const int g = g0 + lane / team;
-    const bool in = g < a.groups;
-    float m = 0.f;
-    if (in) for (int c = t; c < a.cg; c += team) m += pivot[g * a.cg + c] + red[g * a.cg + c].x * inv;
-    const float mean = team_sum(m, team) / (float)a.cg;
-    float q = 0.f;
-    if (in)
-      for (int c = t; c < a.cg; c += team) {
-        const float2 s = red[g * a.cg + c];
-        const float d = (pivot[g * a.cg + c] - mean) + s.x * inv, m2 = s.y - s.x * s.x * inv;
-        q += (m2 < 0.f ? 0.f : m2) + (float)rows * d * d;
+// Teams of a power of two of threads share the entries of a group; f(group, first entry, step) by every thread of the block at once.
+__device__ __forceinline__ int team_of(int groups, int entries) {
+  int t = 1;
+  while (t < 32 && t < entries && 2 * t * groups <= (int)blockDim.x) t *= 2;
+  return t;
+}
+
+// Moments of every group over a part of `len` rows: red holds (mean, m2) of every thread; out[g] = (mean, m2).
+template <int V, bool SAME>
+__device__ __forceinline__ void join_block(const NormArgs& a, const float2* red, int len, float2* out) {
+  const int w = SAME ? a.cg / V : a.cg, row = SAME ? a.vpr : a.C, lanes = len < a.lanes ? len : a.lanes, entries = lanes * w;
+  const int team = team_of(a.groups, entries), teams = blockDim.x / team, t = threadIdx.x % team;
+  for (int g0 = 0; g0 < a.groups; g0 += teams) {
+    const int g = g0 + threadIdx.x / team;
+    Moments m = {0.f, 0.f, 0.f};
+    if (g < a.groups) {
+      int r = t / w, j = t % w;
+      const int dr = team / w, dj = team % w;
+      for (int i = t; i < entries; i += team) {
+        const float2 p = red[r * row + g * w + j];
+        join(m, (float)((len - r + a.lanes - 1) / a.lanes * (SAME ? V : 1)), p.x, p.y);
+        r += dr; j += dj;
+        if (j >= w) { j -= w; ++r; }
       }
-    q = team_sum(q, team);
-    if (in && t == 0) out[g] = make_float2(mean, q);
+    }
+    for (int o = team / 2; o > 0; o >>= 1) {
+      const float n = __shfl_down_sync(0xffffffffu, m.n, o), mean = __shfl_down_sync(0xffffffffu, m.mean, o), m2 = __shfl_down_sync(0xffffffffu, m.m2, o);
+      join(m, n, mean, m2);
+    }
+    if (g < a.groups && t == 0) out[g] = make_float2(m.mean, m.m2);
   }
-  __syncthreads();
 }
 
-// Sums of x - pivot of rows [b, e) into red; the pivots into `pivot`.  KEEP: the thread's first BATCH vectors stay in `keep`.
-template <class T, int V>
-__device__ __forceinline__ void sum_rows(const NormArgs& a, const T* x, long long b, long long e, float2* red, float* pivot, Vec<T, V> (&keep)[BATCH]) {
-  const int cv = threadIdx.x % a.vpr, r = threadIdx.x / a.vpr;
-  if (r < a.lanes) {
-    const T* const col = x + cv * V;
-    float p[V], s1[V] = {}, s2[V] = {};
-    load_f32<T, V>(col + b * a.ld_x, p);
-    for (long long i = b + r; i < e; i += (long long)a.lanes * BATCH) {
-      Vec<T, V> v[BATCH];
+template <class T, int V, bool SAME>
+__device__ __forceinline__ void put_moments(const Place<T, V, SAME>& at, const NormArgs& a, const Moments (&m)[ng<V, SAME>()], float2* red) {
+  if (!at.on) return;
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u) if (i + (long long)u * a.lanes < e) v[u] = load_vec<Vec<T, V>>(col + (i + (long long)u * a.lanes) * a.ld_x);
-#pragma unroll
-      for (int u = 0; u < BATCH; ++u)
-        if (i + (long long)u * a.lanes < e)
-#pragma unroll
-          for (int k = 0; k < V; ++k) { const float d = to_f32<T>(v[u].v[k]) - p[k]; s1[k] += d; s2[k] += d * d; }
-      if (i == b + r)
-#pragma unroll
-        for (int u = 0; u < BATCH; ++u) keep[u] = v[u];
-    }
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      red[r * a.C + cv * V + k] = make_float2(s1[k], s2[k]);
-      if (r == 0) pivot[cv * V + k] = p[k];
-    }
-  }
-  sum_lanes(red, a.C, a.lanes);
+  for (int k = 0; k < ng<V, SAME>(); ++k) red[(at.r * a.vpr + at.cv) * ng<V, SAME>() + k] = make_float2(m[k].mean, m[k].m2);
 }
 
-// y = act((x - mean) rstd gamma + beta) for rows [b, e); stat[g] = (mean, rstd).
-template <class T, int V, bool KEPT>
-__device__ __forceinline__ void write_rows(const NormArgs& a, const T* x, T* y, long long b, long long e, const float2* stat, const Vec<T, V> (&keep)[BATCH]) {
-  const int cv = threadIdx.x % a.vpr, r = threadIdx.x / a.vpr;
-  if (r >= a.lanes) return;
-  float mean[V], mul[V], add[V];
+// y = act((x - mean) rstd gamma + beta) of a thread's vectors; stat: (mean, rstd).
+template <class T, int V, bool SAME>
+struct Apply {
+  float mean[ng<V, SAME>()], mul[V], add[V];
+  __device__ __forceinline__ void set(const Place<T, V, SAME>& at, const float (&gamma)[V], const float (&beta)[V], const float2* stat) {
+    float rstd[ng<V, SAME>()];
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    const int c = cv * V + k;
-    const float2 s = stat[c / a.cg];
-    mean[k] = s.x;
-    mul[k] = s.y * (a.gamma ? a.gamma[c] : 1.f);
-    add[k] = a.beta ? a.beta[c] : 0.f;
+    for (int k = 0; k < ng<V, SAME>(); ++k) { const float2 s = stat[at.g[k]]; mean[k] = s.x; rstd[k] = s.y; }
+#pragma unroll
+    for (int k = 0; k < V; ++k) { mul[k] = rstd[SAME ? 0 : k] * gamma[k]; add[k] = beta[k]; }
   }
-  for (long long i = b + r; i < e; i += (long long)a.lanes * BATCH) {
-    Vec<T, V> v[BATCH];
-    if (KEPT && i == b + r) {
+  template <int ACT>
+  __device__ __forceinline__ void row(const Vec<T, V>& v, T* y) const {
+    float o[V];
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u) v[u] = keep[u];
-    } else {
-#pragma unroll
-      for (int u = 0; u < BATCH; ++u)
-        if (i + (long long)u * a.lanes < e) v[u] = load_vec<Vec<T, V>, KEPT ? LOAD_PLAIN : LOAD_ONCE>(x + (i + (long long)u * a.lanes) * a.ld_x + cv * V);
-    }
-#pragma unroll
-    for (int u = 0; u < BATCH; ++u) {
-      const long long row = i + (long long)u * a.lanes;
-      if (row >= e) break;
-      float o[V];
-#pragma unroll
-      for (int k = 0; k < V; ++k) o[k] = act_f(a.act, (to_f32<T>(v[u].v[k]) - mean[k]) * mul[k] + add[k]);
-      store_f32<T, V>(y + row * a.ld_y + cv * V, o);
-    }
+    for (int k = 0; k < V; ++k) o[k] = act_f<ACT>((to_f32<T>(v.v[k]) - mean[SAME ? 0 : k]) * mul[k] + add[k]);
+    store_f32<T, V>(y, o);
   }
+};
+template <int V>
+__device__ __forceinline__ void affine(const NormArgs& a, int cv, float (&gamma)[V], float (&beta)[V]) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) { gamma[k] = a.gamma ? a.gamma[cv * V + k] : 1.f; beta[k] = a.beta ? a.beta[cv * V + k] : 0.f; }
 }
 
 // Threads of a block: at most 512, but for rows of up to 1 024 vectors.
 constexpr int block_limit(int v) { return MAX_C / v > 512 ? 1024 : 512; }
+// Threads of a block of the kernels for long graphs, and blocks to an SM (80 registers a thread).
+constexpr int ROW_THREADS = 256;
+constexpr int row_limit(int v) { return MAX_C / v > ROW_THREADS ? MAX_C / v : ROW_THREADS; }
+constexpr int row_blocks(int v) { return row_limit(v) > 768 ? 1 : 768 / row_limit(v); }
 
-// Shared memory: red [lanes x C] | pivot [C] | stat [groups], and in the backward pass chan [C].
-__device__ __forceinline__ float2* shared_red() { extern __shared__ __align__(16) float2 norm_shared[]; return norm_shared; }
-
-template <class T, int V>
+template <class T, int V, bool SAME, int ACT>
 __global__ void __launch_bounds__(block_limit(V)) norm_short_kernel(const NormArgs a, const T* x, T* y) {
   float2* const red = shared_red();
-  float2* const stat = red + (size_t)a.lanes * a.C;
-  float* const pivot = reinterpret_cast<float*>(stat + a.groups);
+  float2* const stat = red + (size_t)a.lanes * a.vpr * ng<V, SAME>();
+  const Place<T, V, SAME> at(a);
+  float gamma[V], beta[V];
+  affine<V>(a, at.cv, gamma, beta);
+  const long long step = a.lanes * a.ld_x, ystep = a.lanes * a.ld_y;
   for (long long s = blockIdx.x; s < a.graphs; s += gridDim.x) {
     long long b, e;
-    graph_rows(a, s, &b, &e);
-    if (threadIdx.x == 0 && a.offsets) { long long u, v; group_rows(a.offsets, s, a.n, &u, &v, a.status); }
-    if (e - b > 2 * a.R) continue;                                    // long: the other kernels'
+    graph_rows(a, s, &b, &e, threadIdx.x == 0 ? a.status : nullptr);
+    if (e - b > 2 * a.R) {                                            // long: the other kernels'
+      if (threadIdx.x == 0) *a.any_long = 1;
+      continue;
+    }
     if (b == e) {
       for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
         if (a.mean) a.mean[s * a.groups + g] = 0.f;
@@ -210,30 +261,60 @@ __global__ void __launch_bounds__(block_limit(V)) norm_short_kernel(const NormAr
       }
       continue;
     }
-    Vec<T, V> keep[BATCH];
-    sum_rows<T, V>(a, x, b, e, red, pivot, keep);
-    group_moments(a, red, pivot, e - b, stat);
-    const float inv = 1.f / ((float)(e - b) * (float)a.cg);
+    const int rows = at.rows(a, b, e);
+    const T* p = at.at(x, a.ld_x, b);
+    Vec<T, V> keep[batch<V>()];
+    Moments m[ng<V, SAME>()] = {};
+    if (rows > 0) {
+      load_batch<T, V, batch<V>()>(keep, p, step, rows);
+      add_batch<T, V, batch<V>(), SAME>(m, keep, rows);
+      for (int left = rows - batch<V>(); left > 0; left -= batch<V>()) {
+        Vec<T, V> v[batch<V>()];
+        p += batch<V>() * step;
+        load_batch<T, V, batch<V>()>(v, p, step, left);
+        add_batch<T, V, batch<V>(), SAME>(m, v, left);
+      }
+    }
+    as_loaded(keep);
+    put_moments(at, a, m, red);
+    __syncthreads();
+    join_block<V, SAME>(a, red, (int)(e - b), stat);
+    __syncthreads();
+    const float inv = __fdividef(1.f, (float)(e - b) * (float)a.cg);
     for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
-      const float2 m = stat[g];
-      const float rstd = 1.f / sqrtf(m.y * inv + a.eps);
-      stat[g] = make_float2(m.x, rstd);
-      if (a.mean) a.mean[s * a.groups + g] = m.x;
+      const float2 q = stat[g];
+      const float rstd = 1.f / sqrtf(q.y * inv + a.eps);
+      stat[g] = make_float2(q.x, rstd);
+      if (a.mean) a.mean[s * a.groups + g] = q.x;
       if (a.rstd) a.rstd[s * a.groups + g] = rstd;
     }
     __syncthreads();
-    write_rows<T, V, true>(a, x, y, b, e, stat, keep);
-    __syncthreads();                                                  // stat is written again
+    if (rows > 0) {
+      Apply<T, V, SAME> f;
+      f.set(at, gamma, beta, stat);
+      p = at.at(x, a.ld_x, b);
+      T* q = y + (b + at.r) * a.ld_y + at.cv * V;
+#pragma unroll
+      for (int u = 0; u < batch<V>(); ++u) if (u < rows) f.template row<ACT>(keep[u], q + u * ystep);
+      for (int left = rows - batch<V>(); left > 0; left -= batch<V>()) {
+        Vec<T, V> v[batch<V>()];
+        p += batch<V>() * step; q += batch<V>() * ystep;
+        load_batch<T, V, batch<V>()>(v, p, step, left);
+#pragma unroll
+        for (int u = 0; u < batch<V>(); ++u) if (u < left) f.template row<ACT>(v[u], q + u * ystep);
+      }
+    }
+    __syncthreads();                                                  // red and stat are written again
   }
 }
 
 // The parts of long graphs in block of rows `blk`: slot 0 is the graph of its first row, slot 1 that of its last row where another one begins
 // in the block.  (A long graph has more than 2 R rows, so no third one can meet the block.)
-struct Parts { long long s[2], b[2], e[2], begin[2], end[2]; };     // graph (-1: none), the part's rows, the graph's rows
+struct Parts { long long s[2], b[2], e[2]; };                       // graph (-1: none), the part's rows
 __device__ __forceinline__ void find_parts(const NormArgs& a, long long blk, Parts* p) {     // p in shared memory; by the whole block
   const long long r0 = blk * a.R, r1 = r0 + a.R < a.n ? r0 + a.R : a.n;
-  const int warp = threadIdx.x >> 5;
-  if (warp == 0) {                        // (both by one warp: a block may have no second one)
+  __syncthreads();                        // the block is through with the parts before
+  if (threadIdx.x < 32)                   // (both by one warp: a block may have no second one)
     for (int k = 0; k < 2; ++k) {
       long long s = graph_of(a, k ? r1 - 1 : r0), b = 0, e = 0;
       if (s >= 0) {
@@ -243,28 +324,36 @@ __device__ __forceinline__ void find_parts(const NormArgs& a, long long blk, Par
       if (threadIdx.x == 0) {
         const long long pb = b > r0 ? b : r0, pe = e < r1 ? e : r1;
         if (pb >= pe) s = -1;
-        p->s[k] = s; p->begin[k] = b; p->end[k] = e; p->b[k] = pb; p->e[k] = pe;
+        p->s[k] = s; p->b[k] = pb; p->e[k] = pe;
       }
     }
-  }
   __syncthreads();
 }
 
-template <class T, int V>
-__global__ void __launch_bounds__(block_limit(V)) norm_stats_kernel(const NormArgs a, const T* x) {
+template <class T, int V, bool SAME>
+__global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_stats_kernel(const NormArgs a, const T* x) {
   __shared__ Parts parts;
+  if (!*a.any_long) return;
   float2* const red = shared_red();
-  float2* const stat = red + (size_t)a.lanes * a.C;
-  float* const pivot = reinterpret_cast<float*>(stat + a.groups);
-  const long long blk = blockIdx.x;
-  find_parts(a, blk, &parts);
-  for (int k = 0; k < 2; ++k) {
-    if (parts.s[k] < 0) continue;
-    Vec<T, V> keep[BATCH];
-    sum_rows<T, V>(a, x, parts.b[k], parts.e[k], red, pivot, keep);
-    group_moments(a, red, pivot, parts.e[k] - parts.b[k], stat);
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) a.part[(blk * 2 + k) * a.groups + g] = stat[g];
-    __syncthreads();
+  const Place<T, V, SAME> at(a);
+  const long long step = a.lanes * a.ld_x;
+  for (long long blk = blockIdx.x; blk < a.blocks; blk += gridDim.x) {
+    find_parts(a, blk, &parts);
+    for (int k = 0; k < 2; ++k) {
+      if (parts.s[k] < 0) continue;
+      const T* p = at.at(x, a.ld_x, parts.b[k]);
+      Moments m[ng<V, SAME>()] = {};
+      for (int left = at.rows(a, parts.b[k], parts.e[k]); left > 0; left -= batch<V>()) {
+        Vec<T, V> v[batch<V>()];
+        load_batch<T, V, batch<V>()>(v, p, step, left);
+        add_batch<T, V, batch<V>(), SAME>(m, v, left);
+        p += batch<V>() * step;
+      }
+      put_moments(at, a, m, red);
+      __syncthreads();
+      join_block<V, SAME>(a, red, (int)(parts.e[k] - parts.b[k]), a.part + (blk * 2 + k) * a.groups);
+      __syncthreads();
+    }
   }
 }
 
@@ -274,9 +363,8 @@ __device__ __forceinline__ double warp_sum(double v) {
 }
 
 // The partial results of a long graph lie in slot 0 of the blocks of rows it meets, but for the block it begins in the middle of.
-// Block (x, y): the long graph that begins in block of rows x, groups y * warps + warp.
 struct Owned { long long s, begin, end, first, last; int first_slot; };
-__device__ __forceinline__ bool owned_graph(const NormArgs& a, long long blk, Owned* o) {    // by every warp for itself
+__device__ __forceinline__ bool owned_graph(const NormArgs& a, long long blk, Owned* o) {    // the long graph that begins in block of rows blk; by every warp for itself
   const long long r0 = blk * a.R, r1 = r0 + a.R < a.n ? r0 + a.R : a.n;
   o->s = graph_of(a, r1 - 1);           // a long graph that begins in the block does not end in it
   if (o->s < 0) return false;
@@ -289,231 +377,320 @@ __device__ __forceinline__ double part_rows(const NormArgs& a, const Owned& o, l
   const long long b = blk * a.R > o.begin ? blk * a.R : o.begin, e = (blk + 1) * a.R < o.end ? (blk + 1) * a.R : o.end;
   return (double)(e - b);
 }
+__device__ __forceinline__ float2 part_at(const NormArgs& a, const Owned& o, long long blk, int g) {
+  return a.part[(blk * 2 + (blk == o.first ? o.first_slot : 0)) * a.groups + g];
+}
 
-__global__ void norm_combine_kernel(const NormArgs a) {
-  Owned o;
-  if (!owned_graph(a, blockIdx.x, &o)) return;
-  const int lane = threadIdx.x & 31, g = blockIdx.y * (blockDim.x >> 5) + (threadIdx.x >> 5);
+// Grid (blocks of rows by stride, groups / warps): a warp to a group of the long graph that begins in a block of rows.
+constexpr int COMBINE_WARPS = 8;
+__global__ void __launch_bounds__(32 * COMBINE_WARPS) norm_combine_kernel(const NormArgs a) {
+  if (!*a.any_long) return;
+  const int lane = threadIdx.x & 31, g = blockIdx.y * COMBINE_WARPS + (threadIdx.x >> 5);
   if (g >= a.groups) return;
-  auto at = [&](long long blk) { return a.part[(blk * 2 + (blk == o.first ? o.first_slot : 0)) * a.groups + g]; };
-  const double rows = (double)(o.end - o.begin);
-  double m = 0;
-  for (long long blk = o.first + lane; blk <= o.last; blk += 32) m += part_rows(a, o, blk) * (double)at(blk).x;
-  const double mean = warp_sum(m) / rows;
-  double q = 0;
-  for (long long blk = o.first + lane; blk <= o.last; blk += 32) {
-    const float2 p = at(blk);
-    const double d = (double)p.x - mean;
-    q += (double)p.y + part_rows(a, o, blk) * a.cg * d * d;
-  }
-  q = warp_sum(q);
-  if (lane == 0) {
-    a.mean[o.s * a.groups + g] = (float)mean;
-    a.rstd[o.s * a.groups + g] = (float)(1.0 / sqrt(q / (rows * a.cg) + (double)a.eps));
+  for (long long blk0 = blockIdx.x; blk0 < a.blocks; blk0 += gridDim.x) {
+    Owned o;
+    if (!owned_graph(a, blk0, &o)) continue;
+    // moments about the first part's mean
+    const double rows = (double)(o.end - o.begin), shift = part_at(a, o, o.first, g).x;
+    double s = 0, q = 0;
+#pragma unroll 8
+    for (long long blk = o.first + lane; blk <= o.last; blk += 32) {
+      const float2 p = part_at(a, o, blk, g);
+      const double d = (double)p.x - shift, w = part_rows(a, o, blk) * d;
+      s += w;
+      q += (double)p.y + w * d * a.cg;
+    }
+    s = warp_sum(s) / rows;
+    q = warp_sum(q) / (rows * a.cg) - s * s;
+    if (lane == 0) {
+      a.mean[o.s * a.groups + g] = (float)(shift + s);
+      a.rstd[o.s * a.groups + g] = (float)(1.0 / sqrt((q < 0 ? 0 : q) + (double)a.eps));
+    }
   }
 }
 
-template <class T, int V>
-__global__ void __launch_bounds__(block_limit(V)) norm_apply_kernel(const NormArgs a, const T* x, T* y) {
+// From the last block of rows to the first: the last ones read are still in the L2.
+template <class T, int V, bool SAME, int ACT>
+__global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_apply_kernel(const NormArgs a, const T* x, T* y) {
   __shared__ Parts parts;
+  if (!*a.any_long) return;
+  const Place<T, V, SAME> at(a);
+  float gamma[V], beta[V];
+  affine<V>(a, at.cv, gamma, beta);
   float2* const stat = shared_red();
-  find_parts(a, blockIdx.x, &parts);
-  for (int k = 0; k < 2; ++k) {
-    const long long s = parts.s[k];
-    if (s < 0) continue;
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) stat[g] = make_float2(a.mean[s * a.groups + g], a.rstd[s * a.groups + g]);
-    __syncthreads();
-    Vec<T, V> none[BATCH];
-    write_rows<T, V, false>(a, x, y, parts.b[k], parts.e[k], stat, none);
-    __syncthreads();
+  const long long step = a.lanes * a.ld_x, ystep = a.lanes * a.ld_y;
+  for (long long blk = a.blocks - 1 - blockIdx.x; blk >= 0; blk -= gridDim.x) {
+    find_parts(a, blk, &parts);
+    for (int k = 0; k < 2; ++k) {
+      const long long s = parts.s[k];
+      if (s < 0) continue;
+      for (int g = threadIdx.x; g < a.groups; g += blockDim.x) stat[g] = make_float2(a.mean[s * a.groups + g], a.rstd[s * a.groups + g]);
+      __syncthreads();
+      Apply<T, V, SAME> f;
+      f.set(at, gamma, beta, stat);
+      const T* p = at.at(x, a.ld_x, parts.b[k]);
+      T* q = y + (parts.b[k] + at.r) * a.ld_y + at.cv * V;
+      for (int left = at.rows(a, parts.b[k], parts.e[k]); left > 0; left -= batch<V>()) {
+        Vec<T, V> v[batch<V>()];
+        load_batch<T, V, batch<V>()>(v, p, step, left);
+#pragma unroll
+        for (int u = 0; u < batch<V>(); ++u) if (u < left) f.template row<ACT>(v[u], q + u * ystep);
+        p += batch<V>() * step; q += batch<V>() * ystep;
+      }
+      __syncthreads();
+    }
   }
 }
 
 // ---------------------------------------------------------------------------------------------------------------- gradients
 
-template <int V>
-struct ChannelConsts {
-  float mean[V], rstd[V], gamma[V], beta[V];
-  __device__ __forceinline__ void load(const NormArgs& a, long long s, int cv) {
+template <class T, int V, bool SAME>
+struct Grads {
+  float mean[ng<V, SAME>()], rstd[ng<V, SAME>()];
+  float gamma[V], beta[V];
+  __device__ __forceinline__ void set(const NormArgs& a, const Place<T, V, SAME>& at, long long s) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const int c = cv * V + k, g = c / a.cg;
-      mean[k] = a.mean[s * a.groups + g]; rstd[k] = a.rstd[s * a.groups + g];
-      gamma[k] = a.gamma ? a.gamma[c] : 1.f; beta[k] = a.beta ? a.beta[c] : 0.f;
-    }
+    for (int k = 0; k < ng<V, SAME>(); ++k) { mean[k] = a.mean[s * a.groups + at.g[k]]; rstd[k] = a.rstd[s * a.groups + at.g[k]]; }
+  }
+  template <int ACT>
+  __device__ __forceinline__ void element(int k, T xv, T dyv, float* xh, float* dz) const {
+    *xh = (to_f32<T>(xv) - mean[SAME ? 0 : k]) * rstd[SAME ? 0 : k];
+    *dz = to_f32<T>(dyv) * act_slope<ACT>(*xh * gamma[k] + beta[k]);
   }
 };
-
-// red[c] = (sum dz xh, sum dz) over rows [b, e).
-template <class T, int V>
-__device__ __forceinline__ void sum_grads(const NormArgs& a, const T* x, const T* dy, long long s, long long b, long long e, float2* red) {
-  const int cv = threadIdx.x % a.vpr, r = threadIdx.x / a.vpr;
-  if (r < a.lanes) {
-    ChannelConsts<V> c;
-    c.load(a, s, cv);
-    float s1[V] = {}, s2[V] = {};
-    for (long long i = b + r; i < e; i += (long long)a.lanes * BATCH) {
-      Vec<T, V> v[BATCH], w[BATCH];
+// c1, c2: sums of dz xh and dz by channel; g1, g2: of gamma dz xh and gamma dz by group (of the graph at hand).
+template <int ACT, class T, int V, int U, bool SAME>
+__device__ __forceinline__ void add_grads(const Grads<T, V, SAME>& f, const Vec<T, V> (&v)[U], const Vec<T, V> (&w)[U], int left, float (&c1)[V], float (&c2)[V],
+                                          float (&g1)[ng<V, SAME>()], float (&g2)[ng<V, SAME>()]) {
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u) {
-        const long long row = i + (long long)u * a.lanes;
-        if (row < e) { v[u] = load_vec<Vec<T, V>>(x + row * a.ld_x + cv * V); w[u] = load_vec<Vec<T, V>>(dy + row * a.ld_dy + cv * V); }
-      }
-#pragma unroll
-      for (int u = 0; u < BATCH; ++u)
-        if (i + (long long)u * a.lanes < e)
-#pragma unroll
-          for (int k = 0; k < V; ++k) {
-            const float xh = (to_f32<T>(v[u].v[k]) - c.mean[k]) * c.rstd[k];
-            const float dz = to_f32<T>(w[u].v[k]) * act_slope(a.act, xh * c.gamma[k] + c.beta[k]);
-            s1[k] += dz * xh; s2[k] += dz;
-          }
-    }
-#pragma unroll
-    for (int k = 0; k < V; ++k) red[r * a.C + cv * V + k] = make_float2(s1[k], s2[k]);
-  }
-  sum_lanes(red, a.C, a.lanes);
-}
-
-// out[g] = (sum gamma dz xh, sum gamma dz) over the group's channels.
-__device__ __forceinline__ void group_grads(const NormArgs& a, const float2* red, float2* out) {
-  const int team = team_of(a.cg), per_warp = 32 / team, warps = blockDim.x >> 5;
-  const int lane = threadIdx.x & 31, t = lane % team;
-  for (int g0 = (threadIdx.x >> 5) * per_warp; g0 < a.groups; g0 += warps * per_warp) {
-    const int g = g0 + lane / team;
-    float u = 0.f, v = 0.f;
-    if (g < a.groups)
-      for (int c = g * a.cg + t; c < (g + 1) * a.cg; c += team) {
-        const float w = a.gamma ? a.gamma[c] : 1.f;
-        u += w * red[c].x; v += w * red[c].y;
-      }
-    u = team_sum(u, team); v = team_sum(v, team);
-    if (g < a.groups && t == 0) out[g] = make_float2(u, v);
-  }
-  __syncthreads();
-}
-
-// dx for rows [b, e); mean_g[g] = (mean of gamma dz xh, mean of gamma dz).
-template <class T, int V>
-__device__ __forceinline__ void write_grads(const NormArgs& a, const T* x, const T* dy, T* dx, long long s, long long b, long long e, const float2* mean_g) {
-  const int cv = threadIdx.x % a.vpr, r = threadIdx.x / a.vpr;
-  if (r >= a.lanes) return;
-  ChannelConsts<V> c;
-  c.load(a, s, cv);
-  float m1[V], m2[V];
-#pragma unroll
-  for (int k = 0; k < V; ++k) { const float2 m = mean_g[(cv * V + k) / a.cg]; m1[k] = m.x; m2[k] = m.y; }
-  for (long long i = b + r; i < e; i += (long long)a.lanes * BATCH) {
-    Vec<T, V> v[BATCH], w[BATCH];
-#pragma unroll
-    for (int u = 0; u < BATCH; ++u) {
-      const long long row = i + (long long)u * a.lanes;
-      if (row < e) { v[u] = load_vec<Vec<T, V>, LOAD_ONCE>(x + row * a.ld_x + cv * V); w[u] = load_vec<Vec<T, V>, LOAD_ONCE>(dy + row * a.ld_dy + cv * V); }
-    }
-#pragma unroll
-    for (int u = 0; u < BATCH; ++u) {
-      const long long row = i + (long long)u * a.lanes;
-      if (row >= e) break;
-      float o[V];
+  for (int u = 0; u < U; ++u)
+    if (u < left)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const float xh = (to_f32<T>(v[u].v[k]) - c.mean[k]) * c.rstd[k];
-        const float dz = to_f32<T>(w[u].v[k]) * act_slope(a.act, xh * c.gamma[k] + c.beta[k]);
-        o[k] = c.rstd[k] * (c.gamma[k] * dz - m2[k] - xh * m1[k]);
+        float xh, dz;
+        f.template element<ACT>(k, v[u].v[k], w[u].v[k], &xh, &dz);
+        c1[k] += dz * xh; c2[k] += dz;
+        const float q = f.gamma[k] * dz;
+        g1[SAME ? 0 : k] += q * xh; g2[SAME ? 0 : k] += q;
       }
-      store_f32<T, V>(dx + row * a.ld_y + cv * V, o);
+}
+template <int ACT, class T, int V, bool SAME>
+__device__ __forceinline__ void write_grad(const Grads<T, V, SAME>& f, const Vec<T, V>& v, const Vec<T, V>& w, const float (&m1)[ng<V, SAME>()],
+                                           const float (&m2)[ng<V, SAME>()], T* dx) {
+  float o[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    float xh, dz;
+    f.template element<ACT>(k, v.v[k], w.v[k], &xh, &dz);
+    o[k] = f.rstd[SAME ? 0 : k] * (f.gamma[k] * dz - m2[SAME ? 0 : k] - xh * m1[SAME ? 0 : k]);
+  }
+  store_f32<T, V>(dx, o);
+}
+
+// out[g] = sums of (g1, g2) over a block's threads, from red.
+template <int V, bool SAME>
+__device__ __forceinline__ void sum_block(const NormArgs& a, const float2* red, float2* out) {
+  const int w = SAME ? a.cg / V : a.cg, row = SAME ? a.vpr : a.C, entries = a.lanes * w;
+  const int team = team_of(a.groups, entries), teams = blockDim.x / team, t = threadIdx.x % team;
+  for (int g0 = 0; g0 < a.groups; g0 += teams) {
+    const int g = g0 + threadIdx.x / team;
+    float u = 0.f, v = 0.f;
+    if (g < a.groups) {
+      int r = t / w, j = t % w;
+      const int dr = team / w, dj = team % w;
+      for (int i = t; i < entries; i += team) {
+        const float2 p = red[r * row + g * w + j];
+        u += p.x; v += p.y;
+        r += dr; j += dj;
+        if (j >= w) { j -= w; ++r; }
+      }
     }
+    for (int o = team / 2; o > 0; o >>= 1) { u += __shfl_down_sync(0xffffffffu, u, o); v += __shfl_down_sync(0xffffffffu, v, o); }
+    if (g < a.groups && t == 0) out[g] = make_float2(u, v);
+  }
+}
+template <class T, int V, bool SAME>
+__device__ __forceinline__ void put_sums(const Place<T, V, SAME>& at, const NormArgs& a, const float (&g1)[ng<V, SAME>()], const float (&g2)[ng<V, SAME>()], float2* red) {
+  if (!at.on) return;
+#pragma unroll
+  for (int k = 0; k < ng<V, SAME>(); ++k) red[(at.r * a.vpr + at.cv) * ng<V, SAME>() + k] = make_float2(g1[k], g2[k]);
+}
+// A block's sums by channel, its threads' added in the order of their rows; red has room for lanes x C.
+template <class T, int V, bool SAME>
+__device__ __forceinline__ void put_channels(const Place<T, V, SAME>& at, const NormArgs& a, const float (&c1)[V], const float (&c2)[V], float2* red, float2* out) {
+  __syncthreads();
+  if (at.on)
+#pragma unroll
+    for (int k = 0; k < V; ++k) red[at.r * a.C + at.cv * V + k] = make_float2(c1[k], c2[k]);
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+    float u = 0.f, v = 0.f;
+    for (int r = 0; r < a.lanes; ++r) { const float2 p = red[r * a.C + c]; u += p.x; v += p.y; }
+    out[c] = make_float2(u, v);
   }
 }
 
-template <class T, int V>
+template <class T, int V, bool SAME, int ACT>
 __global__ void __launch_bounds__(block_limit(V)) norm_grad_short_kernel(const NormArgs a, const T* x, const T* dy, T* dx) {
-  float2* const red = shared_red();
-  float2* const stat = red + (size_t)a.lanes * a.C;
-  float2* const chan = stat + a.groups;
-  for (int c = threadIdx.x; c < a.C; c += blockDim.x) chan[c] = make_float2(0.f, 0.f);
+  float2* const stat = shared_red();
+  float2* const red = stat + a.groups;
+  const Place<T, V, SAME> at(a);
+  Grads<T, V, SAME> f;
+  affine<V>(a, at.cv, f.gamma, f.beta);
+  float c1[V] = {}, c2[V] = {};
+  const long long step = a.lanes * a.ld_x, dstep = a.lanes * a.ld_dy, ystep = a.lanes * a.ld_y;
   for (long long s = blockIdx.x; s < a.graphs; s += gridDim.x) {
     long long b, e;
-    graph_rows(a, s, &b, &e);
-    if (threadIdx.x == 0 && a.offsets) { long long u, v; group_rows(a.offsets, s, a.n, &u, &v, a.status); }
-    if (e - b > 2 * a.R || b == e) continue;
-    sum_grads<T, V>(a, x, dy, s, b, e, red);
-    group_grads(a, red, stat);
-    for (int c = threadIdx.x; c < a.C; c += blockDim.x) { chan[c].x += red[c].x; chan[c].y += red[c].y; }
-    const float inv = 1.f / ((float)(e - b) * (float)a.cg);
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) stat[g] = make_float2(stat[g].x * inv, stat[g].y * inv);
+    graph_rows(a, s, &b, &e, threadIdx.x == 0 ? a.status : nullptr);
+    if (e - b > 2 * a.R) {
+      if (threadIdx.x == 0) *a.any_long = 1;
+      continue;
+    }
+    if (b == e) continue;
+    const int rows = at.rows(a, b, e);
+    const T *p = at.at(x, a.ld_x, b), *d = at.at(dy, a.ld_dy, b);
+    Vec<T, V> kx[grad_batch<V>()], kd[grad_batch<V>()];
+    float g1[ng<V, SAME>()] = {}, g2[ng<V, SAME>()] = {};
+    if (rows > 0) {
+      load_batch<T, V, grad_batch<V>()>(kx, p, step, rows);
+      load_batch<T, V, grad_batch<V>()>(kd, d, dstep, rows);
+      f.set(a, at, s);
+      add_grads<ACT>(f, kx, kd, rows, c1, c2, g1, g2);
+      for (int left = rows - grad_batch<V>(); left > 0; left -= grad_batch<V>()) {
+        Vec<T, V> v[grad_batch<V>()], w[grad_batch<V>()];
+        p += grad_batch<V>() * step; d += grad_batch<V>() * dstep;
+        load_batch<T, V, grad_batch<V>()>(v, p, step, left);
+        load_batch<T, V, grad_batch<V>()>(w, d, dstep, left);
+        add_grads<ACT>(f, v, w, left, c1, c2, g1, g2);
+      }
+    }
+    as_loaded(kx);
+    as_loaded(kd);
+    put_sums(at, a, g1, g2, red);
     __syncthreads();
-    write_grads<T, V>(a, x, dy, dx, s, b, e, stat);
+    sum_block<V, SAME>(a, red, stat);
+    __syncthreads();
+    if (rows > 0) {
+      const float inv = __fdividef(1.f, (float)(e - b) * (float)a.cg);
+      float m1[ng<V, SAME>()], m2[ng<V, SAME>()];
+#pragma unroll
+      for (int k = 0; k < ng<V, SAME>(); ++k) { const float2 q = stat[at.g[k]]; m1[k] = q.x * inv; m2[k] = q.y * inv; }
+      p = at.at(x, a.ld_x, b); d = at.at(dy, a.ld_dy, b);
+      T* q = dx + (b + at.r) * a.ld_y + at.cv * V;
+#pragma unroll
+      for (int u = 0; u < grad_batch<V>(); ++u) if (u < rows) write_grad<ACT>(f, kx[u], kd[u], m1, m2, q + u * ystep);
+      for (int left = rows - grad_batch<V>(); left > 0; left -= grad_batch<V>()) {
+        Vec<T, V> v[grad_batch<V>()], w[grad_batch<V>()];
+        p += grad_batch<V>() * step; d += grad_batch<V>() * dstep; q += grad_batch<V>() * ystep;
+        load_batch<T, V, grad_batch<V>()>(v, p, step, left);
+        load_batch<T, V, grad_batch<V>()>(w, d, dstep, left);
+#pragma unroll
+        for (int u = 0; u < grad_batch<V>(); ++u) if (u < left) write_grad<ACT>(f, v[u], w[u], m1, m2, q + u * ystep);
+      }
+    }
     __syncthreads();
   }
-  for (int c = threadIdx.x; c < a.C; c += blockDim.x) a.chan[(size_t)(a.blocks + blockIdx.x) * a.C + c] = chan[c];
+  if (a.chan) put_channels(at, a, c1, c2, red, a.chan + (size_t)(a.row_grid + blockIdx.x) * a.C);
 }
 
-template <class T, int V>
-__global__ void __launch_bounds__(block_limit(V)) norm_grad_stats_kernel(const NormArgs a, const T* x, const T* dy) {
+template <class T, int V, bool SAME, int ACT>
+__global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_grad_stats_kernel(const NormArgs a, const T* x, const T* dy) {
   __shared__ Parts parts;
   float2* const red = shared_red();
-  float2* const stat = red + (size_t)a.lanes * a.C;
-  float2* const chan = stat + a.groups;
-  for (int c = threadIdx.x; c < a.C; c += blockDim.x) chan[c] = make_float2(0.f, 0.f);
-  const long long blk = blockIdx.x;
-  find_parts(a, blk, &parts);
-  for (int k = 0; k < 2; ++k) {
-    if (parts.s[k] < 0) continue;
-    sum_grads<T, V>(a, x, dy, parts.s[k], parts.b[k], parts.e[k], red);
-    group_grads(a, red, stat);
-    for (int c = threadIdx.x; c < a.C; c += blockDim.x) { chan[c].x += red[c].x; chan[c].y += red[c].y; }
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) a.part[(blk * 2 + k) * a.groups + g] = stat[g];
-    __syncthreads();
+  const Place<T, V, SAME> at(a);
+  float c1[V] = {}, c2[V] = {};
+  if (*a.any_long) {
+    Grads<T, V, SAME> f;
+    affine<V>(a, at.cv, f.gamma, f.beta);
+    const long long step = a.lanes * a.ld_x, dstep = a.lanes * a.ld_dy;
+    for (long long blk = blockIdx.x; blk < a.blocks; blk += gridDim.x) {
+      find_parts(a, blk, &parts);
+      for (int k = 0; k < 2; ++k) {
+        if (parts.s[k] < 0) continue;
+        f.set(a, at, parts.s[k]);
+        const T *p = at.at(x, a.ld_x, parts.b[k]), *d = at.at(dy, a.ld_dy, parts.b[k]);
+        float g1[ng<V, SAME>()] = {}, g2[ng<V, SAME>()] = {};
+        for (int left = at.rows(a, parts.b[k], parts.e[k]); left > 0; left -= grad_batch<V>()) {
+          Vec<T, V> v[grad_batch<V>()], w[grad_batch<V>()];
+          load_batch<T, V, grad_batch<V>()>(v, p, step, left);
+          load_batch<T, V, grad_batch<V>()>(w, d, dstep, left);
+          add_grads<ACT>(f, v, w, left, c1, c2, g1, g2);
+          p += grad_batch<V>() * step; d += grad_batch<V>() * dstep;
+        }
+        put_sums(at, a, g1, g2, red);
+        __syncthreads();
+        sum_block<V, SAME>(a, red, a.part + (blk * 2 + k) * a.groups);
+        __syncthreads();
+      }
+    }
   }
-  for (int c = threadIdx.x; c < a.C; c += blockDim.x) a.chan[(size_t)blk * a.C + c] = chan[c];
+  if (a.chan) put_channels(at, a, c1, c2, red, a.chan + (size_t)blockIdx.x * a.C);
 }
 
-__global__ void norm_grad_combine_kernel(const NormArgs a) {
-  Owned o;
-  if (!owned_graph(a, blockIdx.x, &o)) return;
-  const int lane = threadIdx.x & 31, g = blockIdx.y * (blockDim.x >> 5) + (threadIdx.x >> 5);
+// The last blocks of a row of the grid (blockIdx.x from `combine` on; of the first one only) add up the sums by channel: a lane to a channel, the warps
+// share the blocks' sums, which are added in their order.
+__global__ void __launch_bounds__(32 * COMBINE_WARPS) norm_grad_combine_kernel(const NormArgs a, int combine) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if ((int)blockIdx.x >= combine) {
+    __shared__ double2 part[COMBINE_WARPS][32];
+    if (blockIdx.y > 0) return;
+    const int c = ((int)blockIdx.x - combine) * 32 + lane, rows = a.row_grid + a.short_blocks, per = (rows + COMBINE_WARPS - 1) / COMBINE_WARPS;
+    double u = 0, v = 0;
+    if (c < a.C)
+#pragma unroll 8
+      for (int i = warp * per; i < (warp + 1) * per && i < rows; ++i) { const float2 p = a.chan[(size_t)i * a.C + c]; u += p.x; v += p.y; }
+    part[warp][lane] = make_double2(u, v);
+    __syncthreads();
+    if (warp == 0 && c < a.C) {
+      for (int w = 1; w < COMBINE_WARPS; ++w) { u += part[w][lane].x; v += part[w][lane].y; }
+      if (a.grad_gamma) a.grad_gamma[c] = (float)u;
+      if (a.grad_beta) a.grad_beta[c] = (float)v;
+    }
+    return;
+  }
+  if (!*a.any_long) return;
+  const int g = blockIdx.y * COMBINE_WARPS + warp;
   if (g >= a.groups) return;
-  double u = 0, v = 0;
-  for (long long blk = o.first + lane; blk <= o.last; blk += 32) {
-    const float2 p = a.part[(blk * 2 + (blk == o.first ? o.first_slot : 0)) * a.groups + g];
-    u += p.x; v += p.y;
+  for (long long blk0 = blockIdx.x; blk0 < a.blocks; blk0 += combine) {
+    Owned o;
+    if (!owned_graph(a, blk0, &o)) continue;
+    double u = 0, v = 0;
+#pragma unroll 8
+    for (long long blk = o.first + lane; blk <= o.last; blk += 32) { const float2 p = part_at(a, o, blk, g); u += p.x; v += p.y; }
+    u = warp_sum(u); v = warp_sum(v);
+    const double m = (double)(o.end - o.begin) * a.cg;
+    if (lane == 0) a.sums[o.s * a.groups + g] = make_float2((float)(u / m), (float)(v / m));
   }
-  u = warp_sum(u); v = warp_sum(v);
-  const double m = (double)(o.end - o.begin) * a.cg;
-  if (lane == 0) a.sums[o.s * a.groups + g] = make_float2((float)(u / m), (float)(v / m));
 }
 
-template <class T, int V>
-__global__ void __launch_bounds__(block_limit(V)) norm_grad_apply_kernel(const NormArgs a, const T* x, const T* dy, T* dx) {
+template <class T, int V, bool SAME, int ACT>
+__global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_grad_apply_kernel(const NormArgs a, const T* x, const T* dy, T* dx) {
   __shared__ Parts parts;
-  float2* const stat = shared_red();
-  find_parts(a, blockIdx.x, &parts);
-  for (int k = 0; k < 2; ++k) {
-    const long long s = parts.s[k];
-    if (s < 0) continue;
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) stat[g] = a.sums[s * a.groups + g];
-    __syncthreads();
-    write_grads<T, V>(a, x, dy, dx, s, parts.b[k], parts.e[k], stat);
-    __syncthreads();
-  }
-}
-
-// grad_gamma, grad_beta: a lane to a channel, the warps share the blocks' sums, added in their order.
-constexpr int CHANNEL_WARPS = 32;
-__global__ void __launch_bounds__(32 * CHANNEL_WARPS) norm_channels_kernel(const NormArgs a) {
-  __shared__ double2 part[CHANNEL_WARPS][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-  const long long rows = a.blocks + a.short_blocks;
-  double u = 0, v = 0;
-  if (c < a.C)
-    for (long long i = warp; i < rows; i += CHANNEL_WARPS) { const float2 p = a.chan[(size_t)i * a.C + c]; u += p.x; v += p.y; }
-  part[warp][lane] = make_double2(u, v);
-  __syncthreads();
-  if (warp == 0 && c < a.C) {
-    for (int w = 1; w < CHANNEL_WARPS; ++w) { u += part[w][lane].x; v += part[w][lane].y; }
-    if (a.grad_gamma) a.grad_gamma[c] = (float)u;
-    if (a.grad_beta) a.grad_beta[c] = (float)v;
+  if (!*a.any_long) return;
+  const Place<T, V, SAME> at(a);
+  Grads<T, V, SAME> f;
+  affine<V>(a, at.cv, f.gamma, f.beta);
+  const long long step = a.lanes * a.ld_x, dstep = a.lanes * a.ld_dy, ystep = a.lanes * a.ld_y;
+  for (long long blk = a.blocks - 1 - blockIdx.x; blk >= 0; blk -= gridDim.x) {
+    find_parts(a, blk, &parts);
+    for (int k = 0; k < 2; ++k) {
+      const long long s = parts.s[k];
+      if (s < 0) continue;
+      f.set(a, at, s);
+      float m1[ng<V, SAME>()], m2[ng<V, SAME>()];
+#pragma unroll
+      for (int j = 0; j < ng<V, SAME>(); ++j) { const float2 q = a.sums[s * a.groups + at.g[j]]; m1[j] = q.x; m2[j] = q.y; }
+      const T *p = at.at(x, a.ld_x, parts.b[k]), *d = at.at(dy, a.ld_dy, parts.b[k]);
+      T* q = dx + (parts.b[k] + at.r) * a.ld_y + at.cv * V;
+      for (int left = at.rows(a, parts.b[k], parts.e[k]); left > 0; left -= grad_batch<V>()) {
+        Vec<T, V> v[grad_batch<V>()], w[grad_batch<V>()];
+        load_batch<T, V, grad_batch<V>()>(v, p, step, left);
+        load_batch<T, V, grad_batch<V>()>(w, d, dstep, left);
+#pragma unroll
+        for (int u = 0; u < grad_batch<V>(); ++u) if (u < left) write_grad<ACT>(f, v[u], w[u], m1, m2, q + u * ystep);
+        p += grad_batch<V>() * step; d += grad_batch<V>() * dstep; q += grad_batch<V>() * ystep;
+      }
+    }
   }
 }
 
@@ -530,22 +707,24 @@ __global__ void norm_no_rows_kernel(const NormArgs a) {
 
 // ---------------------------------------------------------------------------------------------------------------- host
 
-constexpr int STAT_BLOCKS_PER_SM = 8, DEVICE_SMS = 148;
-// Rows of a block of rows: at least 8 192 elements, and about eight blocks to an SM.  (By the device's number of SMs as built for, so
+constexpr int DEVICE_SMS = 148, ROW_BLOCKS_PER_SM = 8, ROW_GRID_PER_SM = 8;
+// Rows of a block of rows: at least 8 192 elements, and about eight blocks to an SM.  (By the number of SMs this is built for, so
 // that a workspace's size depends on the sizes alone.)
-long long block_rows(int64_t n, int C) { return std::max<long long>(std::max(1, 8192 / C), (n + DEVICE_SMS * STAT_BLOCKS_PER_SM - 1) / (DEVICE_SMS * STAT_BLOCKS_PER_SM)); }
+long long block_rows(int64_t n, int C) { return std::max<long long>(std::max(1, 8192 / C), (n + DEVICE_SMS * ROW_BLOCKS_PER_SM - 1) / (DEVICE_SMS * ROW_BLOCKS_PER_SM)); }
 
-struct NormSpace { long long R, blocks, short_blocks; size_t part, chan, sums, mean, rstd, bytes; };
+struct NormSpace { long long R, blocks; int short_blocks, row_grid; size_t flag, part, chan, sums, mean, rstd, bytes; };
 NormSpace norm_space(int64_t n, int64_t graphs, int C, int groups, bool grad) {
   NormSpace s;
   s.R = block_rows(n, C);
   const bool long_ones = n > 2 * s.R;                            // else no graph can be long
   s.blocks = long_ones ? (n + s.R - 1) / s.R : 0;
-  s.short_blocks = std::min<long long>(graphs, DEVICE_SMS * 16);
+  s.row_grid = (int)std::min<long long>(s.blocks, DEVICE_SMS * ROW_GRID_PER_SM);
+  s.short_blocks = (int)std::min<long long>(graphs, DEVICE_SMS * 32);
   size_t at = 0;
   auto take = [&](size_t b) { const size_t o = at; at += (b + 255) / 256 * 256; return o; };
+  s.flag = take(long_ones ? 4 : 0);
   s.part = take((size_t)s.blocks * 2 * groups * 8);
-  s.chan = take(grad ? (size_t)(s.blocks + s.short_blocks) * C * 8 : 0);
+  s.chan = take(grad ? (size_t)(s.row_grid + s.short_blocks) * C * 8 : 0);
   s.sums = take(grad && long_ones ? (size_t)graphs * groups * 8 : 0);
   s.mean = take(!grad && long_ones ? (size_t)graphs * groups * 4 : 0);
   s.rstd = take(!grad && long_ones ? (size_t)graphs * groups * 4 : 0);
@@ -557,9 +736,11 @@ bool norm_shape_ok(int64_t n, int64_t graphs, int32_t width, int32_t groups) {
   return n >= 0 && n < (1ll << 31) && graphs >= 1 && graphs < (1ll << 31) && width >= 1 && groups >= 1 && width % groups == 0;
 }
 
-int norm_vector(int size, int width, const void* a, int64_t lda, const void* b, int64_t ldb, const void* c, int64_t ldc) {
+// Vectors of at most 16 bytes; of at most four elements where they would reach over several groups (each has moments of its own then).
+int norm_vector(int size, int width, int cg, const void* a, int64_t lda, const void* b, int64_t ldb, const void* c, int64_t ldc) {
   int v = 16 / size;
   auto bad = [&](const void* p, int64_t ld) { return p && (ld % v != 0 || !rows_aligned(p, v * size)); };
+  if (cg % v != 0 && v > 4) v = 4;
   while (v > 1 && (width % v != 0 || bad(a, lda) || bad(b, ldb) || bad(c, ldc))) v >>= 1;
   return v;
 }
@@ -571,11 +752,32 @@ void set_block(NormArgs* a, int v, int threads, int* out_threads) {
   *out_threads = threads;
 }
 
-// Threads for a short graph: about four vectors each for a graph of the average length.
-int short_threads(int64_t n, int64_t graphs, int vpr) {
+// f(tag of the element type, vector length, is a vector of one group, activation) for the kernels that fit; v from norm_vector.
+template <class F>
+void with_norm_kernels(int32_t type, int v, int cg, int act, F f0) {
+  auto f = [&](auto tt, auto vc, auto same) {
+    if (act == TAURUS_ACT_RELU) f0(tt, vc, same, std::integral_constant<int, TAURUS_ACT_RELU>());
+    else if (act == TAURUS_ACT_SILU) f0(tt, vc, same, std::integral_constant<int, TAURUS_ACT_SILU>());
+    else f0(tt, vc, same, std::integral_constant<int, TAURUS_ACT_NONE>());
+  };
+  with_row_type(type, [&](auto tt) {
+    return with_vector(v, [&](auto vc) {
+      constexpr int V = decltype(vc)::value;
+      using Tag = std::decay_t<decltype(tt)>;
+      if constexpr (V * sizeof(typename Tag::type) <= 16) {
+        if (cg % V == 0) f(tt, vc, std::true_type());
+        else if constexpr (V > 1 && V <= 4) f(tt, vc, std::false_type());
+      }
+      return 0;
+    });
+  });
+}
+
+// Threads for a short graph: at most `batch` vectors each for a graph of the average length.
+int short_threads(int64_t n, int64_t graphs, int vpr, int batch) {
   const long long vectors = std::min<long long>(n / graphs + 1, 1ll << 20) * vpr;
   int t = 32;
-  while (t < 512 && t * BATCH < vectors) t *= 2;
+  while (t < 512 && t * batch < vectors) t *= 2;
   return t;
 }
 
@@ -625,9 +827,16 @@ extern "C" int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offset
   char* const ws = static_cast<char*>(workspace);
   NormArgs a = {};
   a.n = n; a.graphs = graphs; a.offsets = reinterpret_cast<const long long*>(offsets); a.ld_x = ld_x; a.ld_y = ld_out; a.C = width; a.groups = groups;
-  a.cg = width / groups; a.act = act; a.eps = eps; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd; a.status = status;
-  a.R = s.R; a.blocks = s.blocks; a.short_blocks = s.blocks > 0 && !offsets ? 0 : s.short_blocks;   // (one graph of n rows: a long one)
-  a.part = reinterpret_cast<float2*>(ws + s.part);
+  a.cg = width / groups; a.eps = eps; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd; a.status = status;
+  a.R = s.R; a.blocks = s.blocks; a.row_grid = s.row_grid;
+  const bool whole = s.blocks > 0 && !offsets;                                              // one graph of n rows: a long one
+  a.short_blocks = whole ? 0 : s.short_blocks;
+  a.any_long = reinterpret_cast<int*>(ws + s.flag);
+  if (s.blocks > 0) {
+    const cudaError_t e = cudaMemsetAsync(a.any_long, whole ? 1 : 0, 4, st);
+    if (e != cudaSuccess) { taurus_note_cuda_error(e, "norm"); return TAURUS_ERR_CUDA; }
+  }
+   a.part = reinterpret_cast<float2*>(ws + s.part);
   if (n == 0) {
     if (mean || rstd) norm_no_rows_kernel<<<(int)std::min<long long>((graphs * groups + 255) / 256, 4096), 256, 0, st>>>(a);
   } else {
@@ -635,30 +844,26 @@ extern "C" int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offset
       if (!a.mean) a.mean = reinterpret_cast<float*>(ws + s.mean);
       if (!a.rstd) a.rstd = reinterpret_cast<float*>(ws + s.rstd);
     }
-    const int v = norm_vector(ts, width, x, ld_x, out_rows, ld_out, nullptr, 0);
-    with_row_type(type, [&](auto tt) {
+    const int v = norm_vector(ts, width, a.cg, x, ld_x, out_rows, ld_out, nullptr, 0);
+    with_norm_kernels(type, v, a.cg, act, [&](auto tt, auto vc, auto same, auto ac) {
       using T = typename decltype(tt)::type;
-      return with_vector(v, [&](auto vc) {
-        constexpr int V = decltype(vc)::value;
-        if constexpr (V * sizeof(T) <= 16) {
-          const T* const xp = static_cast<const T*>(x);
-          T* const yp = static_cast<T*>(out_rows);
-          int threads;
-          if (a.short_blocks > 0) {
-            set_block(&a, V, short_threads(n, graphs, width / V), &threads);
-            const size_t smem = (size_t)a.lanes * width * 8 + (size_t)groups * 8 + (size_t)width * 4;
-            norm_short_kernel<T, V><<<(int)a.short_blocks, threads, smem, st>>>(a, xp, yp);
-          }
-          if (s.blocks > 0) {
-            set_block(&a, V, 256, &threads);
-            const size_t smem = (size_t)a.lanes * width * 8 + (size_t)groups * 8 + (size_t)width * 4;
-            norm_stats_kernel<T, V><<<(int)s.blocks, threads, smem, st>>>(a, xp);
-            norm_combine_kernel<<<dim3((unsigned)s.blocks, (unsigned)((groups + 7) / 8)), 256, 0, st>>>(a);
-            norm_apply_kernel<T, V><<<(int)s.blocks, threads, (size_t)groups * 8, st>>>(a, xp, yp);
-          }
-        }
-        return 0;
-      });
+      constexpr int V = decltype(vc)::value;
+      constexpr bool SAME = decltype(same)::value;
+      constexpr int ACT = decltype(ac)::value;
+      const T* const xp = static_cast<const T*>(x);
+      T* const yp = static_cast<T*>(out_rows);
+      int threads;
+      if (a.short_blocks > 0) {
+        set_block(&a, V, short_threads(n, graphs, width / V, batch<V>()), &threads);
+        const size_t smem = (size_t)a.lanes * a.vpr * ng<V, SAME>() * 8 + (size_t)groups * 8;
+        norm_short_kernel<T, V, SAME, ACT><<<a.short_blocks, threads, smem, st>>>(a, xp, yp);
+      }
+      if (s.blocks > 0) {
+        set_block(&a, V, ROW_THREADS, &threads);
+        norm_stats_kernel<T, V, SAME><<<s.row_grid, threads, (size_t)a.lanes * a.vpr * ng<V, SAME>() * 8, st>>>(a, xp);
+        norm_combine_kernel<<<dim3((unsigned)s.row_grid, (unsigned)((groups + COMBINE_WARPS - 1) / COMBINE_WARPS)), 32 * COMBINE_WARPS, 0, st>>>(a);
+        norm_apply_kernel<T, V, SAME, ACT><<<s.row_grid, threads, (size_t)groups * 8, st>>>(a, xp, yp);
+      }
     });
   }
   const cudaError_t e = cudaGetLastError();
@@ -708,40 +913,45 @@ extern "C" int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* o
   char* const ws = static_cast<char*>(workspace);
   NormArgs a = {};
   a.n = n; a.graphs = graphs; a.offsets = reinterpret_cast<const long long*>(offsets); a.ld_x = ld_x; a.ld_y = ld_grad_x; a.ld_dy = ld_grad; a.C = width; a.groups = groups;
-  a.cg = width / groups; a.act = act; a.gamma = gamma; a.beta = beta; a.status = status; a.grad_gamma = grad_gamma; a.grad_beta = grad_beta;
-  a.R = s.R; a.blocks = s.blocks; a.short_blocks = s.blocks > 0 && !offsets ? 0 : s.short_blocks;   // (one graph of n rows: a long one)
-  a.part = reinterpret_cast<float2*>(ws + s.part); a.chan = reinterpret_cast<float2*>(ws + s.chan);
+  a.cg = width / groups; a.gamma = gamma; a.beta = beta; a.status = status; a.grad_gamma = grad_gamma; a.grad_beta = grad_beta;
+  a.R = s.R; a.blocks = s.blocks; a.row_grid = s.row_grid;
+  const bool whole = s.blocks > 0 && !offsets;                                              // one graph of n rows: a long one
+  a.short_blocks = whole ? 0 : s.short_blocks;
+  a.any_long = reinterpret_cast<int*>(ws + s.flag);
+  if (s.blocks > 0) {
+    const cudaError_t e = cudaMemsetAsync(a.any_long, whole ? 1 : 0, 4, st);
+    if (e != cudaSuccess) { taurus_note_cuda_error(e, "norm"); return TAURUS_ERR_CUDA; }
+  }
+   a.part = reinterpret_cast<float2*>(ws + s.part); a.chan = reinterpret_cast<float2*>(ws + s.chan);
   a.sums = reinterpret_cast<float2*>(ws + s.sums);
   if (n == 0) {
     if (grad_gamma || grad_beta) norm_no_rows_kernel<<<4, 256, 0, st>>>(a);
   } else {
     a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);                 // read only here
-    const int v = norm_vector(ts, width, x, ld_x, grad_out, ld_grad, grad_x, ld_grad_x);
-    with_row_type(type, [&](auto tt) {
+    if (!grad_gamma && !grad_beta) a.chan = nullptr;
+    const int v = norm_vector(ts, width, a.cg, x, ld_x, grad_out, ld_grad, grad_x, ld_grad_x);
+    with_norm_kernels(type, v, a.cg, act, [&](auto tt, auto vc, auto same, auto ac) {
       using T = typename decltype(tt)::type;
-      return with_vector(v, [&](auto vc) {
-        constexpr int V = decltype(vc)::value;
-        if constexpr (V * sizeof(T) <= 16) {
-          const T *const xp = static_cast<const T*>(x), *const dyp = static_cast<const T*>(grad_out);
-          T* const dxp = static_cast<T*>(grad_x);
-          int threads;
-          if (a.short_blocks > 0) {
-            set_block(&a, V, short_threads(n, graphs, width / V), &threads);
-            const size_t smem = (size_t)a.lanes * width * 8 + (size_t)groups * 8 + (size_t)width * 8;
-            norm_grad_short_kernel<T, V><<<(int)a.short_blocks, threads, smem, st>>>(a, xp, dyp, dxp);
-          }
-          if (s.blocks > 0) {
-            set_block(&a, V, 256, &threads);
-            const size_t smem = (size_t)a.lanes * width * 8 + (size_t)groups * 8 + (size_t)width * 8;
-            norm_grad_stats_kernel<T, V><<<(int)s.blocks, threads, smem, st>>>(a, xp, dyp);
-            norm_grad_combine_kernel<<<dim3((unsigned)s.blocks, (unsigned)((groups + 7) / 8)), 256, 0, st>>>(a);
-            norm_grad_apply_kernel<T, V><<<(int)s.blocks, threads, (size_t)groups * 8, st>>>(a, xp, dyp, dxp);
-          }
-        }
-        return 0;
-      });
+      constexpr int V = decltype(vc)::value;
+      constexpr bool SAME = decltype(same)::value;
+      constexpr int ACT = decltype(ac)::value;
+      const T *const xp = static_cast<const T*>(x), *const dyp = static_cast<const T*>(grad_out);
+      T* const dxp = static_cast<T*>(grad_x);
+      int threads;
+      if (a.short_blocks > 0) {
+        set_block(&a, V, short_threads(n, graphs, width / V, grad_batch<V>()), &threads);
+        norm_grad_short_kernel<T, V, SAME, ACT><<<a.short_blocks, threads, (size_t)a.lanes * width * 8 + (size_t)groups * 8, st>>>(a, xp, dyp, dxp);
+      }
+      if (s.blocks > 0) {
+        set_block(&a, V, ROW_THREADS, &threads);
+        norm_grad_stats_kernel<T, V, SAME, ACT><<<s.row_grid, threads, (size_t)a.lanes * width * 8, st>>>(a, xp, dyp);
+      }
+      const int channel_blocks = a.chan ? (width + 31) / 32 : 0;
+      if (s.row_grid + channel_blocks > 0)
+        norm_grad_combine_kernel<<<dim3((unsigned)(s.row_grid + channel_blocks), (unsigned)(s.blocks > 0 ? (groups + COMBINE_WARPS - 1) / COMBINE_WARPS : 1)), 32 * COMBINE_WARPS, 0,
+                                   st>>>(a, s.row_grid);
+      if (s.blocks > 0) norm_grad_apply_kernel<T, V, SAME, ACT><<<s.row_grid, threads, 0, st>>>(a, xp, dyp, dxp);
     });
-    if (grad_gamma || grad_beta) norm_channels_kernel<<<(width + 31) / 32, 32 * CHANNEL_WARPS, 0, st>>>(a);
   }
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) { taurus_note_cuda_error(e, "norm_rows_grad"); return TAURUS_ERR_CUDA; }

@@ -235,32 +235,47 @@ def permute_rows(V: int, width: int, in_rows, ld_in: int, rank, out_rows, ld_out
         raise TaurusError(rc, "taurus_permute_rows")
 
 
+_dtype_names: dict = {}      # torch / numpy dtype -> its name
+
+
+def _dtype_name(dtype) -> str:
+    name = _dtype_names.get(dtype)
+    if name is None:
+        name = _dtype_names[dtype] = str(dtype).replace("torch.", "")
+    return name
+
+
+_ROW_TYPES = {"float32": F32, "bfloat16": BF16, "float16": F16}
+
+
 def _row_type(t) -> int:
     """F32, BF16 or F16 of a torch or numpy dtype, of a tensor or array, or as it is given (F32, ...)."""
     if isinstance(t, int):
         return t
-    name = str(getattr(t, "dtype", t)).replace("torch.", "")
-    if name not in ("float32", "bfloat16", "float16"):
+    name = _dtype_name(getattr(t, "dtype", t))
+    if name not in _ROW_TYPES:
         raise TypeError("rows are float32, bfloat16 or float16, got %s" % name)
-    return {"float32": F32, "bfloat16": BF16, "float16": F16}[name]
+    return _ROW_TYPES[name]
 
 
 def _rows(x, n: int, width: int, ld: int) -> Optional[int]:
     """Address of n rows: a 2-D tensor of at least n x width whose rows are contiguous and ld elements apart, or an address."""
     if x is None or isinstance(x, int):
         return x
-    if x.dim() != 2 or x.shape[0] < n or x.shape[1] < width or (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) != ld):
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 2 or shape[0] < n or shape[1] < width or (stride[1] != 1 and shape[1] > 1) or (stride[0] != ld and shape[0] > 1):
         raise ValueError("expected at least %d contiguous rows of %d elements, %d elements apart" % (n, width, ld))
     return x.data_ptr()
 
 
 def _array(x, dtype: Optional[str], count: int) -> Optional[int]:
     """Address of a contiguous tensor of at least count elements of that dtype, or an address."""
-    if hasattr(x, "numel"):
-        if dtype and str(x.dtype).replace("torch.", "") != dtype:
-            raise TypeError("expected %s, got %s" % (dtype, x.dtype))
-        if x.numel() < count:
-            raise ValueError("expected at least %d elements, got %d" % (count, x.numel()))
+    if x is None or isinstance(x, int):
+        return x
+    if dtype and _dtype_name(x.dtype) != dtype:
+        raise TypeError("expected %s, got %s" % (dtype, x.dtype))
+    if x.numel() < count:
+        raise ValueError("expected at least %d elements, got %d" % (count, x.numel()))
     return _ptr(x)
 
 

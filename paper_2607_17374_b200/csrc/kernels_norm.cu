@@ -240,16 +240,18 @@ constexpr int row_limit(int v) { return MAX_C / v > ROW_THREADS ? MAX_C / v : RO
 constexpr int row_blocks(int v) { return row_limit(v) > 768 ? 1 : 768 / row_limit(v); }
 
 template <class T, int V, bool SAME, int ACT>
-__global__ void __launch_bounds__(block_limit(V)) norm_short_kernel(const NormArgs a, const T* x, T* y) {
+__global__ void __launch_bounds__(block_limit(V), 1024 / block_limit(V)) norm_short_kernel(const NormArgs a, const T* x, T* y) {
   float2* const red = shared_red();
   float2* const stat = red + (size_t)a.lanes * a.vpr * ng<V, SAME>();
   const Place<T, V, SAME> at(a);
   float gamma[V], beta[V];
   affine<V>(a, at.cv, gamma, beta);
   const long long step = a.lanes * a.ld_x, ystep = a.lanes * a.ld_y;
+  long long b, e, next_b, next_e;                                     // (the next graph's offsets are on their way while this one is at work)
+  if (blockIdx.x < a.graphs) graph_rows(a, blockIdx.x, &next_b, &next_e, threadIdx.x == 0 ? a.status : nullptr);
   for (long long s = blockIdx.x; s < a.graphs; s += gridDim.x) {
-    long long b, e;
-    graph_rows(a, s, &b, &e, threadIdx.x == 0 ? a.status : nullptr);
+    b = next_b; e = next_e;
+    if (s + gridDim.x < a.graphs) graph_rows(a, s + gridDim.x, &next_b, &next_e, threadIdx.x == 0 ? a.status : nullptr);
     if (e - b > 2 * a.R) {                                            // long: the other kernels'
       if (threadIdx.x == 0) *a.any_long = 1;
       continue;

@@ -7,16 +7,25 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "taurus_internal.h"
 
 static inline int row_type_size(int32_t t) { return t == TAURUS_F32 ? 4 : t == TAURUS_BF16 || t == TAURUS_F16 ? 2 : 0; }   // 0: no such type
 
-// The device that is current; every operator's arguments have to live there.
+// The device that is current; every operator's arguments have to live there.  (The number of SMs is asked for once per device: it does not change.)
 static inline bool rows_current_device(int* dev, int* sms) {
+  static std::atomic<int> known[64];
   cudaError_t e = cudaGetDevice(dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev);
+  if (e == cudaSuccess) {
+    std::atomic<int>* const k = *dev >= 0 && *dev < 64 ? &known[*dev] : nullptr;
+    *sms = k ? k->load(std::memory_order_relaxed) : 0;
+    if (*sms == 0) {
+      e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev);
+      if (e == cudaSuccess && k) k->store(*sms, std::memory_order_relaxed);
+    }
+  }
   if (e != cudaSuccess) { taurus_note_cuda_error(e, "current device"); return false; }
   return true;
 }

@@ -25,7 +25,8 @@ struct NormArgs {
   long long n, graphs;
   const long long* offsets;              // null: one graph of n rows
   long long ld_x, ld_y, ld_dy;           // ld_y: of the rows written
-  int C, groups, cg, vpr, lanes;         // cg: channels of a group; vpr: vectors of a row; lanes: rows that a block walks at once
+  int C, groups, cg, vpr;                // cg: channels of a group; vpr: vectors of a row
+  int lanes, shift;                      // rows that a block walks at once, 1 << shift
   float eps;
   const float *gamma, *beta;             // null: ones, zeros
   float *mean, *rstd;                    // [graphs x groups]
@@ -39,8 +40,9 @@ struct NormArgs {
   int32_t* status;
 };
 
-// 1 / (1 + e^-z): the division is the hardware's reciprocal (1 ulp); an overflow of e^-z gives 0.
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + expf(-z)); }
+// 1 / (1 + e^-z) by the hardware's exponential and reciprocal.  e^-z is off by about 1.5 |z| 2^-24 of itself, which moves z / (1 + e^-z) by
+// 1.5 z^2 s (1 - s) 2^-24 < 0.7 2^-24 at most; an overflow of e^-z gives 0.
+__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
 template <int ACT>
 __device__ __forceinline__ float act_f(float z) {
   if (ACT == TAURUS_ACT_RELU) return z < 0.f ? 0.f : z;
@@ -84,9 +86,15 @@ __device__ __forceinline__ float2* shared_red() { extern __shared__ __align__(16
 
 // SAME: the V channels of a vector are of one group, and a thread has one mean for them; else one for each (NG of them).
 template <int V, bool SAME> constexpr int ng() { return SAME ? 1 : V; }
-// Row vectors of a thread in flight, and of a short graph's in registers.
+// Row vectors of a thread in flight: of a long graph's rows, and of a short graph's, whose code is run a few times a block only and has to be short
+// (with 4 to 8 of them, twice over, it came from beyond the instruction caches: 15 us for a graph of 40 rows).
 template <int V> constexpr int batch() { return V == 8 ? 4 : 8; }
 template <int V> constexpr int grad_batch() { return V == 8 ? 2 : 4; }
+template <int V> constexpr int short_batch() { return V == 8 ? 2 : 4; }
+template <int V> constexpr int short_grad_batch() { return V == 8 ? 2 : 4; }
+// Vectors of a short graph of average length to a thread: 32 elements, over which what a graph costs each thread is spread (262 144 x 64 in 9 001 graphs,
+// bf16 / fp32, 32 elements 44 / 58 us, 16 .. / 67, 64 45 / ..).
+template <int V> constexpr int short_vectors() { return 32 / V; }
 
 struct Moments { float n, mean, m2; };
 __device__ __forceinline__ void join(Moments& a, float nb, float mb, float m2b) {
@@ -111,9 +119,9 @@ struct Place {
     for (int k = 0; k < ng<V, SAME>(); ++k) g[k] = (cv * V + k) / a.cg;
   }
   // Rows of [b, e) that are this thread's.
-  __device__ __forceinline__ int rows(const NormArgs& a, long long b, long long e) const {
-    const int len = (int)(e - b);
-    return on && len > r ? (len - r + a.lanes - 1) / a.lanes : 0;
+  __device__ __forceinline__ int rows(const NormArgs& a, long long b, long long e) const { return rows(a, (int)(e - b)); }
+  __device__ __forceinline__ int rows(const NormArgs& a, int len) const {
+    return on && len > r ? (len - r + a.lanes - 1) >> a.shift : 0;
   }
   __device__ __forceinline__ const T* at(const T* x, long long ld, long long b) const { return x + (b + r) * ld + cv * V; }
 };
@@ -135,7 +143,7 @@ __device__ __forceinline__ void as_loaded(Vec<T, V> (&v)[U]) {
 }
 // Joins the first min(left, U) vectors to m.
 template <class T, int V, int U, bool SAME>
-__device__ __forceinline__ void add_batch(Moments (&m)[ng<V, SAME>()], const Vec<T, V> (&v)[U], int left) {
+__device__ __forceinline__ void add_batch(Moments (&m)[ng<V, SAME>()], Vec<T, V> (&v)[U], int left) {
   const int count = left < U ? left : U;
   if (SAME) {
     float s = 0.f, q = 0.f;
@@ -145,6 +153,7 @@ __device__ __forceinline__ void add_batch(Moments (&m)[ng<V, SAME>()], const Vec
 #pragma unroll
         for (int k = 0; k < V; ++k) s += to_f32<T>(v[u].v[k]);
     const float n = (float)(count * V), mean = __fdividef(s, n);
+    as_loaded(v);
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (u < left)
@@ -167,36 +176,43 @@ __device__ __forceinline__ void add_batch(Moments (&m)[ng<V, SAME>()], const Vec
   }
 }
 
-// Teams of a power of two of threads share the entries of a group; f(group, first entry, step) by every thread of the block at once.
-__device__ __forceinline__ int team_of(int groups, int entries) {
-  int t = 1;
-  while (t < 32 && t < entries && 2 * t * groups <= (int)blockDim.x) t *= 2;
-  return t;
-}
+// Teams of a power of two of threads share a group's entries in `red`: a.lanes rows of w entries, `row` apart.
+template <int V, bool SAME>
+struct Team {
+  int w, row, entries, size, teams, t, first, r0, j0, dr, dj;
+  __device__ __forceinline__ explicit Team(const NormArgs& a) {
+    w = SAME ? a.cg / V : a.cg; row = SAME ? a.vpr : a.C; entries = a.lanes * w;
+    int log = 0;
+    while (log < 5 && (1 << log) < entries && (2 << log) * a.groups <= (int)blockDim.x) ++log;
+    size = 1 << log;
+    teams = blockDim.x >> log; t = threadIdx.x & (size - 1); first = threadIdx.x >> log;
+    r0 = t / w; j0 = t % w; dr = size / w; dj = size % w;
+  }
+  // f(row, value) for this thread's entries of group g
+  template <class F>
+  __device__ __forceinline__ void each(const float2* red, int g, F f) const {
+    int r = r0, j = j0;
+    for (int i = t; i < entries; i += size) {
+      f(r, red[r * row + g * w + j]);
+      r += dr; j += dj;
+      if (j >= w) { j -= w; ++r; }
+    }
+  }
+};
 
 // Moments of every group over a part of `len` rows: red holds (mean, m2) of every thread; out[g] = (mean, m2).
 template <int V, bool SAME>
-__device__ __forceinline__ void join_block(const NormArgs& a, const float2* red, int len, float2* out) {
-  const int w = SAME ? a.cg / V : a.cg, row = SAME ? a.vpr : a.C, lanes = len < a.lanes ? len : a.lanes, entries = lanes * w;
-  const int team = team_of(a.groups, entries), teams = blockDim.x / team, t = threadIdx.x % team;
-  for (int g0 = 0; g0 < a.groups; g0 += teams) {
-    const int g = g0 + threadIdx.x / team;
+__device__ __forceinline__ void join_block(const NormArgs& a, const Team<V, SAME>& team, const float2* red, int len, float2* out) {
+  for (int g0 = 0; g0 < a.groups; g0 += team.teams) {
+    const int g = g0 + team.first;
     Moments m = {0.f, 0.f, 0.f};
-    if (g < a.groups) {
-      int r = t / w, j = t % w;
-      const int dr = team / w, dj = team % w;
-      for (int i = t; i < entries; i += team) {
-        const float2 p = red[r * row + g * w + j];
-        join(m, (float)((len - r + a.lanes - 1) / a.lanes * (SAME ? V : 1)), p.x, p.y);
-        r += dr; j += dj;
-        if (j >= w) { j -= w; ++r; }
-      }
-    }
-    for (int o = team / 2; o > 0; o >>= 1) {
+    if (g < a.groups)
+      team.each(red, g, [&](int r, float2 p) { join(m, len > r ? (float)(((len - r + a.lanes - 1) >> a.shift) * (SAME ? V : 1)) : 0.f, p.x, p.y); });
+    for (int o = team.size / 2; o > 0; o >>= 1) {
       const float n = __shfl_down_sync(0xffffffffu, m.n, o), mean = __shfl_down_sync(0xffffffffu, m.mean, o), m2 = __shfl_down_sync(0xffffffffu, m.m2, o);
       join(m, n, mean, m2);
     }
-    if (g < a.groups && t == 0) out[g] = make_float2(m.mean, m.m2);
+    if (g < a.groups && team.t == 0) out[g] = make_float2(m.mean, m.m2);
   }
 }
 
@@ -212,11 +228,19 @@ template <class T, int V, bool SAME>
 struct Apply {
   float mean[ng<V, SAME>()], mul[V], add[V];
   __device__ __forceinline__ void set(const Place<T, V, SAME>& at, const float (&gamma)[V], const float (&beta)[V], const float2* stat) {
-    float rstd[ng<V, SAME>()];
-#pragma unroll
-    for (int k = 0; k < ng<V, SAME>(); ++k) { const float2 s = stat[at.g[k]]; mean[k] = s.x; rstd[k] = s.y; }
+    stats(at, stat);
 #pragma unroll
     for (int k = 0; k < V; ++k) { mul[k] = rstd[SAME ? 0 : k] * gamma[k]; add[k] = beta[k]; }
+  }
+  __device__ __forceinline__ void set(const Place<T, V, SAME>& at, const float2* channel, const float2* stat) {
+    stats(at, stat);
+#pragma unroll
+    for (int k = 0; k < V; ++k) { const float2 c = channel[k]; mul[k] = rstd[SAME ? 0 : k] * c.x; add[k] = c.y; }
+  }
+  float rstd[ng<V, SAME>()];
+  __device__ __forceinline__ void stats(const Place<T, V, SAME>& at, const float2* stat) {
+#pragma unroll
+    for (int k = 0; k < ng<V, SAME>(); ++k) { const float2 s = stat[at.g[k]]; mean[k] = s.x; rstd[k] = s.y; }
   }
   template <int ACT>
   __device__ __forceinline__ void row(const Vec<T, V>& v, T* y) const {
@@ -240,71 +264,73 @@ constexpr int row_limit(int v) { return MAX_C / v > ROW_THREADS ? MAX_C / v : RO
 constexpr int row_blocks(int v) { return row_limit(v) > 768 ? 1 : 768 / row_limit(v); }
 
 template <class T, int V, bool SAME, int ACT>
-__global__ void __launch_bounds__(block_limit(V), 1024 / block_limit(V)) norm_short_kernel(const NormArgs a, const T* x, T* y) {
+__global__ void __launch_bounds__(block_limit(V)) norm_short_kernel(const NormArgs a, const T* x, T* y) {
   float2* const red = shared_red();
   float2* const stat = red + (size_t)a.lanes * a.vpr * ng<V, SAME>();
   const Place<T, V, SAME> at(a);
-  float gamma[V], beta[V];
-  affine<V>(a, at.cv, gamma, beta);
+  const Team<V, SAME> team(a);
+  float2* const channel = stat + a.groups;                            // (gamma, beta)
+  for (int c = threadIdx.x; c < a.C; c += blockDim.x) channel[c] = make_float2(a.gamma ? a.gamma[c] : 1.f, a.beta ? a.beta[c] : 0.f);
   const long long step = a.lanes * a.ld_x, ystep = a.lanes * a.ld_y;
-  long long b, e, next_b, next_e;                                     // (the next graph's offsets are on their way while this one is at work)
-  if (blockIdx.x < a.graphs) graph_rows(a, blockIdx.x, &next_b, &next_e, threadIdx.x == 0 ? a.status : nullptr);
-  for (long long s = blockIdx.x; s < a.graphs; s += gridDim.x) {
-    b = next_b; e = next_e;
-    if (s + gridDim.x < a.graphs) graph_rows(a, s + gridDim.x, &next_b, &next_e, threadIdx.x == 0 ? a.status : nullptr);
-    if (e - b > 2 * a.R) {                                            // long: the other kernels'
+  const int graphs = (int)a.graphs, longest = (int)(2 * a.R < a.n ? 2 * a.R : a.n);
+  int b, len, next_b = 0, next_len = 0;                               // (the next graph's offsets are on their way while this one is at work)
+  auto look = [&](int s) {
+    long long u, v;
+    graph_rows(a, s, &u, &v, threadIdx.x == 0 ? a.status : nullptr);
+    next_b = (int)u; next_len = (int)(v - u);
+  };
+  look(blockIdx.x);
+  for (int s = blockIdx.x; s < graphs; s += gridDim.x) {
+    b = next_b; len = next_len;
+    if (s < graphs - (int)gridDim.x) look(s + gridDim.x);
+    if (len > longest) {                                            // long: the other kernels'
       if (threadIdx.x == 0) *a.any_long = 1;
       continue;
     }
-    if (b == e) {
+    if (len == 0) {
       for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
-        if (a.mean) a.mean[s * a.groups + g] = 0.f;
-        if (a.rstd) a.rstd[s * a.groups + g] = 0.f;
+        if (a.mean) a.mean[(long long)s * a.groups + g] = 0.f;
+        if (a.rstd) a.rstd[(long long)s * a.groups + g] = 0.f;
       }
       continue;
     }
-    const int rows = at.rows(a, b, e);
-    const T* p = at.at(x, a.ld_x, b);
-    Vec<T, V> keep[batch<V>()];
-    Moments m[ng<V, SAME>()] = {};
-    if (rows > 0) {
-      load_batch<T, V, batch<V>()>(keep, p, step, rows);
-      add_batch<T, V, batch<V>(), SAME>(m, keep, rows);
-      for (int left = rows - batch<V>(); left > 0; left -= batch<V>()) {
-        Vec<T, V> v[batch<V>()];
-        p += batch<V>() * step;
-        load_batch<T, V, batch<V>()>(v, p, step, left);
-        add_batch<T, V, batch<V>(), SAME>(m, v, left);
+    const int rows = at.rows(a, len);
+    constexpr int U = short_batch<V>();
+    {
+      Moments m[ng<V, SAME>()] = {};
+      const T* p = at.at(x, a.ld_x, b);
+#pragma unroll 1
+      for (int left = rows; left > 0; left -= U) {
+        Vec<T, V> v[U];
+        load_batch<T, V, U>(v, p, step, left);
+        add_batch<T, V, U, SAME>(m, v, left);
+        p += U * step;
       }
+      put_moments(at, a, m, red);
     }
-    as_loaded(keep);
-    put_moments(at, a, m, red);
     __syncthreads();
-    join_block<V, SAME>(a, red, (int)(e - b), stat);
+    join_block(a, team, red, len, stat);
     __syncthreads();
-    const float inv = __fdividef(1.f, (float)(e - b) * (float)a.cg);
+    const float inv = __fdividef(1.f, (float)len * (float)a.cg);
     for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
       const float2 q = stat[g];
-      const float rstd = 1.f / sqrtf(q.y * inv + a.eps);
+      const float rstd = rsqrtf(q.y * inv + a.eps);
       stat[g] = make_float2(q.x, rstd);
-      if (a.mean) a.mean[s * a.groups + g] = q.x;
-      if (a.rstd) a.rstd[s * a.groups + g] = rstd;
+      if (a.mean) a.mean[(long long)s * a.groups + g] = q.x;
+      if (a.rstd) a.rstd[(long long)s * a.groups + g] = rstd;
     }
     __syncthreads();
-    if (rows > 0) {
-      Apply<T, V, SAME> f;
-      f.set(at, gamma, beta, stat);
-      p = at.at(x, a.ld_x, b);
-      T* q = y + (b + at.r) * a.ld_y + at.cv * V;
+    Apply<T, V, SAME> f;
+    if (rows > 0) f.set(at, channel + at.cv * V, stat);
+    const T* p = at.at(x, a.ld_x, b);
+    T* q = y + ((long long)b + at.r) * a.ld_y + at.cv * V;
+#pragma unroll 1
+    for (int left = rows; left > 0; left -= U) {
+      Vec<T, V> v[U];
+      load_batch<T, V, U>(v, p, step, left);
 #pragma unroll
-      for (int u = 0; u < batch<V>(); ++u) if (u < rows) f.template row<ACT>(keep[u], q + u * ystep);
-      for (int left = rows - batch<V>(); left > 0; left -= batch<V>()) {
-        Vec<T, V> v[batch<V>()];
-        p += batch<V>() * step; q += batch<V>() * ystep;
-        load_batch<T, V, batch<V>()>(v, p, step, left);
-#pragma unroll
-        for (int u = 0; u < batch<V>(); ++u) if (u < left) f.template row<ACT>(v[u], q + u * ystep);
-      }
+      for (int u = 0; u < U; ++u) if (u < left) f.template row<ACT>(v[u], q + u * ystep);
+      p += U * step; q += U * ystep;
     }
     __syncthreads();                                                  // red and stat are written again
   }
@@ -338,6 +364,7 @@ __global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_stats_kernel
   if (!*a.any_long) return;
   float2* const red = shared_red();
   const Place<T, V, SAME> at(a);
+  const Team<V, SAME> team(a);
   const long long step = a.lanes * a.ld_x;
   for (long long blk = blockIdx.x; blk < a.blocks; blk += gridDim.x) {
     find_parts(a, blk, &parts);
@@ -353,7 +380,7 @@ __global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_stats_kernel
       }
       put_moments(at, a, m, red);
       __syncthreads();
-      join_block<V, SAME>(a, red, (int)(parts.e[k] - parts.b[k]), a.part + (blk * 2 + k) * a.groups);
+      join_block(a, team, red, (int)(parts.e[k] - parts.b[k]), a.part + (blk * 2 + k) * a.groups);
       __syncthreads();
     }
   }
@@ -383,31 +410,43 @@ __device__ __forceinline__ float2 part_at(const NormArgs& a, const Owned& o, lon
   return a.part[(blk * 2 + (blk == o.first ? o.first_slot : 0)) * a.groups + g];
 }
 
-// Grid (blocks of rows by stride, groups / warps): a warp to a group of the long graph that begins in a block of rows.
-constexpr int COMBINE_WARPS = 8;
+// f(group, step, first block of rows, stride): the groups of a long graph over the threads of the blocks of a column of the grid; a warp to a group where the
+// graph has many parts, else a thread.
+constexpr int COMBINE_WARPS = 8, FEW_PARTS = 16;
+template <class F>
+__device__ __forceinline__ void each_group(const NormArgs& a, const Owned& o, F f) {
+  if (o.last - o.first < FEW_PARTS) {
+    for (int g = blockIdx.y * blockDim.x + threadIdx.x; g < a.groups; g += gridDim.y * blockDim.x) f(g, o.first, 1, false);
+  } else {
+    for (int g = blockIdx.y * COMBINE_WARPS + (threadIdx.x >> 5); g < a.groups; g += gridDim.y * COMBINE_WARPS) f(g, o.first + (threadIdx.x & 31), 32, true);
+  }
+}
+__device__ __forceinline__ double lane_sum(double v, bool warp) { return warp ? warp_sum(v) : v; }
+
+// Grid (blocks of rows by stride, groups): joins the parts of the long graph that begins in a block of rows.
 __global__ void __launch_bounds__(32 * COMBINE_WARPS) norm_combine_kernel(const NormArgs a) {
   if (!*a.any_long) return;
-  const int lane = threadIdx.x & 31, g = blockIdx.y * COMBINE_WARPS + (threadIdx.x >> 5);
-  if (g >= a.groups) return;
   for (long long blk0 = blockIdx.x; blk0 < a.blocks; blk0 += gridDim.x) {
     Owned o;
     if (!owned_graph(a, blk0, &o)) continue;
-    // moments about the first part's mean
-    const double rows = (double)(o.end - o.begin), shift = part_at(a, o, o.first, g).x;
-    double s = 0, q = 0;
+    each_group(a, o, [&](int g, long long from, int stride, bool warp) {
+      // moments about the first part's mean
+      const double rows = (double)(o.end - o.begin), shift = part_at(a, o, o.first, g).x;
+      double s = 0, q = 0;
 #pragma unroll 8
-    for (long long blk = o.first + lane; blk <= o.last; blk += 32) {
-      const float2 p = part_at(a, o, blk, g);
-      const double d = (double)p.x - shift, w = part_rows(a, o, blk) * d;
-      s += w;
-      q += (double)p.y + w * d * a.cg;
-    }
-    s = warp_sum(s) / rows;
-    q = warp_sum(q) / (rows * a.cg) - s * s;
-    if (lane == 0) {
-      a.mean[o.s * a.groups + g] = (float)(shift + s);
-      a.rstd[o.s * a.groups + g] = (float)(1.0 / sqrt((q < 0 ? 0 : q) + (double)a.eps));
-    }
+      for (long long blk = from; blk <= o.last; blk += stride) {
+        const float2 p = part_at(a, o, blk, g);
+        const double d = (double)p.x - shift, w = part_rows(a, o, blk) * d;
+        s += w;
+        q += (double)p.y + w * d * a.cg;
+      }
+      s = lane_sum(s, warp) / rows;
+      q = lane_sum(q, warp) / (rows * a.cg) - s * s;
+      if (!warp || (threadIdx.x & 31) == 0) {
+        a.mean[o.s * a.groups + g] = (float)(shift + s);
+        a.rstd[o.s * a.groups + g] = (float)(1.0 / sqrt((q < 0 ? 0 : q) + (double)a.eps));
+      }
+    });
   }
 }
 
@@ -491,24 +530,13 @@ __device__ __forceinline__ void write_grad(const Grads<T, V, SAME>& f, const Vec
 
 // out[g] = sums of (g1, g2) over a block's threads, from red.
 template <int V, bool SAME>
-__device__ __forceinline__ void sum_block(const NormArgs& a, const float2* red, float2* out) {
-  const int w = SAME ? a.cg / V : a.cg, row = SAME ? a.vpr : a.C, entries = a.lanes * w;
-  const int team = team_of(a.groups, entries), teams = blockDim.x / team, t = threadIdx.x % team;
-  for (int g0 = 0; g0 < a.groups; g0 += teams) {
-    const int g = g0 + threadIdx.x / team;
+__device__ __forceinline__ void sum_block(const NormArgs& a, const Team<V, SAME>& team, const float2* red, float2* out) {
+  for (int g0 = 0; g0 < a.groups; g0 += team.teams) {
+    const int g = g0 + team.first;
     float u = 0.f, v = 0.f;
-    if (g < a.groups) {
-      int r = t / w, j = t % w;
-      const int dr = team / w, dj = team % w;
-      for (int i = t; i < entries; i += team) {
-        const float2 p = red[r * row + g * w + j];
-        u += p.x; v += p.y;
-        r += dr; j += dj;
-        if (j >= w) { j -= w; ++r; }
-      }
-    }
-    for (int o = team / 2; o > 0; o >>= 1) { u += __shfl_down_sync(0xffffffffu, u, o); v += __shfl_down_sync(0xffffffffu, v, o); }
-    if (g < a.groups && t == 0) out[g] = make_float2(u, v);
+    if (g < a.groups) team.each(red, g, [&](int, float2 p) { u += p.x; v += p.y; });
+    for (int o = team.size / 2; o > 0; o >>= 1) { u += __shfl_down_sync(0xffffffffu, u, o); v += __shfl_down_sync(0xffffffffu, v, o); }
+    if (g < a.groups && team.t == 0) out[g] = make_float2(u, v);
   }
 }
 template <class T, int V, bool SAME>
@@ -537,58 +565,61 @@ __global__ void __launch_bounds__(block_limit(V)) norm_grad_short_kernel(const N
   float2* const stat = shared_red();
   float2* const red = stat + a.groups;
   const Place<T, V, SAME> at(a);
+  const Team<V, SAME> team(a);
   Grads<T, V, SAME> f;
   affine<V>(a, at.cv, f.gamma, f.beta);
   float c1[V] = {}, c2[V] = {};
   const long long step = a.lanes * a.ld_x, dstep = a.lanes * a.ld_dy, ystep = a.lanes * a.ld_y;
-  for (long long s = blockIdx.x; s < a.graphs; s += gridDim.x) {
-    long long b, e;
-    graph_rows(a, s, &b, &e, threadIdx.x == 0 ? a.status : nullptr);
-    if (e - b > 2 * a.R) {
+  const int graphs = (int)a.graphs, longest = (int)(2 * a.R < a.n ? 2 * a.R : a.n);
+  int b, len, next_b = 0, next_len = 0;
+  auto look = [&](int s) {
+    long long u, v;
+    graph_rows(a, s, &u, &v, threadIdx.x == 0 ? a.status : nullptr);
+    next_b = (int)u; next_len = (int)(v - u);
+  };
+  look(blockIdx.x);
+  for (int s = blockIdx.x; s < graphs; s += gridDim.x) {
+    b = next_b; len = next_len;
+    if (s < graphs - (int)gridDim.x) look(s + gridDim.x);
+    if (len > longest) {
       if (threadIdx.x == 0) *a.any_long = 1;
       continue;
     }
-    if (b == e) continue;
-    const int rows = at.rows(a, b, e);
-    const T *p = at.at(x, a.ld_x, b), *d = at.at(dy, a.ld_dy, b);
-    Vec<T, V> kx[grad_batch<V>()], kd[grad_batch<V>()];
-    float g1[ng<V, SAME>()] = {}, g2[ng<V, SAME>()] = {};
-    if (rows > 0) {
-      load_batch<T, V, grad_batch<V>()>(kx, p, step, rows);
-      load_batch<T, V, grad_batch<V>()>(kd, d, dstep, rows);
-      f.set(a, at, s);
-      add_grads<ACT>(f, kx, kd, rows, c1, c2, g1, g2);
-      for (int left = rows - grad_batch<V>(); left > 0; left -= grad_batch<V>()) {
-        Vec<T, V> v[grad_batch<V>()], w[grad_batch<V>()];
-        p += grad_batch<V>() * step; d += grad_batch<V>() * dstep;
-        load_batch<T, V, grad_batch<V>()>(v, p, step, left);
-        load_batch<T, V, grad_batch<V>()>(w, d, dstep, left);
+    if (len == 0) continue;
+    const int rows = at.rows(a, len);
+    constexpr int U = short_grad_batch<V>();
+    if (rows > 0) f.set(a, at, s);
+    {
+      const T *p = at.at(x, a.ld_x, b), *d = at.at(dy, a.ld_dy, b);
+      float g1[ng<V, SAME>()] = {}, g2[ng<V, SAME>()] = {};
+#pragma unroll 1
+      for (int left = rows; left > 0; left -= U) {
+        Vec<T, V> v[U], w[U];
+        load_batch<T, V, U>(v, p, step, left);
+        load_batch<T, V, U>(w, d, dstep, left);
         add_grads<ACT>(f, v, w, left, c1, c2, g1, g2);
+        p += U * step; d += U * dstep;
       }
+      put_sums(at, a, g1, g2, red);
     }
-    as_loaded(kx);
-    as_loaded(kd);
-    put_sums(at, a, g1, g2, red);
     __syncthreads();
-    sum_block<V, SAME>(a, red, stat);
+    sum_block(a, team, red, stat);
     __syncthreads();
-    if (rows > 0) {
-      const float inv = __fdividef(1.f, (float)(e - b) * (float)a.cg);
-      float m1[ng<V, SAME>()], m2[ng<V, SAME>()];
+    const float inv = __fdividef(1.f, (float)len * (float)a.cg);
+    float m1[ng<V, SAME>()] = {}, m2[ng<V, SAME>()] = {};
+    if (rows > 0)
 #pragma unroll
       for (int k = 0; k < ng<V, SAME>(); ++k) { const float2 q = stat[at.g[k]]; m1[k] = q.x * inv; m2[k] = q.y * inv; }
-      p = at.at(x, a.ld_x, b); d = at.at(dy, a.ld_dy, b);
-      T* q = dx + (b + at.r) * a.ld_y + at.cv * V;
+    const T *p = at.at(x, a.ld_x, b), *d = at.at(dy, a.ld_dy, b);
+    T* q = dx + ((long long)b + at.r) * a.ld_y + at.cv * V;
+#pragma unroll 1
+    for (int left = rows; left > 0; left -= U) {
+      Vec<T, V> v[U], w[U];
+      load_batch<T, V, U>(v, p, step, left);
+      load_batch<T, V, U>(w, d, dstep, left);
 #pragma unroll
-      for (int u = 0; u < grad_batch<V>(); ++u) if (u < rows) write_grad<ACT>(f, kx[u], kd[u], m1, m2, q + u * ystep);
-      for (int left = rows - grad_batch<V>(); left > 0; left -= grad_batch<V>()) {
-        Vec<T, V> v[grad_batch<V>()], w[grad_batch<V>()];
-        p += grad_batch<V>() * step; d += grad_batch<V>() * dstep; q += grad_batch<V>() * ystep;
-        load_batch<T, V, grad_batch<V>()>(v, p, step, left);
-        load_batch<T, V, grad_batch<V>()>(w, d, dstep, left);
-#pragma unroll
-        for (int u = 0; u < grad_batch<V>(); ++u) if (u < left) write_grad<ACT>(f, v[u], w[u], m1, m2, q + u * ystep);
-      }
+      for (int u = 0; u < U; ++u) if (u < left) write_grad<ACT>(f, v[u], w[u], m1, m2, q + u * ystep);
+      p += U * step; d += U * dstep; q += U * ystep;
     }
     __syncthreads();
   }
@@ -600,8 +631,10 @@ __global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_grad_stats_k
   __shared__ Parts parts;
   float2* const red = shared_red();
   const Place<T, V, SAME> at(a);
+  const Team<V, SAME> team(a);
   float c1[V] = {}, c2[V] = {};
-  if (*a.any_long) {
+  if (!*a.any_long) return;                                           // (its sums by channel are not read either)
+  {
     Grads<T, V, SAME> f;
     affine<V>(a, at.cv, f.gamma, f.beta);
     const long long step = a.lanes * a.ld_x, dstep = a.lanes * a.ld_dy;
@@ -621,7 +654,7 @@ __global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_grad_stats_k
         }
         put_sums(at, a, g1, g2, red);
         __syncthreads();
-        sum_block<V, SAME>(a, red, a.part + (blk * 2 + k) * a.groups);
+        sum_block(a, team, red, a.part + (blk * 2 + k) * a.groups);
         __syncthreads();
       }
     }
@@ -629,39 +662,40 @@ __global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_grad_stats_k
   if (a.chan) put_channels(at, a, c1, c2, red, a.chan + (size_t)blockIdx.x * a.C);
 }
 
-// The last blocks of a row of the grid (blockIdx.x from `combine` on; of the first one only) add up the sums by channel: a lane to a channel, the warps
-// share the blocks' sums, which are added in their order.
+// The last blocks of a row of the grid (blockIdx.x from `combine` on; of the first one only) add up the sums by channel, 8 channels a block: 32 lanes
+// of threads share the blocks' sums, which are added in their order.
 __global__ void __launch_bounds__(32 * COMBINE_WARPS) norm_grad_combine_kernel(const NormArgs a, int combine) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const bool any_long = a.blocks > 0 && *a.any_long;
   if ((int)blockIdx.x >= combine) {
-    __shared__ double2 part[COMBINE_WARPS][32];
+    __shared__ double2 part[32][9];
     if (blockIdx.y > 0) return;
-    const int c = ((int)blockIdx.x - combine) * 32 + lane, rows = a.row_grid + a.short_blocks, per = (rows + COMBINE_WARPS - 1) / COMBINE_WARPS;
+    const int ch = threadIdx.x & 7, share = threadIdx.x >> 3, c = ((int)blockIdx.x - combine) * 8 + ch;
+    const int rows = a.row_grid + a.short_blocks;
     double u = 0, v = 0;
     if (c < a.C)
 #pragma unroll 8
-      for (int i = warp * per; i < (warp + 1) * per && i < rows; ++i) { const float2 p = a.chan[(size_t)i * a.C + c]; u += p.x; v += p.y; }
-    part[warp][lane] = make_double2(u, v);
+      for (int i = (any_long ? 0 : a.row_grid) + share; i < rows; i += 32) { const float2 p = a.chan[(size_t)i * a.C + c]; u += p.x; v += p.y; }
+    part[share][ch] = make_double2(u, v);
     __syncthreads();
-    if (warp == 0 && c < a.C) {
-      for (int w = 1; w < COMBINE_WARPS; ++w) { u += part[w][lane].x; v += part[w][lane].y; }
+    if (share == 0 && c < a.C) {
+      for (int w = 1; w < 32; ++w) { u += part[w][ch].x; v += part[w][ch].y; }
       if (a.grad_gamma) a.grad_gamma[c] = (float)u;
       if (a.grad_beta) a.grad_beta[c] = (float)v;
     }
     return;
   }
-  if (!*a.any_long) return;
-  const int g = blockIdx.y * COMBINE_WARPS + warp;
-  if (g >= a.groups) return;
+  if (!any_long) return;
   for (long long blk0 = blockIdx.x; blk0 < a.blocks; blk0 += combine) {
     Owned o;
     if (!owned_graph(a, blk0, &o)) continue;
-    double u = 0, v = 0;
+    each_group(a, o, [&](int g, long long from, int stride, bool warp) {
+      double u = 0, v = 0;
 #pragma unroll 8
-    for (long long blk = o.first + lane; blk <= o.last; blk += 32) { const float2 p = part_at(a, o, blk, g); u += p.x; v += p.y; }
-    u = warp_sum(u); v = warp_sum(v);
-    const double m = (double)(o.end - o.begin) * a.cg;
-    if (lane == 0) a.sums[o.s * a.groups + g] = make_float2((float)(u / m), (float)(v / m));
+      for (long long blk = from; blk <= o.last; blk += stride) { const float2 p = part_at(a, o, blk, g); u += p.x; v += p.y; }
+      u = lane_sum(u, warp); v = lane_sum(v, warp);
+      const double m = (double)(o.end - o.begin) * a.cg;
+      if (!warp || (threadIdx.x & 31) == 0) a.sums[o.s * a.groups + g] = make_float2((float)(u / m), (float)(v / m));
+    });
   }
 }
 
@@ -710,18 +744,21 @@ __global__ void norm_no_rows_kernel(const NormArgs a) {
 // ---------------------------------------------------------------------------------------------------------------- host
 
 constexpr int DEVICE_SMS = 148, ROW_BLOCKS_PER_SM = 8, ROW_GRID_PER_SM = 8;
-// Rows of a block of rows: at least 8 192 elements, and about eight blocks to an SM.  (By the number of SMs this is built for, so
-// that a workspace's size depends on the sizes alone.)
-long long block_rows(int64_t n, int C) { return std::max<long long>(std::max(1, 8192 / C), (n + DEVICE_SMS * ROW_BLOCKS_PER_SM - 1) / (DEVICE_SMS * ROW_BLOCKS_PER_SM)); }
+// Rows of a block of rows: at least 8 192 elements, about eight blocks to an SM; where there are graphs enough to fill the device, four times the average
+// graph's: the graphs of an ordinary batch are short ones then.  (By the number of SMs this is built for, so that a workspace's size depends on the sizes alone.)
+long long block_rows(int64_t n, int64_t graphs, int C) {
+  const long long even = std::max<long long>(std::max(1, 8192 / C), (n + DEVICE_SMS * ROW_BLOCKS_PER_SM - 1) / (DEVICE_SMS * ROW_BLOCKS_PER_SM));
+  return graphs >= DEVICE_SMS * ROW_BLOCKS_PER_SM ? std::max<long long>(even, 4 * (n / graphs)) : even;
+}
 
 struct NormSpace { long long R, blocks; int short_blocks, row_grid; size_t flag, part, chan, sums, mean, rstd, bytes; };
 NormSpace norm_space(int64_t n, int64_t graphs, int C, int groups, bool grad) {
   NormSpace s;
-  s.R = block_rows(n, C);
+  s.R = block_rows(n, graphs, C);
   const bool long_ones = n > 2 * s.R;                            // else no graph can be long
   s.blocks = long_ones ? (n + s.R - 1) / s.R : 0;
   s.row_grid = (int)std::min<long long>(s.blocks, DEVICE_SMS * ROW_GRID_PER_SM);
-  s.short_blocks = (int)std::min<long long>(graphs, DEVICE_SMS * 32);
+  s.short_blocks = (int)std::min<long long>(graphs, DEVICE_SMS * 16);      // (gradients: at most)
   size_t at = 0;
   auto take = [&](size_t b) { const size_t o = at; at += (b + 255) / 256 * 256; return o; };
   s.flag = take(long_ones ? 4 : 0);
@@ -747,11 +784,13 @@ int norm_vector(int size, int width, int cg, const void* a, int64_t lda, const v
   return v;
 }
 
+// Rows that a block of about `threads` threads walks at once, a power of two, and its threads.
 void set_block(NormArgs* a, int v, int threads, int* out_threads) {
   a->vpr = a->C / v;
-  threads = std::max(threads, (a->vpr + 31) / 32 * 32);
-  a->lanes = threads / a->vpr;
-  *out_threads = threads;
+  a->shift = 0;
+  while ((2 << a->shift) * a->vpr <= threads) ++a->shift;
+  a->lanes = 1 << a->shift;
+  *out_threads = (a->lanes * a->vpr + 31) / 32 * 32;
 }
 
 // f(tag of the element type, vector length, is a vector of one group, activation) for the kernels that fit; v from norm_vector.
@@ -774,6 +813,9 @@ void with_norm_kernels(int32_t type, int v, int cg, int act, F f0) {
     });
   });
 }
+
+// Columns of the grid that joins parts: one for each eight groups where a few graphs have all the parts.
+unsigned combine_columns(long long blocks, int64_t graphs, int groups) { return blocks / graphs >= 64 ? (unsigned)((groups + COMBINE_WARPS - 1) / COMBINE_WARPS) : 1u; }
 
 // Threads for a short graph: at most `batch` vectors each for a graph of the average length.
 int short_threads(int64_t n, int64_t graphs, int vpr, int batch) {
@@ -856,14 +898,14 @@ extern "C" int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offset
       T* const yp = static_cast<T*>(out_rows);
       int threads;
       if (a.short_blocks > 0) {
-        set_block(&a, V, short_threads(n, graphs, width / V, batch<V>()), &threads);
-        const size_t smem = (size_t)a.lanes * a.vpr * ng<V, SAME>() * 8 + (size_t)groups * 8;
-        norm_short_kernel<T, V, SAME, ACT><<<a.short_blocks, threads, smem, st>>>(a, xp, yp);
+        set_block(&a, V, short_threads(n, graphs, width / V, short_vectors<V>()), &threads);
+        const size_t smem = (size_t)a.lanes * a.vpr * ng<V, SAME>() * 8 + (size_t)groups * 8 + (size_t)width * 8;
+        norm_short_kernel<T, V, SAME, ACT><<<(int)std::min<int64_t>(graphs, 1 << 20), threads, smem, st>>>(a, xp, yp);
       }
       if (s.blocks > 0) {
         set_block(&a, V, ROW_THREADS, &threads);
         norm_stats_kernel<T, V, SAME><<<s.row_grid, threads, (size_t)a.lanes * a.vpr * ng<V, SAME>() * 8, st>>>(a, xp);
-        norm_combine_kernel<<<dim3((unsigned)s.row_grid, (unsigned)((groups + COMBINE_WARPS - 1) / COMBINE_WARPS)), 32 * COMBINE_WARPS, 0, st>>>(a);
+        norm_combine_kernel<<<dim3((unsigned)s.row_grid, combine_columns(s.blocks, graphs, groups)), 32 * COMBINE_WARPS, 0, st>>>(a);
         norm_apply_kernel<T, V, SAME, ACT><<<s.row_grid, threads, (size_t)groups * 8, st>>>(a, xp, yp);
       }
     });
@@ -941,16 +983,16 @@ extern "C" int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* o
       T* const dxp = static_cast<T*>(grad_x);
       int threads;
       if (a.short_blocks > 0) {
-        set_block(&a, V, short_threads(n, graphs, width / V, grad_batch<V>()), &threads);
+        set_block(&a, V, short_threads(n, graphs, width / V, short_vectors<V>()), &threads);
         norm_grad_short_kernel<T, V, SAME, ACT><<<a.short_blocks, threads, (size_t)a.lanes * width * 8 + (size_t)groups * 8, st>>>(a, xp, dyp, dxp);
       }
       if (s.blocks > 0) {
         set_block(&a, V, ROW_THREADS, &threads);
         norm_grad_stats_kernel<T, V, SAME, ACT><<<s.row_grid, threads, (size_t)a.lanes * width * 8, st>>>(a, xp, dyp);
       }
-      const int channel_blocks = a.chan ? (width + 31) / 32 : 0;
+      const int channel_blocks = a.chan ? (width + 7) / 8 : 0;
       if (s.row_grid + channel_blocks > 0)
-        norm_grad_combine_kernel<<<dim3((unsigned)(s.row_grid + channel_blocks), (unsigned)(s.blocks > 0 ? (groups + COMBINE_WARPS - 1) / COMBINE_WARPS : 1)), 32 * COMBINE_WARPS, 0,
+        norm_grad_combine_kernel<<<dim3((unsigned)(s.row_grid + channel_blocks), s.blocks > 0 ? combine_columns(s.blocks, graphs, groups) : 1u), 32 * COMBINE_WARPS, 0,
                                    st>>>(a, s.row_grid);
       if (s.blocks > 0) norm_grad_apply_kernel<T, V, SAME, ACT><<<s.row_grid, threads, 0, st>>>(a, xp, dyp, dxp);
     });

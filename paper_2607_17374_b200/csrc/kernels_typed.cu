@@ -169,7 +169,7 @@ extern "C" int64_t taurus_typed_project_workspace(int64_t n, int32_t types, int3
 extern "C" int64_t taurus_typed_project_grad_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type) {
   if (!typed_shape_ok(n, types, d_in, d_out, type)) return TAURUS_ERR_INVALID_ARG;
   if (!typed_supported(types, d_in, d_out)) return TAURUS_ERR_UNSUPPORTED;
-  return n > FEW_ROWS ? (int64_t)(up(typed_tc_pack_bytes(types, d_in, d_out, type)) + up(typed_tc_part_bytes(n, d_in, d_out, type))) : 0;
+  return n > FEW_ROWS ? (int64_t)(up(typed_tc_pack_bytes(types, d_in, d_out, type)) + up(typed_tc_part_bytes(n, types, d_in, d_out, type))) : 0;
 }
 
 extern "C" int taurus_typed_project(int64_t n, int32_t types, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, const void* W,

@@ -8,8 +8,9 @@
 // typed_join_kernel adds up in their order).  Which units there are follows from the offsets in device memory: every CTA works it out for itself.
 // Roles:  warp 0       TMA: operands that stand in memory as the tensor core takes them
 //         warp 1       tcgen05.mma, accumulators in TMEM, two slots of 256 columns: the epilogue of a unit runs beside the products of the next
-//         warps 2..5   epilogue: TMEM -> registers -> transposed through shared memory -> rows
-//         warps 6..13  loaders (LOADED): operands that have to be split, or whose rows TMA cannot address
+//         warps 2..9   epilogue, two to a quadrant of TMEM lanes: TMEM -> registers -> transposed through shared memory -> rows
+//         warps 10..17 loaders (LOADED): operands that have to be split, or whose rows TMA cannot address; without loaders, in GRAD_W, they add up the
+//                      columns of grad_out for the bias, which the loaders do on the way
 //
 // fp32 operands: x = hi + mid + lo, three bf16 values that hold its 24 bits (hi by truncation, so that nothing overflows), and six of the nine
 // products: hi hi into one accumulator, hi mid + mid hi + mid mid + hi lo + lo hi into another.  What is left out is below 2^-24 of a product.
@@ -29,24 +30,30 @@ namespace {
 
 enum { PROJECT = 0, GRAD_X = 1, GRAD_W = 2 };
 
-constexpr int BM = 128, STAGES = 4, MAX_G = TAURUS_MAX_TYPES;
-constexpr int STAGE_BYTES = 48 * 1024;
-constexpr int OPERAND_BYTES = STAGES * STAGE_BYTES;
-constexpr int EPI_WARPS = 4, LOAD_WARPS = 8, LOADERS = 32 * LOAD_WARPS;
-constexpr int EPI_TILE_BYTES = 32 * 128;              // 32 rows x 32 fp32
+constexpr int BM = 128, MAX_STAGES = 4, MAX_G = TAURUS_MAX_TYPES;
+constexpr int STAGE_BYTES = 48 * 1024;                // operands of a stage
+constexpr int OPERAND_BYTES = MAX_STAGES * STAGE_BYTES;
+constexpr int EPI_WARPS = 8, LOAD_WARPS = 8, LOADERS = 32 * LOAD_WARPS;
+constexpr int EPI_TILE_BYTES = 32 * 64;               // 32 rows x 64 bytes
 constexpr unsigned WAIT_LIMIT = 1u << 24;
 
 template <class T> constexpr int planes_of() { return sizeof(T) == 4 ? 3 : 1; }
 template <class T> constexpr int block_k() { return sizeof(T) == 4 ? 32 : 64; }                   // columns (rows) of a stage
 template <class T, bool LOADED> constexpr int block_n() { return LOADED ? 128 : 256; }
+// fp32: half of the operands' shared memory is a ring of rows as they were read, which the loaders fill far ahead of the tensor core: with the rows of one
+// stage in registers instead, each stage took as long as a read of memory.
+template <class T> constexpr int stages_of() { return sizeof(T) == 4 ? 2 : MAX_STAGES; }
+template <int KIND> constexpr int raw_bytes() { return (KIND == GRAD_W ? 2 : 1) * BM * 32 * 4; }
+template <int KIND> constexpr int raw_depth() { return (OPERAND_BYTES - 2 * STAGE_BYTES) / raw_bytes<KIND>(); }
 
-struct Shared {
-  unsigned long long full[STAGES], empty[STAGES], acc_full[2], acc_empty[2];
+struct __align__(16) Shared {
+  unsigned long long full[MAX_STAGES], empty[MAX_STAGES], acc_full[2], acc_empty[2], sums;
   unsigned tmem_base;
   int abort_flag, loads, mmas;
   int begin[MAX_G + 1];       // rows of type g: [begin[g], begin[g + 1]) (the types' rows follow one another)
   int prefix[MAX_G + 1];      // units (row tiles, chunks) in front of type g
   int slot[MAX_G + 1];        // GRAD_W: partial products in front of type g
+  __align__(16) float bias[LOAD_WARPS * 128];   // (read and written four at a time) GRAD_W: sums of grad_out's columns, of each loader warp or of the second half of those who add
 };
 constexpr int SHARED_BYTES = OPERAND_BYTES + EPI_WARPS * EPI_TILE_BYTES + (int)sizeof(Shared);
 static_assert(SHARED_BYTES <= 227 * 1024, "shared memory of a block");
@@ -64,8 +71,10 @@ struct TcArgs {
   void* out;
   long long ld_out;           // PROJECT, GRAD_X
   int out_f32;                // the output is fp32, else of the operands' type
-  int out_vec;                // four columns at a time
+  int out_vec;                // 16 bytes of columns at a time
   const float* bias;
+  int bias_vec;
+  float* db;                  // GRAD_W: gradient of the bias
   float* part;                // GRAD_W: [slots x (M + 1) x N]
   int32_t* status;
 };
@@ -124,20 +133,26 @@ __device__ __forceinline__ void umma(unsigned d, unsigned long long a, unsigned 
 __device__ __forceinline__ void umma_commit(unsigned long long* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-// 32 columns of an accumulator, one row per lane.
-__device__ __forceinline__ void tmem_ld32(unsigned (&v)[32], unsigned taddr) {
+// 16 columns of an accumulator, one row per lane.
+__device__ __forceinline__ void tmem_ld16(unsigned (&v)[16], unsigned taddr) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
-        "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
-        "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
       : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// 16 or 4 bytes from global to shared memory, of which the first `bytes` are read and the others zeros.
+__device__ __forceinline__ void copy16(unsigned dst, const void* src, unsigned bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy4(unsigned dst, const void* src, unsigned bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // ---------------------------------------------------------------------------------------------------------------- units
@@ -201,7 +216,7 @@ __device__ __forceinline__ Unit unit_at(const TcArgs& a, const Shared* s, int w)
 
 // ---------------------------------------------------------------------------------------------------------------- loaders
 // Four neighbouring elements of a row as bf16 planes (fp32) or as they are (16 bits), 8 bytes a plane.
-template <class T> struct Quad { T v[4]; };
+template <class T> struct __align__(sizeof(T) * 4) Quad { T v[4]; };
 
 template <class T>
 __device__ __forceinline__ Quad<T> load_quad(const T* row, int c, int limit, bool vec) {     // row null: zeros
@@ -237,60 +252,146 @@ __device__ __forceinline__ void store_quad(unsigned addr, unsigned plane_bytes, 
   }
 }
 
-// What a loader thread brings of one stage.
+// What a loader thread brings of one stage: its quads of A, and in GRAD_W of B.  place(i): row and column (in quads) of quad i of an operand.
 template <class T, int KIND>
 struct Loader {
   static constexpr int BK = block_k<T>(), QUADS_A = BM * BK / 4 / LOADERS, QUADS_B = KIND == GRAD_W ? QUADS_A : 0;
-  Quad<T> q[QUADS_A + QUADS_B];
+  static constexpr int ROW_QUADS = KIND == GRAD_W ? 32 : BK / 4;      // quads of a row of the tile
+  static __device__ __forceinline__ int row_of(int i, int t) { return (t + i * LOADERS) / ROW_QUADS; }
+  static __device__ __forceinline__ int quad_of(int t) { return t % ROW_QUADS; }      // (the same for every i: LOADERS is a multiple of ROW_QUADS)
 
-  __device__ __forceinline__ void load(const TcArgs& a, const Unit& u, int step, int t) {
-    if constexpr (KIND != GRAD_W) {          // rows of 128-row tile, BK columns
+  // f(i, row or null, column, columns, is A): for each quad, where it comes from
+  template <class F>
+  static __device__ __forceinline__ void each(const TcArgs& a, const Unit& u, int step, int t, F f) {
+    const int q = quad_of(t) * 4;
 #pragma unroll
-      for (int i = 0; i < QUADS_A; ++i) {
-        const int at = t + i * LOADERS, r = at / (BK / 4), c = step * BK + at % (BK / 4) * 4;
-        const T* const row = r < u.rows ? static_cast<const T*>(a.a) + (u.row0 + (long long)r) * a.lda : nullptr;
-        q[i] = load_quad(row, c, a.Kc, a.a_vec);
-      }
-    } else {                                 // BK rows, 128 columns of either operand
-#pragma unroll
-      for (int i = 0; i < QUADS_A; ++i) {
-        const int at = t + i * LOADERS, r = at / 32, c = at % 32 * 4;
+    for (int i = 0; i < QUADS_A; ++i) {
+      const int r = row_of(i, t);
+      if constexpr (KIND != GRAD_W) {
+        f(i, r < u.rows ? static_cast<const T*>(a.a) + (u.row0 + (long long)r) * a.lda : nullptr, step * BK + q, a.Kc, true);
+      } else {
         const bool in = step * BK + r < u.rows;
         const long long row = u.row0 + (long long)step * BK + r;
-        q[i] = load_quad(in ? static_cast<const T*>(a.a) + row * a.lda : nullptr, u.m0 + c, a.M, a.a_vec);
-        q[QUADS_A + i] = load_quad(in && c < u.bw ? static_cast<const T*>(a.b) + row * a.ldb : nullptr, u.n0 + c, a.N, a.b_vec);
+        f(i, in && a.a ? static_cast<const T*>(a.a) + row * a.lda : nullptr, u.m0 + q, a.M, true);
+        f(QUADS_A + i, in && q < u.bw ? static_cast<const T*>(a.b) + row * a.ldb : nullptr, u.n0 + q, a.N, false);
       }
     }
   }
-  __device__ __forceinline__ void store(unsigned stage, int t) const {
+  // 16 bits: into registers
+  static __device__ __forceinline__ void load(Quad<T> (&v)[QUADS_A + QUADS_B], const TcArgs& a, const Unit& u, int step, int t) {
+    each(a, u, step, t, [&](int i, const T* row, int c, int limit, bool is_a) { v[i] = load_quad(row, c, limit, is_a ? a.a_vec : a.b_vec); });
+  }
+  // fp32: into this thread's places of a slot of the ring
+  static __device__ __forceinline__ unsigned raw_at(unsigned slot, int i, int t) { return slot + (i * LOADERS + t) * 16; }
+  static __device__ __forceinline__ void copy(unsigned slot, const TcArgs& a, const Unit& u, int step, int t) {
+    each(a, u, step, t, [&](int i, const T* row, int c, int limit, bool is_a) {
+      const unsigned dst = raw_at(slot, i, t);
+      const int left = row ? min(max(limit - c, 0), 4) : 0;
+      const void* const any = a.offsets;                              // (an address for a copy that reads nothing)
+      if (is_a ? a.a_vec : a.b_vec) {
+        copy16(dst, left > 0 ? static_cast<const void*>(row + c) : any, left * 4);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) copy4(dst + 4 * j, j < left ? static_cast<const void*>(row + c + j) : any, j < left ? 4 : 0);
+      }
+    });
+  }
+  static __device__ __forceinline__ Quad<T> raw(unsigned slot, int i, int t) {
+    Quad<T> q;
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(raw_at(slot, i, t)) : "memory");
+    *reinterpret_cast<float4*>(&q) = v;
+    return q;
+  }
+  // Quad i into its operand's planes.
+  static __device__ __forceinline__ void store(unsigned stage, int i, int t, const Quad<T>& q) {
     constexpr unsigned PLANE = BM * BK * 2;  // bytes of a plane of either operand (blocks of 128 columns)
+    const int r = row_of(i % QUADS_A, t), c = quad_of(t);
     if constexpr (KIND != GRAD_W) {
-#pragma unroll
-      for (int i = 0; i < QUADS_A; ++i) {
-        const int at = t + i * LOADERS, r = at / (BK / 4), c = at % (BK / 4);
-        const int chunk = BK == 64 ? (c >> 1) ^ (r & 7) : (c >> 1) ^ ((r >> 1) & 3);
-        store_quad<T>(stage + r * (BK * 2) + chunk * 16 + (c & 1) * 8, PLANE, q[i]);
-      }
+      const int chunk = BK == 64 ? (c >> 1) ^ (r & 7) : (c >> 1) ^ ((r >> 1) & 3);
+      store_quad<T>(stage + r * (BK * 2) + chunk * 16 + (c & 1) * 8, PLANE, q);
     } else {
-#pragma unroll
-      for (int i = 0; i < QUADS_A; ++i) {
-        const int at = t + i * LOADERS, r = at / 32, c = at % 32;      // quad c: block of 64 columns c / 16
-        const unsigned off = (c >> 4) * (BK * 128) + r * 128 + ((((c & 15) >> 1) ^ (r & 7)) << 4) + (c & 1) * 8;
-        store_quad<T>(stage + off, PLANE, q[i]);
-        store_quad<T>(stage + planes_of<T>() * PLANE + off, PLANE, q[QUADS_A + i]);
-      }
+      // quad c lies in the block of 64 columns c / 16
+      const unsigned off = (c >> 4) * (BK * 128) + r * 128 + ((((c & 15) >> 1) ^ (r & 7)) << 4) + (c & 1) * 8;
+      store_quad<T>(stage + (i < QUADS_A ? 0 : planes_of<T>() * PLANE) + off, PLANE, q);
     }
   }
 };
 
+// The places of a CTA's stages, in order: unit after unit, step after step.
+template <int KIND, int BK>
+struct Walk {
+  int w, k;
+  Unit u;
+  __device__ __forceinline__ Walk(const TcArgs& a, const Shared* s, int units) : w(blockIdx.x), k(0) { find(a, s, units); }
+  __device__ __forceinline__ void find(const TcArgs& a, const Shared* s, int units) {
+    for (; w < units; w += gridDim.x) { u = unit_at<KIND, BK>(a, s, w); if (u.steps > 0) return; }
+  }
+  __device__ __forceinline__ bool last() const { return k + 1 == u.steps; }
+  __device__ __forceinline__ void next(const TcArgs& a, const Shared* s, int units) {
+    if (++k == u.steps) { k = 0; w += gridDim.x; find(a, s, units); }
+  }
+};
+
+// All loader warps meet (a bounded wait, as every other): false when the CTA is aborting.
+__device__ __forceinline__ bool meet(Shared* s, unsigned* phase) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(&s->sums);
+  const bool ok = mbar_wait_warp(&s->sums, *phase, &s->abort_flag);
+  *phase ^= 1;
+  return ok;
+}
+// Where the sums of grad_out's columns of a unit go.
+__device__ __forceinline__ float* bias_place(const TcArgs& a, const Unit& u) {
+  return u.slot >= 0 ? a.part + ((long long)u.slot * (a.M + 1) + a.M) * a.N + u.n0 : a.db + (long long)u.g * a.N + u.n0;
+}
+
+// ---------------------------------------------------------------------------------------------------------------- epilogue
+// PASS columns (64 bytes of the output) of 32 rows: transposed through the warp's tile, 16-byte chunk c of row r at chunk c ^ ((r >> 1) & 3), and written
+// eight rows at a time in pieces of 64 bytes; out: row 0, column 0 of them; rows <= 32.
+template <class O>
+__device__ __forceinline__ void put_rows(unsigned char* tile, const float* v, O* out, long long ld, int rows, int columns, bool vec) {
+  constexpr int PASS = 64 / sizeof(O), PER = 16 / sizeof(O);
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    Vec<O, PER> x;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) x.v[j] = from_f32<O>(v[c * PER + j]);
+    store_vec(tile + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), x);
+  }
+  __syncwarp();
+  if (vec && columns >= PASS) {
+    const int c = lane & 3;
+    O* p = out + (lane >> 2) * ld + c * PER;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = i * 8 + (lane >> 2);
+      if (r < rows) store_vec(p, load_vec<Vec<O, PER>>(tile + r * 64 + ((c ^ ((r >> 1) & 3)) << 4)));
+      p += 8 * ld;
+    }
+  } else {
+    constexpr int AT_ONCE = 32 / PASS;                 // rows
+    const int c = lane % PASS;
+    for (int r = lane / PASS; r < rows; r += AT_ONCE)
+      if (c < columns) out[r * ld + c] = *reinterpret_cast<const O*>(tile + r * 64 + (((c / PER) ^ ((r >> 1) & 3)) << 4) + c % PER * sizeof(O));
+  }
+  __syncwarp();
+}
+
 // ---------------------------------------------------------------------------------------------------------------- kernel
+// Loaders, or in GRAD_W those who add up the columns of grad_out.
+template <int KIND, bool LOADED> constexpr int threads_of() { return 32 * (2 + EPI_WARPS + (LOADED || KIND == GRAD_W ? LOAD_WARPS : 0)); }
+
 template <class T, int KIND, bool LOADED>
-__global__ void __launch_bounds__(32 * (2 + EPI_WARPS + (LOADED ? LOAD_WARPS : 0)), 1)
+__global__ void __launch_bounds__(threads_of<KIND, LOADED>(), 1)
 typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ TcArgs a) {
   static_assert(LOADED || sizeof(T) == 2, "fp32 operands are split by the loaders");
-  constexpr int NP = planes_of<T>(), BK = block_k<T>(), BN = block_n<T, LOADED>(), ROW = BK * 2;
+  constexpr int NP = planes_of<T>(), BK = block_k<T>(), BN = block_n<T, LOADED>(), ROW = BK * 2, STAGES = stages_of<T>();
+  constexpr bool SUMS = KIND == GRAD_W && !LOADED;       // the last warps read the stages too
   constexpr unsigned PLANE_A = BM * BK * 2, PLANE_B = BN * BK * 2;
   static_assert(NP * (PLANE_A + PLANE_B) <= (unsigned)STAGE_BYTES, "a stage's operands");
+  static_assert(sizeof(T) == 2 || raw_depth<KIND>() >= 2, "the ring");
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* const staging = smem + OPERAND_BYTES;
   Shared* const sh = reinterpret_cast<Shared*>(staging + EPI_WARPS * EPI_TILE_BYTES);
@@ -308,8 +409,9 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   if ((int)blockIdx.x >= units) return;
   constexpr bool TMA_A = !LOADED, TMA_B = !LOADED || KIND != GRAD_W;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) { mbar_init(&sh->full[s], (TMA_A || TMA_B ? 1 : 0) + (LOADED ? LOAD_WARPS : 0)); mbar_init(&sh->empty[s], 1); }
+    for (int s = 0; s < STAGES; ++s) { mbar_init(&sh->full[s], (TMA_A || TMA_B ? 1 : 0) + (LOADED ? LOAD_WARPS : 0)); mbar_init(&sh->empty[s], 1 + (SUMS ? LOAD_WARPS : 0)); }
     for (int b = 0; b < 2; ++b) { mbar_init(&sh->acc_full[b], 1); mbar_init(&sh->acc_empty[b], EPI_WARPS); }
+    mbar_init(&sh->sums, LOAD_WARPS);
     sh->abort_flag = 0; sh->loads = 0; sh->mmas = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -336,10 +438,10 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           if (it >= STAGES && !mbar_wait(&sh->empty[s], (it / STAGES & 1) ^ 1, abort_flag)) { ok = false; break; }
           const unsigned st = operands + s * STAGE_BYTES, sb = st + NP * PLANE_A;
           unsigned long long* const bar = &sh->full[s];
-          const unsigned bytes_a = TMA_A ? PLANE_A : 0;
+          const unsigned bytes_a = TMA_A && (KIND != GRAD_W || a.out) ? PLANE_A : 0;      // (no grad_W: only the columns of grad_out count)
           const unsigned bytes_b = KIND == GRAD_X ? NP * a.bn * ROW : NP * boxes_n * (BK * 128);
           mbar_expect_tx(bar, bytes_a + bytes_b);
-          if (TMA_A) {
+          if (bytes_a) {
             if (KIND == GRAD_W) {
               tma_2d(st, &map_a, u.m0, u.row0 + k * BK, bar);
               tma_2d(st + BK * 128, &map_a, u.m0 + 64, u.row0 + k * BK, bar);      // (behind the last column: zeros)
@@ -423,84 +525,75 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     }
     if (lane == 0) sh->mmas = it;
   } else if (warp < 2 + EPI_WARPS) {
-    // ------------------------------------------------------------ epilogue: TMEM lanes 32 (warp % 4) ..
-    const int q = warp & 3;
-    unsigned char* const tile = staging + (warp - 2) * EPI_TILE_BYTES;      // 16-byte chunk c of row r at chunk c ^ (r & 7)
+    // ------------------------------------------------------------ epilogue: TMEM lanes 32 (warp % 4) .., the two warps of a quadrant take turns
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    unsigned char* const tile = staging + (warp - 2) * EPI_TILE_BYTES;
     int nth = 0;
     for (int w = blockIdx.x; w < units; w += gridDim.x) {
       const Unit u = unit_at<KIND, BK>(a, sh, w);
       const int buf = nth & 1;
+      const bool part = KIND == GRAD_W && u.slot >= 0;
+      const bool f32 = part || a.out_f32;
+      const long long ld = KIND == GRAD_W ? a.N : a.ld_out;
+      const int rows = min(32, (KIND == GRAD_W ? a.M - u.m0 : u.rows) - q * 32), columns = min(u.bw, a.N - u.n0);
+      const long long first = (KIND == GRAD_W ? ((long long)(part ? u.slot : u.g) * (part ? a.M + 1 : a.M) + u.m0 + q * 32) * ld : (u.row0 + q * 32ll) * ld) + u.n0;
+      const float* const bias = KIND == PROJECT && a.bias ? a.bias + (long long)u.g * a.N + u.n0 : nullptr;
       if (u.steps > 0) {
         if (!mbar_wait_warp(&sh->acc_full[buf], nth >> 1 & 1, abort_flag)) break;
         ++nth;
         tc_fence_after();
       }
-      const int rows = KIND == GRAD_W ? min(BM, a.M - u.m0) : u.rows, columns = min(u.bw, a.N - u.n0);
-      const int row_of_warp = q * 32;
-      const bool part = KIND == GRAD_W && u.slot >= 0;
-      const bool f32 = part || a.out_f32;
-      const long long ld = KIND == GRAD_W ? a.N : a.ld_out;
-      const long long first = KIND == GRAD_W ? ((long long)(part ? u.slot : u.g) * (part ? a.M + 1 : a.M) + u.m0) * a.N + u.n0 : u.row0 * ld + u.n0;
-      for (int c0 = 0; c0 < columns; c0 += 32) {
-        float o[32];
-        if (u.steps > 0) {
-          const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + buf * 256 + c0;
-          unsigned v[32];
-          tmem_ld32(v, at);
-          if constexpr (NP == 3) {
-            unsigned v2[32];
-            tmem_ld32(v2, at + 128);
-            tmem_wait();
+      if (KIND == GRAD_W && u.steps == 0 && a.db && u.m0 == 0 && warp == 2)                  // no rows: no loader passes here
+        for (int c = lane; c < columns; c += 32) bias_place(a, u)[c] = 0.f;
+      if (rows > 0 && (KIND != GRAD_W || a.out)) {
+#pragma unroll 1
+        for (int c0 = half * 32; c0 < columns; c0 += 64) {
+          float o[32];
+          if (u.steps > 0) {
+            const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + buf * 256 + c0;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float x = __uint_as_float(v[j]), y = x + __uint_as_float(v2[j]);
-              o[j] = (v[j] & 0x7F800000u) == 0x7F800000u ? x : y;
+            for (int h = 0; h < 2; ++h) {
+              unsigned v[16];
+              tmem_ld16(v, at + h * 16);
+              if constexpr (NP == 3) {
+                unsigned v2[16];
+                tmem_ld16(v2, at + 128 + h * 16);
+                tmem_wait();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                  const float x = __uint_as_float(v[j]), y = x + __uint_as_float(v2[j]);
+                  o[h * 16 + j] = (v[j] & 0x7F800000u) == 0x7F800000u ? x : y;
+                }
+              } else {
+                tmem_wait();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[h * 16 + j] = __uint_as_float(v[j]);
+              }
             }
           } else {
-            tmem_wait();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = __uint_as_float(v[j]);
+            for (int j = 0; j < 32; ++j) o[j] = 0.f;
           }
-        } else {
+          if (KIND == PROJECT && bias) {
+            if (a.bias_vec && c0 + 32 <= columns) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) o[j] = 0.f;
-        }
+              for (int j = 0; j < 32; j += 4) {
+                const float4 b = __ldg(reinterpret_cast<const float4*>(bias + c0 + j));
+                o[j] += b.x; o[j + 1] += b.y; o[j + 2] += b.z; o[j + 3] += b.w;
+              }
+            } else {
 #pragma unroll
-        for (int j = 0; j < 32; j += 4)
-          *reinterpret_cast<float4*>(tile + lane * 128 + (((j >> 2) ^ (lane & 7)) << 4)) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
-        __syncwarp();
-        const int ch = lane & 7, c = c0 + ch * 4;
-        float4 add = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (KIND == PROJECT && a.bias) {
-          const float* const b = a.bias + (long long)u.g * a.N + u.n0;
-          if (c < columns) add.x = b[c];
-          if (c + 1 < columns) add.y = b[c + 1];
-          if (c + 2 < columns) add.z = b[c + 2];
-          if (c + 3 < columns) add.w = b[c + 3];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int rr = i * 4 + (lane >> 3), row = row_of_warp + rr;
-          float4 y = *reinterpret_cast<const float4*>(tile + rr * 128 + ((ch ^ (rr & 7)) << 4));
-          if (row >= rows || c >= columns) continue;
-          if (KIND == PROJECT) { y.x += add.x; y.y += add.y; y.z += add.z; y.w += add.w; }
-          const long long at = first + row * ld + c;
-          const float e[4] = {y.x, y.y, y.z, y.w};
+              for (int j = 0; j < 32; ++j) if (c0 + j < columns) o[j] += __ldg(bias + c0 + j);
+            }
+          }
           if (f32) {
-            float* const p = (part ? a.part : static_cast<float*>(a.out)) + at;
-            if (a.out_vec && c + 4 <= columns) *reinterpret_cast<float4*>(p) = y;
-            else
-#pragma unroll
-              for (int j = 0; j < 4; ++j) if (c + j < columns) p[j] = e[j];
+            float* const p = (part ? a.part : static_cast<float*>(a.out)) + first + c0;
+            put_rows<float>(tile, o, p, ld, rows, columns - c0, a.out_vec);
+            if (columns - c0 > 16) put_rows<float>(tile, o + 16, p + 16, ld, rows, columns - c0 - 16, a.out_vec);
           } else {
-            T* const p = static_cast<T*>(a.out) + at;
-            if (a.out_vec && c + 4 <= columns) store_f32<T, 4>(p, e);
-            else
-#pragma unroll
-              for (int j = 0; j < 4; ++j) if (c + j < columns) p[j] = from_f32<T>(e[j]);
+            put_rows<T>(tile, o, static_cast<T*>(a.out) + first + c0, ld, rows, columns - c0, a.out_vec);
           }
         }
-        __syncwarp();
       }
       if (u.steps > 0) {
         tc_fence_before();
@@ -509,27 +602,127 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       }
     }
   } else if constexpr (LOADED) {
-    // ------------------------------------------------------------ loaders: the rows of the next stage are on their way while one is stored
+    // ------------------------------------------------------------ loaders
+    using L = Loader<T, KIND>;
     const int t = threadIdx.x - 32 * (2 + EPI_WARPS);
-    Loader<T, KIND> cur, next;
-    int it = 0, w = blockIdx.x, k = 0;
-    Unit u = {};
-    auto skip_empty = [&] { while (w < units) { u = unit_at<KIND, BK>(a, sh, w); if (u.steps > 0) break; w += gridDim.x; } };
-    skip_empty();
-    if (w < units) cur.load(a, u, 0, t);
-    while (w < units) {
-      if (++k == u.steps) { k = 0; w += gridDim.x; skip_empty(); }
-      if (w < units) next.load(a, u, k, t);
-      const int s = it % STAGES;
-      if (it >= STAGES && !mbar_wait_warp(&sh->empty[s], (it / STAGES & 1) ^ 1, abort_flag)) break;
-      cur.store(operands + s * STAGE_BYTES, t);
+    float sum[4] = {};                                  // GRAD_W: of this thread's four columns of grad_out
+    int it = 0;
+    Walk<KIND, BK> at(a, sh, units);
+    auto arrive = [&](int s) {
       async_fence();                                    // for the tensor core to see
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->full[s]);
-      cur = next;
-      ++it;
+    };
+    auto add = [&](const Quad<T>& q) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[j] += to_f32<T>(q.v[j]);
+    };
+    // The unit's sums: those of the eight warps' rows, added in the warps' order.
+    unsigned phase = 0;
+    auto bias_sums = [&]() -> bool {
+      if (KIND != GRAD_W || !a.db || at.u.m0 != 0 || !at.last()) return true;
+      const int me = warp - 2 - EPI_WARPS, c = L::quad_of(t) * 4, columns = min(at.u.bw, a.N - at.u.n0);
+      *reinterpret_cast<float4*>(sh->bias + me * 128 + c) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+      if (!meet(sh, &phase)) return false;
+      if (me == 0) {
+        float* const place = bias_place(a, at.u);
+        for (int w = 1; w < LOAD_WARPS; ++w) {
+          const float4 o = *reinterpret_cast<const float4*>(sh->bias + w * 128 + c);
+          sum[0] += o.x; sum[1] += o.y; sum[2] += o.z; sum[3] += o.w;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (c + j < columns) place[c + j] = sum[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[j] = 0.f;
+      return meet(sh, &phase);
+    };
+    if constexpr (NP == 3) {
+      // the ring is filled DEPTH stages ahead
+      constexpr int DEPTH = raw_depth<KIND>();
+      const unsigned ring = operands + STAGES * STAGE_BYTES;
+      Walk<KIND, BK> ahead = at;
+      for (int d = 0; d < DEPTH; ++d) {
+        if (ahead.w < units) { L::copy(ring + d * raw_bytes<KIND>(), a, ahead.u, ahead.k, t); ahead.next(a, sh, units); }
+        copy_commit();
+      }
+      for (; at.w < units; ++it) {
+        const int s = it % STAGES;
+        const unsigned slot = ring + it % DEPTH * raw_bytes<KIND>(), stage = operands + s * STAGE_BYTES;
+        copy_wait<DEPTH - 1>();                         // (a thread reads only what it copied itself)
+        if (it >= STAGES && !mbar_wait_warp(&sh->empty[s], (it / STAGES & 1) ^ 1, abort_flag)) break;
+#pragma unroll
+        for (int i = 0; i < L::QUADS_A + L::QUADS_B; ++i) {
+          const Quad<T> q = L::raw(slot, i, t);
+          if (KIND == GRAD_W && i >= L::QUADS_A) add(q);
+          L::store(stage, i, t, q);
+        }
+        arrive(s);
+        if (ahead.w < units) { L::copy(slot, a, ahead.u, ahead.k, t); ahead.next(a, sh, units); }
+        copy_commit();
+        if (!bias_sums()) break;
+        at.next(a, sh, units);
+      }
+      copy_wait<0>();
+    } else {
+      // the rows of the next stage are on their way while one is stored
+      Quad<T> cur[L::QUADS_A + L::QUADS_B], next[L::QUADS_A + L::QUADS_B];
+      Walk<KIND, BK> ahead = at;
+      if (at.w < units) L::load(cur, a, at.u, 0, t);
+      for (; at.w < units; ++it) {
+        ahead.next(a, sh, units);
+        if (ahead.w < units) L::load(next, a, ahead.u, ahead.k, t);
+        const int s = it % STAGES;
+        if (it >= STAGES && !mbar_wait_warp(&sh->empty[s], (it / STAGES & 1) ^ 1, abort_flag)) break;
+#pragma unroll
+        for (int i = 0; i < L::QUADS_A + L::QUADS_B; ++i) {
+          if (KIND == GRAD_W && i >= L::QUADS_A) add(cur[i]);
+          L::store(operands + s * STAGE_BYTES, i, t, cur[i]);
+          cur[i] = next[i];
+        }
+        arrive(s);
+        if (!bias_sums()) break;
+        at.next(a, sh, units);
+      }
     }
     if (t == 0 && !TMA_B) sh->loads = it;
+  } else if constexpr (SUMS) {
+    // ------------------------------------------------------------ columns of grad_out: a thread to two columns, the halves of the block to half of the rows each
+    const int t = threadIdx.x - 32 * (2 + EPI_WARPS), half = t >> 7, c = (t & 127) * 2;
+    float s0 = 0.f, s1 = 0.f;
+    unsigned phase = 0;
+    int it = 0;
+    for (Walk<KIND, BK> at(a, sh, units); at.w < units; ++it) {
+      const int s = it % STAGES;
+      if (!mbar_wait_warp(&sh->full[s], it / STAGES & 1, abort_flag)) break;
+      const bool mine = a.db && at.u.m0 == 0;
+      if (mine && c < at.u.bw) {
+        const unsigned sb = operands + s * STAGE_BYTES + NP * PLANE_A + (c >> 6) * (BK * 128), byte = (c & 63) * 2;
+        const int rows = min(BK, at.u.rows - at.k * BK), r1 = min(rows, (half + 1) * (BK / 2));
+#pragma unroll 8
+        for (int r = half * (BK / 2); r < r1; ++r) {
+          unsigned v;
+          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(sb + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15)) : "memory");
+          const Vec<T, 2> p = *reinterpret_cast<const Vec<T, 2>*>(&v);
+          s0 += to_f32<T>(p.v[0]); s1 += to_f32<T>(p.v[1]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh->empty[s]);
+      if (mine && at.last()) {
+        if (half == 1) { sh->bias[c] = s0; sh->bias[c + 1] = s1; }
+        if (!meet(sh, &phase)) break;
+        if (half == 0) {
+          float* const place = bias_place(a, at.u);
+          const int columns = min(at.u.bw, a.N - at.u.n0);
+          if (c < columns) place[c] = s0 + sh->bias[c];
+          if (c + 1 < columns) place[c + 1] = s1 + sh->bias[c + 1];
+        }
+        if (!meet(sh, &phase)) break;
+        s0 = s1 = 0.f;
+      }
+      at.next(a, sh, units);
+    }
   }
 
   // -------------------------------------------------------------- teardown
@@ -572,7 +765,7 @@ __global__ void __launch_bounds__(256) typed_pack_kernel(const T* __restrict__ W
   }
 }
 
-// ---------------------------------------------------------------------------------------------------------------- gradient of the bias, joins
+// ---------------------------------------------------------------------------------------------------------------- joins
 struct JoinArgs {
   long long n;
   const long long* offsets;
@@ -603,47 +796,13 @@ __device__ __forceinline__ bool offsets_bad(const long long* offsets, int types,
   return __syncthreads_or(bad);
 }
 
-// Column sums of grad_out over a chunk: a block to a chunk and 32 columns.  Grid (blocks of columns, chunks at most, by stride).
-template <class T>
-__global__ void __launch_bounds__(256) typed_bias_kernel(const JoinArgs a, const T* __restrict__ dy, long long ld, float* __restrict__ part, int32_t* status) {
-  __shared__ float red[8][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-  if (offsets_bad(a.offsets, a.types, a.n)) { if (threadIdx.x == 0) rows_status(status, TAURUS_ERR_INVALID_ARG); return; }
-  int unit = 0, slots = 0;                                  // of the types so far
-  for (int g = 0; g < a.types; ++g) {
-    const long long b = a.offsets[g], e = a.offsets[g + 1];
-    const int chunks = max(1, (int)((e - b + a.chunk - 1) / a.chunk));
-    // the chunks of this type that are this block's: unit + i = blockIdx.y modulo gridDim.y
-    int i = (int)blockIdx.y - unit % (int)gridDim.y;
-    if (i < 0) i += gridDim.y;
-    for (; i < chunks; i += gridDim.y) {
-      const long long rb = b + (long long)i * a.chunk, re = min(rb + a.chunk, e);
-      float s = 0.f;
-      if (c < a.N)
-#pragma unroll 8
-        for (long long r = rb + warp; r < re; r += 8) s += to_f32<T>(dy[r * ld + c]);
-      red[warp][lane] = s;
-      __syncthreads();
-      if (warp == 0 && c < a.N) {
-        for (int w = 1; w < 8; ++w) s += red[w][lane];
-        if (chunks > 1) part[((long long)(slots + i) * (a.K + 1) + a.K) * a.N + c] = s;
-        else a.db[(long long)g * a.N + c] = s;
-      }
-      __syncthreads();
-    }
-    unit += chunks;
-    slots += chunks > 1 ? chunks : 0;
-  }
-}
-
 // The partial results of the types of several chunks, added in the chunks' order.  Grid (elements by stride, types).
 template <class O>
 __global__ void __launch_bounds__(256) typed_join_kernel(const JoinArgs a) {
-  if (offsets_bad(a.offsets, a.types, a.n)) return;
   const int g = blockIdx.y;
+  if (a.offsets[g + 1] - a.offsets[g] <= a.chunk || offsets_bad(a.offsets, a.types, a.n)) return;
   int first;
   const int chunks = chunks_of(a, g, &first);
-  if (chunks <= 1) return;
   const long long size = (long long)(a.K + 1) * a.N;
   const long long from = a.dW ? 0 : (long long)a.K * a.N, to = a.db ? size : (long long)a.K * a.N;
   for (long long i = from + (long long)blockIdx.x * 256 + threadIdx.x; i < to; i += (long long)gridDim.x * 256) {
@@ -688,7 +847,7 @@ template <class T, int KIND, bool LOADED>
 int launch(const CUtensorMap& ma, const CUtensorMap& mb, TcArgs a, long long most_units, int sms, cudaStream_t st) {
   const cudaError_t e = cudaFuncSetAttribute(typed_tc_kernel<T, KIND, LOADED>, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED_BYTES);
   if (e != cudaSuccess) { taurus_note_cuda_error(e, "typed_project"); return TAURUS_ERR_CUDA; }
-  const int threads = 32 * (2 + EPI_WARPS + (LOADED ? LOAD_WARPS : 0));
+  constexpr int threads = threads_of<KIND, LOADED>();
   typed_tc_kernel<T, KIND, LOADED><<<(int)std::max<long long>(1, std::min<long long>(most_units, sms)), threads, SHARED_BYTES, st>>>(ma, mb, a);
   return TAURUS_OK;
 }
@@ -710,16 +869,17 @@ bool typed_tc_packs(int32_t type, int d_out) { return type == TAURUS_F32 || d_ou
 size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type) {
   return typed_tc_packs(type, d_out) ? (size_t)types * (type == TAURUS_F32 ? 3 : 1) * d_in * weight_pitch(d_out) * 2 : 0;
 }
-// Rows of a chunk of grad_W: about two units to an SM, 512 rows at least, 4 096 at most.
+// Rows of a chunk of grad_W: about two units to an SM, 1 024 rows at least, 4 096 at most.  fp32: 1 024; the tensor core's sums are cut off, not rounded, and over
+// 2 700 rows (400 000 in 5 types) that made an error of 2.9e-6 of the result where fp32 sums have 1.1e-6.
 int typed_tc_chunk(int64_t n, int d_in, int d_out, int32_t type) {
-  const int most = bn_most(type, false);
-  const long long tiles = (long long)((d_in + BM - 1) / BM) * ((d_out + most - 1) / most);
-  return (int)std::min<long long>(4096, std::max<long long>(512, taurus_round_up((int)std::min<long long>(n * tiles / 296, 1 << 20), 64)));
+  if (type == TAURUS_F32) return 1024;
+  const long long tiles = (long long)((d_in + BM - 1) / BM) * ((d_out + 255) / 256);
+  return (int)std::min<long long>(4096, std::max<long long>(1024, taurus_round_up((int)std::min<long long>(n * tiles / 296, 1 << 20), 64)));
 }
 // A type of more than one chunk has more than `chunk` rows and at most rows / chunk + 1 chunks.
-size_t typed_tc_part_bytes(int64_t n, int d_in, int d_out, int32_t type) {
+size_t typed_tc_part_bytes(int64_t n, int32_t types, int d_in, int d_out, int32_t type) {
   const int chunk = typed_tc_chunk(n, d_in, d_out, type);
-  return (size_t)(2 * (n / chunk)) * (size_t)(d_in + 1) * d_out * 4;
+  return (size_t)(n / chunk + std::min<int64_t>(types, n / chunk)) * (size_t)(d_in + 1) * d_out * 4;
 }
 
 int typed_tc_pack(int32_t type, const void* W, int32_t types, int d_in, int d_out, void* packed, int sms, cudaStream_t st) {
@@ -743,8 +903,8 @@ int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* of
   a.n = n; a.offsets = offsets; a.types = types; a.N = N; a.Kc = Kc;
   a.bn = block_columns(N, bn_most(type, loaded)); a.n_blocks = (N + a.bn - 1) / a.bn;
   a.a = x; a.lda = ld_x; a.a_vec = ld_x % 4 == 0 && rows_aligned(x, 4 * row_type_size(type));
-  a.out = out; a.ld_out = ld_out; a.out_f32 = out_type == TAURUS_F32; a.out_vec = ld_out % 4 == 0 && rows_aligned(out, 4 * row_type_size(out_type));
-  a.bias = bias; a.status = status;
+  a.out = out; a.ld_out = ld_out; a.out_f32 = out_type == TAURUS_F32; a.out_vec = ld_out * row_type_size(out_type) % 16 == 0 && rows_aligned(out, 16);
+  a.bias = bias; a.bias_vec = N % 4 == 0 && rows_aligned(bias, 16); a.status = status;
   const long long pitch = typed_tc_packs(type, d_out) ? weight_pitch(d_out) : d_out;
   CUtensorMap ma = {}, mb = {};
   if (!loaded && !make_map(&ma, type, x, Kc, n, 0, ld_x, bk, BM)) return TAURUS_ERR_CUDA;
@@ -758,36 +918,28 @@ int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* of
 int typed_tc_weights(int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* dy, int64_t ld_dy, int d_in, int d_out, void* dW,
                      int32_t dW_type, float* db, float* part, int32_t* status, int sms, cudaStream_t st) {
   const int chunk = typed_tc_chunk(n, d_in, d_out, type);
-  if (dW) {
-    const bool loaded = type == TAURUS_F32 || !tma_rows(x, ld_x) || !tma_rows(dy, ld_dy);
-    const int bk = type == TAURUS_F32 ? 32 : 64, size = row_type_size(type);
-    TcArgs a = {};
-    a.n = n; a.offsets = offsets; a.types = types; a.M = d_in; a.N = d_out; a.chunk = chunk;
-    a.bn = block_columns(d_out, bn_most(type, loaded)); a.n_blocks = (d_out + a.bn - 1) / a.bn; a.m_blocks = (d_in + BM - 1) / BM;
-    a.a = x; a.lda = ld_x; a.a_vec = ld_x % 4 == 0 && rows_aligned(x, 4 * size);
-    a.b = dy; a.ldb = ld_dy; a.b_vec = ld_dy % 4 == 0 && rows_aligned(dy, 4 * size);
-    a.out = dW; a.out_f32 = dW_type == TAURUS_F32; a.out_vec = d_out % 4 == 0 && rows_aligned(dW, 4 * row_type_size(dW_type)); a.part = part; a.status = status;
-    CUtensorMap ma = {}, mb = {};
-    if (!loaded && (!make_map(&ma, type, x, d_in, n, 0, ld_x, 64, bk) || !make_map(&mb, type, dy, d_out, n, 0, ld_dy, 64, bk))) return TAURUS_ERR_CUDA;
-    const long long units = (n / chunk + types) * a.m_blocks * a.n_blocks;
-    const int rc = launch_type<GRAD_W>(type, loaded, [&](auto f) { return f(ma, mb, a, units, sms, st); });
-    if (rc) return rc;
-  }
+  // (by x's rows too where only grad_bias is asked for: its sums are then formed as they are beside grad_W's)
+  const bool loaded = type == TAURUS_F32 || (x && !tma_rows(x, ld_x)) || !tma_rows(dy, ld_dy);
+  const int bk = type == TAURUS_F32 ? 32 : 64, size = row_type_size(type), out_size = row_type_size(dW_type);
+  TcArgs a = {};
+  a.n = n; a.offsets = offsets; a.types = types; a.M = d_in; a.N = d_out; a.chunk = chunk;
+  a.bn = block_columns(d_out, bn_most(type, loaded)); a.n_blocks = (d_out + a.bn - 1) / a.bn; a.m_blocks = dW ? (d_in + BM - 1) / BM : 1;
+  a.a = dW ? x : nullptr; a.lda = ld_x; a.a_vec = ld_x % 4 == 0 && rows_aligned(x, 4 * size);
+  a.b = dy; a.ldb = ld_dy; a.b_vec = ld_dy % 4 == 0 && rows_aligned(dy, 4 * size);
+  a.out = dW; a.out_f32 = dW_type == TAURUS_F32; a.out_vec = d_out * out_size % 16 == 0 && d_out % 4 == 0 && rows_aligned(dW, 16);
+  a.db = db; a.part = part; a.status = status;
+  CUtensorMap ma = {}, mb = {};
+  if (!loaded && ((dW && !make_map(&ma, type, x, d_in, n, 0, ld_x, 64, bk)) || !make_map(&mb, type, dy, d_out, n, 0, ld_dy, 64, bk))) return TAURUS_ERR_CUDA;
+  const long long units = (n / chunk + types) * a.m_blocks * a.n_blocks;
+  const int rc = launch_type<GRAD_W>(type, loaded, [&](auto f) { return f(ma, mb, a, units, sms, st); });
+  if (rc) return rc;
   JoinArgs j = {};
   j.n = n; j.offsets = offsets; j.types = types; j.K = d_in; j.N = d_out; j.chunk = chunk; j.part = part; j.dW = dW; j.db = db;
-  if (db)
-    with_row_type(type, [&](auto tt) {
-      using T = typename decltype(tt)::type;
-      const int cols = (d_out + 31) / 32;
-      const dim3 grid((unsigned)cols, (unsigned)std::min<long long>(n / chunk + types, std::max(1, sms * 8 / cols)));
-      typed_bias_kernel<T><<<grid, 256, 0, st>>>(j, static_cast<const T*>(dy), ld_dy, part, status);
-      return 0;
-    });
   if (n > chunk)
     with_row_type(dW ? dW_type : TAURUS_F32, [&](auto tt) {
       using O = typename decltype(tt)::type;
       const long long size = (long long)(d_in + 1) * d_out;
-      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 255) / 256, 256), (unsigned)types), 256, 0, st>>>(j);
+      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 1023) / 1024, std::max(8, 8 * sms / types)), (unsigned)types), 256, 0, st>>>(j);
       return 0;
     });
   return TAURUS_OK;

@@ -24,7 +24,7 @@ static __device__ __forceinline__ Split3 split3(float x) {
 bool typed_tc_usable();
 bool typed_tc_packs(int32_t type, int d_out);
 size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type);
-size_t typed_tc_part_bytes(int64_t n, int d_in, int d_out, int32_t type);
+size_t typed_tc_part_bytes(int64_t n, int32_t types, int d_in, int d_out, int32_t type);
 int typed_tc_pack(int32_t type, const void* W, int32_t types, int d_in, int d_out, void* packed, int sms, cudaStream_t st);
 int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* w, const float* bias, int d_in, int d_out,
                   void* out, int32_t out_type, int64_t ld_out, int32_t* status, int sms, cudaStream_t st);

@@ -144,9 +144,12 @@ __device__ __forceinline__ void tmem_ld16(unsigned (&v)[16], unsigned taddr) {
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// 16 or 4 bytes from global to shared memory, of which the first `bytes` are read and the others zeros.
+// 16, 8 or 4 bytes from global to shared memory, of which the first `bytes` are read and the others zeros.
 __device__ __forceinline__ void copy16(unsigned dst, const void* src, unsigned bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy8(unsigned dst, const void* src, unsigned bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy4(unsigned dst, const void* src, unsigned bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -199,7 +202,7 @@ template <int KIND, int BK>
 __device__ __forceinline__ Unit unit_at(const TcArgs& a, const Shared* s, int w) {
   Unit u;
   const int per = KIND == GRAD_W ? a.m_blocks * a.n_blocks : a.n_blocks;
-  const int t = w / per, b = w % per;
+  const int t = w / per, b = (w + t) % per;       // (turned by one from chunk to chunk, for a CTA to meet every kind of tile: the first ones also sum up columns)
   int lo = 0, hi = a.types;                       // the type g with prefix[g] <= t < prefix[g + 1]
   while (hi - lo > 1) { const int m = (lo + hi) >> 1; if (s->prefix[m] <= t) lo = m; else hi = m; }
   u.g = lo;
@@ -230,94 +233,6 @@ __device__ __forceinline__ Quad<T> load_quad(const T* row, int c, int limit, boo
   }
   return q;
 }
-__device__ __forceinline__ unsigned pack2(float a, float b) {
-  const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const unsigned*>(&r);
-}
-template <class T>
-__device__ __forceinline__ void store_quad(unsigned addr, unsigned plane_bytes, const Quad<T>& q) {
-  if constexpr (sizeof(T) == 2) {
-    const uint2 v = *reinterpret_cast<const uint2*>(&q);
-    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
-  } else {
-    unsigned h[2], m[2], l[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const Split3 s0 = split3(q.v[2 * i]), s1 = split3(q.v[2 * i + 1]);
-      h[i] = pack2(s0.hi, s1.hi); m[i] = pack2(s0.mid, s1.mid); l[i] = pack2(s0.lo, s1.lo);
-    }
-    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(h[0]), "r"(h[1]) : "memory");
-    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr + plane_bytes), "r"(m[0]), "r"(m[1]) : "memory");
-    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr + 2 * plane_bytes), "r"(l[0]), "r"(l[1]) : "memory");
-  }
-}
-
-// What a loader thread brings of one stage: its quads of A, and in GRAD_W of B.  place(i): row and column (in quads) of quad i of an operand.
-template <class T, int KIND>
-struct Loader {
-  static constexpr int BK = block_k<T>(), QUADS_A = BM * BK / 4 / LOADERS, QUADS_B = KIND == GRAD_W ? QUADS_A : 0;
-  static constexpr int ROW_QUADS = KIND == GRAD_W ? 32 : BK / 4;      // quads of a row of the tile
-  static __device__ __forceinline__ int row_of(int i, int t) { return (t + i * LOADERS) / ROW_QUADS; }
-  static __device__ __forceinline__ int quad_of(int t) { return t % ROW_QUADS; }      // (the same for every i: LOADERS is a multiple of ROW_QUADS)
-
-  // f(i, row or null, column, columns, is A): for each quad, where it comes from
-  template <class F>
-  static __device__ __forceinline__ void each(const TcArgs& a, const Unit& u, int step, int t, F f) {
-    const int q = quad_of(t) * 4;
-#pragma unroll
-    for (int i = 0; i < QUADS_A; ++i) {
-      const int r = row_of(i, t);
-      if constexpr (KIND != GRAD_W) {
-        f(i, r < u.rows ? static_cast<const T*>(a.a) + (u.row0 + (long long)r) * a.lda : nullptr, step * BK + q, a.Kc, true);
-      } else {
-        const bool in = step * BK + r < u.rows;
-        const long long row = u.row0 + (long long)step * BK + r;
-        f(i, in && a.a ? static_cast<const T*>(a.a) + row * a.lda : nullptr, u.m0 + q, a.M, true);
-        f(QUADS_A + i, in && q < u.bw ? static_cast<const T*>(a.b) + row * a.ldb : nullptr, u.n0 + q, a.N, false);
-      }
-    }
-  }
-  // 16 bits: into registers
-  static __device__ __forceinline__ void load(Quad<T> (&v)[QUADS_A + QUADS_B], const TcArgs& a, const Unit& u, int step, int t) {
-    each(a, u, step, t, [&](int i, const T* row, int c, int limit, bool is_a) { v[i] = load_quad(row, c, limit, is_a ? a.a_vec : a.b_vec); });
-  }
-  // fp32: into this thread's places of a slot of the ring
-  static __device__ __forceinline__ unsigned raw_at(unsigned slot, int i, int t) { return slot + (i * LOADERS + t) * 16; }
-  static __device__ __forceinline__ void copy(unsigned slot, const TcArgs& a, const Unit& u, int step, int t) {
-    each(a, u, step, t, [&](int i, const T* row, int c, int limit, bool is_a) {
-      const unsigned dst = raw_at(slot, i, t);
-      const int left = row ? min(max(limit - c, 0), 4) : 0;
-      const void* const any = a.offsets;                              // (an address for a copy that reads nothing)
-      if (is_a ? a.a_vec : a.b_vec) {
-        copy16(dst, left > 0 ? static_cast<const void*>(row + c) : any, left * 4);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) copy4(dst + 4 * j, j < left ? static_cast<const void*>(row + c + j) : any, j < left ? 4 : 0);
-      }
-    });
-  }
-  static __device__ __forceinline__ Quad<T> raw(unsigned slot, int i, int t) {
-    Quad<T> q;
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(raw_at(slot, i, t)) : "memory");
-    *reinterpret_cast<float4*>(&q) = v;
-    return q;
-  }
-  // Quad i into its operand's planes.
-  static __device__ __forceinline__ void store(unsigned stage, int i, int t, const Quad<T>& q) {
-    constexpr unsigned PLANE = BM * BK * 2;  // bytes of a plane of either operand (blocks of 128 columns)
-    const int r = row_of(i % QUADS_A, t), c = quad_of(t);
-    if constexpr (KIND != GRAD_W) {
-      const int chunk = BK == 64 ? (c >> 1) ^ (r & 7) : (c >> 1) ^ ((r >> 1) & 3);
-      store_quad<T>(stage + r * (BK * 2) + chunk * 16 + (c & 1) * 8, PLANE, q);
-    } else {
-      // quad c lies in the block of 64 columns c / 16
-      const unsigned off = (c >> 4) * (BK * 128) + r * 128 + ((((c & 15) >> 1) ^ (r & 7)) << 4) + (c & 1) * 8;
-      store_quad<T>(stage + (i < QUADS_A ? 0 : planes_of<T>() * PLANE) + off, PLANE, q);
-    }
-  }
-};
-
 // The places of a CTA's stages, in order: unit after unit, step after step.
 template <int KIND, int BK>
 struct Walk {
@@ -328,8 +243,59 @@ struct Walk {
     for (; w < units; w += gridDim.x) { u = unit_at<KIND, BK>(a, s, w); if (u.steps > 0) return; }
   }
   __device__ __forceinline__ bool last() const { return k + 1 == u.steps; }
-  __device__ __forceinline__ void next(const TcArgs& a, const Shared* s, int units) {
-    if (++k == u.steps) { k = 0; w += gridDim.x; find(a, s, units); }
+  // true where another unit begins
+  __device__ __forceinline__ bool next(const TcArgs& a, const Shared* s, int units) {
+    if (++k < u.steps) return false;
+    k = 0; w += gridDim.x;
+    find(a, s, units);
+    return true;
+  }
+};
+
+// What a loader thread brings of a stage: quads of A, and in GRAD_W as many of B, in the same column of every DR-th row of the tile.
+template <class T, int KIND>
+struct Loader {
+  static constexpr int BK = block_k<T>(), QUADS = BM * BK / 4 / LOADERS;               // of an operand
+  static constexpr int ROW_QUADS = KIND == GRAD_W ? 32 : BK / 4, DR = LOADERS / ROW_QUADS;
+  static constexpr int ALL = KIND == GRAD_W ? 2 * QUADS : QUADS;
+  static constexpr unsigned PLANE = BM * BK * 2;                                       // bytes of a plane of either operand (blocks of 128 columns)
+
+  int r0, q;               // row of the first quad in the tile, column
+  const T *pa, *pb;        // where they come from
+  long long da, db;        // from a quad to the next
+  int rows, left_a, left_b;  // rows of the tile from r0 on; columns from q on
+
+  __device__ __forceinline__ explicit Loader(int t) : r0(t / ROW_QUADS), q(t % ROW_QUADS * 4) {}
+  __device__ __forceinline__ void begin(const TcArgs& a, const Unit& u) {
+    const long long row = u.row0 + (long long)r0;
+    rows = u.rows - r0;
+    if (KIND != GRAD_W) {
+      pa = static_cast<const T*>(a.a) + row * a.lda + q; da = DR * a.lda; left_a = a.Kc - q;
+    } else {
+      pa = static_cast<const T*>(a.a) + (a.a ? row * a.lda + u.m0 + q : 0); da = DR * a.lda; left_a = a.a ? a.M - u.m0 - q : 0;
+      pb = static_cast<const T*>(a.b) + row * a.ldb + u.n0 + q; db = DR * a.ldb; left_b = q < u.bw ? a.N - u.n0 - q : 0;
+    }
+  }
+  __device__ __forceinline__ void step(const TcArgs& a) {
+    if (KIND != GRAD_W) { pa += BK; left_a -= BK; }
+    else { pa += BK * a.lda; pb += BK * a.ldb; rows -= BK; }
+  }
+  // f(quad, its address, elements of it that there are: 4 or fewer, perhaps none; of A?)
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i) {
+      const bool in = i * DR < rows;
+      f(i, pa + i * da, in ? left_a : 0, true);
+      if constexpr (KIND == GRAD_W) f(QUADS + i, pb + i * db, in ? left_b : 0, false);
+    }
+  }
+  // Bytes of quad i in its operand's plane.
+  __device__ __forceinline__ unsigned place(int i) const {
+    const int r = r0 + i % QUADS * DR, c = q >> 2;
+    if constexpr (KIND != GRAD_W) return r * (BK * 2) + (((c >> 1) ^ (BK == 64 ? r & 7 : (r >> 1) & 3)) << 4) + (c & 1) * 8;
+    // quad c lies in the block of 64 columns c / 16
+    return (i < QUADS ? 0u : planes_of<T>() * PLANE) + (c >> 4) * (BK * 128) + r * 128 + ((((c & 15) >> 1) ^ (r & 7)) << 4) + (c & 1) * 8;
   }
 };
 
@@ -495,13 +461,14 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           __syncwarp();
         }
         if (lane == 0) {
+          const unsigned long long da0 = A_MN ? desc_mn(st, BK * 128) : desc_k<ROW>(st), db0 = B_MN ? desc_mn(sb, BK * 128) : desc_k<ROW>(sb);
 #pragma unroll
           for (int kk = 0; kk < BK / 16; ++kk) {
             unsigned long long da[NP], db[NP];
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
-              da[p] = A_MN ? desc_mn(st + p * PLANE_A + kk * 2048, BK * 128) : desc_k<ROW>(st + p * PLANE_A + kk * 32);
-              db[p] = B_MN ? desc_mn(sb + p * PLANE_B + kk * 2048, BK * 128) : desc_k<ROW>(sb + p * PLANE_B + kk * 32);
+            for (int p = 0; p < NP; ++p) {               // (addresses are in units of 16 bytes)
+              da[p] = da0 + ((p * PLANE_A + kk * (A_MN ? 2048 : 32)) >> 4);
+              db[p] = db0 + ((p * PLANE_B + kk * (B_MN ? 2048 : 32)) >> 4);
             }
             const unsigned more = (k | kk) != 0;
             if constexpr (NP == 1) {
@@ -603,32 +570,33 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     }
   } else if constexpr (LOADED) {
     // ------------------------------------------------------------ loaders
-    using L = Loader<T, KIND>;
     const int t = threadIdx.x - 32 * (2 + EPI_WARPS);
+    using L = Loader<T, KIND>;
+    L ld(t);
     float sum[4] = {};                                  // GRAD_W: of this thread's four columns of grad_out
     int it = 0;
-    Walk<KIND, BK> at(a, sh, units);
+    Walk<KIND, BK> at(a, sh, units), ahead = at;
+    if (at.w < units) ld.begin(a, at.u);
+    auto go_on = [&] { if (ahead.next(a, sh, units)) { if (ahead.w < units) ld.begin(a, ahead.u); } else ld.step(a); };
+    auto add = [&](float x, float y, float z, float w) { sum[0] += x; sum[1] += y; sum[2] += z; sum[3] += w; };
     auto arrive = [&](int s) {
       async_fence();                                    // for the tensor core to see
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->full[s]);
     };
-    auto add = [&](const Quad<T>& q) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum[j] += to_f32<T>(q.v[j]);
-    };
+    auto free_stage = [&](int i) { return i < STAGES || mbar_wait_warp(&sh->empty[i % STAGES], (i / STAGES & 1) ^ 1, abort_flag); };
     // The unit's sums: those of the eight warps' rows, added in the warps' order.
     unsigned phase = 0;
     auto bias_sums = [&]() -> bool {
       if (KIND != GRAD_W || !a.db || at.u.m0 != 0 || !at.last()) return true;
-      const int me = warp - 2 - EPI_WARPS, c = L::quad_of(t) * 4, columns = min(at.u.bw, a.N - at.u.n0);
+      const int me = warp - 2 - EPI_WARPS, c = ld.q, columns = min(at.u.bw, a.N - at.u.n0);
       *reinterpret_cast<float4*>(sh->bias + me * 128 + c) = make_float4(sum[0], sum[1], sum[2], sum[3]);
       if (!meet(sh, &phase)) return false;
       if (me == 0) {
         float* const place = bias_place(a, at.u);
         for (int w = 1; w < LOAD_WARPS; ++w) {
           const float4 o = *reinterpret_cast<const float4*>(sh->bias + w * 128 + c);
-          sum[0] += o.x; sum[1] += o.y; sum[2] += o.z; sum[3] += o.w;
+          add(o.x, o.y, o.z, o.w);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) if (c + j < columns) place[c + j] = sum[j];
@@ -637,50 +605,100 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       for (int j = 0; j < 4; ++j) sum[j] = 0.f;
       return meet(sh, &phase);
     };
+    const void* const nothing = a.offsets;              // (an address for a copy that reads nothing)
     if constexpr (NP == 3) {
-      // the ring is filled DEPTH stages ahead
+      // a ring of rows as they were read, filled DEPTH stages ahead; quad i of thread t lies at (i LOADERS + t) 16: a thread reads only what it copied itself
       constexpr int DEPTH = raw_depth<KIND>();
-      const unsigned ring = operands + STAGES * STAGE_BYTES;
-      Walk<KIND, BK> ahead = at;
-      for (int d = 0; d < DEPTH; ++d) {
-        if (ahead.w < units) { L::copy(ring + d * raw_bytes<KIND>(), a, ahead.u, ahead.k, t); ahead.next(a, sh, units); }
+      unsigned char* const ring = smem + STAGES * STAGE_BYTES;
+      auto copy = [&](int i) {
+        if (ahead.w < units) {
+          const unsigned slot = smem_u32(ring) + i % DEPTH * raw_bytes<KIND>() + t * 16;
+          ld.each([&](int i, const T* p, int left, bool is_a) {
+            left = min(max(left, 0), 4);
+            const unsigned dst = slot + i * (LOADERS * 16);
+            if (is_a ? a.a_vec : a.b_vec) {
+              copy16(dst, left > 0 ? static_cast<const void*>(p) : nothing, left * 4);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) copy4(dst + 4 * j, j < left ? static_cast<const void*>(p + j) : nothing, j < left ? 4 : 0);
+            }
+          });
+          go_on();
+        }
         copy_commit();
-      }
+      };
+      for (int d = 0; d < DEPTH; ++d) copy(d);
       for (; at.w < units; ++it) {
         const int s = it % STAGES;
-        const unsigned slot = ring + it % DEPTH * raw_bytes<KIND>(), stage = operands + s * STAGE_BYTES;
-        copy_wait<DEPTH - 1>();                         // (a thread reads only what it copied itself)
-        if (it >= STAGES && !mbar_wait_warp(&sh->empty[s], (it / STAGES & 1) ^ 1, abort_flag)) break;
+        copy_wait<DEPTH - 1>();
+        const float4* const mine = reinterpret_cast<const float4*>(ring + it % DEPTH * raw_bytes<KIND>()) + t;
+        float4 v[L::ALL];
 #pragma unroll
-        for (int i = 0; i < L::QUADS_A + L::QUADS_B; ++i) {
-          const Quad<T> q = L::raw(slot, i, t);
-          if (KIND == GRAD_W && i >= L::QUADS_A) add(q);
-          L::store(stage, i, t, q);
+        for (int i = 0; i < L::ALL; ++i) v[i] = mine[i * LOADERS];
+        if (KIND == GRAD_W)
+#pragma unroll
+          for (int i = L::QUADS; i < L::ALL; ++i) add(v[i].x, v[i].y, v[i].z, v[i].w);
+        copy(it + DEPTH);                               // (into the slot just read)
+        if (!free_stage(it)) break;
+        unsigned char* const stage = smem + s * STAGE_BYTES;
+#pragma unroll
+        for (int i = 0; i < L::ALL; ++i) {
+          const Split4 p = split4(v[i].x, v[i].y, v[i].z, v[i].w);
+          unsigned char* const to = stage + ld.place(i);
+          *reinterpret_cast<uint2*>(to) = p.hi;
+          *reinterpret_cast<uint2*>(to + L::PLANE) = p.mid;
+          *reinterpret_cast<uint2*>(to + 2 * L::PLANE) = p.lo;
         }
         arrive(s);
-        if (ahead.w < units) { L::copy(slot, a, ahead.u, ahead.k, t); ahead.next(a, sh, units); }
+        if (!bias_sums()) break;
+        at.next(a, sh, units);
+      }
+      copy_wait<0>();
+    } else if (a.a_vec && (KIND != GRAD_W || a.b_vec)) {
+      // rows whose quads are 8 bytes of aligned memory: copied to their places, AHEAD stages in flight
+      constexpr int AHEAD = 2;
+      auto copy = [&](int i) -> bool {
+        if (ahead.w < units) {
+          if (!free_stage(i)) return false;
+          const unsigned stage = operands + i % STAGES * STAGE_BYTES;
+          ld.each([&](int i, const T* p, int left, bool) { copy8(stage + ld.place(i), left > 0 ? static_cast<const void*>(p) : nothing, min(max(left, 0), 4) * 2); });
+          go_on();
+        }
         copy_commit();
+        return true;
+      };
+      bool ok = true;
+      for (int d = 0; d < AHEAD; ++d) ok = ok && copy(d);
+      for (; ok && at.w < units; ++it) {
+        if (!copy(it + AHEAD)) break;
+        copy_wait<AHEAD>();
+        if (KIND == GRAD_W && a.db && at.u.m0 == 0)
+#pragma unroll
+          for (int i = L::QUADS; i < L::ALL; ++i) {
+            const Vec<T, 4> x = load_vec<Vec<T, 4>>(smem + it % STAGES * STAGE_BYTES + ld.place(i));
+            add(to_f32<T>(x.v[0]), to_f32<T>(x.v[1]), to_f32<T>(x.v[2]), to_f32<T>(x.v[3]));
+          }
+        arrive(it % STAGES);
         if (!bias_sums()) break;
         at.next(a, sh, units);
       }
       copy_wait<0>();
     } else {
-      // the rows of the next stage are on their way while one is stored
-      Quad<T> cur[L::QUADS_A + L::QUADS_B], next[L::QUADS_A + L::QUADS_B];
-      Walk<KIND, BK> ahead = at;
-      if (at.w < units) L::load(cur, a, at.u, 0, t);
+      // element by element
       for (; at.w < units; ++it) {
-        ahead.next(a, sh, units);
-        if (ahead.w < units) L::load(next, a, ahead.u, ahead.k, t);
-        const int s = it % STAGES;
-        if (it >= STAGES && !mbar_wait_warp(&sh->empty[s], (it / STAGES & 1) ^ 1, abort_flag)) break;
+        Vec<T, 4> v[L::ALL];
+        ld.each([&](int i, const T* p, int left, bool) {
 #pragma unroll
-        for (int i = 0; i < L::QUADS_A + L::QUADS_B; ++i) {
-          if (KIND == GRAD_W && i >= L::QUADS_A) add(cur[i]);
-          L::store(operands + s * STAGE_BYTES, i, t, cur[i]);
-          cur[i] = next[i];
+          for (int j = 0; j < 4; ++j) v[i].v[j] = j < left ? p[j] : from_f32<T>(0.f);
+        });
+        go_on();
+        if (!free_stage(it)) break;
+#pragma unroll
+        for (int i = 0; i < L::ALL; ++i) {
+          if (KIND == GRAD_W && i >= L::QUADS) add(to_f32<T>(v[i].v[0]), to_f32<T>(v[i].v[1]), to_f32<T>(v[i].v[2]), to_f32<T>(v[i].v[3]));
+          store_vec(smem + it % STAGES * STAGE_BYTES + ld.place(i), v[i]);
         }
-        arrive(s);
+        arrive(it % STAGES);
         if (!bias_sums()) break;
         at.next(a, sh, units);
       }
@@ -698,13 +716,20 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       const bool mine = a.db && at.u.m0 == 0;
       if (mine && c < at.u.bw) {
         const unsigned sb = operands + s * STAGE_BYTES + NP * PLANE_A + (c >> 6) * (BK * 128), byte = (c & 63) * 2;
-        const int rows = min(BK, at.u.rows - at.k * BK), r1 = min(rows, (half + 1) * (BK / 2));
-#pragma unroll 8
-        for (int r = half * (BK / 2); r < r1; ++r) {
-          unsigned v;
-          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(sb + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15)) : "memory");
-          const Vec<T, 2> p = *reinterpret_cast<const Vec<T, 2>*>(&v);
+        const int rows = min(BK / 2, at.u.rows - at.k * BK - half * (BK / 2));
+        unsigned from[8];                                // the eight rows of a swizzle's period, in bytes of the operands
+#pragma unroll
+        for (int r = 0; r < 8; ++r) from[r] = sb - operands + half * (BK / 2) * 128 + r * 128 + (((byte >> 4) ^ r) << 4) + (byte & 15);
+        auto add = [&](int r) {
+          const Vec<T, 2> p = load_vec<Vec<T, 2>>(smem + from[r & 7] + (r >> 3) * 1024);
           s0 += to_f32<T>(p.v[0]); s1 += to_f32<T>(p.v[1]);
+        };
+        if (rows == BK / 2) {
+#pragma unroll
+          for (int r = 0; r < BK / 2; ++r) add(r);
+        } else {
+#pragma unroll
+          for (int r = 0; r < BK / 2; ++r) if (r < rows) add(r);
         }
       }
       __syncwarp();
@@ -755,12 +780,10 @@ __global__ void __launch_bounds__(256) typed_pack_kernel(const T* __restrict__ W
     } else {
       __nv_bfloat16* const o = static_cast<__nv_bfloat16*>(out) + (g * 3 * K + k) * pitch + c;
       const long long plane = (long long)K * pitch;
-      Split3 s[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) s[j] = split3(q.v[j]);
-      reinterpret_cast<uint2*>(o)[0] = make_uint2(pack2(s[0].hi, s[1].hi), pack2(s[2].hi, s[3].hi));
-      reinterpret_cast<uint2*>(o + plane)[0] = make_uint2(pack2(s[0].mid, s[1].mid), pack2(s[2].mid, s[3].mid));
-      reinterpret_cast<uint2*>(o + 2 * plane)[0] = make_uint2(pack2(s[0].lo, s[1].lo), pack2(s[2].lo, s[3].lo));
+      const Split4 p = split4(q.v[0], q.v[1], q.v[2], q.v[3]);
+      *reinterpret_cast<uint2*>(o) = p.hi;
+      *reinterpret_cast<uint2*>(o + plane) = p.mid;
+      *reinterpret_cast<uint2*>(o + 2 * plane) = p.lo;
     }
   }
 }

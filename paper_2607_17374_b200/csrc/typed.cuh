@@ -4,20 +4,38 @@
 
 #include "rows.cuh"
 
-// An fp32 value as three bf16 values: hi + mid + lo = x exactly while lo is above bf16's smallest.  hi is cut off, not rounded, so that it stays finite.
-// What is not finite is hi alone.
-struct Split3 { float hi, mid, lo; };
-static __device__ __forceinline__ Split3 split3(float x) {
-  Split3 s;
-  s.hi = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-  const float r = x - s.hi;                                         // 16 bits
-  s.mid = __bfloat162float(__float2bfloat16_rn(r));
-  s.lo = r - s.mid;                                                 // at most 8 bits
-  if ((__float_as_uint(x) & 0x7F800000u) == 0x7F800000u) {
-    s.hi = x != x ? __uint_as_float(0x7FC00000u) : x;
-    s.mid = s.lo = 0.f;
-  }
+// Two fp32 values as three pairs of bf16 values: hi + mid + lo = x exactly while lo is above bf16's smallest.  hi is cut off, not rounded, so that it
+// stays finite.  rest: NaN where a value is not finite (its mid and lo then have to be zeros: split_special).
+struct Split2 { unsigned hi, mid, lo; float rest; };
+static __device__ __forceinline__ unsigned bf16_pair(float a, float b) {
+  const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const unsigned*>(&r);
+}
+static __device__ __forceinline__ Split2 split2(float a, float b) {
+  const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
+  Split2 s;
+  s.hi = __byte_perm(ua, ub, 0x7632);
+  const float ra = a - __uint_as_float(ua & 0xFFFF0000u), rb = b - __uint_as_float(ub & 0xFFFF0000u);     // 16 bits
+  s.mid = bf16_pair(ra, rb);
+  s.lo = bf16_pair(ra - __uint_as_float(s.mid << 16), rb - __uint_as_float(s.mid & 0xFFFF0000u));          // at most 8 bits
+  s.rest = ra + rb;
   return s;
+}
+// The same for values of which one may be infinite or NaN: that is hi alone, and a NaN stays one.
+static __device__ __noinline__ Split2 split_special(float a, float b) {
+  const bool fa = fabsf(a) <= 3.402823466e38f, fb = fabsf(b) <= 3.402823466e38f;
+  Split2 s = split2(fa ? a : 0.f, fb ? b : 0.f);
+  if (!fa) s.hi = (s.hi & 0xFFFF0000u) | (a != a ? 0x7FC0u : __float_as_uint(a) >> 16);
+  if (!fb) s.hi = (s.hi & 0xFFFFu) | (b != b ? 0x7FC00000u : __float_as_uint(b) & 0xFFFF0000u);
+  return s;
+}
+// Four values into their three planes of 8 bytes.
+struct Split4 { uint2 hi, mid, lo; };
+static __device__ __forceinline__ Split4 split4(float a, float b, float c, float d) {
+  Split2 p = split2(a, b), q = split2(c, d);
+  const float rest = p.rest + q.rest;
+  if (rest != rest) { p = split_special(a, b); q = split_special(c, d); }
+  return {make_uint2(p.hi, q.hi), make_uint2(p.mid, q.mid), make_uint2(p.lo, q.lo)};
 }
 
 // ---- kernels_typed_tc.cu

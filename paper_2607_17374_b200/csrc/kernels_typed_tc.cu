@@ -31,20 +31,26 @@ namespace {
 enum { PROJECT = 0, GRAD_X = 1, GRAD_W = 2 };
 
 constexpr int BM = 128, MAX_STAGES = 4, MAX_G = TAURUS_MAX_TYPES;
-constexpr int STAGE_BYTES = 48 * 1024;                // operands of a stage
-constexpr int OPERAND_BYTES = MAX_STAGES * STAGE_BYTES;
-constexpr int EPI_WARPS = 8, LOAD_WARPS = 8, LOADERS = 32 * LOAD_WARPS;
+constexpr int OPERAND_BYTES = 192 * 1024;             // shared memory of the operands
 constexpr int EPI_TILE_BYTES = 32 * 64;               // 32 rows x 64 bytes
 constexpr unsigned WAIT_LIMIT = 1u << 24;
 
-template <class T> constexpr int planes_of() { return sizeof(T) == 4 ? 3 : 1; }
-template <class T> constexpr int block_k() { return sizeof(T) == 4 ? 32 : 64; }                   // columns (rows) of a stage
-template <class T, bool LOADED> constexpr int block_n() { return LOADED ? 128 : 256; }
-// fp32: half of the operands' shared memory is a ring of rows as they were read, which the loaders fill far ahead of the tensor core: with the rows of one
-// stage in registers instead, each stage took as long as a read of memory.
-template <class T> constexpr int stages_of() { return sizeof(T) == 4 ? 2 : MAX_STAGES; }
-template <int KIND> constexpr int raw_bytes() { return (KIND == GRAD_W ? 2 : 1) * BM * 32 * 4; }
-template <int KIND> constexpr int raw_depth() { return (OPERAND_BYTES - 2 * STAGE_BYTES) / raw_bytes<KIND>(); }
+// Shapes of the kernel.  BK: columns (rows, in GRAD_W) of a stage; BN: columns of a block at most.  fp32: part of the operands' shared memory is a ring of rows as
+// they were read, which the loaders fill ahead of the tensor core.  GRAD_W splits both operands, and 16 warps share that (8: 651 us for 400 000 rows of 256 and
+// 256, 16: 555); with rows, where one block of 256 columns splits each row once, four warps fewer at the output cost more than eight more loaders bring.
+template <class T, int KIND, bool LOADED>
+struct Shape {
+  static constexpr bool SPLIT = sizeof(T) == 4;
+  static constexpr int NP = SPLIT ? 3 : 1, BK = SPLIT ? 32 : 64, BN = SPLIT ? (KIND == GRAD_W ? 128 : 256) : LOADED ? 128 : 256;
+  static constexpr int EPI_WARPS = SPLIT && KIND == GRAD_W ? 4 : 8, LOAD_WARPS = SPLIT && KIND == GRAD_W ? 16 : 8;
+  static constexpr int PLANE_A = BM * BK * 2, PLANE_B = BN * BK * 2, STAGE_BYTES = NP * (PLANE_A + PLANE_B);
+  static constexpr int STAGES = SPLIT ? 2 : 4;
+  static constexpr int RAW_BYTES = SPLIT ? (KIND == GRAD_W ? 2 : 1) * BM * BK * 4 : 0, RAW_DEPTH = SPLIT ? (OPERAND_BYTES - STAGES * STAGE_BYTES) / (RAW_BYTES + !SPLIT) : 0;
+  // Loaders, or in GRAD_W those who add up the columns of grad_out.
+  static constexpr int THREADS = 32 * (2 + EPI_WARPS + (LOADED || KIND == GRAD_W ? LOAD_WARPS : 0));
+  static constexpr int SHARED_BYTES = OPERAND_BYTES + EPI_WARPS * EPI_TILE_BYTES + LOAD_WARPS * 128 * 4;      // + Shared
+  static_assert(STAGES * STAGE_BYTES <= OPERAND_BYTES && (!SPLIT || RAW_DEPTH >= 3), "operands");
+};
 
 struct __align__(16) Shared {
   unsigned long long full[MAX_STAGES], empty[MAX_STAGES], acc_full[2], acc_empty[2], sums;
@@ -53,11 +59,7 @@ struct __align__(16) Shared {
   int begin[MAX_G + 1];       // rows of type g: [begin[g], begin[g + 1]) (the types' rows follow one another)
   int prefix[MAX_G + 1];      // units (row tiles, chunks) in front of type g
   int slot[MAX_G + 1];        // GRAD_W: partial products in front of type g
-  __align__(16) float bias[LOAD_WARPS * 128];   // (read and written four at a time) GRAD_W: sums of grad_out's columns, of each loader warp or of the second half of those who add
 };
-constexpr int SHARED_BYTES = OPERAND_BYTES + EPI_WARPS * EPI_TILE_BYTES + (int)sizeof(Shared);
-static_assert(SHARED_BYTES <= 227 * 1024, "shared memory of a block");
-
 struct TcArgs {
   long long n;
   const long long* offsets;
@@ -255,7 +257,7 @@ struct Walk {
 // What a loader thread brings of a stage: quads of A, and in GRAD_W as many of B, in the same column of every DR-th row of the tile.
 template <class T, int KIND>
 struct Loader {
-  static constexpr int BK = block_k<T>(), QUADS = BM * BK / 4 / LOADERS;               // of an operand
+  static constexpr int LOADERS = 32 * Shape<T, KIND, true>::LOAD_WARPS, BK = Shape<T, KIND, true>::BK, QUADS = BM * BK / 4 / LOADERS;               // of an operand
   static constexpr int ROW_QUADS = KIND == GRAD_W ? 32 : BK / 4, DR = LOADERS / ROW_QUADS;
   static constexpr int ALL = KIND == GRAD_W ? 2 * QUADS : QUADS;
   static constexpr unsigned PLANE = BM * BK * 2;                                       // bytes of a plane of either operand (blocks of 128 columns)
@@ -295,7 +297,7 @@ struct Loader {
     const int r = r0 + i % QUADS * DR, c = q >> 2;
     if constexpr (KIND != GRAD_W) return r * (BK * 2) + (((c >> 1) ^ (BK == 64 ? r & 7 : (r >> 1) & 3)) << 4) + (c & 1) * 8;
     // quad c lies in the block of 64 columns c / 16
-    return (i < QUADS ? 0u : planes_of<T>() * PLANE) + (c >> 4) * (BK * 128) + r * 128 + ((((c & 15) >> 1) ^ (r & 7)) << 4) + (c & 1) * 8;
+    return (i < QUADS ? 0u : Shape<T, KIND, true>::NP * PLANE) + (c >> 4) * (BK * 128) + r * 128 + ((((c & 15) >> 1) ^ (r & 7)) << 4) + (c & 1) * 8;
   }
 };
 
@@ -346,21 +348,19 @@ __device__ __forceinline__ void put_rows(unsigned char* tile, const float* v, O*
 }
 
 // ---------------------------------------------------------------------------------------------------------------- kernel
-// Loaders, or in GRAD_W those who add up the columns of grad_out.
-template <int KIND, bool LOADED> constexpr int threads_of() { return 32 * (2 + EPI_WARPS + (LOADED || KIND == GRAD_W ? LOAD_WARPS : 0)); }
-
 template <class T, int KIND, bool LOADED>
-__global__ void __launch_bounds__(threads_of<KIND, LOADED>(), 1)
+__global__ void __launch_bounds__(Shape<T, KIND, LOADED>::THREADS, 1)
 typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ TcArgs a) {
   static_assert(LOADED || sizeof(T) == 2, "fp32 operands are split by the loaders");
-  constexpr int NP = planes_of<T>(), BK = block_k<T>(), BN = block_n<T, LOADED>(), ROW = BK * 2, STAGES = stages_of<T>();
+  using S = Shape<T, KIND, LOADED>;
+  constexpr int NP = S::NP, BK = S::BK, ROW = BK * 2, STAGES = S::STAGES, EPI_WARPS = S::EPI_WARPS, LOAD_WARPS = S::LOAD_WARPS;
+  constexpr unsigned PLANE_A = S::PLANE_A, PLANE_B = S::PLANE_B, STAGE_BYTES = S::STAGE_BYTES;
   constexpr bool SUMS = KIND == GRAD_W && !LOADED;       // the last warps read the stages too
-  constexpr unsigned PLANE_A = BM * BK * 2, PLANE_B = BN * BK * 2;
-  static_assert(NP * (PLANE_A + PLANE_B) <= (unsigned)STAGE_BYTES, "a stage's operands");
-  static_assert(sizeof(T) == 2 || raw_depth<KIND>() >= 2, "the ring");
+  static_assert(S::SHARED_BYTES + (int)sizeof(Shared) <= 227 * 1024, "shared memory of a block");
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* const staging = smem + OPERAND_BYTES;
-  Shared* const sh = reinterpret_cast<Shared*>(staging + EPI_WARPS * EPI_TILE_BYTES);
+  float* const bias_smem = reinterpret_cast<float*>(staging + EPI_WARPS * EPI_TILE_BYTES);     // GRAD_W: sums of grad_out's columns, of each loader warp or of the second half of those who add
+  Shared* const sh = reinterpret_cast<Shared*>(bias_smem + LOAD_WARPS * 128);
   volatile int* const abort_flag = &sh->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if ((smem_u32(smem) & 1023u) != 0) {                     // the swizzled tiles want it
@@ -389,6 +389,8 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const unsigned tmem_base = sh->tmem_base;
+  // accumulators: two slots of 256 columns, or with two sums of more than 128 columns one slot
+  const int slots = NP == 3 && a.bn > 128 ? 1 : 2, second = NP == 3 && a.bn > 128 ? 256 : 128;
   const unsigned operands = smem_u32(smem);
 
   if (warp == 0) {
@@ -434,11 +436,11 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     for (int w = blockIdx.x; w < units; w += gridDim.x) {
       const Unit u = unit_at<KIND, BK>(a, sh, w);
       if (u.steps == 0) continue;
-      const int buf = nth & 1;
-      if (nth >= 2 && !mbar_wait_warp(&sh->acc_empty[buf], (nth >> 1 & 1) ^ 1, abort_flag)) break;
+      const int buf = slots == 2 ? nth & 1 : 0;
+      if (nth >= slots && !mbar_wait_warp(&sh->acc_empty[buf], ((slots == 2 ? nth >> 1 : nth) & 1) ^ 1, abort_flag)) break;
       ++nth;
       tc_fence_after();
-      const unsigned d1 = tmem_base + buf * 256, d2 = d1 + 128;
+      const unsigned d1 = tmem_base + buf * 256, d2 = d1 + second;
       constexpr bool A_MN = KIND == GRAD_W, B_MN = KIND != GRAD_X;
       constexpr unsigned FORMAT = std::is_same<T, __half>::value ? 0u : 1u;
       const unsigned idesc = 1u << 4 | FORMAT << 7 | FORMAT << 10 | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | (unsigned)(u.bw >> 3) << 17 | (unsigned)(BM >> 4) << 24;
@@ -498,7 +500,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     int nth = 0;
     for (int w = blockIdx.x; w < units; w += gridDim.x) {
       const Unit u = unit_at<KIND, BK>(a, sh, w);
-      const int buf = nth & 1;
+      const int buf = slots == 2 ? nth & 1 : 0;
       const bool part = KIND == GRAD_W && u.slot >= 0;
       const bool f32 = part || a.out_f32;
       const long long ld = KIND == GRAD_W ? a.N : a.ld_out;
@@ -506,7 +508,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       const long long first = (KIND == GRAD_W ? ((long long)(part ? u.slot : u.g) * (part ? a.M + 1 : a.M) + u.m0 + q * 32) * ld : (u.row0 + q * 32ll) * ld) + u.n0;
       const float* const bias = KIND == PROJECT && a.bias ? a.bias + (long long)u.g * a.N + u.n0 : nullptr;
       if (u.steps > 0) {
-        if (!mbar_wait_warp(&sh->acc_full[buf], nth >> 1 & 1, abort_flag)) break;
+        if (!mbar_wait_warp(&sh->acc_full[buf], (slots == 2 ? nth >> 1 : nth) & 1, abort_flag)) break;
         ++nth;
         tc_fence_after();
       }
@@ -514,7 +516,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         for (int c = lane; c < columns; c += 32) bias_place(a, u)[c] = 0.f;
       if (rows > 0 && (KIND != GRAD_W || a.out)) {
 #pragma unroll 1
-        for (int c0 = half * 32; c0 < columns; c0 += 64) {
+        for (int c0 = half * 32; c0 < columns; c0 += 8 * EPI_WARPS) {
           float o[32];
           if (u.steps > 0) {
             const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + buf * 256 + c0;
@@ -524,7 +526,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
               tmem_ld16(v, at + h * 16);
               if constexpr (NP == 3) {
                 unsigned v2[16];
-                tmem_ld16(v2, at + 128 + h * 16);
+                tmem_ld16(v2, at + second + h * 16);
                 tmem_wait();
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
@@ -590,12 +592,12 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     auto bias_sums = [&]() -> bool {
       if (KIND != GRAD_W || !a.db || at.u.m0 != 0 || !at.last()) return true;
       const int me = warp - 2 - EPI_WARPS, c = ld.q, columns = min(at.u.bw, a.N - at.u.n0);
-      *reinterpret_cast<float4*>(sh->bias + me * 128 + c) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+      *reinterpret_cast<float4*>(bias_smem + me * 128 + c) = make_float4(sum[0], sum[1], sum[2], sum[3]);
       if (!meet(sh, &phase)) return false;
       if (me == 0) {
         float* const place = bias_place(a, at.u);
         for (int w = 1; w < LOAD_WARPS; ++w) {
-          const float4 o = *reinterpret_cast<const float4*>(sh->bias + w * 128 + c);
+          const float4 o = *reinterpret_cast<const float4*>(bias_smem + w * 128 + c);
           add(o.x, o.y, o.z, o.w);
         }
 #pragma unroll
@@ -608,14 +610,14 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const void* const nothing = a.offsets;              // (an address for a copy that reads nothing)
     if constexpr (NP == 3) {
       // a ring of rows as they were read, filled DEPTH stages ahead; quad i of thread t lies at (i LOADERS + t) 16: a thread reads only what it copied itself
-      constexpr int DEPTH = raw_depth<KIND>();
+      constexpr int DEPTH = S::RAW_DEPTH;
       unsigned char* const ring = smem + STAGES * STAGE_BYTES;
       auto copy = [&](int i) {
         if (ahead.w < units) {
-          const unsigned slot = smem_u32(ring) + i % DEPTH * raw_bytes<KIND>() + t * 16;
+          const unsigned slot = smem_u32(ring) + i % DEPTH * S::RAW_BYTES + t * 16;
           ld.each([&](int i, const T* p, int left, bool is_a) {
             left = min(max(left, 0), 4);
-            const unsigned dst = slot + i * (LOADERS * 16);
+            const unsigned dst = slot + i * (L::LOADERS * 16);
             if (is_a ? a.a_vec : a.b_vec) {
               copy16(dst, left > 0 ? static_cast<const void*>(p) : nothing, left * 4);
             } else {
@@ -631,10 +633,10 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       for (; at.w < units; ++it) {
         const int s = it % STAGES;
         copy_wait<DEPTH - 1>();
-        const float4* const mine = reinterpret_cast<const float4*>(ring + it % DEPTH * raw_bytes<KIND>()) + t;
+        const float4* const mine = reinterpret_cast<const float4*>(ring + it % DEPTH * S::RAW_BYTES) + t;
         float4 v[L::ALL];
 #pragma unroll
-        for (int i = 0; i < L::ALL; ++i) v[i] = mine[i * LOADERS];
+        for (int i = 0; i < L::ALL; ++i) v[i] = mine[i * L::LOADERS];
         if (KIND == GRAD_W)
 #pragma unroll
           for (int i = L::QUADS; i < L::ALL; ++i) add(v[i].x, v[i].y, v[i].z, v[i].w);
@@ -735,13 +737,13 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->empty[s]);
       if (mine && at.last()) {
-        if (half == 1) { sh->bias[c] = s0; sh->bias[c + 1] = s1; }
+        if (half == 1) { bias_smem[c] = s0; bias_smem[c + 1] = s1; }
         if (!meet(sh, &phase)) break;
         if (half == 0) {
           float* const place = bias_place(a, at.u);
           const int columns = min(at.u.bw, a.N - at.u.n0);
-          if (c < columns) place[c] = s0 + sh->bias[c];
-          if (c + 1 < columns) place[c + 1] = s1 + sh->bias[c + 1];
+          if (c < columns) place[c] = s0 + bias_smem[c];
+          if (c + 1 < columns) place[c + 1] = s1 + bias_smem[c + 1];
         }
         if (!meet(sh, &phase)) break;
         s0 = s1 = 0.f;
@@ -868,10 +870,11 @@ int block_columns(int N, int most) {
 
 template <class T, int KIND, bool LOADED>
 int launch(const CUtensorMap& ma, const CUtensorMap& mb, TcArgs a, long long most_units, int sms, cudaStream_t st) {
-  const cudaError_t e = cudaFuncSetAttribute(typed_tc_kernel<T, KIND, LOADED>, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED_BYTES);
+  constexpr int shared = Shape<T, KIND, LOADED>::SHARED_BYTES + (int)sizeof(Shared);
+  const cudaError_t e = cudaFuncSetAttribute(typed_tc_kernel<T, KIND, LOADED>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
   if (e != cudaSuccess) { taurus_note_cuda_error(e, "typed_project"); return TAURUS_ERR_CUDA; }
-  constexpr int threads = threads_of<KIND, LOADED>();
-  typed_tc_kernel<T, KIND, LOADED><<<(int)std::max<long long>(1, std::min<long long>(most_units, sms)), threads, SHARED_BYTES, st>>>(ma, mb, a);
+  constexpr int threads = Shape<T, KIND, LOADED>::THREADS;
+  typed_tc_kernel<T, KIND, LOADED><<<(int)std::max<long long>(1, std::min<long long>(most_units, sms)), threads, shared, st>>>(ma, mb, a);
   return TAURUS_OK;
 }
 template <int KIND, class F>
@@ -882,7 +885,7 @@ int launch_type(int32_t type, bool loaded, F f) {     // f(launch function)
 }
 
 int weight_pitch(int d_out) { return taurus_round_up(d_out, 8); }
-int bn_most(int32_t type, bool loaded) { return loaded || type == TAURUS_F32 ? 128 : 256; }
+int bn_most(int32_t type, bool grad_w, bool loaded) { return type == TAURUS_F32 ? (grad_w ? 128 : 256) : loaded ? 128 : 256; }     // Shape::BN
 
 }  // namespace
 
@@ -924,7 +927,7 @@ int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* of
   const int bk = type == TAURUS_F32 ? 32 : 64;
   TcArgs a = {};
   a.n = n; a.offsets = offsets; a.types = types; a.N = N; a.Kc = Kc;
-  a.bn = block_columns(N, bn_most(type, loaded)); a.n_blocks = (N + a.bn - 1) / a.bn;
+  a.bn = block_columns(N, bn_most(type, false, loaded)); a.n_blocks = (N + a.bn - 1) / a.bn;
   a.a = x; a.lda = ld_x; a.a_vec = ld_x % 4 == 0 && rows_aligned(x, 4 * row_type_size(type));
   a.out = out; a.ld_out = ld_out; a.out_f32 = out_type == TAURUS_F32; a.out_vec = ld_out * row_type_size(out_type) % 16 == 0 && rows_aligned(out, 16);
   a.bias = bias; a.bias_vec = N % 4 == 0 && rows_aligned(bias, 16); a.status = status;
@@ -946,7 +949,7 @@ int typed_tc_weights(int64_t n, int32_t types, const long long* offsets, const v
   const int bk = type == TAURUS_F32 ? 32 : 64, size = row_type_size(type), out_size = row_type_size(dW_type);
   TcArgs a = {};
   a.n = n; a.offsets = offsets; a.types = types; a.M = d_in; a.N = d_out; a.chunk = chunk;
-  a.bn = block_columns(d_out, bn_most(type, loaded)); a.n_blocks = (d_out + a.bn - 1) / a.bn; a.m_blocks = dW ? (d_in + BM - 1) / BM : 1;
+  a.bn = block_columns(d_out, bn_most(type, true, loaded)); a.n_blocks = (d_out + a.bn - 1) / a.bn; a.m_blocks = dW ? (d_in + BM - 1) / BM : 1;
   a.a = dW ? x : nullptr; a.lda = ld_x; a.a_vec = ld_x % 4 == 0 && rows_aligned(x, 4 * size);
   a.b = dy; a.ldb = ld_dy; a.b_vec = ld_dy % 4 == 0 && rows_aligned(dy, 4 * size);
   a.out = dW; a.out_f32 = dW_type == TAURUS_F32; a.out_vec = d_out * out_size % 16 == 0 && d_out % 4 == 0 && rows_aligned(dW, 16);

@@ -75,7 +75,6 @@ struct TcArgs {
   int out_f32;                // the output is fp32, else of the operands' type
   int out_vec;                // 16 bytes of columns at a time
   const float* bias;
-  int bias_vec;
   float* db;                  // GRAD_W: gradient of the bias
   float* part;                // GRAD_W: [slots x (M + 1) x N]
   int32_t* status;
@@ -497,6 +496,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     // ------------------------------------------------------------ epilogue: TMEM lanes 32 (warp % 4) .., the two warps of a quadrant take turns
     const int q = warp & 3, half = (warp - 2) >> 2;
     unsigned char* const tile = staging + (warp - 2) * EPI_TILE_BYTES;
+    float* const my_bias = bias_smem + (warp - 2) * 128;    // PROJECT: of the warp's columns, at most four times 32 (as many warps write as load)
     int nth = 0;
     for (int w = blockIdx.x; w < units; w += gridDim.x) {
       const Unit u = unit_at<KIND, BK>(a, sh, w);
@@ -506,7 +506,13 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       const long long ld = KIND == GRAD_W ? a.N : a.ld_out;
       const int rows = min(32, (KIND == GRAD_W ? a.M - u.m0 : u.rows) - q * 32), columns = min(u.bw, a.N - u.n0);
       const long long first = (KIND == GRAD_W ? ((long long)(part ? u.slot : u.g) * (part ? a.M + 1 : a.M) + u.m0 + q * 32) * ld : (u.row0 + q * 32ll) * ld) + u.n0;
-      const float* const bias = KIND == PROJECT && a.bias ? a.bias + (long long)u.g * a.N + u.n0 : nullptr;
+      if (KIND == PROJECT && a.bias) {                  // of this warp's columns; on their way while the products are formed
+        const float* const b = a.bias + (long long)u.g * a.N + u.n0;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const int c = half * 32 + i * 8 * EPI_WARPS + lane; my_bias[i * 32 + lane] = c < columns ? __ldg(b + c) : 0.f; }
+        __syncwarp();
+      }
       if (u.steps > 0) {
         if (!mbar_wait_warp(&sh->acc_full[buf], (slots == 2 ? nth >> 1 : nth) & 1, abort_flag)) break;
         ++nth;
@@ -520,39 +526,31 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           float o[32];
           if (u.steps > 0) {
             const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + buf * 256 + c0;
+            unsigned v[2][16], v2[2][16];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              unsigned v[16];
-              tmem_ld16(v, at + h * 16);
+              tmem_ld16(v[h], at + h * 16);
+              if constexpr (NP == 3) tmem_ld16(v2[h], at + second + h * 16);
+            }
+            tmem_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              o[j] = __uint_as_float(v[j >> 4][j & 15]);
               if constexpr (NP == 3) {
-                unsigned v2[16];
-                tmem_ld16(v2, at + second + h * 16);
-                tmem_wait();
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                  const float x = __uint_as_float(v[j]), y = x + __uint_as_float(v2[j]);
-                  o[h * 16 + j] = (v[j] & 0x7F800000u) == 0x7F800000u ? x : y;
-                }
-              } else {
-                tmem_wait();
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[h * 16 + j] = __uint_as_float(v[j]);
+                const float y = o[j] + __uint_as_float(v2[j >> 4][j & 15]);
+                o[j] = (v[j >> 4][j & 15] & 0x7F800000u) == 0x7F800000u ? o[j] : y;
               }
             }
           } else {
 #pragma unroll
             for (int j = 0; j < 32; ++j) o[j] = 0.f;
           }
-          if (KIND == PROJECT && bias) {
-            if (a.bias_vec && c0 + 32 <= columns) {
+          if (KIND == PROJECT && a.bias) {
+            const float* const b = my_bias + c0 / (8 * EPI_WARPS) * 32;
 #pragma unroll
-              for (int j = 0; j < 32; j += 4) {
-                const float4 b = __ldg(reinterpret_cast<const float4*>(bias + c0 + j));
-                o[j] += b.x; o[j + 1] += b.y; o[j + 2] += b.z; o[j + 3] += b.w;
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) if (c0 + j < columns) o[j] += __ldg(bias + c0 + j);
+            for (int j = 0; j < 32; j += 4) {
+              const float4 x = *reinterpret_cast<const float4*>(b + j);
+              o[j] += x.x; o[j + 1] += x.y; o[j + 2] += x.z; o[j + 3] += x.w;
             }
           }
           if (f32) {
@@ -930,7 +928,7 @@ int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* of
   a.bn = block_columns(N, bn_most(type, false, loaded)); a.n_blocks = (N + a.bn - 1) / a.bn;
   a.a = x; a.lda = ld_x; a.a_vec = ld_x % 4 == 0 && rows_aligned(x, 4 * row_type_size(type));
   a.out = out; a.ld_out = ld_out; a.out_f32 = out_type == TAURUS_F32; a.out_vec = ld_out * row_type_size(out_type) % 16 == 0 && rows_aligned(out, 16);
-  a.bias = bias; a.bias_vec = N % 4 == 0 && rows_aligned(bias, 16); a.status = status;
+  a.bias = bias; a.status = status;
   const long long pitch = typed_tc_packs(type, d_out) ? weight_pitch(d_out) : d_out;
   CUtensorMap ma = {}, mb = {};
   if (!loaded && !make_map(&ma, type, x, Kc, n, 0, ld_x, bk, BM)) return TAURUS_ERR_CUDA;

@@ -31,8 +31,6 @@ namespace {
 enum { PROJECT = 0, GRAD_X = 1, GRAD_W = 2 };
 
 constexpr int BM = 128, MAX_STAGES = 4, MAX_G = TAURUS_MAX_TYPES;
-constexpr int OPERAND_BYTES = 192 * 1024;             // shared memory of the operands
-constexpr int EPI_TILE_BYTES = 32 * 64;               // 32 rows x 64 bytes
 constexpr unsigned WAIT_LIMIT = 1u << 24;
 
 // Shapes of the kernel.  BK: columns (rows, in GRAD_W) of a stage; BN: columns of a block at most.  fp32: part of the operands' shared memory is a ring of rows as
@@ -45,11 +43,12 @@ struct Shape {
   static constexpr int EPI_WARPS = SPLIT && KIND == GRAD_W ? 4 : 8, LOAD_WARPS = SPLIT && KIND == GRAD_W ? 16 : 8;
   static constexpr int PLANE_A = BM * BK * 2, PLANE_B = BN * BK * 2, STAGE_BYTES = NP * (PLANE_A + PLANE_B);
   static constexpr int STAGES = SPLIT ? 2 : 4;
-  static constexpr int RAW_BYTES = SPLIT ? (KIND == GRAD_W ? 2 : 1) * BM * BK * 4 : 0, RAW_DEPTH = SPLIT ? (OPERAND_BYTES - STAGES * STAGE_BYTES) / (RAW_BYTES + !SPLIT) : 0;
+  static constexpr int EPI_ROW = SPLIT && KIND != GRAD_W ? 128 : 64;       // bytes of a row that a warp of the epilogue transposes at a time
+  static constexpr int RAW_BYTES = SPLIT ? (KIND == GRAD_W ? 2 : 1) * BM * BK * 4 : 0, RAW_DEPTH = SPLIT ? (KIND == GRAD_W ? 3 : 2) : 0;
   // Loaders, or in GRAD_W those who add up the columns of grad_out.
   static constexpr int THREADS = 32 * (2 + EPI_WARPS + (LOADED || KIND == GRAD_W ? LOAD_WARPS : 0));
-  static constexpr int SHARED_BYTES = OPERAND_BYTES + EPI_WARPS * EPI_TILE_BYTES + LOAD_WARPS * 128 * 4;      // + Shared
-  static_assert(STAGES * STAGE_BYTES <= OPERAND_BYTES && (!SPLIT || RAW_DEPTH >= 3), "operands");
+  static constexpr int OPERAND_BYTES = STAGES * STAGE_BYTES + RAW_DEPTH * RAW_BYTES;
+  static constexpr int SHARED_BYTES = OPERAND_BYTES + EPI_WARPS * 32 * EPI_ROW + LOAD_WARPS * 128 * 4;      // + Shared
 };
 
 struct __align__(16) Shared {
@@ -133,6 +132,12 @@ __device__ __forceinline__ void umma(unsigned d, unsigned long long a, unsigned 
 }
 __device__ __forceinline__ void umma_commit(unsigned long long* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// One lane of the (converged) warp, known as such to the compiler: MMA operands stay in uniform registers.
+__device__ __forceinline__ bool elected() {
+  unsigned p;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p != 0;
 }
 // 16 columns of an accumulator, one row per lane.
 __device__ __forceinline__ void tmem_ld16(unsigned (&v)[16], unsigned taddr) {
@@ -314,34 +319,41 @@ __device__ __forceinline__ float* bias_place(const TcArgs& a, const Unit& u) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------- epilogue
-// PASS columns (64 bytes of the output) of 32 rows: transposed through the warp's tile, 16-byte chunk c of row r at chunk c ^ ((r >> 1) & 3), and written
-// eight rows at a time in pieces of 64 bytes; out: row 0, column 0 of them; rows <= 32.
-template <class O>
+// PASS columns (ROW bytes of the output) of 32 rows: transposed through the warp's tile, 16-byte chunks of a row in an order of its own, and written
+// in pieces of ROW bytes, several rows at a time; out: row 0, column 0 of them; rows <= 32.
+template <class O, int ROW>
+__device__ __forceinline__ unsigned tile_at(int r, int c) { return r * ROW + ((c ^ (ROW == 128 ? r & 7 : (r >> 1) & 3)) << 4); }
+template <class O, int ROW>
 __device__ __forceinline__ void put_rows(unsigned char* tile, const float* v, O* out, long long ld, int rows, int columns, bool vec) {
-  constexpr int PASS = 64 / sizeof(O), PER = 16 / sizeof(O);
+  constexpr int PASS = ROW / sizeof(O), PER = 16 / sizeof(O), CHUNKS = ROW / 16, AT_ONCE = 32 / CHUNKS;
   const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
+  for (int c = 0; c < CHUNKS; ++c) {
     Vec<O, PER> x;
 #pragma unroll
     for (int j = 0; j < PER; ++j) x.v[j] = from_f32<O>(v[c * PER + j]);
-    store_vec(tile + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), x);
+    store_vec(tile + tile_at<O, ROW>(lane, c), x);
   }
   __syncwarp();
   if (vec && columns >= PASS) {
-    const int c = lane & 3;
-    O* p = out + (lane >> 2) * ld + c * PER;
+    const int c = lane % CHUNKS, r0 = lane / CHUNKS;
+    Vec<O, PER> x[CHUNKS];                              // all read before the first is written: the compiler cannot tell the two memories apart
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = i * 8 + (lane >> 2);
-      if (r < rows) store_vec(p, load_vec<Vec<O, PER>>(tile + r * 64 + ((c ^ ((r >> 1) & 3)) << 4)));
-      p += 8 * ld;
+    for (int i = 0; i < CHUNKS; ++i) x[i] = load_vec<Vec<O, PER>>(tile + tile_at<O, ROW>(i * AT_ONCE + r0, c));
+    O* p = out + r0 * ld + c * PER;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      if (i * AT_ONCE + r0 < rows) store_vec(p, x[i]);
+      p += AT_ONCE * ld;
     }
   } else {
-    constexpr int AT_ONCE = 32 / PASS;                 // rows
-    const int c = lane % PASS;
-    for (int r = lane / PASS; r < rows; r += AT_ONCE)
-      if (c < columns) out[r * ld + c] = *reinterpret_cast<const O*>(tile + r * 64 + (((c / PER) ^ ((r >> 1) & 3)) << 4) + c % PER * sizeof(O));
+    constexpr int FEW = PASS < 32 ? 32 / PASS : 1, WIDE = PASS < 32 ? 1 : PASS / 32;   // rows at once; times 32 columns
+    for (int r = lane / (32 / FEW); r < rows; r += FEW)
+#pragma unroll
+      for (int i = 0; i < WIDE; ++i) {
+        const int c = i * 32 + lane % (32 / FEW);
+        if (c < columns) out[r * ld + c] = *reinterpret_cast<const O*>(tile + tile_at<O, ROW>(r, c / PER) + c % PER * sizeof(O));
+      }
   }
   __syncwarp();
 }
@@ -357,8 +369,8 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   constexpr bool SUMS = KIND == GRAD_W && !LOADED;       // the last warps read the stages too
   static_assert(S::SHARED_BYTES + (int)sizeof(Shared) <= 227 * 1024, "shared memory of a block");
   extern __shared__ __align__(1024) unsigned char smem[];
-  unsigned char* const staging = smem + OPERAND_BYTES;
-  float* const bias_smem = reinterpret_cast<float*>(staging + EPI_WARPS * EPI_TILE_BYTES);     // GRAD_W: sums of grad_out's columns, of each loader warp or of the second half of those who add
+  unsigned char* const staging = smem + S::OPERAND_BYTES;
+  float* const bias_smem = reinterpret_cast<float*>(staging + EPI_WARPS * 32 * S::EPI_ROW);     // GRAD_W: sums of grad_out's columns, of each loader warp or of the second half of those who add
   Shared* const sh = reinterpret_cast<Shared*>(bias_smem + LOAD_WARPS * 128);
   volatile int* const abort_flag = &sh->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -461,41 +473,52 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           async_fence();
           __syncwarp();
         }
-        if (lane == 0) {
-          const unsigned long long da0 = A_MN ? desc_mn(st, BK * 128) : desc_k<ROW>(st), db0 = B_MN ? desc_mn(sb, BK * 128) : desc_k<ROW>(sb);
+        // The stage's number written out: with addresses that the compiler cannot tell to be the same in every lane each MMA took 110 cycles to issue.
+        auto issue = [&](auto stage) {
+          constexpr unsigned AT = decltype(stage)::value * STAGE_BYTES;
+          const unsigned long long da0 = A_MN ? desc_mn(operands + AT, BK * 128) : desc_k<ROW>(operands + AT);
+          const unsigned long long db0 = B_MN ? desc_mn(operands + AT + NP * PLANE_A, BK * 128) : desc_k<ROW>(operands + AT + NP * PLANE_A);
+          if (elected()) {
 #pragma unroll
-          for (int kk = 0; kk < BK / 16; ++kk) {
-            unsigned long long da[NP], db[NP];
+            for (int kk = 0; kk < BK / 16; ++kk) {
+              unsigned long long da[NP], db[NP];
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {               // (addresses are in units of 16 bytes)
-              da[p] = da0 + ((p * PLANE_A + kk * (A_MN ? 2048 : 32)) >> 4);
-              db[p] = db0 + ((p * PLANE_B + kk * (B_MN ? 2048 : 32)) >> 4);
+              for (int p = 0; p < NP; ++p) {             // (addresses are in units of 16 bytes)
+                da[p] = da0 + ((p * PLANE_A + kk * (A_MN ? 2048 : 32)) >> 4);
+                db[p] = db0 + ((p * PLANE_B + kk * (B_MN ? 2048 : 32)) >> 4);
+              }
+              const unsigned more = (k | kk) != 0;
+              if constexpr (NP == 1) {
+                umma(d1, da[0], db[0], idesc, more);
+              } else {
+                umma(d2, da[2], db[0], idesc, more);
+                umma(d2, da[0], db[2], idesc, 1u);
+                umma(d2, da[1], db[1], idesc, 1u);
+                umma(d2, da[1], db[0], idesc, 1u);
+                umma(d2, da[0], db[1], idesc, 1u);
+                umma(d1, da[0], db[0], idesc, more);
+              }
             }
-            const unsigned more = (k | kk) != 0;
-            if constexpr (NP == 1) {
-              umma(d1, da[0], db[0], idesc, more);
-            } else {
-              umma(d2, da[2], db[0], idesc, more);
-              umma(d2, da[0], db[2], idesc, 1u);
-              umma(d2, da[1], db[1], idesc, 1u);
-              umma(d2, da[1], db[0], idesc, 1u);
-              umma(d2, da[0], db[1], idesc, 1u);
-              umma(d1, da[0], db[0], idesc, more);
-            }
+            umma_commit(&sh->empty[decltype(stage)::value]);
           }
-          umma_commit(&sh->empty[s]);
+        };
+        if (s == 0) issue(std::integral_constant<int, 0>());
+        else if (s == 1) issue(std::integral_constant<int, 1>());
+        else if constexpr (STAGES > 2) {
+          if (s == 2) issue(std::integral_constant<int, 2>());
+          else issue(std::integral_constant<int, 3>());
         }
         __syncwarp();
       }
       if (!ok) break;
-      if (lane == 0) umma_commit(&sh->acc_full[buf]);
+      if (elected()) umma_commit(&sh->acc_full[buf]);
       __syncwarp();
     }
     if (lane == 0) sh->mmas = it;
   } else if (warp < 2 + EPI_WARPS) {
     // ------------------------------------------------------------ epilogue: TMEM lanes 32 (warp % 4) .., the two warps of a quadrant take turns
     const int q = warp & 3, half = (warp - 2) >> 2;
-    unsigned char* const tile = staging + (warp - 2) * EPI_TILE_BYTES;
+    unsigned char* const tile = staging + (warp - 2) * 32 * S::EPI_ROW;
     float* const my_bias = bias_smem + (warp - 2) * 128;    // PROJECT: of the warp's columns, at most four times 32 (as many warps write as load)
     int nth = 0;
     for (int w = blockIdx.x; w < units; w += gridDim.x) {
@@ -555,10 +578,14 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           }
           if (f32) {
             float* const p = (part ? a.part : static_cast<float*>(a.out)) + first + c0;
-            put_rows<float>(tile, o, p, ld, rows, columns - c0, a.out_vec);
-            if (columns - c0 > 16) put_rows<float>(tile, o + 16, p + 16, ld, rows, columns - c0 - 16, a.out_vec);
+            if constexpr (S::EPI_ROW == 128) {
+              put_rows<float, 128>(tile, o, p, ld, rows, columns - c0, a.out_vec);
+            } else {
+              put_rows<float, 64>(tile, o, p, ld, rows, columns - c0, a.out_vec);
+              if (columns - c0 > 16) put_rows<float, 64>(tile, o + 16, p + 16, ld, rows, columns - c0 - 16, a.out_vec);
+            }
           } else {
-            put_rows<T>(tile, o, static_cast<T*>(a.out) + first + c0, ld, rows, columns - c0, a.out_vec);
+            if constexpr (NP == 1) put_rows<T, 64>(tile, o, static_cast<T*>(a.out) + first + c0, ld, rows, columns - c0, a.out_vec);
           }
         }
       }
@@ -613,7 +640,9 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       auto copy = [&](int i) {
         if (ahead.w < units) {
           const unsigned slot = smem_u32(ring) + i % DEPTH * S::RAW_BYTES + t * 16;
-          ld.each([&](int i, const T* p, int left, bool is_a) {
+          if (a.a_vec && ld.left_a >= 4 && ld.rows > (L::QUADS - 1) * L::DR && (KIND != GRAD_W || (a.b_vec && ld.left_b >= 4))) {
+            ld.each([&](int i, const T* p, int, bool) { copy16(slot + i * (L::LOADERS * 16), p, 16); });     // all there
+          } else ld.each([&](int i, const T* p, int left, bool is_a) {
             left = min(max(left, 0), 4);
             const unsigned dst = slot + i * (L::LOADERS * 16);
             if (is_a ? a.a_vec : a.b_vec) {

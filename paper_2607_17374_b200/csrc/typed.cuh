@@ -5,19 +5,18 @@
 #include "rows.cuh"
 
 // Two fp32 values as three pairs of bf16 values: hi + mid + lo = x exactly while lo is above bf16's smallest.  hi is cut off, not rounded, so that it
-// stays finite.  rest: NaN where a value is not finite (its mid and lo then have to be zeros: split_special).
+// stays finite; mid is rounded to nearest, by an addition to its bits (the conversion instruction has a fraction of the rate); lo has 8 bits left and is the upper
+// half of its fp32 word.  rest: NaN where a value is not finite (its mid and lo then have to be zeros: split_special).
 struct Split2 { unsigned hi, mid, lo; float rest; };
-static __device__ __forceinline__ unsigned bf16_pair(float a, float b) {
-  const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const unsigned*>(&r);
-}
 static __device__ __forceinline__ Split2 split2(float a, float b) {
   const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
+  const float ra = a - __uint_as_float(ua & 0xFFFF0000u), rb = b - __uint_as_float(ub & 0xFFFF0000u);     // 16 bits
+  const unsigned ma = __float_as_uint(ra) + 0x8000u, mb = __float_as_uint(rb) + 0x8000u;
+  const float la = ra - __uint_as_float(ma & 0xFFFF0000u), lb = rb - __uint_as_float(mb & 0xFFFF0000u);   // at most 8 bits
   Split2 s;
   s.hi = __byte_perm(ua, ub, 0x7632);
-  const float ra = a - __uint_as_float(ua & 0xFFFF0000u), rb = b - __uint_as_float(ub & 0xFFFF0000u);     // 16 bits
-  s.mid = bf16_pair(ra, rb);
-  s.lo = bf16_pair(ra - __uint_as_float(s.mid << 16), rb - __uint_as_float(s.mid & 0xFFFF0000u));          // at most 8 bits
+  s.mid = __byte_perm(ma, mb, 0x7632);
+  s.lo = __byte_perm(__float_as_uint(la), __float_as_uint(lb), 0x7632);
   s.rest = ra + rb;
   return s;
 }

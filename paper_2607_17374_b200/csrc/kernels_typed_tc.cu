@@ -640,8 +640,9 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       auto copy = [&](int i) {
         if (ahead.w < units) {
           const unsigned slot = smem_u32(ring) + i % DEPTH * S::RAW_BYTES + t * 16;
-          if (a.a_vec && ld.left_a >= 4 && ld.rows > (L::QUADS - 1) * L::DR && (KIND != GRAD_W || (a.b_vec && ld.left_b >= 4))) {
-            ld.each([&](int i, const T* p, int, bool) { copy16(slot + i * (L::LOADERS * 16), p, 16); });     // all there
+          if (a.a_vec && (KIND != GRAD_W || a.b_vec) && ld.rows > (L::QUADS - 1) * L::DR) {      // every row is there
+            const unsigned na = min(max(ld.left_a, 0), 4) * 4, nb = KIND == GRAD_W ? min(max(ld.left_b, 0), 4) * 4 : 0;
+            ld.each([&](int i, const T* p, int, bool is_a) { copy16(slot + i * (L::LOADERS * 16), (is_a ? na : nb) ? static_cast<const void*>(p) : nothing, is_a ? na : nb); });
           } else ld.each([&](int i, const T* p, int left, bool is_a) {
             left = min(max(left, 0), 4);
             const unsigned dst = slot + i * (L::LOADERS * 16);

@@ -90,6 +90,27 @@ static __device__ __forceinline__ void store_vec(void* p, const V& r) {
     *reinterpret_cast<uint16_t*>(p) = *reinterpret_cast<const uint16_t*>(&r);
   }
 }
+// Written past the caches' lines that are read again.
+template <class V>
+static __device__ __forceinline__ void store_vec_once(void* p, const V& r) {
+  if constexpr (sizeof(V) % 16 == 0) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(V) / 16; ++i) __stcs(reinterpret_cast<uint4*>(p) + i, reinterpret_cast<const uint4*>(&r)[i]);
+  } else if constexpr (sizeof(V) == 8) {
+    __stcs(reinterpret_cast<uint2*>(p), *reinterpret_cast<const uint2*>(&r));
+  } else if constexpr (sizeof(V) == 4) {
+    __stcs(reinterpret_cast<uint32_t*>(p), *reinterpret_cast<const uint32_t*>(&r));
+  } else {
+    __stcs(reinterpret_cast<uint16_t*>(p), *reinterpret_cast<const uint16_t*>(&r));
+  }
+}
+template <class T, int N>
+static __device__ __forceinline__ void store_f32_once(T* p, const float (&x)[N]) {
+  Vec<T, N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) r.v[i] = from_f32<T>(x[i]);
+  store_vec_once(p, r);
+}
 template <class T, int N>
 static __device__ __forceinline__ void store_f32(T* p, const float (&x)[N]) {
   Vec<T, N> r;

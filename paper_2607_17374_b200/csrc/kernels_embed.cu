@@ -64,7 +64,7 @@ int vector_of(int limit, int size, const void* p, int64_t ld, int width) {
 // Stable counting sort by digits of the ids, least significant first: per pass the digits of each block's items are counted (count), the counts of
 // every digit summed over the blocks in front (scan), and the items moved (move).  Digits of up to 11 bits: a table of up to 2 048 rows takes one pass, of
 // 4 M two.  Up to SMALL items one block does it all.
-constexpr int SORT_THREADS = 256, SORT_WARPS = SORT_THREADS / 32, MAX_DIGIT = 11, MAX_BINS = 1 << MAX_DIGIT, TILE = 2048, MAX_ITEMS = 16 * TILE;
+constexpr int SORT_THREADS = 256, SORT_WARPS = SORT_THREADS / 32, MAX_DIGIT = 11, MAX_BINS = 1 << MAX_DIGIT, TILE = 1024, MAX_ITEMS = 32 * TILE;
 constexpr int SMALL = 2048, SMALL_THREADS = 1024;
 
 struct SortPlan { int passes, bits, items, blocks; };   // bits of a digit; items of a block
@@ -75,7 +75,7 @@ SortPlan sort_plan(int64_t n, int64_t table_rows) {
   p.passes = (key + MAX_DIGIT - 1) / MAX_DIGIT;
   p.bits = (key + p.passes - 1) / p.passes;
   p.items = TILE;
-  while (p.items < MAX_ITEMS && n / p.items > 1024) p.items *= 2;
+  while (p.items < MAX_ITEMS && n / p.items > 300) p.items *= 2;      // two blocks to an SM
   p.blocks = (int)((n + p.items - 1) / p.items);
   return p;
 }
@@ -87,7 +87,7 @@ struct SortArgs {
   const int* pos_in;
   unsigned* key_out;
   int* pos_out;
-  unsigned* hist;              // [bins x blocks]
+  unsigned* hist;              // [blocks x bins]
   int shift, bits, items, blocks;
   int* open_count;             // two words, cleared by the first pass
   int32_t* status;
@@ -133,28 +133,33 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_count_kernel(const SortArg
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < bins; i += SORT_THREADS) a.hist[(size_t)i * a.blocks + blockIdx.x] = h[i];
+  for (int i = threadIdx.x; i < bins; i += SORT_THREADS) a.hist[((size_t)blockIdx.x << a.bits) + i] = h[i];
 }
 
-// hist[d][b] -> items of digit d in the blocks in front of b; the digit's total behind the table (totals[d]).  A warp to a digit.
-__global__ void __launch_bounds__(SORT_THREADS) embed_scan_kernel(unsigned* hist, unsigned* totals, int bins, int blocks) {
-  const int d = blockIdx.x * SORT_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (d >= bins) return;
+// hist[b][d] -> items of digit d in the blocks in front of b; the digit's total in totals[d].  A lane to a digit, the warps share the blocks.
+constexpr int SCAN_WARPS = 32, SCAN_THREADS = 32 * SCAN_WARPS;
+__global__ void __launch_bounds__(SCAN_THREADS) embed_scan_kernel(unsigned* hist, unsigned* totals, int bins, int blocks) {
+  __shared__ unsigned part[SCAN_WARPS][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = blockIdx.x * 32 + lane;
+  const int per = (blocks + SCAN_WARPS - 1) / SCAN_WARPS, from = min(warp * per, blocks), to = min(from + per, blocks);
   unsigned sum = 0;
-  for (int b0 = 0; b0 < blocks; b0 += 128) {
-    unsigned v[4];
+  if (d < bins)
+#pragma unroll 8
+    for (int b = from; b < to; ++b) sum += hist[(size_t)b * bins + d];
+  part[warp][lane] = sum;
+  __syncthreads();
+  unsigned before = 0, all = 0;
+  for (int w = 0; w < SCAN_WARPS; ++w) { const unsigned p = part[w][lane]; before += w < warp ? p : 0; all += p; }
+  if (d >= bins) return;
+  if (warp == 0) totals[d] = all;
+  for (int b0 = from; b0 < to; b0 += 8) {
+    unsigned v[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) { const int b = b0 + u * 32 + lane; v[u] = b < blocks ? hist[(size_t)d * blocks + b] : 0; }
+    for (int u = 0; u < 8; ++u) v[u] = b0 + u < to ? hist[(size_t)(b0 + u) * bins + d] : 0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      unsigned x = v[u];
-      for (int o = 1; o < 32; o <<= 1) { const unsigned y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-      const int b = b0 + u * 32 + lane;
-      if (b < blocks) hist[(size_t)d * blocks + b] = sum + x - v[u];
-      sum += __shfl_sync(0xffffffffu, x, 31);
-    }
+    for (int u = 0; u < 8; ++u)
+      if (b0 + u < to) { hist[(size_t)(b0 + u) * bins + d] = before; before += v[u]; }
   }
-  if (lane == 0) totals[d] = sum;
 }
 
 // Exclusive sums of v[0 .. count) in place, count <= threads * 8; by a whole block of WARPS warps.
@@ -177,11 +182,11 @@ __device__ __forceinline__ void scan_block(unsigned* v, int count, unsigned* war
 // that the warp has moved.
 __global__ void __launch_bounds__(SORT_THREADS) embed_move_kernel(const SortArgs a, const unsigned* __restrict__ totals) {
   __shared__ unsigned base[MAX_BINS];
-  __shared__ unsigned short mine[SORT_WARPS][MAX_BINS];
+  __shared__ __align__(4) unsigned short mine[SORT_WARPS][MAX_BINS];
   __shared__ unsigned warp_sums[SORT_WARPS];
   const int bins = 1 << a.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int i = threadIdx.x; i < bins; i += SORT_THREADS) base[i] = totals[i];
-  for (int i = threadIdx.x; i < SORT_WARPS * bins; i += SORT_THREADS) mine[i / bins][i % bins] = 0;
+  for (int i = threadIdx.x; i < SORT_WARPS * MAX_BINS / 2; i += SORT_THREADS) reinterpret_cast<unsigned*>(&mine[0][0])[i] = 0;
   __syncthreads();
   scan_block<SORT_WARPS>(base, bins, warp_sums);
   const int run = a.items / SORT_WARPS;
@@ -199,7 +204,7 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_move_kernel(const SortArgs
   }
   __syncthreads();
   for (int i = threadIdx.x; i < bins; i += SORT_THREADS) {
-    base[i] += a.hist[(size_t)i * a.blocks + blockIdx.x];
+    base[i] += a.hist[((size_t)blockIdx.x << a.bits) + i];
     unsigned short sum = 0;
 #pragma unroll
     for (int w = 0; w < SORT_WARPS; ++w) { const unsigned short c = mine[w][i]; mine[w][i] = sum; sum += c; }
@@ -478,7 +483,7 @@ embed_join_kernel(const GradArgs a, T* __restrict__ table) {
 
 // Pieces: short ones give warps enough to fill the device a few times over, long ones keep the partial rows few.
 int grad_piece(int64_t n) {
-  int piece = 16;
+  int piece = 32;
   while (piece < 256 && n / (2 * piece) >= 148 * 64) piece *= 2;
   return piece;
 }
@@ -613,7 +618,7 @@ extern "C" int taurus_embed_grad(int64_t n, const int64_t* ids, const void* grad
       }
       q.shift = pass * plan.bits;
       embed_count_kernel<<<plan.blocks, SORT_THREADS, 0, st>>>(q);
-      embed_scan_kernel<<<((1 << plan.bits) + SORT_WARPS - 1) / SORT_WARPS, SORT_THREADS, 0, st>>>(q.hist, totals, 1 << plan.bits, plan.blocks);
+      embed_scan_kernel<<<((1 << plan.bits) + 31) / 32, SCAN_THREADS, 0, st>>>(q.hist, totals, 1 << plan.bits, plan.blocks);
       embed_move_kernel<<<plan.blocks, SORT_THREADS, 0, st>>>(q, totals);
       q.ids = nullptr;
       q.key_in = q.key_out; q.pos_in = q.pos_out;

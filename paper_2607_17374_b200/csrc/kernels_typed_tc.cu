@@ -858,12 +858,20 @@ __global__ void __launch_bounds__(256) typed_join_kernel(const JoinArgs a) {
   const int chunks = chunks_of(a, g, &first);
   const long long size = (long long)(a.K + 1) * a.N;
   const long long from = a.dW ? 0 : (long long)a.K * a.N, to = a.db ? size : (long long)a.K * a.N;
-  for (long long i = from + (long long)blockIdx.x * 256 + threadIdx.x; i < to; i += (long long)gridDim.x * 256) {
-    float s = 0.f;
-#pragma unroll 8
-    for (int c = 0; c < chunks; ++c) s += a.part[(long long)(first + c) * size + i];
-    if (i < (long long)a.K * a.N) static_cast<O*>(a.dW)[(long long)g * a.K * a.N + i] = from_f32<O>(s);
-    else a.db[(long long)g * a.N + (i - (long long)a.K * a.N)] = s;
+  const long long stride = (long long)gridDim.x * 256;
+  for (long long i0 = from + (long long)blockIdx.x * 256 + threadIdx.x; i0 < to; i0 += 4 * stride) {
+    float s[4] = {};
+#pragma unroll 2
+    for (int c = 0; c < chunks; ++c)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) if (i0 + j * stride < to) s[j] += a.part[(long long)(first + c) * size + i0 + j * stride];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const long long i = i0 + j * stride;
+      if (i >= to) break;
+      if (i < (long long)a.K * a.N) static_cast<O*>(a.dW)[(long long)g * a.K * a.N + i] = from_f32<O>(s[j]);
+      else a.db[(long long)g * a.N + (i - (long long)a.K * a.N)] = s[j];
+    }
   }
 }
 

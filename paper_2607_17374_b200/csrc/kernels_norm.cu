@@ -393,13 +393,16 @@ __device__ __forceinline__ double warp_sum(double v) {
 
 // The partial results of a long graph lie in slot 0 of the blocks of rows it meets, but for the block it begins in the middle of.
 struct Owned { long long s, begin, end, first, last; int first_slot; };
-__device__ __forceinline__ bool owned_graph(const NormArgs& a, long long blk, Owned* o) {    // the long graph that begins in block of rows blk; by every warp for itself
-  const long long r0 = blk * a.R, r1 = r0 + a.R < a.n ? r0 + a.R : a.n;
-  o->s = graph_of(a, r1 - 1);           // a long graph that begins in the block does not end in it
+// Long graph number i, if it is one: of the graphs themselves where there are fewer than blocks of rows, else the one that begins in block of rows i.  By every warp for itself.
+__device__ __forceinline__ long long owners(const NormArgs& a) { return a.graphs < a.blocks ? a.graphs : a.blocks; }
+__device__ __forceinline__ bool owned_graph(const NormArgs& a, long long i, Owned* o) {
+  const bool by_graph = a.graphs < a.blocks;
+  const long long r0 = i * a.R, r1 = r0 + a.R < a.n ? r0 + a.R : a.n;
+  o->s = by_graph ? i : graph_of(a, r1 - 1);           // (a long graph that begins in the block does not end in it)
   if (o->s < 0) return false;
   graph_rows(a, o->s, &o->begin, &o->end);
-  if (o->end - o->begin <= 2 * a.R || o->begin < r0 || o->begin >= r1) return false;
-  o->first = blk; o->last = (o->end - 1) / a.R; o->first_slot = o->begin > r0 ? 1 : 0;
+  if (o->end - o->begin <= 2 * a.R || (!by_graph && (o->begin < r0 || o->begin >= r1))) return false;
+  o->first = o->begin / a.R; o->last = (o->end - 1) / a.R; o->first_slot = o->begin > o->first * a.R ? 1 : 0;
   return true;
 }
 __device__ __forceinline__ double part_rows(const NormArgs& a, const Owned& o, long long blk) {
@@ -426,7 +429,7 @@ __device__ __forceinline__ double lane_sum(double v, bool warp) { return warp ? 
 // Grid (blocks of rows by stride, groups): joins the parts of the long graph that begins in a block of rows.
 __global__ void __launch_bounds__(32 * COMBINE_WARPS) norm_combine_kernel(const NormArgs a) {
   if (!*a.any_long) return;
-  for (long long blk0 = blockIdx.x; blk0 < a.blocks; blk0 += gridDim.x) {
+  for (long long blk0 = blockIdx.x; blk0 < owners(a); blk0 += gridDim.x) {
     Owned o;
     if (!owned_graph(a, blk0, &o)) continue;
     each_group(a, o, [&](int g, long long from, int stride, bool warp) {
@@ -499,10 +502,9 @@ struct Grads {
     *dz = to_f32<T>(dyv) * act_slope<ACT>(*xh * gamma[k] + beta[k]);
   }
 };
-// c1, c2: sums of dz xh and dz by channel; g1, g2: of gamma dz xh and gamma dz by group (of the graph at hand).
+// c1, c2: sums of dz xh and dz by channel, of the part at hand.
 template <int ACT, class T, int V, int U, bool SAME>
-__device__ __forceinline__ void add_grads(const Grads<T, V, SAME>& f, const Vec<T, V> (&v)[U], const Vec<T, V> (&w)[U], int left, float (&c1)[V], float (&c2)[V],
-                                          float (&g1)[ng<V, SAME>()], float (&g2)[ng<V, SAME>()]) {
+__device__ __forceinline__ void add_grads(const Grads<T, V, SAME>& f, const Vec<T, V> (&v)[U], const Vec<T, V> (&w)[U], int left, float (&c1)[V], float (&c2)[V]) {
 #pragma unroll
   for (int u = 0; u < U; ++u)
     if (u < left)
@@ -511,8 +513,6 @@ __device__ __forceinline__ void add_grads(const Grads<T, V, SAME>& f, const Vec<
         float xh, dz;
         f.template element<ACT>(k, v[u].v[k], w[u].v[k], &xh, &dz);
         c1[k] += dz * xh; c2[k] += dz;
-        const float q = f.gamma[k] * dz;
-        g1[SAME ? 0 : k] += q * xh; g2[SAME ? 0 : k] += q;
       }
 }
 template <int ACT, class T, int V, bool SAME>
@@ -539,11 +539,19 @@ __device__ __forceinline__ void sum_block(const NormArgs& a, const Team<V, SAME>
     if (g < a.groups && team.t == 0) out[g] = make_float2(u, v);
   }
 }
+// A part's sums by channel: weighted by gamma into red, for the groups, and added to the block's.
 template <class T, int V, bool SAME>
-__device__ __forceinline__ void put_sums(const Place<T, V, SAME>& at, const NormArgs& a, const float (&g1)[ng<V, SAME>()], const float (&g2)[ng<V, SAME>()], float2* red) {
+__device__ __forceinline__ void put_sums(const Place<T, V, SAME>& at, const NormArgs& a, const float (&gamma)[V], const float (&p1)[V], const float (&p2)[V], float (&c1)[V],
+                                         float (&c2)[V], float2* red) {
   if (!at.on) return;
+  float2 g[ng<V, SAME>()] = {};
 #pragma unroll
-  for (int k = 0; k < ng<V, SAME>(); ++k) red[(at.r * a.vpr + at.cv) * ng<V, SAME>() + k] = make_float2(g1[k], g2[k]);
+  for (int k = 0; k < V; ++k) {
+    g[SAME ? 0 : k].x += gamma[k] * p1[k]; g[SAME ? 0 : k].y += gamma[k] * p2[k];
+    c1[k] += p1[k]; c2[k] += p2[k];
+  }
+#pragma unroll
+  for (int k = 0; k < ng<V, SAME>(); ++k) red[(at.r * a.vpr + at.cv) * ng<V, SAME>() + k] = g[k];
 }
 // A block's sums by channel, its threads' added in the order of their rows; red has room for lanes x C.
 template <class T, int V, bool SAME>
@@ -591,16 +599,16 @@ __global__ void __launch_bounds__(block_limit(V)) norm_grad_short_kernel(const N
     if (rows > 0) f.set(a, at, s);
     {
       const T *p = at.at(x, a.ld_x, b), *d = at.at(dy, a.ld_dy, b);
-      float g1[ng<V, SAME>()] = {}, g2[ng<V, SAME>()] = {};
+      float p1[V] = {}, p2[V] = {};
 #pragma unroll 1
       for (int left = rows; left > 0; left -= U) {
         Vec<T, V> v[U], w[U];
         load_batch<T, V, U>(v, p, step, left);
         load_batch<T, V, U>(w, d, dstep, left);
-        add_grads<ACT>(f, v, w, left, c1, c2, g1, g2);
+        add_grads<ACT>(f, v, w, left, p1, p2);
         p += U * step; d += U * dstep;
       }
-      put_sums(at, a, g1, g2, red);
+      put_sums(at, a, f.gamma, p1, p2, c1, c2, red);
     }
     __syncthreads();
     sum_block(a, team, red, stat);
@@ -644,15 +652,15 @@ __global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_grad_stats_k
         if (parts.s[k] < 0) continue;
         f.set(a, at, parts.s[k]);
         const T *p = at.at(x, a.ld_x, parts.b[k]), *d = at.at(dy, a.ld_dy, parts.b[k]);
-        float g1[ng<V, SAME>()] = {}, g2[ng<V, SAME>()] = {};
+        float p1[V] = {}, p2[V] = {};
         for (int left = at.rows(a, parts.b[k], parts.e[k]); left > 0; left -= grad_batch<V>()) {
           Vec<T, V> v[grad_batch<V>()], w[grad_batch<V>()];
           load_batch<T, V, grad_batch<V>()>(v, p, step, left);
           load_batch<T, V, grad_batch<V>()>(w, d, dstep, left);
-          add_grads<ACT>(f, v, w, left, c1, c2, g1, g2);
+          add_grads<ACT>(f, v, w, left, p1, p2);
           p += grad_batch<V>() * step; d += grad_batch<V>() * dstep;
         }
-        put_sums(at, a, g1, g2, red);
+        put_sums(at, a, f.gamma, p1, p2, c1, c2, red);
         __syncthreads();
         sum_block(a, team, red, a.part + (blk * 2 + k) * a.groups);
         __syncthreads();
@@ -685,7 +693,7 @@ __global__ void __launch_bounds__(32 * COMBINE_WARPS) norm_grad_combine_kernel(c
     return;
   }
   if (!any_long) return;
-  for (long long blk0 = blockIdx.x; blk0 < a.blocks; blk0 += combine) {
+  for (long long blk0 = blockIdx.x; blk0 < owners(a); blk0 += combine) {
     Owned o;
     if (!owned_graph(a, blk0, &o)) continue;
     each_group(a, o, [&](int g, long long from, int stride, bool warp) {
@@ -905,7 +913,7 @@ extern "C" int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offset
       if (s.blocks > 0) {
         set_block(&a, V, ROW_THREADS, &threads);
         norm_stats_kernel<T, V, SAME><<<s.row_grid, threads, (size_t)a.lanes * a.vpr * ng<V, SAME>() * 8, st>>>(a, xp);
-        norm_combine_kernel<<<dim3((unsigned)s.row_grid, combine_columns(s.blocks, graphs, groups)), 32 * COMBINE_WARPS, 0, st>>>(a);
+        norm_combine_kernel<<<dim3((unsigned)std::min<int64_t>(s.row_grid, graphs), combine_columns(s.blocks, graphs, groups)), 32 * COMBINE_WARPS, 0, st>>>(a);
         norm_apply_kernel<T, V, SAME, ACT><<<s.row_grid, threads, (size_t)groups * 8, st>>>(a, xp, yp);
       }
     });
@@ -991,9 +999,10 @@ extern "C" int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* o
         norm_grad_stats_kernel<T, V, SAME, ACT><<<s.row_grid, threads, (size_t)a.lanes * width * 8, st>>>(a, xp, dyp);
       }
       const int channel_blocks = a.chan ? (width + 7) / 8 : 0;
-      if (s.row_grid + channel_blocks > 0)
-        norm_grad_combine_kernel<<<dim3((unsigned)(s.row_grid + channel_blocks), s.blocks > 0 ? combine_columns(s.blocks, graphs, groups) : 1u), 32 * COMBINE_WARPS, 0,
-                                   st>>>(a, s.row_grid);
+      const int owner_blocks = (int)std::min<int64_t>(s.row_grid, graphs);
+      if (owner_blocks + channel_blocks > 0)
+        norm_grad_combine_kernel<<<dim3((unsigned)(owner_blocks + channel_blocks), s.blocks > 0 ? combine_columns(s.blocks, graphs, groups) : 1u), 32 * COMBINE_WARPS, 0,
+                                   st>>>(a, owner_blocks);
       if (s.blocks > 0) norm_grad_apply_kernel<T, V, SAME, ACT><<<s.row_grid, threads, 0, st>>>(a, xp, dyp, dxp);
     });
   }

@@ -858,20 +858,12 @@ __global__ void __launch_bounds__(256) typed_join_kernel(const JoinArgs a) {
   const int chunks = chunks_of(a, g, &first);
   const long long size = (long long)(a.K + 1) * a.N;
   const long long from = a.dW ? 0 : (long long)a.K * a.N, to = a.db ? size : (long long)a.K * a.N;
-  const long long stride = (long long)gridDim.x * 256;
-  for (long long i0 = from + (long long)blockIdx.x * 256 + threadIdx.x; i0 < to; i0 += 4 * stride) {
-    float s[4] = {};
-#pragma unroll 2
-    for (int c = 0; c < chunks; ++c)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) if (i0 + j * stride < to) s[j] += a.part[(long long)(first + c) * size + i0 + j * stride];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const long long i = i0 + j * stride;
-      if (i >= to) break;
-      if (i < (long long)a.K * a.N) static_cast<O*>(a.dW)[(long long)g * a.K * a.N + i] = from_f32<O>(s[j]);
-      else a.db[(long long)g * a.N + (i - (long long)a.K * a.N)] = s[j];
-    }
+  for (long long i = from + (long long)blockIdx.x * 256 + threadIdx.x; i < to; i += (long long)gridDim.x * 256) {
+    float s = 0.f;
+#pragma unroll 16
+    for (int c = 0; c < chunks; ++c) s += a.part[(long long)(first + c) * size + i];
+    if (i < (long long)a.K * a.N) static_cast<O*>(a.dW)[(long long)g * a.K * a.N + i] = from_f32<O>(s);
+    else a.db[(long long)g * a.N + (i - (long long)a.K * a.N)] = s;
   }
 }
 
@@ -1001,7 +993,7 @@ int typed_tc_weights(int64_t n, int32_t types, const long long* offsets, const v
     with_row_type(dW ? dW_type : TAURUS_F32, [&](auto tt) {
       using O = typename decltype(tt)::type;
       const long long size = (long long)(d_in + 1) * d_out;
-      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 1023) / 1024, std::max(8, 8 * sms / types)), (unsigned)types), 256, 0, st>>>(j);
+      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 255) / 256, std::max(8, 16 * sms / types)), (unsigned)types), 256, 0, st>>>(j);
       return 0;
     });
   return TAURUS_OK;

@@ -735,8 +735,11 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     }
     if (t == 0 && !TMA_B) sh->loads = it;
   } else if constexpr (SUMS) {
-    // ------------------------------------------------------------ columns of grad_out: a thread to two columns, the halves of the block to half of the rows each
-    const int t = threadIdx.x - 32 * (2 + EPI_WARPS), half = t >> 7, c = (t & 127) * 2;
+    // ------------------------------------------------------------ columns of grad_out: a thread to two columns of a quarter of the rows (half, where the
+    // block has more than 128 columns)
+    static_assert(LOAD_WARPS * 32 == 256, "two columns and a share of the rows to a thread");
+    const int t = threadIdx.x - 32 * (2 + EPI_WARPS);
+    const int shares = a.bn > 128 ? 2 : 4, share = a.bn > 128 ? t >> 7 : t >> 6, c = (a.bn > 128 ? t & 127 : t & 63) * 2;
     float s0 = 0.f, s1 = 0.f;
     unsigned phase = 0;
     int it = 0;
@@ -745,33 +748,38 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       if (!mbar_wait_warp(&sh->full[s], it / STAGES & 1, abort_flag)) break;
       const bool mine = a.db && at.u.m0 == 0;
       if (mine && c < at.u.bw) {
-        const unsigned sb = operands + s * STAGE_BYTES + NP * PLANE_A + (c >> 6) * (BK * 128), byte = (c & 63) * 2;
-        const int rows = min(BK / 2, at.u.rows - at.k * BK - half * (BK / 2));
-        unsigned from[8];                                // the eight rows of a swizzle's period, in bytes of the operands
-#pragma unroll
-        for (int r = 0; r < 8; ++r) from[r] = sb - operands + half * (BK / 2) * 128 + r * 128 + (((byte >> 4) ^ r) << 4) + (byte & 15);
+        const unsigned byte = (c & 63) * 2, column = s * STAGE_BYTES + NP * PLANE_A + (c >> 6) * (BK * 128) + (byte & 15);
+        const int rows = min(BK, at.u.rows - at.k * BK);
+        float x0 = 0.f, x1 = 0.f;
         auto add = [&](int r) {
-          const Vec<T, 2> p = load_vec<Vec<T, 2>>(smem + from[r & 7] + (r >> 3) * 1024);
-          s0 += to_f32<T>(p.v[0]); s1 += to_f32<T>(p.v[1]);
+          const Vec<T, 2> p = load_vec<Vec<T, 2>>(smem + column + r * 128 + (((byte >> 4) ^ (r & 7)) << 4));
+          if (r & 8) { x0 += to_f32<T>(p.v[0]); x1 += to_f32<T>(p.v[1]); }
+          else { s0 += to_f32<T>(p.v[0]); s1 += to_f32<T>(p.v[1]); }
         };
-        if (rows == BK / 2) {
+        if (rows == BK && shares == 4) {
 #pragma unroll
-          for (int r = 0; r < BK / 2; ++r) add(r);
+          for (int r = 0; r < BK / 4; ++r) add(share * (BK / 4) + r);
+        } else if (rows == BK) {
+#pragma unroll
+          for (int r = 0; r < BK / 2; ++r) add(share * (BK / 2) + r);
         } else {
-#pragma unroll
-          for (int r = 0; r < BK / 2; ++r) if (r < rows) add(r);
+          for (int r = share * (BK / shares); r < min(rows, (share + 1) * (BK / shares)); ++r) add(r);
         }
+        s0 += x0; s1 += x1;
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->empty[s]);
       if (mine && at.last()) {
-        if (half == 1) { bias_smem[c] = s0; bias_smem[c + 1] = s1; }
+        float2* const red = reinterpret_cast<float2*>(bias_smem) + (c >> 1);       // [shares - 1][columns / 2]
+        const int pitch = a.bn > 128 ? 128 : 64;
+        if (share > 0) red[(share - 1) * pitch] = make_float2(s0, s1);
         if (!meet(sh, &phase)) break;
-        if (half == 0) {
+        if (share == 0) {
           float* const place = bias_place(a, at.u);
           const int columns = min(at.u.bw, a.N - at.u.n0);
-          if (c < columns) place[c] = s0 + bias_smem[c];
-          if (c + 1 < columns) place[c + 1] = s1 + bias_smem[c + 1];
+          for (int i = 1; i < shares; ++i) { const float2 o = red[(i - 1) * pitch]; s0 += o.x; s1 += o.y; }
+          if (c < columns) place[c] = s0;
+          if (c + 1 < columns) place[c + 1] = s1;
         }
         if (!meet(sh, &phase)) break;
         s0 = s1 = 0.f;
@@ -993,7 +1001,7 @@ int typed_tc_weights(int64_t n, int32_t types, const long long* offsets, const v
     with_row_type(dW ? dW_type : TAURUS_F32, [&](auto tt) {
       using O = typename decltype(tt)::type;
       const long long size = (long long)(d_in + 1) * d_out;
-      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 255) / 256, std::max(8, 16 * sms / types)), (unsigned)types), 256, 0, st>>>(j);
+      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 255) / 256, std::max(8, 4 * sms / types)), (unsigned)types), 256, 0, st>>>(j);
       return 0;
     });
   return TAURUS_OK;

@@ -68,7 +68,7 @@ struct TcArgs {
   int chunk;                  // GRAD_W: rows of a chunk
   const void *a, *b;          // LOADED: rows of A; GRAD_W: rows of B too
   long long lda, ldb;
-  int a_vec, b_vec;           // four elements at a time
+  int a_vec, b_vec;           // elements, at most four, that the rows are aligned to (fp32: four or not)
   void* out;
   long long ld_out;           // PROJECT, GRAD_X
   int out_f32;                // the output is fp32, else of the operands' type
@@ -269,21 +269,21 @@ struct Loader {
   int r0, q;               // row of the first quad in the tile, column
   const T *pa, *pb;        // where they come from
   long long da, db;        // from a quad to the next
-  int rows, left_a, left_b;  // rows of the tile from r0 on; columns from q on
+  int rows, cols_a, cols_b;  // rows of the tile from r0 on that there are; columns from the tile's first on
 
   __device__ __forceinline__ explicit Loader(int t) : r0(t / ROW_QUADS), q(t % ROW_QUADS * 4) {}
   __device__ __forceinline__ void begin(const TcArgs& a, const Unit& u) {
     const long long row = u.row0 + (long long)r0;
     rows = u.rows - r0;
     if (KIND != GRAD_W) {
-      pa = static_cast<const T*>(a.a) + row * a.lda + q; da = DR * a.lda; left_a = a.Kc - q;
+      pa = static_cast<const T*>(a.a) + row * a.lda + q; da = DR * a.lda; cols_a = a.Kc;
     } else {
-      pa = static_cast<const T*>(a.a) + (a.a ? row * a.lda + u.m0 + q : 0); da = DR * a.lda; left_a = a.a ? a.M - u.m0 - q : 0;
-      pb = static_cast<const T*>(a.b) + row * a.ldb + u.n0 + q; db = DR * a.ldb; left_b = q < u.bw ? a.N - u.n0 - q : 0;
+      pa = static_cast<const T*>(a.a) + (a.a ? row * a.lda + u.m0 + q : 0); da = DR * a.lda; cols_a = a.a ? a.M - u.m0 : 0;
+      pb = static_cast<const T*>(a.b) + row * a.ldb + u.n0 + q; db = DR * a.ldb; cols_b = min(u.bw, a.N - u.n0);
     }
   }
   __device__ __forceinline__ void step(const TcArgs& a) {
-    if (KIND != GRAD_W) { pa += BK; left_a -= BK; }
+    if (KIND != GRAD_W) { pa += BK; cols_a -= BK; }
     else { pa += BK * a.lda; pb += BK * a.ldb; rows -= BK; }
   }
   // f(quad, its address, elements of it that there are: 4 or fewer, perhaps none; of A?)
@@ -292,9 +292,32 @@ struct Loader {
 #pragma unroll
     for (int i = 0; i < QUADS; ++i) {
       const bool in = i * DR < rows;
-      f(i, pa + i * da, in ? left_a : 0, true);
-      if constexpr (KIND == GRAD_W) f(QUADS + i, pb + i * db, in ? left_b : 0, false);
+      f(i, pa + i * da, in ? cols_a - q : 0, true);
+      if constexpr (KIND == GRAD_W) f(QUADS + i, pb + i * db, in ? cols_b - q : 0, false);
     }
+  }
+  // The same elements by the warp as a whole, neighbouring lanes neighbouring elements, W at a time, for rows that are not aligned to quads:
+  // f(quad group, element of the warp's 128 in it, row and column in the tile, address, elements that there are, of A?)
+  template <int W, class F>
+  __device__ __forceinline__ void wide(const TcArgs& a, F f) const {
+    const int lane = threadIdx.x & 31, dr = lane / ROW_QUADS;
+    auto operand = [&](int group, const T* p, long long ld, int cols, bool is_a) {
+      p -= dr * ld + q;                                            // the warp's first row, the tile's first column
+#pragma unroll
+      for (int i = 0; i < QUADS; ++i)
+#pragma unroll
+        for (int j = 0; j < 4 / W; ++j) {
+          const int e = (j * 32 + lane) * W, r = e / (4 * ROW_QUADS) + i * DR, c = e % (4 * ROW_QUADS);
+          f(group + i, e, r0 - dr + r, c, p + r * ld + c, r < rows + dr ? min(max(cols - c, 0), W) : 0, is_a);
+        }
+    };
+    operand(0, pa, a.lda, cols_a, true);
+    if constexpr (KIND == GRAD_W) operand(QUADS, pb, a.ldb, cols_b, false);
+  }
+  // Bytes of element (r, c) of the tile behind its operand's A stage.
+  static __device__ __forceinline__ unsigned place_of(int r, int c, bool is_a) {
+    if constexpr (KIND != GRAD_W) return r * (BK * 2) + (((c >> 3) ^ (BK == 64 ? r & 7 : (r >> 1) & 3)) << 4) + (c & 7) * 2;
+    return (is_a ? 0u : Shape<T, KIND, true>::NP * PLANE) + (c >> 6) * (BK * 128) + r * 128 + ((((c & 63) >> 3) ^ (r & 7)) << 4) + (c & 7) * 2;
   }
   // Bytes of quad i in its operand's plane.
   __device__ __forceinline__ unsigned place(int i) const {
@@ -347,13 +370,21 @@ __device__ __forceinline__ void put_rows(unsigned char* tile, const float* v, O*
       p += AT_ONCE * ld;
     }
   } else {
-    constexpr int FEW = PASS < 32 ? 32 / PASS : 1, WIDE = PASS < 32 ? 1 : PASS / 32;   // rows at once; times 32 columns
-    for (int r = lane / (32 / FEW); r < rows; r += FEW)
+    static_assert(PASS <= 32, "a lane to a column");
+    constexpr int FEW = 32 / PASS, BATCH = 8;            // rows at once; of them on their way
+    const int c = lane % PASS, r0 = lane / PASS;
+    O* p = out + r0 * ld + c;
+#pragma unroll 1
+    for (int r = r0; r < rows; r += FEW * BATCH) {
+      O x[BATCH];
 #pragma unroll
-      for (int i = 0; i < WIDE; ++i) {
-        const int c = i * 32 + lane % (32 / FEW);
-        if (c < columns) out[r * ld + c] = *reinterpret_cast<const O*>(tile + tile_at<O, ROW>(r, c / PER) + c % PER * sizeof(O));
+      for (int i = 0; i < BATCH; ++i) x[i] = *reinterpret_cast<const O*>(tile + tile_at<O, ROW>((r + i * FEW) & 31, c / PER) + c % PER * sizeof(O));
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) {
+        if (r + i * FEW < rows && c < columns) *p = x[i];
+        p += FEW * ld;
       }
+    }
   }
   __syncwarp();
 }
@@ -634,25 +665,25 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     };
     const void* const nothing = a.offsets;              // (an address for a copy that reads nothing)
     if constexpr (NP == 3) {
-      // a ring of rows as they were read, filled DEPTH stages ahead; quad i of thread t lies at (i LOADERS + t) 16: a thread reads only what it copied itself
+      // a ring of rows as they were read, filled DEPTH stages ahead; quad i of thread t lies at (i LOADERS + t) 16: a warp reads only what it copied itself
       constexpr int DEPTH = S::RAW_DEPTH;
       unsigned char* const ring = smem + STAGES * STAGE_BYTES;
       auto copy = [&](int i) {
         if (ahead.w < units) {
           const unsigned slot = smem_u32(ring) + i % DEPTH * S::RAW_BYTES + t * 16;
           if (a.a_vec && (KIND != GRAD_W || a.b_vec) && ld.rows > (L::QUADS - 1) * L::DR) {      // every row is there
-            const unsigned na = min(max(ld.left_a, 0), 4) * 4, nb = KIND == GRAD_W ? min(max(ld.left_b, 0), 4) * 4 : 0;
+            const unsigned na = min(max(ld.cols_a - ld.q, 0), 4) * 4, nb = KIND == GRAD_W ? min(max(ld.cols_b - ld.q, 0), 4) * 4 : 0;
             ld.each([&](int i, const T* p, int, bool is_a) { copy16(slot + i * (L::LOADERS * 16), (is_a ? na : nb) ? static_cast<const void*>(p) : nothing, is_a ? na : nb); });
-          } else ld.each([&](int i, const T* p, int left, bool is_a) {
-            left = min(max(left, 0), 4);
-            const unsigned dst = slot + i * (L::LOADERS * 16);
-            if (is_a ? a.a_vec : a.b_vec) {
-              copy16(dst, left > 0 ? static_cast<const void*>(p) : nothing, left * 4);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) copy4(dst + 4 * j, j < left ? static_cast<const void*>(p + j) : nothing, j < left ? 4 : 0);
-            }
-          });
+          } else if (a.a_vec && (KIND != GRAD_W || a.b_vec)) {
+            ld.each([&](int i, const T* p, int left, bool) {
+              left = min(max(left, 0), 4);
+              copy16(slot + i * (L::LOADERS * 16), left > 0 ? static_cast<const void*>(p) : nothing, left * 4);
+            });
+          } else {
+            // (a quad's elements are copied by lanes of its warp)
+            const unsigned warp_slot = slot - (t & 31) * 16;
+            ld.template wide<1>(a, [&](int i, int e, int, int, const T* p, int left, bool) { copy4(warp_slot + i * (L::LOADERS * 16) + e * 4, left > 0 ? static_cast<const void*>(p) : nothing, left * 4); });
+          }
           go_on();
         }
         copy_commit();
@@ -661,6 +692,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       for (; at.w < units; ++it) {
         const int s = it % STAGES;
         copy_wait<DEPTH - 1>();
+        __syncwarp();
         const float4* const mine = reinterpret_cast<const float4*>(ring + it % DEPTH * S::RAW_BYTES) + t;
         float4 v[L::ALL];
 #pragma unroll
@@ -668,6 +700,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         if (KIND == GRAD_W)
 #pragma unroll
           for (int i = L::QUADS; i < L::ALL; ++i) add(v[i].x, v[i].y, v[i].z, v[i].w);
+        __syncwarp();
         copy(it + DEPTH);                               // (into the slot just read)
         if (!free_stage(it)) break;
         unsigned char* const stage = smem + s * STAGE_BYTES;
@@ -684,14 +717,27 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         at.next(a, sh, units);
       }
       copy_wait<0>();
-    } else if (a.a_vec && (KIND != GRAD_W || a.b_vec)) {
-      // rows whose quads are 8 bytes of aligned memory: copied to their places, AHEAD stages in flight
+    } else {
+      // copied to their places, AHEAD stages in flight: quads of 8 bytes, or pairs of elements, by the rows' alignment; odd rows go through registers
       constexpr int AHEAD = 2;
+      const bool quads = a.a_vec == 4 && (KIND != GRAD_W || a.b_vec == 4), pairs = a.a_vec >= 2 && (KIND != GRAD_W || a.b_vec >= 2);
       auto copy = [&](int i) -> bool {
         if (ahead.w < units) {
           if (!free_stage(i)) return false;
-          const unsigned stage = operands + i % STAGES * STAGE_BYTES;
-          ld.each([&](int i, const T* p, int left, bool) { copy8(stage + ld.place(i), left > 0 ? static_cast<const void*>(p) : nothing, min(max(left, 0), 4) * 2); });
+          const unsigned stage = i % STAGES * STAGE_BYTES;
+          if (quads) {
+            ld.each([&](int i, const T* p, int left, bool) {
+              copy8(operands + stage + ld.place(i), left > 0 ? static_cast<const void*>(p) : nothing, min(max(left, 0), 4) * 2);
+            });
+          } else if (pairs) {
+            ld.template wide<2>(a, [&](int, int, int r, int c, const T* p, int left, bool is_a) {
+              copy4(operands + stage + L::place_of(r, c, is_a), left > 0 ? static_cast<const void*>(p) : nothing, left * 2);
+            });
+          } else {
+            ld.template wide<1>(a, [&](int, int, int r, int c, const T* p, int left, bool is_a) {
+              *reinterpret_cast<T*>(smem + stage + L::place_of(r, c, is_a)) = left > 0 ? __ldg(p) : from_f32<T>(0.f);
+            });
+          }
           go_on();
         }
         copy_commit();
@@ -702,6 +748,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       for (; ok && at.w < units; ++it) {
         if (!copy(it + AHEAD)) break;
         copy_wait<AHEAD>();
+        __syncwarp();
         if (KIND == GRAD_W && a.db && at.u.m0 == 0)
 #pragma unroll
           for (int i = L::QUADS; i < L::ALL; ++i) {
@@ -713,25 +760,6 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         at.next(a, sh, units);
       }
       copy_wait<0>();
-    } else {
-      // element by element
-      for (; at.w < units; ++it) {
-        Vec<T, 4> v[L::ALL];
-        ld.each([&](int i, const T* p, int left, bool) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[i].v[j] = j < left ? p[j] : from_f32<T>(0.f);
-        });
-        go_on();
-        if (!free_stage(it)) break;
-#pragma unroll
-        for (int i = 0; i < L::ALL; ++i) {
-          if (KIND == GRAD_W && i >= L::QUADS) add(to_f32<T>(v[i].v[0]), to_f32<T>(v[i].v[1]), to_f32<T>(v[i].v[2]), to_f32<T>(v[i].v[3]));
-          store_vec(smem + it % STAGES * STAGE_BYTES + ld.place(i), v[i]);
-        }
-        arrive(it % STAGES);
-        if (!bias_sums()) break;
-        at.next(a, sh, units);
-      }
     }
     if (t == 0 && !TMA_B) sh->loads = it;
   } else if constexpr (SUMS) {
@@ -896,6 +924,12 @@ bool make_map(CUtensorMap* m, int32_t type, const void* base, long long cols, lo
                      one, CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// TcArgs::a_vec
+int vec_of(const void* p, long long ld, int size) {
+  int v = 4;
+  while (v > 1 && (ld % v != 0 || !rows_aligned(p, v * size))) v >>= 1;
+  return size == 4 && v < 4 ? 0 : v;
+}
 bool tma_rows(const void* p, long long ld) { return ld % 8 == 0 && rows_aligned(p, 16); }      // of 16-bit elements
 
 // Blocks of nearly equal width, a multiple of 16.
@@ -964,7 +998,7 @@ int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* of
   TcArgs a = {};
   a.n = n; a.offsets = offsets; a.types = types; a.N = N; a.Kc = Kc;
   a.bn = block_columns(N, bn_most(type, false, loaded)); a.n_blocks = (N + a.bn - 1) / a.bn;
-  a.a = x; a.lda = ld_x; a.a_vec = ld_x % 4 == 0 && rows_aligned(x, 4 * row_type_size(type));
+  a.a = x; a.lda = ld_x; a.a_vec = vec_of(x, ld_x, row_type_size(type));
   a.out = out; a.ld_out = ld_out; a.out_f32 = out_type == TAURUS_F32; a.out_vec = ld_out * row_type_size(out_type) % 16 == 0 && rows_aligned(out, 16);
   a.bias = bias; a.status = status;
   const long long pitch = typed_tc_packs(type, d_out) ? weight_pitch(d_out) : d_out;
@@ -986,8 +1020,8 @@ int typed_tc_weights(int64_t n, int32_t types, const long long* offsets, const v
   TcArgs a = {};
   a.n = n; a.offsets = offsets; a.types = types; a.M = d_in; a.N = d_out; a.chunk = chunk;
   a.bn = block_columns(d_out, bn_most(type, true, loaded)); a.n_blocks = (d_out + a.bn - 1) / a.bn; a.m_blocks = dW ? (d_in + BM - 1) / BM : 1;
-  a.a = dW ? x : nullptr; a.lda = ld_x; a.a_vec = ld_x % 4 == 0 && rows_aligned(x, 4 * size);
-  a.b = dy; a.ldb = ld_dy; a.b_vec = ld_dy % 4 == 0 && rows_aligned(dy, 4 * size);
+  a.a = dW ? x : nullptr; a.lda = ld_x; a.a_vec = vec_of(x, ld_x, size);
+  a.b = dy; a.ldb = ld_dy; a.b_vec = vec_of(dy, ld_dy, size);
   a.out = dW; a.out_f32 = dW_type == TAURUS_F32; a.out_vec = d_out * out_size % 16 == 0 && d_out % 4 == 0 && rows_aligned(dW, 16);
   a.db = db; a.part = part; a.status = status;
   CUtensorMap ma = {}, mb = {};
@@ -1001,7 +1035,7 @@ int typed_tc_weights(int64_t n, int32_t types, const long long* offsets, const v
     with_row_type(dW ? dW_type : TAURUS_F32, [&](auto tt) {
       using O = typename decltype(tt)::type;
       const long long size = (long long)(d_in + 1) * d_out;
-      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 255) / 256, std::max(8, 4 * sms / types)), (unsigned)types), 256, 0, st>>>(j);
+      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 255) / 256, std::max(8, 16 * sms / types)), (unsigned)types), 256, 0, st>>>(j);
       return 0;
     });
   return TAURUS_OK;

@@ -29,6 +29,7 @@ SHAPES = [
     ([1], 1, 1), ([5], 100, 256), ([0, 3, 0], 37, 130), ([-2, 1, 0, 2, 1, -3], 64, 64), ([130, 1, 127, 128, 129], 128, 128), ([300, 0, 41, 7], 33, 47),
     ([1000], 100, 256), ([257, 511], 512, 200), ([64] * 20, 16, 24), ([700, 90], 1000, 72), ([90, 333], 72, 1000), ([-5, 400, 200, -9], 96, 96), ([2] * 300, 40, 40),
     ([2600], 48, 264), ([5000, 3], 24, 16),
+    ([300, 50, 0, 1], 46, 58), ([64], 50, 36), ([65], 36, 50), ([1500, 1030, 40], 66, 130),
 ]
 
 
@@ -198,6 +199,22 @@ def test_gradients_against_differences():
         i = 0 if grad is dx else 1
         step = plus[i].double() - minus[i].double()
         assert abs((a - b) - float((grad.double() * step).sum())) <= (ma + mb) * (sums(K) + sums(N if grad is dx else 333))
+
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("K,N", [(40, 24), (33, 47)])
+def test_weights_at_any_element(t, K, N):
+    """Weights that begin at an odd element of their storage."""
+    off, n, x, W, bias, dy = make([70, 0, 130], K, N, t)
+    V = torch.empty(W.numel() + 1, dtype=t, device="cuda")[1:].view(W.shape)
+    V.copy_(W)
+    out, dx = torch.empty(n, N, device="cuda"), torch.empty(n, K, dtype=t, device="cuda")
+    forward(off, n, x, V, bias, out)
+    backward(off, n, x, V, dy, dx, None, None)
+    ref, mag = typed(off, x, W, bias)
+    close(out, ref, mag * sums(K))
+    (rx, mx), _, _ = typed_grad(off, x, W, dy)
+    close(dx, rx, mx * sums(N))
 
 
 def test_without_rows():

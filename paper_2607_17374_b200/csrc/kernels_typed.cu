@@ -97,23 +97,32 @@ typed_few_dx_kernel(long long n, int types, const long long* __restrict__ offset
   }
 }
 
-// A thread to an element of grad_W (row K of it stands for the bias), which walks the rows of its type.
-template <class T, class O>
+// A thread to V neighbouring elements of a row of grad_W (row K of it stands for the bias), which walks the rows of its type.
+template <class T, class O, int V>
 __global__ void __launch_bounds__(FEW_THREADS)
 typed_few_dw_kernel(long long n, int types, const long long* __restrict__ offsets, const T* __restrict__ x, long long ld_x, const T* __restrict__ dy,
                     long long ld_dy, int K, int N, O* __restrict__ dW, float* __restrict__ db, int32_t* status) {
   if (blockIdx.x == 0 && blockIdx.y == 0) check_offsets(offsets, types, n, status);
+  const int vpr = N / V, vectors = (K + 1) * vpr;
   for (int g = blockIdx.y; g < types; g += gridDim.y) {
     long long b, e;
     group_rows(offsets, g, n, &b, &e, nullptr);
-    for (long long i = (long long)blockIdx.x * FEW_THREADS + threadIdx.x; i < (long long)(K + 1) * N; i += (long long)gridDim.x * FEW_THREADS) {
-      const int k = (int)(i / N), c = (int)(i % N);
+    for (int i = blockIdx.x * FEW_THREADS + threadIdx.x; i < vectors; i += gridDim.x * FEW_THREADS) {
+      const int k = i / vpr, c = (i - k * vpr) * V;
       if (k == K ? !db : !dW) continue;
-      float acc = 0.f;
+      float acc[V] = {};
 #pragma unroll 4
-      for (long long r = b; r < e; ++r) acc += (k == K ? 1.f : to_f32<T>(x[r * ld_x + k])) * to_f32<T>(dy[r * ld_dy + c]);
-      if (k == K) db[(long long)g * N + c] = acc;
-      else dW[(long long)g * K * N + i] = from_f32<O>(acc);
+      for (long long r = b; r < e; ++r) {
+        const float a = k == K ? 1.f : to_f32<T>(x[r * ld_x + k]);
+        float d[V];
+        load_f32<T, V>(dy + r * ld_dy + c, d);
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += a * d[j];
+      }
+      if (k == K)
+#pragma unroll
+        for (int j = 0; j < V; ++j) db[(long long)g * N + c + j] = acc[j];
+      else store_f32<O, V>(dW + ((long long)g * K + k) * N + c, acc);
     }
   }
 }
@@ -164,12 +173,13 @@ bool space_ok(const void* p, int64_t bytes, int64_t need, int dev, const Region 
 extern "C" int64_t taurus_typed_project_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type) {
   if (!typed_shape_ok(n, types, d_in, d_out, type)) return TAURUS_ERR_INVALID_ARG;
   if (!typed_supported(types, d_in, d_out)) return TAURUS_ERR_UNSUPPORTED;
-  return n > FEW_ROWS ? (int64_t)up(typed_tc_pack_bytes(types, d_in, d_out, type)) : 0;
+  return n > FEW_ROWS ? (int64_t)(up(typed_tc_pack_bytes(types, d_in, d_out, type)) + up(typed_tc_row_bytes(n, d_in, type))) : 0;
 }
 extern "C" int64_t taurus_typed_project_grad_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type) {
   if (!typed_shape_ok(n, types, d_in, d_out, type)) return TAURUS_ERR_INVALID_ARG;
   if (!typed_supported(types, d_in, d_out)) return TAURUS_ERR_UNSUPPORTED;
-  return n > FEW_ROWS ? (int64_t)(up(typed_tc_pack_bytes(types, d_in, d_out, type)) + up(typed_tc_part_bytes(n, types, d_in, d_out, type))) : 0;
+  return n > FEW_ROWS ? (int64_t)(up(typed_tc_pack_bytes(types, d_in, d_out, type)) + up(typed_tc_part_bytes(n, types, d_in, d_out, type)) + up(typed_tc_row_bytes(n, d_in, type)) +
+                                 up(typed_tc_row_bytes(n, d_out, type))) : 0;
 }
 
 extern "C" int taurus_typed_project(int64_t n, int32_t types, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, const void* W,
@@ -198,7 +208,14 @@ extern "C" int taurus_typed_project(int64_t n, int32_t types, const int64_t* off
   if (on_tensor_cores(n, type, W, d_out)) {
     const bool packs = typed_tc_packs(type, d_out);
     if (packs) rc = typed_tc_pack(type, W, types, d_in, d_out, workspace, sms, st);
-    if (!rc) rc = typed_tc_rows(false, n, types, off, x, ld_x, type, packs ? workspace : W, bias, d_in, d_out, out, out_type, ld_out, status, sms, st);
+    const void* rows = x;
+    int64_t ld_rows = ld_x;
+    if (typed_tc_packs_rows(x, ld_x, d_in, type)) {
+      void* const at = static_cast<char*>(workspace) + up(typed_tc_pack_bytes(types, d_in, d_out, type));
+      typed_tc_pack_rows(x, ld_x, n, d_in, at, sms, st);
+      rows = at; ld_rows = typed_tc_row_pitch(d_in);
+    }
+    if (!rc) rc = typed_tc_rows(false, n, types, off, rows, ld_rows, type, packs ? workspace : W, bias, d_in, d_out, out, out_type, ld_out, status, sms, st);
   } else with_row_type(type, [&](auto tt) {
     using T = typename decltype(tt)::type;
     return with_vector(vector_of(ts, W, d_out), [&](auto vc) {
@@ -252,11 +269,25 @@ extern "C" int taurus_typed_project_grad(int64_t n, int32_t types, const int64_t
     const bool packs = typed_tc_packs(type, d_out);
     char* const space = static_cast<char*>(workspace);
     if (grad_x && packs) rc = typed_tc_pack(type, W, types, d_in, d_out, space, sms, st);
+    // the rows at other pitches, where they need it: behind the partial results
+    char* at = space + up(typed_tc_pack_bytes(types, d_in, d_out, type)) + up(typed_tc_part_bytes(n, types, d_in, d_out, type));
+    auto laid_out = [&](const void** rows, int64_t* ld, int width) {
+      if (typed_tc_packs_rows(*rows, *ld, width, type)) {
+        typed_tc_pack_rows(*rows, *ld, n, width, at, sms, st);
+        *rows = at; *ld = typed_tc_row_pitch(width);
+      }
+      at += up(typed_tc_row_bytes(n, width, type));
+    };
+    const void *dy_rows = grad_out, *x_rows = x;
+    int64_t ld_dy_rows = ld_grad, ld_x_rows = ld_x;
+    laid_out(&dy_rows, &ld_dy_rows, d_out);
+    if (grad_W) laid_out(&x_rows, &ld_x_rows, d_in);
+    else if (x && typed_tc_packs_rows(x, ld_x, d_in, type)) x_rows = nullptr;      // (grad_bias as beside grad_W)
     if (!rc && grad_x)
-      rc = typed_tc_rows(true, n, types, off, grad_out, ld_grad, type, packs ? space : W, nullptr, d_in, d_out, grad_x, type, ld_grad_x, status, sms, st);
+      rc = typed_tc_rows(true, n, types, off, dy_rows, ld_dy_rows, type, packs ? space : W, nullptr, d_in, d_out, grad_x, type, ld_grad_x, status, sms, st);
     float* const part = reinterpret_cast<float*>(space + up(typed_tc_pack_bytes(types, d_in, d_out, type)));
     if (!rc && (grad_W || grad_bias))
-      rc = typed_tc_weights(n, types, off, x, ld_x, type, grad_out, ld_grad, d_in, d_out, grad_W, grad_W_type, grad_bias, part, status, sms, st);
+      rc = typed_tc_weights(n, types, off, x_rows, ld_x_rows, type, dy_rows, ld_dy_rows, d_in, d_out, grad_W, grad_W_type, grad_bias, part, status, sms, st);
   } else with_row_type(type, [&](auto tt) {
     using T = typename decltype(tt)::type;
     const T *const xp = static_cast<const T*>(x), *const wp = static_cast<const T*>(W), *const dyp = static_cast<const T*>(grad_out);
@@ -271,11 +302,19 @@ extern "C" int taurus_typed_project_grad(int64_t n, int32_t types, const int64_t
         return 0;
       });
     if (grad_W || grad_bias) {
-      const dim3 grid((unsigned)std::min<long long>(((long long)(d_in + 1) * d_out + FEW_THREADS - 1) / FEW_THREADS, 1024), (unsigned)types);
-      if (grad_W_type == type)
-        typed_few_dw_kernel<T, T><<<grid, FEW_THREADS, 0, st>>>(n, types, off, xp, ld_x, dyp, ld_grad, d_in, d_out, static_cast<T*>(grad_W), grad_bias, status);
-      else
-        typed_few_dw_kernel<T, float><<<grid, FEW_THREADS, 0, st>>>(n, types, off, xp, ld_x, dyp, ld_grad, d_in, d_out, static_cast<float*>(grad_W), grad_bias, status);
+      const bool four = vector_of(ts, grad_out, ld_grad) >= 4 && d_out % 4 == 0 && rows_aligned(grad_W, 16);
+      auto go = [&](auto vc, auto* dw) {
+        constexpr int V = decltype(vc)::value;
+        using O = std::remove_pointer_t<decltype(dw)>;
+        const dim3 grid((unsigned)std::min((((d_in + 1) * (d_out / V)) + FEW_THREADS - 1) / FEW_THREADS, 1024), (unsigned)types);
+        typed_few_dw_kernel<T, O, V><<<grid, FEW_THREADS, 0, st>>>(n, types, off, xp, ld_x, dyp, ld_grad, d_in, d_out, dw, grad_bias, status);
+      };
+      auto with_output = [&](auto vc) {
+        if (grad_W_type == type) go(vc, static_cast<T*>(grad_W));
+        else go(vc, static_cast<float*>(grad_W));
+      };
+      if (four) with_output(std::integral_constant<int, 4>());
+      else with_output(std::integral_constant<int, 1>());
     }
     return 0;
   });

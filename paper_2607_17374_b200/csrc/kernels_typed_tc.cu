@@ -854,6 +854,35 @@ __global__ void __launch_bounds__(256) typed_pack_kernel(const T* __restrict__ W
   }
 }
 
+// Rows of 16-bit elements whose pitch TMA cannot take, to a pitch that it can: 16 bytes a thread, from words of 4 bytes shifted where a row begins in the middle of one.
+__global__ void __launch_bounds__(256) typed_pack_rows_kernel(const unsigned short* __restrict__ rows, long long ld, long long n, int width, int pitch, uint4* __restrict__ out) {
+  const int chunks = pitch / 8;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n * chunks; i += (long long)gridDim.x * 256) {
+    const long long r = i / chunks;
+    const int c = (int)(i - r * chunks) * 8;
+    const unsigned short* const p = rows + r * ld + c;
+    union { unsigned w[4]; unsigned short h[8]; uint4 v; } x;
+    if (c + 8 <= width) {
+      const unsigned odd = (unsigned)(reinterpret_cast<uintptr_t>(p) >> 1) & 1u;
+      if (odd) {                                           // h[0] | four words, the last of which ends the chunk with its first half
+        const unsigned* const q = reinterpret_cast<const unsigned*>(p + 1);
+        unsigned before = (unsigned)__ldg(p) << 16;
+#pragma unroll
+        for (int j = 0; j < 3; ++j) { const unsigned w = __ldg(q + j); x.w[j] = __funnelshift_l(before, w, 16); before = w; }
+        x.w[3] = before >> 16 | (unsigned)__ldg(p + 7) << 16;
+      } else {
+        const unsigned* const q = reinterpret_cast<const unsigned*>(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.w[j] = __ldg(q + j);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x.h[j] = c + j < width ? __ldg(p + j) : (unsigned short)0;
+    }
+    out[i] = x.v;
+  }
+}
+
 // ---------------------------------------------------------------------------------------------------------------- joins
 struct JoinArgs {
   long long n;
@@ -964,6 +993,15 @@ bool typed_tc_usable() { return encode_fn() != nullptr; }
 bool typed_tc_packs(int32_t type, int d_out) { return type == TAURUS_F32 || d_out % 8 != 0; }
 size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type) {
   return typed_tc_packs(type, d_out) ? (size_t)types * (type == TAURUS_F32 ? 3 : 1) * d_in * weight_pitch(d_out) * 2 : 0;
+}
+// Rows of a width that keeps TMA off, fp32 aside: room for them at another pitch, and whether these need it (rows of such a width whose own pitch suits TMA do not).
+int64_t typed_tc_row_pitch(int width) { return taurus_round_up(width, 8); }
+size_t typed_tc_row_bytes(int64_t n, int width, int32_t type) { return type == TAURUS_F32 || width % 8 == 0 ? 0 : (size_t)n * (size_t)typed_tc_row_pitch(width) * 2; }
+bool typed_tc_packs_rows(const void* p, int64_t ld, int width, int32_t type) { return typed_tc_row_bytes(1, width, type) > 0 && !tma_rows(p, ld); }
+void typed_tc_pack_rows(const void* rows, int64_t ld, int64_t n, int width, void* packed, int sms, cudaStream_t st) {
+  const int pitch = (int)typed_tc_row_pitch(width);
+  const int grid = (int)std::min<long long>((n * (pitch / 8) + 255) / 256, (long long)sms * 32);
+  typed_pack_rows_kernel<<<grid, 256, 0, st>>>(static_cast<const unsigned short*>(rows), ld, n, width, pitch, static_cast<uint4*>(packed));
 }
 // Rows of a chunk of grad_W: about two units to an SM, 1 024 rows at least, 4 096 at most.  fp32: 1 024; the tensor core's sums are cut off, not rounded, and over
 // 2 700 rows (400 000 in 5 types) that made an error of 2.9e-6 of the result where fp32 sums have 1.1e-6.

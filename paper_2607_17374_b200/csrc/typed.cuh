@@ -41,6 +41,10 @@ static __device__ __forceinline__ Split4 split4(float a, float b, float c, float
 bool typed_tc_usable();
 bool typed_tc_packs(int32_t type, int d_out);
 size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type);
+size_t typed_tc_row_bytes(int64_t n, int width, int32_t type);
+int64_t typed_tc_row_pitch(int width);
+bool typed_tc_packs_rows(const void* p, int64_t ld, int width, int32_t type);
+void typed_tc_pack_rows(const void* rows, int64_t ld, int64_t n, int width, void* packed, int sms, cudaStream_t st);
 size_t typed_tc_part_bytes(int64_t n, int32_t types, int d_in, int d_out, int32_t type);
 int typed_tc_pack(int32_t type, const void* W, int32_t types, int d_in, int d_out, void* packed, int sms, cudaStream_t st);
 int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* w, const float* bias, int d_in, int d_out,

@@ -246,24 +246,32 @@ def _dtype_name(dtype) -> str:
 
 
 _ROW_TYPES = {"float32": F32, "bfloat16": BF16, "float16": F16}
+_row_codes: dict = {}        # dtype -> F32, BF16 or F16
 
 
 def _row_type(t) -> int:
     """F32, BF16 or F16 of a torch or numpy dtype, of a tensor or array, or as it is given (F32, ...)."""
     if isinstance(t, int):
         return t
-    name = _dtype_name(getattr(t, "dtype", t))
-    if name not in _ROW_TYPES:
-        raise TypeError("rows are float32, bfloat16 or float16, got %s" % name)
-    return _ROW_TYPES[name]
+    dtype = getattr(t, "dtype", t)
+    code = _row_codes.get(dtype)
+    if code is None:
+        name = _dtype_name(dtype)
+        if name not in _ROW_TYPES:
+            raise TypeError("rows are float32, bfloat16 or float16, got %s" % name)
+        code = _row_codes[dtype] = _ROW_TYPES[name]
+    return code
 
 
 def _rows(x, n: int, width: int, ld: int) -> Optional[int]:
     """Address of n rows: a 2-D tensor of at least n x width whose rows are contiguous and ld elements apart, or an address."""
     if x is None or isinstance(x, int):
         return x
-    shape, stride = x.shape, x.stride()
-    if len(shape) != 2 or shape[0] < n or shape[1] < width or (stride[1] != 1 and shape[1] > 1) or (stride[0] != ld and shape[0] > 1):
+    try:
+        (rows, columns), (apart, step) = x.shape, x.stride()
+    except ValueError:
+        raise ValueError("expected a matrix of rows") from None
+    if rows < n or columns < width or (apart != ld and rows > 1) or (step != 1 and columns > 1):
         raise ValueError("expected at least %d contiguous rows of %d elements, %d elements apart" % (n, width, ld))
     return x.data_ptr()
 
@@ -272,11 +280,13 @@ def _array(x, dtype: Optional[str], count: int) -> Optional[int]:
     """Address of a contiguous tensor of at least count elements of that dtype, or an address."""
     if x is None or isinstance(x, int):
         return x
-    if dtype and _dtype_name(x.dtype) != dtype:
+    if dtype and _dtype_names.get(x.dtype) != dtype and _dtype_name(x.dtype) != dtype:
         raise TypeError("expected %s, got %s" % (dtype, x.dtype))
     if x.numel() < count:
         raise ValueError("expected at least %d elements, got %d" % (count, x.numel()))
-    return _ptr(x)
+    if not x.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    return x.data_ptr()
 
 
 def _space(workspace):

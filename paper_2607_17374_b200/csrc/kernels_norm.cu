@@ -266,6 +266,7 @@ constexpr int row_blocks(int v) { return row_limit(v) > 768 ? 1 : 768 / row_limi
 // (64 registers a thread, a few of them in local memory: 2 000 graphs of 250 x 256 fp32, forward and backward, 801 -> 752 us)
 template <class T, int V, bool SAME, int ACT>
 __global__ void __launch_bounds__(block_limit(V), V > 1 ? 2 : 1) norm_short_kernel(const NormArgs a, const T* x, T* y) {
+  early_start();
   float2* const red = shared_red();
   float2* const stat = red + (size_t)a.lanes * a.vpr * ng<V, SAME>();
   const Place<T, V, SAME> at(a);
@@ -361,6 +362,7 @@ __device__ __forceinline__ void find_parts(const NormArgs& a, long long blk, Par
 
 template <class T, int V, bool SAME>
 __global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_stats_kernel(const NormArgs a, const T* x) {
+  early_start();
   __shared__ Parts parts;
   if (!*a.any_long) return;
   float2* const red = shared_red();
@@ -429,6 +431,7 @@ __device__ __forceinline__ double lane_sum(double v, bool warp) { return warp ? 
 
 // Grid (blocks of rows by stride, groups): joins the parts of the long graph that begins in a block of rows.
 __global__ void __launch_bounds__(32 * COMBINE_WARPS) norm_combine_kernel(const NormArgs a) {
+  early_start();
   if (!*a.any_long) return;
   for (long long blk0 = blockIdx.x; blk0 < owners(a); blk0 += gridDim.x) {
     Owned o;
@@ -457,6 +460,7 @@ __global__ void __launch_bounds__(32 * COMBINE_WARPS) norm_combine_kernel(const 
 // From the last block of rows to the first: the last ones read are still in the L2.
 template <class T, int V, bool SAME, int ACT>
 __global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_apply_kernel(const NormArgs a, const T* x, T* y) {
+  early_start();
   __shared__ Parts parts;
   if (!*a.any_long) return;
   const Place<T, V, SAME> at(a);
@@ -571,6 +575,7 @@ __device__ __forceinline__ void put_channels(const Place<T, V, SAME>& at, const 
 
 template <class T, int V, bool SAME, int ACT>
 __global__ void __launch_bounds__(block_limit(V)) norm_grad_short_kernel(const NormArgs a, const T* x, const T* dy, T* dx) {
+  early_start();
   float2* const stat = shared_red();
   float2* const red = stat + a.groups;
   const Place<T, V, SAME> at(a);
@@ -638,6 +643,7 @@ __global__ void __launch_bounds__(block_limit(V)) norm_grad_short_kernel(const N
 // (128 registers: with 80, three blocks to an SM, sums by channel went to local memory: 1 366 us a step of 1 M x 256 fp32, forward and backward, against 1 323)
 template <class T, int V, bool SAME, int ACT>
 __global__ void __launch_bounds__(row_limit(V), row_limit(V) > 256 ? 1 : 2) norm_grad_stats_kernel(const NormArgs a, const T* x, const T* dy) {
+  early_start();
   __shared__ Parts parts;
   float2* const red = shared_red();
   const Place<T, V, SAME> at(a);
@@ -675,6 +681,7 @@ __global__ void __launch_bounds__(row_limit(V), row_limit(V) > 256 ? 1 : 2) norm
 // The last blocks of a row of the grid (blockIdx.x from `combine` on; of the first one only) add up the sums by channel, 4 channels a block: 64 groups
 // of threads share the blocks' sums, which are added in their order.
 __global__ void __launch_bounds__(32 * COMBINE_WARPS) norm_grad_combine_kernel(const NormArgs a, int combine) {
+  early_start();
   const bool any_long = a.blocks > 0 && *a.any_long;
   if ((int)blockIdx.x >= combine) {
     constexpr int CHANNELS = 4, SHARES = 32 * COMBINE_WARPS / CHANNELS;
@@ -712,6 +719,7 @@ __global__ void __launch_bounds__(32 * COMBINE_WARPS) norm_grad_combine_kernel(c
 
 template <class T, int V, bool SAME, int ACT>
 __global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_grad_apply_kernel(const NormArgs a, const T* x, const T* dy, T* dx) {
+  early_start();
   __shared__ Parts parts;
   if (!*a.any_long) return;
   const Place<T, V, SAME> at(a);
@@ -742,6 +750,7 @@ __global__ void __launch_bounds__(row_limit(V), row_blocks(V)) norm_grad_apply_k
 }
 
 __global__ void norm_no_rows_kernel(const NormArgs a) {
+  early_start();
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < a.graphs * a.groups; i += (long long)gridDim.x * blockDim.x) {
     if (a.mean) a.mean[i] = 0.f;
     if (a.rstd) a.rstd[i] = 0.f;
@@ -879,6 +888,7 @@ extern "C" int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offset
     }
   }
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  Launches enqueue = {st};
   char* const ws = static_cast<char*>(workspace);
   NormArgs a = {};
   a.n = n; a.graphs = graphs; a.offsets = reinterpret_cast<const long long*>(offsets); a.ld_x = ld_x; a.ld_y = ld_out; a.C = width; a.groups = groups;
@@ -893,7 +903,7 @@ extern "C" int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offset
   }
    a.part = reinterpret_cast<float2*>(ws + s.part);
   if (n == 0) {
-    if (mean || rstd) norm_no_rows_kernel<<<(int)std::min<long long>((graphs * groups + 255) / 256, 4096), 256, 0, st>>>(a);
+    if (mean || rstd) enqueue(norm_no_rows_kernel, dim3((unsigned)((int)std::min<long long>((graphs * groups + 255) / 256, 4096))), 256, 0, a);
   } else {
     if (s.blocks > 0) {
       if (!a.mean) a.mean = reinterpret_cast<float*>(ws + s.mean);
@@ -911,19 +921,17 @@ extern "C" int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offset
       if (a.short_blocks > 0) {
         set_block(&a, V, short_threads(n, graphs, width / V, short_vectors<V>()), &threads);
         const size_t smem = (size_t)a.lanes * a.vpr * ng<V, SAME>() * 8 + (size_t)groups * 8 + (size_t)width * 8;
-        norm_short_kernel<T, V, SAME, ACT><<<(int)std::min<int64_t>(graphs, 1 << 20), threads, smem, st>>>(a, xp, yp);
+        enqueue(norm_short_kernel<T, V, SAME, ACT>, dim3((unsigned)((int)std::min<int64_t>(graphs, 1 << 20))), threads, smem, a, xp, yp);
       }
       if (s.blocks > 0) {
         set_block(&a, V, ROW_THREADS, &threads);
-        norm_stats_kernel<T, V, SAME><<<s.row_grid, threads, (size_t)a.lanes * a.vpr * ng<V, SAME>() * 8, st>>>(a, xp);
-        norm_combine_kernel<<<dim3((unsigned)std::min<int64_t>(s.row_grid, graphs), combine_columns(s.blocks, graphs, groups)), 32 * COMBINE_WARPS, 0, st>>>(a);
-        norm_apply_kernel<T, V, SAME, ACT><<<s.row_grid, threads, (size_t)groups * 8, st>>>(a, xp, yp);
+        enqueue(norm_stats_kernel<T, V, SAME>, dim3((unsigned)(s.row_grid)), threads, (size_t)a.lanes * a.vpr * ng<V, SAME>() * 8, a, xp);
+        enqueue(norm_combine_kernel, dim3((unsigned)std::min<int64_t>(s.row_grid, graphs), combine_columns(s.blocks, graphs, groups)), 32 * COMBINE_WARPS, 0, a);
+        enqueue(norm_apply_kernel<T, V, SAME, ACT>, dim3((unsigned)(s.row_grid)), threads, (size_t)groups * 8, a, xp, yp);
       }
     });
   }
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) { taurus_note_cuda_error(e, "norm_rows"); return TAURUS_ERR_CUDA; }
-  return TAURUS_OK;
+  return enqueue.done("norm_rows");
 }
 
 extern "C" int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, int32_t width, int32_t groups,
@@ -965,6 +973,7 @@ extern "C" int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* o
     }
   }
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  Launches enqueue = {st};
   char* const ws = static_cast<char*>(workspace);
   NormArgs a = {};
   a.n = n; a.graphs = graphs; a.offsets = reinterpret_cast<const long long*>(offsets); a.ld_x = ld_x; a.ld_y = ld_grad_x; a.ld_dy = ld_grad; a.C = width; a.groups = groups;
@@ -980,7 +989,7 @@ extern "C" int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* o
    a.part = reinterpret_cast<float2*>(ws + s.part); a.chan = reinterpret_cast<float2*>(ws + s.chan);
   a.sums = reinterpret_cast<float2*>(ws + s.sums);
   if (n == 0) {
-    if (grad_gamma || grad_beta) norm_no_rows_kernel<<<4, 256, 0, st>>>(a);
+    if (grad_gamma || grad_beta) enqueue(norm_no_rows_kernel, dim3((unsigned)(4)), 256, 0, a);
   } else {
     a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);                 // read only here
     if (!grad_gamma && !grad_beta) a.chan = nullptr;
@@ -995,21 +1004,18 @@ extern "C" int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* o
       int threads;
       if (a.short_blocks > 0) {
         set_block(&a, V, short_threads(n, graphs, width / V, short_vectors<V>()), &threads);
-        norm_grad_short_kernel<T, V, SAME, ACT><<<a.short_blocks, threads, (size_t)a.lanes * width * 8 + (size_t)groups * 8, st>>>(a, xp, dyp, dxp);
+        enqueue(norm_grad_short_kernel<T, V, SAME, ACT>, dim3((unsigned)(a.short_blocks)), threads, (size_t)a.lanes * width * 8 + (size_t)groups * 8, a, xp, dyp, dxp);
       }
       if (s.blocks > 0) {
         set_block(&a, V, ROW_THREADS, &threads);
-        norm_grad_stats_kernel<T, V, SAME, ACT><<<s.row_grid, threads, (size_t)a.lanes * width * 8, st>>>(a, xp, dyp);
+        enqueue(norm_grad_stats_kernel<T, V, SAME, ACT>, dim3((unsigned)(s.row_grid)), threads, (size_t)a.lanes * width * 8, a, xp, dyp);
       }
       const int channel_blocks = a.chan ? (width + 3) / 4 : 0;
       const int owner_blocks = (int)std::min<int64_t>(s.row_grid, graphs);
       if (owner_blocks + channel_blocks > 0)
-        norm_grad_combine_kernel<<<dim3((unsigned)(owner_blocks + channel_blocks), s.blocks > 0 ? combine_columns(s.blocks, graphs, groups) : 1u), 32 * COMBINE_WARPS, 0,
-                                   st>>>(a, owner_blocks);
-      if (s.blocks > 0) norm_grad_apply_kernel<T, V, SAME, ACT><<<s.row_grid, threads, 0, st>>>(a, xp, dyp, dxp);
+        enqueue(norm_grad_combine_kernel, dim3((unsigned)(owner_blocks + channel_blocks), s.blocks > 0 ? combine_columns(s.blocks, graphs, groups) : 1u), 32 * COMBINE_WARPS, 0, a, owner_blocks);
+      if (s.blocks > 0) enqueue(norm_grad_apply_kernel<T, V, SAME, ACT>, dim3((unsigned)(s.row_grid)), threads, 0, a, xp, dyp, dxp);
     });
   }
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) { taurus_note_cuda_error(e, "norm_rows_grad"); return TAURUS_ERR_CUDA; }
-  return TAURUS_OK;
+  return enqueue.done("norm_rows_grad");
 }

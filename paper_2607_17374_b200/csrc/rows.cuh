@@ -44,6 +44,36 @@ static inline size_t rows_bytes(int64_t n, int64_t ld, int64_t width, int size) 
 // n rows of ld elements of `size` bytes stay below 2^62 bytes, so that no product of sizes overflows.
 static inline bool rows_fit(int64_t n, int64_t ld, int size) { return n == 0 || ld <= (int64_t)((1ll << 62) / size) / n; }
 
+// The launches of a call: each but the first may come up while the one before it ends (early_start at the start of every kernel waits for what that
+// wrote).  Data of an earlier kernel of the call is not read through __restrict__ pointers: such loads may be moved ahead of the wait.  For the norm, most of whose
+// launches find nothing to do in a batch of short graphs: 262 144 x 64 bf16 in 9 001 graphs 43.5 -> 41 us.  The sort of the ids lost by it (161 -> 184 us for 500 000:
+// blocks that wait take the places of blocks that work), the products by type did not change.
+struct Launches {
+  cudaStream_t st;
+  bool early = false;
+  template <class... P, class... A>
+  void operator()(void (*kernel)(P...), dim3 grid, int threads, size_t smem, A... args) {
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid; cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.attrs = &at; cfg.numAttrs = early ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+    if (e != cudaSuccess && error == cudaSuccess) error = e;
+    early = true;
+  }
+  cudaError_t error = cudaSuccess;
+  // The call's result: what a launch said, with its text kept.
+  int done(const char* what) {
+    const cudaError_t last = cudaGetLastError();
+    const cudaError_t e = error != cudaSuccess ? error : last;
+    if (e == cudaSuccess) return TAURUS_OK;
+    taurus_note_cuda_error(e, what);
+    return TAURUS_ERR_CUDA;
+  }
+};
+
 // A status word keeps the first error of the calls it was given to.
 static __device__ __forceinline__ void rows_status(int32_t* status, int code) { if (status) atomicCAS(status, 0, code); }
 

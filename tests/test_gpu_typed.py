@@ -30,6 +30,7 @@ SHAPES = [
     ([1000], 100, 256), ([257, 511], 512, 200), ([64] * 20, 16, 24), ([700, 90], 1000, 72), ([90, 333], 72, 1000), ([-5, 400, 200, -9], 96, 96), ([2] * 300, 40, 40),
     ([2600], 48, 264), ([5000, 3], 24, 16),
     ([300, 50, 0, 1], 46, 58), ([64], 50, 36), ([65], 36, 50), ([1500, 1030, 40], 66, 130),
+    ([1, 2, 0] * 70, 260, 24), ([70, 65] * 40, 392, 120), ([9000], 136, 264),
 ]
 
 
@@ -215,6 +216,19 @@ def test_weights_at_any_element(t, K, N):
     close(out, ref, mag * sums(K))
     (rx, mx), _, _ = typed_grad(off, x, W, dy)
     close(dx, rx, mx * sums(N))
+
+
+@pytest.mark.parametrize("n", [30, 300])
+def test_what_is_not_asked_for_needs_no_arguments(n):
+    """grad_bias alone: no x, no W, no pitches of either, no type of grad_W."""
+    off, dy = torch.tensor([0, 10, n], device="cuda"), torch.randn(n, 24, device="cuda")
+    db = torch.empty(2, 24, device="cuda")
+    ws = workspace(tb.typed_project_grad_workspace(n, 2, 16, 24, dy))
+    rc = tb.load_library().taurus_typed_project_grad(n, 2, off.data_ptr(), None, 0, tb.F32, None, dy.data_ptr(), 24, 16, 24, None, 0, None, -1, db.data_ptr(),
+                                                     ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0, None, None)
+    assert rc == 0
+    ref, mag = torch.stack([dy[:10].double().sum(0), dy[10:].double().sum(0)]), torch.stack([dy[:10].double().abs().sum(0), dy[10:].double().abs().sum(0)])
+    close(db, ref, mag * sums(n))
 
 
 def test_without_rows():

@@ -465,7 +465,8 @@ int taurus_permute_rows(int64_t V, int32_t width, const float* in_rows, int64_t 
  * whose addresses and pitches are multiples of 16 bytes are the fast ones.  All work is enqueued on `cuda_stream` of the current
  * device and the call returns without waiting; no call allocates or synchronises, so all may be captured into a graph.  A call reads
  * nothing that an earlier one left in a workspace.  Calls that may run at the same time (two streams, two graphs) need
- * workspaces of their own; calls in order may share one.  Outputs may not overlap inputs, the workspace or each other except where stated.
+ * workspaces of their own; calls in order may share one.  Outputs may not share memory with inputs, the workspace or each other except
+ * where stated (some columns of a matrix may be an input and others of it an output).
  * Element types of rows are TAURUS_F32, TAURUS_BF16, TAURUS_F16; products, sums and statistics are formed in fp32 or wider and
  * rounded to the output's type once.  Results do not depend on the launch: the same call gives the same bits.
  * Widths are 1 .. TAURUS_MAX_ROW_WIDTH (else TAURUS_ERR_UNSUPPORTED), numbers of rows below 2^31; n = 0 is allowed.
@@ -526,7 +527,7 @@ int taurus_typed_project_grad(int64_t n, int32_t types, const int64_t* offsets, 
  * with the mean and the (biased) variance over the graph's rows and the group's channels.  groups = 1 normalises a graph as a whole, groups = width
  * each channel by itself.  offsets: [graphs + 1] as in taurus_typed_project (rows outside are left as they are), or NULL for one graph of n rows (graphs = 1).
  * gamma, beta: [width] fp32 or NULL (ones, zeros).  mean, rstd: [graphs x groups] fp32, NULL unless the gradient will be taken (zeros for a graph without
- * rows).  out_rows may be x itself with the same pitch.
+ * rows).  out_rows may be x itself with the same pitch.  graphs: at most 2^30.
  */
 int64_t taurus_norm_rows_workspace(int64_t n, int64_t graphs, int32_t width, int32_t groups);
 int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, int32_t width,

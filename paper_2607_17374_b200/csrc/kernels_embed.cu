@@ -521,9 +521,9 @@ extern "C" int taurus_embed_rows(int64_t n, const int64_t* ids, const void* tabl
   int dev = 0, sms = 0;
   if (!ids || !table || !out_rows || !rows_aligned(ids, 8) || !rows_aligned(table, ts) || !rows_aligned(out_rows, os) || !rows_aligned(status, 4)) return TAURUS_ERR_INVALID_ARG;
   if (!rows_current_device(&dev, &sms)) return TAURUS_ERR_CUDA;
-  if (!rows_on_device(ids, dev) || !rows_on_device(table, dev) || !rows_on_device(out_rows, dev) || (status && !rows_on_device(status, dev))) return TAURUS_ERR_INVALID_ARG;
-  const size_t out_bytes = rows_bytes(n, ld_out, width, os);
-  if (rows_overlap(out_rows, out_bytes, table, rows_bytes(table_rows, ld_table, width, ts)) || rows_overlap(out_rows, out_bytes, ids, (size_t)n * 8)) return TAURUS_ERR_INVALID_ARG;
+  const Region outs[] = {region_of_rows(out_rows, n, ld_out, width, os), region_of(status, 4)};
+  const Region ins[] = {region_of_rows(table, table_rows, ld_table, width, ts), region_of(ids, (size_t)n * 8)};
+  if (!regions_on_device(outs, dev) || !regions_on_device(ins, dev) || !regions_apart(outs, ins)) return TAURUS_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   // vectors of 16 bytes of the table; of a 16-bit table 32 bytes of fp32 output, as two of 16
   const int limit = ts == 2 ? 8 : 4;
@@ -571,18 +571,11 @@ extern "C" int taurus_embed_grad(int64_t n, const int64_t* ids, const void* grad
   if (n > 0 && (!ids || !grad_rows || !workspace || !rows_aligned(ids, 8) || !rows_aligned(grad_rows, gs) || !rows_aligned(workspace, 256))) return TAURUS_ERR_INVALID_ARG;
   int dev = 0, sms = 0;
   if (!rows_current_device(&dev, &sms)) return TAURUS_ERR_CUDA;
-  if (!rows_on_device(grad_table, dev) || (status && !rows_on_device(status, dev))) return TAURUS_ERR_INVALID_ARG;
   const GradSpace s = grad_space(n, table_rows, width);
-  const size_t table_bytes = rows_bytes(table_rows, ld_table, width, ts);
-  if (n > 0) {
-    if (!rows_on_device(ids, dev) || !rows_on_device(grad_rows, dev) || !rows_on_device(workspace, dev)) return TAURUS_ERR_INVALID_ARG;
-    if (workspace_bytes < (int64_t)s.bytes) return TAURUS_ERR_INVALID_ARG;
-    const size_t grad_bytes = rows_bytes(n, ld_grad, width, gs), id_bytes = (size_t)n * 8;
-    if (rows_overlap(grad_table, table_bytes, grad_rows, grad_bytes) || rows_overlap(grad_table, table_bytes, ids, id_bytes) ||
-        rows_overlap(workspace, s.bytes, grad_table, table_bytes) || rows_overlap(workspace, s.bytes, grad_rows, grad_bytes) ||
-        rows_overlap(workspace, s.bytes, ids, id_bytes))
-      return TAURUS_ERR_INVALID_ARG;
-  }
+  const Region outs[] = {region_of_rows(grad_table, table_rows, ld_table, width, ts), region_of(status, 4)};
+  const Region ins[] = {region_of_rows(grad_rows, n, ld_grad, width, gs), region_of(ids, (size_t)n * 8)};
+  if (!regions_on_device(outs, dev) || !regions_on_device(ins, dev) || !regions_apart(outs, ins) || !workspace_ok(workspace, workspace_bytes, (int64_t)s.bytes, dev, outs, ins))
+    return TAURUS_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   char* const ws = static_cast<char*>(workspace);
   const int limit = gs == 2 && ts == 2 ? 8 : 4;

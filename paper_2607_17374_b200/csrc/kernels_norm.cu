@@ -795,7 +795,7 @@ NormSpace norm_space(int64_t n, int64_t graphs, int C, int groups, bool grad) {
 }
 
 bool norm_shape_ok(int64_t n, int64_t graphs, int32_t width, int32_t groups) {
-  return n >= 0 && n < (1ll << 31) && graphs >= 1 && graphs < (1ll << 31) && width >= 1 && groups >= 1 && width % groups == 0;
+  return n >= 0 && n < (1ll << 31) && graphs >= 1 && graphs <= (1ll << 30) && width >= 1 && groups >= 1 && width % groups == 0;
 }
 
 // Vectors of at most 16 bytes; of at most four elements where they would reach over several groups (each has moments of its own then).
@@ -874,22 +874,14 @@ extern "C" int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offset
   int dev = 0, sms = 0;
   if (!rows_current_device(&dev, &sms)) return TAURUS_ERR_CUDA;
   const NormSpace s = norm_space(n, graphs, width, groups, false);
-  const size_t stat_bytes = (size_t)graphs * groups * 4;
-  for (const void* p : {(const void*)offsets, (const void*)gamma, (const void*)beta, (const void*)mean, (const void*)rstd, (const void*)status})
-    if (p && !rows_on_device(p, dev)) return TAURUS_ERR_INVALID_ARG;
-  if (n > 0) {
-    if (!rows_on_device(x, dev) || !rows_on_device(out_rows, dev)) return TAURUS_ERR_INVALID_ARG;
-    const size_t out_bytes = rows_bytes(n, ld_out, width, ts), x_bytes = rows_bytes(n, ld_x, width, ts);
-    if (rows_overlap(out_rows, out_bytes, x, x_bytes) && !(out_rows == x && ld_out == ld_x)) return TAURUS_ERR_INVALID_ARG;
-    struct { const void* p; size_t n; } in[] = {{offsets, offsets ? (size_t)(graphs + 1) * 8 : 0}, {gamma, gamma ? (size_t)width * 4 : 0}, {beta, beta ? (size_t)width * 4 : 0},
-                                                {mean, mean ? stat_bytes : 0}, {rstd, rstd ? stat_bytes : 0}};
-    for (auto& i : in) if (rows_overlap(out_rows, out_bytes, i.p, i.n)) return TAURUS_ERR_INVALID_ARG;
-    if (s.bytes) {
-      if (!workspace || !rows_aligned(workspace, 256) || workspace_bytes < (int64_t)s.bytes || !rows_on_device(workspace, dev)) return TAURUS_ERR_INVALID_ARG;
-      if (rows_overlap(workspace, s.bytes, out_rows, out_bytes) || rows_overlap(workspace, s.bytes, x, x_bytes)) return TAURUS_ERR_INVALID_ARG;
-      for (auto& i : in) if (rows_overlap(workspace, s.bytes, i.p, i.n)) return TAURUS_ERR_INVALID_ARG;
-    }
-  }
+  const size_t stat_bytes = (size_t)graphs * groups * 4, cb = (size_t)width * 4;
+  const Region rows = region_of_rows(x, n, ld_x, width, ts);
+  const bool in_place = out_rows == x && ld_out == ld_x;
+  const Region outs[] = {region_of_rows(out_rows, n, ld_out, width, ts), region_of(mean, stat_bytes), region_of(rstd, stat_bytes), region_of(status, 4)};
+  const Region ins[] = {in_place ? region_of(nullptr, 0) : rows, region_of(offsets, (size_t)(graphs + 1) * 8), region_of(gamma, cb), region_of(beta, cb)};
+  if (!regions_on_device(outs, dev) || !regions_on_device(ins, dev) || !regions_apart(outs, ins) ||
+      !workspace_ok(workspace, workspace_bytes, n > 0 ? (int64_t)s.bytes : 0, dev, outs, ins))
+    return TAURUS_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   Launches enqueue = {st};
   char* const ws = static_cast<char*>(workspace);
@@ -953,28 +945,14 @@ extern "C" int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* o
   if (!rows_current_device(&dev, &sms)) return TAURUS_ERR_CUDA;
   const NormSpace s = norm_space(n, graphs, width, groups, true);
   const size_t stat_bytes = (size_t)graphs * groups * 4, cb = (size_t)width * 4;
-  for (const void* p : {(const void*)offsets, (const void*)gamma, (const void*)beta, (const void*)mean, (const void*)rstd, (const void*)grad_gamma, (const void*)grad_beta,
-                        (const void*)status})
-    if (p && !rows_on_device(p, dev)) return TAURUS_ERR_INVALID_ARG;
-  if (rows_overlap(grad_gamma, grad_gamma ? cb : 0, grad_beta, grad_beta ? cb : 0)) return TAURUS_ERR_INVALID_ARG;
-  struct { const void* p; size_t n; } in[] = {{offsets, offsets ? (size_t)(graphs + 1) * 8 : 0}, {gamma, gamma ? cb : 0}, {beta, beta ? cb : 0}, {mean, stat_bytes}, {rstd, stat_bytes}};
-  struct { const void* p; size_t n; } sum[] = {{grad_gamma, grad_gamma ? cb : 0}, {grad_beta, grad_beta ? cb : 0}};
-  for (auto& o : sum) for (auto& i : in) if (rows_overlap(o.p, o.n, i.p, i.n)) return TAURUS_ERR_INVALID_ARG;
-  if (n > 0) {
-    if (!rows_on_device(x, dev) || !rows_on_device(grad_out, dev) || !rows_on_device(grad_x, dev)) return TAURUS_ERR_INVALID_ARG;
-    const size_t dx_bytes = rows_bytes(n, ld_grad_x, width, ts), x_bytes = rows_bytes(n, ld_x, width, ts), dy_bytes = rows_bytes(n, ld_grad, width, ts);
-    if (rows_overlap(grad_x, dx_bytes, x, x_bytes) && !(grad_x == x && ld_grad_x == ld_x)) return TAURUS_ERR_INVALID_ARG;
-    if (rows_overlap(grad_x, dx_bytes, grad_out, dy_bytes) && !(grad_x == grad_out && ld_grad_x == ld_grad)) return TAURUS_ERR_INVALID_ARG;
-    for (auto& i : in) if (rows_overlap(grad_x, dx_bytes, i.p, i.n)) return TAURUS_ERR_INVALID_ARG;
-    for (auto& o : sum)
-      if (rows_overlap(o.p, o.n, grad_x, dx_bytes) || rows_overlap(o.p, o.n, x, x_bytes) || rows_overlap(o.p, o.n, grad_out, dy_bytes)) return TAURUS_ERR_INVALID_ARG;
-    if (s.bytes) {
-      if (!workspace || !rows_aligned(workspace, 256) || workspace_bytes < (int64_t)s.bytes || !rows_on_device(workspace, dev)) return TAURUS_ERR_INVALID_ARG;
-      if (rows_overlap(workspace, s.bytes, grad_x, dx_bytes) || rows_overlap(workspace, s.bytes, x, x_bytes) || rows_overlap(workspace, s.bytes, grad_out, dy_bytes)) return TAURUS_ERR_INVALID_ARG;
-      for (auto& i : in) if (rows_overlap(workspace, s.bytes, i.p, i.n)) return TAURUS_ERR_INVALID_ARG;
-      for (auto& o : sum) if (rows_overlap(workspace, s.bytes, o.p, o.n)) return TAURUS_ERR_INVALID_ARG;
-    }
-  }
+  const bool over_x = grad_x == x && ld_grad_x == ld_x, over_grad = grad_x == grad_out && ld_grad_x == ld_grad;      // in place
+  const Region rows = region_of_rows(x, n, ld_x, width, ts), grads = region_of_rows(grad_out, n, ld_grad, width, ts);
+  const Region outs[] = {region_of_rows(grad_x, n, ld_grad_x, width, ts), region_of(grad_gamma, cb), region_of(grad_beta, cb), region_of(status, 4)};
+  const Region ins[] = {over_x ? region_of(nullptr, 0) : rows, over_grad ? region_of(nullptr, 0) : grads, region_of(offsets, (size_t)(graphs + 1) * 8),
+                        region_of(gamma, cb), region_of(beta, cb), region_of(mean, stat_bytes), region_of(rstd, stat_bytes)};
+  if (!regions_on_device(outs, dev) || !regions_on_device(ins, dev) || !regions_apart(outs, ins) ||
+      !workspace_ok(workspace, workspace_bytes, n > 0 ? (int64_t)s.bytes : 0, dev, outs, ins))
+    return TAURUS_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   Launches enqueue = {st};
   char* const ws = static_cast<char*>(workspace);

@@ -139,48 +139,30 @@ int vector_of(int size, const void* p, int64_t ld) {
   return v;
 }
 
-// Does a call take the tensor cores?  TMA wants 16-bit weights that begin at a multiple of 16 bytes; others are laid out anew (typed_tc_packs) or, where only
-// the first address is off, left to the kernels for few rows.
-bool on_tensor_cores(int64_t n, int32_t type, const void* W, int32_t d_out) {
-  return n > FEW_ROWS && typed_tc_usable() && (typed_tc_packs(type, d_out) || rows_aligned(W, 16));
-}
-size_t up(size_t b) { return (b + 255) / 256 * 256; }
-
-struct Region { const void* p; size_t n; };
-// No region of `out` shares a byte with one of `in` or with another of `out`.
-template <int A, int B>
-bool apart(const Region (&out)[A], const Region (&in)[B]) {
-  for (int i = 0; i < A; ++i) {
-    for (int j = 0; j < B; ++j) if (rows_overlap(out[i].p, out[i].n, in[j].p, in[j].n)) return false;
-    for (int j = 0; j < i; ++j) if (rows_overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return false;
+// A call's workspace: W laid out anew (where it is: packs), partial results of grad_W, rows of grad_out and of x at other pitches.  The workspace functions
+// answer for weights at any address, a call asks for what it uses.
+struct Space {
+  size_t part = 0, dy = 0, x = 0, bytes = 0;
+  Space(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type, bool packs, bool grad) {
+    if (n <= FEW_ROWS) return;
+    auto take = [&](size_t b) { const size_t o = bytes; bytes += (b + 255) / 256 * 256; return o; };
+    if (packs) take(typed_tc_pack_bytes(types, d_in, d_out, type));
+    if (grad) { part = take(typed_tc_part_bytes(n, types, d_in, d_out, type)); dy = take(typed_tc_row_bytes(n, d_out, type)); }
+    x = take(typed_tc_row_bytes(n, d_in, type));
   }
-  return true;
-}
-template <int A>
-bool all_on_device(const Region (&r)[A], int dev) {
-  for (const Region& i : r) if (i.p && !rows_on_device(i.p, dev)) return false;
-  return true;
-}
-template <int A, int B>
-bool space_ok(const void* p, int64_t bytes, int64_t need, int dev, const Region (&out)[A], const Region (&in)[B]) {
-  if (need == 0) return true;
-  if (!p || !rows_aligned(p, 256) || bytes < need || !rows_on_device(p, dev)) return false;
-  const Region mine[] = {{p, (size_t)need}};
-  return apart(mine, out) && apart(mine, in);
-}
+};
 
 }  // namespace
 
 extern "C" int64_t taurus_typed_project_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type) {
   if (!typed_shape_ok(n, types, d_in, d_out, type)) return TAURUS_ERR_INVALID_ARG;
   if (!typed_supported(types, d_in, d_out)) return TAURUS_ERR_UNSUPPORTED;
-  return n > FEW_ROWS ? (int64_t)(up(typed_tc_pack_bytes(types, d_in, d_out, type)) + up(typed_tc_row_bytes(n, d_in, type))) : 0;
+  return (int64_t)Space(n, types, d_in, d_out, type, true, false).bytes;
 }
 extern "C" int64_t taurus_typed_project_grad_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type) {
   if (!typed_shape_ok(n, types, d_in, d_out, type)) return TAURUS_ERR_INVALID_ARG;
   if (!typed_supported(types, d_in, d_out)) return TAURUS_ERR_UNSUPPORTED;
-  return n > FEW_ROWS ? (int64_t)(up(typed_tc_pack_bytes(types, d_in, d_out, type)) + up(typed_tc_part_bytes(n, types, d_in, d_out, type)) + up(typed_tc_row_bytes(n, d_in, type)) +
-                                 up(typed_tc_row_bytes(n, d_out, type))) : 0;
+  return (int64_t)Space(n, types, d_in, d_out, type, true, true).bytes;
 }
 
 extern "C" int taurus_typed_project(int64_t n, int32_t types, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, const void* W,
@@ -197,22 +179,23 @@ extern "C" int taurus_typed_project(int64_t n, int32_t types, const int64_t* off
     return TAURUS_ERR_INVALID_ARG;
   int dev = 0, sms = 0;
   if (!rows_current_device(&dev, &sms)) return TAURUS_ERR_CUDA;
-  const Region outs[] = {{out, rows_bytes(n, ld_out, d_out, os)}, {status, status ? 4u : 0u}};
-  const Region ins[] = {{offsets, (size_t)(types + 1) * 8}, {x, rows_bytes(n, ld_x, d_in, ts)}, {W, (size_t)types * d_in * d_out * ts},
-                        {bias, bias ? (size_t)types * d_out * 4 : 0}};
-  if (!all_on_device(outs, dev) || !all_on_device(ins, dev) || !apart(outs, ins)) return TAURUS_ERR_INVALID_ARG;
-  const int64_t space = taurus_typed_project_workspace(n, types, d_in, d_out, type);
-  if (!space_ok(workspace, workspace_bytes, space, dev, outs, ins)) return TAURUS_ERR_INVALID_ARG;
+  const Region outs[] = {region_of_rows(out, n, ld_out, d_out, os), region_of(status, 4)};
+  const Region ins[] = {region_of(offsets, (size_t)(types + 1) * 8), region_of_rows(x, n, ld_x, d_in, ts), region_of(W, (size_t)types * d_in * d_out * ts),
+                        region_of(bias, (size_t)types * d_out * 4)};
+  const bool packs = typed_tc_packs(W, type, d_out);
+  const Space space(n, types, d_in, d_out, type, packs, false);
+  if (!regions_on_device(outs, dev) || !regions_on_device(ins, dev) || !regions_apart(outs, ins) ||
+      !workspace_ok(workspace, workspace_bytes, (int64_t)space.bytes, dev, outs, ins))
+    return TAURUS_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const long long* const off = reinterpret_cast<const long long*>(offsets);
   int rc = TAURUS_OK;
-  if (on_tensor_cores(n, type, W, d_out)) {
-    const bool packs = typed_tc_packs(type, d_out);
+  if (n > FEW_ROWS) {
     if (packs) rc = typed_tc_pack(type, W, types, d_in, d_out, workspace, sms, st);
     const void* rows = x;
     int64_t ld_rows = ld_x;
     if (typed_tc_packs_rows(x, ld_x, d_in, type)) {
-      void* const at = static_cast<char*>(workspace) + up(typed_tc_pack_bytes(types, d_in, d_out, type));
+      void* const at = static_cast<char*>(workspace) + space.x;
       typed_tc_pack_rows(x, ld_x, n, d_in, at, sms, st);
       rows = at; ld_rows = typed_tc_row_pitch(d_in);
     }
@@ -256,38 +239,33 @@ extern "C" int taurus_typed_project_grad(int64_t n, int32_t types, const int64_t
   int dev = 0, sms = 0;
   if (!rows_current_device(&dev, &sms)) return TAURUS_ERR_CUDA;
   const size_t w_count = (size_t)types * d_in * d_out;
-  const Region outs[] = {{grad_x, grad_x ? rows_bytes(n, ld_grad_x, d_in, ts) : 0}, {grad_W, grad_W ? w_count * ws : 0}, {grad_bias, grad_bias ? (size_t)types * d_out * 4 : 0},
-                         {status, status ? 4u : 0u}};
-  const Region ins[] = {{offsets, (size_t)(types + 1) * 8}, {x, x ? rows_bytes(n, ld_x, d_in, ts) : 0}, {W, W ? w_count * ts : 0},
-                        {grad_out, grad_out ? rows_bytes(n, ld_grad, d_out, ts) : 0}};
-  if (!apart(outs, ins)) return TAURUS_ERR_INVALID_ARG;
-  for (const Region& r : outs) if (r.n > 0 && !rows_on_device(r.p, dev)) return TAURUS_ERR_INVALID_ARG;
-  for (const Region& r : ins) if (r.n > 0 && !rows_on_device(r.p, dev)) return TAURUS_ERR_INVALID_ARG;
-  if (!space_ok(workspace, workspace_bytes, taurus_typed_project_grad_workspace(n, types, d_in, d_out, type), dev, outs, ins)) return TAURUS_ERR_INVALID_ARG;
+  const Region outs[] = {region_of_rows(grad_x, n, ld_grad_x, d_in, ts), region_of(grad_W, w_count * ws), region_of(grad_bias, (size_t)types * d_out * 4), region_of(status, 4)};
+  const Region ins[] = {region_of(offsets, (size_t)(types + 1) * 8), region_of_rows(x, n, ld_x, d_in, ts), region_of(W, w_count * ts), region_of_rows(grad_out, n, ld_grad, d_out, ts)};
+  const bool packs = grad_x && typed_tc_packs(W, type, d_out);
+  const Space space(n, types, d_in, d_out, type, packs, true);
+  if (!regions_on_device(outs, dev) || !regions_on_device(ins, dev) || !regions_apart(outs, ins) ||
+      !workspace_ok(workspace, workspace_bytes, (int64_t)space.bytes, dev, outs, ins))
+    return TAURUS_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const long long* const off = reinterpret_cast<const long long*>(offsets);
   int rc = TAURUS_OK;
-  if (on_tensor_cores(n, type, grad_x ? W : nullptr, d_out)) {
-    const bool packs = typed_tc_packs(type, d_out);
-    char* const space = static_cast<char*>(workspace);
-    if (grad_x && packs) rc = typed_tc_pack(type, W, types, d_in, d_out, space, sms, st);
-    // the rows at other pitches, where they need it: behind the partial results
-    char* at = space + up(typed_tc_pack_bytes(types, d_in, d_out, type)) + up(typed_tc_part_bytes(n, types, d_in, d_out, type));
-    auto laid_out = [&](const void** rows, int64_t* ld, int width) {
+  if (n > FEW_ROWS) {
+    char* const at = static_cast<char*>(workspace);
+    if (packs) rc = typed_tc_pack(type, W, types, d_in, d_out, at, sms, st);
+    auto laid_out = [&](const void** rows, int64_t* ld, int width, size_t where) {
       if (typed_tc_packs_rows(*rows, *ld, width, type)) {
-        typed_tc_pack_rows(*rows, *ld, n, width, at, sms, st);
-        *rows = at; *ld = typed_tc_row_pitch(width);
+        typed_tc_pack_rows(*rows, *ld, n, width, at + where, sms, st);
+        *rows = at + where; *ld = typed_tc_row_pitch(width);
       }
-      at += up(typed_tc_row_bytes(n, width, type));
     };
     const void *dy_rows = grad_out, *x_rows = x;
     int64_t ld_dy_rows = ld_grad, ld_x_rows = ld_x;
-    laid_out(&dy_rows, &ld_dy_rows, d_out);
-    if (grad_W) laid_out(&x_rows, &ld_x_rows, d_in);
+    laid_out(&dy_rows, &ld_dy_rows, d_out, space.dy);
+    if (grad_W) laid_out(&x_rows, &ld_x_rows, d_in, space.x);
     else if (x && typed_tc_packs_rows(x, ld_x, d_in, type)) x_rows = nullptr;      // (grad_bias as beside grad_W)
     if (!rc && grad_x)
-      rc = typed_tc_rows(true, n, types, off, dy_rows, ld_dy_rows, type, packs ? space : W, nullptr, d_in, d_out, grad_x, type, ld_grad_x, status, sms, st);
-    float* const part = reinterpret_cast<float*>(space + up(typed_tc_pack_bytes(types, d_in, d_out, type)));
+      rc = typed_tc_rows(true, n, types, off, dy_rows, ld_dy_rows, type, packs ? at : W, nullptr, d_in, d_out, grad_x, type, ld_grad_x, status, sms, st);
+    float* const part = reinterpret_cast<float*>(at + space.part);
     if (!rc && (grad_W || grad_bias))
       rc = typed_tc_weights(n, types, off, x_rows, ld_x_rows, type, dy_rows, ld_dy_rows, d_in, d_out, grad_W, grad_W_type, grad_bias, part, status, sms, st);
   } else with_row_type(type, [&](auto tt) {

@@ -185,8 +185,8 @@ __device__ __forceinline__ bool plan(const TcArgs& a, Shared* s) {
       const int g = g0 + threadIdx.x, len = g < a.types ? s->begin[g + 1] - s->begin[g] : 0;
       int u = 0, p = 0;
       if (g < a.types) {
-        if (KIND == GRAD_W) { u = len > 0 ? (len + a.chunk - 1) / a.chunk : 1; p = u > 1 ? u : 0; }
-        else u = (len + BM - 1) / BM;
+        if (KIND == GRAD_W) { u = len > 0 ? (int)(((unsigned)len + a.chunk - 1) / a.chunk) : 1; p = u > 1 ? u : 0; }
+        else u = (int)(((unsigned)len + BM - 1) / BM);                             // (unsigned: a type may have 2^31 - 1 rows)
       }
       int iu = u, ip = p;
       for (int o = 1; o < 32; o <<= 1) {
@@ -957,7 +957,8 @@ bool make_map(CUtensorMap* m, int32_t type, const void* base, long long cols, lo
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)depth};
   const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
   const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
-  return encode_fn()(m, type == TAURUS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, depth > 0 ? 3 : 2, const_cast<void*>(base), dims, strides, box,
+  const EncodeTiledFn encode = encode_fn();
+  return encode && encode(m, type == TAURUS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, depth > 0 ? 3 : 2, const_cast<void*>(base), dims, strides, box,
                      one, CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -996,12 +997,9 @@ int bn_most(int32_t type, bool grad_w, bool loaded) { return type == TAURUS_F32 
 
 }  // namespace
 
-bool typed_tc_usable() { return encode_fn() != nullptr; }
-// Does W have to be laid out anew?
-bool typed_tc_packs(int32_t type, int d_out) { return type == TAURUS_F32 || d_out % 8 != 0; }
-size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type) {
-  return typed_tc_packs(type, d_out) ? (size_t)types * (type == TAURUS_F32 ? 3 : 1) * d_in * weight_pitch(d_out) * 2 : 0;
-}
+// Does W have to be laid out anew?  Room for it (whatever its address, which a workspace's size does not depend on).
+bool typed_tc_packs(const void* W, int32_t type, int d_out) { return type == TAURUS_F32 || d_out % 8 != 0 || !rows_aligned(W, 16); }
+size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type) { return (size_t)types * (type == TAURUS_F32 ? 3 : 1) * d_in * weight_pitch(d_out) * 2; }
 // Rows of a width that keeps TMA off, fp32 aside: room for them at another pitch, and whether these need it (rows of such a width whose own pitch suits TMA do not).
 int64_t typed_tc_row_pitch(int width) { return taurus_round_up(width, 8); }
 size_t typed_tc_row_bytes(int64_t n, int width, int32_t type) { return type == TAURUS_F32 || width % 8 == 0 ? 0 : (size_t)n * (size_t)typed_tc_row_pitch(width) * 2; }
@@ -1047,10 +1045,9 @@ int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* of
   a.a = x; a.lda = ld_x; a.a_vec = vec_of(x, ld_x, row_type_size(type));
   a.out = out; a.ld_out = ld_out; a.out_f32 = out_type == TAURUS_F32; a.out_vec = ld_out * row_type_size(out_type) % 16 == 0 && rows_aligned(out, 16);
   a.bias = bias; a.status = status;
-  const long long pitch = typed_tc_packs(type, d_out) ? weight_pitch(d_out) : d_out;
   CUtensorMap ma = {}, mb = {};
   if (!loaded && !make_map(&ma, type, x, Kc, n, 0, ld_x, bk, BM)) return TAURUS_ERR_CUDA;
-  if (!make_map(&mb, type, w, d_out, d_in, (long long)types * planes, pitch, transposed ? bk : 64, transposed ? a.bn : bk)) return TAURUS_ERR_CUDA;
+  if (!make_map(&mb, type, w, d_out, d_in, (long long)types * planes, weight_pitch(d_out), transposed ? bk : 64, transposed ? a.bn : bk)) return TAURUS_ERR_CUDA;
   const long long units = (n / BM + std::min<long long>(types, n)) * a.n_blocks;
   auto go = [&](auto f) { return f(ma, mb, a, units, sms, st); };
   return transposed ? launch_type<GRAD_X>(type, loaded, go) : launch_type<PROJECT>(type, loaded, go);

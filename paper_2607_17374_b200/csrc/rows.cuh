@@ -35,12 +35,46 @@ static inline bool rows_on_device(const void* p, int dev) {
   return (at.type == cudaMemoryTypeDevice && at.device == dev) || at.type == cudaMemoryTypeManaged;
 }
 static inline bool rows_aligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
-// Do [a, a + an) and [b, b + bn) share a byte?
-static inline bool rows_overlap(const void* a, size_t an, const void* b, size_t bn) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return an > 0 && bn > 0 && x < y + bn && y < x + an;
+// An array of a call: `rows` rows of `width` bytes, `pitch` bytes apart; no rows where there is none.
+struct Region {
+  const void* p;
+  size_t rows, width, pitch;
+  size_t bytes() const { return rows > 0 ? (rows - 1) * pitch + width : 0; }
+};
+static inline Region region_of(const void* p, size_t bytes) { return {p, p && bytes ? (size_t)1 : (size_t)0, bytes, bytes}; }
+static inline Region region_of_rows(const void* p, int64_t n, int64_t ld, int64_t width, int size) {
+  return {p, p ? (size_t)n : (size_t)0, (size_t)width * (size_t)size, (size_t)ld * (size_t)size};
 }
-static inline size_t rows_bytes(int64_t n, int64_t ld, int64_t width, int size) { return n > 0 ? ((size_t)(n - 1) * (size_t)ld + (size_t)width) * (size_t)size : 0; }
+// Do two arrays share a byte?  Columns of one matrix do not share any with others of it: rows of one pitch are compared by where they lie in it.
+static inline bool regions_share(const Region& a, const Region& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  if (a.rows == 0 || b.rows == 0 || x >= y + b.bytes() || y >= x + a.bytes()) return false;
+  if ((a.rows == 1 && b.rows == 1) || (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch)) return true;
+  const size_t pitch = a.rows > 1 ? a.pitch : b.pitch, d = y >= x ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;
+  return d < a.width || d + b.width > pitch;
+}
+// No array of `out` shares a byte with one of `in`, nor with another of `out`.
+template <int A, int B>
+static inline bool regions_apart(const Region (&out)[A], const Region (&in)[B]) {
+  for (int i = 0; i < A; ++i) {
+    for (int j = 0; j < B; ++j) if (regions_share(out[i], in[j])) return false;
+    for (int j = 0; j < i; ++j) if (regions_share(out[i], out[j])) return false;
+  }
+  return true;
+}
+template <int A>
+static inline bool regions_on_device(const Region (&r)[A], int dev) {
+  for (const Region& i : r) if (i.rows > 0 && !rows_on_device(i.p, dev)) return false;
+  return true;
+}
+// Is the workspace of the call, `need` bytes, there and apart from its arrays?
+template <int A, int B>
+static inline bool workspace_ok(const void* p, int64_t bytes, int64_t need, int dev, const Region (&out)[A], const Region (&in)[B]) {
+  if (need == 0) return true;
+  if (!p || !rows_aligned(p, 256) || bytes < need || !rows_on_device(p, dev)) return false;
+  const Region mine[] = {region_of(p, (size_t)need)};
+  return regions_apart(mine, out) && regions_apart(mine, in);
+}
 // n rows of ld elements of `size` bytes stay below 2^62 bytes, so that no product of sizes overflows.
 static inline bool rows_fit(int64_t n, int64_t ld, int size) { return n == 0 || ld <= (int64_t)((1ll << 62) / size) / n; }
 

@@ -38,8 +38,7 @@ static __device__ __forceinline__ Split4 split4(float a, float b, float c, float
 }
 
 // ---- kernels_typed_tc.cu
-bool typed_tc_usable();
-bool typed_tc_packs(int32_t type, int d_out);
+bool typed_tc_packs(const void* W, int32_t type, int d_out);
 size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type);
 size_t typed_tc_row_bytes(int64_t n, int width, int32_t type);
 int64_t typed_tc_row_pitch(int width);

@@ -182,3 +182,66 @@ def test_rows_beyond_32_bits():
     assert ((y[n - 300:].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 1e-5).all()
     ref, _, _ = norm([0, 69_700], x[n - 70_000:n - 300], 8, None, None, EPS, 1)
     assert ((y[n - 70_000:n - 300].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 1e-4).all()
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [40, 1000])
+def test_columns_of_one_matrix(t, n):
+    """Inputs and outputs that are neighbouring columns of one matrix give what matrices of their own give; columns that meet are refused."""
+    g = torch.Generator("cuda").manual_seed(n)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    d, h, ids = 64, 96, torch.randint(0, 50, (n,), generator=g, device="cuda")
+    table, W, off, dy = r(50, d).to(t), r(2, d, h).to(t), torch.tensor([0, n // 3, n], device="cuda"), r(n, h).to(t)
+    ws = torch.empty(max(tb.embed_grad_workspace(n, 50, d), tb.typed_project_grad_workspace(n, 2, d, h, t), tb.norm_rows_grad_workspace(n, 2, h, 4)), dtype=torch.uint8, device="cuda")
+
+    def run(x, p, y, dp, dx):
+        mean, rstd, dtable = torch.empty(2, 4, device="cuda"), torch.empty(2, 4, device="cuda"), torch.empty_like(table)
+        tb.embed_rows(n, ids, table, 50, d, d, x, x.stride(0))
+        tb.typed_project(n, 2, off, x, x.stride(0), W, None, d, h, p, p.stride(0), ws)
+        tb.norm_rows(n, 2, off, p, p.stride(0), h, 4, None, None, EPS, tb.ACT_SILU, y, y.stride(0), mean, rstd, ws)
+        tb.norm_rows_grad(n, 2, off, p, p.stride(0), h, 4, None, None, tb.ACT_SILU, mean, rstd, dy, h, dp, dp.stride(0), None, None, ws)
+        tb.typed_project_grad(n, 2, off, x, x.stride(0), W, dp, dp.stride(0), d, h, dx, dx.stride(0), workspace=ws)
+        tb.embed_grad(n, ids, dx, dx.stride(0), d, dtable, 50, d, ws)
+        return [v.clone() for v in (x, p, y, dp, dx, dtable)]
+
+    own = run(*(torch.empty(n, w, dtype=t, device="cuda") for w in (d, h, h, h, d)))
+    big = torch.full((n, 2 * d + 3 * h + 8), 7.0, dtype=t, device="cuda")
+    at, cut = 0, []
+    for w in (d, h, h, h, d):
+        cut.append(big[:, at:at + w])
+        at += w
+    for a, b in zip(own, run(*cut)):
+        assert torch.equal(a, b)
+    assert (big[:, at:] == 7.0).all()
+    x, p, over, first = cut[0], cut[1], big[:, d - 8:d - 8 + h], big[1:, :h]
+    before = big.clone()
+    for call in (lambda: tb.typed_project(n, 2, off, x, x.stride(0), W, None, d, h, over, over.stride(0), ws),
+                 lambda: tb.embed_rows(n - 1, ids, over[:, :d], 50, d, over.stride(0), first[:, :d], first.stride(0)) if n > 50 else tb.embed_rows(
+                     n, ids, over[:, :d], n, d, over.stride(0), x, x.stride(0)),
+                 lambda: tb.norm_rows(n, 2, off, p, p.stride(0), h, 4, None, None, EPS, 0, over, over.stride(0), workspace=ws),
+                 lambda: tb.norm_rows_grad(n, 2, off, p, p.stride(0), h, 4, None, None, 0, torch.zeros(2, 4, device="cuda"), torch.zeros(2, 4, device="cuda"), dy, h, over,
+                                           over.stride(0), workspace=ws)):
+        with pytest.raises(tb.TaurusError) as e:
+            call()
+        assert e.value.code == tb.ERROR_CODES["INVALID_ARG"]
+    assert torch.equal(big, before)
+
+
+def test_most_rows_of_one_type():
+    """2^31 - 1 rows of one type: small whole numbers, whose products and sums fp32 holds (a sum of ones to its nearest value)."""
+    n = (1 << 31) - 1
+    x, out, off = torch.ones(n, 1, device="cuda"), torch.zeros(n, 1, device="cuda"), torch.tensor([0, 0, n], device="cuda")
+    x[-1], x[1 << 30] = 5.0, 7.0
+    W, b = torch.tensor([[[2.0]], [[3.0]]], device="cuda"), torch.tensor([[9.0], [1.0]], device="cuda")
+    ws = torch.empty(tb.typed_project_grad_workspace(n, 2, 1, 1, x), dtype=torch.uint8, device="cuda")
+    tb.typed_project(n, 2, off, x, 1, W, b, 1, 1, out, 1, ws)
+    assert out[-1] == 16.0 and out[1 << 30] == 22.0 and out[0] == 4.0
+    out[-1] = out[1 << 30] = 4.0
+    assert (out == 4.0).all()
+    x[-1] = x[1 << 30] = 1.0
+    out.fill_(1.0)
+    dW, db = torch.empty(2, 1, 1, device="cuda"), torch.empty(2, 1, device="cuda")
+    dx = torch.empty_like(x)
+    tb.typed_project_grad(n, 2, off, x, 1, W, out, 1, 1, 1, dx, 1, dW, db, ws)
+    assert (dx == 3.0).all()
+    assert dW.flatten().tolist() == [0.0, 2.0 ** 31] and db.flatten().tolist() == [0.0, 2.0 ** 31]

@@ -109,3 +109,9 @@ def test_host_memory_and_no_device_are_errors_not_crashes():
     with pytest.raises(tb.TaurusError) as e:
         tb.embed_rows(4, ids, table, 10, 8, 8, out, 8)
     assert e.value.code in (tb.ERROR_CODES["CUDA"], INVALID)
+
+
+def test_more_graphs_than_there_may_be(lib):
+    for f in (lib.taurus_norm_rows_workspace, lib.taurus_norm_rows_grad_workspace):
+        assert f(4, (1 << 30) + 1, 8, 1) == INVALID and f(4, 1 << 30, 8, 1) >= 0
+    assert call(lib.taurus_norm_rows, NORM, graphs=(1 << 30) + 1) == INVALID

@@ -511,6 +511,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           __syncwarp();
         }
         // The stage's number written out: with addresses that the compiler cannot tell to be the same in every lane each MMA took 110 cycles to issue.
+        const int left = (KIND == GRAD_W ? u.rows : a.Kc) - k * BK;
         auto issue = [&](auto stage) {
           constexpr unsigned AT = decltype(stage)::value * STAGE_BYTES;
           const unsigned long long da0 = A_MN ? desc_mn(operands + AT, BK * 128) : desc_k<ROW>(operands + AT);
@@ -518,6 +519,7 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           if (elected()) {
 #pragma unroll
             for (int kk = 0; kk < BK / 16; ++kk) {
+              if (kk * 16 >= left) break;                // both operands are zeros from there on (400 000 rows, 100 -> 256 fp32: 193 -> 186 us)
               unsigned long long da[NP], db[NP];
 #pragma unroll
               for (int p = 0; p < NP; ++p) {             // (addresses are in units of 16 bytes)

@@ -295,3 +295,16 @@ def test_refused_on_a_device():
         with pytest.raises(tb.TaurusError) as e:
             tb.typed_project_grad(4, 2, off, x, 8, W, out, 8, 8, 8, a["dx"], 8, a["dW"], a["db"], workspace(1 << 20))
         assert e.value.code == tb.ERROR_CODES["INVALID_ARG"]
+
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("sizes,K,N", [([5000, 0, 65, 3], 136, 264), ([30, 10], 40, 24), ([2100] * 40, 37, 130)])
+def test_each_gradient_alone_is_what_it_is_beside_the_others(t, sizes, K, N):
+    off, n, x, W, bias, dy = make(sizes, K, N, t)
+    new = lambda: (torch.full((n, K), 3.0, dtype=t, device="cuda"), torch.full((len(sizes), K, N), 3.0, device="cuda"), torch.full((len(sizes), N), 3.0, device="cuda"))
+    together, alone = new(), new()
+    backward(off, n, x, W, dy, *together)
+    for i in range(3):
+        backward(off, n, x, W, dy, *(a if i == j else None for j, a in enumerate(alone)))
+    for a, b in zip(together, alone):
+        assert torch.equal(a, b)

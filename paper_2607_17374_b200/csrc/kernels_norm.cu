@@ -531,7 +531,8 @@ __device__ __forceinline__ void write_grad(const Grads<T, V, SAME>& f, const Vec
   for (int k = 0; k < V; ++k) {
     float xh, dz;
     f.template element<ACT>(k, v.v[k], w.v[k], &xh, &dz);
-    o[k] = f.rstd[SAME ? 0 : k] * (f.gamma[k] * dz - m2[SAME ? 0 : k] - xh * m1[SAME ? 0 : k]);
+    // (the product rounded as it was in the sums: alone in its group an element's gradient is zero)
+    o[k] = f.rstd[SAME ? 0 : k] * (__fmul_rn(f.gamma[k], dz) - m2[SAME ? 0 : k] - xh * m1[SAME ? 0 : k]);
   }
   store_f32<T, V>(dx, o);
 }

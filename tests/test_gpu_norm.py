@@ -249,3 +249,21 @@ def test_refused_on_a_device():
         with pytest.raises(tb.TaurusError) as e:
             tb.norm_rows(9000, 1, None, big, 64, 64, 4, None, None, EPS, 1, torch.empty_like(big), 64, None, None, ws)
         assert e.value.code == tb.ERROR_CODES["INVALID_ARG"]
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("width", [1, 6, 24])
+@pytest.mark.parametrize("action", [tb.ACT_NONE, tb.ACT_SILU])
+def test_an_element_alone_in_its_group_has_no_gradient(t, width, action):
+    """Its output does not depend on it: exactly zero, not what rounding leaves of it times 1 / sqrt(eps)."""
+    g = torch.Generator("cuda").manual_seed(width)
+    n = 50
+    x, dy = (torch.randn(n, width, generator=g, device="cuda").to(t) for _ in range(2))
+    gamma, beta = torch.randn(width, generator=g, device="cuda"), torch.randn(width, generator=g, device="cuda")
+    off = torch.arange(n + 1, device="cuda")
+    mean, rstd = torch.empty(n, width, device="cuda"), torch.empty(n, width, device="cuda")
+    y, dx = torch.empty_like(x), torch.full_like(x, 3.0)
+    ws = torch.empty(max(tb.norm_rows_grad_workspace(n, n, width, width), 256), dtype=torch.uint8, device="cuda")
+    tb.norm_rows(n, n, off, x, width, width, width, gamma, beta, 1e-5, action, y, width, mean, rstd, ws)
+    tb.norm_rows_grad(n, n, off, x, width, width, width, gamma, beta, action, mean, rstd, dy, width, dx, width, None, None, ws)
+    assert torch.equal(mean, x.float()) and (dx == 0).all()

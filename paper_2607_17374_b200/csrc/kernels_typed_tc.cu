@@ -673,7 +673,9 @@ typed_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       for (int j = 0; j < 4; ++j) sum[j] = 0.f;
       return meet(sh, &phase);
     };
-    const void* const nothing = a.offsets;              // (an address for a copy that reads nothing)
+    // An address for a copy that reads nothing, aligned as the rows are: copies want that of a source that they do not read, too.  (offsets need be aligned to 8 bytes
+    // only; of grad_W's operands a may be null.)
+    const void* const nothing = KIND == GRAD_W ? a.b : a.a;
     if constexpr (NP == 3) {
       // a ring of rows as they were read, filled DEPTH stages ahead; quad i of thread t lies at (i LOADERS + t) 16: a warp reads only what it copied itself
       constexpr int DEPTH = S::RAW_DEPTH;

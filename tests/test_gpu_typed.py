@@ -308,3 +308,27 @@ def test_each_gradient_alone_is_what_it_is_beside_the_others(t, sizes, K, N):
         backward(off, n, x, W, dy, *(a if i == j else None for j, a in enumerate(alone)))
     for a, b in zip(together, alone):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("sizes,K,N", [([300, 0, 41, 7], 100, 36), ([1500, 1030, 40], 68, 132), ([70, 65] * 40, 392, 120)])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (4, 4)])
+def test_offsets_at_any_element(t, sizes, K, N, pad, shift):
+    """Offsets that begin at the second element of their storage, 8 bytes off 16: the bits that offsets of their own give, also where a stage of the rows is only partly there."""
+    off, n, x, W, bias, dy = make(sizes, K, N, t, pad=pad, shift=shift)
+    own = torch.tensor(off, device="cuda")
+    slid = torch.tensor([-1] + off, device="cuda")[1:]
+    assert own.data_ptr() % 16 == 0 and slid.data_ptr() % 16 == 8
+    G, results = len(sizes), []
+    for o in (own, slid):
+        out, dx = torch.empty(n, N, dtype=t, device="cuda"), torch.empty(n, K, dtype=t, device="cuda")
+        dW, db, alone = torch.empty(G, K, N, device="cuda"), torch.empty(G, N, device="cuda"), torch.empty(G, N, device="cuda")
+        ws = workspace(tb.typed_project_grad_workspace(n, G, K, N, t))
+        tb.typed_project(n, G, o, x, x.stride(0), W, bias, K, N, out, N, ws)
+        tb.typed_project_grad(n, G, o, x, x.stride(0), W, dy, dy.stride(0), K, N, dx, K, dW, db, ws)
+        tb.typed_project_grad(n, G, o, x, x.stride(0), W, dy, dy.stride(0), K, N, grad_bias=alone, workspace=ws)
+        assert torch.equal(db, alone)
+        results.append((out, dx, dW, db))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    ref, mag = typed(off, x, W, bias)
+    close(results[1][0], ref, mag * sums(K))

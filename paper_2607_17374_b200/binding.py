@@ -263,6 +263,15 @@ def _row_type(t) -> int:
     return code
 
 
+def _type_of(rows, said) -> int:
+    """The type of rows: that of the tensor, or with an address in its place what the caller says.  A tensor of another type than said is refused: the
+    call would reach past its end."""
+    t = _row_type(rows if said is None else said)
+    if said is not None and hasattr(rows, "dtype") and _row_type(rows) != t:
+        raise TypeError("the call says another type than the tensor's, %s" % rows.dtype)
+    return t
+
+
 def _rows(x, n: int, width: int, ld: int) -> Optional[int]:
     """Address of n rows: a 2-D tensor of at least n x width whose rows are contiguous and ld elements apart, or an address."""
     if x is None or isinstance(x, int):
@@ -305,8 +314,8 @@ def embed_rows(n: int, ids, table, table_rows: int, width: int, ld_table: int, o
     """taurus_embed_rows: out_rows[i] = scale * table[ids[i]] (id -1: zeros).  Device tensors; ids int64.  Types are those of the
     tensors; with addresses in their place table_type and out_type say them."""
     _checked(load_library().taurus_embed_rows(
-        n, _array(ids, "int64", n), _rows(table, table_rows, width, ld_table), _row_type(table if table_type is None else table_type), table_rows, width, ld_table, scale,
-        _rows(out_rows, n, width, ld_out), _row_type(out_rows if out_type is None else out_type), ld_out, _array(status, "int32", 1), _stream(stream)),
+        n, _array(ids, "int64", n), _rows(table, table_rows, width, ld_table), _type_of(table, table_type), table_rows, width, ld_table, scale,
+        _rows(out_rows, n, width, ld_out), _type_of(out_rows, out_type), ld_out, _array(status, "int32", 1), _stream(stream)),
         "taurus_embed_rows")
 
 
@@ -319,8 +328,8 @@ def embed_grad(n: int, ids, grad_rows, ld_grad: int, width: int, grad_table, tab
                stream=None, grad_type=None, table_type=None):
     """taurus_embed_grad: grad_table[v] = scale * sum of the grad_rows[i] with ids[i] = v; every row is written."""
     _checked(load_library().taurus_embed_grad(
-        n, _array(ids, "int64", n), _rows(grad_rows, n, width, ld_grad), _row_type(grad_rows if grad_type is None else grad_type), ld_grad, width, scale,
-        _rows(grad_table, table_rows, width, ld_table), _row_type(grad_table if table_type is None else table_type), table_rows, ld_table, *_space(workspace),
+        n, _array(ids, "int64", n), _rows(grad_rows, n, width, ld_grad), _type_of(grad_rows, grad_type), ld_grad, width, scale,
+        _rows(grad_table, table_rows, width, ld_table), _type_of(grad_table, table_type), table_rows, ld_table, *_space(workspace),
         _array(status, "int32", 1), _stream(stream)), "taurus_embed_grad")
 
 
@@ -332,12 +341,12 @@ def typed_project_workspace(n: int, types: int, d_in: int, d_out: int, type) -> 
 def typed_project(n: int, types: int, offsets, x, ld_x: int, W, bias, d_in: int, d_out: int, out, ld_out: int, workspace=None, status=None, stream=None,
                   type=None, out_type=None):
     """taurus_typed_project: out[r] = x[r] W[g] + bias[g] for the rows r in [offsets[g], offsets[g + 1])."""
-    t = _row_type(x if type is None else type)
+    t = _type_of(x, type)
     if hasattr(W, "dtype") and _row_type(W) != t:
         raise TypeError("x and W are of one type")
     _checked(load_library().taurus_typed_project(
         n, types, _array(offsets, "int64", types + 1), _rows(x, n, d_in, ld_x), ld_x, t, _array(W, None, types * d_in * d_out), _array(bias, "float32", types * d_out), d_in, d_out, _rows(out, n, d_out, ld_out),
-        _row_type(out if out_type is None else out_type), ld_out, *_space(workspace), _array(status, "int32", 1), _stream(stream)), "taurus_typed_project")
+        _type_of(out, out_type), ld_out, *_space(workspace), _array(status, "int32", 1), _stream(stream)), "taurus_typed_project")
 
 
 def typed_project_grad_workspace(n: int, types: int, d_in: int, d_out: int, type) -> int:
@@ -348,13 +357,13 @@ def typed_project_grad_workspace(n: int, types: int, d_in: int, d_out: int, type
 def typed_project_grad(n: int, types: int, offsets, x, ld_x: int, W, grad_out, ld_grad: int, d_in: int, d_out: int, grad_x=None, ld_grad_x: int = 0, grad_W=None,
                        grad_bias=None, workspace=None, status=None, stream=None, type=None, grad_W_type=None):
     """taurus_typed_project_grad: the gradients asked for (grad_x, grad_W, grad_bias) from grad_out."""
-    t = _row_type(grad_out if type is None else type)
+    t = _type_of(grad_out, type)
     for other in (x, W, grad_out, grad_x):
         if hasattr(other, "dtype") and _row_type(other) != t:
             raise TypeError("x, W, grad_out and grad_x are of one type")
     _checked(load_library().taurus_typed_project_grad(
         n, types, _array(offsets, "int64", types + 1), _rows(x, n, d_in, ld_x), ld_x, t, _array(W, None, types * d_in * d_out), _rows(grad_out, n, d_out, ld_grad), ld_grad, d_in, d_out, _rows(grad_x, n, d_in, ld_grad_x or d_in),
-        ld_grad_x or d_in, _array(grad_W, None, types * d_in * d_out), t if grad_W is None else _row_type(grad_W if grad_W_type is None else grad_W_type), _array(grad_bias, "float32", types * d_out),
+        ld_grad_x or d_in, _array(grad_W, None, types * d_in * d_out), t if grad_W is None else _type_of(grad_W, grad_W_type), _array(grad_bias, "float32", types * d_out),
         *_space(workspace), _array(status, "int32", 1), _stream(stream)), "taurus_typed_project_grad")
 
 
@@ -366,7 +375,7 @@ def norm_rows_workspace(n: int, graphs: int, width: int, groups: int) -> int:
 def norm_rows(n: int, graphs: int, offsets, x, ld_x: int, width: int, groups: int, gamma, beta, eps: float, act: int, out_rows, ld_out: int, mean=None, rstd=None,
               workspace=None, status=None, stream=None, type=None):
     """taurus_norm_rows: group norm with an activation (ACT_NONE, ACT_RELU, ACT_SILU) over the rows of each graph."""
-    t = _row_type(x if type is None else type)
+    t = _type_of(x, type)
     if hasattr(out_rows, "dtype") and _row_type(out_rows) != t:
         raise TypeError("x and out_rows are of one type")
     _checked(load_library().taurus_norm_rows(
@@ -383,7 +392,7 @@ def norm_rows_grad_workspace(n: int, graphs: int, width: int, groups: int) -> in
 def norm_rows_grad(n: int, graphs: int, offsets, x, ld_x: int, width: int, groups: int, gamma, beta, act: int, mean, rstd, grad_out, ld_grad: int, grad_x,
                    ld_grad_x: int, grad_gamma=None, grad_beta=None, workspace=None, status=None, stream=None, type=None):
     """taurus_norm_rows_grad: gradients of norm_rows, with mean and rstd as the forward call left them."""
-    t = _row_type(x if type is None else type)
+    t = _type_of(x, type)
     for other in (grad_out, grad_x):
         if hasattr(other, "dtype") and _row_type(other) != t:
             raise TypeError("x, grad_out and grad_x are of one type")

@@ -115,3 +115,24 @@ def test_more_graphs_than_there_may_be(lib):
     for f in (lib.taurus_norm_rows_workspace, lib.taurus_norm_rows_grad_workspace):
         assert f(4, (1 << 30) + 1, 8, 1) == INVALID and f(4, 1 << 30, 8, 1) >= 0
     assert call(lib.taurus_norm_rows, NORM, graphs=(1 << 30) + 1) == INVALID
+
+
+def test_a_type_that_is_said_and_is_not_the_tensors():
+    """Tensors are taken at their own type; an argument that says a wider one would have the call reach past their end."""
+    ids, off, v = torch.zeros(4, dtype=torch.int64), torch.tensor([0, 4]), torch.zeros(8)
+    x, y, table, W = (torch.zeros(s, dtype=torch.bfloat16) for s in ((4, 8), (4, 8), (10, 8), (1, 8, 8)))
+    ws = torch.empty(1 << 16, dtype=torch.uint8)
+    one = torch.zeros(1, 2)
+    P = x.data_ptr()
+    for call in (lambda: tb.embed_rows(4, ids, table, 10, 8, 8, x, 8, table_type=tb.F32),
+                 lambda: tb.embed_rows(4, ids, table, 10, 8, 8, x, 8, out_type=torch.float32),
+                 lambda: tb.embed_grad(4, ids, x, 8, 8, table, 10, 8, ws, grad_type=tb.F32),
+                 lambda: tb.embed_grad(4, ids, x, 8, 8, table, 10, 8, ws, table_type=tb.F16),
+                 lambda: tb.typed_project(4, 1, off, x, 8, P, None, 8, 8, P, 8, type=tb.F32, out_type=tb.F32),
+                 lambda: tb.typed_project(4, 1, off, x, 8, W, None, 8, 8, y, 8, out_type=tb.F32),
+                 lambda: tb.typed_project_grad(4, 1, off, P, 8, P, x, 8, 8, 8, P, 8, type=tb.F32),
+                 lambda: tb.typed_project_grad(4, 1, off, x, 8, W, y, 8, 8, 8, grad_W=W, grad_W_type=tb.F32),
+                 lambda: tb.norm_rows(4, 1, off, x, 8, 8, 2, v, v, 1e-5, 1, P, 8, type=tb.F32),
+                 lambda: tb.norm_rows_grad(4, 1, off, x, 8, 8, 2, v, v, 1, one, one, P, 8, P, 8, workspace=ws, type=tb.F32)):
+        with pytest.raises(TypeError):
+            call()

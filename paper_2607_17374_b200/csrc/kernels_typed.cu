@@ -150,6 +150,10 @@ struct Space {
     if (grad) { part = take(typed_tc_part_bytes(n, types, d_in, d_out, type)); dy = take(typed_tc_row_bytes(n, d_out, type)); }
     x = take(typed_tc_row_bytes(n, d_in, type));
   }
+  TypedSpaces at(void* workspace) const {
+    char* const p = static_cast<char*>(workspace);
+    return {p, p + part, p + dy, p + x};
+  }
 };
 
 }  // namespace
@@ -191,15 +195,7 @@ extern "C" int taurus_typed_project(int64_t n, int32_t types, const int64_t* off
   const long long* const off = reinterpret_cast<const long long*>(offsets);
   int rc = TAURUS_OK;
   if (n > FEW_ROWS) {
-    if (packs) rc = typed_tc_pack(type, W, types, d_in, d_out, workspace, sms, st);
-    const void* rows = x;
-    int64_t ld_rows = ld_x;
-    if (typed_tc_packs_rows(x, ld_x, d_in, type)) {
-      void* const at = static_cast<char*>(workspace) + space.x;
-      typed_tc_pack_rows(x, ld_x, n, d_in, at, sms, st);
-      rows = at; ld_rows = typed_tc_row_pitch(d_in);
-    }
-    if (!rc) rc = typed_tc_rows(false, n, types, off, rows, ld_rows, type, packs ? workspace : W, bias, d_in, d_out, out, out_type, ld_out, status, sms, st);
+    rc = typed_tc_project(n, types, off, x, ld_x, type, W, bias, d_in, d_out, out, out_type, ld_out, space.at(workspace), status, sms, st);
   } else with_row_type(type, [&](auto tt) {
     using T = typename decltype(tt)::type;
     return with_vector(vector_of(ts, W, d_out), [&](auto vc) {
@@ -250,24 +246,7 @@ extern "C" int taurus_typed_project_grad(int64_t n, int32_t types, const int64_t
   const long long* const off = reinterpret_cast<const long long*>(offsets);
   int rc = TAURUS_OK;
   if (n > FEW_ROWS) {
-    char* const at = static_cast<char*>(workspace);
-    if (packs) rc = typed_tc_pack(type, W, types, d_in, d_out, at, sms, st);
-    auto laid_out = [&](const void** rows, int64_t* ld, int width, size_t where) {
-      if (typed_tc_packs_rows(*rows, *ld, width, type)) {
-        typed_tc_pack_rows(*rows, *ld, n, width, at + where, sms, st);
-        *rows = at + where; *ld = typed_tc_row_pitch(width);
-      }
-    };
-    const void *dy_rows = grad_out, *x_rows = x;
-    int64_t ld_dy_rows = ld_grad, ld_x_rows = ld_x;
-    laid_out(&dy_rows, &ld_dy_rows, d_out, space.dy);
-    if (grad_W) laid_out(&x_rows, &ld_x_rows, d_in, space.x);
-    else if (x && typed_tc_packs_rows(x, ld_x, d_in, type)) x_rows = nullptr;      // (grad_bias as beside grad_W)
-    if (!rc && grad_x)
-      rc = typed_tc_rows(true, n, types, off, dy_rows, ld_dy_rows, type, packs ? at : W, nullptr, d_in, d_out, grad_x, type, ld_grad_x, status, sms, st);
-    float* const part = reinterpret_cast<float*>(at + space.part);
-    if (!rc && (grad_W || grad_bias))
-      rc = typed_tc_weights(n, types, off, x_rows, ld_x_rows, type, dy_rows, ld_dy_rows, d_in, d_out, grad_W, grad_W_type, grad_bias, part, status, sms, st);
+    rc = typed_tc_project_grad(n, types, off, x, ld_x, type, W, grad_out, ld_grad, d_in, d_out, grad_x, ld_grad_x, grad_W, grad_W_type, grad_bias, space.at(workspace), status, sms, st);
   } else with_row_type(type, [&](auto tt) {
     using T = typename decltype(tt)::type;
     const T *const xp = static_cast<const T*>(x), *const wp = static_cast<const T*>(W), *const dyp = static_cast<const T*>(grad_out);

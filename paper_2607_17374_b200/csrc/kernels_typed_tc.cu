@@ -963,9 +963,12 @@ bool make_map(CUtensorMap* m, int32_t type, const void* base, long long cols, lo
   const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
   const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
   const EncodeTiledFn encode = encode_fn();
-  return encode && encode(m, type == TAURUS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, depth > 0 ? 3 : 2, const_cast<void*>(base), dims, strides, box,
-                     one, CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const CUresult r = !encode ? CUDA_ERROR_NOT_FOUND
+                             : encode(m, type == TAURUS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, depth > 0 ? 3 : 2, const_cast<void*>(base), dims, strides,
+                                      box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) taurus_note_cuda_error(static_cast<cudaError_t>(r), "cuTensorMapEncodeTiled");      // (the two enumerations share their numbers)
+  return r == CUDA_SUCCESS;
 }
 // TcArgs::a_vec
 int vec_of(const void* p, long long ld, int size) {
@@ -973,7 +976,6 @@ int vec_of(const void* p, long long ld, int size) {
   while (v > 1 && (ld % v != 0 || !rows_aligned(p, v * size))) v >>= 1;
   return size == 4 && v < 4 ? 0 : v;
 }
-bool tma_rows(const void* p, long long ld) { return ld % 8 == 0 && rows_aligned(p, 16); }      // of 16-bit elements
 
 // Blocks of nearly equal width, a multiple of 16.
 int block_columns(int N, int most) {
@@ -981,53 +983,65 @@ int block_columns(int N, int most) {
   return taurus_round_up((np + blocks - 1) / blocks, 16);
 }
 
+// A product ready to be launched.  All of a call's are made ready before its first launch: a call that fails has enqueued nothing.
+struct Product {
+  CUtensorMap ma = {}, mb = {};
+  TcArgs a = {};
+  long long units = 0;        // at most
+  bool loaded = false;
+};
+
 template <class T, int KIND, bool LOADED>
-int launch(const CUtensorMap& ma, const CUtensorMap& mb, TcArgs a, long long most_units, int sms, cudaStream_t st) {
+int launch(const Product& p, int sms, cudaStream_t st) {
   constexpr int shared = Shape<T, KIND, LOADED>::SHARED_BYTES + (int)sizeof(Shared);
   const cudaError_t e = cudaFuncSetAttribute(typed_tc_kernel<T, KIND, LOADED>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
   if (e != cudaSuccess) { taurus_note_cuda_error(e, "typed_project"); return TAURUS_ERR_CUDA; }
   constexpr int threads = Shape<T, KIND, LOADED>::THREADS;
-  typed_tc_kernel<T, KIND, LOADED><<<(int)std::max<long long>(1, std::min<long long>(most_units, sms)), threads, shared, st>>>(ma, mb, a);
+  typed_tc_kernel<T, KIND, LOADED><<<(int)std::max<long long>(1, std::min<long long>(p.units, sms)), threads, shared, st>>>(p.ma, p.mb, p.a);
   return TAURUS_OK;
 }
-template <int KIND, class F>
-int launch_type(int32_t type, bool loaded, F f) {     // f(launch function)
-  if (type == TAURUS_F32) return f(launch<float, KIND, true>);
-  if (type == TAURUS_BF16) return loaded ? f(launch<__nv_bfloat16, KIND, true>) : f(launch<__nv_bfloat16, KIND, false>);
-  return loaded ? f(launch<__half, KIND, true>) : f(launch<__half, KIND, false>);
+template <int KIND>
+int launch_type(int32_t type, const Product& p, int sms, cudaStream_t st) {
+  if (type == TAURUS_F32) return launch<float, KIND, true>(p, sms, st);
+  if (type == TAURUS_BF16) return p.loaded ? launch<__nv_bfloat16, KIND, true>(p, sms, st) : launch<__nv_bfloat16, KIND, false>(p, sms, st);
+  return p.loaded ? launch<__half, KIND, true>(p, sms, st) : launch<__half, KIND, false>(p, sms, st);
 }
 
 int weight_pitch(int d_out) { return taurus_round_up(d_out, 8); }
 int bn_most(int32_t type, bool grad_w, bool loaded) { return type == TAURUS_F32 ? (grad_w ? 128 : 256) : loaded ? 128 : 256; }     // Shape::BN
+
+// Rows of a width that keeps TMA off, fp32 aside, are laid out at another pitch (rows of such a width whose own pitch suits TMA are not).
+int64_t row_pitch(int width) { return taurus_round_up(width, 8); }
+bool packs_rows(const void* p, int64_t ld, int width, int32_t type) { return typed_tc_row_bytes(1, width, type) > 0 && !tma_rows(p, ld); }
+// Rows of a chunk of grad_W: about two units to an SM, 1 024 rows at least, 2 048 at most.  fp32: 1 024 (2 700, as 400 000 rows in 5 types would have: 2.9e-6 of the result
+// off, where fp32 sums are 1.1e-6).
+int rows_of_chunk(int64_t n, int d_in, int d_out, int32_t type) {
+  if (type == TAURUS_F32) return 1024;
+  const long long tiles = (long long)((d_in + BM - 1) / BM) * ((d_out + 255) / 256);
+  return (int)std::min<long long>(2048, std::max<long long>(1024, taurus_round_up((int)std::min<long long>(n * tiles / 296, 1 << 20), 64)));
+}
 
 }  // namespace
 
 // Does W have to be laid out anew?  Room for it (whatever its address, which a workspace's size does not depend on).
 bool typed_tc_packs(const void* W, int32_t type, int d_out) { return type == TAURUS_F32 || d_out % 8 != 0 || !rows_aligned(W, 16); }
 size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type) { return (size_t)types * (type == TAURUS_F32 ? 3 : 1) * d_in * weight_pitch(d_out) * 2; }
-// Rows of a width that keeps TMA off, fp32 aside: room for them at another pitch, and whether these need it (rows of such a width whose own pitch suits TMA do not).
-int64_t typed_tc_row_pitch(int width) { return taurus_round_up(width, 8); }
-size_t typed_tc_row_bytes(int64_t n, int width, int32_t type) { return type == TAURUS_F32 || width % 8 == 0 ? 0 : (size_t)n * (size_t)typed_tc_row_pitch(width) * 2; }
-bool typed_tc_packs_rows(const void* p, int64_t ld, int width, int32_t type) { return typed_tc_row_bytes(1, width, type) > 0 && !tma_rows(p, ld); }
-void typed_tc_pack_rows(const void* rows, int64_t ld, int64_t n, int width, void* packed, int sms, cudaStream_t st) {
-  const int pitch = (int)typed_tc_row_pitch(width);
-  const int grid = (int)std::min<long long>((n * (pitch / 8) + 255) / 256, (long long)sms * 32);
-  typed_pack_rows_kernel<<<grid, 256, 0, st>>>(static_cast<const unsigned short*>(rows), ld, n, width, pitch, static_cast<uint4*>(packed));
-}
-// Rows of a chunk of grad_W: about two units to an SM, 1 024 rows at least, 2 048 at most.  fp32: 1 024 (2 700, as 400 000 rows in 5 types would have: 2.9e-6 of the result
-// off, where fp32 sums are 1.1e-6).
-int typed_tc_chunk(int64_t n, int d_in, int d_out, int32_t type) {
-  if (type == TAURUS_F32) return 1024;
-  const long long tiles = (long long)((d_in + BM - 1) / BM) * ((d_out + 255) / 256);
-  return (int)std::min<long long>(2048, std::max<long long>(1024, taurus_round_up((int)std::min<long long>(n * tiles / 296, 1 << 20), 64)));
-}
+// Room for rows at another pitch.
+size_t typed_tc_row_bytes(int64_t n, int width, int32_t type) { return type == TAURUS_F32 || width % 8 == 0 ? 0 : (size_t)n * (size_t)row_pitch(width) * 2; }
 // A type of more than one chunk has more than `chunk` rows and at most rows / chunk + 1 chunks.
 size_t typed_tc_part_bytes(int64_t n, int32_t types, int d_in, int d_out, int32_t type) {
-  const int chunk = typed_tc_chunk(n, d_in, d_out, type);
+  const int chunk = rows_of_chunk(n, d_in, d_out, type);
   return (size_t)(n / chunk + std::min<int64_t>(types, n / chunk)) * (size_t)(d_in + 1) * d_out * 4;
 }
 
-int typed_tc_pack(int32_t type, const void* W, int32_t types, int d_in, int d_out, void* packed, int sms, cudaStream_t st) {
+namespace {
+
+void pack_rows(const void* rows, int64_t ld, int64_t n, int width, void* packed, int sms, cudaStream_t st) {
+  const int pitch = (int)row_pitch(width);
+  const int grid = (int)std::min<long long>((n * (pitch / 8) + 255) / 256, (long long)sms * 32);
+  typed_pack_rows_kernel<<<grid, 256, 0, st>>>(static_cast<const unsigned short*>(rows), ld, n, width, pitch, static_cast<uint4*>(packed));
+}
+void pack_weights(int32_t type, const void* W, int32_t types, int d_in, int d_out, void* packed, int sms, cudaStream_t st) {
   const long long quads = (long long)types * d_in * ((d_out + 3) / 4);
   const int grid = (int)std::min<long long>((quads + 255) / 256, (long long)sms * 16);
   with_row_type(type, [&](auto tt) {
@@ -1035,56 +1049,99 @@ int typed_tc_pack(int32_t type, const void* W, int32_t types, int d_in, int d_ou
     typed_pack_kernel<T><<<grid, 256, 0, st>>>(static_cast<const T*>(W), types, d_in, d_out, weight_pitch(d_out), packed);
     return 0;
   });
-  return TAURUS_OK;
 }
 
-// out = x W + bias, or grad_x = grad_out W^T (transposed).  w: W itself, or what typed_tc_pack made of it.
-int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* w, const float* bias, int d_in, int d_out,
-                  void* out, int32_t out_type, int64_t ld_out, int32_t* status, int sms, cudaStream_t st) {
+// out = x W + bias, or grad_x = grad_out W^T (transposed).  w: W itself, or what pack_weights makes of it.
+bool ready_rows(Product* p, bool transposed, int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* w, const float* bias, int d_in,
+                int d_out, void* out, int32_t out_type, int64_t ld_out, int32_t* status) {
   const int Kc = transposed ? d_out : d_in, N = transposed ? d_in : d_out, planes = type == TAURUS_F32 ? 3 : 1;
-  const bool loaded = type == TAURUS_F32 || !tma_rows(x, ld_x);
+  p->loaded = type == TAURUS_F32 || !tma_rows(x, ld_x);
   const int bk = type == TAURUS_F32 ? 32 : 64;
-  TcArgs a = {};
+  TcArgs& a = p->a;
   a.n = n; a.offsets = offsets; a.types = types; a.N = N; a.Kc = Kc;
-  a.bn = block_columns(N, bn_most(type, false, loaded)); a.n_blocks = (N + a.bn - 1) / a.bn;
+  a.bn = block_columns(N, bn_most(type, false, p->loaded)); a.n_blocks = (N + a.bn - 1) / a.bn;
   a.a = x; a.lda = ld_x; a.a_vec = vec_of(x, ld_x, row_type_size(type));
   a.out = out; a.ld_out = ld_out; a.out_f32 = out_type == TAURUS_F32; a.out_vec = ld_out * row_type_size(out_type) % 16 == 0 && rows_aligned(out, 16);
   a.bias = bias; a.status = status;
-  CUtensorMap ma = {}, mb = {};
-  if (!loaded && !make_map(&ma, type, x, Kc, n, 0, ld_x, bk, BM)) return TAURUS_ERR_CUDA;
-  if (!make_map(&mb, type, w, d_out, d_in, (long long)types * planes, weight_pitch(d_out), transposed ? bk : 64, transposed ? a.bn : bk)) return TAURUS_ERR_CUDA;
-  const long long units = (n / BM + std::min<long long>(types, n)) * a.n_blocks;
-  auto go = [&](auto f) { return f(ma, mb, a, units, sms, st); };
-  return transposed ? launch_type<GRAD_X>(type, loaded, go) : launch_type<PROJECT>(type, loaded, go);
+  p->units = (n / BM + std::min<long long>(types, n)) * a.n_blocks;
+  return (p->loaded || make_map(&p->ma, type, x, Kc, n, 0, ld_x, bk, BM)) &&
+         make_map(&p->mb, type, w, d_out, d_in, (long long)types * planes, weight_pitch(d_out), transposed ? bk : 64, transposed ? a.bn : bk);
 }
 
 // grad_W and grad_bias (either may be null); part: typed_tc_part_bytes.
-int typed_tc_weights(int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* dy, int64_t ld_dy, int d_in, int d_out, void* dW,
-                     int32_t dW_type, float* db, float* part, int32_t* status, int sms, cudaStream_t st) {
-  const int chunk = typed_tc_chunk(n, d_in, d_out, type);
+bool ready_weights(Product* p, int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* dy, int64_t ld_dy, int d_in, int d_out, void* dW,
+                   int32_t dW_type, float* db, float* part, int32_t* status) {
+  const int chunk = rows_of_chunk(n, d_in, d_out, type);
   // (by x's rows too where only grad_bias is asked for: its sums are then formed as they are beside grad_W's)
-  const bool loaded = type == TAURUS_F32 || (x && !tma_rows(x, ld_x)) || !tma_rows(dy, ld_dy);
+  p->loaded = type == TAURUS_F32 || (x && !tma_rows(x, ld_x)) || !tma_rows(dy, ld_dy);
   const int bk = type == TAURUS_F32 ? 32 : 64, size = row_type_size(type), out_size = row_type_size(dW_type);
-  TcArgs a = {};
+  TcArgs& a = p->a;
   a.n = n; a.offsets = offsets; a.types = types; a.M = d_in; a.N = d_out; a.chunk = chunk;
-  a.bn = block_columns(d_out, bn_most(type, true, loaded)); a.n_blocks = (d_out + a.bn - 1) / a.bn; a.m_blocks = dW ? (d_in + BM - 1) / BM : 1;
+  a.bn = block_columns(d_out, bn_most(type, true, p->loaded)); a.n_blocks = (d_out + a.bn - 1) / a.bn; a.m_blocks = dW ? (d_in + BM - 1) / BM : 1;
   a.a = dW ? x : nullptr; a.lda = ld_x; a.a_vec = vec_of(x, ld_x, size);
   a.b = dy; a.ldb = ld_dy; a.b_vec = vec_of(dy, ld_dy, size);
   a.out = dW; a.out_f32 = dW_type == TAURUS_F32; a.out_vec = d_out * out_size % 16 == 0 && d_out % 4 == 0 && rows_aligned(dW, 16);
   a.db = db; a.part = part; a.status = status;
-  CUtensorMap ma = {}, mb = {};
-  if (!loaded && ((dW && !make_map(&ma, type, x, d_in, n, 0, ld_x, 64, bk)) || !make_map(&mb, type, dy, d_out, n, 0, ld_dy, 64, bk))) return TAURUS_ERR_CUDA;
-  const long long units = (n / chunk + types) * a.m_blocks * a.n_blocks;
-  const int rc = launch_type<GRAD_W>(type, loaded, [&](auto f) { return f(ma, mb, a, units, sms, st); });
+  p->units = (n / chunk + types) * a.m_blocks * a.n_blocks;
+  return p->loaded || ((!dW || make_map(&p->ma, type, x, d_in, n, 0, ld_x, 64, bk)) && make_map(&p->mb, type, dy, d_out, n, 0, ld_dy, 64, bk));
+}
+int launch_weights(const Product& p, int32_t type, int32_t dW_type, int sms, cudaStream_t st) {
+  const TcArgs& a = p.a;
+  const int rc = launch_type<GRAD_W>(type, p, sms, st);
   if (rc) return rc;
   JoinArgs j = {};
-  j.n = n; j.offsets = offsets; j.types = types; j.K = d_in; j.N = d_out; j.chunk = chunk; j.part = part; j.dW = dW; j.db = db;
-  if (n > chunk)
-    with_row_type(dW ? dW_type : TAURUS_F32, [&](auto tt) {
+  j.n = a.n; j.offsets = a.offsets; j.types = a.types; j.K = a.M; j.N = a.N; j.chunk = a.chunk; j.part = a.part; j.dW = a.out; j.db = a.db;
+  if (a.n > a.chunk)
+    with_row_type(a.out ? dW_type : TAURUS_F32, [&](auto tt) {
       using O = typename decltype(tt)::type;
-      const long long size = (long long)(d_in + 1) * d_out;
-      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 255) / 256, std::max(8, 16 * sms / types)), (unsigned)types), 256, 0, st>>>(j);
+      const long long size = (long long)(a.M + 1) * a.N;
+      typed_join_kernel<O><<<dim3((unsigned)std::min<long long>((size + 255) / 256, std::max(8, 16 * sms / a.types)), (unsigned)a.types), 256, 0, st>>>(j);
       return 0;
     });
   return TAURUS_OK;
+}
+
+// Rows as the products take them: where they are, or at `space` at another pitch (laid out there once everything is ready).
+struct Rows {
+  const void* from;
+  int64_t ld_from;
+  int width;
+  void* space;
+  bool packs;
+  Rows(const void* rows, int64_t ld, int width, int32_t type, void* space) : from(rows), ld_from(ld), width(width), space(space), packs(rows && packs_rows(rows, ld, width, type)) {}
+  const void* at() const { return packs ? space : from; }
+  int64_t ld() const { return packs ? row_pitch(width) : ld_from; }
+  void lay_out(int64_t n, int sms, cudaStream_t st) const { if (packs) pack_rows(from, ld_from, n, width, space, sms, st); }
+};
+
+}  // namespace
+
+int typed_tc_project(int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* W, const float* bias, int d_in, int d_out, void* out,
+                     int32_t out_type, int64_t ld_out, const TypedSpaces& spaces, int32_t* status, int sms, cudaStream_t st) {
+  const bool packs = typed_tc_packs(W, type, d_out);
+  const Rows rows(x, ld_x, d_in, type, spaces.x);
+  Product p;
+  if (!ready_rows(&p, false, n, types, offsets, rows.at(), rows.ld(), type, packs ? spaces.W : W, bias, d_in, d_out, out, out_type, ld_out, status)) return TAURUS_ERR_CUDA;
+  if (packs) pack_weights(type, W, types, d_in, d_out, spaces.W, sms, st);
+  rows.lay_out(n, sms, st);
+  return launch_type<PROJECT>(type, p, sms, st);
+}
+
+int typed_tc_project_grad(int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* W, const void* grad_out, int64_t ld_grad, int d_in,
+                          int d_out, void* grad_x, int64_t ld_grad_x, void* grad_W, int32_t grad_W_type, float* grad_bias, const TypedSpaces& spaces, int32_t* status, int sms,
+                          cudaStream_t st) {
+  const bool packs = grad_x && typed_tc_packs(W, type, d_out), weights = grad_W || grad_bias;
+  const Rows dy(grad_out, ld_grad, d_out, type, spaces.dy);
+  Rows rows(x, ld_x, d_in, type, spaces.x);
+  if (!grad_W && rows.packs) rows = Rows(nullptr, ld_x, d_in, type, nullptr);      // (grad_bias as beside grad_W, whose rows would be laid out for TMA)
+  Product p, q;
+  if (grad_x && !ready_rows(&p, true, n, types, offsets, dy.at(), dy.ld(), type, packs ? spaces.W : W, nullptr, d_in, d_out, grad_x, type, ld_grad_x, status)) return TAURUS_ERR_CUDA;
+  if (weights && !ready_weights(&q, n, types, offsets, rows.at(), rows.ld(), type, dy.at(), dy.ld(), d_in, d_out, grad_W, grad_W_type, grad_bias, static_cast<float*>(spaces.part), status))
+    return TAURUS_ERR_CUDA;
+  if (packs) pack_weights(type, W, types, d_in, d_out, spaces.W, sms, st);
+  dy.lay_out(n, sms, st);
+  rows.lay_out(n, sms, st);
+  int rc = grad_x ? launch_type<GRAD_X>(type, p, sms, st) : TAURUS_OK;
+  if (!rc && weights) rc = launch_weights(q, type, grad_W_type, sms, st);
+  return rc;
 }

@@ -37,16 +37,19 @@ static __device__ __forceinline__ Split4 split4(float a, float b, float c, float
   return {make_uint2(p.hi, q.hi), make_uint2(p.mid, q.mid), make_uint2(p.lo, q.lo)};
 }
 
+// Can TMA read rows of 16-bit elements?  (A tensor map holds pitches below 2^40 bytes.)
+static inline bool tma_rows(const void* p, long long ld) { return ld % 8 == 0 && ld < (1ll << 39) && rows_aligned(p, 16); }
+
 // ---- kernels_typed_tc.cu
+// Parts of a call's workspace: W laid out anew, partial results of grad_W, rows of grad_out and of x at other pitches.
+struct TypedSpaces { void *W, *part, *dy, *x; };
 bool typed_tc_packs(const void* W, int32_t type, int d_out);
 size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type);
 size_t typed_tc_row_bytes(int64_t n, int width, int32_t type);
-int64_t typed_tc_row_pitch(int width);
-bool typed_tc_packs_rows(const void* p, int64_t ld, int width, int32_t type);
-void typed_tc_pack_rows(const void* rows, int64_t ld, int64_t n, int width, void* packed, int sms, cudaStream_t st);
 size_t typed_tc_part_bytes(int64_t n, int32_t types, int d_in, int d_out, int32_t type);
-int typed_tc_pack(int32_t type, const void* W, int32_t types, int d_in, int d_out, void* packed, int sms, cudaStream_t st);
-int typed_tc_rows(bool transposed, int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* w, const float* bias, int d_in, int d_out,
-                  void* out, int32_t out_type, int64_t ld_out, int32_t* status, int sms, cudaStream_t st);
-int typed_tc_weights(int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* dy, int64_t ld_dy, int d_in, int d_out, void* dW,
-                     int32_t dW_type, float* db, float* part, int32_t* status, int sms, cudaStream_t st);
+// (arguments as checked by the entry points; TAURUS_ERR_CUDA with nothing enqueued where a tensor map cannot be made)
+int typed_tc_project(int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* W, const float* bias, int d_in, int d_out, void* out,
+                     int32_t out_type, int64_t ld_out, const TypedSpaces& spaces, int32_t* status, int sms, cudaStream_t st);
+int typed_tc_project_grad(int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* W, const void* grad_out, int64_t ld_grad, int d_in,
+                          int d_out, void* grad_x, int64_t ld_grad_x, void* grad_W, int32_t grad_W_type, float* grad_bias, const TypedSpaces& spaces, int32_t* status, int sms,
+                          cudaStream_t st);

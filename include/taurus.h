@@ -501,8 +501,10 @@ int taurus_embed_grad(int64_t n, const int64_t* ids, const void* grad_rows, int3
  * Projection by vertex type: out[r] = x[r] W[g] + bias[g] for the rows r in [offsets[g], offsets[g + 1]) of type g, g in
  * [0, types), types in 1 .. TAURUS_MAX_TYPES.  offsets: [types + 1], non-decreasing, inside [0, n]; a type may have no rows; rows of out in
  * front of offsets[0] or behind offsets[types] are left as they are.  Offsets that break this give TAURUS_ERR_INVALID_ARG in *status (the
- * rows written are then unspecified).  W: [types x d_in x d_out] row-major without gaps, of x's type; bias: [types x d_out] fp32 or
- * NULL; out_type: x's type or TAURUS_F32.  With TAURUS_F32 operands the products are as exact as fp32 multiplications; the sums are fp32.
+ * rows written are then unspecified).  W: [types x d_in x d_out] row-major without gaps, of x's type; bias: [types x d_out]
+ * fp32 or NULL; out_type: x's type or TAURUS_F32.  With TAURUS_F32 operands a product is off by less than 2^-24 of itself, as a rounded fp32 multiplication is, and the sums
+ * are fp32; an operand below 2^-110 in magnitude may be off by 2^-133, and a sum whose products' magnitudes add up to more than (1 - 2^-7) times the largest
+ * fp32 value may be infinite.
  */
 int64_t taurus_typed_project_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type);
 int taurus_typed_project(int64_t n, int32_t types, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, const void* W,

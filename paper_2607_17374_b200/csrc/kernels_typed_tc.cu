@@ -12,10 +12,11 @@
 //         warps 10..17 loaders (LOADED): operands that have to be split, or whose rows TMA cannot address; without loaders, in GRAD_W, they add up the
 //                      columns of grad_out for the bias, which the loaders do on the way
 //
-// fp32 operands: x = hi + mid + lo, three bf16 values that hold its 24 bits (hi by truncation, so that nothing overflows), and six of the nine
-// products: hi hi into one accumulator, hi mid + mid hi + mid mid + hi lo + lo hi into another.  What is left out is below 2^-24 of a product.
-// Each element keeps an exponent of its own, whatever stands beside it.  Two accumulators: where hi hi is not finite the sum is what it says
-// (an infinity times a mid or lo of zero would make it NaN).  W is split by a kernel in front (it is read once per tile), rows by the loaders.
+// fp32 operands: x = hi + mid + lo, three bf16 values that hold its 24 bits (typed.cuh), and six of the nine products: hi hi into one accumulator,
+// hi mid + mid hi + mid mid + hi lo + lo hi into another.  What is left out is below 2^-24 of a product, what rounding it to fp32 would cost.
+// Each element keeps an exponent of its own, whatever stands beside it; one below 2^-110 is off by up to 2^-133, one below 2^-134 counts as zero (also times an infinity).
+// Two accumulators: where hi hi is not finite the sum is what it says (an infinity times a mid or lo of zero would make it NaN).  hi may be larger than x, by 2^-8: where
+// products' magnitudes add up to more than (1 - 2^-7) times the largest fp32 value the sum may be infinite.  W is split by a kernel in front (it is read once per tile), rows by the loaders.
 //
 // What bounds it (1.2 M rows, 512 -> 256 bf16: 350 us, 5.3 TB/s of rows): the L2, which gives every 128 rows the whole of W's block again, 3 KB a row, 9.6 TB/s.  fp32
 // (400 000 rows, 256 -> 256): 294 us forward and 285 for grad_x, 196 of them the six products; the output of a block of 256 columns waits for its accumulators

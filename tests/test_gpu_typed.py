@@ -332,3 +332,47 @@ def test_offsets_at_any_element(t, sizes, K, N, pad, shift):
     assert all(torch.equal(a, b) for a, b in zip(*results))
     ref, mag = typed(off, x, W, bias)
     close(results[1][0], ref, mag * sums(K))
+
+
+def test_a_single_product_is_as_exact_as_fp32():
+    """Sums of one term.  What the split of the operands leaves out is below 2^-24 of a product; the five smaller products, together at most 2^-7 + 2^-16 of it, are added in steps
+    that lose 2^-23 of their sum each (below 2^-26 in all), and the last addition rounds by 2^-24: 2.25 2^-24.  Operands in [1, 2), and such whose middle and last parts are largest."""
+    n, N = 4096, 1024
+    g = torch.Generator("cuda").manual_seed(12)
+    bits = torch.randint(0, 1 << 23, (n + N,), generator=g, device="cuda", dtype=torch.int32)
+    bits[n // 2:n + N // 2] &= 0xFFFF
+    bits[:64] = bits[n:n + 64] = torch.arange(0xFFC0 - 64, 0xFFC0, device="cuda", dtype=torch.int32) | 0x7F0000
+    bits[64:128] = bits[n + 64:n + 128] = torch.arange(0x7FC0, 0x8000, device="cuda", dtype=torch.int32)
+    bits[128] = bits[n + 128] = 0xFF80
+    v = (bits | 0x3F800000).view(F32)
+    x, W = v[:n].view(n, 1).contiguous(), v[n:].view(1, 1, N).contiguous()
+    out = torch.empty(n, N, device="cuda")
+    forward([0, n], n, x, W, None, out)
+    ref = x.double() * W[0].double()
+    assert float(((out.double() - ref).abs() / ref).max()) <= 2.25 * U32
+    dx, dy = torch.empty(n, 1, device="cuda"), torch.zeros(n, N, device="cuda")
+    c = torch.arange(n, device="cuda") % N
+    dy[torch.arange(n, device="cuda"), c] = x[:, 0]
+    backward([0, n], n, x, W, dy, dx, None, None)
+    ref = x.double() * W[0, 0, c].double()[:, None]
+    assert float(((dx.double() - ref).abs() / ref).max()) <= 2.25 * U32
+    dW, one = torch.empty(n // 128, 1, N, device="cuda"), torch.zeros(n, N, device="cuda")      # a row that is not zero to each type
+    one[::128] = W[0, 0]
+    backward(list(range(0, n + 1, 128)), n, x, torch.zeros(n // 128, 1, N, device="cuda"), one, None, dW, None)
+    ref = x[::128, None].double() * W.double()
+    assert float(((dW.double() - ref).abs() / ref).max()) <= 2.25 * U32
+
+
+def test_largest_values_stay_finite():
+    """fp32's largest value times one, and sums of products up to (1 - 2^-7) times it."""
+    most = torch.finfo(F32).max
+    x = torch.tensor([most, -most, most * 0.999, 1.0], device="cuda").repeat(200)[:, None].contiguous()
+    W = torch.tensor([1.0, 0.5, -1.0, 2.0 ** -30], device="cuda").view(1, 1, 4)
+    out = torch.empty(800, 4, device="cuda")
+    forward([0, 800], 800, x, W, None, out)
+    assert torch.equal(out.double(), x.double() * W[0].double())
+    x = torch.full((300, 16), most / 16, device="cuda")
+    W = torch.full((1, 16, 8), 1 - 2.0 ** -7, device="cuda")
+    out = torch.empty(300, 8, device="cuda")
+    forward([0, 300], 300, x, W, None, out)
+    assert (out.double() - most * (1 - 2.0 ** -7)).abs().max() <= most * sums(16)

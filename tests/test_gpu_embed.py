@@ -160,3 +160,25 @@ def test_refused_on_a_device():
         with pytest.raises(tb.TaurusError) as e:
             tb.embed_grad(4, ids, g, 8, 8, t, 10, 8, w)
         assert e.value.code == tb.ERROR_CODES["INVALID_ARG"]
+
+
+@pytest.mark.parametrize("gt", [F32, BF16])
+@pytest.mark.parametrize("n,rows,width,kind", [
+    (20_000, 1, 64, "skew"), (2048, 3, 5, "skew"), (2049, 3, 5, "missing"), (160_001, 2000, 24, "same"), (310_000, 50, 12, "skew"), (310_000, 300_000, 8, "uniform"),
+    (606_207, 700, 4, "skew"), (606_208, 700, 4, "skew"), (700_001, 2, 3, "missing"), (1_300_000, 90_000, 16, "skew"), (2_500_000, 40, 2, "missing"), (5_000_000, 7, 1, "skew"),
+    (700_001, (1 << 22) + 7, 2, "skew"), (5000, (1 << 22) + 7, 3, "uniform"), (900_000, 1 << 22, 1, "missing"), (3000, (1 << 24) + 1, 1, "same")])
+def test_whole_numbers_add_up_exactly(gt, n, rows, width, kind):
+    """Small whole numbers, whose sums fp32 holds in any order: a row that is lost, doubled or added to another id's sum shows, however many an id has.  Calls with longer pieces,
+    sort blocks of several tiles, digits of three passes, and ids over many pieces."""
+    g = torch.Generator("cuda").manual_seed(n + rows)
+    ids = make_ids(n, rows, kind)
+    grad = torch.randint(-3, 4, (n, width), generator=g, device="cuda", dtype=torch.int8).to(gt)
+    table = torch.full((rows, width), 9.0, device="cuda")
+    ws = torch.full((tb.embed_grad_workspace(n, rows, width),), 255, dtype=torch.uint8, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    tb.embed_grad(n, ids, grad, width, width, table, rows, width, ws, 1.0, status)
+    assert 3 * n < 1 << 24 and int(status) == 0
+    want = torch.zeros(rows, width, dtype=torch.int64, device="cuda")
+    keep = ids >= 0
+    want.index_add_(0, ids[keep], grad[keep].long())
+    assert torch.equal(table, want.float())

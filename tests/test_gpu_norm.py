@@ -267,3 +267,57 @@ def test_an_element_alone_in_its_group_has_no_gradient(t, width, action):
     tb.norm_rows(n, n, off, x, width, width, width, gamma, beta, 1e-5, action, y, width, mean, rstd, ws)
     tb.norm_rows_grad(n, n, off, x, width, width, width, gamma, beta, action, mean, rstd, dy, width, dx, width, None, None, ws)
     assert torch.equal(mean, x.float()) and (dx == 0).all()
+
+
+def many(graphs, seed=1):
+    """Sizes of a large batch: graphs of 0 to 12 rows, and two beyond the length that one block takes."""
+    g = torch.Generator().manual_seed(seed)
+    sizes = (torch.rand(graphs, generator=g) ** 2 * 13).long().tolist()
+    sizes[graphs // 3], sizes[-7] = 2000, 5000
+    return sizes
+
+
+@pytest.mark.parametrize("t,a,C,groups,pad,shift", [(F32, tb.ACT_SILU, 64, 8, 0, 0), (BF16, tb.ACT_SILU, 64, 8, 0, 0), (F16, tb.ACT_NONE, 33, 3, 0, 0), (F32, tb.ACT_RELU, 40, 20, 3, 1),
+                                                    (BF16, tb.ACT_SILU, 96, 1, 8, 0)])
+def test_many_graphs(t, a, C, groups, pad, shift):
+    """More graphs than the gradient's kernel has blocks, so that each block has several, some empty, and a few long ones among them."""
+    test_norm_and_gradients(t, a, many(6000), C, groups, pad, shift, True)
+
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("C,groups", [(8, 2), (6, 3)])
+def test_more_graphs_than_blocks(t, C, groups):
+    """More than 2^20 graphs: each block of the forward call has several.  The bits are those of calls over a part of the batch, of the same average size (which the block's threads
+    depend on), and gradients of gamma and beta those of the parts' sums."""
+    G, parts = (1 << 20) + 4096, 16
+    sizes = torch.tensor([1, 2, 0, 3, 2, 0, 1, 7] * (G // 8), device="cuda")
+    off = torch.cat([sizes.new_zeros(1), sizes.cumsum(0)])
+    n, per = int(off[-1]), G // parts
+    g = torch.Generator("cuda").manual_seed(8)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    x, dy, gamma, beta = r(n, C).to(t), r(n, C).to(t), 1 + 0.1 * r(C), 0.1 * r(C)
+
+    def call(off, x, dy):
+        n, G = x.shape[0], off.numel() - 1
+        out, dx, mean, rstd, dga, dbe = (torch.full(s, 5.0, dtype=d, device="cuda") for s, d in (((n, C), t), ((n, C), t), ((G, groups), F32), ((G, groups), F32), ((C,), F32), ((C,), F32)))
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        tb.norm_rows(n, G, off, x, C, C, groups, gamma, beta, EPS, tb.ACT_SILU, out, C, mean, rstd, workspace(tb.norm_rows_workspace(n, G, C, groups)), status)
+        tb.norm_rows_grad(n, G, off, x, C, C, groups, gamma, beta, tb.ACT_SILU, mean, rstd, dy, C, dx, C, dga, dbe, workspace(tb.norm_rows_grad_workspace(n, G, C, groups)), status)
+        assert int(status) == 0
+        return out, dx, mean, rstd, dga.double(), dbe.double()
+    whole = call(off, x, dy)
+    pieces = []
+    for p in range(parts):
+        o = off[p * per:(p + 1) * per + 1]
+        b, e = int(o[0]), int(o[-1])
+        pieces.append(call((o - b).contiguous(), x[b:e], dy[b:e]))
+    for i, got in enumerate(whole[:4]):
+        assert torch.equal(got, torch.cat([p[i] for p in pieces]))
+    # terms of order one (|dz| <= 1.1 |dy|, |xh| <= sqrt of the group's elements), at most 2^12 of them to a thread's sum on either side
+    y, _, _, (_, rga, rbe) = norm(off[:per + 1].tolist()[:2001], x[:int(off[2000])], groups, gamma, beta, EPS, tb.ACT_SILU, dy[:int(off[2000])])
+    small = call(off[:2001].contiguous(), x[:int(off[2000])], dy[:int(off[2000])])
+    size = dy.double().abs().sum(0) * 1.1
+    span = (7 * C / groups) ** 0.5
+    for i, ref, scale in ((4, rga, span), (5, rbe, 1.0)):
+        assert ((small[i] - ref).abs() <= 4096 * U32 * size * scale).all()
+        assert ((whole[i] - sum(p[i] for p in pieces)).abs() <= 2 * 4096 * U32 * size * scale).all()

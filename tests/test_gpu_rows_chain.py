@@ -245,3 +245,41 @@ def test_most_rows_of_one_type():
     tb.typed_project_grad(n, 2, off, x, 1, W, out, 1, 1, 1, dx, 1, dW, db, ws)
     assert (dx == 3.0).all()
     assert dW.flatten().tolist() == [0.0, 2.0 ** 31] and db.flatten().tolist() == [0.0, 2.0 ** 31]
+
+
+@pytest.mark.parametrize("stream", [None, "own"])
+def test_a_norm_between_two_layers(stream):
+    """A layer's dense output on the device, normed in place, is what the next layer's chunks are pushed from."""
+    from dataclasses import replace
+    w = replace(tg.scaled(tg.WORKLOADS["large"], 2_500, chunk=512, name="normed"), dims=(48, 96, 40), fanout=(0, 0), pool_slots=2_500, hub_count=5, mode=tg.SAGE_MEAN)
+    g, m = tg.make_graph(w), tg.make_model(w, bias_scale=0.3)
+    stream = torch.cuda.Stream() if stream else None
+    r = torch.Generator("cuda").manual_seed(6)
+    x = torch.randn(g.V, 48, generator=r, device="cuda")
+    gamma, beta = 1 + 0.2 * torch.randn(96, generator=r, device="cuda"), 0.2 * torch.randn(96, generator=r, device="cuda")
+    h, out = torch.empty(g.V, 96, device="cuda"), torch.empty(g.V, 40, device="cuda")
+    off = torch.tensor([0, g.V // 3, g.V], device="cuda")      # (two graphs of a batch, for the norm)
+    ws = torch.empty(tb.norm_rows_workspace(g.V, 2, 96, 8), dtype=torch.uint8, device="cuda")
+    ctx = tb.Context(g.V, g.E, g.row_ptr, g.col_idx, g.in_degree, w.mode, w.dims, m.W_neigh, m.W_self, m.bias, m.act, w.chunk, w.pool_slots, w.hub_count, w.fanout, w.seed, 0, g.V)
+    torch.cuda.synchronize()
+    for l, (src, dst) in enumerate(((x, h), (h, out))):
+        ctx.layer_begin(l, stream)
+        ctx.layer_set_dense_output(dst, dst.shape[1])
+        for b in range(0, g.V, w.chunk):
+            ctx.push_chunk(b, min(b + w.chunk, g.V), src[b:b + w.chunk], stream)
+        assert ctx.layer_end()["completed"] == g.V
+        if l == 0:
+            tb.norm_rows(g.V, 2, off, h, 96, 96, 8, gamma, beta, EPS, tb.ACT_SILU, h, 96, workspace=ws, stream=stream)
+    torch.cuda.synchronize()
+
+    def layer(l, x):
+        agg = np.zeros_like(x)
+        for u in range(g.V):
+            np.add.at(agg, g.col_idx[g.row_ptr[u]:g.row_ptr[u + 1]], x[u])
+        agg /= np.maximum(g.in_degree, 1)[:, None]
+        y = agg @ m.W_neigh[l].astype(np.float64) + x @ m.W_self[l].astype(np.float64) + m.bias[l]
+        return np.maximum(y, 0) if m.act[l] else y
+    y, _, _ = norm(off.tolist(), torch.from_numpy(layer(0, x.double().cpu().numpy())).cuda(), 8, gamma, beta, EPS, tb.ACT_SILU)
+    assert float((h.double() - y).norm()) <= 1e-4 * float(y.norm())
+    want = layer(1, y.cpu().numpy())
+    assert np.linalg.norm(out.double().cpu().numpy() - want) <= 1e-4 * np.linalg.norm(want)

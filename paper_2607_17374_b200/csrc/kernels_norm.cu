@@ -6,7 +6,7 @@
 //   dx = rstd (gamma dz - mean_g(gamma dz) - xh mean_g(gamma dz xh))
 //
 // Bytes bound it: x in, y out (dx: x and dy in, dx out).  Statistics need all of a graph before its first row can be written.  A short graph
-// is the work of one block, which has its rows in registers or finds them in the caches when it writes.  The rows of a long graph are spread over
+// is the work of one block, which reads its rows twice, the second time from the caches where they are few.  The rows of a long graph are spread over
 // blocks of R rows (stats), their partial statistics joined in a fixed order (combine), and the rows are read again and written (apply).  How long
 // a graph is stands in device memory: the kernel for short graphs leaves a word that says whether there are others.
 //
@@ -14,8 +14,8 @@
 // deviations) and joined as (count, mean, sum of squared deviations): neither an offset nor a single large value eats the variance, as they would with sums of squares.
 // All in fp32, the parts of a long graph in fp64.
 //
-// 1 M x 256 fp32 in 3 graphs: forward 507 us (three passes over the matrix, 6.1 TB/s), backward 810 (five, 6.3 TB/s).  262 144 x 64 bf16 in 9 001 graphs: 41 us, for
-// which instructions count (some 20 an element), not the 10 us that its bytes take.
+// 1 M x 256 fp32 in 3 graphs: forward 506 us (three passes over the matrix, 6.1 TB/s), backward 808 (five, 6.3 TB/s).  262 144 x 64 bf16 in 9 001 graphs: 41 to 45 us replayed, 46
+// with inputs that are new each pass, for which instructions and latency count (22 M by warps, 1 220 a warp and graph, 0.63 a cycle and scheduler), not the 10 us that its bytes take.
 #include <algorithm>
 
 #include "rows.cuh"
@@ -43,8 +43,9 @@ struct NormArgs {
   int32_t* status;
 };
 
-// 1 / (1 + e^-z) by the hardware's exponential and reciprocal.  e^-z is off by about 1.5 |z| 2^-24 of itself, which moves z / (1 + e^-z) by
-// 1.5 z^2 s (1 - s) 2^-24 < 0.7 2^-24 at most; an overflow of e^-z gives 0.
+// 1 / (1 + e^-z) by the hardware's exponential and reciprocal.  By their documented bounds (2 + 1.173 |z| ulp and 2 ulp) z / (1 + e^-z) is off by at most
+// |z| s (1 - s) (2 + 1.173 |z|) 2^-23 < 2^-23 from the exponential, largest near |z| = 2, and 2.5 2^-23 of itself from the sum and the division.  Where e^-z is above
+// 2^126 the quotient is 0: below z = -87.3, where the value is above -1.2e-36.
 __device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
 template <int ACT>
 __device__ __forceinline__ float act_f(float z) {
@@ -96,7 +97,7 @@ template <int V> constexpr int grad_batch() { return V == 8 ? 2 : 4; }
 template <int V> constexpr int short_batch() { return V == 8 ? 2 : 4; }
 template <int V> constexpr int short_grad_batch() { return V == 8 ? 2 : 4; }
 // Vectors of a short graph of average length to a thread: 32 elements, over which what a graph costs each thread is spread (262 144 x 64 in 9 001 graphs,
-// bf16 / fp32, 32 elements 44 / 58 us, 16 .. / 67, 64 45 / ..).
+// bf16 / fp32, 32 elements 41 / 49 us, 16 47 / 54, 64 44 / 55; with the gradient 150 / 149, 145 / 147, 187 / 190).
 template <int V> constexpr int short_vectors() { return 32 / V; }
 
 struct Moments { float n, mean, m2; };

@@ -3,15 +3,23 @@
 //   out[r] = x[r] W[g] + bias[g],  grad_x[r] = grad_out[r] W[g]^T,  grad_W[g] = sum_r x[r]^T grad_out[r],  grad_bias[g] = sum_r grad_out[r]
 //
 // over the rows r in [offsets[g], offsets[g + 1]), offsets in device memory.  This file: arguments, and the kernels for few rows, which read
-// every weight once per row and add in fp32 FMAs (bytes and latency bound them: 64 rows of 64 -> 64 fp32 in 3 types 4.5 us, gradients 10; on the tensor cores 100 rows
-// take 8.6 and 17, a tile of 128 rows and its set-up); kernels_typed_tc.cu: the others.
+// every weight once per row and add in fp32 FMAs (bytes and latency bound them; measured at FEW_ROWS); kernels_typed_tc.cu: the others.
 #include <algorithm>
 
 #include "typed.cuh"
 
 namespace {
 
-// Rows up to which the kernels for few rows are taken.
+// Rows up to which the kernels for few rows are taken, whatever the widths.  Both sides at 64 rows of one type, us (these kernels / the tensor cores):
+//                   64 -> 64       256 -> 256     1 024 -> 1 024
+//   fp32  forward   2.9 / 7.7      4.2 / 16.9     23 / 44
+//         grad_x    2.7 / 7.6      3.9 / 15.7     21 / 40
+//         grad_W    7.9 / 7.4      8.3 / 8.9      17 / 9.2
+//   bf16  forward   3.0 / 4.3      4.3 / 6.7      18 / 11
+//         grad_x    2.8 / 4.2      3.4 / 6.3      17 / 9.7
+//         grad_W    18 / 5.1       19 / 6.8       31 / 6.9
+// They win at 8 to 32 rows too, but for 16-bit rows of 1 024 columns and for grad_W of types of more than some 16 rows (16 bits) or 32 (fp32), which a thread
+// walks one after another.
 constexpr int FEW_ROWS = 64;
 constexpr int FEW_THREADS = 256, COL_VECTORS = 8, K_LANES = FEW_THREADS / COL_VECTORS;
 

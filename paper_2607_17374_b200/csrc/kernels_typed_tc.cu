@@ -7,7 +7,8 @@
 // grad_W[g] and a block of columns, over one chunk of the type's rows; a type of several chunks leaves one partial product a chunk, which
 // typed_join_kernel adds up in their order).  Which units there are follows from the offsets in device memory: every CTA works it out for itself.
 // Roles:  warp 0       TMA: operands that stand in memory as the tensor core takes them
-//         warp 1       tcgen05.mma, accumulators in TMEM, two slots of 256 columns: the epilogue of a unit runs beside the products of the next
+//         warp 1       tcgen05.mma, accumulators in TMEM, two slots of 256 columns: the epilogue of a unit runs beside the products of the next.  (Where two sums
+//                      of more than 128 columns are kept, fp32 rows and 16-bit grad_W, there is one slot, and they take turns.)
 //         warps 2..9   epilogue, two to a quadrant of TMEM lanes: TMEM -> registers -> transposed through shared memory -> rows
 //         warps 10..17 loaders (LOADED): operands that have to be split, or whose rows TMA cannot address; without loaders, in GRAD_W, they add up the
 //                      columns of grad_out for the bias, which the loaders do on the way
@@ -18,9 +19,9 @@
 // Two accumulators: where hi hi is not finite the sum is what it says (an infinity times a mid or lo of zero would make it NaN).  hi may be larger than x, by 2^-8: where
 // products' magnitudes add up to more than (1 - 2^-7) times the largest fp32 value the sum may be infinite.  W is split by a kernel in front (it is read once per tile), rows by the loaders.
 //
-// What bounds it (1.2 M rows, 512 -> 256 bf16: 350 us, 5.3 TB/s of rows): the L2, which gives every 128 rows the whole of W's block again, 3 KB a row, 9.6 TB/s.  fp32
-// (400 000 rows, 256 -> 256): 294 us forward and 285 for grad_x, 196 of them the six products; the output of a block of 256 columns waits for its accumulators
-// and they for it.  grad_W 440 to 530: the loaders' split of both operands.
+// What bounds it (1.2 M rows, 512 -> 256 bf16: 359 us replayed on the same inputs, 433 with new ones each pass, 5.1 and 4.3 TB/s of rows): the L2, which gives every 128 rows
+// the whole of W's block again, 3 KB a row, 10 TB/s; DRAM at 60 %, the tensor core at 44 %.  fp32 (400 000 rows, 256 -> 256): 299 us forward and 288 for grad_x, 196 of them the six
+// products; the output of a block of 256 columns waits for its accumulators and they for it.  grad_W 468 to 514: the loaders' split of both operands.
 //
 // Every wait is bounded, as in the projection of the layers: a CTA that gives up records TAURUS_ERR_INTERNAL, waits (bounded) for its copies and
 // products in flight, frees its TMEM and returns.  Every TMA load is a plain load of the issuing CTA alone.

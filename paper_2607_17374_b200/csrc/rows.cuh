@@ -80,7 +80,7 @@ static inline bool rows_fit(int64_t n, int64_t ld, int size) { return n == 0 || 
 
 // The launches of a call: each but the first may come up while the one before it ends (early_start at the start of every kernel waits for what that
 // wrote).  Data of an earlier kernel of the call is not read through __restrict__ pointers: such loads may be moved ahead of the wait.  For the norm, most of whose
-// launches find nothing to do in a batch of short graphs: 262 144 x 64 bf16 in 9 001 graphs 43.5 -> 41 us.  The sort of the ids lost by it (161 -> 184 us for 500 000:
+// launches find nothing to do in a batch of short graphs: 262 144 x 64 bf16 in 9 001 graphs 43.1 -> 41.3 us.  The sort of the ids lost by it (161 -> 184 us for 500 000:
 // blocks that wait take the places of blocks that work), the products by type did not change.
 struct Launches {
   cudaStream_t st;

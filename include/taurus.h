@@ -473,7 +473,8 @@ int taurus_permute_rows(int64_t V, int32_t width, const float* in_rows, int64_t 
  * Where the argument checks need the device's memory contents (ids, offsets) the kernels check them: nothing outside the arrays is
  * read or written, and the first error is stored in *status (device int32, may be NULL; a TAURUS_ERR_* code, never cleared by the
  * library: a program clears it once and reads it when it likes).
- * The *_workspace functions return bytes (0: none needed) or a negative TAURUS_ERR_* code; workspaces are 256-byte aligned.
+ * The *_workspace functions return bytes (0: none needed) or a negative TAURUS_ERR_* code; workspaces are 256-byte aligned.  What is enough for n rows is
+ * for fewer, and for a norm of fewer graphs (the other arguments being the same).
  */
 enum { TAURUS_F32 = 0, TAURUS_BF16 = 1, TAURUS_F16 = 2 };
 enum { TAURUS_ACT_NONE = 0, TAURUS_ACT_RELU = 1, TAURUS_ACT_SILU = 2 };

@@ -68,6 +68,7 @@ int vector_of(int limit, int size, const void* p, int64_t ld, int width) {
 // 4 M two.  Up to SMALL items one block does it all.
 constexpr int SORT_THREADS = 256, SORT_WARPS = SORT_THREADS / 32, MAX_DIGIT = 11, MAX_BINS = 1 << MAX_DIGIT, TILE = 1024, MAX_ITEMS = 32 * TILE;
 constexpr int SMALL = 2048, SMALL_THREADS = 1024;
+constexpr int SORT_BLOCKS = 300;      // beyond which a block takes more items
 
 struct SortPlan { int passes, bits, items, blocks; };   // bits of a digit; items of a block
 SortPlan sort_plan(int64_t n, int64_t table_rows) {
@@ -77,7 +78,7 @@ SortPlan sort_plan(int64_t n, int64_t table_rows) {
   p.passes = (key + MAX_DIGIT - 1) / MAX_DIGIT;
   p.bits = (key + p.passes - 1) / p.passes;
   p.items = TILE;
-  while (p.items < MAX_ITEMS && n / p.items > 300) p.items *= 2;      // two blocks to an SM
+  while (p.items < MAX_ITEMS && n / p.items > SORT_BLOCKS) p.items *= 2;      // two blocks to an SM
   p.blocks = (int)((n + p.items - 1) / p.items);
   return p;
 }
@@ -484,16 +485,22 @@ embed_join_kernel(const GradArgs a, T* __restrict__ table) {
 }
 
 // Pieces: short ones give warps enough to fill the device a few times over, long ones keep the partial rows few.
+constexpr int GRAD_PIECES = 148 * 64;      // at least, before they get longer
 int grad_piece(int64_t n) {
   int piece = 32;
-  while (piece < 256 && n / (2 * piece) >= 148 * 64) piece *= 2;
+  while (piece < 256 && n / (2 * piece) >= GRAD_PIECES) piece *= 2;
   return piece;
 }
 
 struct GradSpace { size_t key[2], pos[2], hist, totals, open, open_long, head, tail, bytes; };
-GradSpace grad_space(int64_t n, int64_t table_rows, int32_t width) {
-  const size_t pieces = (size_t)((n + grad_piece(n) - 1) / grad_piece(n));
-  const SortPlan p = sort_plan(n, table_rows);
+// most: what no call with as many ids, or fewer, exceeds (where pieces and sort blocks get longer there are fewer of them).
+GradSpace grad_space(int64_t n, int64_t table_rows, int32_t width, bool most = false) {
+  size_t pieces = (size_t)((n + grad_piece(n) - 1) / grad_piece(n));
+  SortPlan p = sort_plan(n, table_rows);
+  if (most) {
+    pieces = std::max(pieces, (size_t)std::min<int64_t>((n + 31) / 32, 2 * GRAD_PIECES));
+    p.blocks = std::max(p.blocks, (int)std::min<int64_t>((n + TILE - 1) / TILE, SORT_BLOCKS + 1));
+  }
   GradSpace s;
   size_t at = 0;
   auto take = [&](size_t b) { const size_t o = at; at += (b + 255) / 256 * 256; return o; };
@@ -558,7 +565,7 @@ extern "C" int taurus_embed_rows(int64_t n, const int64_t* ids, const void* tabl
 extern "C" int64_t taurus_embed_grad_workspace(int64_t n, int64_t table_rows, int32_t width) {
   if (!table_shape_ok(n, table_rows, width, width, width)) return TAURUS_ERR_INVALID_ARG;
   if (width > TAURUS_MAX_ROW_WIDTH) return TAURUS_ERR_UNSUPPORTED;
-  return (int64_t)grad_space(n, table_rows, width).bytes;
+  return (int64_t)grad_space(n, table_rows, width, true).bytes;
 }
 
 extern "C" int taurus_embed_grad(int64_t n, const int64_t* ids, const void* grad_rows, int32_t grad_type, int64_t ld_grad, int32_t width, float scale,

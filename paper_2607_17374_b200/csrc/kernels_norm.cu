@@ -777,11 +777,13 @@ long long block_rows(int64_t n, int64_t graphs, int C) {
 }
 
 struct NormSpace { long long R, blocks; int short_blocks, row_grid; size_t flag, part, chan, sums, mean, rstd, bytes; };
-NormSpace norm_space(int64_t n, int64_t graphs, int C, int groups, bool grad) {
+// most: what no call with as many rows and graphs, or fewer, exceeds (the blocks of rows are longer where there are many graphs).
+NormSpace norm_space(int64_t n, int64_t graphs, int C, int groups, bool grad, bool most = false) {
   NormSpace s;
-  s.R = block_rows(n, graphs, C);
+  s.R = block_rows(n, most ? 1 : graphs, C);
   const bool long_ones = n > 2 * s.R;                            // else no graph can be long
   s.blocks = long_ones ? (n + s.R - 1) / s.R : 0;
+  if (most && long_ones) s.blocks = std::min<long long>(DEVICE_SMS * ROW_BLOCKS_PER_SM, (n + std::max(1, 8192 / C) - 1) / std::max(1, 8192 / C));
   s.row_grid = (int)std::min<long long>(s.blocks, DEVICE_SMS * ROW_GRID_PER_SM);
   s.short_blocks = (int)std::min<long long>(graphs, DEVICE_SMS * 16);      // (gradients: at most)
   size_t at = 0;
@@ -855,12 +857,12 @@ int short_threads(int64_t n, int64_t graphs, int vpr, int batch) {
 extern "C" int64_t taurus_norm_rows_workspace(int64_t n, int64_t graphs, int32_t width, int32_t groups) {
   if (!norm_shape_ok(n, graphs, width, groups)) return TAURUS_ERR_INVALID_ARG;
   if (width > MAX_C) return TAURUS_ERR_UNSUPPORTED;
-  return (int64_t)norm_space(n, graphs, width, groups, false).bytes;
+  return (int64_t)norm_space(n, graphs, width, groups, false, true).bytes;
 }
 extern "C" int64_t taurus_norm_rows_grad_workspace(int64_t n, int64_t graphs, int32_t width, int32_t groups) {
   if (!norm_shape_ok(n, graphs, width, groups)) return TAURUS_ERR_INVALID_ARG;
   if (width > MAX_C) return TAURUS_ERR_UNSUPPORTED;
-  return (int64_t)norm_space(n, graphs, width, groups, true).bytes;
+  return (int64_t)norm_space(n, graphs, width, groups, true, true).bytes;
 }
 
 extern "C" int taurus_norm_rows(int64_t n, int64_t graphs, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, int32_t width, int32_t groups,

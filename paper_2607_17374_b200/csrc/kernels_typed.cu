@@ -148,14 +148,14 @@ int vector_of(int size, const void* p, int64_t ld) {
 }
 
 // A call's workspace: W laid out anew (where it is: packs), partial results of grad_W, rows of grad_out and of x at other pitches.  The workspace functions
-// answer for weights at any address, a call asks for what it uses.
+// answer for weights at any address and for as many rows or fewer (most), a call asks for what it uses.
 struct Space {
   size_t part = 0, dy = 0, x = 0, bytes = 0;
-  Space(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type, bool packs, bool grad) {
+  Space(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type, bool packs, bool grad, bool most = false) {
     if (n <= FEW_ROWS) return;
     auto take = [&](size_t b) { const size_t o = bytes; bytes += (b + 255) / 256 * 256; return o; };
     if (packs) take(typed_tc_pack_bytes(types, d_in, d_out, type));
-    if (grad) { part = take(typed_tc_part_bytes(n, types, d_in, d_out, type)); dy = take(typed_tc_row_bytes(n, d_out, type)); }
+    if (grad) { part = take(typed_tc_part_bytes(n, types, d_in, d_out, type, most)); dy = take(typed_tc_row_bytes(n, d_out, type)); }
     x = take(typed_tc_row_bytes(n, d_in, type));
   }
   TypedSpaces at(void* workspace) const {
@@ -169,12 +169,12 @@ struct Space {
 extern "C" int64_t taurus_typed_project_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type) {
   if (!typed_shape_ok(n, types, d_in, d_out, type)) return TAURUS_ERR_INVALID_ARG;
   if (!typed_supported(types, d_in, d_out)) return TAURUS_ERR_UNSUPPORTED;
-  return (int64_t)Space(n, types, d_in, d_out, type, true, false).bytes;
+  return (int64_t)Space(n, types, d_in, d_out, type, true, false, true).bytes;
 }
 extern "C" int64_t taurus_typed_project_grad_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type) {
   if (!typed_shape_ok(n, types, d_in, d_out, type)) return TAURUS_ERR_INVALID_ARG;
   if (!typed_supported(types, d_in, d_out)) return TAURUS_ERR_UNSUPPORTED;
-  return (int64_t)Space(n, types, d_in, d_out, type, true, true).bytes;
+  return (int64_t)Space(n, types, d_in, d_out, type, true, true, true).bytes;
 }
 
 extern "C" int taurus_typed_project(int64_t n, int32_t types, const int64_t* offsets, const void* x, int64_t ld_x, int32_t type, const void* W,

@@ -1017,10 +1017,11 @@ int64_t row_pitch(int width) { return taurus_round_up(width, 8); }
 bool packs_rows(const void* p, int64_t ld, int width, int32_t type) { return typed_tc_row_bytes(1, width, type) > 0 && !tma_rows(p, ld); }
 // Rows of a chunk of grad_W: about two units to an SM, 1 024 rows at least, 2 048 at most.  fp32: 1 024 (2 700, as 400 000 rows in 5 types would have: 2.9e-6 of the result
 // off, where fp32 sums are 1.1e-6).
+constexpr int CHUNK_LEAST = 1024;
+long long weight_tiles(int d_in, int d_out) { return (long long)((d_in + BM - 1) / BM) * ((d_out + 255) / 256); }
 int rows_of_chunk(int64_t n, int d_in, int d_out, int32_t type) {
-  if (type == TAURUS_F32) return 1024;
-  const long long tiles = (long long)((d_in + BM - 1) / BM) * ((d_out + 255) / 256);
-  return (int)std::min<long long>(2048, std::max<long long>(1024, taurus_round_up((int)std::min<long long>(n * tiles / 296, 1 << 20), 64)));
+  if (type == TAURUS_F32) return CHUNK_LEAST;
+  return (int)std::min<long long>(2048, std::max<long long>(CHUNK_LEAST, taurus_round_up((int)std::min<long long>(n * weight_tiles(d_in, d_out) / (2 * 148), 1 << 20), 64)));
 }
 
 }  // namespace
@@ -1031,9 +1032,12 @@ size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type) { r
 // Room for rows at another pitch.
 size_t typed_tc_row_bytes(int64_t n, int width, int32_t type) { return type == TAURUS_F32 || width % 8 == 0 ? 0 : (size_t)n * (size_t)row_pitch(width) * 2; }
 // A type of more than one chunk has more than `chunk` rows and at most rows / chunk + 1 chunks.
-size_t typed_tc_part_bytes(int64_t n, int32_t types, int d_in, int d_out, int32_t type) {
-  const int chunk = rows_of_chunk(n, d_in, d_out, type);
-  return (size_t)(n / chunk + std::min<int64_t>(types, n / chunk)) * (size_t)(d_in + 1) * d_out * 4;
+// most: what no call with as many rows, or fewer, exceeds.  (Between the shortest and the longest chunk n / chunk is about two units to an SM, y / (y - 1) of it at most for
+// y = n tiles / 296 >= 1 024: less than one more.)
+size_t typed_tc_part_bytes(int64_t n, int32_t types, int d_in, int d_out, int32_t type, bool most) {
+  int64_t chunks = n / rows_of_chunk(n, d_in, d_out, type);
+  if (most) chunks = std::max(chunks, std::min<int64_t>(n / CHUNK_LEAST, 2 * 148 / weight_tiles(d_in, d_out) + 1));
+  return (size_t)(chunks + std::min<int64_t>(types, chunks)) * (size_t)(d_in + 1) * d_out * 4;
 }
 
 namespace {

@@ -86,7 +86,7 @@ struct TypedSpaces { void *W, *part, *dy, *x; };
 bool typed_tc_packs(const void* W, int32_t type, int d_out);
 size_t typed_tc_pack_bytes(int32_t types, int d_in, int d_out, int32_t type);
 size_t typed_tc_row_bytes(int64_t n, int width, int32_t type);
-size_t typed_tc_part_bytes(int64_t n, int32_t types, int d_in, int d_out, int32_t type);
+size_t typed_tc_part_bytes(int64_t n, int32_t types, int d_in, int d_out, int32_t type, bool most);
 // (arguments as checked by the entry points; TAURUS_ERR_CUDA with nothing enqueued where a tensor map cannot be made)
 int typed_tc_project(int64_t n, int32_t types, const long long* offsets, const void* x, int64_t ld_x, int32_t type, const void* W, const float* bias, int d_in, int d_out, void* out,
                      int32_t out_type, int64_t ld_out, const TypedSpaces& spaces, int32_t* status, int sms, cudaStream_t st);

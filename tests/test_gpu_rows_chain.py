@@ -283,3 +283,25 @@ def test_a_norm_between_two_layers(stream):
     assert float((h.double() - y).norm()) <= 1e-4 * float(y.norm())
     want = layer(1, y.cpu().numpy())
     assert np.linalg.norm(out.double().cpu().numpy() - want) <= 1e-4 * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("most,n", [(606_300, 606_207), (310_000, 308_223), (300_000, 150_000)])
+def test_a_workspace_asked_for_once(most, n):
+    """A workspace of the largest batch's size takes a smaller batch, whose pieces, chunks or blocks may be more than the largest one's."""
+    ids = torch.randint(-1, 900, (n,), device="cuda")
+    grad, table = torch.ones(n, 8, device="cuda"), torch.empty(900, 8, device="cuda")
+    tb.embed_grad(n, ids, grad, 8, 8, table, 900, 8, torch.full((tb.embed_grad_workspace(most, 900, 8),), 255, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(table[:, 3], torch.bincount(ids[ids >= 0], minlength=900).float())
+    x, W = torch.ones(n, 72, dtype=torch.bfloat16, device="cuda"), torch.ones(3, 72, 40, dtype=torch.bfloat16, device="cuda")
+    dy, dW, off = torch.ones(n, 40, dtype=torch.bfloat16, device="cuda"), torch.empty(3, 72, 40, device="cuda"), torch.tensor([0, 1000, 1000, n], device="cuda")
+    tb.typed_project_grad(n, 3, off, x, 72, W, dy, 40, 72, 40, grad_W=dW,
+                          workspace=torch.full((tb.typed_project_grad_workspace(most, 3, 72, 40, x),), 255, dtype=torch.uint8, device="cuda"))
+    assert dW[:, 5, 7].tolist() == [1000.0, 0.0, n - 1000.0]
+    graphs = n // 3
+    off = torch.cat([torch.arange(graphs, device="cuda") * 3, torch.tensor([n], device="cuda")])
+    y, g, mean, rstd = torch.randn(n, 16, device="cuda"), torch.empty(n, 16, device="cuda"), torch.empty(graphs, 1, device="cuda"), torch.empty(graphs, 1, device="cuda")
+    ws = torch.full((max(tb.norm_rows_workspace(most, graphs, 16, 1), tb.norm_rows_grad_workspace(most, graphs, 16, 1)),), 255, dtype=torch.uint8, device="cuda")
+    tb.norm_rows(n, graphs, off, y, 16, 16, 1, None, None, EPS, 0, g, 16, mean, rstd, ws)
+    assert float(g[:3].mean().abs()) < 1e-6
+    tb.norm_rows_grad(n, graphs, off, y, 16, 16, 1, None, None, 0, mean, rstd, y, 16, g, 16, workspace=ws)
+    assert torch.isfinite(g).all()

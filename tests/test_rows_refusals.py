@@ -136,3 +136,25 @@ def test_a_type_that_is_said_and_is_not_the_tensors():
                  lambda: tb.norm_rows_grad(4, 1, off, x, 8, 8, 2, v, v, 1, one, one, P, 8, P, 8, workspace=ws, type=tb.F32)):
         with pytest.raises(TypeError):
             call()
+
+
+def test_a_workspace_for_more_rows_does_for_fewer(lib):
+    """A program that asks once, for its largest batch, has enough for the others."""
+    import random
+    rng = random.Random(4)
+    sizes = sorted({1, 64, 65, 606_207, 606_208, 1_212_415, 1_212_416, 2_424_831, 2_424_832, 2_424_833, 308_223, 308_224, 151_552, 151_553, 303_104, 303_105, (1 << 31) - 1}
+                   | {int(2 ** rng.uniform(0, 31)) - 1 for _ in range(600)} | {k * 1184 + d for k in (2, 3, 4, 8, 9, 100) for d in (-1, 0, 1)})
+    cases = [(lib.taurus_embed_grad_workspace, a) for a in ((1003, 47), (400_000, 128), (1 << 22, 1024), (5, 1))]
+    cases += [(f, a) for f in (lib.taurus_typed_project_workspace, lib.taurus_typed_project_grad_workspace) for a in
+              ((1, 64, 64, 0), (16, 512, 256, 1), (200, 128, 128, 2), (1000, 1024, 1024, 1), (7, 37, 130, 1), (7, 37, 130, 0), (3, 300, 1000, 2))]
+    for f, rest in cases:
+        got = [f(n, *rest) for n in sizes]
+        assert all(g >= 0 for g in got) and got == sorted(got), (f.__name__, rest)
+    for f in (lib.taurus_norm_rows_workspace, lib.taurus_norm_rows_grad_workspace):
+        for width, groups in ((64, 8), (1024, 1024), (1, 1), (257, 1), (1024, 32)):
+            for graphs in (1, 3, 1183, 1184, 9001, 100_000):
+                got = [f(n, graphs, width, groups) for n in sizes]
+                assert all(g >= 0 for g in got) and got == sorted(got), (f.__name__, width, groups, graphs)
+            for n in (5000, 262_144, 3_000_000):      # and one for more graphs does for fewer
+                got = [f(n, graphs, width, groups) for graphs in (1, 2, 100, 1183, 1184, 1185, 2368, 2369, 5000, 100_000, 1 << 30)]
+                assert got == sorted(got), (f.__name__, width, groups, n)

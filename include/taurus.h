@@ -458,7 +458,9 @@ int taurus_permute_rows(int64_t V, int32_t width, const float* in_rows, int64_t 
  * Operators on typed rows: what makes the rows that a layer takes and what stands between two layers (no counterpart in
  * the paper, whose vertices all have features of one kind).  taurus_embed_rows looks rows up in a learned table,
  * taurus_typed_project gives each vertex type a weight matrix of its own, taurus_norm_rows is a norm with an activation over
- * a batch of graphs; each has its gradient, so that tables, weights and norms can be trained.
+ * a batch of graphs.  Each has its gradient, for a program that trains tables, weights and norms with a loss of its own on what they
+ * make: the layers have no backward call.  A norm between two layers needs the rows of a graph in one device matrix, such as a dense output; layers
+ * chained through sorted runs have none.
  *
  * Rules common to them.  They need no context.  Every pointer is DEVICE memory of the current device, aligned to its element
  * (anything else: TAURUS_ERR_INVALID_ARG); a pitch ld is in elements, at least the row's width; rows need no alignment, but rows
@@ -502,9 +504,9 @@ int taurus_embed_grad(int64_t n, const int64_t* ids, const void* grad_rows, int3
  * Projection by vertex type: out[r] = x[r] W[g] + bias[g] for the rows r in [offsets[g], offsets[g + 1]) of type g, g in
  * [0, types), types in 1 .. TAURUS_MAX_TYPES.  offsets: [types + 1], non-decreasing, inside [0, n]; a type may have no rows; rows of out in
  * front of offsets[0] or behind offsets[types] are left as they are.  Offsets that break this give TAURUS_ERR_INVALID_ARG in *status (the
- * rows written are then unspecified).  W: [types x d_in x d_out] row-major without gaps, of x's type; bias: [types x d_out]
+ * rows written are then unspecified); with n = 0 they are not looked at.  W: [types x d_in x d_out] row-major without gaps, of x's type; bias: [types x d_out]
  * fp32 or NULL; out_type: x's type or TAURUS_F32.  With TAURUS_F32 operands a product is off by less than 2^-24 of itself, as a rounded fp32 multiplication is, and the sums
- * are fp32; an operand below 2^-110 in magnitude may be off by 2^-133, and a sum whose products' magnitudes add up to more than (1 - 2^-7) times the largest
+ * are fp32 (for more than 64 rows the tensor core's, which cut off instead of rounding); an operand below 2^-110 in magnitude may be off by 2^-133, and a sum whose products' magnitudes add up to more than (1 - 2^-7) times the largest
  * fp32 value may be infinite.
  */
 int64_t taurus_typed_project_workspace(int64_t n, int32_t types, int32_t d_in, int32_t d_out, int32_t type);

@@ -482,6 +482,8 @@ enum { TAURUS_F32 = 0, TAURUS_BF16 = 1, TAURUS_F16 = 2 };
 enum { TAURUS_ACT_NONE = 0, TAURUS_ACT_RELU = 1, TAURUS_ACT_SILU = 2 };
 #define TAURUS_MAX_ROW_WIDTH 1024
 #define TAURUS_MAX_TYPES 1024
+#define TAURUS_MAX_CLASSES (1 << 20)
+#define TAURUS_MAX_TOP 16
 
 /*
  * out_rows[i] = scale * table[ids[i]] for i in [0, n); id -1 stands for "no entry" and gives a row of zeros.  Any other id
@@ -547,6 +549,31 @@ int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* offsets, con
                           int32_t groups, const float* gamma, const float* beta, int32_t act, const float* mean, const float* rstd,
                           const void* grad_out, int64_t ld_grad, void* grad_x, int64_t ld_grad_x, float* grad_gamma, float* grad_beta,
                           void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+
+/*
+ * Log probabilities of given classes from rows of logits ([n x classes], classes in 1 .. TAURUS_MAX_CLASSES: these rows may be wider than TAURUS_MAX_ROW_WIDTH), with the
+ * entropy and the top alternatives.  With m the largest logit of a row, l = log sum exp(x - m) and log p_j = (x_j - m) - l:
+ *   logprob[i] = log p of class labels[i]; label -1 stands for "none" and gives 0, any other label outside [0, classes) too, with TAURUS_ERR_INVALID_ARG in *status
+ *   entropy[i] = - sum p_j log p_j
+ *   stats[i]   = (m, l), fp32 pairs, 8-byte aligned: m + l is the logarithm of the sum of exponentials; taurus_class_logprob_grad takes them
+ *   top_logprob[i * k + r], top_class[i * k + r] = the r-th largest log p and its class, r in [0, k), k in 0 .. TAURUS_MAX_TOP; of equal logits the lowest class comes first
+ * Each of the outputs may be NULL (logprob needs labels; with k > 0 one of the two tops at least is there).  A logit of -inf masks its class: its probability is 0, it is not among the top, whose
+ * places behind the last class hold -inf and -1.  A row with no other logits has l = 0, entropy 0 and log probabilities of -inf.  A row that holds a NaN or +inf
+ * has NaN in every output but the classes, which are in the order of the values that are numbers.
+ * taurus_class_logprob_train also forms the gradient of the logits, for weights of the rows that are known ahead, in one pass where the rows are short:
+ *   grad_logits[i][j] = grad_logprob[i] ([j = label] - p_j) - grad_entropy[i] p_j (log p_j + entropy[i])         (logits' type; 0 for masked classes)
+ * (either weight may be NULL: zeros; a row without a label takes no part of grad_logprob).  taurus_class_logprob_grad forms it from stats, and entropy where there is a
+ * grad_entropy, as an earlier call left them.  grad_logits may be the logits themselves with the same pitch.  The workspace of taurus_class_logprob_train is
+ * that of taurus_class_logprob with k = 0.
+ */
+int64_t taurus_class_logprob_workspace(int64_t n, int32_t classes, int32_t k);
+int taurus_class_logprob(int64_t n, int32_t classes, const void* logits, int64_t ld, int32_t type, const int64_t* labels, float* logprob, float* entropy, float* stats,
+                         int32_t k, float* top_logprob, int64_t* top_class, void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+int taurus_class_logprob_train(int64_t n, int32_t classes, const void* logits, int64_t ld, int32_t type, const int64_t* labels, const float* grad_logprob,
+                               const float* grad_entropy, float* logprob, float* entropy, float* stats, void* grad_logits, int64_t ld_grad, void* workspace,
+                               int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+int taurus_class_logprob_grad(int64_t n, int32_t classes, const void* logits, int64_t ld, int32_t type, const int64_t* labels, const float* stats, const float* entropy,
+                              const float* grad_logprob, const float* grad_entropy, void* grad_logits, int64_t ld_grad, int32_t* status, void* cuda_stream);
 
 /* Which order layer `layer` runs in: *out_aggregate_first = 1 when it aggregates (scaled) input rows and applies the
  * weights to the finished rows (see TAURUS_FLAG_PROJECT_FIRST), 0 when it projects every chunk first;

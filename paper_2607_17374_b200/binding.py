@@ -21,6 +21,7 @@ RUNS_HOST, RUNS_DEVICE = 0, 1
 F32, BF16, F16 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 MAX_ROW_WIDTH, MAX_TYPES = 1024, 1024
+MAX_CLASSES, MAX_TOP = 1 << 20, 16
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _lib = None
@@ -96,7 +97,8 @@ EXPORTS = [
     "taurus_get_sample_digest", "taurus_gat_project_chunk_from_runs", "taurus_relabel_csr", "taurus_permute_rows",
     "taurus_embed_rows", "taurus_embed_grad", "taurus_embed_grad_workspace", "taurus_typed_project", "taurus_typed_project_workspace",
     "taurus_typed_project_grad", "taurus_typed_project_grad_workspace", "taurus_norm_rows", "taurus_norm_rows_workspace",
-    "taurus_norm_rows_grad", "taurus_norm_rows_grad_workspace",
+    "taurus_norm_rows_grad", "taurus_norm_rows_grad_workspace", "taurus_class_logprob", "taurus_class_logprob_workspace", "taurus_class_logprob_train",
+    "taurus_class_logprob_grad",
 ]
 NOALLOC_MAX_VERTICES = 4 * 1024 * 1024
 
@@ -155,7 +157,11 @@ def load_library():
     lib.taurus_embed_grad_workspace.argtypes = [i64, i64, i32]
     lib.taurus_typed_project_workspace.argtypes = lib.taurus_typed_project_grad_workspace.argtypes = [i64, i32, i32, i32, i32]
     lib.taurus_norm_rows_workspace.argtypes = lib.taurus_norm_rows_grad_workspace.argtypes = [i64, i64, i32, i32]
-    for name in ("embed_grad", "typed_project", "typed_project_grad", "norm_rows", "norm_rows_grad"):
+    lib.taurus_class_logprob_workspace.argtypes = [i64, i32, i32]
+    lib.taurus_class_logprob.argtypes = [i64, i32, vp, i64, i32, vp, vp, vp, vp, i32, vp, vp, vp, i64, vp, vp]
+    lib.taurus_class_logprob_train.argtypes = [i64, i32, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp]
+    lib.taurus_class_logprob_grad.argtypes = [i64, i32, vp, i64, i32, vp, vp, vp, vp, vp, vp, i64, vp, vp]
+    for name in ("class_logprob", "embed_grad", "typed_project", "typed_project_grad", "norm_rows", "norm_rows_grad"):
         getattr(lib, "taurus_%s_workspace" % name).restype = i64
     lib.taurus_get_layer_plan.argtypes = [vp, ctypes.c_int32, vp, vp]
     lib.taurus_launch_count.argtypes = [vp]
@@ -400,6 +406,43 @@ def norm_rows_grad(n: int, graphs: int, offsets, x, ld_x: int, width: int, group
         n, graphs, _array(offsets, "int64", graphs + 1), _rows(x, n, width, ld_x), ld_x, t, width, groups, _array(gamma, "float32", width), _array(beta, "float32", width), act, _array(mean, "float32", graphs * groups),
         _array(rstd, "float32", graphs * groups), _rows(grad_out, n, width, ld_grad), ld_grad, _rows(grad_x, n, width, ld_grad_x), ld_grad_x, _array(grad_gamma, "float32", width), _array(grad_beta, "float32", width),
         *_space(workspace), _array(status, "int32", 1), _stream(stream)), "taurus_norm_rows_grad")
+
+
+def class_logprob_workspace(n: int, classes: int, k: int = 0) -> int:
+    """Bytes of class_logprob's workspace (k = 0: of class_logprob_train's)."""
+    return _checked(load_library().taurus_class_logprob_workspace(n, classes, k), "taurus_class_logprob_workspace")
+
+
+def class_logprob(n: int, classes: int, logits, ld: int, labels=None, logprob=None, entropy=None, stats=None, k: int = 0, top_logprob=None, top_class=None, workspace=None,
+                  status=None, stream=None, type=None):
+    """taurus_class_logprob: log probabilities of the labels' classes, entropy, (maximum, log of the sum) and the k top alternatives of each row of logits."""
+    _checked(load_library().taurus_class_logprob(
+        n, classes, _rows(logits, n, classes, ld), ld, _type_of(logits, type), _array(labels, "int64", n), _array(logprob, "float32", n), _array(entropy, "float32", n),
+        _array(stats, "float32", 2 * n), k, _array(top_logprob, "float32", n * k), _array(top_class, "int64", n * k), *_space(workspace), _array(status, "int32", 1), _stream(stream)),
+        "taurus_class_logprob")
+
+
+def class_logprob_train(n: int, classes: int, logits, ld: int, labels, grad_logprob, grad_entropy, logprob, entropy, stats, grad_logits, ld_grad: int, workspace=None, status=None,
+                        stream=None, type=None):
+    """taurus_class_logprob_train: class_logprob with the gradient of the logits, for weights of the rows that are known ahead."""
+    t = _type_of(logits, type)
+    if hasattr(grad_logits, "dtype") and _row_type(grad_logits) != t:
+        raise TypeError("logits and grad_logits are of one type")
+    _checked(load_library().taurus_class_logprob_train(
+        n, classes, _rows(logits, n, classes, ld), ld, t, _array(labels, "int64", n), _array(grad_logprob, "float32", n), _array(grad_entropy, "float32", n),
+        _array(logprob, "float32", n), _array(entropy, "float32", n), _array(stats, "float32", 2 * n), _rows(grad_logits, n, classes, ld_grad), ld_grad, *_space(workspace),
+        _array(status, "int32", 1), _stream(stream)), "taurus_class_logprob_train")
+
+
+def class_logprob_grad(n: int, classes: int, logits, ld: int, labels, stats, entropy, grad_logprob, grad_entropy, grad_logits, ld_grad: int, status=None, stream=None, type=None):
+    """taurus_class_logprob_grad: gradient of the logits from what class_logprob left in stats and entropy."""
+    t = _type_of(logits, type)
+    if hasattr(grad_logits, "dtype") and _row_type(grad_logits) != t:
+        raise TypeError("logits and grad_logits are of one type")
+    _checked(load_library().taurus_class_logprob_grad(
+        n, classes, _rows(logits, n, classes, ld), ld, t, _array(labels, "int64", n), _array(stats, "float32", 2 * n), _array(entropy, "float32", n),
+        _array(grad_logprob, "float32", n), _array(grad_entropy, "float32", n), _rows(grad_logits, n, classes, ld_grad), ld_grad, _array(status, "int32", 1), _stream(stream)),
+        "taurus_class_logprob_grad")
 
 
 class Runs:

@@ -479,11 +479,14 @@ int taurus_permute_rows(int64_t V, int32_t width, const float* in_rows, int64_t 
  * for fewer, and for a norm of fewer graphs (the other arguments being the same).
  */
 enum { TAURUS_F32 = 0, TAURUS_BF16 = 1, TAURUS_F16 = 2 };
+enum { TAURUS_E4M3 = 3 };                                  /* states of taurus_adamw_step only */
+enum { TAURUS_NORM_LAYER = 0, TAURUS_NORM_RMS = 1 };       /* norms of taurus_residual_norm */
 enum { TAURUS_ACT_NONE = 0, TAURUS_ACT_RELU = 1, TAURUS_ACT_SILU = 2 };
 #define TAURUS_MAX_ROW_WIDTH 1024
 #define TAURUS_MAX_TYPES 1024
 #define TAURUS_MAX_CLASSES (1 << 20)
 #define TAURUS_MAX_TOP 16
+#define TAURUS_STATE_BLOCK 256
 
 /*
  * out_rows[i] = scale * table[ids[i]] for i in [0, n); id -1 stands for "no entry" and gives a row of zeros.  Any other id
@@ -574,6 +577,68 @@ int taurus_class_logprob_train(int64_t n, int32_t classes, const void* logits, i
                                int64_t workspace_bytes, int32_t* status, void* cuda_stream);
 int taurus_class_logprob_grad(int64_t n, int32_t classes, const void* logits, int64_t ld, int32_t type, const int64_t* labels, const float* stats, const float* entropy,
                               const float* grad_logprob, const float* grad_entropy, void* grad_logits, int64_t ld_grad, int32_t* status, void* cuda_stream);
+
+/*
+ * The norms before and after a block of a network, with its gate and its residual scale, by row (taurus_norm_rows is over the rows of a graph):
+ *     u = post ? N(block) post_gamma : block,      out_res = res + alpha gate[g] u,      out = N(out_res) gamma + beta
+ * N is (x - mean) / sqrt(var + eps) over a row's channels (TAURUS_NORM_LAYER) or x / sqrt(mean(x^2) + eps) (TAURUS_NORM_RMS); out is formed from out_res before that is
+ * rounded.  res and out_res are of res_type (`type` or TAURUS_F32), block and out of `type`.  gate: [groups x width] fp32, a row for each group (a vertex type, or a
+ * graph with a condition of its own); group g owns rows [offsets[g], offsets[g + 1]), offsets as in taurus_typed_project (rows outside are left as they are), or NULL for one
+ * group of all rows (groups = 1).  gate NULL: ones, groups 0, offsets NULL.  post_gamma (with post = 1 only), gamma, beta: [width] fp32 or NULL (ones, ones, zeros).  block NULL:
+ * the norm alone, out = N(res) gamma + beta, with post 0 and gate, out_res NULL.  stats: [n x 4] fp32, 16-byte aligned, mean and 1 / sqrt(...) of the first norm and of
+ * the second, NULL unless the gradient will be taken.  out_res may be res, and out may be block, with the same pitch.  groups: at most 2^30.
+ */
+int taurus_residual_norm(int64_t n, int32_t width, const void* res, int64_t ld_res, int32_t res_type, const void* block, int64_t ld_block, int32_t type, int32_t kind,
+                         int32_t post, const float* post_gamma, int32_t groups, const int64_t* offsets, const float* gate, float alpha, const float* gamma,
+                         const float* beta, float eps, void* out_res, int64_t ld_out_res, void* out, int64_t ld_out, float* stats, int32_t* status, void* cuda_stream);
+/*
+ * Gradients of taurus_residual_norm from grad_out_res (res_type) and grad_out (`type`), one of which may be NULL (zeros), with res and block as the forward call had them and
+ * stats as it left them.  grad_block may be NULL (and is, where block is); grad_post_gamma, grad_gamma, grad_beta: [width], grad_gate: [groups x width] (zeros for a group without
+ * rows), fp32, each may be NULL.  grad_res may be res or grad_out_res, grad_block may be block or grad_out, with the same pitch.  Of a layer norm of two channels,
+ * and an RMS norm of one, the gradient is the difference of two equal numbers but for eps, and is rounding for the most part.
+ */
+int64_t taurus_residual_norm_grad_workspace(int64_t n, int32_t width, int32_t groups);
+int taurus_residual_norm_grad(int64_t n, int32_t width, const void* res, int64_t ld_res, int32_t res_type, const void* block, int64_t ld_block, int32_t type, int32_t kind,
+                              int32_t post, const float* post_gamma, int32_t groups, const int64_t* offsets, const float* gate, float alpha, const float* gamma,
+                              const float* stats, const void* grad_out_res, int64_t ld_grad_out_res, const void* grad_out, int64_t ld_grad_out, void* grad_res,
+                              int64_t ld_grad_res, void* grad_block, int64_t ld_grad_block, float* grad_post_gamma, float* grad_gate, float* grad_gamma, float* grad_beta,
+                              void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream);
+
+/*
+ * AdamW over many tensors at once.  With g = *grad_scale grad, t = *step:
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *     param = param - lr weight_decay param - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * taurus_adamw_create checks a list of tensors once and keeps it in device memory (it allocates and blocks; not while a stream is being captured); taurus_adamw_step does one step for all of
+ * them: one launch for those with states in 32 bits and one for those with states in 8, asynchronous, capturable.  The arrays stay the caller's and where they are until
+ * taurus_adamw_destroy (which waits for the device); a graph that holds a step is not replayed after it.  What is written (param, m, v, scales, master) shares no byte
+ * with any other array of the list; gradients may share with each other.  Arrays need no alignment beyond their element's; at multiples of 16 bytes they are the fast ones.
+ *   param, grad: `count` elements of param_type and grad_type (TAURUS_F32, TAURUS_BF16, TAURUS_F16); a tensor with count 0, or without a gradient (NULL), is left alone
+ *   master:      NULL, or the parameters in fp32 beside param of 16 bits: the step is made on master, and param receives it rounded
+ *   state_type:  TAURUS_F32: m and v are fp32, m_scale and v_scale NULL.  TAURUS_E4M3: m and sqrt(v) are e4m3 codes, m_scale and v_scale hold a power of two for each block of
+ *                TAURUS_STATE_BLOCK elements (the last one may be short); codes and scales of zeros begin.  Written, a block's scale puts its largest value into [2^7, 2^8); values
+ *                are rounded up with the probability of what is cut off, by a hash of (seed, step, the tensor's place in the list, element), so that the same call gives the same bits;
+ *                an sqrt(v) that is not 0 is not rounded to 0.  The step itself is made from m and v before they are rounded.  Values that are not finite become NaN.
+ * step: the number of this step, from 1 on; lr: learning rate; grad_scale: NULL for 1 (device memory all three, so that a captured step can be replayed with others).  A *step below 1 changes
+ * nothing and gives TAURUS_ERR_INVALID_ARG in *status; a *grad_scale that is not finite (gradients that overflowed) changes nothing.  beta1, beta2 in [0, 1), eps > 0 (as fp32).
+ * The step is made on the device that was current at creation, which has to be current.  Steps of one list do not run at the same time.
+ */
+typedef struct taurus_adamw taurus_adamw;
+typedef struct {
+  void* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  float* master;
+  int64_t count;
+  float weight_decay;
+  int32_t param_type, grad_type, state_type;
+} taurus_adamw_tensor;
+int taurus_adamw_create(taurus_adamw** out, const taurus_adamw_tensor* tensors, int64_t count);
+int taurus_adamw_step(taurus_adamw* adamw, const int64_t* step, const float* lr, double beta1, double beta2, double eps, const float* grad_scale, uint64_t seed,
+                      int32_t* status, void* cuda_stream);
+void taurus_adamw_destroy(taurus_adamw* adamw);
 
 /* Which order layer `layer` runs in: *out_aggregate_first = 1 when it aggregates (scaled) input rows and applies the
  * weights to the finished rows (see TAURUS_FLAG_PROJECT_FIRST), 0 when it projects every chunk first;

@@ -9,6 +9,7 @@ from .binding import (  # noqa: F401
     embed_rows, embed_grad, embed_grad_workspace, typed_project, typed_project_workspace, typed_project_grad, typed_project_grad_workspace,
     norm_rows, norm_rows_workspace, norm_rows_grad, norm_rows_grad_workspace,
     class_logprob, class_logprob_workspace, class_logprob_train, class_logprob_grad,
+    residual_norm, residual_norm_grad, residual_norm_grad_workspace, AdamW, E4M3, NORM_LAYER, NORM_RMS, STATE_BLOCK,
     F32, BF16, F16, ACT_NONE, ACT_RELU, ACT_SILU, MAX_ROW_WIDTH, MAX_TYPES, MAX_CLASSES, MAX_TOP,
     SAGE_MEAN, GCN_SYM, GIN_SUM, GAT, GEMM_FP32, GEMM_BF16, FLAG_SIMT_GEMM, FLAG_NO_GROUPING, FLAG_PROJECT_FIRST, FLAG_PUSH_FORM, EVICT_FEWEST_PENDING, EVICT_FIFO, EVICT_LRU, EVICT_RANDOM, CHUNK_LOG_COLUMNS, ERROR_CODES,
 )

@@ -18,10 +18,12 @@ ERROR_CODES = {
     "CUDA": -6, "INTERNAL": -7, "NOMEM": -8, "UNSUPPORTED": -9, "RUN_STORE_FULL": -10, "RUNS_INCOMPLETE": -11,
 }
 RUNS_HOST, RUNS_DEVICE = 0, 1
-F32, BF16, F16 = 0, 1, 2
+F32, BF16, F16, E4M3 = 0, 1, 2, 3
+NORM_LAYER, NORM_RMS = 0, 1
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 MAX_ROW_WIDTH, MAX_TYPES = 1024, 1024
 MAX_CLASSES, MAX_TOP = 1 << 20, 16
+STATE_BLOCK = 256
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _lib = None
@@ -63,6 +65,12 @@ class _Run(ctypes.Structure):
                 ("evict_policy", ctypes.c_int32)]
 
 
+class _AdamWTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("master", ctypes.c_void_p), ("count", ctypes.c_int64), ("weight_decay", ctypes.c_float),
+                ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("state_type", ctypes.c_int32)]
+
+
 class Stats(ctypes.Structure):
     _fields_ = [("evictions", ctypes.c_int64), ("reloads", ctypes.c_int64), ("max_reload_count", ctypes.c_int64),
                 ("reload_histogram", ctypes.c_int64 * 17), ("peak_occupancy", ctypes.c_int64),
@@ -98,7 +106,8 @@ EXPORTS = [
     "taurus_embed_rows", "taurus_embed_grad", "taurus_embed_grad_workspace", "taurus_typed_project", "taurus_typed_project_workspace",
     "taurus_typed_project_grad", "taurus_typed_project_grad_workspace", "taurus_norm_rows", "taurus_norm_rows_workspace",
     "taurus_norm_rows_grad", "taurus_norm_rows_grad_workspace", "taurus_class_logprob", "taurus_class_logprob_workspace", "taurus_class_logprob_train",
-    "taurus_class_logprob_grad",
+    "taurus_class_logprob_grad", "taurus_residual_norm", "taurus_residual_norm_grad", "taurus_residual_norm_grad_workspace",
+    "taurus_adamw_create", "taurus_adamw_step", "taurus_adamw_destroy",
 ]
 NOALLOC_MAX_VERTICES = 4 * 1024 * 1024
 
@@ -161,6 +170,15 @@ def load_library():
     lib.taurus_class_logprob.argtypes = [i64, i32, vp, i64, i32, vp, vp, vp, vp, i32, vp, vp, vp, i64, vp, vp]
     lib.taurus_class_logprob_train.argtypes = [i64, i32, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp]
     lib.taurus_class_logprob_grad.argtypes = [i64, i32, vp, i64, i32, vp, vp, vp, vp, vp, vp, i64, vp, vp]
+    lib.taurus_residual_norm.argtypes = [i64, i32, vp, i64, i32, vp, i64, i32, i32, i32, vp, i32, vp, vp, f32, vp, vp, f32, vp, i64, vp, i64, vp, vp, vp]
+    lib.taurus_residual_norm_grad.argtypes = [i64, i32, vp, i64, i32, vp, i64, i32, i32, i32, vp, i32, vp, vp, f32, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp,
+                                              vp, i64, vp, vp]
+    lib.taurus_residual_norm_grad_workspace.argtypes = [i64, i32, i32]
+    lib.taurus_residual_norm_grad_workspace.restype = i64
+    lib.taurus_adamw_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(_AdamWTensor), i64]
+    lib.taurus_adamw_step.argtypes = [vp, vp, vp, ctypes.c_double, ctypes.c_double, ctypes.c_double, vp, ctypes.c_uint64, vp, vp]
+    lib.taurus_adamw_destroy.argtypes = [vp]
+    lib.taurus_adamw_destroy.restype = None
     for name in ("class_logprob", "embed_grad", "typed_project", "typed_project_grad", "norm_rows", "norm_rows_grad"):
         getattr(lib, "taurus_%s_workspace" % name).restype = i64
     lib.taurus_get_layer_plan.argtypes = [vp, ctypes.c_int32, vp, vp]
@@ -443,6 +461,94 @@ def class_logprob_grad(n: int, classes: int, logits, ld: int, labels, stats, ent
         n, classes, _rows(logits, n, classes, ld), ld, t, _array(labels, "int64", n), _array(stats, "float32", 2 * n), _array(entropy, "float32", n),
         _array(grad_logprob, "float32", n), _array(grad_entropy, "float32", n), _rows(grad_logits, n, classes, ld_grad), ld_grad, _array(status, "int32", 1), _stream(stream)),
         "taurus_class_logprob_grad")
+
+
+def residual_norm(n: int, width: int, res, ld_res: int, block, ld_block: int, kind: int, post, post_gamma, groups: int, offsets, gate, alpha: float, gamma, beta, eps: float,
+                  out_res, ld_out_res: int, out, ld_out: int, stats=None, status=None, stream=None, type=None, res_type=None):
+    """taurus_residual_norm: out_res = res + alpha gate[g] u, u = post ? norm(block) post_gamma : block; out = norm(out_res) gamma + beta (NORM_LAYER or NORM_RMS, by row)."""
+    t, r = _type_of(out, type), _type_of(res, res_type)
+    if hasattr(block, "dtype") and _row_type(block) != t:
+        raise TypeError("block and out are of one type")
+    if hasattr(out_res, "dtype") and _row_type(out_res) != r:
+        raise TypeError("res and out_res are of one type")
+    _checked(load_library().taurus_residual_norm(
+        n, width, _rows(res, n, width, ld_res), ld_res, r, _rows(block, n, width, ld_block), ld_block, t, kind, int(post), _array(post_gamma, "float32", width), groups,
+        _array(offsets, "int64", groups + 1), _array(gate, "float32", groups * width), alpha, _array(gamma, "float32", width), _array(beta, "float32", width), eps,
+        _rows(out_res, n, width, ld_out_res), ld_out_res, _rows(out, n, width, ld_out), ld_out, _array(stats, "float32", 4 * n), _array(status, "int32", 1), _stream(stream)),
+        "taurus_residual_norm")
+
+
+def residual_norm_grad_workspace(n: int, width: int, groups: int) -> int:
+    """Bytes of residual_norm_grad's workspace."""
+    return _checked(load_library().taurus_residual_norm_grad_workspace(n, width, groups), "taurus_residual_norm_grad_workspace")
+
+
+def residual_norm_grad(n: int, width: int, res, ld_res: int, block, ld_block: int, kind: int, post, post_gamma, groups: int, offsets, gate, alpha: float, gamma, stats, grad_out_res,
+                       ld_grad_out_res: int, grad_out, ld_grad_out: int, grad_res, ld_grad_res: int, grad_block=None, ld_grad_block: int = 0, grad_post_gamma=None, grad_gate=None,
+                       grad_gamma=None, grad_beta=None, workspace=None, status=None, stream=None, type=None, res_type=None):
+    """taurus_residual_norm_grad: gradients of residual_norm, with stats as the forward call left them.  Without block, grad_out and grad_block `type` says their type."""
+    t = next((_type_of(x, type) for x in (block, grad_out, grad_block) if hasattr(x, "dtype")), None)
+    t, r = _row_type(type) if t is None else t, _type_of(res, res_type)
+    for x, want in ((block, t), (grad_out, t), (grad_block, t), (grad_out_res, r), (grad_res, r)):
+        if hasattr(x, "dtype") and _row_type(x) != want:
+            raise TypeError("block, grad_out and grad_block are of one type, and so are res, grad_out_res and grad_res")
+    ld_grad_block = ld_grad_block or width
+    _checked(load_library().taurus_residual_norm_grad(
+        n, width, _rows(res, n, width, ld_res), ld_res, r, _rows(block, n, width, ld_block), ld_block, t, kind, int(post), _array(post_gamma, "float32", width), groups,
+        _array(offsets, "int64", groups + 1), _array(gate, "float32", groups * width), alpha, _array(gamma, "float32", width), _array(stats, "float32", 4 * n),
+        _rows(grad_out_res, n, width, ld_grad_out_res), ld_grad_out_res, _rows(grad_out, n, width, ld_grad_out), ld_grad_out, _rows(grad_res, n, width, ld_grad_res), ld_grad_res,
+        _rows(grad_block, n, width, ld_grad_block), ld_grad_block, _array(grad_post_gamma, "float32", width), _array(grad_gate, "float32", groups * width),
+        _array(grad_gamma, "float32", width), _array(grad_beta, "float32", width), *_space(workspace), _array(status, "int32", 1), _stream(stream)), "taurus_residual_norm_grad")
+
+
+class AdamW:
+    """One taurus_adamw: a list of tensors (device tensors, contiguous) that one call steps.  Lists of one length; grads may hold None.  States: float32 tensors, or
+    float8_e4m3fn (or uint8) codes with m_scale and v_scale of one float32 for each STATE_BLOCK elements; master: None, or a list with None for tensors without one."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, master=None, weight_decay=0.0):
+        self._lib = load_library()
+        self._h = ctypes.c_void_p()
+        count = len(params)
+        decay = [float(weight_decay)] * count if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        m_scale, v_scale, master = (x if x is not None else [None] * count for x in (m_scale, v_scale, master))
+        if any(len(x) != count for x in (grads, m, v, m_scale, v_scale, master, decay)):
+            raise ValueError("lists of different lengths")
+        table = (_AdamWTensor * max(count, 1))()
+        for e, p, g, mm, vv, ms, vs, w, d in zip(table, params, grads, m, v, m_scale, v_scale, master, decay):
+            n = p.numel()
+            kinds = {_dtype_name(x.dtype) for x in (mm, vv)}
+            if kinds != {"float32"} and not kinds <= {"float8_e4m3fn", "uint8"}:
+                raise TypeError("m and v are float32, or codes of float8_e4m3fn")
+            eight, blocks = kinds != {"float32"}, -(-n // STATE_BLOCK)
+            e.param, e.param_type, e.count, e.weight_decay = _array(p, None, n), _row_type(p), n, d
+            e.grad, e.grad_type = _array(g, None, n), _row_type(p if g is None else g)
+            if g is not None and g.numel() != n:
+                raise ValueError("a gradient of %d elements for a tensor of %d" % (g.numel(), n))
+            e.m, e.v, e.state_type = _array(mm, None, n), _array(vv, None, n), E4M3 if eight else F32
+            e.m_scale, e.v_scale = (_array(x, "float32", blocks) if eight else None for x in (ms, vs))
+            e.master = _array(w, "float32", n)
+        rc = self._lib.taurus_adamw_create(ctypes.byref(self._h), table, count)
+        if rc != 0:
+            self._h = ctypes.c_void_p()
+            raise TaurusError(rc, "taurus_adamw_create", self._lib.taurus_last_cuda_error().decode() if rc == ERROR_CODES["CUDA"] else "")
+        self._keep = (list(params), list(grads), list(m), list(v), list(m_scale), list(v_scale), list(master))     # the library reads and writes them until destroy()
+
+    def step(self, step, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale=None, seed: int = 0, status=None, stream=None):
+        """taurus_adamw_step.  step (int64), lr, grad_scale (float32): device tensors of one element."""
+        _checked(self._lib.taurus_adamw_step(self._h, _array(step, "int64", 1), _array(lr, "float32", 1), beta1, beta2, eps, _array(grad_scale, "float32", 1), seed,
+                                             _array(status, "int32", 1), _stream(stream)), "taurus_adamw_step")
+
+    def destroy(self):
+        if self._h:
+            self._lib.taurus_adamw_destroy(self._h)
+            self._h = ctypes.c_void_p()
+            self._keep = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
 
 
 class Runs:

@@ -1,0 +1,276 @@
+"""AdamW over lists of tensors: types, sizes, alignments, states in 32 bits and in 8, what is left alone, steps that are skipped, captured and replayed."""
+import pytest
+import torch
+
+import paper_2607_17374_b200 as tb
+from adamw_reference import BLOCK, codes, element_bits, key, scales, step32, update
+from rows_reference import close
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16, E4M3 = torch.float32, torch.bfloat16, torch.float16, torch.float8_e4m3fn
+B1, B2, EPS = 0.9, 0.999, 1e-8
+
+
+def placed(n, dtype, shift):
+    """n elements, `shift` behind an aligned address, and the storage around them."""
+    store = torch.zeros(n + shift + 16, dtype=dtype, device="cuda")
+    return store[shift:shift + n], store
+
+
+class List:
+    def __init__(self, sizes, pt, gt, eight, master=False, shift=0, seed=1, decay=0.01, scale=1e-2):
+        g = torch.Generator("cuda").manual_seed(seed)
+        self.sizes, self.eight, self.n = sizes, eight, len(sizes)
+        self.p, self.g, self.m, self.v, self.ms, self.vs, self.w, self.stores = [], [], [], [], [], [], [], []
+        for n in sizes:
+            def put(x, dtype):
+                y, s = placed(n, dtype, shift)
+                y.copy_(x)
+                self.stores.append((s, y))
+                return y
+
+            def normal():
+                return torch.randn(n, generator=g, device="cuda")
+
+            w = normal()
+            self.p.append(put(w, pt))
+            self.w.append(put(w, F32) if master else None)
+            self.g.append(put(normal() * scale, gt))
+            m, r = normal() * scale, normal().abs() * scale
+            if eight:
+                sm, sv = scales(m.double(), (r * r).double())
+                bits = torch.full((n,), 1 << 15, device="cuda")
+                self.m.append(put(torch.copysign(codes(m.double(), sm, bits).float(), m).to(E4M3), E4M3))
+                self.v.append(put(codes(r.double(), sv, bits).float().to(E4M3), E4M3))
+                nb = -(-n // BLOCK)
+                self.ms.append(sm.float()[:nb].clone())
+                self.vs.append(sv.float()[:nb].clone())
+                m, r = self.held(len(self.m) - 1)
+                self.m[-1].copy_((m.double() / sm.repeat_interleave(BLOCK)[:n]).float().to(E4M3))
+            else:
+                self.m.append(put(m, F32))
+                self.v.append(put(r * r, F32))
+                self.ms.append(None)
+                self.vs.append(None)
+        self.decay = [decay * (i % 2) for i in range(self.n)]
+        self.adamw = tb.AdamW(self.p, self.g, self.m, self.v, self.ms if eight else None, self.vs if eight else None, self.w if master else None, self.decay)
+        self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def held(self, i):
+        """m and the root of v as fp32 values."""
+        if not self.eight:
+            return self.m[i].clone(), self.v[i].clone()
+        n = self.sizes[i]
+        return tuple(x[i].float() * s[i].repeat_interleave(BLOCK)[:n] for x, s in ((self.m, self.ms), (self.v, self.vs)))
+
+    def step(self, t=10, lr=1e-2, gs=None, seed=77, check=True, **kw):
+        step = torch.tensor([t], device="cuda")
+        lr_t = torch.tensor([lr], device="cuda")
+        gs_t = None if gs is None else torch.tensor([gs], device="cuda")
+        before = [(self.held(i), (self.w[i] if self.w[i] is not None else self.p[i]).clone()) for i in range(self.n)]
+        around = [s.clone() for s, _ in self.stores]
+        self.adamw.step(step, lr_t, B1, B2, EPS, gs_t, seed, self.status, **kw)
+        if not check:
+            return
+        assert int(self.status) == 0
+        for i in range(self.n):
+            (m, v), p = before[i]
+            g = self.g[i].float()
+            g = g if gs is None else g * gs_t
+            m, v = step32(m, v * v if self.eight else v, g, B1, B2)
+            new, err = update(p, m, v, t, float(lr_t), torch.tensor(self.decay[i]).float().item(), B1, B2, EPS)
+            close(self.p[i], new, err)
+            if self.w[i] is not None:
+                close(self.w[i], new, err)
+                assert torch.equal(self.p[i], self.w[i].to(self.p[i].dtype))
+            if not self.eight:
+                assert torch.equal(self.m[i], m) and torch.equal(self.v[i], v)
+                continue
+            sm, sv = scales(m.double(), v.double())
+            n, nb = self.sizes[i], -(-self.sizes[i] // BLOCK)
+            assert torch.equal(self.ms[i].double(), sm[:nb]) and torch.equal(self.vs[i].double(), sv[:nb])
+            bits = element_bits(key(seed, t, i), n, "cuda")
+            want = torch.copysign(codes(m.double(), sm, bits & 0xFFFF), m.double())
+            assert torch.equal(self.m[i].double(), want)
+            finite = torch.isfinite(v)                                             # a square that overflows leaves a NaN
+            root = torch.sqrt(torch.where(finite, v, 0.0).double())
+            lo, hi = codes(root, sv, bits >> 16, -2.0 ** -21), codes(root, sv, bits >> 16, 2.0 ** -21)      # the hardware's root: 2 ulp and more
+            least = torch.where(v > 0, 2.0 ** -9, 0.0)
+            got = self.v[i].double()
+            assert ((got >= torch.maximum(lo, least)) & (got <= torch.maximum(hi, least)) | ~finite).all() and torch.isnan(got[~finite]).all()
+            assert (lo != hi).double().mean() < 1e-3 or n < 1000
+        for (s, y), old in zip(self.stores, around):                              # nothing around the tensors
+            old.narrow(0, y.storage_offset(), y.numel()).copy_(y)
+            assert torch.equal(s.view(torch.uint8), old.view(torch.uint8))
+
+
+SIZES = [1, 7, 8, 9, 255, 256, 257, 2047, 2048, 2049, 5000, 100_003]
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("pt,gt,master", [(F32, F32, False), (F32, BF16, False), (BF16, BF16, False), (BF16, F32, True), (F16, F16, True), (F16, F32, False), (BF16, F16, False)])
+@pytest.mark.parametrize("shift,gs", [(0, None), (0, 0.25), (1, 0.25), (16, None)])
+def test_one_step(eight, pt, gt, master, shift, gs):
+    a = List(SIZES, pt, gt, eight, master, shift)
+    a.step(gs=gs)
+    a.step(t=11, lr=3e-3, gs=gs)
+
+
+@pytest.mark.parametrize("t", [1, 2, 1000, 10 ** 6, 10 ** 12])
+@pytest.mark.parametrize("eight", [False, True])
+def test_steps_of_every_number(t, eight):
+    List([3000], F32, F32, eight).step(t=t)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_from_zeros(eight):
+    a = List([777, 256], F32, F32, eight)
+    for i in range(2):
+        a.m[i].zero_()
+        a.v[i].zero_()
+        if eight:
+            a.ms[i].zero_()
+            a.vs[i].zero_()
+    a.g[0][100:600] = 0                               # rows that no id named: nothing moves but by the decay
+    a.decay = [0.0, 0.01]
+    p = a.p[0].clone()
+    a.step(t=1)
+    a.step(t=2)
+    assert torch.equal(a.p[0][100:600], p[100:600])
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-18, 1e-8, 1e6, 1e15])
+def test_gradients_of_every_size(scale):
+    for eight in (False, True):
+        a = List([5000], F32, F32, eight, scale=scale)
+        g = torch.Generator("cuda").manual_seed(4)
+        a.g[0] *= torch.exp(4 * torch.randn(5000, generator=g, device="cuda"))
+        if scale == 1e-30:                            # squares below the smallest number: v is what the states had
+            a.step(check=False)
+            assert torch.isfinite(a.p[0]).all()
+        else:
+            a.step()
+
+
+def test_many_tensors_of_both_states_and_what_is_left_alone():
+    gen = torch.Generator().manual_seed(3)
+    sizes = torch.randint(0, 3000, (400,), generator=gen).tolist()
+    ts = []
+    for i, n in enumerate(sizes):
+        eight = i % 3 == 0
+        p, g = torch.randn(n, device="cuda"), None if i % 7 == 0 else torch.randn(n, device="cuda")
+        m, v = (torch.zeros(n, device="cuda", dtype=E4M3 if eight else F32) for _ in range(2))
+        s = [torch.zeros(-(-n // BLOCK), device="cuda") if eight else None for _ in range(2)]
+        ts.append((p, g, m, v, s[0], s[1]))
+    kept = [p.clone() for p, *_ in ts]
+    a = tb.AdamW(*(list(x) for x in zip(*ts)))
+    lr, step = torch.tensor([1e-2], device="cuda"), torch.tensor([1], device="cuda")
+    a.step(step, lr)
+    for (p, g, m, v, ms, vs), old in zip(ts, kept):
+        if g is None:
+            assert torch.equal(p, old) and (m.float() == 0).all()
+        else:
+            close(p, *update(old, *step32(torch.zeros_like(old), torch.zeros_like(old), g, B1, B2), 1, float(lr), 0.0, B1, B2, EPS))
+            assert ((m.float() != 0) | (g.abs() < 1e-3)).all()
+    a.destroy()
+    tb.AdamW([], [], [], []).step(step, lr)
+
+
+def test_steps_that_are_refused_or_left_out():
+    a = List([1000, 300], F32, F32, True)
+    kept = [x.clone() for x in a.p + a.ms + a.vs] + [x.float() for x in a.m + a.v]
+
+    def same():
+        return all(torch.equal(x, y) for x, y in zip(kept, [x for x in a.p + a.ms + a.vs] + [x.float() for x in a.m + a.v]))
+
+    for gs in (float("inf"), float("nan"), -float("inf")):
+        a.step(gs=gs, check=False)
+        assert same() and int(a.status) == 0
+    for t in (0, -5):
+        a.status.zero_()
+        a.step(t=t, check=False)
+        assert same() and int(a.status) == tb.ERROR_CODES["INVALID_ARG"]
+
+
+def test_gradients_that_are_not_finite_stay_where_they_are():
+    for eight in (False, True):
+        a, b = List([1000], F32, F32, eight), List([1000], F32, F32, eight)
+        bad = torch.tensor([5, 300, 999], device="cuda")
+        a.g[0][bad] = torch.tensor([float("nan"), float("inf"), -float("inf")], device="cuda")
+        b.g[0][bad] = 0.0
+        b.m[0][bad] = 0.0                             # nor do they count for the scale of their block
+        b.v[0][bad] = 0.0
+        a.step(check=False)
+        b.step(check=False)
+        rest = torch.ones(1000, dtype=torch.bool, device="cuda")
+        rest[bad] = False
+        assert torch.equal(a.p[0][rest], b.p[0][rest]) and torch.equal(a.m[0].float()[rest], b.m[0].float()[rest]) and torch.equal(a.v[0].float()[rest], b.v[0].float()[rest])
+        assert torch.isnan(a.p[0][bad]).all() if not eight else torch.isnan(a.m[0].float()[bad]).all()
+
+
+def test_rounding_by_chance_has_no_bias():
+    """Constant gradients: m and the root of v in 8 bits go where those in 32 go, though a step moves v by a thousandth."""
+    n = 1 << 16
+    p, g = torch.zeros(n, device="cuda"), torch.full((n,), 0.37, device="cuda")
+    m, v = (torch.zeros(n, dtype=E4M3, device="cuda") for _ in range(2))
+    ms, vs = (torch.zeros(n // BLOCK, device="cuda") for _ in range(2))
+    a = tb.AdamW([p], [g], [m], [v], [ms], [vs])
+    lr, step = torch.zeros(1, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    steps = 600
+    for _ in range(steps):
+        step += 1
+        a.step(step, lr, B1, B2, EPS, None, 5)
+    # A code is off by at most a step of 1/8 of the value, up or down by chance: over 65 536 elements and the last 1 000 steps that v remembers the mean of v is off by
+    # less than 2 % (the squares' own mean is 1/4 1/64 above: 0.4 % a thousand steps)
+    mean_m, mean_v = float((m.float() * ms.repeat_interleave(BLOCK)).double().mean()), float(((v.float() * vs.repeat_interleave(BLOCK)) ** 2).double().mean())
+    assert abs(mean_m / (0.37 * (1 - B1 ** steps)) - 1) < 0.02
+    want = 0.37 ** 2 * (1 - B2 ** steps)
+    assert -0.02 < mean_v / want - 1 < 0.02 + 0.25 / 64 * steps
+
+
+def test_the_same_bits_again_and_others_with_another_seed():
+    def one(seed, t=4, stream=None):
+        a = List([3000, 500], BF16, BF16, True)
+        torch.cuda.synchronize()
+        a.step(t=t, seed=seed, check=False, stream=stream)
+        torch.cuda.synchronize()
+        return [x.float() for x in a.p + a.m + a.v]
+
+    first = one(9)
+    assert all(torch.equal(x, y) for x, y in zip(first, one(9, stream=torch.cuda.Stream())))
+    other = one(10)
+    assert torch.equal(first[0], other[0]) and not torch.equal(first[2], other[2])
+    assert not torch.equal(first[2], one(9, t=5)[2])
+
+
+def test_captured_and_replayed_with_the_next_step():
+    a, b = List([4000, 77], F32, BF16, True), List([4000, 77], F32, BF16, True)
+    step, lr = torch.ones(1, dtype=torch.int64, device="cuda"), torch.full((1,), 1e-2, device="cuda")
+    torch.cuda.synchronize()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=stream):
+        a.adamw.step(step, lr, B1, B2, EPS, None, 3, a.status, stream)
+    for t in (1, 2, 3):
+        step.fill_(t)
+        lr.fill_(1e-2 / t)
+        graph.replay()
+        b.step(t=t, lr=1e-2 / t, seed=3)
+        assert torch.equal(a.p[0], b.p[0]) and torch.equal(a.m[1].float(), b.m[1].float()) and torch.equal(a.v[0].float(), b.v[0].float())
+
+
+def test_arrays_that_overlap_are_refused():
+    p, g, m, v = (torch.zeros(1000, device="cuda") for _ in range(4))
+    ok = dict(params=[p], grads=[g], m=[m], v=[v])
+    tb.AdamW(**ok)
+    tb.AdamW([p[:500], p[500:]], [g[:500], g[:500]], [m[:500], m[500:]], [v[:500], v[500:]])       # gradients may be the same
+    for change in (dict(grads=[p]), dict(m=[v]), dict(v=[p])):
+        with pytest.raises(tb.TaurusError) as e:
+            tb.AdamW(**dict(ok, **change))
+        assert e.value.code == tb.ERROR_CODES["INVALID_ARG"]
+    with pytest.raises(tb.TaurusError):
+        tb.AdamW([p[:600], p[500:]], [g[:600], g[500:]], [m[:600], torch.zeros(500, device="cuda")], [v[:600], torch.zeros(500, device="cuda")])
+    a = tb.AdamW(**ok)
+    with pytest.raises(tb.TaurusError):
+        a.step(torch.ones(1, dtype=torch.int64, device="cuda"), p[3:4])
+    with pytest.raises(tb.TaurusError):
+        a.step(torch.ones(1, dtype=torch.int64), torch.zeros(1, device="cuda"))           # host memory

@@ -8,8 +8,9 @@
 // masked class (-inf, or a type's lowest value) then adds 0 to both sums, and no 0 x inf comes up.  A NaN goes into m, and with it into everything; +inf is treated as NaN.
 //
 // Bytes bound it: the logits in, once (and their gradient out).
-// Few classes: a thread to a row (rows_kernel).  A tile of rows comes into shared memory in 16-byte loads whatever the rows' width, each row on an odd number of words,
-// so that the threads of a warp read a column without conflicts; top alternatives stay sorted in registers.
+// Few classes: a thread to a row (rows_kernel).  A tile of rows comes into shared memory in 16-byte loads whatever the rows' width, each row on an odd number of words
+// (16-bit rows of odd width: of halves), so that the threads of a warp read a column without conflicts.  The top's candidates are few: values not below the k-th largest of some
+// maxima that the first pass over the row leaves.
 // Many classes: a warp or a block to a row, or to a part of one where there are few rows (stream_kernel), in one pass with a running maximum of the warp; parts are joined in their
 // order by join_kernel.  Candidates for the top are few (a value has to be above the k-th best so far): they go to a list of the warp in shared memory, sorted when it is half full.
 #include <algorithm>
@@ -135,160 +136,231 @@ __device__ __forceinline__ float grad_of_label(const GradRow& r, float x) {
 
 // ---- few classes: a thread to a row ------------------------------------------------------------------------------------------------------------------
 
-enum { TILE_ELEMENTS = 0, TILE_FLAT = 1, TILE_VECTORS = 2 };      // single elements | rows without gaps, 16-byte vectors over them all | vectors within rows
+// How a tile of rows lies in global memory: single elements | 16-byte vectors over rows without gaps | vectors within rows of a pitch.
+enum { TILE_ELEMENTS = 0, TILE_FLAT = 1, TILE_VECTORS = 2 };
 enum { FORWARD = 0, TRAIN = 1, GRAD = 2 };
 
-// f(place in the tile of shared memory, row, column, elements) for every vector of the tile; vectors of fewer than V elements at the end.
-template <class T, int V>
+// Words of shared memory, one element each, or two where 16-bit rows have an even width.
+template <class T, bool PAIRS> struct Word { using type = T; static constexpr int n = 1; };
+template <class T> struct Word<T, true> { using type = uint32_t; static constexpr int n = 2; };
+
+// Brings a tile of `rows` rows of C words in and out.  P: words of a row in shared memory.
+template <class W>
 struct Tile {
-  const Args& a;
-  int rows;
+  static constexpr int V = 16 / (int)sizeof(W);
+  int rows, C, P, vectors;
+  unsigned by_C, by_vectors;
   __device__ __forceinline__ unsigned div(unsigned f, unsigned by) const { return by ? __umulhi(f, by) : f; }     // f < 2^16
-  __device__ __forceinline__ void load(T* sm, const T* x, int mode) const {
-    const int C = a.C, P = a.pitch;
-    if (mode == TILE_FLAT) {
-      const int total = rows * C, whole = total / V;
-      for (int v0 = threadIdx.x; v0 < whole; v0 += 4 * ROW_THREADS) {
-        Vec<T, V> r[4];
+  // The places of a vector's words: those that reach into the next row are P - C further.  (Rows shorter than a vector: any number of rows further.)
+  __device__ __forceinline__ void places(int f, int (&at)[V]) const {
+    const int row = div(f, by_C), col = f - row * C;
+    if (C >= V) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) if (v0 + u * ROW_THREADS < whole) r[u] = load_vec<Vec<T, V>, LOAD_ONCE>(x + (v0 + u * ROW_THREADS) * V);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int v = v0 + u * ROW_THREADS;
-          if (v < whole) {
-            int row = div(v * V, a.by_C), col = v * V - row * C;
-            T* p = sm + row * P + col;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-              *p = r[u].v[i];
-              ++p;
-              if (++col == C) { col = 0; p += P - C; }
-            }
-          }
-        }
-      }
-      for (int f = whole * V + threadIdx.x; f < total; f += ROW_THREADS) { const int row = div(f, a.by_C); sm[row * P + f - row * C] = x[f]; }
-    } else if (mode == TILE_VECTORS) {
-      const int total = rows * a.vectors;
-      for (int v0 = threadIdx.x; v0 < total; v0 += 4 * ROW_THREADS) {
-        Vec<T, V> r[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int v = v0 + u * ROW_THREADS;
-          if (v < total) {
-            const int row = div(v, a.by_vectors), col = (v - row * a.vectors) * V;
-            const T* p = x + row * a.ld + col;
-            if (col + V <= C) r[u] = load_vec<Vec<T, V>, LOAD_ONCE>(p);
-            else
-#pragma unroll
-              for (int i = 0; i < V; ++i) if (col + i < C) r[u].v[i] = p[i];
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int v = v0 + u * ROW_THREADS;
-          if (v < total) {
-            const int row = div(v, a.by_vectors), col = (v - row * a.vectors) * V;
-#pragma unroll
-            for (int i = 0; i < V; ++i) if (col + i < C) sm[row * P + col + i] = r[u].v[i];
-          }
-        }
-      }
+      for (int i = 0; i < V; ++i) at[i] = row * P + col + i + (col + i >= C ? P - C : 0);
     } else {
-      for (int f = threadIdx.x; f < rows * C; f += ROW_THREADS) { const int row = div(f, a.by_C), col = f - row * C; sm[row * P + col] = x[row * a.ld + col]; }
+#pragma unroll
+      for (int i = 0; i < V; ++i) { const int r = div(f + i, by_C); at[i] = r * P + f + i - r * C; }
     }
   }
-  __device__ __forceinline__ void store(const T* sm, T* y, int mode) const {
-    const int C = a.C, P = a.pitch;
-    if (mode == TILE_FLAT) {
-      const int total = rows * C, whole = total / V;
-      for (int v = threadIdx.x; v < whole; v += ROW_THREADS) {
-        int row = div(v * V, a.by_C), col = v * V - row * C;
-        const T* p = sm + row * P + col;
-        Vec<T, V> r;
+  __device__ __forceinline__ void load(W* sm, const W* x, long long ld, int mode) const {
+    if (mode == TILE_ELEMENTS) {
+      for (int f = threadIdx.x; f < rows * C; f += ROW_THREADS) { const int row = div(f, by_C), col = f - row * C; sm[row * P + col] = x[row * ld + col]; }
+      return;
+    }
+    const bool flat = mode == TILE_FLAT;
+    const int words = rows * C, total = flat ? words / V : rows * vectors;
+    for (int v0 = threadIdx.x; v0 < total; v0 += 4 * ROW_THREADS) {
+      Vec<W, V> r[4];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          r.v[i] = *p;
-          ++p;
-          if (++col == C) { col = 0; p += P - C; }
+      for (int u = 0; u < 4; ++u) {
+        const int v = v0 + u * ROW_THREADS;
+        if (v >= total) break;
+        if (flat) r[u] = load_vec<Vec<W, V>, LOAD_ONCE>(x + v * V);
+        else {
+          const int row = div(v, by_vectors), col = (v - row * vectors) * V;
+          const W* const p = x + row * ld + col;
+          if (col + V <= C) r[u] = load_vec<Vec<W, V>, LOAD_ONCE>(p);
+          else
+#pragma unroll
+            for (int i = 0; i < V; ++i) if (col + i < C) r[u].v[i] = p[i];
         }
-        store_vec(y + v * V, r);
       }
-      for (int f = whole * V + threadIdx.x; f < total; f += ROW_THREADS) { const int row = div(f, a.by_C); y[f] = sm[row * P + f - row * C]; }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int v = v0 + u * ROW_THREADS;
+        if (v >= total) break;
+        if (flat && P == C) store_vec(sm + v * V, r[u]);
+        else if (flat) {
+          int at[V];
+          places(v * V, at);
+#pragma unroll
+          for (int i = 0; i < V; ++i) sm[at[i]] = r[u].v[i];
+        } else {
+          const int row = div(v, by_vectors), col = (v - row * vectors) * V;
+#pragma unroll
+          for (int i = 0; i < V; ++i) if (col + i < C) sm[row * P + col + i] = r[u].v[i];
+        }
+      }
+    }
+    if (flat)
+      for (int f = total * V + threadIdx.x; f < words; f += ROW_THREADS) { const int row = div(f, by_C); sm[row * P + f - row * C] = x[f]; }
+  }
+  __device__ __forceinline__ void store(const W* sm, W* y, long long ld, int mode) const {
+    if (mode == TILE_FLAT) {
+      const int words = rows * C, total = words / V;
+      for (int v = threadIdx.x; v < total; v += ROW_THREADS) {
+        Vec<W, V> r;
+        if (P == C) r = load_vec<Vec<W, V>>(sm + v * V);
+        else {
+          int at[V];
+          places(v * V, at);
+#pragma unroll
+          for (int i = 0; i < V; ++i) r.v[i] = sm[at[i]];
+        }
+        store_vec_once(y + v * V, r);
+      }
+      for (int f = total * V + threadIdx.x; f < words; f += ROW_THREADS) { const int row = div(f, by_C); y[f] = sm[row * P + f - row * C]; }
     } else if (mode == TILE_VECTORS) {
-      for (int v = threadIdx.x; v < rows * a.vectors; v += ROW_THREADS) {
-        const int row = div(v, a.by_vectors), col = (v - row * a.vectors) * V;
-        T* const p = y + row * a.ld_dx + col;
+      for (int v = threadIdx.x; v < rows * vectors; v += ROW_THREADS) {
+        const int row = div(v, by_vectors), col = (v - row * vectors) * V;
+        W* const p = y + row * ld + col;
         if (col + V <= C) {
-          Vec<T, V> r;
+          Vec<W, V> r;
 #pragma unroll
           for (int i = 0; i < V; ++i) r.v[i] = sm[row * P + col + i];
-          store_vec(p, r);
+          store_vec_once(p, r);
         } else {
           for (int i = 0; col + i < C; ++i) p[i] = sm[row * P + col + i];
         }
       }
     } else {
-      for (int f = threadIdx.x; f < rows * C; f += ROW_THREADS) { const int row = div(f, a.by_C), col = f - row * C; y[row * a.ld_dx + col] = sm[row * P + col]; }
+      for (int f = threadIdx.x; f < rows * C; f += ROW_THREADS) { const int row = div(f, by_C), col = f - row * C; y[row * ld + col] = sm[row * P + col]; }
     }
   }
 };
 
+template <class T>
+__device__ __forceinline__ void unpack(T w, float (&x)[1]) { x[0] = to_f32<T>(w); }
+template <class T>
+__device__ __forceinline__ void unpack(uint32_t w, float (&x)[2]) {
+  if constexpr (std::is_same_v<T, __nv_bfloat16>) { x[0] = __uint_as_float(w << 16); x[1] = __uint_as_float(w & 0xffff0000u); }
+  else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); x[0] = f.x; x[1] = f.y; }
+}
+template <class T>
+__device__ __forceinline__ T pack(const float (&x)[1]) { return from_f32<T>(x[0]); }
+template <class T>
+__device__ __forceinline__ uint32_t pack(const float (&x)[2]) {
+  Vec<T, 2> r;
+  r.v[0] = from_f32<T>(x[0]); r.v[1] = from_f32<T>(x[1]);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
 // KMAX: places for the top in registers (k <= KMAX; 0: none asked for).
-template <class T, int MODE, int KMAX>
+template <class T, bool PAIRS, int MODE, int KMAX>
 __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
   extern __shared__ __align__(16) unsigned char logprob_shared[];
-  constexpr int V = 16 / (int)sizeof(T);
-  T* const sm = reinterpret_cast<T*>(logprob_shared);
-  const T* const x = static_cast<const T*>(a.x);
-  const int C = a.C;
+  using W = typename Word<T, PAIRS>::type;
+  constexpr int NW = Word<T, PAIRS>::n;
+  W* const sm = reinterpret_cast<W*>(logprob_shared);
+  const int C = a.C, CW = C / NW;
   const long long tiles = (a.n + ROW_THREADS - 1) / ROW_THREADS;
   for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const long long row0 = tile * ROW_THREADS, row = row0 + threadIdx.x;
-    const Tile<T, V> t = {a, (int)(a.n - row0 < ROW_THREADS ? a.n - row0 : ROW_THREADS)};
-    t.load(sm, x + row0 * a.ld, a.mode_in);
+    const Tile<W> t = {(int)(a.n - row0 < ROW_THREADS ? a.n - row0 : ROW_THREADS), CW, a.pitch, a.vectors, a.by_C, a.by_vectors};
+    t.load(sm, reinterpret_cast<const W*>(static_cast<const T*>(a.x) + row0 * a.ld), a.ld / NW, a.mode_in);
     __syncthreads();
     if (row < a.n) {
-      T* const mine = sm + threadIdx.x * a.pitch;
+      W* const mine = sm + threadIdx.x * a.pitch;
+      const T* const elements = reinterpret_cast<const T*>(mine);
       const int label = label_of(a, row);
       RowResult r;
       if (MODE != GRAD) {
-        float m = -INFINITY, any = -INFINITY;
-        int first = -1;
-        float top[KMAX ? KMAX : 1];
+        // Maxima of G classes of classes: the k-th largest of them has k values at least that are not below it, so what is below it is not among the top k.
+        constexpr int G = KMAX == 0 ? 4 : KMAX <= 4 ? 8 : 32;
+        float most[G];
+#pragma unroll
+        for (int i = 0; i < G; ++i) most[i] = -INFINITY;
+        int j = 0;
+        for (; j + G / NW <= CW; j += G / NW)
+#pragma unroll
+          for (int i = 0; i < G / NW; ++i) {
+            float v[NW];
+            unpack<T>(mine[j + i], v);
+#pragma unroll
+            for (int e = 0; e < NW; ++e) most[i * NW + e] = max_nan(most[i * NW + e], v[e]);
+          }
+#pragma unroll
+        for (int i = 0; i < G / NW; ++i)
+          if (j + i < CW) {
+            float v[NW];
+            unpack<T>(mine[j + i], v);
+#pragma unroll
+            for (int e = 0; e < NW; ++e) most[i * NW + e] = max_nan(most[i * NW + e], v[e]);
+          }
+        float m = most[0];
+#pragma unroll
+        for (int i = 1; i < G; ++i) m = max_nan(m, most[i]);
+        const bool bad = !(m < INFINITY);
+        float top[KMAX ? KMAX : 1], floor = -INFINITY;
         int cls[KMAX ? KMAX : 1];
+        if (KMAX) {
 #pragma unroll
-        for (int i = 0; i < KMAX; ++i) { top[i] = -INFINITY; cls[i] = -1; }
-#pragma unroll 4
-        for (int j = 0; j < C; ++j) {
-          const float v = to_f32<T>(mine[j]);
-          any = max_nan(any, v);
-          if (KMAX) {
-            if (v > top[KMAX - 1]) {                       // equal ones keep their places: they have the lower classes
+          for (int i = 0; i < KMAX; ++i) { top[i] = -INFINITY; cls[i] = -1; }
 #pragma unroll
-              for (int i = KMAX - 1; i > 0; --i) {
-                const bool down = v > top[i - 1];
-                const bool here = !down && v > top[i];
-                cls[i] = down ? cls[i - 1] : here ? j : cls[i];
-                top[i] = down ? top[i - 1] : here ? v : top[i];
-              }
-              if (v > top[0]) { top[0] = v; cls[0] = j; }
-            }
-          } else if (v > m) { m = v; first = j; }
+          for (int g = 0; g < G; ++g) {
+            float v = most[g];
+#pragma unroll
+            for (int i = 0; i < KMAX; ++i) { const float up = fmaxf(top[i], v); v = fminf(top[i], v); top[i] = up; }
+          }
+#pragma unroll
+          for (int i = 0; i < KMAX; ++i) if (i == a.k - 1) floor = top[i];
+          if (bad) floor = -INFINITY;                       // a NaN hides its class of classes
+#pragma unroll
+          for (int i = 0; i < KMAX; ++i) top[i] = -INFINITY;
         }
-        if (KMAX) { m = top[0]; first = cls[0]; }
-        const T kept = first >= 0 ? mine[first] : T();
-        if (first >= 0) mine[first] = from_f32<T>(-INFINITY);                     // its term is the 1
+        // The sums, of what is below the maximum; how often that comes up; the top's candidates, 32 classes at a time.
         float s = 0.f, q = 0.f;
-#pragma unroll 4
-        for (int j = 0; j < C; ++j) {
-          const float d = fmaxf(to_f32<T>(mine[j]) - m, LEAST), e = ex2(d * LOG2E);
-          s += e;
-          q = fmaf(e, d, q);
+        int same = 0;
+        constexpr int CHUNK = 32 / NW;
+        for (int j0 = 0; j0 < CW; j0 += CHUNK) {
+          uint32_t found = 0;
+          const auto one = [&](int i) {
+            float v[NW];
+            unpack<T>(mine[j0 + i], v);
+#pragma unroll
+            for (int e = 0; e < NW; ++e) {
+              const float d = fmaxf(v[e] - m, LEAST), p = ex2(d * LOG2E);
+              const bool is = v[e] == m;
+              same += is;
+              s += is ? 0.f : p;
+              q = fmaf(p, d, q);
+              if (KMAX && v[e] >= floor) found |= 1u << (i * NW + e);
+            }
+          };
+          if (j0 + CHUNK <= CW) {
+#pragma unroll 8
+            for (int i = 0; i < CHUNK; ++i) one(i);
+          } else {
+            for (int i = 0; j0 + i < CW; ++i) one(i);
+          }
+          if (KMAX)
+            while (found) {
+              const int b = __ffs(found) - 1, at = j0 * NW + b;
+              found &= found - 1;
+              const float v = to_f32<T>(elements[at]);
+              if (v > top[KMAX - 1]) {                     // equal ones keep their places: they have the lower classes
+#pragma unroll
+                for (int i = KMAX - 1; i > 0; --i) {
+                  const bool down = v > top[i - 1], here = !down && v > top[i];
+                  cls[i] = down ? cls[i - 1] : here ? at : cls[i];
+                  top[i] = down ? top[i - 1] : here ? v : top[i];
+                }
+                if (v > top[0]) { top[0] = v; cls[0] = at; }
+              }
+            }
         }
-        if (first >= 0) mine[first] = kept;
-        r = row_result({m, s, q}, !(any < INFINITY));
-        if (a.logprob) a.logprob[row] = label < 0 ? 0.f : log_p(to_f32<T>(mine[label]), r);
+        r = row_result({m, s + (float)(same - 1), m == -INFINITY ? 0.f : q}, bad);
+        if (a.logprob) a.logprob[row] = label < 0 ? 0.f : log_p(to_f32<T>(elements[label]), r);
         if (a.entropy) a.entropy[row] = r.H;
         if (a.stats) a.stats[row] = make_float2(r.m, r.l);
 #pragma unroll
@@ -303,15 +375,21 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
       }
       if (MODE != FORWARD) {
         const GradRow gr = grad_row(a, row, label, r);
-        const float at = label >= 0 ? to_f32<T>(mine[label]) : 0.f;
-#pragma unroll 4
-        for (int j = 0; j < C; ++j) mine[j] = from_f32<T>(grad_of(gr, to_f32<T>(mine[j])));
-        if (label >= 0) mine[label] = from_f32<T>(grad_of_label(gr, at));
+        const float at = label >= 0 ? to_f32<T>(elements[label]) : 0.f;
+#pragma unroll 8
+        for (int j = 0; j < CW; ++j) {
+          float v[NW];
+          unpack<T>(mine[j], v);
+#pragma unroll
+          for (int e = 0; e < NW; ++e) v[e] = grad_of(gr, v[e]);
+          mine[j] = pack<T>(v);
+        }
+        if (label >= 0) reinterpret_cast<T*>(mine)[label] = from_f32<T>(grad_of_label(gr, at));
       }
     }
     __syncthreads();
     if (MODE != FORWARD) {
-      t.store(sm, static_cast<T*>(a.dx) + row0 * a.ld_dx, a.mode_out);
+      t.store(sm, reinterpret_cast<W*>(static_cast<T*>(a.dx) + row0 * a.ld_dx), a.ld_dx / NW, a.mode_out);
       __syncthreads();
     }
   }
@@ -340,56 +418,86 @@ struct Span {
   }
 };
 
-// A warp's candidates for the top: `count` keys, the first `held` of them sorted; limit: the key of the k-th best of what has been sorted.
+// Largest element of a vector; a NaN is larger than all.
+__device__ __forceinline__ float vector_max(const Vec<float, 4>& r) { return max_nan(max_nan(r.v[0], r.v[1]), max_nan(r.v[2], r.v[3])); }
+__device__ __forceinline__ float vector_max(const Vec<__nv_bfloat16, 8>& r) {
+  const __nv_bfloat162* const h = reinterpret_cast<const __nv_bfloat162*>(&r);
+  const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+  return max_nan(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ float vector_max(const Vec<__half, 8>& r) {
+  const __half2* const h = reinterpret_cast<const __half2*>(&r);
+  const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+  return max_nan(__low2float(m), __high2float(m));
+}
+
+// A warp's candidates for the top: `count` keys in shared memory.  After a sort they are the k best so far; limit: the k-th best's key (0: fewer than k yet), above: its value.  Classes that
+// come later have to be larger than that.  atleast: the largest such value of the block's warps: what is below it is not among the best k of the row.
 struct Candidates {
   u64* list;
   int count;
   u64 limit;
-  float above;                                   // limit's value: later classes have to be larger
-  __device__ __forceinline__ void sort(int k) {
-    const int lane = threadIdx.x & 31;
-    __syncwarp();
-    const u64 a = lane < count ? list[lane] : 0, b = lane + 32 < count ? list[lane + 32] : 0;
-    int ra = 0, rb = 0;
-    for (int i = 0; i < count; ++i) { const u64 o = list[i]; ra += o > a; rb += o > b; }
-    __syncwarp();
-    if (a && ra < k) list[ra] = a;
-    if (b && rb < k) list[rb] = b;
-    count = min(k, __popc(__ballot_sync(0xffffffffu, a != 0)) + __popc(__ballot_sync(0xffffffffu, b != 0)));
-    __syncwarp();
-    if (count == k) { limit = list[k - 1]; above = key_value(limit); }
+  float above, atleast;
+};
+// Keeps the best k, in order.
+__device__ __noinline__ void sort_candidates(Candidates& c, int k, uint32_t* shared_limit) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+  const int count = c.count;
+  const u64 a = lane < count ? c.list[lane] : 0, b = lane + 32 < count ? c.list[lane + 32] : 0;
+  int ra = 0, rb = 0;
+  for (int i = 0; i < count; ++i) { const u64 o = c.list[i]; ra += o > a; rb += o > b; }
+  __syncwarp();
+  if (a && ra < k) c.list[ra] = a;
+  if (b && rb < k) c.list[rb] = b;
+  __syncwarp();
+  c.count = min(k, count);
+  if (c.count == k) {
+    c.limit = c.list[k - 1];
+    c.above = key_value(c.limit);
+    if (lane == 0) atomicMax(shared_limit, (uint32_t)(c.limit >> 32));
   }
-  // Elements of the lanes' vectors: those before the k-th best are put down, 32 at most at a time.
-  template <int N, class ClassOf>
-  __device__ __forceinline__ void add(const float (&x)[N], float most, int k, ClassOf class_of) {
-    const int lane = threadIdx.x & 31;
-    // At least k of the lanes have a value that is not below the k-th largest of the lanes' maxima: what is below that is not among the best k.
-    float kth = most != most ? -INFINITY : most;
-    int rank = 0;
-    for (int i = 0; i < 32; ++i) { const float o = __shfl_sync(0xffffffffu, kth, i); rank += o > kth || (o == kth && i < lane); }
-    kth = __shfl_sync(0xffffffffu, kth, __ffs(__ballot_sync(0xffffffffu, rank == k - 1)) - 1);
-    const float floor = fmaxf(kth, above);
-    const bool mine = most != most || most >= floor;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
+}
+// Every element of a batch, 32 at a time: for the first batch, and for one that brings more candidates than the list takes.
+template <class T>
+__device__ __noinline__ void add_all(Candidates& c, const Span<T> span, int v0, int U, float most, int k, uint32_t* shared_limit) {
+  constexpr int V = Span<T>::V;
+  const int lane = threadIdx.x & 31;
+  // At least k of the lanes have a value that is not below the k-th largest of the lanes' maxima: what is below that is not among the best k.
+  float kth = most != most ? -INFINITY : most;
+  int rank = 0;
+#pragma unroll 1
+  for (int i = 0; i < 32; ++i) { const float o = __shfl_sync(0xffffffffu, kth, i); rank += o > kth || (o == kth && i < lane); }
+  kth = __shfl_sync(0xffffffffu, kth, __ffs(__ballot_sync(0xffffffffu, rank == k - 1)) - 1);
+  const float floor = fmaxf(kth, fmaxf(c.above, c.atleast));
+#pragma unroll 1
+  for (int u = 0; u < U; ++u) {
+    const int at = span.column(v0 + u * 32 + lane);
+#pragma unroll 1
+    for (int i = 0; i < V; ++i) {
       u64 key = 0;
-      if (mine && x[e] >= floor) key = key_of(x[e], class_of(e));
-      const unsigned yes = __ballot_sync(0xffffffffu, key > limit);
+      if (at + i >= span.begin && at + i < span.end) {
+        const float x = to_f32<T>(span.row[at + i]);
+        if (x >= floor) key = key_of(x, at + i);
+      }
+      const unsigned yes = __ballot_sync(0xffffffffu, key > c.limit);
       if (yes) {
-        if (key > limit) list[count + __popc(yes & ((1u << lane) - 1))] = key;
-        count += __popc(yes);
-        if (count > LIST - 32) sort(k);
+        if (key > c.limit) c.list[c.count + __popc(yes & ((1u << lane) - 1))] = key;
+        c.count += __popc(yes);
+        if (c.count > LIST - 32) sort_candidates(c, k, shared_limit);
       }
     }
   }
-};
+  sort_candidates(c, k, shared_limit);
+}
 
 template <class T, bool TOP, int WPR, bool WITH_GRAD>
 __global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
-  constexpr int V = 16 / (int)sizeof(T), U = 64 / 16, N = U * V, STEP = 32 * U;
+  constexpr int V = 16 / (int)sizeof(T), U = 4, STEP = 32 * U;
   __shared__ u64 lists[TOP ? WARPS * LIST : 1];
   __shared__ float4 warp_sums[WARPS];
   __shared__ float4 shared_result;
+  __shared__ uint32_t shared_limit[WARPS];
   early_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = WPR == 1 ? 0 : warp;
   const long long units = a.n * a.parts, stride = WPR == 1 ? (long long)gridDim.x * WARPS : gridDim.x;
@@ -401,29 +509,65 @@ __global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
     const Span<T> span(x, begin, end);
     Sums sums = {-INFINITY, 0.f, 0.f};
     bool bad = false;
-    Candidates top = {lists + (TOP ? warp * LIST : 0), 0, 0, -INFINITY};
+    Candidates top = {lists + (TOP ? warp * LIST : 0), 0, 0, -INFINITY, -INFINITY};
+    uint32_t* const limit = &shared_limit[WPR == 1 ? warp : 0];
+    if (TOP) {
+      if (WPR == 1 ? lane == 0 : threadIdx.x == 0) *limit = 0;
+      if (WPR == 1) __syncwarp(); else __syncthreads();
+    }
     for (int v0 = span.first() + sub * STEP; v0 < span.last(); v0 += WPR * STEP) {
-      float v[N];
-      {
-        Vec<T, V> raw[U];
+      Vec<T, V> raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int at = v0 + u * 32 + lane;
-          if (at < span.last()) raw[u] = span.template load<WITH_GRAD ? LOAD_PLAIN : LOAD_ONCE>(at);
-          else
+      for (int u = 0; u < U; ++u) {
+        const int at = v0 + u * 32 + lane;
+        if (at < span.last()) raw[u] = span.template load<WITH_GRAD ? LOAD_PLAIN : LOAD_ONCE>(at);
+        else
 #pragma unroll
-            for (int i = 0; i < V; ++i) raw[u].v[i] = from_f32<T>(-INFINITY);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int i = 0; i < V; ++i) v[u * V + i] = to_f32<T>(raw[u].v[i]);
+          for (int i = 0; i < V; ++i) raw[u].v[i] = from_f32<T>(-INFINITY);
       }
-      float most = v[0];
+      float most = vector_max(raw[0]);
 #pragma unroll
-      for (int e = 1; e < N; ++e) most = max_nan(most, v[e]);
-      if (TOP && __any_sync(0xffffffffu, !(most <= top.above)))
-        top.add(v, most, a.k, [&](int e) { return span.column(v0 + (e / V) * 32 + lane) + e % V; });
+      for (int u = 1; u < U; ++u) most = max_nan(most, vector_max(raw[u]));
+      if (TOP) {
+        if (WPR > 1) {
+          const uint32_t o = *reinterpret_cast<volatile uint32_t*>(limit);
+          if (o) top.atleast = key_value((u64)o << 32);
+        }
+        // (not !(most <= ...): a NaN has its lane looked through)
+        if (__any_sync(0xffffffffu, !(most <= top.above) && !(most < top.atleast))) {
+          bool all = top.limit == 0;
+          if (!all) {
+            const int had = top.count;
+            int mine = 0;
+            if (!(most <= top.above) && !(most < top.atleast)) {
+#pragma unroll
+              for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < V; ++i) { const float x = to_f32<T>(raw[u].v[i]); mine += x > top.above && x >= top.atleast; }
+            }
+            int upto = mine;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(0xffffffffu, upto, d); if (lane >= d) upto += o; }
+            const int more = __shfl_sync(0xffffffffu, upto, 31);
+            all = had + more > LIST;
+            if (!all) {
+              if (mine) {
+                u64* to = top.list + had + upto - mine;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                  for (int i = 0; i < V; ++i) {
+                    const float x = to_f32<T>(raw[u].v[i]);
+                    if (x > top.above && x >= top.atleast) *to++ = key_of(x, span.column(v0 + u * 32 + lane) + i);
+                  }
+              }
+              top.count = had + more;
+              if (top.count > LIST / 2) sort_candidates(top, a.k, limit);
+            }
+          }
+          if (all) add_all<T>(top, span, v0, U, most, a.k, limit);
+        }
+      }
       if (__any_sync(0xffffffffu, !(most <= sums.m))) {
         float w = most;
 #pragma unroll
@@ -439,16 +583,20 @@ __global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
           if (lane == __ffs(__ballot_sync(0xffffffffu, most == w)) - 1) {        // this lane has the term that is 1
             bool found = false;
 #pragma unroll
-            for (int e = 0; e < N; ++e) if (!found && v[e] == w) { v[e] = -INFINITY; found = true; }
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+              for (int i = 0; i < V; ++i) if (!found && to_f32<T>(raw[u].v[i]) == w) { raw[u].v[i] = from_f32<T>(-INFINITY); found = true; }
           }
         }
       }
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float d = fmaxf(v[e] - sums.m, LEAST), p = ex2(d * LOG2E);
-        sums.s += p;
-        sums.t = fmaf(p, d, sums.t);
-      }
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float d = fmaxf(to_f32<T>(raw[u].v[i]) - sums.m, LEAST), p = ex2(d * LOG2E);
+          sums.s += p;
+          sums.t = fmaf(p, d, sums.t);
+        }
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
@@ -456,7 +604,7 @@ __global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
       sums.t += __shfl_xor_sync(0xffffffffu, sums.t, d);
     }
     if (TOP) {
-      top.sort(a.k);
+      sort_candidates(top, a.k, limit);
       if (lane >= top.count && lane < a.k) top.list[lane] = 0;
     }
     if (WPR > 1) {
@@ -631,32 +779,41 @@ Space space_of(int64_t n, int C, int k) {
   return s;
 }
 
-template <class T>
+template <class T, bool PAIRS>
 void set_tile(Args* a) {
-  constexpr int V = 16 / (int)sizeof(T);
-  const int C = a->C;
-  a->pitch = sizeof(T) == 4 ? (C | 1) : 2 * (((C + 1) / 2) | 1);
+  constexpr int NW = PAIRS ? 2 : 1, V = 16 / (NW * (int)sizeof(T));               // elements of a word, words of a vector
+  const int C = a->C / NW;
+  a->pitch = sizeof(T) * NW == 2 ? C : C | 1;                                     // (PAIRS: even widths; else odd ones of 16 bits, or fp32)
   const auto by = [](int d) { return d == 1 ? 0u : (unsigned)(((1ull << 32) + d - 1) / d); };
   a->vectors = (C + V - 1) / V;
   a->by_C = by(C); a->by_vectors = by(a->vectors);
   const auto mode = [&](const void* p, long long ld) {
     if (!rows_aligned(p, 16)) return (int)TILE_ELEMENTS;
-    return ld == C ? (int)TILE_FLAT : ld % V == 0 ? (int)TILE_VECTORS : (int)TILE_ELEMENTS;
+    return ld == a->C ? (int)TILE_FLAT : ld % (V * NW) == 0 ? (int)TILE_VECTORS : (int)TILE_ELEMENTS;
   };
   a->mode_in = mode(a->x, a->ld);
   a->mode_out = mode(a->dx, a->ld_dx);
 }
 
-template <class T, int MODE, int KMAX>
-void launch_rows(Launches& enqueue, Args a, int sms) {
-  set_tile<T>(&a);
-  const size_t smem = (size_t)a.pitch * sizeof(T) * ROW_THREADS;
+template <class T, bool PAIRS, int MODE, int KMAX>
+void launch_tiles(Launches& enqueue, Args a) {
+  set_tile<T, PAIRS>(&a);
+  const size_t smem = (size_t)a.pitch * sizeof(T) * (PAIRS ? 2 : 1) * ROW_THREADS;
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(rows_kernel<T, MODE, KMAX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(rows_kernel<T, PAIRS, MODE, KMAX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) { enqueue.error = e; return; }
   }
   const int64_t tiles = (a.n + ROW_THREADS - 1) / ROW_THREADS;
-  enqueue(rows_kernel<T, MODE, KMAX>, dim3((unsigned)std::min<int64_t>(tiles, 1 << 30)), ROW_THREADS, smem, a);
+  enqueue(rows_kernel<T, PAIRS, MODE, KMAX>, dim3((unsigned)std::min<int64_t>(tiles, 1 << 30)), ROW_THREADS, smem, a);
+}
+template <class T, int MODE, int KMAX>
+void launch_rows(Launches& enqueue, const Args& a) {
+  // Pairs: rows of 16 bits that begin at even elements everywhere.
+  if constexpr (sizeof(T) == 2) {
+    const auto even = [](const void* p, long long ld) { return rows_aligned(p, 4) && ld % 2 == 0; };
+    if (a.C % 2 == 0 && even(a.x, a.ld) && (MODE == FORWARD || even(a.dx, a.ld_dx))) { launch_tiles<T, true, MODE, KMAX>(enqueue, a); return; }
+  }
+  launch_tiles<T, false, MODE, KMAX>(enqueue, a);
 }
 template <class T>
 void launch_grad(Launches& enqueue, const Args& a, int sms) {
@@ -694,11 +851,11 @@ int class_call(Args a, int32_t type, int what, int in_place_ok, void* workspace,
   with_row_type(type, [&](auto tt) {
     using T = typename decltype(tt)::type;
     if (by_thread(a.C, ts)) {
-      if (what == GIVEN_STATS) launch_rows<T, GRAD, 0>(enqueue, a, sms);
-      else if (what == GIVEN_WEIGHTS) launch_rows<T, TRAIN, 0>(enqueue, a, sms);
-      else if (a.k == 0) launch_rows<T, FORWARD, 0>(enqueue, a, sms);
-      else if (a.k <= 4) launch_rows<T, FORWARD, 4>(enqueue, a, sms);
-      else launch_rows<T, FORWARD, MAX_TOP>(enqueue, a, sms);
+      if (what == GIVEN_STATS) launch_rows<T, GRAD, 0>(enqueue, a);
+      else if (what == GIVEN_WEIGHTS) launch_rows<T, TRAIN, 0>(enqueue, a);
+      else if (a.k == 0) launch_rows<T, FORWARD, 0>(enqueue, a);
+      else if (a.k <= 4) launch_rows<T, FORWARD, 4>(enqueue, a);
+      else launch_rows<T, FORWARD, MAX_TOP>(enqueue, a);
       return 0;
     }
     if (what == GIVEN_STATS) { launch_grad<T>(enqueue, a, sms); return 0; }

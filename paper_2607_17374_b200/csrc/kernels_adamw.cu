@@ -3,8 +3,8 @@
 //   g = s grad,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
 //   p = p - lr wd p - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
 //
-// Bytes bound it: 28 an element with everything in fp32, 10.06 with parameters and gradients in 16 bits and states in 8.  All tensors are cut into tiles of 2 048
-// elements, which the blocks of one launch take in turn: a tensor costs no launch, and its description and a tile's tensor are read from device memory.
+// Bytes bound it: 28 an element with everything in fp32, 10.06 with parameters and gradients in 16 bits and states in 8.  All tensors are cut into tiles of 8 192
+// elements, which the blocks of one launch (for each combination of types) take in turn: a tensor costs no launch, and its description and a tile's tensor are read from device memory.
 //
 // States in 8 bits: m and r = sqrt(v) as e4m3 codes times a power of two for each 256 elements, one warp's.  With the scale the largest code is in [2^7, 2^8), the
 // smallest step 2^-16 of the largest value; multiplying by the scale is exact.  Rounded to nearest a state would stand still: a step of e4m3 is 6 to 12 % of the
@@ -22,7 +22,7 @@
 
 namespace {
 
-constexpr int THREADS = 256, E = 8, TILE = THREADS * E, BLOCK = TAURUS_STATE_BLOCK;
+constexpr int THREADS = 256, E = 8, STEPS = 1, TILE = STEPS * THREADS * E, BLOCK = TAURUS_STATE_BLOCK;
 static_assert(32 * E == BLOCK, "a block of states is a warp's");
 
 struct Tensor {
@@ -45,6 +45,7 @@ struct Args {
   const long long* step;
   const float *lr, *grad_scale;
   float beta1, rest1, beta2, rest2, eps;
+  float none;                                    // -0, as a number that the compiler does not know: a product and -0 is the rounded product, which no later sum takes in unrounded
   double log_beta1, log_beta2;
   unsigned long long seed;
   int32_t* status;
@@ -56,74 +57,245 @@ __device__ __forceinline__ unsigned long long mix64(unsigned long long z) {
   return z ^ (z >> 31);
 }
 __device__ __forceinline__ unsigned long long absorb(unsigned long long h, unsigned long long x) { return mix64(h ^ (0x9E3779B97F4A7C15ull * (x + 1))); }
-// 32 bits for element i: the published finaliser lowbias32 (Wellons).
-__device__ __forceinline__ uint32_t element_bits(unsigned long long key, long long i) {
-  uint32_t x = ((uint32_t)i ^ (uint32_t)key) + (uint32_t)(key >> 32) + (uint32_t)(i >> 32) * 0x85EBCA6Bu;
+// 32 bits for element i of a tensor: the published finaliser lowbias32 (Wellons) of (i ^ key) + (key >> 32) + (i >> 32) 0x85EBCA6B.
+__device__ __forceinline__ uint32_t finish_bits(uint32_t x) {
   x = (x ^ (x >> 16)) * 0x7FEB352Du;
   x = (x ^ (x >> 15)) * 0x846CA68Bu;
   return x ^ (x >> 16);
 }
 
-// 8 elements as they lie in memory.
-struct Raw { uint4 a, b; };
-__device__ __forceinline__ Raw load_raw(const void* p, long long i, int type) {
-  Raw r;
-  const char* const at = static_cast<const char*>(p) + i * (type == TAURUS_F32 ? 4 : 2);
-  r.a = __ldcs(reinterpret_cast<const uint4*>(at));
-  r.b = type == TAURUS_F32 ? __ldcs(reinterpret_cast<const uint4*>(at) + 1) : make_uint4(0, 0, 0, 0);
-  return r;
-}
-__device__ __forceinline__ float load_one(const void* p, long long i, int type) {
-  if (type == TAURUS_F32) return static_cast<const float*>(p)[i];
-  if (type == TAURUS_BF16) return to_f32(static_cast<const __nv_bfloat16*>(p)[i]);
-  return to_f32(static_cast<const __half*>(p)[i]);
-}
-__device__ __forceinline__ void store_one(void* p, long long i, int type, float x) {
-  if (type == TAURUS_F32) static_cast<float*>(p)[i] = x;
-  else if (type == TAURUS_BF16) static_cast<__nv_bfloat16*>(p)[i] = from_f32<__nv_bfloat16>(x);
-  else static_cast<__half*>(p)[i] = from_f32<__half>(x);
-}
-__device__ __forceinline__ void raw_to_f32(const Raw& r, int type, float (&x)[E]) {
-  const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
-  if (type == TAURUS_F32) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = __uint_as_float(w[e]);
-  } else if (type == TAURUS_BF16) {
-#pragma unroll
-    for (int e = 0; e < E; e += 2) { x[e] = __uint_as_float(w[e / 2] << 16); x[e + 1] = __uint_as_float(w[e / 2] & 0xffff0000u); }
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[e / 2]));
-      x[e] = f.x; x[e + 1] = f.y;
-    }
-  }
-}
-__device__ __forceinline__ void store_vector(void* p, long long i, int type, const float (&x)[E]) {
-  if (type == TAURUS_F32) store_f32_once<float, E>(static_cast<float*>(p) + i, x);
-  else if (type == TAURUS_BF16) store_f32_once<__nv_bfloat16, E>(static_cast<__nv_bfloat16*>(p) + i, x);
-  else store_f32_once<__half, E>(static_cast<__half*>(p) + i, x);
-}
+// Two fp32 values in one register pair, and their arithmetic in one instruction.
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ F2 f2(float a) { return f2(a, a); }
+__device__ __forceinline__ float lo(F2 x) { float a, b; asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); return a; }
+__device__ __forceinline__ float hi(F2 x) { float a, b; asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); return b; }
+__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+__device__ __forceinline__ float root_of(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float reciprocal(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
-__device__ __forceinline__ void codes_to_f32(uint2 c, float scale, float (&x)[E]) {
+template <class T>
+__device__ __forceinline__ void to_pairs(const Vec<T, E>& r, F2 (&x)[E / 2]) {
+#pragma unroll
+  for (int e = 0; e < E; e += 2) x[e / 2] = f2(to_f32<T>(r.v[e]), to_f32<T>(r.v[e + 1]));
+}
+__device__ __forceinline__ void codes_to_pairs(uint2 c, F2 scale, F2 (&x)[E / 2]) {
   const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
   for (int e = 0; e < E; e += 2) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[e / 4] >> (8 * (e & 2))), __NV_E4M3);
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    x[e] = f.x * scale; x[e + 1] = f.y * scale;
+    x[e / 2] = mul(f2(f.x, f.y), scale);
   }
 }
-// |x| below 2^8 as an e4m3 code, up with the probability of what is cut off: bits are added below the three that stay.  Below 2^-6 the step is 2^-9: with
-// 2^-6 added (rounded down, as is everything behind the last place of the sum) those values have the same three bits.
-__device__ __forceinline__ uint32_t code_of(float q, uint32_t bits16) {
-  const bool low = q < 0x1p-6f;
-  const float y = low ? __fadd_rz(q, 0x1p-6f) : q;
-  return ((__float_as_uint(y) + (bits16 << 4)) >> 20) - (low ? 121u * 8 : 120u * 8);
-}
+__device__ __forceinline__ float mul_down(float a, float b) { float r; asm("mul.rz.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 constexpr uint32_t NOT_FINITE = 0x7f800000u, CODE_NAN = 0x7f;
 
-template <bool EIGHT>
+// What a step multiplies and adds with.
+struct Factors { F2 beta1, rest1, beta2, rest2, none, gs, c2, eps, rate, keep; };
+
+// Which elements of a warp's 256 a lane has: 8 in a row where they are 16 bytes at most; else four and four, so that the warp's loads of 16 bytes touch every sector once (8 fp32
+// values in a row would be two loads of half of each).
+template <bool WIDE>
+struct Places {
+  static constexpr int GROUP = WIDE ? 4 : 8;
+  static __device__ __forceinline__ constexpr int element(int e) { return WIDE ? e / 4 * 128 + e % 4 : e; }
+  static __device__ __forceinline__ int lane_place(int lane) { return lane * GROUP; }
+  template <class T>
+  static __device__ __forceinline__ Vec<T, E> load(const T* p, int lane) {
+    if (!WIDE) return load_vec<Vec<T, E>, LOAD_ONCE>(p + lane * E);
+    Vec<T, E> r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const auto q = load_vec<Vec<T, 4>, LOAD_ONCE>(p + h * 128 + lane * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.v[h * 4 + i] = q.v[i];
+    }
+    return r;
+  }
+  template <class T>
+  static __device__ __forceinline__ void store(T* p, int lane, const F2 (&x)[E / 2]) {
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; e += 2) { v[e] = lo(x[e / 2]); v[e + 1] = hi(x[e / 2]); }
+    if (!WIDE) { store_f32_once<T, E>(p + lane * E, v); return; }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float q[4] = {v[h * 4], v[h * 4 + 1], v[h * 4 + 2], v[h * 4 + 3]};
+      store_f32_once<T, 4>(p + h * 128 + lane * 4, q);
+    }
+  }
+  static __device__ __forceinline__ uint2 load_codes(const uint8_t* p, int lane) {
+    if (!WIDE) return __ldcs(reinterpret_cast<const uint2*>(p + lane * E));
+    return make_uint2(__ldcs(reinterpret_cast<const uint32_t*>(p + lane * 4)), __ldcs(reinterpret_cast<const uint32_t*>(p + 128 + lane * 4)));
+  }
+  static __device__ __forceinline__ void store_codes(uint8_t* p, int lane, uint2 c) {
+    if (!WIDE) { __stcs(reinterpret_cast<uint2*>(p + lane * E), c); return; }
+    __stcs(reinterpret_cast<uint32_t*>(p + lane * 4), c.x);
+    __stcs(reinterpret_cast<uint32_t*>(p + 128 + lane * 4), c.y);
+  }
+};
+
+// A warp's 256 elements of a tensor, from b on.
+template <class PT, class GT, bool EIGHT>
+__device__ __forceinline__ void step_block(const Tensor& t, const Factors& f, unsigned long long key, long long b) {
+  using P = Places<!EIGHT || sizeof(PT) == 4 || sizeof(GT) == 4>;
+  const int lane = threadIdx.x & 31, first = P::lane_place(lane);
+  const int left = (int)(t.count - b < BLOCK ? t.count - b : BLOCK);    // 1 at least
+  const bool whole = t.vectors && left == BLOCK;
+  const auto in = [&](int e) { return first + P::element(e) < left; };
+  PT* const pp = static_cast<PT*>(t.p) + b;
+  const GT* const gp = static_cast<const GT*>(t.g) + b;
+  uint8_t *const mc = static_cast<uint8_t*>(t.m) + b, *const vc = static_cast<uint8_t*>(t.v) + b;
+  float *const mf = static_cast<float*>(t.m) + b, *const vf = static_cast<float*>(t.v) + b;
+  F2 p[E / 2], g[E / 2], m[E / 2], v[E / 2];
+  if (whole) {
+    // all on their way before the first is used
+    const auto rg = P::template load<GT>(gp, lane);
+    uint2 cm, cv;
+    Vec<float, E> rm, rv, rw;
+    Vec<PT, E> rp;
+    float ms, vs;
+    if (EIGHT) {
+      cm = P::load_codes(mc, lane); cv = P::load_codes(vc, lane);
+      ms = t.m_scale[b / BLOCK]; vs = t.v_scale[b / BLOCK];
+    } else {
+      rm = P::template load<float>(mf, lane); rv = P::template load<float>(vf, lane);
+    }
+    if (sizeof(PT) == 2 && t.master) rw = P::template load<float>(t.master + b, lane);
+    else rp = P::template load<PT>(pp, lane);
+    if (EIGHT) {
+      codes_to_pairs(cm, f2(ms), m);
+      codes_to_pairs(cv, f2(vs), v);
+    } else {
+      to_pairs<float>(rm, m);
+      to_pairs<float>(rv, v);
+    }
+    if (sizeof(PT) == 2 && t.master) to_pairs<float>(rw, p);
+    else to_pairs<PT>(rp, p);
+    to_pairs<GT>(rg, g);
+  } else {
+    float x[E] = {}, y[E] = {}, c[E] = {}, d[E] = {};
+    uint2 cm = make_uint2(0, 0), cv = make_uint2(0, 0);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (in(e)) {
+        const int at = first + P::element(e);
+        x[e] = sizeof(PT) == 2 && t.master ? t.master[b + at] : to_f32<PT>(pp[at]);
+        y[e] = to_f32<GT>(gp[at]);
+        if (EIGHT) {
+          (e < 4 ? cm.x : cm.y) |= (uint32_t)mc[at] << (8 * (e & 3));
+          (e < 4 ? cv.x : cv.y) |= (uint32_t)vc[at] << (8 * (e & 3));
+        } else { c[e] = mf[at]; d[e] = vf[at]; }
+      }
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      p[e / 2] = f2(x[e], x[e + 1]); g[e / 2] = f2(y[e], y[e + 1]);
+      if (!EIGHT) { m[e / 2] = f2(c[e], c[e + 1]); v[e / 2] = f2(d[e], d[e + 1]); }
+    }
+    if (EIGHT) {
+      codes_to_pairs(cm, f2(t.m_scale[b / BLOCK]), m);
+      codes_to_pairs(cv, f2(t.v_scale[b / BLOCK]), v);
+    }
+  }
+  float root[E];
+#pragma unroll
+  for (int k = 0; k < E / 2; ++k) {
+    const F2 ge = mul(g[k], f.gs);
+    m[k] = add(fma(f.beta1, m[k], f.none), fma(f.rest1, ge, f.none));
+    if (EIGHT) v[k] = mul(v[k], v[k]);
+    v[k] = add(fma(f.beta2, v[k], f.none), fma(mul(f.rest2, ge), ge, f.none));
+    root[2 * k] = root_of(lo(v[k])); root[2 * k + 1] = root_of(hi(v[k]));
+    const F2 below = fma(f2(root[2 * k], root[2 * k + 1]), f.c2, f.eps);
+    p[k] = fma(mul(m[k], f.rate), f2(reciprocal(lo(below)), reciprocal(hi(below))), mul(p[k], f.keep));
+  }
+  if (whole) {
+    P::template store<PT>(pp, lane, p);
+    if (sizeof(PT) == 2 && t.master) P::template store<float>(t.master + b, lane, p);
+    if (!EIGHT) {
+      P::template store<float>(mf, lane, m);
+      P::template store<float>(vf, lane, v);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (in(e)) {
+        const int at = first + P::element(e);
+        const float x = e & 1 ? hi(p[e / 2]) : lo(p[e / 2]);
+        pp[at] = from_f32<PT>(x);
+        if (sizeof(PT) == 2 && t.master) t.master[b + at] = x;
+        if (!EIGHT) {
+          mf[at] = e & 1 ? hi(m[e / 2]) : lo(m[e / 2]);
+          vf[at] = e & 1 ? hi(v[e / 2]) : lo(v[e / 2]);
+        }
+      }
+  }
+  if (EIGHT) {
+    float mm = 0.f, mv = 0.f;
+#pragma unroll
+    for (int k = 0; k < E / 2; ++k) {
+      mm = max_nan(max_nan(mm, fabsf(lo(m[k]))), fabsf(hi(m[k])));
+      mv = max_nan(max_nan(mv, lo(v[k])), hi(v[k]));
+    }
+    uint32_t most_m = __reduce_max_sync(0xffffffffu, __float_as_uint(mm) & 0x7fffffffu), most_v = __reduce_max_sync(0xffffffffu, __float_as_uint(mv) & 0x7fffffffu);
+    const bool odd = most_m >= NOT_FINITE || most_v >= NOT_FINITE;      // somewhere in the block: scales by what is finite
+    if (odd) {
+      uint32_t am = 0, av = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint32_t bm = __float_as_uint(e & 1 ? hi(m[e / 2]) : lo(m[e / 2])) & 0x7fffffffu, bv = __float_as_uint(e & 1 ? hi(v[e / 2]) : lo(v[e / 2])) & 0x7fffffffu;
+        if (bm < NOT_FINITE) am = max(am, bm);
+        if (bv < NOT_FINITE) av = max(av, bv);
+      }
+      most_m = __reduce_max_sync(0xffffffffu, am);
+      most_v = __reduce_max_sync(0xffffffffu, av);
+    }
+    // The whole part of the largest one's logarithm, down by 7; of sqrt(v) half of v's.
+    const int em = (int)max(most_m >> 23, 8u) - 7, ev = (((int)max(most_v >> 23, 1u) - 127) >> 1) + 120;
+    // Codes.  x / scale 2^-120 has e4m3's exponent, 7 above its own, where fp32 has its exponent's last four bits, and below e4m3's smallest exponent it is a subnormal
+    // number of fp32 (rounded down at 2^-149, 20 places below the last that stays): its bits 20 to 26 are the code, whatever its size, once the 16 random bits are added below
+    // them.  Four places further up a code is a byte.  The factor is applied in two parts: one may be too small for fp32.
+    const float part_m = __int_as_float(em < 234 ? (234 - em) << 23 : 1 << (256 - em)), part_v = __int_as_float((234 - ev) << 23);      // 2^(107 - e)
+    const uint32_t base = (uint32_t)b ^ (uint32_t)key ^ (uint32_t)P::lane_place(lane), more = (uint32_t)(key >> 32) + (uint32_t)(b >> 32) * 0x85EBCA6Bu;     // (places differ in bits of their own)
+    uint32_t cm[E], cv[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float me = e & 1 ? hi(m[e / 2]) : lo(m[e / 2]);
+      const uint32_t bits = finish_bits((base ^ (uint32_t)P::element(e)) + more);
+      const float zm = mul_down(fabsf(me) * part_m, 0x1p-100f);
+      const float least = fminf(root[e] * 0x1p60f, __uint_as_float(1u << 20));                    // code 1 where the root is not 0
+      const float zv = fmaxf(mul_down(root[e] * part_v, 0x1p-100f), least);
+      cm[e] = ((__float_as_uint(zm) << 4) + __byte_perm(bits, 0, 0x4104)) | (__float_as_uint(me) & 0x80000000u);
+      cv[e] = (__float_as_uint(zv) << 4) + __byte_perm(bits, 0, 0x4324);
+    }
+    if (odd) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float me = e & 1 ? hi(m[e / 2]) : lo(m[e / 2]);
+        if (!(fabsf(me) < INFINITY)) cm[e] = CODE_NAN << 24;
+        if (!(root[e] < INFINITY)) cv[e] = CODE_NAN << 24;
+      }
+    }
+    const auto four = [](const uint32_t* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410); };
+    if (lane == 0) {
+      t.m_scale[b / BLOCK] = __uint_as_float((uint32_t)em << 23);
+      t.v_scale[b / BLOCK] = __uint_as_float((uint32_t)ev << 23);
+    }
+    if (whole) {
+      P::store_codes(mc, lane, make_uint2(four(cm), four(cm + 4)));
+      P::store_codes(vc, lane, make_uint2(four(cv), four(cv + 4)));
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (in(e)) { mc[first + P::element(e)] = (uint8_t)(cm[e] >> 24); vc[first + P::element(e)] = (uint8_t)(cv[e] >> 24); }
+    }
+  }
+}
+
+template <class PT, class GT, bool EIGHT>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(const Args a) {
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const long long step = *a.step;
@@ -135,118 +307,38 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const Args a) {
   const float lr = *a.lr;
   // 1 - b^t = -(e^(t ln b) - 1)
   const float c1 = -1.f / expm1f((float)((double)step * a.log_beta1)), c2 = rsqrtf(-expm1f((float)((double)step * a.log_beta2)));
-  const int lane = threadIdx.x & 31;
+  Factors f = {f2(a.beta1), f2(a.rest1), f2(a.beta2), f2(a.rest2), f2(a.none), f2(gs), f2(c2), f2(a.eps), f2(-lr * c1), f2(1.f)};
   unsigned long long seed_key = 0, key = 0;
   if (EIGHT) seed_key = absorb(absorb(0x243F6A8885A308D3ull, a.seed), (unsigned long long)step);
   int known = -1;
-  Tensor t;
+  __shared__ Tensor t;                           // (in registers it would take the place of 22 of them)
   for (long long tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
     const int which = a.tile_tensor[tile];
     if (which != known) {
-      t = a.tensors[which];
+      __syncthreads();
+      if (threadIdx.x < sizeof(Tensor) / 4) reinterpret_cast<uint32_t*>(&t)[threadIdx.x] = reinterpret_cast<const uint32_t*>(a.tensors + which)[threadIdx.x];
+      __syncthreads();
       known = which;
+      f.keep = f2(fmaf(-lr, t.decay, 1.f));
       if (EIGHT) key = absorb(seed_key, t.index);
     }
-    const long long i = (tile - t.first_tile) * TILE + threadIdx.x * E;
-    const int left = (int)(t.count - i < E ? t.count - i : E);          // (0 or less: none)
-    const bool whole = t.vectors && left == E;
-    float p[E], g[E], m[E], v[E];
-    float ms = 0.f, vs = 0.f;
-    if (EIGHT && left > 0) { ms = t.m_scale[i / BLOCK]; vs = t.v_scale[i / BLOCK]; }
-    if (whole) {
-      const Raw rg = load_raw(t.g, i, t.g_type), rp = t.master ? load_raw(t.master, i, TAURUS_F32) : load_raw(t.p, i, t.p_type);
-      if (EIGHT) {
-        const uint2 cm = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.m) + i)), cv = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + i));
-        codes_to_f32(cm, ms, m);
-        codes_to_f32(cv, vs, v);
-      } else {
-        const Raw rm = load_raw(t.m, i, TAURUS_F32), rv = load_raw(t.v, i, TAURUS_F32);
-        raw_to_f32(rm, TAURUS_F32, m);
-        raw_to_f32(rv, TAURUS_F32, v);
-      }
-      raw_to_f32(rg, t.g_type, g);
-      raw_to_f32(rp, t.master ? TAURUS_F32 : t.p_type, p);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        p[e] = g[e] = m[e] = v[e] = 0.f;
-        if (e < left) {
-          g[e] = load_one(t.g, i + e, t.g_type);
-          p[e] = t.master ? t.master[i + e] : load_one(t.p, i + e, t.p_type);
-          if (EIGHT) {
-            __nv_fp8_e4m3 c;
-            c.__x = static_cast<const uint8_t*>(t.m)[i + e]; m[e] = (float)c * ms;
-            c.__x = static_cast<const uint8_t*>(t.v)[i + e]; v[e] = (float)c * vs;
-          } else {
-            m[e] = static_cast<const float*>(t.m)[i + e];
-            v[e] = static_cast<const float*>(t.v)[i + e];
-          }
-        }
-      }
-    }
-    float root[E];
-    const float keep = fmaf(-lr, t.decay, 1.f);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float ge = a.grad_scale ? g[e] * gs : g[e];
-      m[e] = __fadd_rn(__fmul_rn(a.beta1, m[e]), __fmul_rn(a.rest1, ge));
-      if (EIGHT) v[e] = __fmul_rn(v[e], v[e]);
-      v[e] = __fadd_rn(__fmul_rn(a.beta2, v[e]), __fmul_rn(__fmul_rn(a.rest2, ge), ge));
-      asm("sqrt.approx.f32 %0, %1;" : "=f"(root[e]) : "f"(v[e]));
-      p[e] = fmaf(-lr, __fdividef(m[e] * c1, fmaf(root[e], c2, a.eps)), p[e] * keep);
-    }
-    if (whole) {
-      store_vector(t.p, i, t.p_type, p);
-      if (t.master) store_vector(t.master, i, TAURUS_F32, p);
-      if (!EIGHT) {
-        store_vector(t.m, i, TAURUS_F32, m);
-        store_vector(t.v, i, TAURUS_F32, v);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (e < left) {
-          store_one(t.p, i + e, t.p_type, p[e]);
-          if (t.master) t.master[i + e] = p[e];
-          if (!EIGHT) { static_cast<float*>(t.m)[i + e] = m[e]; static_cast<float*>(t.v)[i + e] = v[e]; }
-        }
-    }
-    if (EIGHT) {
-      uint32_t most_m = 0, most_v = 0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const uint32_t bm = __float_as_uint(m[e]) & 0x7fffffffu, bv = __float_as_uint(v[e]);
-        if (bm < NOT_FINITE) most_m = max(most_m, bm);
-        if (bv < NOT_FINITE) most_v = max(most_v, bv);                 // (v is never negative)
-      }
-      most_m = __reduce_max_sync(0xffffffffu, most_m);
-      most_v = __reduce_max_sync(0xffffffffu, most_v);
-      // The whole part of the largest one's logarithm, down by 7; of sqrt(v) half of v's.
-      const int em = (int)max(most_m >> 23, 8u) - 7, ev = (((int)max(most_v >> 23, 1u) - 127) >> 1) + 120;
-      const float inv_m = __uint_as_float((uint32_t)(254 - em) << 23), inv_v = __uint_as_float((uint32_t)(254 - ev) << 23);
-      uint32_t cm[E], cv[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const uint32_t bits = element_bits(key, i + e), bm = __float_as_uint(m[e]);
-        const uint32_t c = code_of(fabsf(m[e]) * inv_m, bits & 0xffff) | ((bm >> 24) & 0x80u), d = code_of(root[e] * inv_v, bits >> 16);
-        cm[e] = (bm & 0x7fffffffu) < NOT_FINITE ? c : CODE_NAN;
-        cv[e] = __float_as_uint(v[e]) < NOT_FINITE ? (v[e] > 0.f ? max(d, 1u) : 0u) : CODE_NAN;
-      }
-      if (left > 0 && lane == 0) {
-        t.m_scale[i / BLOCK] = __uint_as_float((uint32_t)em << 23);
-        t.v_scale[i / BLOCK] = __uint_as_float((uint32_t)ev << 23);
-      }
-      if (whole) {
-        const auto four = [](const uint32_t* c) { return c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24); };
-        __stcs(reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.m) + i), make_uint2(four(cm), four(cm + 4)));
-        __stcs(reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.v) + i), make_uint2(four(cv), four(cv + 4)));
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (e < left) { static_cast<uint8_t*>(t.m)[i + e] = (uint8_t)cm[e]; static_cast<uint8_t*>(t.v)[i + e] = (uint8_t)cv[e]; }
-      }
-    }
+    const long long i0 = (tile - t.first_tile) * TILE, most = i0 + TILE < t.count ? i0 + TILE : t.count;
+#pragma unroll 1
+    for (long long b = i0 + (threadIdx.x >> 5) * BLOCK; b < most; b += THREADS * E) step_block<PT, GT, EIGHT>(t, f, key, b);
   }
+}
+
+// f(tags of the parameters' and the gradients' type, of the states' kind): tensors are stepped by kind, a launch each.
+constexpr int KINDS = 18;
+inline int kind_of(int32_t p, int32_t g, bool eight) { return (eight * 3 + p) * 3 + g; }
+template <class F>
+void with_kind(int kind, F f) {
+  with_row_type(kind / 3 % 3, [&](auto pt) {
+    return with_row_type(kind % 3, [&](auto gt) {
+      if (kind >= 9) f(pt, gt, std::true_type()); else f(pt, gt, std::false_type());
+      return 0;
+    });
+  });
 }
 
 struct Interval { uintptr_t begin, end; };
@@ -256,9 +348,9 @@ struct Interval { uintptr_t begin, end; };
 struct taurus_adamw {
   int device = 0, sms = 0;
   Tensor* tensors = nullptr;                     // device memory, with the tiles' tensors behind them
-  int32_t* tile_tensor[2] = {nullptr, nullptr};  // by state: fp32, 8 bits
-  long long tiles[2] = {0, 0};
-  int resident[2] = {1, 1};                      // blocks of an SM
+  int32_t* tile_tensor[KINDS] = {};
+  long long tiles[KINDS] = {};
+  int resident[KINDS] = {};                      // blocks of an SM
   std::vector<Interval> written;                 // sorted
 };
 
@@ -273,7 +365,8 @@ bool touches(const std::vector<Interval>& v, const void* p, size_t bytes) {
 
 int adamw_create(taurus_adamw** out, const taurus_adamw_tensor* list, int64_t count) {
   std::vector<Tensor> tensors;
-  std::vector<int32_t> tiles[2];
+  std::vector<int32_t> tiles[KINDS];
+  long long all = 0;
   std::vector<Interval> written, read;
   tensors.reserve((size_t)count);
   for (int64_t k = 0; k < count; ++k) {
@@ -297,10 +390,11 @@ int adamw_create(taurus_adamw** out, const taurus_adamw_tensor* list, int64_t co
     t.p = c.param; t.g = c.grad; t.m = c.m; t.v = c.v; t.m_scale = c.m_scale; t.v_scale = c.v_scale; t.master = c.master; t.count = c.count;
     t.decay = c.weight_decay; t.p_type = c.param_type; t.g_type = c.grad_type; t.index = (uint32_t)k;
     t.vectors = rows_aligned(c.param, 16) && rows_aligned(c.grad, 16) && rows_aligned(c.m, eight ? 8 : 16) && rows_aligned(c.v, eight ? 8 : 16) && (!c.master || rows_aligned(c.master, 16));
-    std::vector<int32_t>& mine = tiles[eight];
+    std::vector<int32_t>& mine = tiles[kind_of(c.param_type, c.grad_type, eight)];
     t.first_tile = (long long)mine.size();
     const long long more = (c.count + TILE - 1) / TILE;
-    if ((long long)tiles[0].size() + (long long)tiles[1].size() + more > (1ll << 30)) return TAURUS_ERR_UNSUPPORTED;
+    all += more;
+    if (all > (1ll << 30)) return TAURUS_ERR_UNSUPPORTED;
     mine.insert(mine.end(), (size_t)more, (int32_t)tensors.size());
     tensors.push_back(t);
   }
@@ -316,23 +410,28 @@ int adamw_create(taurus_adamw** out, const taurus_adamw_tensor* list, int64_t co
   taurus_adamw* h = new taurus_adamw;
   h->device = dev; h->sms = sms;
   h->written.swap(written);
-  const size_t tb = (tensors.size() * sizeof(Tensor) + 255) / 256 * 256, b0 = (tiles[0].size() * 4 + 255) / 256 * 256, b1 = tiles[1].size() * 4;
+  const size_t tb = (tensors.size() * sizeof(Tensor) + 255) / 256 * 256;
   cudaError_t e = cudaSuccess;
   if (!tensors.empty()) {
     char* mem = nullptr;
-    e = cudaMalloc(reinterpret_cast<void**>(&mem), tb + b0 + b1);
+    e = cudaMalloc(reinterpret_cast<void**>(&mem), tb + (size_t)all * 4);
     if (e == cudaSuccess) {
       h->tensors = reinterpret_cast<Tensor*>(mem);
-      h->tile_tensor[0] = reinterpret_cast<int32_t*>(mem + tb);
-      h->tile_tensor[1] = reinterpret_cast<int32_t*>(mem + tb + b0);
       e = cudaMemcpy(h->tensors, tensors.data(), tensors.size() * sizeof(Tensor), cudaMemcpyHostToDevice);
     }
-    for (int k = 0; k < 2; ++k) {
+    int32_t* at = reinterpret_cast<int32_t*>(mem + tb);
+    for (int k = 0; k < KINDS && e == cudaSuccess; ++k) {
       h->tiles[k] = (long long)tiles[k].size();
-      if (e == cudaSuccess && h->tiles[k]) e = cudaMemcpy(h->tile_tensor[k], tiles[k].data(), tiles[k].size() * 4, cudaMemcpyHostToDevice);
+      if (!h->tiles[k]) continue;
+      h->tile_tensor[k] = at;
+      at += h->tiles[k];
+      e = cudaMemcpy(h->tile_tensor[k], tiles[k].data(), tiles[k].size() * 4, cudaMemcpyHostToDevice);
+      with_kind(k, [&](auto pt, auto gt, auto eight) {
+        using PT = typename decltype(pt)::type;
+        using GT = typename decltype(gt)::type;
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&h->resident[k], adamw_kernel<PT, GT, decltype(eight)::value>, THREADS, 0);
+      });
     }
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&h->resident[0], adamw_kernel<false>, THREADS, 0);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&h->resident[1], adamw_kernel<true>, THREADS, 0);
   }
   if (e != cudaSuccess) {
     taurus_note_cuda_error(e, "taurus_adamw_create");
@@ -373,15 +472,18 @@ extern "C" int taurus_adamw_step(taurus_adamw* h, const int64_t* step, const flo
   Launches enqueue = {static_cast<cudaStream_t>(cuda_stream)};
   Args a = {};
   a.tensors = h->tensors; a.step = reinterpret_cast<const long long*>(step); a.lr = lr; a.grad_scale = grad_scale;
-  a.beta1 = (float)beta1; a.rest1 = (float)(1.0 - beta1); a.beta2 = (float)beta2; a.rest2 = (float)(1.0 - beta2); a.eps = (float)eps;
+  a.beta1 = (float)beta1; a.rest1 = (float)(1.0 - beta1); a.beta2 = (float)beta2; a.rest2 = (float)(1.0 - beta2); a.eps = (float)eps; a.none = -0.f;
   a.log_beta1 = std::log(beta1); a.log_beta2 = std::log(beta2); a.seed = seed; a.status = status;
-  for (int k = 0; k < 2; ++k) {
+  for (int k = 0; k < KINDS; ++k) {
     if (!h->tiles[k]) continue;
     a.tile_tensor = h->tile_tensor[k]; a.tiles = h->tiles[k];
     const dim3 grid((unsigned)std::min<long long>(a.tiles, (long long)h->sms * std::max(h->resident[k], 1)));
     enqueue.early = false;                       // the kernels do not wait for one another: they touch different tensors, in stream order
-    if (k == 0) enqueue(adamw_kernel<false>, grid, THREADS, 0, a);
-    else enqueue(adamw_kernel<true>, grid, THREADS, 0, a);
+    with_kind(k, [&](auto pt, auto gt, auto eight) {
+      using PT = typename decltype(pt)::type;
+      using GT = typename decltype(gt)::type;
+      enqueue(adamw_kernel<PT, GT, decltype(eight)::value>, grid, THREADS, 0, a);
+    });
   }
   return enqueue.done("taurus_adamw_step");
 }

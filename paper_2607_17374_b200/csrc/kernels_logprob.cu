@@ -8,11 +8,11 @@
 // masked class (-inf, or a type's lowest value) then adds 0 to both sums, and no 0 x inf comes up.  A NaN goes into m, and with it into everything; +inf is treated as NaN.
 //
 // Bytes bound it: the logits in, once (and their gradient out).
-// Few classes: a thread to a row (rows_kernel).  A tile of rows comes into shared memory in 16-byte loads whatever the rows' width, each row on an odd number of words
-// (16-bit rows of odd width: of halves), so that the threads of a warp read a column without conflicts.  The top's candidates are few: values not below the k-th largest of some
-// maxima that the first pass over the row leaves.
-// Many classes: a warp or a block to a row, or to a part of one where there are few rows (stream_kernel), in one pass with a running maximum of the warp; parts are joined in their
-// order by join_kernel.  Candidates for the top are few (a value has to be above the k-th best so far): they go to a list of the warp in shared memory, sorted when it is half full.
+// Rows that fit the registers of 2, 8 or 32 lanes are read once and stay there, for the gradient too (team_kernel).  Wider ones are the work of a warp or a block, or of several
+// blocks where there are few rows (stream_kernel, join_kernel): every thread keeps a maximum and sums of its own over its vectors, without a branch, and they are joined at the end.
+// The term that is 1 stands in one thread's sum and has eaten that thread's small terms: its vectors are read again without it, by all threads.  The top needs no work in
+// the pass either: with the k-th largest of the threads' maxima known, the top k are in the vectors of the k threads whose maxima are not below it, and only those are looked
+// through again.
 #include <algorithm>
 
 #include "rows.cuh"
@@ -23,7 +23,7 @@ constexpr int MAX_TOP = TAURUS_MAX_TOP;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LEAST = -200.f;
 constexpr int ROW_THREADS = 128;               // threads and rows of a block of rows_kernel
-constexpr int WARPS = 8;                       // warps of a block of stream_kernel
+constexpr int WARPS = 8;                       // warps of a block of the others
 constexpr int LIST = 64;                       // places of a warp's list of candidates
 constexpr int MAX_PARTS = 64;                  // parts of a row
 
@@ -59,6 +59,24 @@ struct Args {
 
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+
+__device__ __forceinline__ float fma_sat(float a, float b, float c) { float r; asm("fma.rn.sat.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+__device__ __forceinline__ float mul_sat(float a, float b) { float r; asm("mul.rn.sat.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+// (m - x) / 256, at most 1, for m8 = m / 256: the cut that keeps infinities out, in the same instruction as the difference (minima, comparisons and selections go at half
+// the rate of multiplications).  Scaling by 2^-8 is exact.  Of two infinities: 0.
+constexpr float CUT = 256.f;
+__device__ __forceinline__ float below(float x, float m8) { return fma_sat(x, -1.f / CUT, m8); }
+__device__ __forceinline__ float exp_below(float z) { return ex2(z * (-CUT * LOG2E)); }
+// Sums over classes with the maximum known: s without the terms that equal it (weight 0; else 1), q of z e^-256z, others: how many are below.
+struct RowSums {
+  float s = 0.f, q = 0.f, others = 0.f;
+  __device__ __forceinline__ void add(float x, float m8) {
+    const float z = below(x, m8), e = exp_below(z), w = mul_sat(z, 0x1p126f);
+    s = fmaf(e, w, s);
+    q = fmaf(e, z, q);
+    others += w;
+  }
+};
 
 // Order of candidates: larger value first, of equal ones the lower class.  0: none (-inf, NaN).  -0 counts as 0.
 __device__ __forceinline__ u64 key_of(float x, int cls) {
@@ -118,32 +136,96 @@ __device__ __forceinline__ void write_top(const Args& a, long long row, int i, u
 
 // What the gradient of a row needs.
 struct GradRow {
-  float m, l, H, g, h, c;
+  float m8, l, H, g, h, c;                       // m8: the maximum / 256
   int label;
 };
 __device__ __forceinline__ GradRow grad_row(const Args& a, long long row, int label, const RowResult& r) {
   const float g = label >= 0 && a.grad_logprob ? a.grad_logprob[row] : 0.f, h = a.grad_entropy ? a.grad_entropy[row] : 0.f;
-  return {r.m, r.l, r.H, g, h, h == 0.f ? -g : fmaf(-h, r.H, -g), label};
+  if (r.m == -INFINITY) return {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, label};                        // all masked
+  return {r.m * (1.f / CUT), r.l, r.H, g, h, h == 0.f ? -g : fmaf(-h, r.H, -g), label};
 }
 __device__ __forceinline__ float grad_of(const GradRow& r, float x) {
-  const float lp = fmaxf(x - r.m, LEAST) - r.l, p = ex2(lp * LOG2E);
-  return x == -INFINITY ? 0.f : p * fmaf(-r.h, lp, r.c);
+  const float lp = fmaf(below(x, r.m8), -CUT, -r.l), p = ex2(lp * LOG2E);
+  return p * fmaf(-r.h, lp, r.c);                // (masked: p = 0)
 }
 __device__ __forceinline__ float grad_of_label(const GradRow& r, float x) {
-  const float lp = fmaxf(x - r.m, LEAST) - r.l, p = ex2(lp * LOG2E);
+  const float lp = fmaf(below(x, r.m8), -CUT, -r.l), p = ex2(lp * LOG2E);
   return x == -INFINITY ? 0.f : -r.g * expm1f(lp) - r.h * p * (lp + r.H);
 }
 
-// ---- few classes: a thread to a row ------------------------------------------------------------------------------------------------------------------
+// Pairs of fp32 values and their arithmetic in one instruction.
+struct F2 { u64 v; };
+__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void split(F2 x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x.v)); }
+__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+
+// ---- the top: candidates of a warp ---------------------------------------------------------------------------------------------------------------------
+
+// A warp's candidates: `count` keys in shared memory.  After a sort they are the k best so far; limit: the k-th best's key (0: fewer than k yet), above: its value.
+struct Candidates {
+  u64* list;
+  int count;
+  u64 limit;
+  float above;
+};
+// Keeps the best k, in order.
+__device__ __noinline__ void sort_candidates(Candidates& c, int k) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+  const int count = c.count;
+  const u64 a = lane < count ? c.list[lane] : 0, b = lane + 32 < count ? c.list[lane + 32] : 0;
+  int ra = 0, rb = 0;
+  for (int i = 0; i < count; ++i) { const u64 o = c.list[i]; ra += o > a; rb += o > b; }
+  __syncwarp();
+  if (a && ra < k) c.list[ra] = a;
+  if (b && rb < k) c.list[rb] = b;
+  __syncwarp();
+  c.count = min(k, count);
+  if (c.count == k) { c.limit = c.list[k - 1]; c.above = key_value(c.limit); }
+}
+// Puts down the lanes' keys that are better than the limit (0: none).
+__device__ __noinline__ void put_candidates(Candidates& c, u64 key, int k) {
+  const unsigned yes = __ballot_sync(0xffffffffu, key > c.limit);
+  if (!yes) return;
+  if (key > c.limit) c.list[c.count + __popc(yes & ((1u << (threadIdx.x & 31)) - 1))] = key;
+  c.count += __popc(yes);
+  if (c.count > LIST - 32) sort_candidates(c, k);
+}
+// The lane's place among the lanes' maxima.  The k-th largest has k values at least that are not below it: what is below it is not among the best k.
+__device__ __noinline__ int rank_of_lanes(float mine) {
+  const int lane = threadIdx.x & 31;
+  int rank = 0;
+#pragma unroll 8
+  for (int i = 0; i < 32; ++i) { const float o = __shfl_sync(0xffffffffu, mine, i); rank += o > mine || (o == mine && i < lane); }
+  return rank;
+}
+
+enum { FORWARD = 0, TRAIN = 1, GRAD = 2 };
+
+// What a lane loads at once: an element, or two where 16-bit rows have an even width.
+template <class T, bool PAIRS> struct Word { using type = T; static constexpr int n = 1; };
+template <class T> struct Word<T, true> { using type = uint32_t; static constexpr int n = 2; };
+template <class T>
+__device__ __forceinline__ void unpack(T w, float (&x)[1]) { x[0] = to_f32<T>(w); }
+template <class T>
+__device__ __forceinline__ void unpack(uint32_t w, float (&x)[2]) {
+  if constexpr (std::is_same_v<T, __nv_bfloat16>) { x[0] = __uint_as_float(w << 16); x[1] = __uint_as_float(w & 0xffff0000u); }
+  else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); x[0] = f.x; x[1] = f.y; }
+}
+template <class T>
+__device__ __forceinline__ T pack(const float (&x)[1]) { return from_f32<T>(x[0]); }
+template <class T>
+__device__ __forceinline__ uint32_t pack(const float (&x)[2]) {
+  if constexpr (std::is_same_v<T, __nv_bfloat16>) { const __nv_bfloat162 r = __floats2bfloat162_rn(x[0], x[1]); return *reinterpret_cast<const uint32_t*>(&r); }
+  else { const __half2 r = __floats2half2_rn(x[0], x[1]); return *reinterpret_cast<const uint32_t*>(&r); }
+}
+
+// ---- few classes: a thread to a row of a tile in shared memory ---------------------------------------------------------------------------------------
 
 // How a tile of rows lies in global memory: single elements | 16-byte vectors over rows without gaps | vectors within rows of a pitch.
 enum { TILE_ELEMENTS = 0, TILE_FLAT = 1, TILE_VECTORS = 2 };
-enum { FORWARD = 0, TRAIN = 1, GRAD = 2 };
-
-// Words of shared memory, one element each, or two where 16-bit rows have an even width.
-template <class T, bool PAIRS> struct Word { using type = T; static constexpr int n = 1; };
-template <class T> struct Word<T, true> { using type = uint32_t; static constexpr int n = 2; };
-
 // Brings a tile of `rows` rows of C words in and out.  P: words of a row in shared memory.
 template <class W>
 struct Tile {
@@ -239,28 +321,13 @@ struct Tile {
   }
 };
 
-template <class T>
-__device__ __forceinline__ void unpack(T w, float (&x)[1]) { x[0] = to_f32<T>(w); }
-template <class T>
-__device__ __forceinline__ void unpack(uint32_t w, float (&x)[2]) {
-  if constexpr (std::is_same_v<T, __nv_bfloat16>) { x[0] = __uint_as_float(w << 16); x[1] = __uint_as_float(w & 0xffff0000u); }
-  else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); x[0] = f.x; x[1] = f.y; }
-}
-template <class T>
-__device__ __forceinline__ T pack(const float (&x)[1]) { return from_f32<T>(x[0]); }
-template <class T>
-__device__ __forceinline__ uint32_t pack(const float (&x)[2]) {
-  Vec<T, 2> r;
-  r.v[0] = from_f32<T>(x[0]); r.v[1] = from_f32<T>(x[1]);
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
 
-// KMAX: places for the top in registers (k <= KMAX; 0: none asked for).
+// A thread to a row.  KMAX: places for the top in registers (k <= KMAX; 0: none asked for).
 template <class T, bool PAIRS, int MODE, int KMAX>
 __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
   extern __shared__ __align__(16) unsigned char logprob_shared[];
   using W = typename Word<T, PAIRS>::type;
-  constexpr int NW = Word<T, PAIRS>::n;
+  constexpr int NW = Word<T, PAIRS>::n, STEP = 8 / NW;
   W* const sm = reinterpret_cast<W*>(logprob_shared);
   const int C = a.C, CW = C / NW;
   const long long tiles = (a.n + ROW_THREADS - 1) / ROW_THREADS;
@@ -268,15 +335,15 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
     const long long row0 = tile * ROW_THREADS, row = row0 + threadIdx.x;
     const Tile<W> t = {(int)(a.n - row0 < ROW_THREADS ? a.n - row0 : ROW_THREADS), CW, a.pitch, a.vectors, a.by_C, a.by_vectors};
     t.load(sm, reinterpret_cast<const W*>(static_cast<const T*>(a.x) + row0 * a.ld), a.ld / NW, a.mode_in);
+    const int label = row < a.n ? label_of(a, row) : -1;
     __syncthreads();
     if (row < a.n) {
       W* const mine = sm + threadIdx.x * a.pitch;
       const T* const elements = reinterpret_cast<const T*>(mine);
-      const int label = label_of(a, row);
       RowResult r;
       if (MODE != GRAD) {
         // Maxima of G classes of classes: the k-th largest of them has k values at least that are not below it, so what is below it is not among the top k.
-        constexpr int G = KMAX == 0 ? 4 : KMAX <= 4 ? 8 : 32;
+        constexpr int G = KMAX <= 4 ? 8 : 32;
         float most[G];
 #pragma unroll
         for (int i = 0; i < G; ++i) most[i] = -INFINITY;
@@ -318,35 +385,42 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
 #pragma unroll
           for (int i = 0; i < KMAX; ++i) top[i] = -INFINITY;
         }
-        // The sums, of what is below the maximum; how often that comes up; the top's candidates, 32 classes at a time.
-        float s = 0.f, q = 0.f;
-        int same = 0;
-        constexpr int CHUNK = 32 / NW;
-        for (int j0 = 0; j0 < CW; j0 += CHUNK) {
-          uint32_t found = 0;
-          const auto one = [&](int i) {
-            float v[NW];
-            unpack<T>(mine[j0 + i], v);
+        // The sums, and the top's candidates, 64 classes at a time.
+        RowSums sum;
+        const float m8 = m * (1.f / CUT);
+        for (int j0 = 0; j0 < CW; j0 += 64 / NW) {
+          uint32_t found[2] = {0, 0};
 #pragma unroll
-            for (int e = 0; e < NW; ++e) {
-              const float d = fmaxf(v[e] - m, LEAST), p = ex2(d * LOG2E);
-              const bool is = v[e] == m;
-              same += is;
-              s += is ? 0.f : p;
-              q = fmaf(p, d, q);
-              if (KMAX && v[e] >= floor) found |= 1u << (i * NW + e);
+          for (int half = 0; half < 2; ++half)
+#pragma unroll 1
+            for (int i0 = 0; i0 < 32 / NW; i0 += STEP) {
+              const int j1 = j0 + half * (32 / NW) + i0;
+              if (j1 >= CW) break;
+              uint32_t bits = 0;
+              const auto one = [&](int i) {
+                float v[NW];
+                unpack<T>(mine[j1 + i], v);
+#pragma unroll
+                for (int e = 0; e < NW; ++e) {
+                  sum.add(v[e], m8);
+                  if (KMAX && v[e] >= floor) bits |= 1u << (i * NW + e);
+                }
+              };
+              if (j1 + STEP <= CW) {
+#pragma unroll
+                for (int i = 0; i < STEP; ++i) one(i);
+              } else {
+#pragma unroll
+                for (int i = 0; i < STEP; ++i) if (j1 + i < CW) one(i);
+              }
+              if (KMAX) found[half] |= bits << (i0 * NW);
             }
-          };
-          if (j0 + CHUNK <= CW) {
-#pragma unroll 8
-            for (int i = 0; i < CHUNK; ++i) one(i);
-          } else {
-            for (int i = 0; j0 + i < CW; ++i) one(i);
-          }
           if (KMAX)
-            while (found) {
-              const int b = __ffs(found) - 1, at = j0 * NW + b;
-              found &= found - 1;
+            while (found[0] | found[1]) {
+              const bool low = found[0] != 0;
+              const uint32_t bits = low ? found[0] : found[1];
+              const int at = j0 * NW + (low ? 0 : 32) + __ffs(bits) - 1;
+              if (low) found[0] = bits & (bits - 1); else found[1] = bits & (bits - 1);
               const float v = to_f32<T>(elements[at]);
               if (v > top[KMAX - 1]) {                     // equal ones keep their places: they have the lower classes
 #pragma unroll
@@ -359,7 +433,7 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
               }
             }
         }
-        r = row_result({m, s + (float)(same - 1), m == -INFINITY ? 0.f : q}, bad);
+        r = row_result({m, sum.s + ((float)(C - 1) - sum.others), -CUT * sum.q}, bad);
         if (a.logprob) a.logprob[row] = label < 0 ? 0.f : log_p(to_f32<T>(elements[label]), r);
         if (a.entropy) a.entropy[row] = r.H;
         if (a.stats) a.stats[row] = make_float2(r.m, r.l);
@@ -376,8 +450,21 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
       if (MODE != FORWARD) {
         const GradRow gr = grad_row(a, row, label, r);
         const float at = label >= 0 ? to_f32<T>(elements[label]) : 0.f;
-#pragma unroll 8
-        for (int j = 0; j < CW; ++j) {
+        int j = 0;
+        for (; j + STEP <= CW; j += STEP) {
+          W w[STEP];
+#pragma unroll
+          for (int i = 0; i < STEP; ++i) w[i] = mine[j + i];
+#pragma unroll
+          for (int i = 0; i < STEP; ++i) {
+            float v[NW];
+            unpack<T>(w[i], v);
+#pragma unroll
+            for (int e = 0; e < NW; ++e) v[e] = grad_of(gr, v[e]);
+            mine[j + i] = pack<T>(v);
+          }
+        }
+        for (; j < CW; ++j) {
           float v[NW];
           unpack<T>(mine[j], v);
 #pragma unroll
@@ -391,6 +478,135 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
     if (MODE != FORWARD) {
       t.store(sm, reinterpret_cast<W*>(static_cast<T*>(a.dx) + row0 * a.ld_dx), a.ld_dx / NW, a.mode_out);
       __syncthreads();
+    }
+  }
+}
+
+// ---- rows in the registers of a team of lanes ----------------------------------------------------------------------------------------------------------
+
+// A row is on LANES lanes with up to W words each: word i of lane l is word i LANES + l of the row.
+template <class T, bool PAIRS, int LANES, int W, int MODE>
+__global__ void __launch_bounds__(32 * WARPS) team_kernel(const Args a) {
+  using Wd = typename Word<T, PAIRS>::type;
+  constexpr int NW = Word<T, PAIRS>::n, TEAMS = 32 * WARPS / LANES;
+  __shared__ u64 lists[MODE == FORWARD && LANES == 32 ? WARPS * LIST : 1];
+  const int lane = threadIdx.x % LANES, CW = a.C / NW;
+  for (long long row0 = (long long)blockIdx.x * TEAMS; row0 < a.n; row0 += (long long)gridDim.x * TEAMS) {
+    const long long at = row0 + threadIdx.x / LANES;
+    const bool have = at < a.n;
+    const long long row = have ? at : a.n - 1;                       // a team without a row goes along with the last one
+    const Wd* const x = reinterpret_cast<const Wd*>(static_cast<const T*>(a.x) + row * a.ld) + lane;
+    float v[W][NW];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+#pragma unroll
+      for (int e = 0; e < NW; ++e) v[i][e] = -INFINITY;
+      if (i * LANES + lane < CW) unpack<T>(x[i * LANES], v[i]);
+    }
+    const int label = label_of(a, row);
+    RowResult r;
+    if (MODE != GRAD) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        if (i * LANES >= CW) continue;
+#pragma unroll
+        for (int e = 0; e < NW; ++e) m = max_nan(m, v[i][e]);
+      }
+      const float mine = m;
+#pragma unroll
+      for (int d = LANES / 2; d; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
+      RowSums sum;
+      const float m8 = m * (1.f / CUT);
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        if (i * LANES >= CW) continue;
+        if (i * LANES + lane < CW) {
+#pragma unroll
+          for (int e = 0; e < NW; ++e) sum.add(v[i][e], m8);
+        }
+      }
+#pragma unroll
+      for (int d = LANES / 2; d; d >>= 1) {
+        sum.s += __shfl_xor_sync(0xffffffffu, sum.s, d);
+        sum.q += __shfl_xor_sync(0xffffffffu, sum.q, d);
+        sum.others += __shfl_xor_sync(0xffffffffu, sum.others, d);
+      }
+      r = row_result({m, sum.s + ((float)(a.C - 1) - sum.others), -CUT * sum.q}, !(m < INFINITY));
+      if (lane == 0 && have) {
+        if (a.logprob) a.logprob[row] = label < 0 ? 0.f : log_p(to_f32<T>(static_cast<const T*>(a.x)[row * a.ld + label]), r);
+        if (a.entropy) a.entropy[row] = r.H;
+        if (a.stats) a.stats[row] = make_float2(r.m, r.l);
+      }
+      if (MODE == FORWARD && a.k > 0) {
+        if (LANES == 32) {
+          Candidates top = {lists + (threadIdx.x >> 5) * LIST, 0, 0, -INFINITY};
+          const float known = mine != mine ? -INFINITY : mine;
+          const int rank = rank_of_lanes(known);
+          const float floor = __shfl_sync(0xffffffffu, known, __ffs(__ballot_sync(0xffffffffu, rank == a.k - 1)) - 1);
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            if (i * LANES >= CW) continue;
+#pragma unroll
+            for (int e = 0; e < NW; ++e)
+              if (__any_sync(0xffffffffu, v[i][e] >= floor)) put_candidates(top, v[i][e] >= floor ? key_of(v[i][e], (i * LANES + lane) * NW + e) : 0, a.k);
+          }
+          sort_candidates(top, a.k);
+          if (lane < a.k && have) write_top(a, row, lane, lane < top.count ? top.list[lane] : 0, r);
+          __syncwarp();
+        } else {
+          // the team's best, k times
+          for (int t = 0; t < a.k; ++t) {
+            float best = -INFINITY;
+            int where = -1;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+              if (i * LANES >= CW) continue;
+#pragma unroll
+              for (int e = 0; e < NW; ++e) if (v[i][e] > best) { best = v[i][e]; where = i * NW + e; }
+            }
+            int cls = where < 0 ? 0x7fffffff : ((where / NW) * LANES + lane) * NW + where % NW;
+            const int own = cls;
+#pragma unroll
+            for (int d = LANES / 2; d; d >>= 1) {
+              const float o = __shfl_xor_sync(0xffffffffu, best, d);
+              const int oc = __shfl_xor_sync(0xffffffffu, cls, d);
+              if (o > best || (o == best && oc < cls)) { best = o; cls = oc; }
+            }
+            const bool none = cls == 0x7fffffff;
+            if (lane == 0 && have) {
+              if (a.top_logprob) a.top_logprob[row * a.k + t] = none ? -INFINITY : log_p(best, r);
+              if (a.top_class) a.top_class[row * a.k + t] = none ? -1 : cls;
+            }
+            if (own != cls) where = -1;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+              if (i * LANES >= CW) continue;
+#pragma unroll
+              for (int e = 0; e < NW; ++e) if (where == i * NW + e) v[i][e] = -INFINITY;
+            }
+          }
+        }
+      }
+    } else {
+      const float2 ml = a.stats_in[row];
+      r = {ml.x, ml.y, a.entropy_in ? a.entropy_in[row] : 0.f};
+    }
+    if (MODE != FORWARD) {
+      const GradRow gr = grad_row(a, row, label, r);
+      const bool special = have && label >= 0 && label / NW % LANES == lane;       // this lane has the label's word
+      const float at = special ? to_f32<T>(static_cast<const T*>(a.x)[row * a.ld + label]) : 0.f;
+      __syncwarp();                              // the label's logit has been read before its place is written
+      Wd* const dx = reinterpret_cast<Wd*>(static_cast<T*>(a.dx) + row * a.ld_dx) + lane;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        if (i * LANES >= CW) continue;
+        float y[NW];
+#pragma unroll
+        for (int e = 0; e < NW; ++e) y[e] = grad_of(gr, v[i][e]);
+        if (have && i * LANES + lane < CW) dx[i * LANES] = pack<T>(y);
+      }
+      if (special) static_cast<T*>(a.dx)[row * a.ld_dx + label] = from_f32<T>(grad_of_label(gr, at));
     }
   }
 }
@@ -431,251 +647,272 @@ __device__ __forceinline__ float vector_max(const Vec<__half, 8>& r) {
   return max_nan(__low2float(m), __high2float(m));
 }
 
-// A warp's candidates for the top: `count` keys in shared memory.  After a sort they are the k best so far; limit: the k-th best's key (0: fewer than k yet), above: its value.  Classes that
-// come later have to be larger than that.  atleast: the largest such value of the block's warps: what is below it is not among the best k of the row.
-struct Candidates {
-  u64* list;
-  int count;
-  u64 limit;
-  float above, atleast;
-};
-// Keeps the best k, in order.
-__device__ __noinline__ void sort_candidates(Candidates& c, int k, uint32_t* shared_limit) {
-  const int lane = threadIdx.x & 31;
-  __syncwarp();
-  const int count = c.count;
-  const u64 a = lane < count ? c.list[lane] : 0, b = lane + 32 < count ? c.list[lane + 32] : 0;
-  int ra = 0, rb = 0;
-  for (int i = 0; i < count; ++i) { const u64 o = c.list[i]; ra += o > a; rb += o > b; }
-  __syncwarp();
-  if (a && ra < k) c.list[ra] = a;
-  if (b && rb < k) c.list[rb] = b;
-  __syncwarp();
-  c.count = min(k, count);
-  if (c.count == k) {
-    c.limit = c.list[k - 1];
-    c.above = key_value(c.limit);
-    if (lane == 0) atomicMax(shared_limit, (uint32_t)(c.limit >> 32));
-  }
-}
-// Every element of a batch, 32 at a time: for the first batch, and for one that brings more candidates than the list takes.
-template <class T>
-__device__ __noinline__ void add_all(Candidates& c, const Span<T> span, int v0, int U, float most, int k, uint32_t* shared_limit) {
-  constexpr int V = Span<T>::V;
-  const int lane = threadIdx.x & 31;
-  // At least k of the lanes have a value that is not below the k-th largest of the lanes' maxima: what is below that is not among the best k.
-  float kth = most != most ? -INFINITY : most;
-  int rank = 0;
-#pragma unroll 1
-  for (int i = 0; i < 32; ++i) { const float o = __shfl_sync(0xffffffffu, kth, i); rank += o > kth || (o == kth && i < lane); }
-  kth = __shfl_sync(0xffffffffu, kth, __ffs(__ballot_sync(0xffffffffu, rank == k - 1)) - 1);
-  const float floor = fmaxf(kth, fmaxf(c.above, c.atleast));
-#pragma unroll 1
-  for (int u = 0; u < U; ++u) {
-    const int at = span.column(v0 + u * 32 + lane);
-#pragma unroll 1
-    for (int i = 0; i < V; ++i) {
-      u64 key = 0;
-      if (at + i >= span.begin && at + i < span.end) {
-        const float x = to_f32<T>(span.row[at + i]);
-        if (x >= floor) key = key_of(x, at + i);
-      }
-      const unsigned yes = __ballot_sync(0xffffffffu, key > c.limit);
-      if (yes) {
-        if (key > c.limit) c.list[c.count + __popc(yes & ((1u << lane) - 1))] = key;
-        c.count += __popc(yes);
-        if (c.count > LIST - 32) sort_candidates(c, k, shared_limit);
-      }
-    }
-  }
-  sort_candidates(c, k, shared_limit);
+// A vector's 16 bytes as pairs.
+template <class T, int V>
+__device__ __forceinline__ void to_pairs(const Vec<T, V>& r, F2 (&x)[V / 2]) {
+#pragma unroll
+  for (int i = 0; i < V; i += 2) x[i / 2] = f2(to_f32<T>(r.v[i]), to_f32<T>(r.v[i + 1]));
 }
 
+// The best k of a row of a warp by way of candidates, batch after batch: where more values than a list takes are as large as the k-th of the threads' maxima.
+template <class T>
+__device__ __noinline__ void stream_candidates(Candidates& c, const Span<T> span, int v0, int step, int k) {
+  constexpr int V = Span<T>::V;
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (; v0 < span.last(); v0 += step) {
+    const int v = v0 + lane, at = span.column(v);
+    float most = -INFINITY;
+    if (v < span.last()) most = vector_max(span.template load<LOAD_PLAIN>(v));
+    if (!__any_sync(0xffffffffu, !(most <= c.above))) continue;
+#pragma unroll 1
+    for (int i = 0; i < V; ++i)
+      put_candidates(c, v < span.last() && at + i >= span.begin && at + i < span.end ? key_of(to_f32<T>(span.row[at + i]), at + i) : 0, k);
+    sort_candidates(c, k);
+  }
+  sort_candidates(c, k);
+}
+
+// WPR warps to a row or a part of one.  Thread t has the vectors t, t + 32 WPR, ... of it.
 template <class T, bool TOP, int WPR, bool WITH_GRAD>
 __global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
-  constexpr int V = 16 / (int)sizeof(T), U = 4, STEP = 32 * U;
+  constexpr int V = 16 / (int)sizeof(T), U = 4, TEAM = 32 * WPR, PLACES = LIST * WPR, SHARES = WARPS / WPR;
   __shared__ u64 lists[TOP ? WARPS * LIST : 1];
-  __shared__ float4 warp_sums[WARPS];
-  __shared__ float4 shared_result;
-  __shared__ uint32_t shared_limit[WARPS];
+  __shared__ u64 best[TOP ? SHARES * MAX_TOP : 1];
+  __shared__ float warp_top[TOP ? WARPS * MAX_TOP : 1];
+  __shared__ float2 warp_sums[WARPS];
+  __shared__ float warp_max[WARPS], warp_rest[WARPS];
+  __shared__ int warp_same[WARPS], counts[SHARES], owners[SHARES];
+  __shared__ unsigned chosen[WARPS];
   early_start();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = WPR == 1 ? 0 : warp;
-  const long long units = a.n * a.parts, stride = WPR == 1 ? (long long)gridDim.x * WARPS : gridDim.x;
-  for (long long unit = WPR == 1 ? (long long)blockIdx.x * WARPS + warp : blockIdx.x; unit < units; unit += stride) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = warp / WPR, mine = threadIdx.x % TEAM, w0 = share * WPR;     // w0: the team's first warp
+  const auto sync = [&] {
+    if (WPR == 1) __syncwarp();
+    else if (WPR == WARPS) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(share + 1), "n"(TEAM) : "memory");
+  };
+  const long long units = a.n * a.parts, stride = (long long)gridDim.x * SHARES;
+  for (long long unit = (long long)blockIdx.x * SHARES + share; unit < units; unit += stride) {
     const long long row = a.parts == 1 ? unit : unit / a.parts;
     const int part = a.parts == 1 ? 0 : (int)(unit - row * a.parts);
     const T* const x = static_cast<const T*>(a.x) + row * a.ld;
     const int begin = part * a.part_len, end = a.C - begin < a.part_len ? a.C : begin + a.part_len;
     const Span<T> span(x, begin, end);
-    Sums sums = {-INFINITY, 0.f, 0.f};
-    bool bad = false;
-    Candidates top = {lists + (TOP ? warp * LIST : 0), 0, 0, -INFINITY, -INFINITY};
-    uint32_t* const limit = &shared_limit[WPR == 1 ? warp : 0];
-    if (TOP) {
-      if (WPR == 1 ? lane == 0 : threadIdx.x == 0) *limit = 0;
-      if (WPR == 1) __syncwarp(); else __syncthreads();
-    }
-    for (int v0 = span.first() + sub * STEP; v0 < span.last(); v0 += WPR * STEP) {
+    const int first = span.first(), last = span.last();
+    float m = -INFINITY;
+    F2 s2 = f2(0.f, 0.f), t2 = s2;
+    for (int v0 = first; v0 < last; v0 += U * TEAM) {
       Vec<T, V> raw[U];
+      if (v0 > first && v0 + U * TEAM < last) {                       // whole vectors
+        const T* const p = x + span.column(v0 + mine);
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = load_vec<Vec<T, V>, WITH_GRAD ? LOAD_PLAIN : LOAD_ONCE>(p + u * TEAM * V);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int v = v0 + u * TEAM + mine;
+          if (v < last) raw[u] = span.template load<LOAD_PLAIN>(v);
+          else
+#pragma unroll
+            for (int i = 0; i < V; ++i) raw[u].v[i] = from_f32<T>(-INFINITY);
+        }
+      }
+      float now = m;
+#pragma unroll
+      for (int u = 0; u < U; ++u) now = max_nan(now, vector_max(raw[u]));
+      const float d = fmaxf(m - now, LEAST), f = ex2(d * LOG2E);       // (nothing before: both sums are 0)
+      const F2 d2 = f2(d, d), g2 = f2(f, f), minus = f2(-now, -now), log2e = f2(LOG2E, LOG2E);
+      t2 = mul(fma(s2, d2, t2), g2);
+      s2 = mul(s2, g2);
+      m = now;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int at = v0 + u * 32 + lane;
-        if (at < span.last()) raw[u] = span.template load<WITH_GRAD ? LOAD_PLAIN : LOAD_ONCE>(at);
-        else
+        F2 v[V / 2];
+        to_pairs<T, V>(raw[u], v);
 #pragma unroll
-          for (int i = 0; i < V; ++i) raw[u].v[i] = from_f32<T>(-INFINITY);
-      }
-      float most = vector_max(raw[0]);
-#pragma unroll
-      for (int u = 1; u < U; ++u) most = max_nan(most, vector_max(raw[u]));
-      if (TOP) {
-        if (WPR > 1) {
-          const uint32_t o = *reinterpret_cast<volatile uint32_t*>(limit);
-          if (o) top.atleast = key_value((u64)o << 32);
-        }
-        // (not !(most <= ...): a NaN has its lane looked through)
-        if (__any_sync(0xffffffffu, !(most <= top.above) && !(most < top.atleast))) {
-          bool all = top.limit == 0;
-          if (!all) {
-            const int had = top.count;
-            int mine = 0;
-            if (!(most <= top.above) && !(most < top.atleast)) {
-#pragma unroll
-              for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < V; ++i) { const float x = to_f32<T>(raw[u].v[i]); mine += x > top.above && x >= top.atleast; }
-            }
-            int upto = mine;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(0xffffffffu, upto, d); if (lane >= d) upto += o; }
-            const int more = __shfl_sync(0xffffffffu, upto, 31);
-            all = had + more > LIST;
-            if (!all) {
-              if (mine) {
-                u64* to = top.list + had + upto - mine;
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                  for (int i = 0; i < V; ++i) {
-                    const float x = to_f32<T>(raw[u].v[i]);
-                    if (x > top.above && x >= top.atleast) *to++ = key_of(x, span.column(v0 + u * 32 + lane) + i);
-                  }
-              }
-              top.count = had + more;
-              if (top.count > LIST / 2) sort_candidates(top, a.k, limit);
-            }
-          }
-          if (all) add_all<T>(top, span, v0, U, most, a.k, limit);
+        for (int i = 0; i < V / 2; ++i) {
+          float p, q;
+          split(add(v[i], minus), &p, &q);
+          const F2 e = f2(fmaxf(p, LEAST), fmaxf(q, LEAST));
+          split(mul(e, log2e), &p, &q);
+          const F2 w = f2(ex2(p), ex2(q));
+          s2 = add(s2, w);
+          t2 = fma(w, e, t2);
         }
       }
-      if (__any_sync(0xffffffffu, !(most <= sums.m))) {
-        float w = most;
+    }
+    // The team's maximum, the first thread that has it, and the sums without that thread's.
+    float most = m, s, t, lo, hi;
 #pragma unroll
-        for (int d = 16; d; d >>= 1) w = max_nan(w, __shfl_xor_sync(0xffffffffu, w, d));
-        bad |= !(w < INFINITY);
-        if (w > sums.m) {
-          if (sums.m > -INFINITY) {
-            const float d = fmaxf(sums.m - w, LEAST), f = ex2(d * LOG2E), s1 = sums.s + (lane == 0 ? 1.f : 0.f);
-            sums.t = f * fmaf(s1, d, sums.t);
-            sums.s = f * s1;
-          }
-          sums.m = w;
-          if (lane == __ffs(__ballot_sync(0xffffffffu, most == w)) - 1) {        // this lane has the term that is 1
-            bool found = false;
+    for (int d = 16; d; d >>= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
+    if (WPR > 1) {
+      if (lane == 0) warp_max[warp] = most;
+      sync();
+      most = warp_max[w0];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+      for (int w = 1; w < WPR; ++w) most = max_nan(most, warp_max[w0 + w]);
+    }
+    const bool bad = !(most < INFINITY), none = most == -INFINITY;
+    split(s2, &lo, &hi); s = lo + hi;
+    split(t2, &lo, &hi); t = lo + hi;
+    const float d = fmaxf(m - most, LEAST), f = ex2(d * LOG2E);
+    t = f * fmaf(s, d, t);
+    s *= f;
+    const unsigned have = __ballot_sync(0xffffffffu, m == most);
+    int owner = __ffs(have) - 1;
+    if (WPR > 1) {
+      int w = 0;
+      while (w < WPR - 1 && warp_max[w0 + w] != most) ++w;
+      if (w0 + w == warp) { if (lane == owner) s = 0.f; if (lane == 0) owners[share] = owner; }
+      owner = w * 32;                            // its lane comes with the sums
+    } else if (lane == owner) s = 0.f;
 #pragma unroll
-              for (int i = 0; i < V; ++i) if (!found && to_f32<T>(raw[u].v[i]) == w) { raw[u].v[i] = from_f32<T>(-INFINITY); found = true; }
-          }
-        }
-      }
+    for (int k = 16; k; k >>= 1) { s += __shfl_xor_sync(0xffffffffu, s, k); t += __shfl_xor_sync(0xffffffffu, t, k); }
+    if (WPR > 1) {
+      if (lane == 0) warp_sums[warp] = make_float2(s, t);
+      sync();
+      s = t = 0.f;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int w = 0; w < WPR; ++w) { s += warp_sums[w0 + w].x; t += warp_sums[w0 + w].y; }
+      owner += owners[share];
+    }
+    // That thread's vectors again, by all, without what equals the maximum.
+    float rest = 0.f;
+    int same = 0;
+    if (!bad && !none) {
+      for (int v = first + owner + mine * TEAM; v < last; v += TEAM * TEAM) {
+        const Vec<T, V> r = span.template load<LOAD_PLAIN>(v);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const float d = fmaxf(to_f32<T>(raw[u].v[i]) - sums.m, LEAST), p = ex2(d * LOG2E);
-          sums.s += p;
-          sums.t = fmaf(p, d, sums.t);
+          const float y = to_f32<T>(r.v[i]);
+          if (y == most) ++same;
+          else rest += ex2(fmaxf(y - most, LEAST) * LOG2E);
         }
+      }
     }
 #pragma unroll
-    for (int d = 16; d; d >>= 1) {
-      sums.s += __shfl_xor_sync(0xffffffffu, sums.s, d);
-      sums.t += __shfl_xor_sync(0xffffffffu, sums.t, d);
+    for (int k = 16; k; k >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, k);
+    same = __reduce_add_sync(0xffffffffu, same);
+    if (WPR > 1) {
+      if (lane == 0) { warp_rest[warp] = rest; warp_same[warp] = same; }
+      sync();
+      rest = 0.f;
+      same = 0;
+#pragma unroll
+      for (int w = 0; w < WPR; ++w) { rest += warp_rest[w0 + w]; same += warp_same[w0 + w]; }
+    }
+    const Sums sums = {most, s + rest + (float)(same - 1), t};
+    const RowResult r = row_result(sums, bad);
+    const int label = a.parts == 1 ? label_of(a, row) : -1;
+    if (mine == 0) {
+      if (a.parts == 1) write_row<T>(a, row, label, r);
+      else a.part[unit] = none ? make_float4(-INFINITY, 0.f, 0.f, bad) : make_float4(sums.m, sums.s, sums.t, bad);
     }
     if (TOP) {
-      sort_candidates(top, a.k, limit);
-      if (lane >= top.count && lane < a.k) top.list[lane] = 0;
-    }
-    if (WPR > 1) {
-      if (lane == 0) warp_sums[warp] = make_float4(sums.m, sums.s, sums.t, bad ? 1.f : 0.f);
-      __syncthreads();
-      if (warp == 0) {
-        const float4 first = warp_sums[0];
-        sums = {first.x, first.y, first.z};
-        bad = first.w != 0.f;
-        for (int w = 1; w < WARPS; ++w) {
-          const float4 o = warp_sums[w];
-          join(sums, {o.x, o.y, o.z});
-          bad |= o.w != 0.f;
+      // The k-th largest of the threads' maxima.
+      const float known = m != m ? -INFINITY : m;
+      const int rank = rank_of_lanes(known);
+      if (rank < a.k) warp_top[warp * MAX_TOP + rank] = known;
+      if (mine == 0) counts[share] = 0;
+      sync();
+      float kth = warp_top[warp * MAX_TOP + a.k - 1];
+      if (WPR > 1) {
+        int head = 0;
+        for (int i = 0; i < a.k; ++i) {
+          const float h = lane < WPR && head < a.k ? warp_top[(w0 + lane) * MAX_TOP + head] : -INFINITY;
+          kth = h;
+#pragma unroll
+          for (int k = WPR / 2; k; k >>= 1) kth = fmaxf(kth, __shfl_xor_sync(0xffffffffu, kth, k));
+          kth = __shfl_sync(0xffffffffu, kth, 0);
+          const unsigned has = __ballot_sync(0xffffffffu, lane < WPR && head < a.k && h == kth);
+          if (lane == __ffs(has) - 1) ++head;
         }
       }
-    }
-    RowResult r = row_result(sums, bad);
-    const int label = a.parts == 1 ? label_of(a, row) : -1;
-    if (WPR == 1 || warp == 0) {
-      if (lane == 0) {
-        if (a.parts == 1) write_row<T>(a, row, label, r);
-        else a.part[unit] = make_float4(sums.m, sums.s, sums.t, bad ? 1.f : 0.f);
-        if (WPR > 1 && WITH_GRAD) shared_result = make_float4(r.m, r.l, r.H, 0.f);
+      const unsigned look = __ballot_sync(0xffffffffu, m != m || (m >= kth && m > -INFINITY));
+      if (WPR > 1) {
+        if (lane == 0) chosen[warp] = look;
+        sync();
       }
-      if (TOP) {
-        if (WPR == 1) {
-          __syncwarp();
-          if (lane < a.k) write_top(a, row, lane, top.list[lane], r);
-        } else {
+      u64* const list = lists + w0 * LIST;
+      for (int w = 0; w < WPR; ++w) {
+        unsigned todo = WPR > 1 ? chosen[w0 + w] : look;
+        while (todo) {
+          const int who = w * 32 + __ffs(todo) - 1;
+          todo &= todo - 1;
+          for (int v = first + who + mine * TEAM; v < last; v += TEAM * TEAM) {
+            const Vec<T, V> got = span.template load<LOAD_PLAIN>(v);
+            if (vector_max(got) < kth) continue;
+            for (int i = 0; i < V; ++i) {
+              const float y = to_f32<T>(got.v[i]);
+              if (y >= kth && y > -INFINITY) {
+                const int to = atomicAdd(&counts[share], 1);
+                if (to < PLACES) list[to] = key_of(y, span.column(v) + i);
+              }
+            }
+          }
+        }
+      }
+      sync();
+      const int count = counts[share];
+      u64* const out = best + share * MAX_TOP;
+      if (count <= PLACES) {
+        if (mine < MAX_TOP) out[mine] = 0;
+        sync();
+        for (int j = mine; j < count; j += TEAM) {
+          const u64 key = list[j];
+          int place = 0;
+          for (int i = 0; i < count; ++i) place += list[i] > key;
+          if (place < a.k) out[place] = key;
+        }
+        sync();
+      } else {
+        sync();
+        Candidates c = {lists + warp * LIST, 0, 0, -INFINITY};
+        stream_candidates<T>(c, span, first + (warp - w0) * 32, TEAM, a.k);
+        if (lane >= c.count && lane < a.k) c.list[lane] = 0;
+        sync();
+        if (warp == w0) {
           // the lists' heads, the best of them taken k times
           int head = 0;
-          u64 mine = lane < WARPS ? lists[lane * LIST] : 0, keep = 0;
+          u64 h = lane < WPR ? list[lane * LIST] : 0;
           for (int i = 0; i < a.k; ++i) {
-            const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32));
-            const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32) == hi ? (uint32_t)mine : 0u);
-            const u64 best = ((u64)hi << 32) | lo;
-            if (lane == i) keep = best;
-            if (best && mine == best) { ++head; mine = head < a.k ? lists[lane * LIST + head] : 0; }
-          }
-          if (lane < a.k) {
-            if (a.parts == 1) write_top(a, row, lane, keep, r);
-            else a.part_top[unit * a.k + lane] = keep;
+            const uint32_t up = __reduce_max_sync(0xffffffffu, (uint32_t)(h >> 32));
+            const uint32_t down = __reduce_max_sync(0xffffffffu, (uint32_t)(h >> 32) == up ? (uint32_t)h : 0u);
+            const u64 top = ((u64)up << 32) | down;
+            if (lane == 0) out[i] = top;
+            if (top && h == top) { ++head; h = head < a.k ? list[lane * LIST + head] : 0; }
           }
         }
+        sync();
+      }
+      if (mine < a.k) {
+        if (a.parts == 1) write_top(a, row, mine, out[mine], r);
+        else a.part_top[unit * a.k + mine] = out[mine];
       }
     }
     if (WITH_GRAD) {
-      __syncwarp();                             // the label's logit has been read before its place is written
-      if (WPR > 1) {
-        __syncthreads();
-        const float4 sr = shared_result;
-        r = {sr.x, sr.y, sr.z};
-      }
+      sync();                                    // the label's logit has been read before its place is written
       const GradRow gr = grad_row(a, row, label, r);
       T* const dx = static_cast<T*>(a.dx) + row * a.ld_dx;
       const bool alike = ((reinterpret_cast<uintptr_t>(dx) ^ reinterpret_cast<uintptr_t>(x)) & 15) == 0;
       // from the end, which the caches have had last
-      for (int v = span.last() - 1 - (WPR == 1 ? lane : (int)threadIdx.x); v >= span.first(); v -= 32 * WPR) {
+      for (int v = last - 1 - mine; v >= first; v -= TEAM) {
         const Vec<T, V> in = span.template load<LOAD_PLAIN>(v);
         const int c = span.column(v);
         Vec<T, V> out;
 #pragma unroll
-        for (int i = 0; i < V; ++i) out.v[i] = from_f32<T>(c + i == label ? grad_of_label(gr, to_f32<T>(in.v[i])) : grad_of(gr, to_f32<T>(in.v[i])));
+        for (int i = 0; i < V; ++i) out.v[i] = from_f32<T>(grad_of(gr, to_f32<T>(in.v[i])));
+        if (label >= c && label < c + V) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) if (c + i == label) out.v[i] = from_f32<T>(grad_of_label(gr, to_f32<T>(in.v[i])));
+        }
         if (alike && c >= 0 && c + V <= a.C) store_vec_once(dx + c, out);
         else
 #pragma unroll
           for (int i = 0; i < V; ++i) if (c + i >= 0 && c + i < a.C) dx[c + i] = out.v[i];
       }
     }
-    if (WPR > 1) __syncthreads();
-    else __syncwarp();
+    sync();
   }
 }
 
@@ -742,7 +979,11 @@ __global__ void __launch_bounds__(256) grad_kernel(const Args a, int chunks) {
       const int c = span.column(v);
       Vec<T, V> out;
 #pragma unroll
-      for (int i = 0; i < V; ++i) out.v[i] = from_f32<T>(c + i == gr.label ? grad_of_label(gr, to_f32<T>(in[u].v[i])) : grad_of(gr, to_f32<T>(in[u].v[i])));
+      for (int i = 0; i < V; ++i) out.v[i] = from_f32<T>(grad_of(gr, to_f32<T>(in[u].v[i])));
+      if (gr.label >= c && gr.label < c + V) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) if (c + i == gr.label) out.v[i] = from_f32<T>(grad_of_label(gr, to_f32<T>(in[u].v[i])));
+      }
       if (alike && c >= 0 && c + V <= a.C) store_vec_once(dx + c, out);
       else
 #pragma unroll
@@ -753,11 +994,18 @@ __global__ void __launch_bounds__(256) grad_kernel(const Args a, int chunks) {
 
 // ---- host --------------------------------------------------------------------------------------------------------------------------------------------
 
-constexpr int ROWS_BYTES = 512;                // widest row, in bytes, that a thread takes
-inline bool by_thread(int C, int ts) { return (int64_t)C * ts <= ROWS_BYTES; }
+// Rows that fit the registers of a warp: 32 elements a lane.  Pairs: 16-bit rows that begin at even elements everywhere.
+constexpr int TEAM_CLASSES = 1024;
+// Rows that a thread each takes: where there are enough of them, and a tile leaves room for other blocks beside it.
+constexpr int THREAD_ROWS = 4096, THREAD_BYTES = 512;
+inline bool by_thread(const Args& a, int ts) { return a.n >= THREAD_ROWS && a.C * ts <= THREAD_BYTES; }
+inline bool in_pairs(const Args& a, int ts, bool grad) {
+  const auto even = [](const void* p, long long ld) { return rows_aligned(p, 4) && ld % 2 == 0; };
+  return ts == 2 && a.C % 2 == 0 && even(a.x, a.ld) && (!grad || even(a.dx, a.ld_dx));
+}
 
 // How a row of many classes is split.  What does for n rows does for fewer: parts x n is largest for the fewest rows of a kind, so workspaces are counted for any n below.
-constexpr int ENOUGH_WARPS = 148 * 16, ENOUGH_BLOCKS = 148 * 4, PART_MIN = 8192;
+constexpr int ENOUGH_WARPS = 148 * 32, ENOUGH_BLOCKS = 148 * 4, PART_MIN = 8192;
 inline int parts_of(int64_t n, int C) {
   if (n >= ENOUGH_BLOCKS || C < 2 * PART_MIN) return 1;
   const int64_t want = (ENOUGH_BLOCKS + n - 1) / n, most = C / PART_MIN;
@@ -806,14 +1054,18 @@ void launch_tiles(Launches& enqueue, Args a) {
   const int64_t tiles = (a.n + ROW_THREADS - 1) / ROW_THREADS;
   enqueue(rows_kernel<T, PAIRS, MODE, KMAX>, dim3((unsigned)std::min<int64_t>(tiles, 1 << 30)), ROW_THREADS, smem, a);
 }
-template <class T, int MODE, int KMAX>
-void launch_rows(Launches& enqueue, const Args& a) {
-  // Pairs: rows of 16 bits that begin at even elements everywhere.
-  if constexpr (sizeof(T) == 2) {
-    const auto even = [](const void* p, long long ld) { return rows_aligned(p, 4) && ld % 2 == 0; };
-    if (a.C % 2 == 0 && even(a.x, a.ld) && (MODE == FORWARD || even(a.dx, a.ld_dx))) { launch_tiles<T, true, MODE, KMAX>(enqueue, a); return; }
-  }
-  launch_tiles<T, false, MODE, KMAX>(enqueue, a);
+template <class T, bool PAIRS, int MODE>
+void launch_team(Launches& enqueue, const Args& a) {
+  const int words = a.C / Word<T, PAIRS>::n;
+  const auto go = [&](auto lanes, auto w) {
+    constexpr int L = decltype(lanes)::value, W = decltype(w)::value, TEAMS = 32 * WARPS / L;
+    enqueue(team_kernel<T, PAIRS, L, W, MODE>, dim3((unsigned)std::min<int64_t>((a.n + TEAMS - 1) / TEAMS, 1 << 30)), 32 * WARPS, 0, a);
+  };
+  using std::integral_constant;
+  if (words <= 64) go(integral_constant<int, 8>(), integral_constant<int, 8>());
+  else if (words <= 128) go(integral_constant<int, 8>(), integral_constant<int, 16>());
+  else if (words <= 512) go(integral_constant<int, 32>(), integral_constant<int, 16>());
+  else if constexpr (!PAIRS) go(integral_constant<int, 32>(), integral_constant<int, 32>());
 }
 template <class T>
 void launch_grad(Launches& enqueue, const Args& a, int sms) {
@@ -821,12 +1073,18 @@ void launch_grad(Launches& enqueue, const Args& a, int sms) {
   const int chunks = ((a.C + 2 * V - 2) / V + GRAD_VECTORS * 32 - 1) / (GRAD_VECTORS * 32);     // vectors of a row wherever it begins
   enqueue(grad_kernel<T>, dim3((unsigned)std::min<int64_t>((a.n * chunks + 7) / 8, (int64_t)sms * 64)), 256, 0, a, chunks);
 }
+// The smallest team, of 1, 2, 4 or 8 warps, with which there are enough warps: what comes behind a row's pass is latency, and more rows at once hide it.
 template <class T, bool TOP, bool WITH_GRAD>
-void launch_stream(Launches& enqueue, const Args& a, int sms) {
-  if (a.parts == 1 && a.n >= ENOUGH_WARPS)
-    enqueue(stream_kernel<T, TOP, 1, WITH_GRAD>, dim3((unsigned)std::min<int64_t>((a.n + WARPS - 1) / WARPS, 1 << 30)), 32 * WARPS, 0, a);
-  else
-    enqueue(stream_kernel<T, TOP, WARPS, WITH_GRAD>, dim3((unsigned)std::min<int64_t>(a.n * a.parts, 1 << 30)), 32 * WARPS, 0, a);
+void launch_stream(Launches& enqueue, const Args& a) {
+  const auto go = [&](auto wpr) {
+    constexpr int WPR = decltype(wpr)::value, SHARES = WARPS / WPR;
+    enqueue(stream_kernel<T, TOP, WPR, WITH_GRAD>, dim3((unsigned)std::min<int64_t>((a.n * a.parts + SHARES - 1) / SHARES, 1 << 30)), 32 * WARPS, 0, a);
+  };
+  const int64_t rows = a.n * a.parts;
+  if (rows >= ENOUGH_WARPS) go(std::integral_constant<int, 1>());
+  else if (rows * 2 >= ENOUGH_WARPS) go(std::integral_constant<int, 2>());
+  else if (rows * 4 >= ENOUGH_WARPS) go(std::integral_constant<int, 4>());
+  else go(std::integral_constant<int, 8>());
 }
 
 enum { GIVEN_WEIGHTS = 1, GIVEN_STATS = 2 };
@@ -842,7 +1100,8 @@ int class_call(Args a, int32_t type, int what, int in_place_ok, void* workspace,
                          region_of(a.top_logprob, nb * a.k * 4), region_of(a.top_class, nb * a.k * 8), region_of(a.status, 4)};
   const Region ins[] = {in_place ? region_of(nullptr, 0) : region_of_rows(a.x, n, a.ld, a.C, ts), region_of(a.labels, nb * 8), region_of(a.grad_logprob, nb * 4),
                         region_of(a.grad_entropy, nb * 4), region_of(a.stats_in, nb * 8), region_of(a.entropy_in, nb * 4)};
-  a.parts = by_thread(a.C, ts) ? 1 : parts_of(n, a.C);
+  const bool pairs = in_pairs(a, ts, grad), team = a.C <= TEAM_CLASSES;
+  a.parts = team ? 1 : parts_of(n, a.C);
   const int64_t need = what != GIVEN_STATS && a.parts > 1 ? (int64_t)sp.bytes : 0;
   if (!regions_on_device(outs, dev) || !regions_on_device(ins, dev) || !regions_apart(outs, ins) || !workspace_ok(workspace, workspace_bytes, need, dev, outs, ins))
     return TAURUS_ERR_INVALID_ARG;
@@ -850,19 +1109,31 @@ int class_call(Args a, int32_t type, int what, int in_place_ok, void* workspace,
   Launches enqueue = {st};
   with_row_type(type, [&](auto tt) {
     using T = typename decltype(tt)::type;
-    if (by_thread(a.C, ts)) {
-      if (what == GIVEN_STATS) launch_rows<T, GRAD, 0>(enqueue, a);
-      else if (what == GIVEN_WEIGHTS) launch_rows<T, TRAIN, 0>(enqueue, a);
-      else if (a.k == 0) launch_rows<T, FORWARD, 0>(enqueue, a);
-      else if (a.k <= 4) launch_rows<T, FORWARD, 4>(enqueue, a);
-      else launch_rows<T, FORWARD, MAX_TOP>(enqueue, a);
+    if (team) {
+      const auto how = [&](auto mode, auto both) {
+        constexpr int MODE = decltype(mode)::value;
+        constexpr bool PAIRS = decltype(both)::value;
+        if (!by_thread(a, ts)) launch_team<T, PAIRS, MODE>(enqueue, a);
+        else if (MODE != FORWARD || a.k == 0) launch_tiles<T, PAIRS, MODE, 0>(enqueue, a);
+        else if constexpr (MODE == FORWARD) {
+          if (a.k <= 4) launch_tiles<T, PAIRS, MODE, 4>(enqueue, a);
+          else launch_tiles<T, PAIRS, MODE, MAX_TOP>(enqueue, a);
+        }
+      };
+      const auto with = [&](auto mode) {
+        if constexpr (sizeof(T) == 2) { if (pairs) { how(mode, std::true_type()); return; } }
+        how(mode, std::false_type());
+      };
+      if (what == GIVEN_STATS) with(std::integral_constant<int, GRAD>());
+      else if (what == GIVEN_WEIGHTS) with(std::integral_constant<int, TRAIN>());
+      else with(std::integral_constant<int, FORWARD>());
       return 0;
     }
     if (what == GIVEN_STATS) { launch_grad<T>(enqueue, a, sms); return 0; }
     if (a.parts == 1) {
-      if (what == GIVEN_WEIGHTS) launch_stream<T, false, true>(enqueue, a, sms);
-      else if (a.k) launch_stream<T, true, false>(enqueue, a, sms);
-      else launch_stream<T, false, false>(enqueue, a, sms);
+      if (what == GIVEN_WEIGHTS) launch_stream<T, false, true>(enqueue, a);
+      else if (a.k) launch_stream<T, true, false>(enqueue, a);
+      else launch_stream<T, false, false>(enqueue, a);
       return 0;
     }
     char* const ws = static_cast<char*>(workspace);
@@ -873,8 +1144,8 @@ int class_call(Args a, int32_t type, int what, int in_place_ok, void* workspace,
       if (!a.entropy) a.entropy = reinterpret_cast<float*>(ws + sp.entropy);
       a.stats_in = a.stats; a.entropy_in = a.entropy;
     }
-    if (a.k) launch_stream<T, true, false>(enqueue, a, sms);
-    else launch_stream<T, false, false>(enqueue, a, sms);
+    if (a.k) launch_stream<T, true, false>(enqueue, a);
+    else launch_stream<T, false, false>(enqueue, a);
     enqueue(join_kernel<T>, dim3((unsigned)std::min<int64_t>((n + 3) / 4, 1 << 20)), 128, 0, a);
     if (grad) launch_grad<T>(enqueue, a, sms);
     return 0;

@@ -45,7 +45,7 @@ struct Args {
   const long long* step;
   const float *lr, *grad_scale;
   float beta1, rest1, beta2, rest2, eps;
-  float none;                                    // -0, as a number that the compiler does not know: a product and -0 is the rounded product, which no later sum takes in unrounded
+  int small_eps;                                 // beside a larger one the root of a subnormal number, 1e-19, is nothing
   double log_beta1, log_beta2;
   unsigned long long seed;
   int32_t* status;
@@ -64,38 +64,30 @@ __device__ __forceinline__ uint32_t finish_bits(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-// Two fp32 values in one register pair, and their arithmetic in one instruction.
-struct F2 { unsigned long long v; };
-__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ F2 f2(float a) { return f2(a, a); }
-__device__ __forceinline__ float lo(F2 x) { float a, b; asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); return a; }
-__device__ __forceinline__ float hi(F2 x) { float a, b; asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); return b; }
-__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
-__device__ __forceinline__ float root_of(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+// The root of a subnormal number is 0 with the one, its own with the other, which takes four instructions.
+__device__ __forceinline__ float root_of(float x) { float r; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float any_root_of(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float reciprocal(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 
 template <class T>
-__device__ __forceinline__ void to_pairs(const Vec<T, E>& r, F2 (&x)[E / 2]) {
+__device__ __forceinline__ void to_floats(const Vec<T, E>& r, float (&x)[E]) {
 #pragma unroll
-  for (int e = 0; e < E; e += 2) x[e / 2] = f2(to_f32<T>(r.v[e]), to_f32<T>(r.v[e + 1]));
+  for (int e = 0; e < E; ++e) x[e] = to_f32<T>(r.v[e]);
 }
-__device__ __forceinline__ void codes_to_pairs(uint2 c, F2 scale, F2 (&x)[E / 2]) {
+__device__ __forceinline__ void codes_to_floats(uint2 c, float scale, float (&x)[E]) {
   const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
   for (int e = 0; e < E; e += 2) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[e / 4] >> (8 * (e & 2))), __NV_E4M3);
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    x[e / 2] = mul(f2(f.x, f.y), scale);
+    x[e] = f.x * scale; x[e + 1] = f.y * scale;
   }
 }
-__device__ __forceinline__ float mul_down(float a, float b) { float r; asm("mul.rz.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 constexpr uint32_t NOT_FINITE = 0x7f800000u, CODE_NAN = 0x7f;
 
-// What a step multiplies and adds with.
-struct Factors { F2 beta1, rest1, beta2, rest2, none, gs, c2, eps, rate, keep; };
+// What a step multiplies with, besides the arguments: the gradients' scale, 1 / sqrt(1 - b2^t), -lr / (1 - b1^t), 1 - lr wd.
+struct Factors { float gs, c2, rate, keep; };
 
 // Which elements of a warp's 256 a lane has: 8 in a row where they are 16 bytes at most; else four and four, so that the warp's loads of 16 bytes touch every sector once (8 fp32
 // values in a row would be two loads of half of each).
@@ -117,10 +109,7 @@ struct Places {
     return r;
   }
   template <class T>
-  static __device__ __forceinline__ void store(T* p, int lane, const F2 (&x)[E / 2]) {
-    float v[E];
-#pragma unroll
-    for (int e = 0; e < E; e += 2) { v[e] = lo(x[e / 2]); v[e + 1] = hi(x[e / 2]); }
+  static __device__ __forceinline__ void store(T* p, int lane, const float (&v)[E]) {
     if (!WIDE) { store_f32_once<T, E>(p + lane * E, v); return; }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -139,19 +128,18 @@ struct Places {
   }
 };
 
-// A warp's 256 elements of a tensor, from b on.
-template <class PT, class GT, bool EIGHT>
-__device__ __forceinline__ void step_block(const Tensor& t, const Factors& f, unsigned long long key, long long b) {
+// A warp's 256 elements of a tensor, from b on.  whole: all 256 are there, in arrays that allow vectors.
+template <class PT, class GT, bool EIGHT, bool whole>
+__device__ __forceinline__ void step_block(const Args& a, const Tensor& t, const Factors f, unsigned long long key, long long b) {
   using P = Places<!EIGHT || sizeof(PT) == 4 || sizeof(GT) == 4>;
   const int lane = threadIdx.x & 31, first = P::lane_place(lane);
   const int left = (int)(t.count - b < BLOCK ? t.count - b : BLOCK);    // 1 at least
-  const bool whole = t.vectors && left == BLOCK;
   const auto in = [&](int e) { return first + P::element(e) < left; };
   PT* const pp = static_cast<PT*>(t.p) + b;
   const GT* const gp = static_cast<const GT*>(t.g) + b;
   uint8_t *const mc = static_cast<uint8_t*>(t.m) + b, *const vc = static_cast<uint8_t*>(t.v) + b;
   float *const mf = static_cast<float*>(t.m) + b, *const vf = static_cast<float*>(t.v) + b;
-  F2 p[E / 2], g[E / 2], m[E / 2], v[E / 2];
+  float p[E], g[E], m[E], v[E];
   if (whole) {
     // all on their way before the first is used
     const auto rg = P::template load<GT>(gp, lane);
@@ -168,49 +156,44 @@ __device__ __forceinline__ void step_block(const Tensor& t, const Factors& f, un
     if (sizeof(PT) == 2 && t.master) rw = P::template load<float>(t.master + b, lane);
     else rp = P::template load<PT>(pp, lane);
     if (EIGHT) {
-      codes_to_pairs(cm, f2(ms), m);
-      codes_to_pairs(cv, f2(vs), v);
+      codes_to_floats(cm, ms, m);
+      codes_to_floats(cv, vs, v);
     } else {
-      to_pairs<float>(rm, m);
-      to_pairs<float>(rv, v);
+      to_floats<float>(rm, m);
+      to_floats<float>(rv, v);
     }
-    if (sizeof(PT) == 2 && t.master) to_pairs<float>(rw, p);
-    else to_pairs<PT>(rp, p);
-    to_pairs<GT>(rg, g);
+    if (sizeof(PT) == 2 && t.master) to_floats<float>(rw, p);
+    else to_floats<PT>(rp, p);
+    to_floats<GT>(rg, g);
   } else {
-    float x[E] = {}, y[E] = {}, c[E] = {}, d[E] = {};
     uint2 cm = make_uint2(0, 0), cv = make_uint2(0, 0);
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int e = 0; e < E; ++e) {
+      p[e] = g[e] = m[e] = v[e] = 0.f;
       if (in(e)) {
         const int at = first + P::element(e);
-        x[e] = sizeof(PT) == 2 && t.master ? t.master[b + at] : to_f32<PT>(pp[at]);
-        y[e] = to_f32<GT>(gp[at]);
+        p[e] = sizeof(PT) == 2 && t.master ? t.master[b + at] : to_f32<PT>(pp[at]);
+        g[e] = to_f32<GT>(gp[at]);
         if (EIGHT) {
           (e < 4 ? cm.x : cm.y) |= (uint32_t)mc[at] << (8 * (e & 3));
           (e < 4 ? cv.x : cv.y) |= (uint32_t)vc[at] << (8 * (e & 3));
-        } else { c[e] = mf[at]; d[e] = vf[at]; }
+        } else { m[e] = mf[at]; v[e] = vf[at]; }
       }
-#pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      p[e / 2] = f2(x[e], x[e + 1]); g[e / 2] = f2(y[e], y[e + 1]);
-      if (!EIGHT) { m[e / 2] = f2(c[e], c[e + 1]); v[e / 2] = f2(d[e], d[e + 1]); }
     }
     if (EIGHT) {
-      codes_to_pairs(cm, f2(t.m_scale[b / BLOCK]), m);
-      codes_to_pairs(cv, f2(t.v_scale[b / BLOCK]), v);
+      codes_to_floats(cm, t.m_scale[b / BLOCK], m);
+      codes_to_floats(cv, t.v_scale[b / BLOCK], v);
     }
   }
   float root[E];
 #pragma unroll
-  for (int k = 0; k < E / 2; ++k) {
-    const F2 ge = mul(g[k], f.gs);
-    m[k] = add(fma(f.beta1, m[k], f.none), fma(f.rest1, ge, f.none));
-    if (EIGHT) v[k] = mul(v[k], v[k]);
-    v[k] = add(fma(f.beta2, v[k], f.none), fma(mul(f.rest2, ge), ge, f.none));
-    root[2 * k] = root_of(lo(v[k])); root[2 * k + 1] = root_of(hi(v[k]));
-    const F2 below = fma(f2(root[2 * k], root[2 * k + 1]), f.c2, f.eps);
-    p[k] = fma(mul(m[k], f.rate), f2(reciprocal(lo(below)), reciprocal(hi(below))), mul(p[k], f.keep));
+  for (int e = 0; e < E; ++e) {
+    const float ge = g[e] * f.gs;
+    m[e] = __fadd_rn(__fmul_rn(a.beta1, m[e]), __fmul_rn(a.rest1, ge));
+    if (EIGHT) v[e] = __fmul_rn(v[e], v[e]);
+    v[e] = __fadd_rn(__fmul_rn(a.beta2, v[e]), __fmul_rn(__fmul_rn(a.rest2, ge), ge));
+    root[e] = a.small_eps ? any_root_of(v[e]) : root_of(v[e]);
+    p[e] = fmaf(m[e] * f.rate, reciprocal(fmaf(root[e], f.c2, a.eps)), p[e] * f.keep);
   }
   if (whole) {
     P::template store<PT>(pp, lane, p);
@@ -224,21 +207,17 @@ __device__ __forceinline__ void step_block(const Tensor& t, const Factors& f, un
     for (int e = 0; e < E; ++e)
       if (in(e)) {
         const int at = first + P::element(e);
-        const float x = e & 1 ? hi(p[e / 2]) : lo(p[e / 2]);
-        pp[at] = from_f32<PT>(x);
-        if (sizeof(PT) == 2 && t.master) t.master[b + at] = x;
-        if (!EIGHT) {
-          mf[at] = e & 1 ? hi(m[e / 2]) : lo(m[e / 2]);
-          vf[at] = e & 1 ? hi(v[e / 2]) : lo(v[e / 2]);
-        }
+        pp[at] = from_f32<PT>(p[e]);
+        if (sizeof(PT) == 2 && t.master) t.master[b + at] = p[e];
+        if (!EIGHT) { mf[at] = m[e]; vf[at] = v[e]; }
       }
   }
   if (EIGHT) {
     float mm = 0.f, mv = 0.f;
 #pragma unroll
-    for (int k = 0; k < E / 2; ++k) {
-      mm = max_nan(max_nan(mm, fabsf(lo(m[k]))), fabsf(hi(m[k])));
-      mv = max_nan(max_nan(mv, lo(v[k])), hi(v[k]));
+    for (int e = 0; e < E; e += 2) {
+      mm = max_nan(mm, fabsf(m[e]), fabsf(m[e + 1]));
+      mv = max_nan(mv, v[e], v[e + 1]);
     }
     uint32_t most_m = __reduce_max_sync(0xffffffffu, __float_as_uint(mm) & 0x7fffffffu), most_v = __reduce_max_sync(0xffffffffu, __float_as_uint(mv) & 0x7fffffffu);
     const bool odd = most_m >= NOT_FINITE || most_v >= NOT_FINITE;      // somewhere in the block: scales by what is finite
@@ -246,7 +225,7 @@ __device__ __forceinline__ void step_block(const Tensor& t, const Factors& f, un
       uint32_t am = 0, av = 0;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const uint32_t bm = __float_as_uint(e & 1 ? hi(m[e / 2]) : lo(m[e / 2])) & 0x7fffffffu, bv = __float_as_uint(e & 1 ? hi(v[e / 2]) : lo(v[e / 2])) & 0x7fffffffu;
+        const uint32_t bm = __float_as_uint(m[e]) & 0x7fffffffu, bv = __float_as_uint(v[e]) & 0x7fffffffu;
         if (bm < NOT_FINITE) am = max(am, bm);
         if (bv < NOT_FINITE) av = max(av, bv);
       }
@@ -257,26 +236,27 @@ __device__ __forceinline__ void step_block(const Tensor& t, const Factors& f, un
     const int em = (int)max(most_m >> 23, 8u) - 7, ev = (((int)max(most_v >> 23, 1u) - 127) >> 1) + 120;
     // Codes.  x / scale 2^-120 has e4m3's exponent, 7 above its own, where fp32 has its exponent's last four bits, and below e4m3's smallest exponent it is a subnormal
     // number of fp32 (rounded down at 2^-149, 20 places below the last that stays): its bits 20 to 26 are the code, whatever its size, once the 16 random bits are added below
-    // them.  Four places further up a code is a byte.  The factor is applied in two parts: one may be too small for fp32.
+    // them.  Four places further up a code is a byte, and the sign is gone.  The factor is applied in two parts: one may be too small for fp32.
+    if (most_v < (35u << 23) && !a.small_eps) {                       // all below 2^-92: roots of subnormal numbers count too (in other blocks they are below code 1)
+#pragma unroll
+      for (int e = 0; e < E; ++e) root[e] = any_root_of(v[e]);
+    }
     const float part_m = __int_as_float(em < 234 ? (234 - em) << 23 : 1 << (256 - em)), part_v = __int_as_float((234 - ev) << 23);      // 2^(107 - e)
     const uint32_t base = (uint32_t)b ^ (uint32_t)key ^ (uint32_t)P::lane_place(lane), more = (uint32_t)(key >> 32) + (uint32_t)(b >> 32) * 0x85EBCA6Bu;     // (places differ in bits of their own)
     uint32_t cm[E], cv[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const float me = e & 1 ? hi(m[e / 2]) : lo(m[e / 2]);
+      const float zm = __fmul_rz(m[e] * part_m, 0x1p-100f), zv = __fmul_rz(root[e] * part_v, 0x1p-100f);
+      const float least = fminf(v[e] * 0x1p100f, __uint_as_float(1u << 20));                          // code 1 where v is not 0
       const uint32_t bits = finish_bits((base ^ (uint32_t)P::element(e)) + more);
-      const float zm = mul_down(fabsf(me) * part_m, 0x1p-100f);
-      const float least = fminf(root[e] * 0x1p60f, __uint_as_float(1u << 20));                    // code 1 where the root is not 0
-      const float zv = fmaxf(mul_down(root[e] * part_v, 0x1p-100f), least);
-      cm[e] = ((__float_as_uint(zm) << 4) + __byte_perm(bits, 0, 0x4104)) | (__float_as_uint(me) & 0x80000000u);
-      cv[e] = (__float_as_uint(zv) << 4) + __byte_perm(bits, 0, 0x4324);
+      cm[e] = ((__float_as_uint(zm) << 4) + __byte_perm(bits, 0, 0x4104)) | (__float_as_uint(m[e]) & 0x80000000u);
+      cv[e] = (__float_as_uint(fmaxf(zv, least)) << 4) + __byte_perm(bits, 0, 0x4324);
     }
     if (odd) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float me = e & 1 ? hi(m[e / 2]) : lo(m[e / 2]);
-        if (!(fabsf(me) < INFINITY)) cm[e] = CODE_NAN << 24;
-        if (!(root[e] < INFINITY)) cv[e] = CODE_NAN << 24;
+        if (!(fabsf(m[e]) < INFINITY)) cm[e] = CODE_NAN << 24;
+        if (!(v[e] < INFINITY)) cv[e] = CODE_NAN << 24;
       }
     }
     const auto four = [](const uint32_t* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410); };
@@ -296,7 +276,10 @@ __device__ __forceinline__ void step_block(const Tensor& t, const Factors& f, un
 }
 
 template <class PT, class GT, bool EIGHT>
-__global__ void __launch_bounds__(THREADS) adamw_kernel(const Args a) {
+__device__ __noinline__ void step_block_by_element(const Args& a, const Tensor& t, const Factors f, unsigned long long key, long long b) { step_block<PT, GT, EIGHT, false>(a, t, f, key, b); }
+
+template <class PT, class GT, bool EIGHT>
+__global__ void __launch_bounds__(THREADS, 3) adamw_kernel(const __grid_constant__ Args a) {
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const long long step = *a.step;
   if (step < 1) {
@@ -307,7 +290,7 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const Args a) {
   const float lr = *a.lr;
   // 1 - b^t = -(e^(t ln b) - 1)
   const float c1 = -1.f / expm1f((float)((double)step * a.log_beta1)), c2 = rsqrtf(-expm1f((float)((double)step * a.log_beta2)));
-  Factors f = {f2(a.beta1), f2(a.rest1), f2(a.beta2), f2(a.rest2), f2(a.none), f2(gs), f2(c2), f2(a.eps), f2(-lr * c1), f2(1.f)};
+  Factors f = {gs, c2, -lr * c1, 1.f};
   unsigned long long seed_key = 0, key = 0;
   if (EIGHT) seed_key = absorb(absorb(0x243F6A8885A308D3ull, a.seed), (unsigned long long)step);
   int known = -1;
@@ -319,12 +302,15 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const Args a) {
       if (threadIdx.x < sizeof(Tensor) / 4) reinterpret_cast<uint32_t*>(&t)[threadIdx.x] = reinterpret_cast<const uint32_t*>(a.tensors + which)[threadIdx.x];
       __syncthreads();
       known = which;
-      f.keep = f2(fmaf(-lr, t.decay, 1.f));
+      f.keep = fmaf(-lr, t.decay, 1.f);
       if (EIGHT) key = absorb(seed_key, t.index);
     }
     const long long i0 = (tile - t.first_tile) * TILE, most = i0 + TILE < t.count ? i0 + TILE : t.count;
 #pragma unroll 1
-    for (long long b = i0 + (threadIdx.x >> 5) * BLOCK; b < most; b += THREADS * E) step_block<PT, GT, EIGHT>(t, f, key, b);
+    for (long long b = i0 + (threadIdx.x >> 5) * BLOCK; b < most; b += THREADS * E) {
+      if (t.vectors && b + BLOCK <= most) step_block<PT, GT, EIGHT, true>(a, t, f, key, b);
+      else step_block_by_element<PT, GT, EIGHT>(a, t, f, key, b);
+    }
   }
 }
 
@@ -472,7 +458,7 @@ extern "C" int taurus_adamw_step(taurus_adamw* h, const int64_t* step, const flo
   Launches enqueue = {static_cast<cudaStream_t>(cuda_stream)};
   Args a = {};
   a.tensors = h->tensors; a.step = reinterpret_cast<const long long*>(step); a.lr = lr; a.grad_scale = grad_scale;
-  a.beta1 = (float)beta1; a.rest1 = (float)(1.0 - beta1); a.beta2 = (float)beta2; a.rest2 = (float)(1.0 - beta2); a.eps = (float)eps; a.none = -0.f;
+  a.beta1 = (float)beta1; a.rest1 = (float)(1.0 - beta1); a.beta2 = (float)beta2; a.rest2 = (float)(1.0 - beta2); a.eps = (float)eps; a.small_eps = eps < 1e-11;
   a.log_beta1 = std::log(beta1); a.log_beta2 = std::log(beta2); a.seed = seed; a.status = status;
   for (int k = 0; k < KINDS; ++k) {
     if (!h->tiles[k]) continue;

@@ -1047,7 +1047,7 @@ template <class T, bool PAIRS, int MODE, int KMAX>
 void launch_tiles(Launches& enqueue, Args a) {
   set_tile<T, PAIRS>(&a);
   const size_t smem = (size_t)a.pitch * sizeof(T) * (PAIRS ? 2 : 1) * ROW_THREADS;
-  if (smem > 48 * 1024) {
+  if (smem > 40 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(rows_kernel<T, PAIRS, MODE, KMAX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) { enqueue.error = e; return; }
   }

@@ -5,10 +5,12 @@
 //   dgamma = sum dy h2,  dbeta = sum dy         h: normalised rows,  N'(d) = rstd (d - mean(d) - h mean(d h)), without the first mean for RMS
 //
 // Bytes bound it: r and b in, r' and y out; r, b, dr', dy in, dr and db out.  A row is the work of a team of 1 to 128 neighbouring threads with 8 elements each, which
-// stay in registers from the load to the store: statistics first the mean, then the squares of deviations.  A team takes neighbouring rows, so that the group of a row (the last one whose
-// offset is not above it) is looked for once a group, and reads the next row before it sums up the one that it has.
-// Sums by channel of the gradient stay in the threads' registers (a thread keeps its columns), are joined by block in shared memory, then by resnorm_join_kernel in the blocks' order.
-// Sums by group: a group inside a team's rows is written at once; one that reaches over leaves a part in each team, "first" where it began before, "last" where it
+// stay in registers from the load to the store: statistics first the mean, then the squares of deviations.  A team walks over neighbouring rows, so that the group of a row (the last one whose
+// offset is not above it) is looked for once a group.  Rows are on their way some rows ahead, by asynchronous copies into places of shared memory that are a thread's own: a thread
+// waits for its own copies and for nobody.
+// Sums by channel stay in the threads' registers (a thread keeps its columns).  Those of post_gamma and of the gate come from one: with S_g = sum over the group's rows of D h1,
+// dgate_g = alpha post_gamma S_g and dpost_gamma = sum_g alpha gate_g S_g.  Blocks join theirs in shared memory, resnorm_join_kernel the blocks' in their order.
+// A group inside a team's rows has its sums written at once; one that reaches over leaves a part in each team, "first" where it began before, "last" where it
 // begins there and goes on; the join kernel adds them up in the teams' order.
 #include <algorithm>
 
@@ -81,8 +83,11 @@ __device__ __forceinline__ void check_offsets(const Args& a) {
   }
 }
 
+// Teams smaller than a warp, of a warp, of several warps.
+enum { PART = 0, WARP = 1, MULTI = 2 };
+
 // A thread's place in its team and the columns that it keeps: vectors lane, lane + size, ... of V elements.
-template <int V, bool MULTI>
+template <int V, int KIND>
 struct Team {
   static constexpr int NV = N / V;
   int size, lane, warps, id;                     // id: of the block's teams
@@ -92,7 +97,8 @@ struct Team {
   int flip = 0;
   __device__ __forceinline__ explicit Team(const Args& a) {
     __shared__ float2 slots[2 * THREADS / 32];
-    size = 1 << a.team_shift; lane = threadIdx.x & (size - 1); id = threadIdx.x >> a.team_shift; warps = size >> 5;
+    size = KIND == WARP ? 32 : 1 << a.team_shift;
+    lane = threadIdx.x & (size - 1); id = KIND == WARP ? threadIdx.x >> 5 : threadIdx.x >> a.team_shift; warps = size >> 5;
     slot = slots + id * 2 * warps;
 #pragma unroll
     for (int j = 0; j < NV; ++j) { col[j] = (j * size + lane) * V; on[j] = col[j] < a.C; }
@@ -100,14 +106,14 @@ struct Team {
   __device__ __forceinline__ float2 sum(float x, float y) {
 #pragma unroll
     for (int d = 16; d; d >>= 1)
-      if (MULTI || d < size) { x += __shfl_xor_sync(0xffffffffu, x, d); y += __shfl_xor_sync(0xffffffffu, y, d); }
-    return MULTI ? across(x, y) : make_float2(x, y);
+      if (KIND != PART || d < size) { x += __shfl_xor_sync(0xffffffffu, x, d); y += __shfl_xor_sync(0xffffffffu, y, d); }
+    return KIND == MULTI ? across(x, y) : make_float2(x, y);
   }
   __device__ __forceinline__ float sum(float x) {
 #pragma unroll
     for (int d = 16; d; d >>= 1)
-      if (MULTI || d < size) x += __shfl_xor_sync(0xffffffffu, x, d);
-    return MULTI ? across(x, 0.f).x : x;
+      if (KIND != PART || d < size) x += __shfl_xor_sync(0xffffffffu, x, d);
+    return KIND == MULTI ? across(x, 0.f).x : x;
   }
   // The two halves of the slots are used in turn: a warp that is through with one sum may write the next while others still read.
   __device__ __forceinline__ float2 across(float x, float y) {
@@ -119,37 +125,13 @@ struct Team {
     for (int w = 1; w < warps; ++w) { t.x += s[w].x; t.y += s[w].y; }
     return t;
   }
-  template <class T>
-  __device__ __forceinline__ void load(const T* row, float (&x)[N]) const {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float v[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = 0.f;
-      if (on[j]) load_f32<T, V, LOAD_ONCE>(row + col[j], v);
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[j * V + i] = v[i];
-    }
-  }
-  template <class T>
-  __device__ __forceinline__ void load_raw(const T* row, Vec<T, V> (&x)[NV]) const {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) if (on[j]) x[j] = load_vec<Vec<T, V>, LOAD_ONCE>(row + col[j]);
-  }
-  template <class T>
-  __device__ __forceinline__ void to_floats(const Vec<T, V> (&r)[NV], float (&x)[N]) const {
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[j * V + i] = on[j] ? to_f32<T>(r[j].v[i]) : 0.f;
-  }
-  // A row of fp32 parameters, or `otherwise` where there is none.
+  // A row of fp32 parameters, or `otherwise` where there is none; zeros behind the row.
   __device__ __forceinline__ void load_row(const float* row, float otherwise, float (&x)[N]) const {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float v[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = otherwise;
+      for (int i = 0; i < V; ++i) v[i] = on[j] ? otherwise : 0.f;
       if (row && on[j]) load_f32<float, V>(row + col[j], v);
 #pragma unroll
       for (int i = 0; i < V; ++i) x[j * V + i] = v[i];
@@ -174,201 +156,340 @@ struct Team {
       if (on[j]) store_f32<float, V>(row + col[j], v);
     }
   }
-  __device__ __forceinline__ bool valid(int e) const { return on[e / V]; }
-  // (mean, rstd) of a row; RMS: mean 0.
-  __device__ __forceinline__ float2 statistics(const Args& a, const float (&x)[N]) {
-    float mean = 0.f, q = 0.f;
+  // (1 / sqrt(var + eps)) of a row that is left without its mean (RMS: as it is); elements behind the row are 0 before and after.
+  __device__ __forceinline__ float2 centre(const Args& a, float (&x)[N]) {
+    float mean = 0.f;
     if (a.layer) {
       float s = 0.f;
 #pragma unroll
       for (int e = 0; e < N; ++e) s += x[e];
       mean = sum(s) * a.inv_C;
-    }
 #pragma unroll
-    for (int e = 0; e < N; ++e) { const float d = valid(e) ? x[e] - mean : 0.f; q = fmaf(d, d, q); }
+      for (int j = 0; j < NV; ++j) {
+        const float m = on[j] ? mean : 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[j * V + i] -= m;
+      }
+    }
+    float q = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) q = fmaf(x[e], x[e], q);
     return make_float2(mean, rsqrtf(fmaf(sum(q), a.inv_C, a.eps)));
   }
 };
 
-template <class T, class R, int V, bool MULTI>
-__global__ void __launch_bounds__(THREADS) resnorm_kernel(const Args a) {
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  const uint32_t s = (uint32_t)__cvta_generic_to_shared(to);
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(s), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void end_of_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void wait_for_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// The rows of one array, AHEAD of them on their way: into shared memory (a thread's pieces of a row 16 bytes apart from its neighbours'), or for single elements, which
+// asynchronous copies do not take, one row into registers.
+template <class T, int V, int AHEAD>
+struct Source {
+  static constexpr int NV = N / V, VB = V * (int)sizeof(T), PB = VB < 16 ? VB : 16, PIECES = VB / PB, BYTES = AHEAD * NV * VB * THREADS;
+  unsigned char* mine;
+  __device__ __forceinline__ unsigned char* at(int place, int j, int piece) const { return mine + (((place * NV + j) * PIECES + piece) * THREADS) * PB; }
+  template <class Place>
+  __device__ __forceinline__ void open(unsigned char* smem, const Place& team) {
+    mine = smem + threadIdx.x * PB;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (!team.on[j])
+        for (int p = 0; p < AHEAD; ++p)
+#pragma unroll
+          for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+            for (int w = 0; w < PB / 4; ++w) reinterpret_cast<uint32_t*>(at(p, j, k))[w] = 0;
+  }
+  template <class Place>
+  __device__ __forceinline__ void fetch(const T* row, int place, const Place& team) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (team.on[j])
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) copy_async<PB>(at(place, j, k), reinterpret_cast<const unsigned char*>(row + team.col[j]) + k * PB);
+  }
+  __device__ __forceinline__ void get(int place, float (&x)[N]) const {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) {
+        const auto r = load_vec<Vec<T, PB / (int)sizeof(T)>>(at(place, j, k));
+#pragma unroll
+        for (int i = 0; i < PB / (int)sizeof(T); ++i) x[j * V + k * (PB / (int)sizeof(T)) + i] = to_f32<T>(r.v[i]);
+      }
+  }
+};
+template <class T, int AHEAD>
+struct Source<T, 1, AHEAD> {
+  static constexpr int BYTES = 0;
+  T x_[N];
+  template <class Place>
+  __device__ __forceinline__ void open(unsigned char*, const Place&) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x_[e] = T(0.f);
+  }
+  template <class Place>
+  __device__ __forceinline__ void fetch(const T* row, int, const Place& team) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) if (team.on[e]) x_[e] = row[team.col[e]];
+  }
+  __device__ __forceinline__ void get(int, float (&x)[N]) const {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = to_f32<T>(x_[e]);
+  }
+};
+template <int V> constexpr int ahead(int rows) { return V == 1 ? 1 : rows; }
+constexpr int FORWARD_AHEAD = 4, GRAD_AHEAD = 3;
+
+// Rows that the threads of a warp go through together: as many as the longest of its teams has (the exchanges take all threads).
+template <int KIND>
+__device__ __forceinline__ int rows_to_walk(long long begin, long long end) {
+  const int mine = begin < end ? (int)(end - begin) : 0;
+  return KIND == PART ? (int)__reduce_max_sync(0xffffffffu, (unsigned)mine) : mine;
+}
+
+template <class T, class R, int V, int KIND>
+__global__ void __launch_bounds__(THREADS, 2) resnorm_kernel(const __grid_constant__ Args a) {
+  extern __shared__ __align__(16) unsigned char resnorm_rows[];
+  constexpr int AHEAD = ahead<V>(FORWARD_AHEAD);
   check_offsets(a);
-  Team<V, MULTI> team(a);
-  constexpr int NV = Team<V, MULTI>::NV;
-  const long long mine = ((long long)blockIdx.x * THREADS + threadIdx.x) >> a.team_shift;
+  Team<V, KIND> team(a);
+  const long long mine = KIND == WARP ? (long long)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5) : ((long long)blockIdx.x * THREADS + threadIdx.x) >> a.team_shift;
   const long long begin = mine * a.rows_a_team, end = begin + a.rows_a_team < a.n ? begin + a.rows_a_team : a.n;
-  // A warp of small teams goes on while one of its teams has rows: the shuffles take all of its threads.
-  const long long most = MULTI || a.team_shift >= 5 ? end : __reduce_max_sync(0xffffffffu, begin < end ? (unsigned)(end - begin) : 0u) + begin;
-  float ga[N], be[N], pg[N], gt[N];
+  const int rows = begin < end ? (int)(end - begin) : 0, walk = rows_to_walk<KIND>(begin, end);
+  Source<R, V, AHEAD> res;
+  Source<T, V, AHEAD> block;
+  res.open(resnorm_rows, team);
+  block.open(resnorm_rows + res.BYTES, team);
+  const R* next_res = static_cast<const R*>(a.res) + begin * a.ld_res;
+  const T* next_block = static_cast<const T*>(a.block) + begin * a.ld_block;
+  R* out_res = static_cast<R*>(a.out_res) + begin * a.ld_out_res;
+  T* out = static_cast<T*>(a.out) + begin * a.ld_out;
+  int place = 0;
+  const auto fetch = [&](int i) {
+    if (i < rows) {
+      res.fetch(next_res, place, team);
+      if (a.block) block.fetch(next_block, place, team);
+      next_res += a.ld_res;
+      next_block += a.ld_block;
+    }
+    end_of_copies();
+    place = place + 1 == AHEAD ? 0 : place + 1;
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fetch(i);
+  float ga[N], be[N], gt[N];                     // gt: alpha gate post_gamma
   team.load_row(a.gamma, 1.f, ga);
   team.load_row(a.beta, 0.f, be);
-  team.load_row(a.post_gamma, 1.f, pg);
+  const auto gate = [&](int g) {
+    float pg[N];
+    team.load_row(a.post_gamma, 1.f, pg);
+    team.load_row(g < 0 ? nullptr : a.gate + (long long)g * a.C, 1.f, gt);
 #pragma unroll
-  for (int e = 0; e < N; ++e) gt[e] = a.alpha;
-  const R* const res = static_cast<const R*>(a.res);
-  const T* const block = static_cast<const T*>(a.block);
-  Vec<R, V> raw_r[NV];
-  Vec<T, V> raw_b[NV];
-  const auto fetch = [&](long long row) {
-    if (row >= end) return;
-    team.load_raw(res + row * a.ld_res, raw_r);
-    if (block) team.load_raw(block + row * a.ld_block, raw_b);
+    for (int e = 0; e < N; ++e) gt[e] = gt[e] * a.alpha * pg[e];
   };
-  fetch(begin);
+  gate(-1);
   Group group = {-1, 0, 0};
-  for (long long row = begin; row < most; ++row) {
-    const bool have = row < end;
-    if (have && a.gate && (row == begin || row >= group.end)) {
+  for (int i = 0; i < walk; ++i) {
+    const long long row = begin + i;
+    const bool have = i < rows;
+    if (a.gate && have && (i == 0 || row >= group.end)) {
       find_group(a, row, &group);
-      if (group.g >= 0) {
-        team.load_row(a.gate + (long long)group.g * a.C, 1.f, gt);
-#pragma unroll
-        for (int e = 0; e < N; ++e) gt[e] *= a.alpha;
-      }
+      if (group.g >= 0) gate(group.g);
     }
+    wait_for_copies<AHEAD - 1>();
     float r[N], b[N];
-    team.to_floats(raw_r, r);
-    if (block) team.to_floats(raw_b, b);
-    fetch(row + 1);
+    res.get(place, r);
+    if (a.block) block.get(place, b);
     float2 s1 = make_float2(0.f, 0.f);
-    if (block) {
+    if (a.block) {
+      float scale = 1.f;
       if (a.post) {
-        s1 = team.statistics(a, b);
-#pragma unroll
-        for (int e = 0; e < N; ++e) b[e] = (b[e] - s1.x) * s1.y * pg[e];
+        s1 = team.centre(a, b);
+        scale = s1.y;
       }
 #pragma unroll
-      for (int e = 0; e < N; ++e) r[e] = team.valid(e) ? fmaf(gt[e], b[e], r[e]) : 0.f;
+      for (int e = 0; e < N; ++e) r[e] = fmaf(gt[e], b[e] * scale, r[e]);
     }
-    const float2 s2 = team.statistics(a, r);
-    if (have && (!a.gate || group.g >= 0)) {
-      if (a.out_res) team.store(static_cast<R*>(a.out_res) + row * a.ld_out_res, r);
+    const bool write = have && (!a.gate || group.g >= 0);
+    if (write && a.out_res) team.store(out_res, r);
+    const float2 s2 = team.centre(a, r);
+    fetch(i + AHEAD);                            // into the place of this row, whose values have gone into the sums
 #pragma unroll
-      for (int e = 0; e < N; ++e) r[e] = fmaf((r[e] - s2.x) * s2.y, ga[e], be[e]);
-      team.store(static_cast<T*>(a.out) + row * a.ld_out, r);
+    for (int e = 0; e < N; ++e) r[e] = fmaf(r[e] * s2.y, ga[e], be[e]);
+    if (write) {
+      team.store(out, r);
       if (a.stats && team.lane == 0) a.stats[row] = make_float4(s1.x, s1.y, s2.x, s2.y);
     }
+    out_res += a.ld_out_res;
+    out += a.ld_out;
   }
 }
 
-template <class T, class R, int V, bool MULTI>
-__global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) resnorm_grad_kernel(const Args a) {
-  extern __shared__ __align__(16) float resnorm_shared[];             // [teams of the block x C]
+template <class T, class R, int V, int KIND>
+__global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) resnorm_grad_kernel(const __grid_constant__ Args a) {
+  extern __shared__ __align__(16) unsigned char resnorm_rows[];                // the rows on their way; at the end [teams of the block x C] sums
+  constexpr int AHEAD = ahead<V>(GRAD_AHEAD);
   check_offsets(a);
-  Team<V, MULTI> team(a);
-  const long long mine = ((long long)blockIdx.x * THREADS + threadIdx.x) >> a.team_shift;
+  Team<V, KIND> team(a);
+  const long long mine = KIND == WARP ? (long long)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5) : ((long long)blockIdx.x * THREADS + threadIdx.x) >> a.team_shift;
   const long long begin = mine * a.rows_a_team, end = begin + a.rows_a_team < a.n ? begin + a.rows_a_team : a.n;
-  const long long most = MULTI || a.team_shift >= 5 ? end : __reduce_max_sync(0xffffffffu, begin < end ? (unsigned)(end - begin) : 0u) + begin;
-  float ga[N], pg[N], gt[N];
-  team.load_row(a.gamma, 1.f, ga);
-  team.load_row(a.post_gamma, 1.f, pg);
+  const int rows = begin < end ? (int)(end - begin) : 0, walk = rows_to_walk<KIND>(begin, end);
+  Source<R, V, AHEAD> res, dres;
+  Source<T, V, AHEAD> block, dy;
+  res.open(resnorm_rows, team);
+  dres.open(resnorm_rows + res.BYTES, team);
+  block.open(resnorm_rows + 2 * res.BYTES, team);
+  dy.open(resnorm_rows + 2 * res.BYTES + block.BYTES, team);
+  long long ahead_row = begin;
+  int place = 0;
+  const auto fetch = [&](int i) {
+    if (i < rows) {
+      res.fetch(static_cast<const R*>(a.res) + ahead_row * a.ld_res, place, team);
+      if (a.block) block.fetch(static_cast<const T*>(a.block) + ahead_row * a.ld_block, place, team);
+      if (a.dres) dres.fetch(static_cast<const R*>(a.dres) + ahead_row * a.ld_dres, place, team);
+      if (a.dy) dy.fetch(static_cast<const T*>(a.dy) + ahead_row * a.ld_dy, place, team);
+    }
+    ++ahead_row;
+    end_of_copies();
+    place = place + 1 == AHEAD ? 0 : place + 1;
+  };
 #pragma unroll
-  for (int e = 0; e < N; ++e) gt[e] = a.alpha;
-  float sum_ga[N] = {}, sum_be[N] = {}, sum_pg[N] = {}, sum_gt[N] = {};
+  for (int i = 0; i < AHEAD; ++i) fetch(i);
+  float4 next_stats = rows > 0 ? a.stats[begin] : make_float4(0.f, 0.f, 0.f, 0.f);
+  float ga[N], gt[N];                            // gt: alpha gate post_gamma
+  team.load_row(a.gamma, 1.f, ga);
+  const auto gate = [&](int g) {
+    float pg[N];
+    team.load_row(a.post_gamma, 1.f, pg);
+    team.load_row(g < 0 ? nullptr : a.gate + (long long)g * a.C, 1.f, gt);
+#pragma unroll
+    for (int e = 0; e < N; ++e) gt[e] = gt[e] * a.alpha * pg[e];
+  };
+  gate(-1);
+  float sum_ga[N] = {}, sum_be[N] = {}, sum_pg[N] = {}, sum_h[N] = {};         // sum_h: of D h1 over the group's rows
   Group group = {-1, 0, 0};
-  const R *const res = static_cast<const R*>(a.res), *const dres = static_cast<const R*>(a.dres);
-  const T *const block = static_cast<const T*>(a.block), *const dy = static_cast<const T*>(a.dy);
   int2 goes_on = make_int2(-1, 0);
   // The sums of the group that ends in front of `row`.
   const auto close_group = [&](long long row) {
-    if (!a.d_gate || group.g < 0) return;
+    if (a.gate && group.g < 0) return;
+    float x[N];
+    if (a.d_post) {
+      team.load_row(a.gate ? a.gate + (long long)group.g * a.C : nullptr, 1.f, x);
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum_gt[e] *= a.alpha;
-    const bool before = group.begin < begin, after = row >= end && group.end > end;
-    if (!before && !after) team.store_row(a.d_gate + (long long)group.g * a.C, sum_gt);
-    else if (before) team.store_row(a.first + mine * a.C, sum_gt);
-    else {
-      team.store_row(a.last + mine * a.C, sum_gt);
-      goes_on = make_int2(group.g, (int)((group.end < a.n ? group.end - 1 : a.n - 1) / a.rows_a_team - mine));
+      for (int e = 0; e < N; ++e) sum_pg[e] = fmaf(x[e] * a.alpha, sum_h[e], sum_pg[e]);
     }
+    if (a.d_gate) {
+      team.load_row(a.post_gamma, 1.f, x);
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum_gt[e] = 0.f;
-  };
-  for (long long row = begin; row < most; ++row) {
-    const bool have = row < end;
-    if (have && a.gate && (row == begin || row >= group.end)) {
-      if (row > begin) close_group(row);
-      find_group(a, row, &group);
-      if (group.g >= 0) {
-        team.load_row(a.gate + (long long)group.g * a.C, 1.f, gt);
-#pragma unroll
-        for (int e = 0; e < N; ++e) gt[e] *= a.alpha;
+      for (int e = 0; e < N; ++e) x[e] *= a.alpha * sum_h[e];
+      const bool before = group.begin < begin, after = row >= end && group.end > end;
+      if (!before && !after) team.store_row(a.d_gate + (long long)group.g * a.C, x);
+      else if (before) team.store_row(a.first + mine * a.C, x);
+      else {
+        team.store_row(a.last + mine * a.C, x);
+        goes_on = make_int2(group.g, (int)((group.end < a.n ? group.end - 1 : a.n - 1) / a.rows_a_team - mine));
       }
     }
-    const bool live = have && (!a.gate || group.g >= 0);
-    float x[N], u[N], d[N], g[N];
-    float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (live) {
-      team.load(res + row * a.ld_res, x);
-      if (block) team.load(block + row * a.ld_block, u);
-      if (dres) team.load(dres + row * a.ld_dres, d);
-      if (dy) team.load(dy + row * a.ld_dy, g);
-      st = a.stats[row];
-    } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = u[e] = 0.f;
+    for (int e = 0; e < N; ++e) sum_h[e] = 0.f;
+  };
+  for (int i = 0; i < walk; ++i) {
+    const long long row = begin + i;
+    const bool have = i < rows;
+    if (a.gate && have && (i == 0 || row >= group.end)) {
+      if (i > 0) close_group(row);
+      find_group(a, row, &group);
+      if (group.g >= 0) gate(group.g);
     }
-    if (!live || !dres) {
+    const bool live = have && (!a.gate || group.g >= 0);
+    float4 st = next_stats;
+    if (i + 1 < rows) next_stats = a.stats[row + 1];
+    wait_for_copies<AHEAD - 1>();
+    float x[N], u[N], d[N], g[N];
+    res.get(place, x);
+    if (a.block) block.get(place, u);
+    if (a.dres) dres.get(place, d);
+    if (a.dy) dy.get(place, g);
+    if (!live) {                                 // whatever stands there, it adds to nothing
+      st = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = u[e] = d[e] = g[e] = 0.f;
+    }
+    if (!a.dres) {
 #pragma unroll
       for (int e = 0; e < N; ++e) d[e] = 0.f;
     }
-    if (!live || !dy) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) g[e] = 0.f;
-    }
-    if (block) {
+    if (a.block) {
       if (a.post) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) u[e] = team.valid(e) ? (u[e] - st.x) * st.y : 0.f;                  // h1
+        for (int j = 0; j < N / V; ++j) {
+          const float m = team.on[j] ? st.x : 0.f;
+#pragma unroll
+          for (int k = 0; k < V; ++k) u[j * V + k] = (u[j * V + k] - m) * st.y;        // h1
+        }
       }
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = fmaf(gt[e], a.post ? u[e] * pg[e] : u[e], x[e]);
+      for (int e = 0; e < N; ++e) x[e] = fmaf(gt[e], u[e], x[e]);
     }
-    if (dy) {
+    if (a.dy) {
       float s = 0.f, q = 0.f;
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        x[e] = team.valid(e) ? (x[e] - st.z) * st.w : 0.f;                                              // h2
-        sum_be[e] += g[e];
-        sum_ga[e] = fmaf(g[e], x[e], sum_ga[e]);
-        g[e] *= ga[e];
-        s += g[e];
-        q = fmaf(g[e], x[e], q);
+      for (int j = 0; j < N / V; ++j) {
+        const float m = team.on[j] ? st.z : 0.f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const int e = j * V + k;
+          x[e] = (x[e] - m) * st.w;                                                    // h2
+          sum_be[e] += g[e];
+          sum_ga[e] = fmaf(g[e], x[e], sum_ga[e]);
+          g[e] *= ga[e];
+          s += g[e];
+          q = fmaf(g[e], x[e], q);
+        }
       }
       const float2 t = team.sum(s, q);
       const float m1 = a.layer ? t.x * a.inv_C : 0.f, m2 = t.y * a.inv_C;
 #pragma unroll
-      for (int e = 0; e < N; ++e) d[e] = fmaf(st.w, g[e] - m1 - x[e] * m2, d[e]);
+      for (int j = 0; j < N / V; ++j) {
+        const float m = team.on[j] ? m1 : 0.f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) { const int e = j * V + k; d[e] = fmaf(st.w, fmaf(-x[e], m2, g[e] - m), d[e]); }
+      }
     }
     if (live) team.store(static_cast<R*>(a.out_res) + row * a.ld_out_res, d);
-    if (block) {
+    if (a.block) {
       float s = 0.f, q = 0.f;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float dv = team.valid(e) ? d[e] : 0.f;
-        sum_gt[e] = fmaf(dv, a.post ? u[e] * pg[e] : u[e], sum_gt[e]);
-        d[e] = dv * gt[e];                                                                              // du
-        if (a.post) {
-          sum_pg[e] = fmaf(d[e], u[e], sum_pg[e]);
-          d[e] *= pg[e];
-          s += d[e];
-          q = fmaf(d[e], u[e], q);
-        }
+        sum_h[e] = fmaf(d[e], u[e], sum_h[e]);
+        d[e] *= gt[e];                                                                 // du post_gamma
+        s += d[e];
+        q = fmaf(d[e], u[e], q);
       }
       if (a.post) {
         const float2 t = team.sum(s, q);
         const float m1 = a.layer ? t.x * a.inv_C : 0.f, m2 = t.y * a.inv_C;
 #pragma unroll
-        for (int e = 0; e < N; ++e) d[e] = st.y * (d[e] - m1 - u[e] * m2);
+        for (int e = 0; e < N; ++e) d[e] = st.y * fmaf(-u[e], m2, d[e] - m1);
       }
       if (live && a.out) team.store(static_cast<T*>(a.out) + row * a.ld_out, d);
     }
+    fetch(i + AHEAD);                            // into the place of this row, whose values have been used
   }
-  if (begin < end) close_group(end);
+  if (rows > 0) close_group(end);
   if (a.span && team.lane == 0 && mine < a.teams) a.span[mine] = goes_on;
   if (a.chan) {
+    wait_for_copies<0>();
+    float* const sums = reinterpret_cast<float*>(resnorm_rows);
     const int teams = THREADS >> a.team_shift;
-    float* const mine_row = resnorm_shared + team.id * a.C;
+    float* const mine_row = sums + team.id * a.C;
     for (int which = 0; which < 3; ++which) {
       __syncthreads();
       if (which == 0) team.store_row(mine_row, sum_ga);
@@ -377,7 +498,7 @@ __global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) resnorm_grad_kernel(cons
       __syncthreads();
       for (int c = threadIdx.x; c < a.C; c += THREADS) {
         float s = 0.f;
-        for (int t = 0; t < teams; ++t) s += resnorm_shared[t * a.C + c];
+        for (int t = 0; t < teams; ++t) s += sums[t * a.C + c];
         a.chan[((long long)blockIdx.x * 3 + which) * a.C + c] = s;
       }
     }
@@ -412,9 +533,20 @@ __global__ void __launch_bounds__(JOIN * JOIN) resnorm_join_kernel(const Args a,
     if (tx == 0 && cw < a.C) out[cw] = s;
   }
   if (!a.d_gate) return;
+  // Groups over several teams: up to SHORT parts by one warp, a column a thread; more by the block.
+  constexpr int SHORT = 4 * JOIN;
+  for (long long t = unit0 * JOIN + ty; t < a.teams; t += units * JOIN) {
+    const int2 span = a.span[t];
+    if (span.x < 0 || span.y > SHORT || c >= a.C) continue;
+    float s = a.last[t * a.C + c];
+    const long long to = t + span.y < a.teams ? t + span.y : a.teams - 1;
+#pragma unroll 8
+    for (long long i = t + 1; i <= to; ++i) s += a.first[i * a.C + c];
+    a.d_gate[(long long)span.x * a.C + c] = s;
+  }
   for (long long t = unit0; t < a.teams; t += units) {
     const int2 span = a.span[t];
-    if (span.x < 0) continue;
+    if (span.x < 0 || span.y <= SHORT) continue;
     float s = 0.f;
     if (c < a.C) {
       if (ty == 0) s = a.last[t * a.C + c];
@@ -448,10 +580,10 @@ Plan plan_of(int64_t n, int C, int64_t rows_a_team) {
   const int64_t a_block = THREADS >> team_shift_of(C), teams = (n + rows_a_team - 1) / rows_a_team;
   return {rows_a_team, teams, (teams + a_block - 1) / a_block};
 }
-// Forward: up to 16 rows, as long as eight blocks an SM have work.
-Plan forward_plan(int64_t n, int C, int sms) {
-  const int64_t a_block = THREADS >> team_shift_of(C);
-  return plan_of(n, C, std::max<int64_t>(1, std::min<int64_t>(16, n / (a_block * sms * 8))));
+// All rows over the blocks that are resident at once.
+Plan forward_plan(int64_t n, int C, int64_t blocks) {
+  const int64_t teams = (THREADS >> team_shift_of(C)) * blocks;
+  return plan_of(n, C, std::max<int64_t>(1, (n + teams - 1) / teams));
 }
 // Gradient: all rows over the blocks that are resident at once, two rows a team at least.
 Plan grad_plan(int64_t n, int C, int sms) {
@@ -505,6 +637,13 @@ void with_rows(int32_t type, int32_t res_type, int v, F f) {
   });
 }
 
+template <class F>
+void with_kind(int team_shift, F f) {
+  if (team_shift > 5) f(std::integral_constant<int, MULTI>());
+  else if (team_shift == 5) f(std::integral_constant<int, WARP>());
+  else f(std::integral_constant<int, PART>());
+}
+
 bool shape_ok(int64_t n, int32_t width, int32_t groups) { return n >= 0 && n < (1ll << 31) && width >= 1 && groups >= 0 && groups <= (1 << 30); }
 
 int resnorm_check(int64_t n, int32_t width, const void* res, int64_t ld_res, int32_t res_type, const void* block, int64_t ld_block, int32_t type, int32_t kind, int32_t post,
@@ -545,8 +684,6 @@ extern "C" int taurus_residual_norm(int64_t n, int32_t width, const void* res, i
   a.inv_C = 1.f / (float)width; a.res = res; a.ld_res = ld_res; a.block = block; a.ld_block = ld_block; a.out_res = out_res; a.ld_out_res = ld_out_res; a.out = out; a.ld_out = ld_out;
   a.post_gamma = post_gamma; a.gate = gate; a.gamma = gamma; a.beta = beta; a.offsets = reinterpret_cast<const long long*>(offsets); a.stats = reinterpret_cast<float4*>(stats);
   a.status = status;
-  const Plan p = forward_plan(n, width, sms);
-  a.rows_a_team = p.rows_a_team; a.teams = p.teams;
   const Rows rows[] = {{res, ld_res, rs}, {block, ld_block, ts}, {out_res, ld_out_res, rs}, {out, ld_out, ts}};
   const void* const params[] = {post_gamma, gate, gamma, beta};
   Launches enqueue = {static_cast<cudaStream_t>(cuda_stream)};
@@ -554,8 +691,18 @@ extern "C" int taurus_residual_norm(int64_t n, int32_t width, const void* res, i
     using T = typename decltype(tt)::type;
     using R = typename decltype(rt)::type;
     constexpr int V = decltype(vc)::value;
-    if (a.team_shift > 5) enqueue(resnorm_kernel<T, R, V, true>, dim3((unsigned)p.blocks), THREADS, 0, a);
-    else enqueue(resnorm_kernel<T, R, V, false>, dim3((unsigned)p.blocks), THREADS, 0, a);
+    const auto go = [&](auto kind) {
+      constexpr int KIND = decltype(kind)::value;
+      constexpr size_t smem = Source<R, V, ahead<V>(FORWARD_AHEAD)>::BYTES + Source<T, V, ahead<V>(FORWARD_AHEAD)>::BYTES;
+      int resident = 0;
+      cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+      if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, resnorm_kernel<T, R, V, KIND>, THREADS, smem);
+      if (e != cudaSuccess) { enqueue.error = e; return; }
+      const Plan p = forward_plan(n, width, (int64_t)sms * std::max(resident, 1));
+      a.rows_a_team = p.rows_a_team; a.teams = p.teams;
+      enqueue(resnorm_kernel<T, R, V, KIND>, dim3((unsigned)p.blocks), THREADS, smem, a);
+    };
+    with_kind(a.team_shift, go);
   });
   return enqueue.done("residual norm");
 }
@@ -615,9 +762,15 @@ extern "C" int taurus_residual_norm_grad(int64_t n, int32_t width, const void* r
       using T = typename decltype(tt)::type;
       using R = typename decltype(rt)::type;
       constexpr int V = decltype(vc)::value;
-      const size_t smem = a.chan ? (size_t)(THREADS >> a.team_shift) * width * 4 : 0;
-      if (a.team_shift > 5) enqueue(resnorm_grad_kernel<T, R, V, true>, dim3((unsigned)p.blocks), THREADS, smem, a);
-      else enqueue(resnorm_grad_kernel<T, R, V, false>, dim3((unsigned)p.blocks), THREADS, smem, a);
+      const auto go = [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+        constexpr size_t rows_bytes = 2 * (Source<R, V, ahead<V>(GRAD_AHEAD)>::BYTES + Source<T, V, ahead<V>(GRAD_AHEAD)>::BYTES);
+        constexpr size_t smem = std::max<size_t>(rows_bytes, (size_t)THREADS * N * 4);            // (a block's teams x columns are at most its threads x elements)
+        const cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_grad_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+        if (e != cudaSuccess) { enqueue.error = e; return; }
+        enqueue(resnorm_grad_kernel<T, R, V, KIND>, dim3((unsigned)p.blocks), THREADS, smem, a);
+      };
+      with_kind(a.team_shift, go);
     });
   }
   if (joins) {

@@ -255,14 +255,17 @@ __device__ __forceinline__ int rows_to_walk(long long begin, long long end) {
 }
 
 template <class T, class R, int V, int KIND>
-__global__ void __launch_bounds__(THREADS, 2) resnorm_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(THREADS, V == 1 || KIND == MULTI ? 2 : 3) resnorm_kernel(const __grid_constant__ Args a) {
   extern __shared__ __align__(16) unsigned char resnorm_rows[];
   constexpr int AHEAD = ahead<V>(FORWARD_AHEAD);
   check_offsets(a);
   Team<V, KIND> team(a);
-  const long long mine = KIND == WARP ? (long long)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5) : ((long long)blockIdx.x * THREADS + threadIdx.x) >> a.team_shift;
-  const long long begin = mine * a.rows_a_team, end = begin + a.rows_a_team < a.n ? begin + a.rows_a_team : a.n;
-  const int rows = begin < end ? (int)(end - begin) : 0, walk = rows_to_walk<KIND>(begin, end);
+  // A block has neighbouring rows, which its teams take in turn.
+  const int teams = KIND == WARP ? THREADS / 32 : THREADS >> a.team_shift;
+  const long long block_begin = (long long)blockIdx.x * a.rows_a_team * teams, begin = block_begin + team.id;
+  const long long left = (block_begin + a.rows_a_team * teams < a.n ? block_begin + a.rows_a_team * teams : a.n) - begin;
+  const int rows = left > 0 ? (int)((left + teams - 1) / teams) : 0, walk = KIND == PART ? (int)__reduce_max_sync(0xffffffffu, (unsigned)rows) : rows;
+  const long long step_res = teams * a.ld_res, step_block = teams * a.ld_block, step_out_res = teams * a.ld_out_res, step_out = teams * a.ld_out;
   Source<R, V, AHEAD> res;
   Source<T, V, AHEAD> block;
   res.open(resnorm_rows, team);
@@ -276,8 +279,8 @@ __global__ void __launch_bounds__(THREADS, 2) resnorm_kernel(const __grid_consta
     if (i < rows) {
       res.fetch(next_res, place, team);
       if (a.block) block.fetch(next_block, place, team);
-      next_res += a.ld_res;
-      next_block += a.ld_block;
+      next_res += step_res;
+      next_block += step_block;
     }
     end_of_copies();
     place = place + 1 == AHEAD ? 0 : place + 1;
@@ -297,7 +300,7 @@ __global__ void __launch_bounds__(THREADS, 2) resnorm_kernel(const __grid_consta
   gate(-1);
   Group group = {-1, 0, 0};
   for (int i = 0; i < walk; ++i) {
-    const long long row = begin + i;
+    const long long row = begin + (long long)i * teams;
     const bool have = i < rows;
     if (a.gate && have && (i == 0 || row >= group.end)) {
       find_group(a, row, &group);
@@ -327,8 +330,8 @@ __global__ void __launch_bounds__(THREADS, 2) resnorm_kernel(const __grid_consta
       team.store(out, r);
       if (a.stats && team.lane == 0) a.stats[row] = make_float4(s1.x, s1.y, s2.x, s2.y);
     }
-    out_res += a.ld_out_res;
-    out += a.ld_out;
+    out_res += step_out_res;
+    out += step_out;
   }
 }
 
@@ -417,10 +420,12 @@ __global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) resnorm_grad_kernel(cons
     if (a.block) block.get(place, u);
     if (a.dres) dres.get(place, d);
     if (a.dy) dy.get(place, g);
-    if (!live) {                                 // whatever stands there, it adds to nothing
-      st = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (KIND == PART ? !__all_sync(0xffffffffu, live) : !live) {     // whatever stands in a row that does not count, it adds to nothing
+      if (!live) {
+        st = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = u[e] = d[e] = g[e] = 0.f;
+        for (int e = 0; e < N; ++e) x[e] = u[e] = d[e] = g[e] = 0.f;
+      }
     }
     if (!a.dres) {
 #pragma unroll
@@ -528,6 +533,7 @@ __global__ void __launch_bounds__(JOIN * JOIN) resnorm_join_kernel(const Args a,
     if (!out) continue;
     float s = 0.f;
     if (c < a.C)
+#pragma unroll 8
       for (int b = ty; b < a.blocks; b += JOIN) s += a.chan[((long long)b * 3 + unit) * a.C + c];
     s = join_columns(s);
     if (tx == 0 && cw < a.C) out[cw] = s;
@@ -535,26 +541,35 @@ __global__ void __launch_bounds__(JOIN * JOIN) resnorm_join_kernel(const Args a,
   if (!a.d_gate) return;
   // Groups over several teams: up to SHORT parts by one warp, a column a thread; more by the block.
   constexpr int SHORT = 4 * JOIN;
-  for (long long t = unit0 * JOIN + ty; t < a.teams; t += units * JOIN) {
-    const int2 span = a.span[t];
-    if (span.x < 0 || span.y > SHORT || c >= a.C) continue;
-    float s = a.last[t * a.C + c];
-    const long long to = t + span.y < a.teams ? t + span.y : a.teams - 1;
+  __shared__ int longer[JOIN];
+  for (long long t0 = unit0 * JOIN; t0 < a.teams; t0 += units * JOIN) {
+    const long long t = t0 + ty;
+    const int2 span = t < a.teams ? a.span[t] : make_int2(-1, 0);
+    const bool more = span.x >= 0 && span.y > SHORT;
+    if (tx == 0) longer[ty] = more;
+    if (span.x >= 0 && !more && c < a.C) {
+      float s = a.last[t * a.C + c];
+      const float* const first = a.first + (t + 1) * a.C + c;
+      const int parts = (int)(t + span.y < a.teams ? span.y : a.teams - 1 - t);
 #pragma unroll 8
-    for (long long i = t + 1; i <= to; ++i) s += a.first[i * a.C + c];
-    a.d_gate[(long long)span.x * a.C + c] = s;
-  }
-  for (long long t = unit0; t < a.teams; t += units) {
-    const int2 span = a.span[t];
-    if (span.x < 0 || span.y <= SHORT) continue;
-    float s = 0.f;
-    if (c < a.C) {
-      if (ty == 0) s = a.last[t * a.C + c];
-      const long long to = t + span.y < a.teams ? t + span.y : a.teams - 1;
-      for (long long i = t + 1 + ty; i <= to; i += JOIN) s += a.first[i * a.C + c];
+      for (int i = 0; i < parts; ++i) s += first[(long long)i * a.C];
+      a.d_gate[(long long)span.x * a.C + c] = s;
     }
-    s = join_columns(s);
-    if (tx == 0 && cw < a.C) a.d_gate[(long long)span.x * a.C + cw] = s;
+    if (!__syncthreads_or(more)) continue;
+    for (int k = 0; k < JOIN; ++k) {
+      if (!longer[k]) continue;
+      const int2 of = a.span[t0 + k];
+      float s = 0.f;
+      if (c < a.C) {
+        if (ty == 0) s = a.last[(t0 + k) * a.C + c];
+        const long long to = t0 + k + of.y < a.teams ? t0 + k + of.y : a.teams - 1;
+#pragma unroll 8
+        for (long long i = t0 + k + 1 + ty; i <= to; i += JOIN) s += a.first[i * a.C + c];
+      }
+      s = join_columns(s);
+      if (tx == 0 && cw < a.C) a.d_gate[(long long)of.x * a.C + cw] = s;
+    }
+    __syncthreads();
   }
   // groups without rows
   for (long long g = unit0 * JOIN + ty; g < a.groups; g += units * JOIN) {
@@ -775,7 +790,7 @@ extern "C" int taurus_residual_norm_grad(int64_t n, int32_t width, const void* r
   }
   if (joins) {
     const int column_blocks = (width + JOIN - 1) / JOIN;
-    const int64_t units = std::max<int64_t>(3, std::min<int64_t>(grad_gate ? std::max<int64_t>(a.teams, groups / JOIN) : 3, 1184 / column_blocks));
+    const int64_t units = std::max<int64_t>(3, std::min<int64_t>(grad_gate ? std::max<int64_t>(a.teams, groups) / JOIN + 1 : 3, 2 * SMS / column_blocks));
     if (n == 0) a.blocks = 0;
     enqueue.early = n > 0;
     enqueue(resnorm_join_kernel, dim3((unsigned)(units * column_blocks)), JOIN * JOIN, 0, a, column_blocks);

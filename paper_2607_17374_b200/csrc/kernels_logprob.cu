@@ -22,7 +22,7 @@ namespace {
 constexpr int MAX_TOP = TAURUS_MAX_TOP;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LEAST = -200.f;
-constexpr int ROW_THREADS = 128;               // threads and rows of a block of rows_kernel
+constexpr int ROWS = 128;                      // rows of a block of rows_kernel
 constexpr int WARPS = 8;                       // warps of a block of the others
 constexpr int LIST = 64;                       // places of a warp's list of candidates
 constexpr int MAX_PARTS = 64;                  // parts of a row
@@ -67,15 +67,28 @@ __device__ __forceinline__ float mul_sat(float a, float b) { float r; asm("mul.r
 constexpr float CUT = 256.f;
 __device__ __forceinline__ float below(float x, float m8) { return fma_sat(x, -1.f / CUT, m8); }
 __device__ __forceinline__ float exp_below(float z) { return ex2(z * (-CUT * LOG2E)); }
-// Sums over classes with the maximum known: s without the terms that equal it (weight 0; else 1), q of z e^-256z, others: how many are below.
+// Pairs of fp32 values and their arithmetic in one instruction.
+struct F2 { u64 v; };
+__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void split(F2 x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x.v)); }
+__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+
+// Sums over classes with the maximum known, two at a time: s without the terms that equal it (weight 0; else 1), q of z e^-256z, others: how many are below.
 struct RowSums {
-  float s = 0.f, q = 0.f, others = 0.f;
-  __device__ __forceinline__ void add(float x, float m8) {
-    const float z = below(x, m8), e = exp_below(z), w = mul_sat(z, 0x1p126f);
-    s = fmaf(e, w, s);
-    q = fmaf(e, z, q);
-    others += w;
+  F2 s = {0}, q = {0}, others = {0};
+  __device__ __forceinline__ void add2(float x, float y, float m8) {
+    const float zx = below(x, m8), zy = below(y, m8);
+    const F2 z = f2(zx, zy), w = f2(mul_sat(zx, 0x1p126f), mul_sat(zy, 0x1p126f));
+    float a, b;
+    split(mul(z, f2(-CUT * LOG2E, -CUT * LOG2E)), &a, &b);
+    const F2 e = f2(ex2(a), ex2(b));
+    s = fma(e, w, s);
+    q = fma(e, z, q);
+    others = add(others, w);
   }
+  __device__ __forceinline__ static float both(F2 x) { float a, b; split(x, &a, &b); return a + b; }
 };
 
 // Order of candidates: larger value first, of equal ones the lower class.  0: none (-inf, NaN).  -0 counts as 0.
@@ -112,7 +125,7 @@ __device__ __forceinline__ RowResult row_result(const Sums& s, bool bad) {
   if (bad) return {NAN, NAN, NAN};
   if (!(s.m > -INFINITY)) return {s.m, 0.f, 0.f};
   const float l = log1pf(s.s);
-  return {s.m, l, l - s.t / (1.f + s.s)};
+  return {s.m, l, l - __fdividef(s.t, 1.f + s.s)};
 }
 __device__ __forceinline__ float log_p(float x, const RowResult& r) { return r.m == -INFINITY ? -INFINITY : (x - r.m) - r.l; }
 
@@ -148,18 +161,16 @@ __device__ __forceinline__ float grad_of(const GradRow& r, float x) {
   const float lp = fmaf(below(x, r.m8), -CUT, -r.l), p = ex2(lp * LOG2E);
   return p * fmaf(-r.h, lp, r.c);                // (masked: p = 0)
 }
+__device__ __forceinline__ void grad_of2(const GradRow& r, float x, float y, float* dx, float* dy) {
+  const F2 lp = fma(f2(below(x, r.m8), below(y, r.m8)), f2(-CUT, -CUT), f2(-r.l, -r.l));
+  float a, b;
+  split(mul(lp, f2(LOG2E, LOG2E)), &a, &b);
+  split(mul(f2(ex2(a), ex2(b)), fma(f2(-r.h, -r.h), lp, f2(r.c, r.c))), dx, dy);
+}
 __device__ __forceinline__ float grad_of_label(const GradRow& r, float x) {
   const float lp = fmaf(below(x, r.m8), -CUT, -r.l), p = ex2(lp * LOG2E);
   return x == -INFINITY ? 0.f : -r.g * expm1f(lp) - r.h * p * (lp + r.H);
 }
-
-// Pairs of fp32 values and their arithmetic in one instruction.
-struct F2 { u64 v; };
-__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ void split(F2 x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x.v)); }
-__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
 
 // ---- the top: candidates of a warp ---------------------------------------------------------------------------------------------------------------------
 
@@ -246,16 +257,16 @@ struct Tile {
   }
   __device__ __forceinline__ void load(W* sm, const W* x, long long ld, int mode) const {
     if (mode == TILE_ELEMENTS) {
-      for (int f = threadIdx.x; f < rows * C; f += ROW_THREADS) { const int row = div(f, by_C), col = f - row * C; sm[row * P + col] = x[row * ld + col]; }
+      for (int f = threadIdx.x; f < rows * C; f += (int)blockDim.x) { const int row = div(f, by_C), col = f - row * C; sm[row * P + col] = x[row * ld + col]; }
       return;
     }
     const bool flat = mode == TILE_FLAT;
     const int words = rows * C, total = flat ? words / V : rows * vectors;
-    for (int v0 = threadIdx.x; v0 < total; v0 += 4 * ROW_THREADS) {
+    for (int v0 = threadIdx.x; v0 < total; v0 += 4 * (int)blockDim.x) {
       Vec<W, V> r[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int v = v0 + u * ROW_THREADS;
+        const int v = v0 + u * (int)blockDim.x;
         if (v >= total) break;
         if (flat) r[u] = load_vec<Vec<W, V>, LOAD_ONCE>(x + v * V);
         else {
@@ -269,7 +280,7 @@ struct Tile {
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int v = v0 + u * ROW_THREADS;
+        const int v = v0 + u * (int)blockDim.x;
         if (v >= total) break;
         if (flat && P == C) store_vec(sm + v * V, r[u]);
         else if (flat) {
@@ -285,12 +296,12 @@ struct Tile {
       }
     }
     if (flat)
-      for (int f = total * V + threadIdx.x; f < words; f += ROW_THREADS) { const int row = div(f, by_C); sm[row * P + f - row * C] = x[f]; }
+      for (int f = total * V + threadIdx.x; f < words; f += (int)blockDim.x) { const int row = div(f, by_C); sm[row * P + f - row * C] = x[f]; }
   }
   __device__ __forceinline__ void store(const W* sm, W* y, long long ld, int mode) const {
     if (mode == TILE_FLAT) {
       const int words = rows * C, total = words / V;
-      for (int v = threadIdx.x; v < total; v += ROW_THREADS) {
+      for (int v = threadIdx.x; v < total; v += (int)blockDim.x) {
         Vec<W, V> r;
         if (P == C) r = load_vec<Vec<W, V>>(sm + v * V);
         else {
@@ -301,9 +312,9 @@ struct Tile {
         }
         store_vec_once(y + v * V, r);
       }
-      for (int f = total * V + threadIdx.x; f < words; f += ROW_THREADS) { const int row = div(f, by_C); y[f] = sm[row * P + f - row * C]; }
+      for (int f = total * V + threadIdx.x; f < words; f += (int)blockDim.x) { const int row = div(f, by_C); y[f] = sm[row * P + f - row * C]; }
     } else if (mode == TILE_VECTORS) {
-      for (int v = threadIdx.x; v < rows * vectors; v += ROW_THREADS) {
+      for (int v = threadIdx.x; v < rows * vectors; v += (int)blockDim.x) {
         const int row = div(v, by_vectors), col = (v - row * vectors) * V;
         W* const p = y + row * ld + col;
         if (col + V <= C) {
@@ -316,57 +327,67 @@ struct Tile {
         }
       }
     } else {
-      for (int f = threadIdx.x; f < rows * C; f += ROW_THREADS) { const int row = div(f, by_C), col = f - row * C; y[row * ld + col] = sm[row * P + col]; }
+      for (int f = threadIdx.x; f < rows * C; f += (int)blockDim.x) { const int row = div(f, by_C), col = f - row * C; y[row * ld + col] = sm[row * P + col]; }
     }
   }
 };
 
 
-// A thread to a row.  KMAX: places for the top in registers (k <= KMAX; 0: none asked for).
-template <class T, bool PAIRS, int MODE, int KMAX>
-__global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
+// TPR threads to a row, which take its words in turn.  KMAX: places for the top in registers (k <= KMAX; 0: none asked for; with a top TPR is 1).
+template <class T, bool PAIRS, int MODE, int KMAX, int TPR>
+__global__ void __launch_bounds__(ROWS * TPR) rows_kernel(const Args a) {
   extern __shared__ __align__(16) unsigned char logprob_shared[];
   using W = typename Word<T, PAIRS>::type;
-  constexpr int NW = Word<T, PAIRS>::n, STEP = 8 / NW;
+  constexpr int NW = Word<T, PAIRS>::n, STEP = 8 / NW;      // words of 8 classes
   W* const sm = reinterpret_cast<W*>(logprob_shared);
-  const int C = a.C, CW = C / NW;
-  const long long tiles = (a.n + ROW_THREADS - 1) / ROW_THREADS;
+  const int C = a.C, all = C / NW, sub = threadIdx.x % TPR, CW = (all - sub + TPR - 1) / TPR;      // CW: words of this thread
+  const long long tiles = (a.n + ROWS - 1) / ROWS;
   for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const long long row0 = tile * ROW_THREADS, row = row0 + threadIdx.x;
-    const Tile<W> t = {(int)(a.n - row0 < ROW_THREADS ? a.n - row0 : ROW_THREADS), CW, a.pitch, a.vectors, a.by_C, a.by_vectors};
+    const long long row0 = tile * ROWS, row = row0 + threadIdx.x / TPR;
+    const Tile<W> t = {(int)(a.n - row0 < ROWS ? a.n - row0 : ROWS), all, a.pitch, a.vectors, a.by_C, a.by_vectors};
     t.load(sm, reinterpret_cast<const W*>(static_cast<const T*>(a.x) + row0 * a.ld), a.ld / NW, a.mode_in);
     const int label = row < a.n ? label_of(a, row) : -1;
     __syncthreads();
-    if (row < a.n) {
-      W* const mine = sm + threadIdx.x * a.pitch;
-      const T* const elements = reinterpret_cast<const T*>(mine);
+    if (TPR > 1 || row < a.n) {                  // (exchanges take all threads of a warp: rows behind the last are whatever the tile held)
+      W* const whole_row = sm + threadIdx.x / TPR * a.pitch;
+      W* const mine = whole_row + sub;           // its words are TPR apart
+      const T* const elements = reinterpret_cast<const T*>(whole_row);
       RowResult r;
       if (MODE != GRAD) {
         // Maxima of G classes of classes: the k-th largest of them has k values at least that are not below it, so what is below it is not among the top k.
         constexpr int G = KMAX <= 4 ? 8 : 32;
         float most[G];
+        if constexpr (NW == 2) {
+          using T2 = std::conditional_t<std::is_same_v<T, __nv_bfloat16>, __nv_bfloat162, __half2>;
+          T2 two[G / 2];
+          const T least = from_f32<T>(-INFINITY);
+          T2 none;
+          none.x = none.y = least;
 #pragma unroll
-        for (int i = 0; i < G; ++i) most[i] = -INFINITY;
-        int j = 0;
-        for (; j + G / NW <= CW; j += G / NW)
+          for (int i = 0; i < G / 2; ++i) two[i] = none;
+          int j = 0;
+          for (; j + G / 2 <= CW; j += G / 2)
 #pragma unroll
-          for (int i = 0; i < G / NW; ++i) {
-            float v[NW];
-            unpack<T>(mine[j + i], v);
+            for (int i = 0; i < G / 2; ++i) two[i] = __hmax2_nan(two[i], reinterpret_cast<const T2*>(mine)[(j + i) * TPR]);
 #pragma unroll
-            for (int e = 0; e < NW; ++e) most[i * NW + e] = max_nan(most[i * NW + e], v[e]);
-          }
+          for (int i = 0; i < G / 2; ++i) if (j + i < CW) two[i] = __hmax2_nan(two[i], reinterpret_cast<const T2*>(mine)[(j + i) * TPR]);
 #pragma unroll
-        for (int i = 0; i < G / NW; ++i)
-          if (j + i < CW) {
-            float v[NW];
-            unpack<T>(mine[j + i], v);
+          for (int i = 0; i < G / 2; ++i) { most[2 * i] = to_f32<T>(two[i].x); most[2 * i + 1] = to_f32<T>(two[i].y); }
+        } else {
 #pragma unroll
-            for (int e = 0; e < NW; ++e) most[i * NW + e] = max_nan(most[i * NW + e], v[e]);
-          }
+          for (int i = 0; i < G; ++i) most[i] = -INFINITY;
+          int j = 0;
+          for (; j + G <= CW; j += G)
+#pragma unroll
+            for (int i = 0; i < G; ++i) most[i] = max_nan(most[i], to_f32<T>(reinterpret_cast<const T*>(mine)[(j + i) * TPR]));
+#pragma unroll
+          for (int i = 0; i < G; ++i) if (j + i < CW) most[i] = max_nan(most[i], to_f32<T>(reinterpret_cast<const T*>(mine)[(j + i) * TPR]));
+        }
         float m = most[0];
 #pragma unroll
         for (int i = 1; i < G; ++i) m = max_nan(m, most[i]);
+#pragma unroll
+        for (int d = TPR / 2; d; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
         const bool bad = !(m < INFINITY);
         float top[KMAX ? KMAX : 1], floor = -INFINITY;
         int cls[KMAX ? KMAX : 1];
@@ -387,6 +408,7 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
         }
         // The sums, and the top's candidates, 64 classes at a time.
         RowSums sum;
+        int behind = 0;
         const float m8 = m * (1.f / CUT);
         for (int j0 = 0; j0 < CW; j0 += 64 / NW) {
           uint32_t found[2] = {0, 0};
@@ -396,22 +418,36 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
             for (int i0 = 0; i0 < 32 / NW; i0 += STEP) {
               const int j1 = j0 + half * (32 / NW) + i0;
               if (j1 >= CW) break;
-              uint32_t bits = 0;
-              const auto one = [&](int i) {
-                float v[NW];
-                unpack<T>(mine[j1 + i], v);
-#pragma unroll
-                for (int e = 0; e < NW; ++e) {
-                  sum.add(v[e], m8);
-                  if (KMAX && v[e] >= floor) bits |= 1u << (i * NW + e);
-                }
-              };
+              // 8 classes; behind the row's end a class that is masked adds nothing to s and q (and one to others)
+              float v[8];
               if (j1 + STEP <= CW) {
 #pragma unroll
-                for (int i = 0; i < STEP; ++i) one(i);
+                for (int i = 0; i < STEP; ++i) {
+                  float w[NW];
+                  unpack<T>(mine[(j1 + i) * TPR], w);
+#pragma unroll
+                  for (int e = 0; e < NW; ++e) v[i * NW + e] = w[e];
+                }
               } else {
 #pragma unroll
-                for (int i = 0; i < STEP; ++i) if (j1 + i < CW) one(i);
+                for (int i = 0; i < STEP; ++i) {
+                  float w[NW];
+#pragma unroll
+                  for (int e = 0; e < NW; ++e) w[e] = -INFINITY;
+                  if (j1 + i < CW) unpack<T>(mine[(j1 + i) * TPR], w);
+#pragma unroll
+                  for (int e = 0; e < NW; ++e) v[i * NW + e] = w[e];
+                }
+                behind = (j1 + STEP - CW) * NW;
+              }
+              uint32_t bits = 0;
+#pragma unroll
+              for (int e = 0; e < 8; e += 2) {
+                sum.add2(v[e], v[e + 1], m8);
+                if (KMAX) {
+                  if (v[e] >= floor) bits |= 1u << e;
+                  if (v[e + 1] >= floor) bits |= 2u << e;
+                }
               }
               if (KMAX) found[half] |= bits << (i0 * NW);
             }
@@ -421,7 +457,7 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
               const uint32_t bits = low ? found[0] : found[1];
               const int at = j0 * NW + (low ? 0 : 32) + __ffs(bits) - 1;
               if (low) found[0] = bits & (bits - 1); else found[1] = bits & (bits - 1);
-              const float v = to_f32<T>(elements[at]);
+              const float v = at < C ? to_f32<T>(elements[at]) : -INFINITY;
               if (v > top[KMAX - 1]) {                     // equal ones keep their places: they have the lower classes
 #pragma unroll
                 for (int i = KMAX - 1; i > 0; --i) {
@@ -433,10 +469,19 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
               }
             }
         }
-        r = row_result({m, sum.s + ((float)(C - 1) - sum.others), -CUT * sum.q}, bad);
-        if (a.logprob) a.logprob[row] = label < 0 ? 0.f : log_p(to_f32<T>(elements[label]), r);
-        if (a.entropy) a.entropy[row] = r.H;
-        if (a.stats) a.stats[row] = make_float2(r.m, r.l);
+        float sums = sum.both(sum.s), q = sum.both(sum.q), others = sum.both(sum.others) - (float)behind;
+#pragma unroll
+        for (int d = TPR / 2; d; d >>= 1) {
+          sums += __shfl_xor_sync(0xffffffffu, sums, d);
+          q += __shfl_xor_sync(0xffffffffu, q, d);
+          others += __shfl_xor_sync(0xffffffffu, others, d);
+        }
+        r = row_result({m, sums + ((float)(C - 1) - others), -CUT * q}, bad);
+        if (sub == 0 && row < a.n) {
+          if (a.logprob) a.logprob[row] = label < 0 ? 0.f : log_p(to_f32<T>(elements[label]), r);
+          if (a.entropy) a.entropy[row] = r.H;
+          if (a.stats) a.stats[row] = make_float2(r.m, r.l);
+        }
 #pragma unroll
         for (int i = 0; i < KMAX; ++i)
           if (i < a.k) {
@@ -444,34 +489,38 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
             if (a.top_class) a.top_class[row * a.k + i] = cls[i];
           }
       } else {
-        const float2 ml = a.stats_in[row];
-        r = {ml.x, ml.y, a.entropy_in ? a.entropy_in[row] : 0.f};
+        const long long from = row < a.n ? row : a.n - 1;
+        const float2 ml = a.stats_in[from];
+        r = {ml.x, ml.y, a.entropy_in ? a.entropy_in[from] : 0.f};
       }
       if (MODE != FORWARD) {
-        const GradRow gr = grad_row(a, row, label, r);
-        const float at = label >= 0 ? to_f32<T>(elements[label]) : 0.f;
+        const GradRow gr = grad_row(a, row < a.n ? row : a.n - 1, label, r);
+        const bool special = label >= 0 && label / NW % TPR == sub;              // this thread has the label's word
+        const float at = special ? to_f32<T>(elements[label]) : 0.f;
+        if (TPR > 1) __syncwarp();               // (its logit has been read for the row's log probability too)
         int j = 0;
         for (; j + STEP <= CW; j += STEP) {
           W w[STEP];
 #pragma unroll
-          for (int i = 0; i < STEP; ++i) w[i] = mine[j + i];
+          for (int i = 0; i < STEP; ++i) w[i] = mine[(j + i) * TPR];
 #pragma unroll
-          for (int i = 0; i < STEP; ++i) {
-            float v[NW];
-            unpack<T>(w[i], v);
-#pragma unroll
-            for (int e = 0; e < NW; ++e) v[e] = grad_of(gr, v[e]);
-            mine[j + i] = pack<T>(v);
+          for (int i = 0; i < STEP; i += 2 / NW) {
+            float v[2], y[2];
+            if constexpr (NW == 2) unpack<T>(w[i], v);
+            else { v[0] = to_f32<T>(w[i]); v[1] = to_f32<T>(w[i + 1]); }
+            grad_of2(gr, v[0], v[1], y, y + 1);
+            if constexpr (NW == 2) mine[(j + i) * TPR] = pack<T>(y);
+            else { mine[(j + i) * TPR] = from_f32<T>(y[0]); mine[(j + i + 1) * TPR] = from_f32<T>(y[1]); }
           }
         }
         for (; j < CW; ++j) {
           float v[NW];
-          unpack<T>(mine[j], v);
+          unpack<T>(mine[j * TPR], v);
 #pragma unroll
           for (int e = 0; e < NW; ++e) v[e] = grad_of(gr, v[e]);
-          mine[j] = pack<T>(v);
+          mine[j * TPR] = pack<T>(v);
         }
-        if (label >= 0) reinterpret_cast<T*>(mine)[label] = from_f32<T>(grad_of_label(gr, at));
+        if (special) reinterpret_cast<T*>(whole_row)[label] = from_f32<T>(grad_of_label(gr, at));
       }
     }
     __syncthreads();
@@ -516,23 +565,25 @@ __global__ void __launch_bounds__(32 * WARPS) team_kernel(const Args a) {
       const float mine = m;
 #pragma unroll
       for (int d = LANES / 2; d; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
+      // (words behind the row are masked classes: they add nothing but one each to others)
       RowSums sum;
       const float m8 = m * (1.f / CUT);
+      int words = 0;
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
+      for (int i = 0; i < W; i += 2 / NW) {
         if (i * LANES >= CW) continue;
-        if (i * LANES + lane < CW) {
-#pragma unroll
-          for (int e = 0; e < NW; ++e) sum.add(v[i][e], m8);
-        }
+        words += 2 / NW;
+        if constexpr (NW == 2) sum.add2(v[i][0], v[i][1], m8);
+        else sum.add2(v[i][0], v[i + 1][0], m8);
       }
+      float s = sum.both(sum.s), q = sum.both(sum.q), others = sum.both(sum.others);
 #pragma unroll
       for (int d = LANES / 2; d; d >>= 1) {
-        sum.s += __shfl_xor_sync(0xffffffffu, sum.s, d);
-        sum.q += __shfl_xor_sync(0xffffffffu, sum.q, d);
-        sum.others += __shfl_xor_sync(0xffffffffu, sum.others, d);
+        s += __shfl_xor_sync(0xffffffffu, s, d);
+        q += __shfl_xor_sync(0xffffffffu, q, d);
+        others += __shfl_xor_sync(0xffffffffu, others, d);
       }
-      r = row_result({m, sum.s + ((float)(a.C - 1) - sum.others), -CUT * sum.q}, !(m < INFINITY));
+      r = row_result({m, s + ((float)(words * NW * LANES - 1) - others), -CUT * q}, !(m < INFINITY));
       if (lane == 0 && have) {
         if (a.logprob) a.logprob[row] = label < 0 ? 0.f : log_p(to_f32<T>(static_cast<const T*>(a.x)[row * a.ld + label]), r);
         if (a.entropy) a.entropy[row] = r.H;
@@ -599,12 +650,17 @@ __global__ void __launch_bounds__(32 * WARPS) team_kernel(const Args a) {
       __syncwarp();                              // the label's logit has been read before its place is written
       Wd* const dx = reinterpret_cast<Wd*>(static_cast<T*>(a.dx) + row * a.ld_dx) + lane;
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
+      for (int i = 0; i < W; i += 2 / NW) {
         if (i * LANES >= CW) continue;
-        float y[NW];
-#pragma unroll
-        for (int e = 0; e < NW; ++e) y[e] = grad_of(gr, v[i][e]);
-        if (have && i * LANES + lane < CW) dx[i * LANES] = pack<T>(y);
+        float y[2];
+        if constexpr (NW == 2) {
+          grad_of2(gr, v[i][0], v[i][1], y, y + 1);
+          if (have && i * LANES + lane < CW) dx[i * LANES] = pack<T>(y);
+        } else {
+          grad_of2(gr, v[i][0], v[i + 1][0], y, y + 1);
+          if (have && i * LANES + lane < CW) dx[i * LANES] = from_f32<T>(y[0]);
+          if (have && (i + 1) * LANES + lane < CW) dx[(i + 1) * LANES] = from_f32<T>(y[1]);
+        }
       }
       if (special) static_cast<T*>(a.dx)[row * a.ld_dx + label] = from_f32<T>(grad_of_label(gr, at));
     }
@@ -673,10 +729,14 @@ __device__ __noinline__ void stream_candidates(Candidates& c, const Span<T> span
   sort_candidates(c, k);
 }
 
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+
 // WPR warps to a row or a part of one.  Thread t has the vectors t, t + 32 WPR, ... of it.
 template <class T, bool TOP, int WPR, bool WITH_GRAD>
-__global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
-  constexpr int V = 16 / (int)sizeof(T), U = 4, TEAM = 32 * WPR, PLACES = LIST * WPR, SHARES = WARPS / WPR;
+__global__ void __launch_bounds__(32 * WARPS, 4) stream_kernel(const Args a) {
+  constexpr int V = 16 / (int)sizeof(T), U = 4, AHEAD = 2, TEAM = 32 * WPR, PLACES = LIST * WPR, SHARES = WARPS / WPR;
   __shared__ u64 lists[TOP ? WARPS * LIST : 1];
   __shared__ u64 best[TOP ? SHARES * MAX_TOP : 1];
   __shared__ float warp_top[TOP ? WARPS * MAX_TOP : 1];
@@ -684,6 +744,8 @@ __global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
   __shared__ float warp_max[WARPS], warp_rest[WARPS];
   __shared__ int warp_same[WARPS], counts[SHARES], owners[SHARES];
   __shared__ unsigned chosen[WARPS];
+  __shared__ uint8_t who[TOP ? 32 * WARPS : 1];
+  __shared__ Vec<T, V> ahead[AHEAD * U * 32 * WARPS];
   early_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = warp / WPR, mine = threadIdx.x % TEAM, w0 = share * WPR;     // w0: the team's first warp
   const auto sync = [&] {
@@ -701,25 +763,36 @@ __global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
     const int first = span.first(), last = span.last();
     float m = -INFINITY;
     F2 s2 = f2(0.f, 0.f), t2 = s2;
-    for (int v0 = first; v0 < last; v0 += U * TEAM) {
-      Vec<T, V> raw[U];
-      if (v0 > first && v0 + U * TEAM < last) {                       // whole vectors
-        const T* const p = x + span.column(v0 + mine);
+    // Batches ahead, by asynchronous copies into places of the thread's own.  The first and the last vector of a span may be cut: those come by element.
+    int place = 0;
+    const auto fetch = [&](int v0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = load_vec<Vec<T, V>, WITH_GRAD ? LOAD_PLAIN : LOAD_ONCE>(p + u * TEAM * V);
-      } else {
+      for (int u = 0; u < U; ++u) {
+        const int v = v0 + u * TEAM + mine;
+        Vec<T, V>* const to = &ahead[(place * U + u) * (32 * WARPS) + threadIdx.x];
+        if (v > first && v < last - 1) copy_async(to, x + span.column(v));
+        else if (v < last) *to = span.template load<LOAD_PLAIN>(v);
+        else {
+          Vec<T, V> none;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int v = v0 + u * TEAM + mine;
-          if (v < last) raw[u] = span.template load<LOAD_PLAIN>(v);
-          else
-#pragma unroll
-            for (int i = 0; i < V; ++i) raw[u].v[i] = from_f32<T>(-INFINITY);
+          for (int i = 0; i < V; ++i) none.v[i] = from_f32<T>(-INFINITY);
+          *to = none;
         }
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      place = place + 1 == AHEAD ? 0 : place + 1;
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) fetch(first + i * U * TEAM);
+    for (int v0 = first; v0 < last; v0 += U * TEAM) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
+      Vec<T, V> raw[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = load_vec<Vec<T, V>>(&ahead[(place * U + u) * (32 * WARPS) + threadIdx.x]);
       float now = m;
 #pragma unroll
       for (int u = 0; u < U; ++u) now = max_nan(now, vector_max(raw[u]));
+      fetch(v0 + AHEAD * U * TEAM);              // into the place of this batch, which has been read
       const float d = fmaxf(m - now, LEAST), f = ex2(d * LOG2E);       // (nothing before: both sums are 0)
       const F2 d2 = f2(d, d), g2 = f2(f, f), minus = f2(-now, -now), log2e = f2(LOG2E, LOG2E);
       t2 = mul(fma(s2, d2, t2), g2);
@@ -834,21 +907,27 @@ __global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
         sync();
       }
       u64* const list = lists + w0 * LIST;
+      // Those threads' numbers in a row, then their vectors, all at once.
+      int before = 0, threads = 0;
+#pragma unroll
       for (int w = 0; w < WPR; ++w) {
-        unsigned todo = WPR > 1 ? chosen[w0 + w] : look;
-        while (todo) {
-          const int who = w * 32 + __ffs(todo) - 1;
-          todo &= todo - 1;
-          for (int v = first + who + mine * TEAM; v < last; v += TEAM * TEAM) {
-            const Vec<T, V> got = span.template load<LOAD_PLAIN>(v);
-            if (vector_max(got) < kth) continue;
-            for (int i = 0; i < V; ++i) {
-              const float y = to_f32<T>(got.v[i]);
-              if (y >= kth && y > -INFINITY) {
-                const int to = atomicAdd(&counts[share], 1);
-                if (to < PLACES) list[to] = key_of(y, span.column(v) + i);
-              }
-            }
+        const int c = __popc(WPR > 1 ? chosen[w0 + w] : look);
+        if (w0 + w < warp) before += c;
+        threads += c;
+      }
+      if (look >> lane & 1) who[w0 * 32 + before + __popc(look & ((1u << lane) - 1))] = (uint8_t)mine;
+      sync();
+      const int each = (last - first + TEAM - 1) / TEAM;
+      for (int f = mine; f < threads * each; f += TEAM) {
+        const int j = f / threads, v = first + who[w0 * 32 + f - j * threads] + j * TEAM;
+        if (v >= last) continue;
+        const Vec<T, V> got = span.template load<LOAD_PLAIN>(v);
+        if (vector_max(got) < kth) continue;
+        for (int i = 0; i < V; ++i) {
+          const float y = to_f32<T>(got.v[i]);
+          if (y >= kth && y > -INFINITY) {
+            const int to = atomicAdd(&counts[share], 1);
+            if (to < PLACES) list[to] = key_of(y, span.column(v) + i);
           }
         }
       }
@@ -901,7 +980,12 @@ __global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
         const int c = span.column(v);
         Vec<T, V> out;
 #pragma unroll
-        for (int i = 0; i < V; ++i) out.v[i] = from_f32<T>(grad_of(gr, to_f32<T>(in.v[i])));
+        for (int i = 0; i < V; i += 2) {
+          float y, z;
+          grad_of2(gr, to_f32<T>(in.v[i]), to_f32<T>(in.v[i + 1]), &y, &z);
+          out.v[i] = from_f32<T>(y);
+          out.v[i + 1] = from_f32<T>(z);
+        }
         if (label >= c && label < c + V) {
 #pragma unroll
           for (int i = 0; i < V; ++i) if (c + i == label) out.v[i] = from_f32<T>(grad_of_label(gr, to_f32<T>(in.v[i])));
@@ -916,38 +1000,51 @@ __global__ void __launch_bounds__(32 * WARPS) stream_kernel(const Args a) {
   }
 }
 
-// The parts of a row, in their order: a warp to a row.
+// The parts of a row: a block to a row.  Sums by a tree in a fixed order, the top by the heads of the parts' lists.
+constexpr int JOIN_THREADS = 128;
 template <class T>
-__global__ void __launch_bounds__(128) join_kernel(const Args a) {
+__global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const Args a) {
+  __shared__ u64 lists[MAX_PARTS * MAX_TOP];
   early_start();
   const int lane = threadIdx.x & 31;
-  for (long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); row < a.n; row += (long long)gridDim.x * 4) {
-    const float4* const part = a.part + row * a.parts;
-    Sums sums = {-INFINITY, 0.f, 0.f};
-    bool bad = false;
-    for (int i = 0; i < a.parts; ++i) {
-      const float4 o = part[i];
-      join(sums, {o.x, o.y, o.z});
-      bad |= o.w != 0.f;
-    }
-    const RowResult r = row_result(sums, bad);
-    const int label = label_of(a, row);
-    if (lane == 0) write_row<T>(a, row, label, r);
-    if (a.k) {
-      const u64* const top = a.part_top + row * a.parts * a.k;
-      int head0 = 0, head1 = 0;
-      u64 h0 = lane < a.parts ? top[lane * a.k] : 0, h1 = lane + 32 < a.parts ? top[(lane + 32) * a.k] : 0, keep = 0;
-      for (int i = 0; i < a.k; ++i) {
-        const u64 mine = h0 > h1 ? h0 : h1;
-        const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32));
-        const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32) == hi ? (uint32_t)mine : 0u);
-        const u64 best = ((u64)hi << 32) | lo;
-        if (lane == i) keep = best;
-        if (best && h0 == best) { ++head0; h0 = head0 < a.k ? top[lane * a.k + head0] : 0; }
-        else if (best && h1 == best) { ++head1; h1 = head1 < a.k ? top[(lane + 32) * a.k + head1] : 0; }
+  for (long long row = blockIdx.x; row < a.n; row += gridDim.x) {
+    const u64* const top = a.part_top + row * a.parts * a.k;
+    for (int i = threadIdx.x; i < a.parts * a.k; i += JOIN_THREADS) lists[i] = top[i];
+    __syncthreads();
+    if (threadIdx.x < 32) {
+      const float4* const part = a.part + row * a.parts;
+      Sums sums = {-INFINITY, 0.f, 0.f};
+      bool bad = false;
+      for (int i = lane; i < a.parts; i += 32) {
+        const float4 o = part[i];
+        join(sums, {o.x, o.y, o.z});
+        bad |= o.w != 0.f;
       }
-      if (lane < a.k) write_top(a, row, lane, keep, r);
+#pragma unroll
+      for (int d = 16; d; d >>= 1) {
+        const Sums o = {__shfl_down_sync(0xffffffffu, sums.m, d), __shfl_down_sync(0xffffffffu, sums.s, d), __shfl_down_sync(0xffffffffu, sums.t, d)};
+        if (lane < d) join(sums, o);
+      }
+      sums = {__shfl_sync(0xffffffffu, sums.m, 0), __shfl_sync(0xffffffffu, sums.s, 0), __shfl_sync(0xffffffffu, sums.t, 0)};
+      const RowResult r = row_result(sums, __any_sync(0xffffffffu, bad));
+      const int label = label_of(a, row);
+      if (lane == 0) write_row<T>(a, row, label, r);
+      if (a.k) {
+        int head0 = 0, head1 = 0;
+        u64 h0 = lane < a.parts ? lists[lane * a.k] : 0, h1 = lane + 32 < a.parts ? lists[(lane + 32) * a.k] : 0, keep = 0;
+        for (int i = 0; i < a.k; ++i) {
+          const u64 mine = h0 > h1 ? h0 : h1;
+          const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32));
+          const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32) == hi ? (uint32_t)mine : 0u);
+          const u64 best = ((u64)hi << 32) | lo;
+          if (lane == i) keep = best;
+          if (best && h0 == best) { ++head0; h0 = head0 < a.k ? lists[lane * a.k + head0] : 0; }
+          else if (best && h1 == best) { ++head1; h1 = head1 < a.k ? lists[(lane + 32) * a.k + head1] : 0; }
+        }
+        if (lane < a.k) write_top(a, row, lane, keep, r);
+      }
     }
+    __syncthreads();
   }
 }
 
@@ -979,7 +1076,12 @@ __global__ void __launch_bounds__(256) grad_kernel(const Args a, int chunks) {
       const int c = span.column(v);
       Vec<T, V> out;
 #pragma unroll
-      for (int i = 0; i < V; ++i) out.v[i] = from_f32<T>(grad_of(gr, to_f32<T>(in[u].v[i])));
+      for (int i = 0; i < V; i += 2) {
+        float y, z;
+        grad_of2(gr, to_f32<T>(in[u].v[i]), to_f32<T>(in[u].v[i + 1]), &y, &z);
+        out.v[i] = from_f32<T>(y);
+        out.v[i + 1] = from_f32<T>(z);
+      }
       if (gr.label >= c && gr.label < c + V) {
 #pragma unroll
         for (int i = 0; i < V; ++i) if (c + i == gr.label) out.v[i] = from_f32<T>(grad_of_label(gr, to_f32<T>(in[u].v[i])));
@@ -997,7 +1099,7 @@ __global__ void __launch_bounds__(256) grad_kernel(const Args a, int chunks) {
 // Rows that fit the registers of a warp: 32 elements a lane.  Pairs: 16-bit rows that begin at even elements everywhere.
 constexpr int TEAM_CLASSES = 1024;
 // Rows that a thread each takes: where there are enough of them, and a tile leaves room for other blocks beside it.
-constexpr int THREAD_ROWS = 4096, THREAD_BYTES = 512;
+constexpr int THREAD_ROWS = 4096, THREAD_BYTES = 512, TWO_THREADS_BYTES = 128;      // (from there on tiles leave an SM few threads: two to a row)
 inline bool by_thread(const Args& a, int ts) { return a.n >= THREAD_ROWS && a.C * ts <= THREAD_BYTES; }
 inline bool in_pairs(const Args& a, int ts, bool grad) {
   const auto even = [](const void* p, long long ld) { return rows_aligned(p, 4) && ld % 2 == 0; };
@@ -1031,7 +1133,9 @@ template <class T, bool PAIRS>
 void set_tile(Args* a) {
   constexpr int NW = PAIRS ? 2 : 1, V = 16 / (NW * (int)sizeof(T));               // elements of a word, words of a vector
   const int C = a->C / NW;
-  a->pitch = sizeof(T) * NW == 2 ? C : C | 1;                                     // (PAIRS: even widths; else odd ones of 16 bits, or fp32)
+  // A thread's row begins pitch words behind its neighbour's: with a common divisor d of pitch and 32, d threads of a warp meet in a bank.  Up to four cost less than rows set apart, which
+  // cannot be copied by vectors.  (Rows of 16-bit elements have odd widths here.)
+  a->pitch = sizeof(T) * NW == 4 && C % 8 == 0 ? C + 1 : C;
   const auto by = [](int d) { return d == 1 ? 0u : (unsigned)(((1ull << 32) + d - 1) / d); };
   a->vectors = (C + V - 1) / V;
   a->by_C = by(C); a->by_vectors = by(a->vectors);
@@ -1043,16 +1147,16 @@ void set_tile(Args* a) {
   a->mode_out = mode(a->dx, a->ld_dx);
 }
 
-template <class T, bool PAIRS, int MODE, int KMAX>
+template <class T, bool PAIRS, int MODE, int KMAX, int TPR>
 void launch_tiles(Launches& enqueue, Args a) {
   set_tile<T, PAIRS>(&a);
-  const size_t smem = (size_t)a.pitch * sizeof(T) * (PAIRS ? 2 : 1) * ROW_THREADS;
+  const size_t smem = (size_t)a.pitch * sizeof(T) * (PAIRS ? 2 : 1) * ROWS;
   if (smem > 40 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(rows_kernel<T, PAIRS, MODE, KMAX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(rows_kernel<T, PAIRS, MODE, KMAX, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) { enqueue.error = e; return; }
   }
-  const int64_t tiles = (a.n + ROW_THREADS - 1) / ROW_THREADS;
-  enqueue(rows_kernel<T, PAIRS, MODE, KMAX>, dim3((unsigned)std::min<int64_t>(tiles, 1 << 30)), ROW_THREADS, smem, a);
+  const int64_t tiles = (a.n + ROWS - 1) / ROWS;
+  enqueue(rows_kernel<T, PAIRS, MODE, KMAX, TPR>, dim3((unsigned)std::min<int64_t>(tiles, 1 << 30)), ROWS * TPR, smem, a);
 }
 template <class T, bool PAIRS, int MODE>
 void launch_team(Launches& enqueue, const Args& a) {
@@ -1114,10 +1218,13 @@ int class_call(Args a, int32_t type, int what, int in_place_ok, void* workspace,
         constexpr int MODE = decltype(mode)::value;
         constexpr bool PAIRS = decltype(both)::value;
         if (!by_thread(a, ts)) launch_team<T, PAIRS, MODE>(enqueue, a);
-        else if (MODE != FORWARD || a.k == 0) launch_tiles<T, PAIRS, MODE, 0>(enqueue, a);
+        else if (MODE != FORWARD || a.k == 0) {
+          if (a.C * ts >= TWO_THREADS_BYTES) launch_tiles<T, PAIRS, MODE, 0, 2>(enqueue, a);
+          else launch_tiles<T, PAIRS, MODE, 0, 1>(enqueue, a);
+        }
         else if constexpr (MODE == FORWARD) {
-          if (a.k <= 4) launch_tiles<T, PAIRS, MODE, 4>(enqueue, a);
-          else launch_tiles<T, PAIRS, MODE, MAX_TOP>(enqueue, a);
+          if (a.k <= 4) launch_tiles<T, PAIRS, MODE, 4, 1>(enqueue, a);
+          else launch_tiles<T, PAIRS, MODE, MAX_TOP, 1>(enqueue, a);
         }
       };
       const auto with = [&](auto mode) {
@@ -1146,7 +1253,7 @@ int class_call(Args a, int32_t type, int what, int in_place_ok, void* workspace,
     }
     if (a.k) launch_stream<T, true, false>(enqueue, a);
     else launch_stream<T, false, false>(enqueue, a);
-    enqueue(join_kernel<T>, dim3((unsigned)std::min<int64_t>((n + 3) / 4, 1 << 20)), 128, 0, a);
+    enqueue(join_kernel<T>, dim3((unsigned)std::min<int64_t>(n, 1 << 20)), JOIN_THREADS, 0, a);
     if (grad) launch_grad<T>(enqueue, a, sms);
     return 0;
   });

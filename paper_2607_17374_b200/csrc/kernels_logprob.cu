@@ -765,20 +765,27 @@ __global__ void __launch_bounds__(32 * WARPS, 4) stream_kernel(const Args a) {
     F2 s2 = f2(0.f, 0.f), t2 = s2;
     // Batches ahead, by asynchronous copies into places of the thread's own.  The first and the last vector of a span may be cut: those come by element.
     int place = 0;
+    const T* from = x + span.column(first + mine);
     const auto fetch = [&](int v0) {
+      Vec<T, V>* const to = &ahead[place * U * (32 * WARPS) + threadIdx.x];
+      if (v0 > first && v0 + U * TEAM < last) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int v = v0 + u * TEAM + mine;
-        Vec<T, V>* const to = &ahead[(place * U + u) * (32 * WARPS) + threadIdx.x];
-        if (v > first && v < last - 1) copy_async(to, x + span.column(v));
-        else if (v < last) *to = span.template load<LOAD_PLAIN>(v);
-        else {
-          Vec<T, V> none;
+        for (int u = 0; u < U; ++u) copy_async(to + u * (32 * WARPS), from + u * TEAM * V);
+      } else if (v0 < last) {
+#pragma unroll 1
+        for (int u = 0; u < U; ++u) {
+          const int v = v0 + u * TEAM + mine;
+          if (v > first && v < last - 1) copy_async(to + u * (32 * WARPS), from + u * TEAM * V);
+          else if (v < last) to[u * (32 * WARPS)] = span.template load<LOAD_PLAIN>(v);
+          else {
+            Vec<T, V> none;
 #pragma unroll
-          for (int i = 0; i < V; ++i) none.v[i] = from_f32<T>(-INFINITY);
-          *to = none;
+            for (int i = 0; i < V; ++i) none.v[i] = from_f32<T>(-INFINITY);
+            to[u * (32 * WARPS)] = none;
+          }
         }
       }
+      from += U * TEAM * V;
       asm volatile("cp.async.commit_group;" ::: "memory");
       place = place + 1 == AHEAD ? 0 : place + 1;
     };
@@ -1099,7 +1106,7 @@ __global__ void __launch_bounds__(256) grad_kernel(const Args a, int chunks) {
 // Rows that fit the registers of a warp: 32 elements a lane.  Pairs: 16-bit rows that begin at even elements everywhere.
 constexpr int TEAM_CLASSES = 1024;
 // Rows that a thread each takes: where there are enough of them, and a tile leaves room for other blocks beside it.
-constexpr int THREAD_ROWS = 4096, THREAD_BYTES = 512, TWO_THREADS_BYTES = 128;      // (from there on tiles leave an SM few threads: two to a row)
+constexpr int THREAD_ROWS = 4096, THREAD_BYTES = 512, TWO_THREADS_BYTES = 256;      // (from there on tiles leave an SM few threads: two to a row)
 inline bool by_thread(const Args& a, int ts) { return a.n >= THREAD_ROWS && a.C * ts <= THREAD_BYTES; }
 inline bool in_pairs(const Args& a, int ts, bool grad) {
   const auto even = [](const void* p, long long ld) { return rows_aligned(p, 4) && ld % 2 == 0; };

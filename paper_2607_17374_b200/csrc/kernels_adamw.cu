@@ -129,7 +129,7 @@ struct Places {
 };
 
 // A warp's 256 elements of a tensor, from b on.  whole: all 256 are there, in arrays that allow vectors.
-template <class PT, class GT, bool EIGHT, bool whole>
+template <class PT, class GT, bool EIGHT, bool MASTER, bool whole>
 __device__ __forceinline__ void step_block(const Args& a, const Tensor& t, const Factors f, unsigned long long key, long long b) {
   using P = Places<!EIGHT || sizeof(PT) == 4 || sizeof(GT) == 4>;
   const int lane = threadIdx.x & 31, first = P::lane_place(lane);
@@ -153,7 +153,7 @@ __device__ __forceinline__ void step_block(const Args& a, const Tensor& t, const
     } else {
       rm = P::template load<float>(mf, lane); rv = P::template load<float>(vf, lane);
     }
-    if (sizeof(PT) == 2 && t.master) rw = P::template load<float>(t.master + b, lane);
+    if (MASTER) rw = P::template load<float>(t.master + b, lane);
     else rp = P::template load<PT>(pp, lane);
     if (EIGHT) {
       codes_to_floats(cm, ms, m);
@@ -162,7 +162,7 @@ __device__ __forceinline__ void step_block(const Args& a, const Tensor& t, const
       to_floats<float>(rm, m);
       to_floats<float>(rv, v);
     }
-    if (sizeof(PT) == 2 && t.master) to_floats<float>(rw, p);
+    if (MASTER) to_floats<float>(rw, p);
     else to_floats<PT>(rp, p);
     to_floats<GT>(rg, g);
   } else {
@@ -172,7 +172,7 @@ __device__ __forceinline__ void step_block(const Args& a, const Tensor& t, const
       p[e] = g[e] = m[e] = v[e] = 0.f;
       if (in(e)) {
         const int at = first + P::element(e);
-        p[e] = sizeof(PT) == 2 && t.master ? t.master[b + at] : to_f32<PT>(pp[at]);
+        p[e] = MASTER ? t.master[b + at] : to_f32<PT>(pp[at]);
         g[e] = to_f32<GT>(gp[at]);
         if (EIGHT) {
           (e < 4 ? cm.x : cm.y) |= (uint32_t)mc[at] << (8 * (e & 3));
@@ -197,7 +197,7 @@ __device__ __forceinline__ void step_block(const Args& a, const Tensor& t, const
   }
   if (whole) {
     P::template store<PT>(pp, lane, p);
-    if (sizeof(PT) == 2 && t.master) P::template store<float>(t.master + b, lane, p);
+    if (MASTER) P::template store<float>(t.master + b, lane, p);
     if (!EIGHT) {
       P::template store<float>(mf, lane, m);
       P::template store<float>(vf, lane, v);
@@ -208,7 +208,7 @@ __device__ __forceinline__ void step_block(const Args& a, const Tensor& t, const
       if (in(e)) {
         const int at = first + P::element(e);
         pp[at] = from_f32<PT>(p[e]);
-        if (sizeof(PT) == 2 && t.master) t.master[b + at] = p[e];
+        if (MASTER) t.master[b + at] = p[e];
         if (!EIGHT) { mf[at] = m[e]; vf[at] = v[e]; }
       }
   }
@@ -243,43 +243,50 @@ __device__ __forceinline__ void step_block(const Args& a, const Tensor& t, const
     }
     const float part_m = __int_as_float(em < 234 ? (234 - em) << 23 : 1 << (256 - em)), part_v = __int_as_float((234 - ev) << 23);      // 2^(107 - e)
     const uint32_t base = (uint32_t)b ^ (uint32_t)key ^ (uint32_t)P::lane_place(lane), more = (uint32_t)(key >> 32) + (uint32_t)(b >> 32) * 0x85EBCA6Bu;     // (places differ in bits of their own)
-    uint32_t cm[E], cv[E];
+    uint32_t cm[E / 4], cv[E / 4];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float zm = __fmul_rz(m[e] * part_m, 0x1p-100f), zv = __fmul_rz(root[e] * part_v, 0x1p-100f);
-      const float least = fminf(v[e] * 0x1p100f, __uint_as_float(1u << 20));                          // code 1 where v is not 0
-      const uint32_t bits = finish_bits((base ^ (uint32_t)P::element(e)) + more);
-      cm[e] = ((__float_as_uint(zm) << 4) + __byte_perm(bits, 0, 0x4104)) | (__float_as_uint(m[e]) & 0x80000000u);
-      cv[e] = (__float_as_uint(fmaxf(zv, least)) << 4) + __byte_perm(bits, 0, 0x4324);
-    }
-    if (odd) {
+    for (int h = 0; h < E / 4; ++h) {
+      uint32_t wm[4], wv[4];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (!(fabsf(m[e]) < INFINITY)) cm[e] = CODE_NAN << 24;
-        if (!(v[e] < INFINITY)) cv[e] = CODE_NAN << 24;
+      for (int i = 0; i < 4; ++i) {
+        const int e = 4 * h + i;
+        const float zm = __fmul_rz(m[e] * part_m, 0x1p-100f), zv = __fmul_rz(root[e] * part_v, 0x1p-100f);
+        const float least = fminf(v[e] * 0x1p100f, __uint_as_float(1u << 20));                        // code 1 where v is not 0
+        const uint32_t bits = finish_bits((base ^ (uint32_t)P::element(e)) + more);
+        wm[i] = ((__float_as_uint(zm) << 4) + __byte_perm(bits, 0, 0x4104)) | (__float_as_uint(m[e]) & 0x80000000u);
+        wv[i] = (__float_as_uint(fmaxf(zv, least)) << 4) + __byte_perm(bits, 0, 0x4324);
       }
+      const auto four = [](const uint32_t* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410); };
+      cm[h] = four(wm);
+      cv[h] = four(wv);
+      if (odd)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t byte = 0xffu << (8 * i), nan = CODE_NAN << (8 * i);
+          if (!(fabsf(m[4 * h + i]) < INFINITY)) cm[h] = (cm[h] & ~byte) | nan;
+          if (!(v[4 * h + i] < INFINITY)) cv[h] = (cv[h] & ~byte) | nan;
+        }
     }
-    const auto four = [](const uint32_t* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410); };
     if (lane == 0) {
       t.m_scale[b / BLOCK] = __uint_as_float((uint32_t)em << 23);
       t.v_scale[b / BLOCK] = __uint_as_float((uint32_t)ev << 23);
     }
     if (whole) {
-      P::store_codes(mc, lane, make_uint2(four(cm), four(cm + 4)));
-      P::store_codes(vc, lane, make_uint2(four(cv), four(cv + 4)));
+      P::store_codes(mc, lane, make_uint2(cm[0], cm[1]));
+      P::store_codes(vc, lane, make_uint2(cv[0], cv[1]));
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (in(e)) { mc[first + P::element(e)] = (uint8_t)(cm[e] >> 24); vc[first + P::element(e)] = (uint8_t)(cv[e] >> 24); }
+        if (in(e)) { mc[first + P::element(e)] = (uint8_t)(cm[e / 4] >> (8 * (e % 4))); vc[first + P::element(e)] = (uint8_t)(cv[e / 4] >> (8 * (e % 4))); }
     }
   }
 }
 
-template <class PT, class GT, bool EIGHT>
-__device__ __noinline__ void step_block_by_element(const Args& a, const Tensor& t, const Factors f, unsigned long long key, long long b) { step_block<PT, GT, EIGHT, false>(a, t, f, key, b); }
+template <class PT, class GT, bool EIGHT, bool MASTER>
+__device__ __noinline__ void step_block_by_element(const Args& a, const Tensor& t, const Factors f, unsigned long long key, long long b) { step_block<PT, GT, EIGHT, MASTER, false>(a, t, f, key, b); }
 
-template <class PT, class GT, bool EIGHT>
-__global__ void __launch_bounds__(THREADS, 3) adamw_kernel(const __grid_constant__ Args a) {
+template <class PT, class GT, bool EIGHT, bool MASTER>
+__global__ void __launch_bounds__(THREADS, EIGHT && !MASTER ? 4 : 3) adamw_kernel(const __grid_constant__ Args a) {
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const long long step = *a.step;
   if (step < 1) {
@@ -308,20 +315,22 @@ __global__ void __launch_bounds__(THREADS, 3) adamw_kernel(const __grid_constant
     const long long i0 = (tile - t.first_tile) * TILE, most = i0 + TILE < t.count ? i0 + TILE : t.count;
 #pragma unroll 1
     for (long long b = i0 + (threadIdx.x >> 5) * BLOCK; b < most; b += THREADS * E) {
-      if (t.vectors && b + BLOCK <= most) step_block<PT, GT, EIGHT, true>(a, t, f, key, b);
-      else step_block_by_element<PT, GT, EIGHT>(a, t, f, key, b);
+      if (t.vectors && b + BLOCK <= most) step_block<PT, GT, EIGHT, MASTER, true>(a, t, f, key, b);
+      else step_block_by_element<PT, GT, EIGHT, MASTER>(a, t, f, key, b);
     }
   }
 }
 
 // f(tags of the parameters' and the gradients' type, of the states' kind): tensors are stepped by kind, a launch each.
-constexpr int KINDS = 18;
-inline int kind_of(int32_t p, int32_t g, bool eight) { return (eight * 3 + p) * 3 + g; }
+constexpr int KINDS = 36;
+inline int kind_of(int32_t p, int32_t g, bool eight, bool master) { return ((master * 2 + eight) * 3 + p) * 3 + g; }
 template <class F>
 void with_kind(int kind, F f) {
   with_row_type(kind / 3 % 3, [&](auto pt) {
     return with_row_type(kind % 3, [&](auto gt) {
-      if (kind >= 9) f(pt, gt, std::true_type()); else f(pt, gt, std::false_type());
+      const auto with = [&](auto master) { if (kind / 9 % 2) f(pt, gt, std::true_type(), master); else f(pt, gt, std::false_type(), master); };
+      if constexpr (sizeof(typename decltype(pt)::type) == 2) { if (kind >= 18) { with(std::true_type()); return 0; } }
+      with(std::false_type());
       return 0;
     });
   });
@@ -376,7 +385,7 @@ int adamw_create(taurus_adamw** out, const taurus_adamw_tensor* list, int64_t co
     t.p = c.param; t.g = c.grad; t.m = c.m; t.v = c.v; t.m_scale = c.m_scale; t.v_scale = c.v_scale; t.master = c.master; t.count = c.count;
     t.decay = c.weight_decay; t.p_type = c.param_type; t.g_type = c.grad_type; t.index = (uint32_t)k;
     t.vectors = rows_aligned(c.param, 16) && rows_aligned(c.grad, 16) && rows_aligned(c.m, eight ? 8 : 16) && rows_aligned(c.v, eight ? 8 : 16) && (!c.master || rows_aligned(c.master, 16));
-    std::vector<int32_t>& mine = tiles[kind_of(c.param_type, c.grad_type, eight)];
+    std::vector<int32_t>& mine = tiles[kind_of(c.param_type, c.grad_type, eight, c.master != nullptr)];
     t.first_tile = (long long)mine.size();
     const long long more = (c.count + TILE - 1) / TILE;
     all += more;
@@ -412,10 +421,10 @@ int adamw_create(taurus_adamw** out, const taurus_adamw_tensor* list, int64_t co
       h->tile_tensor[k] = at;
       at += h->tiles[k];
       e = cudaMemcpy(h->tile_tensor[k], tiles[k].data(), tiles[k].size() * 4, cudaMemcpyHostToDevice);
-      with_kind(k, [&](auto pt, auto gt, auto eight) {
+      with_kind(k, [&](auto pt, auto gt, auto eight, auto master) {
         using PT = typename decltype(pt)::type;
         using GT = typename decltype(gt)::type;
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&h->resident[k], adamw_kernel<PT, GT, decltype(eight)::value>, THREADS, 0);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&h->resident[k], adamw_kernel<PT, GT, decltype(eight)::value, decltype(master)::value>, THREADS, 0);
       });
     }
   }
@@ -465,10 +474,10 @@ extern "C" int taurus_adamw_step(taurus_adamw* h, const int64_t* step, const flo
     a.tile_tensor = h->tile_tensor[k]; a.tiles = h->tiles[k];
     const dim3 grid((unsigned)std::min<long long>(a.tiles, (long long)h->sms * std::max(h->resident[k], 1)));
     enqueue.early = false;                       // the kernels do not wait for one another: they touch different tensors, in stream order
-    with_kind(k, [&](auto pt, auto gt, auto eight) {
+    with_kind(k, [&](auto pt, auto gt, auto eight, auto master) {
       using PT = typename decltype(pt)::type;
       using GT = typename decltype(gt)::type;
-      enqueue(adamw_kernel<PT, GT, decltype(eight)::value>, grid, THREADS, 0, a);
+      enqueue(adamw_kernel<PT, GT, decltype(eight)::value, decltype(master)::value>, grid, THREADS, 0, a);
     });
   }
   return enqueue.done("taurus_adamw_step");

@@ -1,176 +1,7 @@
-// Log probabilities of given classes from rows of logits, with the entropy and the top alternatives, and the gradient of the logits.
-//
-//   m = max x,  l = log sum e^(x - m),  log p_j = (x_j - m) - l,  H = -sum p log p = l - (sum e^(x - m) (x - m)) / e^l
-//   grad x_j = g (delta_j,label - p_j) - h p_j (log p_j + H)           g: weight of log p_label, h: weight of H
-//
-// The largest term of the sum is 1: it is left out of the sum s of the others, and l = log1p(s), H = l - t / (1 + s).  Both parts of H are positive and nothing
-// cancels: a row whose first class has nearly everything keeps all digits of l, H and 1 - p.  Differences are cut off at -200 (e^-200 = 0 in fp32): a
-// masked class (-inf, or a type's lowest value) then adds 0 to both sums, and no 0 x inf comes up.  A NaN goes into m, and with it into everything; +inf is treated as NaN.
-//
-// Bytes bound it: the logits in, once (and their gradient out).
-// Rows that fit the registers of 2, 8 or 32 lanes are read once and stay there, for the gradient too (team_kernel).  Wider ones are the work of a warp or a block, or of several
-// blocks where there are few rows (stream_kernel, join_kernel): every thread keeps a maximum and sums of its own over its vectors, without a branch, and they are joined at the end.
-// The term that is 1 stands in one thread's sum and has eaten that thread's small terms: its vectors are read again without it, by all threads.  The top needs no work in
-// the pass either: with the k-th largest of the threads' maxima known, the top k are in the vectors of the k threads whose maxima are not below it, and only those are looked
-// through again.
-#include <algorithm>
-
-#include "rows.cuh"
+// Class log probabilities: the top's candidates, rows in registers, wide rows and their parts, the entry points (see logprob.cuh).
+#include "logprob.cuh"
 
 namespace {
-
-constexpr int MAX_TOP = TAURUS_MAX_TOP;
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LEAST = -200.f;
-constexpr int ROWS = 128;                      // rows of a block of rows_kernel
-constexpr int WARPS = 8;                       // warps of a block of the others
-constexpr int LIST = 64;                       // places of a warp's list of candidates
-constexpr int MAX_PARTS = 64;                  // parts of a row
-
-typedef unsigned long long u64;
-
-struct Args {
-  long long n;
-  int C;
-  const void* x;
-  long long ld;
-  const long long* labels;
-  float *logprob, *entropy;
-  float2* stats;
-  int k;
-  float* top_logprob;
-  long long* top_class;
-  // gradient
-  const float *grad_logprob, *grad_entropy;
-  const float2* stats_in;
-  const float* entropy_in;
-  void* dx;
-  long long ld_dx;
-  int32_t* status;
-  // parts of a row
-  int parts, part_len;
-  float4* part;                                // [n x parts] (m, s, t, bad)
-  u64* part_top;                               // [n x parts x k]
-  // tiles of rows_kernel
-  int pitch, mode_in, mode_out;
-  unsigned by_C, by_vectors;                   // 2^32 / C, 2^32 / vectors of a row, rounded up
-  int vectors;
-};
-
-__device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
-
-__device__ __forceinline__ float fma_sat(float a, float b, float c) { float r; asm("fma.rn.sat.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
-__device__ __forceinline__ float mul_sat(float a, float b) { float r; asm("mul.rn.sat.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
-// (m - x) / 256, at most 1, for m8 = m / 256: the cut that keeps infinities out, in the same instruction as the difference (minima, comparisons and selections go at half
-// the rate of multiplications).  Scaling by 2^-8 is exact.  Of two infinities: 0.
-constexpr float CUT = 256.f;
-__device__ __forceinline__ float below(float x, float m8) { return fma_sat(x, -1.f / CUT, m8); }
-__device__ __forceinline__ float exp_below(float z) { return ex2(z * (-CUT * LOG2E)); }
-// Pairs of fp32 values and their arithmetic in one instruction.
-struct F2 { u64 v; };
-__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ void split(F2 x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x.v)); }
-__device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
-
-// Sums over classes with the maximum known, two at a time: s without the terms that equal it (weight 0; else 1), q of z e^-256z, others: how many are below.
-struct RowSums {
-  F2 s = {0}, q = {0}, others = {0};
-  __device__ __forceinline__ void add2(float x, float y, float m8) {
-    const float zx = below(x, m8), zy = below(y, m8);
-    const F2 z = f2(zx, zy), w = f2(mul_sat(zx, 0x1p126f), mul_sat(zy, 0x1p126f));
-    float a, b;
-    split(mul(z, f2(-CUT * LOG2E, -CUT * LOG2E)), &a, &b);
-    const F2 e = f2(ex2(a), ex2(b));
-    s = fma(e, w, s);
-    q = fma(e, z, q);
-    others = add(others, w);
-  }
-  __device__ __forceinline__ static float both(F2 x) { float a, b; split(x, &a, &b); return a + b; }
-};
-
-// Order of candidates: larger value first, of equal ones the lower class.  0: none (-inf, NaN).  -0 counts as 0.
-__device__ __forceinline__ u64 key_of(float x, int cls) {
-  if (!(x > -INFINITY)) return 0;
-  const uint32_t b = __float_as_uint(x + 0.f);
-  const uint32_t o = b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
-  return ((u64)o << 32) | (0xffffffffu - (uint32_t)cls);
-}
-__device__ __forceinline__ float key_value(u64 key) {
-  const uint32_t o = (uint32_t)(key >> 32);
-  return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu));
-}
-__device__ __forceinline__ int key_class(u64 key) { return (int)(0xffffffffu - (uint32_t)key); }
-
-// Sums of some classes of a row.  m: their largest value, whose own term (1) is in neither sum; -inf: no classes yet.
-struct Sums { float m, s, t; };
-// Joins b's classes, which come behind a's.
-__device__ __forceinline__ void join(Sums& a, const Sums& b) {
-  if (!(b.m > -INFINITY)) return;
-  if (!(a.m > -INFINITY)) { a = b; return; }
-  const bool up = b.m > a.m;
-  const float d = fmaxf(up ? a.m - b.m : b.m - a.m, LEAST), f = ex2(d * LOG2E);
-  const float ws = up ? b.s : a.s, wt = up ? b.t : a.t, os = up ? a.s : b.s, ot = up ? a.t : b.t;     // the side of the maximum, the other side
-  const float o1 = 1.f + os;
-  a.s = fmaf(o1, f, ws);
-  a.t = wt + f * fmaf(o1, d, ot);
-  if (up) a.m = b.m;
-}
-
-// What a row's sums say.
-struct RowResult { float m, l, H; };
-__device__ __forceinline__ RowResult row_result(const Sums& s, bool bad) {
-  if (bad) return {NAN, NAN, NAN};
-  if (!(s.m > -INFINITY)) return {s.m, 0.f, 0.f};
-  const float l = log1pf(s.s);
-  return {s.m, l, l - __fdividef(s.t, 1.f + s.s)};
-}
-__device__ __forceinline__ float log_p(float x, const RowResult& r) { return r.m == -INFINITY ? -INFINITY : (x - r.m) - r.l; }
-
-// -1: no label; one outside the classes is reported.
-__device__ __forceinline__ int label_of(const Args& a, long long row) {
-  if (!a.labels) return -1;
-  const long long v = a.labels[row];
-  if (v < -1 || v >= a.C) { rows_status(a.status, TAURUS_ERR_INVALID_ARG); return -1; }
-  return (int)v;
-}
-template <class T>
-__device__ __forceinline__ void write_row(const Args& a, long long row, int label, const RowResult& r) {
-  if (a.logprob) a.logprob[row] = label < 0 ? 0.f : log_p(to_f32<T>(static_cast<const T*>(a.x)[row * a.ld + label]), r);
-  if (a.entropy) a.entropy[row] = r.H;
-  if (a.stats) a.stats[row] = make_float2(r.m, r.l);
-}
-__device__ __forceinline__ void write_top(const Args& a, long long row, int i, u64 key, const RowResult& r) {
-  if (a.top_logprob) a.top_logprob[row * a.k + i] = key ? log_p(key_value(key), r) : -INFINITY;
-  if (a.top_class) a.top_class[row * a.k + i] = key ? key_class(key) : -1;
-}
-
-// What the gradient of a row needs.
-struct GradRow {
-  float m8, l, H, g, h, c;                       // m8: the maximum / 256
-  int label;
-};
-__device__ __forceinline__ GradRow grad_row(const Args& a, long long row, int label, const RowResult& r) {
-  const float g = label >= 0 && a.grad_logprob ? a.grad_logprob[row] : 0.f, h = a.grad_entropy ? a.grad_entropy[row] : 0.f;
-  if (r.m == -INFINITY) return {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, label};                        // all masked
-  return {r.m * (1.f / CUT), r.l, r.H, g, h, h == 0.f ? -g : fmaf(-h, r.H, -g), label};
-}
-__device__ __forceinline__ float grad_of(const GradRow& r, float x) {
-  const float lp = fmaf(below(x, r.m8), -CUT, -r.l), p = ex2(lp * LOG2E);
-  return p * fmaf(-r.h, lp, r.c);                // (masked: p = 0)
-}
-__device__ __forceinline__ void grad_of2(const GradRow& r, float x, float y, float* dx, float* dy) {
-  const F2 lp = fma(f2(below(x, r.m8), below(y, r.m8)), f2(-CUT, -CUT), f2(-r.l, -r.l));
-  float a, b;
-  split(mul(lp, f2(LOG2E, LOG2E)), &a, &b);
-  split(mul(f2(ex2(a), ex2(b)), fma(f2(-r.h, -r.h), lp, f2(r.c, r.c))), dx, dy);
-}
-__device__ __forceinline__ float grad_of_label(const GradRow& r, float x) {
-  const float lp = fmaf(below(x, r.m8), -CUT, -r.l), p = ex2(lp * LOG2E);
-  return x == -INFINITY ? 0.f : -r.g * expm1f(lp) - r.h * p * (lp + r.H);
-}
 
 // ---- the top: candidates of a warp ---------------------------------------------------------------------------------------------------------------------
 
@@ -211,324 +42,6 @@ __device__ __noinline__ int rank_of_lanes(float mine) {
 #pragma unroll 8
   for (int i = 0; i < 32; ++i) { const float o = __shfl_sync(0xffffffffu, mine, i); rank += o > mine || (o == mine && i < lane); }
   return rank;
-}
-
-enum { FORWARD = 0, TRAIN = 1, GRAD = 2 };
-
-// What a lane loads at once: an element, or two where 16-bit rows have an even width.
-template <class T, bool PAIRS> struct Word { using type = T; static constexpr int n = 1; };
-template <class T> struct Word<T, true> { using type = uint32_t; static constexpr int n = 2; };
-template <class T>
-__device__ __forceinline__ void unpack(T w, float (&x)[1]) { x[0] = to_f32<T>(w); }
-template <class T>
-__device__ __forceinline__ void unpack(uint32_t w, float (&x)[2]) {
-  if constexpr (std::is_same_v<T, __nv_bfloat16>) { x[0] = __uint_as_float(w << 16); x[1] = __uint_as_float(w & 0xffff0000u); }
-  else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); x[0] = f.x; x[1] = f.y; }
-}
-template <class T>
-__device__ __forceinline__ T pack(const float (&x)[1]) { return from_f32<T>(x[0]); }
-template <class T>
-__device__ __forceinline__ uint32_t pack(const float (&x)[2]) {
-  if constexpr (std::is_same_v<T, __nv_bfloat16>) { const __nv_bfloat162 r = __floats2bfloat162_rn(x[0], x[1]); return *reinterpret_cast<const uint32_t*>(&r); }
-  else { const __half2 r = __floats2half2_rn(x[0], x[1]); return *reinterpret_cast<const uint32_t*>(&r); }
-}
-
-// ---- few classes: a thread to a row of a tile in shared memory ---------------------------------------------------------------------------------------
-
-// How a tile of rows lies in global memory: single elements | 16-byte vectors over rows without gaps | vectors within rows of a pitch.
-enum { TILE_ELEMENTS = 0, TILE_FLAT = 1, TILE_VECTORS = 2 };
-// Brings a tile of `rows` rows of C words in and out.  P: words of a row in shared memory.
-template <class W>
-struct Tile {
-  static constexpr int V = 16 / (int)sizeof(W);
-  int rows, C, P, vectors;
-  unsigned by_C, by_vectors;
-  __device__ __forceinline__ unsigned div(unsigned f, unsigned by) const { return by ? __umulhi(f, by) : f; }     // f < 2^16
-  // The places of a vector's words: those that reach into the next row are P - C further.  (Rows shorter than a vector: any number of rows further.)
-  __device__ __forceinline__ void places(int f, int (&at)[V]) const {
-    const int row = div(f, by_C), col = f - row * C;
-    if (C >= V) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) at[i] = row * P + col + i + (col + i >= C ? P - C : 0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) { const int r = div(f + i, by_C); at[i] = r * P + f + i - r * C; }
-    }
-  }
-  __device__ __forceinline__ void load(W* sm, const W* x, long long ld, int mode) const {
-    if (mode == TILE_ELEMENTS) {
-      for (int f = threadIdx.x; f < rows * C; f += (int)blockDim.x) { const int row = div(f, by_C), col = f - row * C; sm[row * P + col] = x[row * ld + col]; }
-      return;
-    }
-    const bool flat = mode == TILE_FLAT;
-    const int words = rows * C, total = flat ? words / V : rows * vectors;
-    for (int v0 = threadIdx.x; v0 < total; v0 += 4 * (int)blockDim.x) {
-      Vec<W, V> r[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int v = v0 + u * (int)blockDim.x;
-        if (v >= total) break;
-        if (flat) r[u] = load_vec<Vec<W, V>, LOAD_ONCE>(x + v * V);
-        else {
-          const int row = div(v, by_vectors), col = (v - row * vectors) * V;
-          const W* const p = x + row * ld + col;
-          if (col + V <= C) r[u] = load_vec<Vec<W, V>, LOAD_ONCE>(p);
-          else
-#pragma unroll
-            for (int i = 0; i < V; ++i) if (col + i < C) r[u].v[i] = p[i];
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int v = v0 + u * (int)blockDim.x;
-        if (v >= total) break;
-        if (flat && P == C) store_vec(sm + v * V, r[u]);
-        else if (flat) {
-          int at[V];
-          places(v * V, at);
-#pragma unroll
-          for (int i = 0; i < V; ++i) sm[at[i]] = r[u].v[i];
-        } else {
-          const int row = div(v, by_vectors), col = (v - row * vectors) * V;
-#pragma unroll
-          for (int i = 0; i < V; ++i) if (col + i < C) sm[row * P + col + i] = r[u].v[i];
-        }
-      }
-    }
-    if (flat)
-      for (int f = total * V + threadIdx.x; f < words; f += (int)blockDim.x) { const int row = div(f, by_C); sm[row * P + f - row * C] = x[f]; }
-  }
-  __device__ __forceinline__ void store(const W* sm, W* y, long long ld, int mode) const {
-    if (mode == TILE_FLAT) {
-      const int words = rows * C, total = words / V;
-      for (int v = threadIdx.x; v < total; v += (int)blockDim.x) {
-        Vec<W, V> r;
-        if (P == C) r = load_vec<Vec<W, V>>(sm + v * V);
-        else {
-          int at[V];
-          places(v * V, at);
-#pragma unroll
-          for (int i = 0; i < V; ++i) r.v[i] = sm[at[i]];
-        }
-        store_vec_once(y + v * V, r);
-      }
-      for (int f = total * V + threadIdx.x; f < words; f += (int)blockDim.x) { const int row = div(f, by_C); y[f] = sm[row * P + f - row * C]; }
-    } else if (mode == TILE_VECTORS) {
-      for (int v = threadIdx.x; v < rows * vectors; v += (int)blockDim.x) {
-        const int row = div(v, by_vectors), col = (v - row * vectors) * V;
-        W* const p = y + row * ld + col;
-        if (col + V <= C) {
-          Vec<W, V> r;
-#pragma unroll
-          for (int i = 0; i < V; ++i) r.v[i] = sm[row * P + col + i];
-          store_vec_once(p, r);
-        } else {
-          for (int i = 0; col + i < C; ++i) p[i] = sm[row * P + col + i];
-        }
-      }
-    } else {
-      for (int f = threadIdx.x; f < rows * C; f += (int)blockDim.x) { const int row = div(f, by_C), col = f - row * C; y[row * ld + col] = sm[row * P + col]; }
-    }
-  }
-};
-
-
-// TPR threads to a row, which take its words in turn.  KMAX: places for the top in registers (k <= KMAX; 0: none asked for; with a top TPR is 1).
-template <class T, bool PAIRS, int MODE, int KMAX, int TPR>
-__global__ void __launch_bounds__(ROWS * TPR) rows_kernel(const Args a) {
-  extern __shared__ __align__(16) unsigned char logprob_shared[];
-  using W = typename Word<T, PAIRS>::type;
-  constexpr int NW = Word<T, PAIRS>::n, STEP = 8 / NW;      // words of 8 classes
-  W* const sm = reinterpret_cast<W*>(logprob_shared);
-  const int C = a.C, all = C / NW, sub = threadIdx.x % TPR, CW = (all - sub + TPR - 1) / TPR;      // CW: words of this thread
-  const long long tiles = (a.n + ROWS - 1) / ROWS;
-  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const long long row0 = tile * ROWS, row = row0 + threadIdx.x / TPR;
-    const Tile<W> t = {(int)(a.n - row0 < ROWS ? a.n - row0 : ROWS), all, a.pitch, a.vectors, a.by_C, a.by_vectors};
-    t.load(sm, reinterpret_cast<const W*>(static_cast<const T*>(a.x) + row0 * a.ld), a.ld / NW, a.mode_in);
-    const int label = row < a.n ? label_of(a, row) : -1;
-    __syncthreads();
-    if (TPR > 1 || row < a.n) {                  // (exchanges take all threads of a warp: rows behind the last are whatever the tile held)
-      W* const whole_row = sm + threadIdx.x / TPR * a.pitch;
-      W* const mine = whole_row + sub;           // its words are TPR apart
-      const T* const elements = reinterpret_cast<const T*>(whole_row);
-      RowResult r;
-      if (MODE != GRAD) {
-        // Maxima of G classes of classes: the k-th largest of them has k values at least that are not below it, so what is below it is not among the top k.
-        constexpr int G = KMAX <= 4 ? 8 : 32;
-        float most[G];
-        if constexpr (NW == 2) {
-          using T2 = std::conditional_t<std::is_same_v<T, __nv_bfloat16>, __nv_bfloat162, __half2>;
-          T2 two[G / 2];
-          const T least = from_f32<T>(-INFINITY);
-          T2 none;
-          none.x = none.y = least;
-#pragma unroll
-          for (int i = 0; i < G / 2; ++i) two[i] = none;
-          int j = 0;
-          for (; j + G / 2 <= CW; j += G / 2)
-#pragma unroll
-            for (int i = 0; i < G / 2; ++i) two[i] = __hmax2_nan(two[i], reinterpret_cast<const T2*>(mine)[(j + i) * TPR]);
-#pragma unroll
-          for (int i = 0; i < G / 2; ++i) if (j + i < CW) two[i] = __hmax2_nan(two[i], reinterpret_cast<const T2*>(mine)[(j + i) * TPR]);
-#pragma unroll
-          for (int i = 0; i < G / 2; ++i) { most[2 * i] = to_f32<T>(two[i].x); most[2 * i + 1] = to_f32<T>(two[i].y); }
-        } else {
-#pragma unroll
-          for (int i = 0; i < G; ++i) most[i] = -INFINITY;
-          int j = 0;
-          for (; j + G <= CW; j += G)
-#pragma unroll
-            for (int i = 0; i < G; ++i) most[i] = max_nan(most[i], to_f32<T>(reinterpret_cast<const T*>(mine)[(j + i) * TPR]));
-#pragma unroll
-          for (int i = 0; i < G; ++i) if (j + i < CW) most[i] = max_nan(most[i], to_f32<T>(reinterpret_cast<const T*>(mine)[(j + i) * TPR]));
-        }
-        float m = most[0];
-#pragma unroll
-        for (int i = 1; i < G; ++i) m = max_nan(m, most[i]);
-#pragma unroll
-        for (int d = TPR / 2; d; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
-        const bool bad = !(m < INFINITY);
-        float top[KMAX ? KMAX : 1], floor = -INFINITY;
-        int cls[KMAX ? KMAX : 1];
-        if (KMAX) {
-#pragma unroll
-          for (int i = 0; i < KMAX; ++i) { top[i] = -INFINITY; cls[i] = -1; }
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            float v = most[g];
-#pragma unroll
-            for (int i = 0; i < KMAX; ++i) { const float up = fmaxf(top[i], v); v = fminf(top[i], v); top[i] = up; }
-          }
-#pragma unroll
-          for (int i = 0; i < KMAX; ++i) if (i == a.k - 1) floor = top[i];
-          if (bad) floor = -INFINITY;                       // a NaN hides its class of classes
-#pragma unroll
-          for (int i = 0; i < KMAX; ++i) top[i] = -INFINITY;
-        }
-        // The sums, and the top's candidates, 64 classes at a time.
-        RowSums sum;
-        int behind = 0;
-        const float m8 = m * (1.f / CUT);
-        for (int j0 = 0; j0 < CW; j0 += 64 / NW) {
-          uint32_t found[2] = {0, 0};
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-#pragma unroll 1
-            for (int i0 = 0; i0 < 32 / NW; i0 += STEP) {
-              const int j1 = j0 + half * (32 / NW) + i0;
-              if (j1 >= CW) break;
-              // 8 classes; behind the row's end a class that is masked adds nothing to s and q (and one to others)
-              float v[8];
-              if (j1 + STEP <= CW) {
-#pragma unroll
-                for (int i = 0; i < STEP; ++i) {
-                  float w[NW];
-                  unpack<T>(mine[(j1 + i) * TPR], w);
-#pragma unroll
-                  for (int e = 0; e < NW; ++e) v[i * NW + e] = w[e];
-                }
-              } else {
-#pragma unroll
-                for (int i = 0; i < STEP; ++i) {
-                  float w[NW];
-#pragma unroll
-                  for (int e = 0; e < NW; ++e) w[e] = -INFINITY;
-                  if (j1 + i < CW) unpack<T>(mine[(j1 + i) * TPR], w);
-#pragma unroll
-                  for (int e = 0; e < NW; ++e) v[i * NW + e] = w[e];
-                }
-                behind = (j1 + STEP - CW) * NW;
-              }
-              uint32_t bits = 0;
-#pragma unroll
-              for (int e = 0; e < 8; e += 2) {
-                sum.add2(v[e], v[e + 1], m8);
-                if (KMAX) {
-                  if (v[e] >= floor) bits |= 1u << e;
-                  if (v[e + 1] >= floor) bits |= 2u << e;
-                }
-              }
-              if (KMAX) found[half] |= bits << (i0 * NW);
-            }
-          if (KMAX)
-            while (found[0] | found[1]) {
-              const bool low = found[0] != 0;
-              const uint32_t bits = low ? found[0] : found[1];
-              const int at = j0 * NW + (low ? 0 : 32) + __ffs(bits) - 1;
-              if (low) found[0] = bits & (bits - 1); else found[1] = bits & (bits - 1);
-              const float v = at < C ? to_f32<T>(elements[at]) : -INFINITY;
-              if (v > top[KMAX - 1]) {                     // equal ones keep their places: they have the lower classes
-#pragma unroll
-                for (int i = KMAX - 1; i > 0; --i) {
-                  const bool down = v > top[i - 1], here = !down && v > top[i];
-                  cls[i] = down ? cls[i - 1] : here ? at : cls[i];
-                  top[i] = down ? top[i - 1] : here ? v : top[i];
-                }
-                if (v > top[0]) { top[0] = v; cls[0] = at; }
-              }
-            }
-        }
-        float sums = sum.both(sum.s), q = sum.both(sum.q), others = sum.both(sum.others) - (float)behind;
-#pragma unroll
-        for (int d = TPR / 2; d; d >>= 1) {
-          sums += __shfl_xor_sync(0xffffffffu, sums, d);
-          q += __shfl_xor_sync(0xffffffffu, q, d);
-          others += __shfl_xor_sync(0xffffffffu, others, d);
-        }
-        r = row_result({m, sums + ((float)(C - 1) - others), -CUT * q}, bad);
-        if (sub == 0 && row < a.n) {
-          if (a.logprob) a.logprob[row] = label < 0 ? 0.f : log_p(to_f32<T>(elements[label]), r);
-          if (a.entropy) a.entropy[row] = r.H;
-          if (a.stats) a.stats[row] = make_float2(r.m, r.l);
-        }
-#pragma unroll
-        for (int i = 0; i < KMAX; ++i)
-          if (i < a.k) {
-            if (a.top_logprob) a.top_logprob[row * a.k + i] = cls[i] < 0 ? -INFINITY : log_p(top[i], r);
-            if (a.top_class) a.top_class[row * a.k + i] = cls[i];
-          }
-      } else {
-        const long long from = row < a.n ? row : a.n - 1;
-        const float2 ml = a.stats_in[from];
-        r = {ml.x, ml.y, a.entropy_in ? a.entropy_in[from] : 0.f};
-      }
-      if (MODE != FORWARD) {
-        const GradRow gr = grad_row(a, row < a.n ? row : a.n - 1, label, r);
-        const bool special = label >= 0 && label / NW % TPR == sub;              // this thread has the label's word
-        const float at = special ? to_f32<T>(elements[label]) : 0.f;
-        if (TPR > 1) __syncwarp();               // (its logit has been read for the row's log probability too)
-        int j = 0;
-        for (; j + STEP <= CW; j += STEP) {
-          W w[STEP];
-#pragma unroll
-          for (int i = 0; i < STEP; ++i) w[i] = mine[(j + i) * TPR];
-#pragma unroll
-          for (int i = 0; i < STEP; i += 2 / NW) {
-            float v[2], y[2];
-            if constexpr (NW == 2) unpack<T>(w[i], v);
-            else { v[0] = to_f32<T>(w[i]); v[1] = to_f32<T>(w[i + 1]); }
-            grad_of2(gr, v[0], v[1], y, y + 1);
-            if constexpr (NW == 2) mine[(j + i) * TPR] = pack<T>(y);
-            else { mine[(j + i) * TPR] = from_f32<T>(y[0]); mine[(j + i + 1) * TPR] = from_f32<T>(y[1]); }
-          }
-        }
-        for (; j < CW; ++j) {
-          float v[NW];
-          unpack<T>(mine[j * TPR], v);
-#pragma unroll
-          for (int e = 0; e < NW; ++e) v[e] = grad_of(gr, v[e]);
-          mine[j * TPR] = pack<T>(v);
-        }
-        if (special) reinterpret_cast<T*>(whole_row)[label] = from_f32<T>(grad_of_label(gr, at));
-      }
-    }
-    __syncthreads();
-    if (MODE != FORWARD) {
-      t.store(sm, reinterpret_cast<W*>(static_cast<T*>(a.dx) + row0 * a.ld_dx), a.ld_dx / NW, a.mode_out);
-      __syncthreads();
-    }
-  }
 }
 
 // ---- rows in the registers of a team of lanes ----------------------------------------------------------------------------------------------------------
@@ -1106,8 +619,13 @@ __global__ void __launch_bounds__(256) grad_kernel(const Args a, int chunks) {
 // Rows that fit the registers of a warp: 32 elements a lane.  Pairs: 16-bit rows that begin at even elements everywhere.
 constexpr int TEAM_CLASSES = 1024;
 // Rows that a thread each takes: where there are enough of them, and a tile leaves room for other blocks beside it.
-constexpr int THREAD_ROWS = 4096, THREAD_BYTES = 512, TWO_THREADS_BYTES = 256;      // (from there on tiles leave an SM few threads: two to a row)
-inline bool by_thread(const Args& a, int ts) { return a.n >= THREAD_ROWS && a.C * ts <= THREAD_BYTES; }
+constexpr int THREAD_ROWS = 4096;
+// fp32 rows of some length are better in registers, read once, than three times from a tile: 100 000 x 1 000 with the gradient 133 / 182 us, 256 69 / 67, without it and without a top
+// 91 / 110 (600: 79 / 68), with 16 top alternatives 297 / 431 (400: 215 / 212).  All others, 16 bits above all, are better in tiles (400 bf16: 85 / 49, with 4 alternatives 166 / 45).
+inline bool by_tile(const Args& a, int ts, bool grad) {
+  if (a.n < THREAD_ROWS || a.C > TEAM_CLASSES) return false;
+  return ts == 2 || a.C <= (grad ? 384 : a.k == 0 ? 768 : a.k > 8 ? 512 : TEAM_CLASSES);
+}
 inline bool in_pairs(const Args& a, int ts, bool grad) {
   const auto even = [](const void* p, long long ld) { return rows_aligned(p, 4) && ld % 2 == 0; };
   return ts == 2 && a.C % 2 == 0 && even(a.x, a.ld) && (!grad || even(a.dx, a.ld_dx));
@@ -1136,35 +654,6 @@ Space space_of(int64_t n, int C, int k) {
   return s;
 }
 
-template <class T, bool PAIRS>
-void set_tile(Args* a) {
-  constexpr int NW = PAIRS ? 2 : 1, V = 16 / (NW * (int)sizeof(T));               // elements of a word, words of a vector
-  const int C = a->C / NW;
-  // A thread's row begins pitch words behind its neighbour's: with a common divisor d of pitch and 32, d threads of a warp meet in a bank.  Up to four cost less than rows set apart, which
-  // cannot be copied by vectors.  (Rows of 16-bit elements have odd widths here.)
-  a->pitch = sizeof(T) * NW == 4 && C % 8 == 0 ? C + 1 : C;
-  const auto by = [](int d) { return d == 1 ? 0u : (unsigned)(((1ull << 32) + d - 1) / d); };
-  a->vectors = (C + V - 1) / V;
-  a->by_C = by(C); a->by_vectors = by(a->vectors);
-  const auto mode = [&](const void* p, long long ld) {
-    if (!rows_aligned(p, 16)) return (int)TILE_ELEMENTS;
-    return ld == a->C ? (int)TILE_FLAT : ld % (V * NW) == 0 ? (int)TILE_VECTORS : (int)TILE_ELEMENTS;
-  };
-  a->mode_in = mode(a->x, a->ld);
-  a->mode_out = mode(a->dx, a->ld_dx);
-}
-
-template <class T, bool PAIRS, int MODE, int KMAX, int TPR>
-void launch_tiles(Launches& enqueue, Args a) {
-  set_tile<T, PAIRS>(&a);
-  const size_t smem = (size_t)a.pitch * sizeof(T) * (PAIRS ? 2 : 1) * ROWS;
-  if (smem > 40 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(rows_kernel<T, PAIRS, MODE, KMAX, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) { enqueue.error = e; return; }
-  }
-  const int64_t tiles = (a.n + ROWS - 1) / ROWS;
-  enqueue(rows_kernel<T, PAIRS, MODE, KMAX, TPR>, dim3((unsigned)std::min<int64_t>(tiles, 1 << 30)), ROWS * TPR, smem, a);
-}
 template <class T, bool PAIRS, int MODE>
 void launch_team(Launches& enqueue, const Args& a) {
   const int words = a.C / Word<T, PAIRS>::n;
@@ -1221,22 +710,16 @@ int class_call(Args a, int32_t type, int what, int in_place_ok, void* workspace,
   with_row_type(type, [&](auto tt) {
     using T = typename decltype(tt)::type;
     if (team) {
-      const auto how = [&](auto mode, auto both) {
-        constexpr int MODE = decltype(mode)::value;
-        constexpr bool PAIRS = decltype(both)::value;
-        if (!by_thread(a, ts)) launch_team<T, PAIRS, MODE>(enqueue, a);
-        else if (MODE != FORWARD || a.k == 0) {
-          if (a.C * ts >= TWO_THREADS_BYTES) launch_tiles<T, PAIRS, MODE, 0, 2>(enqueue, a);
-          else launch_tiles<T, PAIRS, MODE, 0, 1>(enqueue, a);
-        }
-        else if constexpr (MODE == FORWARD) {
-          if (a.k <= 4) launch_tiles<T, PAIRS, MODE, 4, 1>(enqueue, a);
-          else launch_tiles<T, PAIRS, MODE, MAX_TOP, 1>(enqueue, a);
-        }
-      };
       const auto with = [&](auto mode) {
-        if constexpr (sizeof(T) == 2) { if (pairs) { how(mode, std::true_type()); return; } }
-        how(mode, std::false_type());
+        constexpr int MODE = decltype(mode)::value;
+        if (by_tile(a, ts, grad)) {
+          if constexpr (std::is_same_v<T, float>) logprob_rows_f32(enqueue, a, MODE);
+          else if constexpr (std::is_same_v<T, __nv_bfloat16>) logprob_rows_bf16(enqueue, a, MODE, pairs);
+          else logprob_rows_f16(enqueue, a, MODE, pairs);
+          return;
+        }
+        if constexpr (sizeof(T) == 2) { if (pairs) { launch_team<T, true, MODE>(enqueue, a); return; } }
+        launch_team<T, false, MODE>(enqueue, a);
       };
       if (what == GIVEN_STATS) with(std::integral_constant<int, GRAD>());
       else if (what == GIVEN_WEIGHTS) with(std::integral_constant<int, TRAIN>());

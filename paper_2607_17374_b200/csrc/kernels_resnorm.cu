@@ -35,6 +35,7 @@ struct Args {
   const long long* offsets;
   float4* stats;
   long long rows_a_team, teams;
+  int edge_rows;                                 // rows that reach less than 15 bytes from an end of a matrix of rows without gaps
   int32_t* status;
   // backward
   int blocks;
@@ -125,6 +126,11 @@ struct Team {
     for (int w = 1; w < warps; ++w) { t.x += s[w].x; t.y += s[w].y; }
     return t;
   }
+  // All threads of the team have come here.
+  __device__ __forceinline__ void sync() const {
+    if (KIND == MULTI) asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "r"(size) : "memory");
+    else __syncwarp();
+  }
   // A row of fp32 parameters, or `otherwise` where there is none; zeros behind the row.
   __device__ __forceinline__ void load_row(const float* row, float otherwise, float (&x)[N]) const {
 #pragma unroll
@@ -187,15 +193,16 @@ __device__ __forceinline__ void copy_async(void* to, const void* from) {
 __device__ __forceinline__ void end_of_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void wait_for_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// The rows of one array, AHEAD of them on their way: into shared memory (a thread's pieces of a row 16 bytes apart from its neighbours'), or for single elements, which
-// asynchronous copies do not take, one row into registers.
+// The rows of one array, AHEAD of them on their way into shared memory.  Vectors: a thread's pieces of a row, 16 bytes apart from its neighbours', for itself alone.
 template <class T, int V, int AHEAD>
 struct Source {
-  static constexpr int NV = N / V, VB = V * (int)sizeof(T), PB = VB < 16 ? VB : 16, PIECES = VB / PB, BYTES = AHEAD * NV * VB * THREADS;
+  static constexpr int NV = N / V, VB = V * (int)sizeof(T), PB = VB < 16 ? VB : 16, PIECES = VB / PB;
+  static constexpr bool SHARED = false;          // with the team's other threads
+  static __host__ __device__ int bytes(int, int) { return AHEAD * NV * VB * THREADS; }
   unsigned char* mine;
   __device__ __forceinline__ unsigned char* at(int place, int j, int piece) const { return mine + (((place * NV + j) * PIECES + piece) * THREADS) * PB; }
   template <class Place>
-  __device__ __forceinline__ void open(unsigned char* smem, const Place& team) {
+  __device__ __forceinline__ void open(unsigned char* smem, const Place& team, int) {
     mine = smem + threadIdx.x * PB;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -207,14 +214,15 @@ struct Source {
             for (int w = 0; w < PB / 4; ++w) reinterpret_cast<uint32_t*>(at(p, j, k))[w] = 0;
   }
   template <class Place>
-  __device__ __forceinline__ void fetch(const T* row, int place, const Place& team) {
+  __device__ __forceinline__ void fetch(const T* row, int place, const Place& team, int, bool) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
       if (team.on[j])
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) copy_async<PB>(at(place, j, k), reinterpret_cast<const unsigned char*>(row + team.col[j]) + k * PB);
   }
-  __device__ __forceinline__ void get(int place, float (&x)[N]) const {
+  template <class Place>
+  __device__ __forceinline__ void get(const T*, int place, const Place&, float (&x)[N]) const {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -225,26 +233,42 @@ struct Source {
       }
   }
 };
+// Rows that vectors do not fit: the team copies the 16-byte words that a row touches, wherever it begins, and its threads take elements from them.  What the first and the last of
+// these words hold beside the row are other rows of the matrix; rows less than a word from its ends are brought by element.
 template <class T, int AHEAD>
 struct Source<T, 1, AHEAD> {
-  static constexpr int BYTES = 0;
-  T x_[N];
+  static constexpr bool SHARED = true;
+  static __host__ __device__ int window(int C) { return (C * (int)sizeof(T) + 15 + 15) / 16 * 16; }
+  static __host__ __device__ int bytes(int C, int teams) { return AHEAD * window(C) * teams; }
+  unsigned char* mine;
+  int step;
   template <class Place>
-  __device__ __forceinline__ void open(unsigned char*, const Place&) {
+  __device__ __forceinline__ void open(unsigned char* smem, const Place& team, int C) {
+    step = window(C);
+    mine = smem + team.id * AHEAD * step;
+  }
+  static __device__ __forceinline__ int shift(const T* row) { return (int)(reinterpret_cast<uintptr_t>(row) & 15); }
+  template <class Place>
+  __device__ __forceinline__ void fetch(const T* row, int place, const Place& team, int C, bool edge) {
+    unsigned char* const to = mine + place * step;
+    const int s = shift(row);
+    if (edge) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) x_[e] = T(0.f);
+      for (int e = 0; e < N; ++e) if (team.on[e]) reinterpret_cast<T*>(to + s)[team.col[e]] = row[team.col[e]];
+      return;
+    }
+    const unsigned char* const from = reinterpret_cast<const unsigned char*>(row) - s;
+    const int words = (s + C * (int)sizeof(T) + 15) / 16;
+    for (int w = team.lane; w < words; w += team.size) copy_async<16>(to + 16 * w, from + 16 * w);
   }
   template <class Place>
-  __device__ __forceinline__ void fetch(const T* row, int, const Place& team) {
+  __device__ __forceinline__ void get(const T* row, int place, const Place& team, float (&x)[N]) const {
+    const T* const from = reinterpret_cast<const T*>(mine + place * step + shift(row));
 #pragma unroll
-    for (int e = 0; e < N; ++e) if (team.on[e]) x_[e] = row[team.col[e]];
-  }
-  __device__ __forceinline__ void get(int, float (&x)[N]) const {
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = to_f32<T>(x_[e]);
+    for (int e = 0; e < N; ++e) x[e] = team.on[e] ? to_f32<T>(from[team.col[e]]) : 0.f;
   }
 };
-template <int V> constexpr int ahead(int rows) { return V == 1 ? 1 : rows; }
+template <int V> constexpr int ahead(int rows) { return V == 1 ? 2 : rows; }
 constexpr int FORWARD_AHEAD = 4, GRAD_AHEAD = 3;
 
 // Rows that the threads of a warp go through together: as many as the longest of its teams has (the exchanges take all threads).
@@ -268,8 +292,8 @@ __global__ void __launch_bounds__(THREADS, V == 1 || KIND == MULTI ? 2 : 3) resn
   const long long step_res = teams * a.ld_res, step_block = teams * a.ld_block, step_out_res = teams * a.ld_out_res, step_out = teams * a.ld_out;
   Source<R, V, AHEAD> res;
   Source<T, V, AHEAD> block;
-  res.open(resnorm_rows, team);
-  block.open(resnorm_rows + res.BYTES, team);
+  res.open(resnorm_rows, team, a.C);
+  block.open(resnorm_rows + res.bytes(a.C, teams), team, a.C);
   const R* next_res = static_cast<const R*>(a.res) + begin * a.ld_res;
   const T* next_block = static_cast<const T*>(a.block) + begin * a.ld_block;
   R* out_res = static_cast<R*>(a.out_res) + begin * a.ld_out_res;
@@ -277,8 +301,10 @@ __global__ void __launch_bounds__(THREADS, V == 1 || KIND == MULTI ? 2 : 3) resn
   int place = 0;
   const auto fetch = [&](int i) {
     if (i < rows) {
-      res.fetch(next_res, place, team);
-      if (a.block) block.fetch(next_block, place, team);
+      const long long r = begin + (long long)i * teams;
+      const bool edge = r < a.edge_rows || r >= a.n - a.edge_rows;
+      res.fetch(next_res, place, team, a.C, edge);
+      if (a.block) block.fetch(next_block, place, team, a.C, edge);
       next_res += step_res;
       next_block += step_block;
     }
@@ -307,9 +333,10 @@ __global__ void __launch_bounds__(THREADS, V == 1 || KIND == MULTI ? 2 : 3) resn
       if (group.g >= 0) gate(group.g);
     }
     wait_for_copies<AHEAD - 1>();
+    if (res.SHARED) team.sync();
     float r[N], b[N];
-    res.get(place, r);
-    if (a.block) block.get(place, b);
+    res.get(static_cast<const R*>(a.res) + row * a.ld_res, place, team, r);
+    if (a.block) block.get(static_cast<const T*>(a.block) + row * a.ld_block, place, team, b);
     float2 s1 = make_float2(0.f, 0.f);
     if (a.block) {
       float scale = 1.f;
@@ -323,7 +350,7 @@ __global__ void __launch_bounds__(THREADS, V == 1 || KIND == MULTI ? 2 : 3) resn
     const bool write = have && (!a.gate || group.g >= 0);
     if (write && a.out_res) team.store(out_res, r);
     const float2 s2 = team.centre(a, r);
-    fetch(i + AHEAD);                            // into the place of this row, whose values have gone into the sums
+    fetch(i + AHEAD);                            // into the place of this row, whose values have gone into the sums (of all of the team's threads)
 #pragma unroll
     for (int e = 0; e < N; ++e) r[e] = fmaf(r[e] * s2.y, ga[e], be[e]);
     if (write) {
@@ -346,18 +373,22 @@ __global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) resnorm_grad_kernel(cons
   const int rows = begin < end ? (int)(end - begin) : 0, walk = rows_to_walk<KIND>(begin, end);
   Source<R, V, AHEAD> res, dres;
   Source<T, V, AHEAD> block, dy;
-  res.open(resnorm_rows, team);
-  dres.open(resnorm_rows + res.BYTES, team);
-  block.open(resnorm_rows + 2 * res.BYTES, team);
-  dy.open(resnorm_rows + 2 * res.BYTES + block.BYTES, team);
+  {
+    const int teams = THREADS >> a.team_shift, rb = res.bytes(a.C, teams), tb = block.bytes(a.C, teams);
+    res.open(resnorm_rows, team, a.C);
+    dres.open(resnorm_rows + rb, team, a.C);
+    block.open(resnorm_rows + 2 * rb, team, a.C);
+    dy.open(resnorm_rows + 2 * rb + tb, team, a.C);
+  }
   long long ahead_row = begin;
   int place = 0;
   const auto fetch = [&](int i) {
     if (i < rows) {
-      res.fetch(static_cast<const R*>(a.res) + ahead_row * a.ld_res, place, team);
-      if (a.block) block.fetch(static_cast<const T*>(a.block) + ahead_row * a.ld_block, place, team);
-      if (a.dres) dres.fetch(static_cast<const R*>(a.dres) + ahead_row * a.ld_dres, place, team);
-      if (a.dy) dy.fetch(static_cast<const T*>(a.dy) + ahead_row * a.ld_dy, place, team);
+      const bool edge = ahead_row < a.edge_rows || ahead_row >= a.n - a.edge_rows;
+      res.fetch(static_cast<const R*>(a.res) + ahead_row * a.ld_res, place, team, a.C, edge);
+      if (a.block) block.fetch(static_cast<const T*>(a.block) + ahead_row * a.ld_block, place, team, a.C, edge);
+      if (a.dres) dres.fetch(static_cast<const R*>(a.dres) + ahead_row * a.ld_dres, place, team, a.C, edge);
+      if (a.dy) dy.fetch(static_cast<const T*>(a.dy) + ahead_row * a.ld_dy, place, team, a.C, edge);
     }
     ++ahead_row;
     end_of_copies();
@@ -415,11 +446,13 @@ __global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) resnorm_grad_kernel(cons
     float4 st = next_stats;
     if (i + 1 < rows) next_stats = a.stats[row + 1];
     wait_for_copies<AHEAD - 1>();
+    if (res.SHARED) team.sync();
     float x[N], u[N], d[N], g[N];
-    res.get(place, x);
-    if (a.block) block.get(place, u);
-    if (a.dres) dres.get(place, d);
-    if (a.dy) dy.get(place, g);
+    res.get(static_cast<const R*>(a.res) + row * a.ld_res, place, team, x);
+    if (a.block) block.get(static_cast<const T*>(a.block) + row * a.ld_block, place, team, u);
+    if (a.dres) dres.get(static_cast<const R*>(a.dres) + row * a.ld_dres, place, team, d);
+    if (a.dy) dy.get(static_cast<const T*>(a.dy) + row * a.ld_dy, place, team, g);
+    if (res.SHARED) team.sync();                 // every thread has its elements: the place may be filled again
     if (KIND == PART ? !__all_sync(0xffffffffu, live) : !live) {     // whatever stands in a row that does not count, it adds to nothing
       if (!live) {
         st = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -696,7 +729,7 @@ extern "C" int taurus_residual_norm(int64_t n, int32_t width, const void* res, i
   if (!regions_on_device(outs, dev) || !regions_on_device(ins, dev) || !regions_apart(outs, ins)) return TAURUS_ERR_INVALID_ARG;
   Args a = {};
   a.n = n; a.C = width; a.team_shift = team_shift_of(width); a.layer = kind == TAURUS_NORM_LAYER; a.post = post; a.groups = groups; a.alpha = alpha; a.eps = eps;
-  a.inv_C = 1.f / (float)width; a.res = res; a.ld_res = ld_res; a.block = block; a.ld_block = ld_block; a.out_res = out_res; a.ld_out_res = ld_out_res; a.out = out; a.ld_out = ld_out;
+  a.inv_C = 1.f / (float)width; a.edge_rows = 1 + 15 / (width * std::min(ts, rs)); a.res = res; a.ld_res = ld_res; a.block = block; a.ld_block = ld_block; a.out_res = out_res; a.ld_out_res = ld_out_res; a.out = out; a.ld_out = ld_out;
   a.post_gamma = post_gamma; a.gate = gate; a.gamma = gamma; a.beta = beta; a.offsets = reinterpret_cast<const long long*>(offsets); a.stats = reinterpret_cast<float4*>(stats);
   a.status = status;
   const Rows rows[] = {{res, ld_res, rs}, {block, ld_block, ts}, {out_res, ld_out_res, rs}, {out, ld_out, ts}};
@@ -708,7 +741,8 @@ extern "C" int taurus_residual_norm(int64_t n, int32_t width, const void* res, i
     constexpr int V = decltype(vc)::value;
     const auto go = [&](auto kind) {
       constexpr int KIND = decltype(kind)::value;
-      constexpr size_t smem = Source<R, V, ahead<V>(FORWARD_AHEAD)>::BYTES + Source<T, V, ahead<V>(FORWARD_AHEAD)>::BYTES;
+      const int teams = THREADS >> a.team_shift;
+      const size_t smem = (size_t)Source<R, V, ahead<V>(FORWARD_AHEAD)>::bytes(width, teams) + (size_t)Source<T, V, ahead<V>(FORWARD_AHEAD)>::bytes(width, teams);
       int resident = 0;
       cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
       if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, resnorm_kernel<T, R, V, KIND>, THREADS, smem);
@@ -760,7 +794,7 @@ extern "C" int taurus_residual_norm_grad(int64_t n, int32_t width, const void* r
   if (n == 0 && !joins) return TAURUS_OK;
   char* const ws = static_cast<char*>(workspace);
   Args a = {};
-  a.n = n; a.C = width; a.team_shift = team_shift_of(width); a.layer = kind == TAURUS_NORM_LAYER; a.post = post; a.groups = groups; a.alpha = alpha; a.inv_C = 1.f / (float)width;
+  a.n = n; a.C = width; a.team_shift = team_shift_of(width); a.layer = kind == TAURUS_NORM_LAYER; a.post = post; a.groups = groups; a.alpha = alpha; a.inv_C = 1.f / (float)width; a.edge_rows = 1 + 15 / (width * std::min(ts, rs));
   a.res = res; a.ld_res = ld_res; a.block = block; a.ld_block = ld_block; a.dres = grad_out_res; a.ld_dres = ld_grad_out_res; a.dy = grad_out; a.ld_dy = ld_grad_out;
   a.out_res = grad_res; a.ld_out_res = ld_grad_res; a.out = grad_block; a.ld_out = ld_grad_block; a.post_gamma = post_gamma; a.gate = gate; a.gamma = gamma;
   a.offsets = reinterpret_cast<const long long*>(offsets); a.stats = reinterpret_cast<float4*>(const_cast<float*>(stats)); a.status = status;      // read only here
@@ -779,8 +813,9 @@ extern "C" int taurus_residual_norm_grad(int64_t n, int32_t width, const void* r
       constexpr int V = decltype(vc)::value;
       const auto go = [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;
-        constexpr size_t rows_bytes = 2 * (Source<R, V, ahead<V>(GRAD_AHEAD)>::BYTES + Source<T, V, ahead<V>(GRAD_AHEAD)>::BYTES);
-        constexpr size_t smem = std::max<size_t>(rows_bytes, (size_t)THREADS * N * 4);            // (a block's teams x columns are at most its threads x elements)
+        const int teams = THREADS >> a.team_shift;
+        const size_t rows_bytes = 2 * ((size_t)Source<R, V, ahead<V>(GRAD_AHEAD)>::bytes(width, teams) + (size_t)Source<T, V, ahead<V>(GRAD_AHEAD)>::bytes(width, teams));
+        const size_t smem = std::max<size_t>(rows_bytes, (size_t)THREADS * N * 4);            // (a block's teams x columns are at most its threads x elements)
         const cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_grad_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
         if (e != cudaSuccess) { enqueue.error = e; return; }
         enqueue(resnorm_grad_kernel<T, R, V, KIND>, dim3((unsigned)p.blocks), THREADS, smem, a);

@@ -246,26 +246,23 @@ __device__ __forceinline__ void copy_async(void* to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
 
-// WPR warps to a row or a part of one.  Thread t has the vectors t, t + 32 WPR, ... of it.
+constexpr int block_warps(int wpr) { return wpr == 1 ? WARPS : wpr; }
+// WPR warps to a row or a part of one: a block to itself, or eight rows of a warp each in a block.  Thread t has the vectors t, t + 32 WPR, ... of it.
 template <class T, bool TOP, int WPR, bool WITH_GRAD>
-__global__ void __launch_bounds__(32 * WARPS, 4) stream_kernel(const Args a) {
-  constexpr int V = 16 / (int)sizeof(T), U = 4, AHEAD = 2, TEAM = 32 * WPR, PLACES = LIST * WPR, SHARES = WARPS / WPR;
-  __shared__ u64 lists[TOP ? WARPS * LIST : 1];
+__global__ void __launch_bounds__(32 * block_warps(WPR), 4 * WARPS / block_warps(WPR)) stream_kernel(const Args a) {
+  constexpr int V = 16 / (int)sizeof(T), U = 4, AHEAD = 2, TEAM = 32 * WPR, PLACES = LIST * WPR, BW = block_warps(WPR), SHARES = BW / WPR;
+  __shared__ u64 lists[TOP ? BW * LIST : 1];
   __shared__ u64 best[TOP ? SHARES * MAX_TOP : 1];
-  __shared__ float warp_top[TOP ? WARPS * MAX_TOP : 1];
-  __shared__ float2 warp_sums[WARPS];
-  __shared__ float warp_max[WARPS], warp_rest[WARPS];
-  __shared__ int warp_same[WARPS], counts[SHARES], owners[SHARES];
-  __shared__ unsigned chosen[WARPS];
-  __shared__ uint8_t who[TOP ? 32 * WARPS : 1];
-  __shared__ Vec<T, V> ahead[AHEAD * U * 32 * WARPS];
+  __shared__ float warp_top[TOP ? BW * MAX_TOP : 1];
+  __shared__ float2 warp_sums[BW];
+  __shared__ float warp_max[BW], warp_rest[BW];
+  __shared__ int warp_same[BW], counts[SHARES], owners[SHARES];
+  __shared__ unsigned chosen[BW];
+  __shared__ uint8_t who[TOP ? 32 * BW : 1];
+  __shared__ Vec<T, V> ahead[AHEAD * U * 32 * BW];
   early_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = warp / WPR, mine = threadIdx.x % TEAM, w0 = share * WPR;     // w0: the team's first warp
-  const auto sync = [&] {
-    if (WPR == 1) __syncwarp();
-    else if (WPR == WARPS) __syncthreads();
-    else asm volatile("bar.sync %0, %1;" ::"r"(share + 1), "n"(TEAM) : "memory");
-  };
+  const auto sync = [] { if (WPR == 1) __syncwarp(); else __syncthreads(); };
   const long long units = a.n * a.parts, stride = (long long)gridDim.x * SHARES;
   for (long long unit = (long long)blockIdx.x * SHARES + share; unit < units; unit += stride) {
     const long long row = a.parts == 1 ? unit : unit / a.parts;
@@ -280,21 +277,21 @@ __global__ void __launch_bounds__(32 * WARPS, 4) stream_kernel(const Args a) {
     int place = 0;
     const T* from = x + span.column(first + mine);
     const auto fetch = [&](int v0) {
-      Vec<T, V>* const to = &ahead[place * U * (32 * WARPS) + threadIdx.x];
+      Vec<T, V>* const to = &ahead[place * U * (32 * BW) + threadIdx.x];
       if (v0 > first && v0 + U * TEAM < last) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) copy_async(to + u * (32 * WARPS), from + u * TEAM * V);
+        for (int u = 0; u < U; ++u) copy_async(to + u * (32 * BW), from + u * TEAM * V);
       } else if (v0 < last) {
 #pragma unroll 1
         for (int u = 0; u < U; ++u) {
           const int v = v0 + u * TEAM + mine;
-          if (v > first && v < last - 1) copy_async(to + u * (32 * WARPS), from + u * TEAM * V);
-          else if (v < last) to[u * (32 * WARPS)] = span.template load<LOAD_PLAIN>(v);
+          if (v > first && v < last - 1) copy_async(to + u * (32 * BW), from + u * TEAM * V);
+          else if (v < last) to[u * (32 * BW)] = span.template load<LOAD_PLAIN>(v);
           else {
             Vec<T, V> none;
 #pragma unroll
             for (int i = 0; i < V; ++i) none.v[i] = from_f32<T>(-INFINITY);
-            to[u * (32 * WARPS)] = none;
+            to[u * (32 * BW)] = none;
           }
         }
       }
@@ -308,7 +305,7 @@ __global__ void __launch_bounds__(32 * WARPS, 4) stream_kernel(const Args a) {
       asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
       Vec<T, V> raw[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) raw[u] = load_vec<Vec<T, V>>(&ahead[(place * U + u) * (32 * WARPS) + threadIdx.x]);
+      for (int u = 0; u < U; ++u) raw[u] = load_vec<Vec<T, V>>(&ahead[(place * U + u) * (32 * BW) + threadIdx.x]);
       float now = m;
 #pragma unroll
       for (int u = 0; u < U; ++u) now = max_nan(now, vector_max(raw[u]));
@@ -677,8 +674,8 @@ void launch_grad(Launches& enqueue, const Args& a, int sms) {
 template <class T, bool TOP, bool WITH_GRAD>
 void launch_stream(Launches& enqueue, const Args& a) {
   const auto go = [&](auto wpr) {
-    constexpr int WPR = decltype(wpr)::value, SHARES = WARPS / WPR;
-    enqueue(stream_kernel<T, TOP, WPR, WITH_GRAD>, dim3((unsigned)std::min<int64_t>((a.n * a.parts + SHARES - 1) / SHARES, 1 << 30)), 32 * WARPS, 0, a);
+    constexpr int WPR = decltype(wpr)::value, BW = block_warps(WPR), SHARES = BW / WPR;
+    enqueue(stream_kernel<T, TOP, WPR, WITH_GRAD>, dim3((unsigned)std::min<int64_t>((a.n * a.parts + SHARES - 1) / SHARES, 1 << 30)), 32 * BW, 0, a);
   };
   const int64_t rows = a.n * a.parts;
   if (rows >= ENOUGH_WARPS) go(std::integral_constant<int, 1>());

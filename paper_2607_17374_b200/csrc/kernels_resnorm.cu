@@ -4,7 +4,7 @@
 //   D = dr' + N2'(dy gamma),  dr = D,  dgate_g = alpha sum D u,  du = alpha gate_g D,  dpost_gamma = sum du h1,  db = N1'(du post_gamma) (or du)
 //   dgamma = sum dy h2,  dbeta = sum dy         h: normalised rows,  N'(d) = rstd (d - mean(d) - h mean(d h)), without the first mean for RMS
 //
-// Bytes bound it: r and b in, r' and y out; r, b, dr', dy in, dr and db out.  A row is the work of a team of 1 to 128 neighbouring threads with 8 elements each, which
+// Bytes bound it: r and b in, r' and y out; r, b, dr', dy in, dr and db out.  A row is the work of a team of 1 to 128 neighbouring threads (a power of two up to a warp, then whole warps, which are a block) with 8 elements each, which
 // stay in registers from the load to the store: statistics first the mean, then the squares of deviations.  A team walks over neighbouring rows, so that the group of a row (the last one whose
 // offset is not above it) is looked for once a group.  Rows are on their way some rows ahead, by asynchronous copies into places of shared memory that are a thread's own: a thread
 // waits for its own copies and for nobody.
@@ -18,13 +18,13 @@
 
 namespace {
 
-constexpr int THREADS = 256, N = 8;             // threads of a block, elements of a thread
+constexpr int THREADS = 256, N = 8;             // threads of a block (of a team of several warps: that team's), elements of a thread
 constexpr int MAX_C = TAURUS_MAX_ROW_WIDTH;
 constexpr int GRAD_BLOCKS = 2;                   // blocks of an SM that the gradient is spread over
 
 struct Args {
   long long n;
-  int C, team_shift;                             // a team is 1 << team_shift threads
+  int C, team_shift;                             // a team is 1 << team_shift threads (up to a warp)
   int layer, post, groups;
   float alpha, eps, inv_C;
   const void *res, *block, *dres, *dy;
@@ -78,7 +78,7 @@ __device__ __forceinline__ void find_group(const Args& a, long long r, Group* at
 }
 __device__ __forceinline__ void check_offsets(const Args& a) {
   if (!a.offsets) return;
-  for (long long g = (long long)blockIdx.x * THREADS + threadIdx.x; g < a.groups; g += (long long)gridDim.x * THREADS) {
+  for (long long g = (long long)blockIdx.x * blockDim.x + threadIdx.x; g < a.groups; g += (long long)gridDim.x * blockDim.x) {
     const long long b = a.offsets[g], e = a.offsets[g + 1];
     if (b < 0 || e > a.n || e < b) rows_status(a.status, TAURUS_ERR_INVALID_ARG);
   }
@@ -91,16 +91,17 @@ enum { PART = 0, WARP = 1, MULTI = 2 };
 template <int V, int KIND>
 struct Team {
   static constexpr int NV = N / V;
-  int size, lane, warps, id;                     // id: of the block's teams
+  int size, lane, warps, id, threads;            // id: of the block's teams; threads: of the block
   int col[NV];
   bool on[NV];
   float2* slot;                                  // shared memory of teams of several warps: [2][warps]
   int flip = 0;
   __device__ __forceinline__ explicit Team(const Args& a) {
-    __shared__ float2 slots[2 * THREADS / 32];
-    size = KIND == WARP ? 32 : 1 << a.team_shift;
-    lane = threadIdx.x & (size - 1); id = KIND == WARP ? threadIdx.x >> 5 : threadIdx.x >> a.team_shift; warps = size >> 5;
-    slot = slots + id * 2 * warps;
+    __shared__ float2 slots[KIND == MULTI ? 2 * 4 : 1];
+    size = KIND == MULTI ? blockDim.x : KIND == WARP ? 32 : 1 << a.team_shift;
+    lane = KIND == MULTI ? threadIdx.x : threadIdx.x & (size - 1); id = KIND == MULTI ? 0 : KIND == WARP ? threadIdx.x >> 5 : threadIdx.x >> a.team_shift; warps = size >> 5;
+    threads = KIND == MULTI ? size : THREADS;    // a team of several warps is a block
+    slot = slots;
 #pragma unroll
     for (int j = 0; j < NV; ++j) { col[j] = (j * size + lane) * V; on[j] = col[j] < a.C; }
   }
@@ -121,14 +122,14 @@ struct Team {
     float2* const s = slot + flip * warps;
     flip ^= 1;
     if ((threadIdx.x & 31) == 0) s[lane >> 5] = make_float2(x, y);
-    asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "r"(size) : "memory");
+    __syncthreads();
     float2 t = s[0];
     for (int w = 1; w < warps; ++w) { t.x += s[w].x; t.y += s[w].y; }
     return t;
   }
   // All threads of the team have come here.
   __device__ __forceinline__ void sync() const {
-    if (KIND == MULTI) asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "r"(size) : "memory");
+    if (KIND == MULTI) __syncthreads();
     else __syncwarp();
   }
   // A row of fp32 parameters, or `otherwise` where there is none; zeros behind the row.
@@ -198,12 +199,14 @@ template <class T, int V, int AHEAD>
 struct Source {
   static constexpr int NV = N / V, VB = V * (int)sizeof(T), PB = VB < 16 ? VB : 16, PIECES = VB / PB;
   static constexpr bool SHARED = false;          // with the team's other threads
-  static __host__ __device__ int bytes(int, int) { return AHEAD * NV * VB * THREADS; }
+  static __host__ __device__ int bytes(int, int, int threads) { return AHEAD * NV * VB * threads; }
   unsigned char* mine;
-  __device__ __forceinline__ unsigned char* at(int place, int j, int piece) const { return mine + (((place * NV + j) * PIECES + piece) * THREADS) * PB; }
+  int apart;                                     // bytes from a piece to the next
+  __device__ __forceinline__ unsigned char* at(int place, int j, int piece) const { return mine + ((place * NV + j) * PIECES + piece) * apart; }
   template <class Place>
   __device__ __forceinline__ void open(unsigned char* smem, const Place& team, int) {
     mine = smem + threadIdx.x * PB;
+    apart = team.threads * PB;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
       if (!team.on[j])
@@ -239,7 +242,7 @@ template <class T, int AHEAD>
 struct Source<T, 1, AHEAD> {
   static constexpr bool SHARED = true;
   static __host__ __device__ int window(int C) { return (C * (int)sizeof(T) + 15 + 15) / 16 * 16; }
-  static __host__ __device__ int bytes(int C, int teams) { return AHEAD * window(C) * teams; }
+  static __host__ __device__ int bytes(int C, int teams, int) { return AHEAD * window(C) * teams; }
   unsigned char* mine;
   int step;
   template <class Place>
@@ -279,13 +282,13 @@ __device__ __forceinline__ int rows_to_walk(long long begin, long long end) {
 }
 
 template <class T, class R, int V, int KIND>
-__global__ void __launch_bounds__(THREADS, V == 1 || KIND == MULTI ? 2 : 3) resnorm_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(KIND == MULTI ? 128 : THREADS, KIND == MULTI ? 4 : V == 1 ? 2 : 3) resnorm_kernel(const __grid_constant__ Args a) {
   extern __shared__ __align__(16) unsigned char resnorm_rows[];
   constexpr int AHEAD = ahead<V>(FORWARD_AHEAD);
   check_offsets(a);
   Team<V, KIND> team(a);
   // A block has neighbouring rows, which its teams take in turn.
-  const int teams = KIND == WARP ? THREADS / 32 : THREADS >> a.team_shift;
+  const int teams = KIND == MULTI ? 1 : KIND == WARP ? THREADS / 32 : THREADS >> a.team_shift;
   const long long block_begin = (long long)blockIdx.x * a.rows_a_team * teams, begin = block_begin + team.id;
   const long long left = (block_begin + a.rows_a_team * teams < a.n ? block_begin + a.rows_a_team * teams : a.n) - begin;
   const int rows = left > 0 ? (int)((left + teams - 1) / teams) : 0, walk = KIND == PART ? (int)__reduce_max_sync(0xffffffffu, (unsigned)rows) : rows;
@@ -293,7 +296,7 @@ __global__ void __launch_bounds__(THREADS, V == 1 || KIND == MULTI ? 2 : 3) resn
   Source<R, V, AHEAD> res;
   Source<T, V, AHEAD> block;
   res.open(resnorm_rows, team, a.C);
-  block.open(resnorm_rows + res.bytes(a.C, teams), team, a.C);
+  block.open(resnorm_rows + res.bytes(a.C, teams, team.threads), team, a.C);
   const R* next_res = static_cast<const R*>(a.res) + begin * a.ld_res;
   const T* next_block = static_cast<const T*>(a.block) + begin * a.ld_block;
   R* out_res = static_cast<R*>(a.out_res) + begin * a.ld_out_res;
@@ -363,18 +366,18 @@ __global__ void __launch_bounds__(THREADS, V == 1 || KIND == MULTI ? 2 : 3) resn
 }
 
 template <class T, class R, int V, int KIND>
-__global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) resnorm_grad_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(KIND == MULTI ? 128 : THREADS, KIND == MULTI ? 2 * GRAD_BLOCKS : GRAD_BLOCKS) resnorm_grad_kernel(const __grid_constant__ Args a) {
   extern __shared__ __align__(16) unsigned char resnorm_rows[];                // the rows on their way; at the end [teams of the block x C] sums
   constexpr int AHEAD = ahead<V>(GRAD_AHEAD);
   check_offsets(a);
   Team<V, KIND> team(a);
-  const long long mine = KIND == WARP ? (long long)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5) : ((long long)blockIdx.x * THREADS + threadIdx.x) >> a.team_shift;
+  const long long mine = KIND == MULTI ? blockIdx.x : KIND == WARP ? (long long)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5) : ((long long)blockIdx.x * THREADS + threadIdx.x) >> a.team_shift;
   const long long begin = mine * a.rows_a_team, end = begin + a.rows_a_team < a.n ? begin + a.rows_a_team : a.n;
   const int rows = begin < end ? (int)(end - begin) : 0, walk = rows_to_walk<KIND>(begin, end);
   Source<R, V, AHEAD> res, dres;
   Source<T, V, AHEAD> block, dy;
   {
-    const int teams = THREADS >> a.team_shift, rb = res.bytes(a.C, teams), tb = block.bytes(a.C, teams);
+    const int teams = KIND == MULTI ? 1 : THREADS >> a.team_shift, rb = res.bytes(a.C, teams, team.threads), tb = block.bytes(a.C, teams, team.threads);
     res.open(resnorm_rows, team, a.C);
     dres.open(resnorm_rows + rb, team, a.C);
     block.open(resnorm_rows + 2 * rb, team, a.C);
@@ -526,7 +529,7 @@ __global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) resnorm_grad_kernel(cons
   if (a.chan) {
     wait_for_copies<0>();
     float* const sums = reinterpret_cast<float*>(resnorm_rows);
-    const int teams = THREADS >> a.team_shift;
+    const int teams = KIND == MULTI ? 1 : THREADS >> a.team_shift;
     float* const mine_row = sums + team.id * a.C;
     for (int which = 0; which < 3; ++which) {
       __syncthreads();
@@ -534,7 +537,7 @@ __global__ void __launch_bounds__(THREADS, GRAD_BLOCKS) resnorm_grad_kernel(cons
       else if (which == 1) team.store_row(mine_row, sum_be);
       else team.store_row(mine_row, sum_pg);
       __syncthreads();
-      for (int c = threadIdx.x; c < a.C; c += THREADS) {
+      for (int c = threadIdx.x; c < a.C; c += team.threads) {
         float s = 0.f;
         for (int t = 0; t < teams; ++t) s += sums[t * a.C + c];
         a.chan[((long long)blockIdx.x * 3 + which) * a.C + c] = s;
@@ -623,19 +626,24 @@ inline int team_shift_of(int C) {
 constexpr int SMS = 148;                         // for workspaces, which are counted without a device
 constexpr int MIN_ROWS = 2;                      // rows of a team at least
 
+// Threads and teams of a block.
+inline int block_threads(int C) { return C > 32 * N ? (C + 32 * N - 1) / (32 * N) * 32 : THREADS; }
+inline int64_t block_teams(int C) { return C > 32 * N ? 1 : THREADS >> team_shift_of(C); }
+// Blocks of the gradient on an SM: of 256 threads, or as many threads in smaller ones.
+inline int64_t grad_blocks(int C) { return (int64_t)GRAD_BLOCKS * (THREADS / block_threads(C)); }
 struct Plan { int64_t rows_a_team, teams, blocks; };
 Plan plan_of(int64_t n, int C, int64_t rows_a_team) {
-  const int64_t a_block = THREADS >> team_shift_of(C), teams = (n + rows_a_team - 1) / rows_a_team;
+  const int64_t a_block = block_teams(C), teams = (n + rows_a_team - 1) / rows_a_team;
   return {rows_a_team, teams, (teams + a_block - 1) / a_block};
 }
 // All rows over the blocks that are resident at once.
 Plan forward_plan(int64_t n, int C, int64_t blocks) {
-  const int64_t teams = (THREADS >> team_shift_of(C)) * blocks;
+  const int64_t teams = block_teams(C) * blocks;
   return plan_of(n, C, std::max<int64_t>(1, (n + teams - 1) / teams));
 }
 // Gradient: all rows over the blocks that are resident at once, two rows a team at least.
 Plan grad_plan(int64_t n, int C, int sms) {
-  const int64_t a_block = THREADS >> team_shift_of(C), teams = a_block * std::min(sms, SMS) * GRAD_BLOCKS;
+  const int64_t teams = block_teams(C) * std::min(sms, SMS) * grad_blocks(C);
   return plan_of(n, C, std::max<int64_t>(MIN_ROWS, (n + teams - 1) / teams));
 }
 struct Space { size_t chan, first, last, span, bytes; };
@@ -643,8 +651,8 @@ Space space_of(int64_t n, int C, int groups) {
   Space s = {};
   if (n == 0) return s;
   // (what does for n rows does for fewer: the number of blocks and of teams is bounded by that of the largest plan)
-  const int64_t a_block = THREADS >> team_shift_of(C);
-  const int64_t blocks = std::min<int64_t>((int64_t)SMS * GRAD_BLOCKS, (n + a_block - 1) / a_block), teams = std::min<int64_t>(blocks * a_block, n);
+  const int64_t a_block = block_teams(C);
+  const int64_t blocks = std::min<int64_t>((int64_t)SMS * grad_blocks(C), (n + a_block - 1) / a_block), teams = std::min<int64_t>(blocks * a_block, n);
   size_t at = 0;
   const auto take = [&](size_t b) { const size_t here = at; at += (b + 255) / 256 * 256; return here; };
   s.chan = take((size_t)blocks * 3 * C * 4);
@@ -741,15 +749,15 @@ extern "C" int taurus_residual_norm(int64_t n, int32_t width, const void* res, i
     constexpr int V = decltype(vc)::value;
     const auto go = [&](auto kind) {
       constexpr int KIND = decltype(kind)::value;
-      const int teams = THREADS >> a.team_shift;
-      const size_t smem = (size_t)Source<R, V, ahead<V>(FORWARD_AHEAD)>::bytes(width, teams) + (size_t)Source<T, V, ahead<V>(FORWARD_AHEAD)>::bytes(width, teams);
+      const int teams = (int)block_teams(width), threads = block_threads(width);
+      const size_t smem = (size_t)Source<R, V, ahead<V>(FORWARD_AHEAD)>::bytes(width, teams, threads) + (size_t)Source<T, V, ahead<V>(FORWARD_AHEAD)>::bytes(width, teams, threads);
       int resident = 0;
       cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
-      if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, resnorm_kernel<T, R, V, KIND>, THREADS, smem);
+      if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, resnorm_kernel<T, R, V, KIND>, threads, smem);
       if (e != cudaSuccess) { enqueue.error = e; return; }
       const Plan p = forward_plan(n, width, (int64_t)sms * std::max(resident, 1));
       a.rows_a_team = p.rows_a_team; a.teams = p.teams;
-      enqueue(resnorm_kernel<T, R, V, KIND>, dim3((unsigned)p.blocks), THREADS, smem, a);
+      enqueue(resnorm_kernel<T, R, V, KIND>, dim3((unsigned)p.blocks), threads, smem, a);
     };
     with_kind(a.team_shift, go);
   });
@@ -813,12 +821,12 @@ extern "C" int taurus_residual_norm_grad(int64_t n, int32_t width, const void* r
       constexpr int V = decltype(vc)::value;
       const auto go = [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;
-        const int teams = THREADS >> a.team_shift;
-        const size_t rows_bytes = 2 * ((size_t)Source<R, V, ahead<V>(GRAD_AHEAD)>::bytes(width, teams) + (size_t)Source<T, V, ahead<V>(GRAD_AHEAD)>::bytes(width, teams));
-        const size_t smem = std::max<size_t>(rows_bytes, (size_t)THREADS * N * 4);            // (a block's teams x columns are at most its threads x elements)
+        const int teams = (int)block_teams(width), threads = block_threads(width);
+        const size_t rows_bytes = 2 * ((size_t)Source<R, V, ahead<V>(GRAD_AHEAD)>::bytes(width, teams, threads) + (size_t)Source<T, V, ahead<V>(GRAD_AHEAD)>::bytes(width, teams, threads));
+        const size_t smem = std::max<size_t>(rows_bytes, (size_t)threads * N * 4);            // (a block's teams x columns are at most its threads x elements)
         const cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_grad_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
         if (e != cudaSuccess) { enqueue.error = e; return; }
-        enqueue(resnorm_grad_kernel<T, R, V, KIND>, dim3((unsigned)p.blocks), THREADS, smem, a);
+        enqueue(resnorm_grad_kernel<T, R, V, KIND>, dim3((unsigned)p.blocks), threads, smem, a);
       };
       with_kind(a.team_shift, go);
     });

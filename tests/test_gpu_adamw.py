@@ -274,3 +274,14 @@ def test_arrays_that_overlap_are_refused():
         a.step(torch.ones(1, dtype=torch.int64, device="cuda"), p[3:4])
     with pytest.raises(tb.TaurusError):
         a.step(torch.ones(1, dtype=torch.int64), torch.zeros(1, device="cuda"))           # host memory
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_an_eps_beside_which_the_root_of_a_subnormal_number_counts(eight):
+    a = List([5000], F32, F32, eight, scale=1e-20)     # squares of 1e-40: subnormal
+    before, p = a.held(0), a.p[0].clone()
+    m, v = step32(before[0], before[1] * before[1] if eight else before[1], a.g[0], B1, B2)
+    step, lr = torch.tensor([3], device="cuda"), torch.tensor([1e-3], device="cuda")
+    a.adamw.step(step, lr, B1, B2, 1e-25, None, 5)
+    # the reference's root, of the subnormal v that the step forms, in 64 bits: the hardware's is off by 2 ulp of a normal number
+    close(a.p[0], *update(p, m, v, 3, float(lr), 0.0, B1, B2, float(torch.tensor(1e-25))))

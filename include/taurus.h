@@ -458,14 +458,15 @@ int taurus_permute_rows(int64_t V, int32_t width, const float* in_rows, int64_t 
  * Operators on typed rows: what makes the rows that a layer takes and what stands between two layers (no counterpart in
  * the paper, whose vertices all have features of one kind).  taurus_embed_rows looks rows up in a learned table,
  * taurus_typed_project gives each vertex type a weight matrix of its own, taurus_norm_rows is a norm with an activation over
- * a batch of graphs.  Each has its gradient, for a program that trains tables, weights and norms with a loss of its own on what they
- * make: the layers have no backward call.  A norm between two layers needs the rows of a graph in one device matrix, such as a dense output; layers
+ * a batch of graphs.  Each has its gradient, for a program that trains tables, weights and norms with a loss on what they
+ * make: the layers have no backward call.  Such a program goes on with taurus_residual_norm (between two products), taurus_class_logprob (its loss and its answers)
+ * and taurus_adamw_step.  A norm between two layers needs the rows of a graph in one device matrix, such as a dense output; layers
  * chained through sorted runs have none.
  *
  * Rules common to them.  They need no context.  Every pointer is DEVICE memory of the current device, aligned to its element
  * (anything else: TAURUS_ERR_INVALID_ARG); a pitch ld is in elements, at least the row's width; rows need no alignment, but rows
  * whose addresses and pitches are multiples of 16 bytes are the fast ones.  All work is enqueued on `cuda_stream` of the current
- * device and the call returns without waiting; no call allocates or synchronises, so all may be captured into a graph.  A call reads
+ * device and the call returns without waiting; no call allocates or synchronises (taurus_adamw_create and taurus_adamw_destroy apart), so all may be captured into a graph.  A call reads
  * nothing that an earlier one left in a workspace.  Calls that may run at the same time (two streams, two graphs) need
  * workspaces of their own; calls in order may share one.  Outputs may not share memory with inputs, the workspace or each other except
  * where stated (some columns of a matrix may be an input and others of it an output).

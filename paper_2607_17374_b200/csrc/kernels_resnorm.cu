@@ -624,6 +624,9 @@ inline int team_shift_of(int C) {
 }
 
 constexpr int SMS = 148;                         // for workspaces, which are counted without a device
+// Shared memory that a kernel may ask for: the same figure in every call, so that calls of several host threads do not take it from one another.  (The gradient's four arrays
+// three rows ahead, 256 threads of 8 fp32 elements: 96 KB.)
+constexpr int SHARED_MOST = 96 * 1024;
 constexpr int MIN_ROWS = 2;                      // rows of a team at least
 
 // Threads and teams of a block.
@@ -752,7 +755,7 @@ extern "C" int taurus_residual_norm(int64_t n, int32_t width, const void* res, i
       const int teams = (int)block_teams(width), threads = block_threads(width);
       const size_t smem = (size_t)Source<R, V, ahead<V>(FORWARD_AHEAD)>::bytes(width, teams, threads) + (size_t)Source<T, V, ahead<V>(FORWARD_AHEAD)>::bytes(width, teams, threads);
       int resident = 0;
-      cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+      cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED_MOST) : cudaSuccess;
       if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, resnorm_kernel<T, R, V, KIND>, threads, smem);
       if (e != cudaSuccess) { enqueue.error = e; return; }
       const Plan p = forward_plan(n, width, (int64_t)sms * std::max(resident, 1));
@@ -824,7 +827,7 @@ extern "C" int taurus_residual_norm_grad(int64_t n, int32_t width, const void* r
         const int teams = (int)block_teams(width), threads = block_threads(width);
         const size_t rows_bytes = 2 * ((size_t)Source<R, V, ahead<V>(GRAD_AHEAD)>::bytes(width, teams, threads) + (size_t)Source<T, V, ahead<V>(GRAD_AHEAD)>::bytes(width, teams, threads));
         const size_t smem = std::max<size_t>(rows_bytes, (size_t)threads * N * 4);            // (a block's teams x columns are at most its threads x elements)
-        const cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_grad_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+        const cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_grad_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED_MOST) : cudaSuccess;
         if (e != cudaSuccess) { enqueue.error = e; return; }
         enqueue(resnorm_grad_kernel<T, R, V, KIND>, dim3((unsigned)p.blocks), threads, smem, a);
       };

@@ -356,13 +356,16 @@ void set_tile(Args* a, int tpr) {
   a->mode_out = mode(a->dx, a->ld_dx);
 }
 
+// What a kernel may ask for is set to the same figure by every call: calls of several host threads do not take it from one another.  (A tile of one thread to a row has 64 KB and
+// what sets its rows apart.)
+constexpr int TILE_MOST = 72 * 1024;
 template <class T, bool PAIRS, int MODE, int KMAX, int TPR>
 void launch_tiles(Launches& enqueue, Args a) {
   constexpr int ROWS = ROW_THREADS / TPR;
   set_tile<T, PAIRS>(&a, TPR);
   const size_t smem = (size_t)a.pitch * sizeof(T) * (PAIRS ? 2 : 1) * ROWS;
   if (smem > 40 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(rows_kernel<T, PAIRS, MODE, KMAX, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(rows_kernel<T, PAIRS, MODE, KMAX, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, TILE_MOST);
     if (e != cudaSuccess) { enqueue.error = e; return; }
   }
   const int64_t tiles = (a.n + ROWS - 1) / ROWS;

@@ -3,7 +3,7 @@
 //   g = s grad,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
 //   p = p - lr wd p - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
 //
-// Bytes bound it: 28 an element with everything in fp32, 10.06 with parameters and gradients in 16 bits and states in 8.  All tensors are cut into tiles of 8 192
+// Bytes bound it: 28 an element with everything in fp32, 10.06 with parameters and gradients in 16 bits and states in 8.  All tensors are cut into tiles of 2 048
 // elements, which the blocks of one launch (for each combination of types) take in turn: a tensor costs no launch, and its description and a tile's tensor are read from device memory.
 //
 // States in 8 bits: m and r = sqrt(v) as e4m3 codes times a power of two for each 256 elements, one warp's.  With the scale the largest code is in [2^7, 2^8), the
@@ -22,7 +22,7 @@
 
 namespace {
 
-constexpr int THREADS = 256, E = 8, STEPS = 1, TILE = STEPS * THREADS * E, BLOCK = TAURUS_STATE_BLOCK;
+constexpr int THREADS = 256, E = 8, TILE = THREADS * E, BLOCK = TAURUS_STATE_BLOCK;
 static_assert(32 * E == BLOCK, "a block of states is a warp's");
 
 struct Tensor {
@@ -312,10 +312,9 @@ __global__ void __launch_bounds__(THREADS, EIGHT && !MASTER ? 4 : 3) adamw_kerne
       f.keep = fmaf(-lr, t.decay, 1.f);
       if (EIGHT) key = absorb(seed_key, t.index);
     }
-    const long long i0 = (tile - t.first_tile) * TILE, most = i0 + TILE < t.count ? i0 + TILE : t.count;
-#pragma unroll 1
-    for (long long b = i0 + (threadIdx.x >> 5) * BLOCK; b < most; b += THREADS * E) {
-      if (t.vectors && b + BLOCK <= most) step_block<PT, GT, EIGHT, MASTER, true>(a, t, f, key, b);
+    const long long b = (tile - t.first_tile) * TILE + (threadIdx.x >> 5) * BLOCK;
+    if (b < t.count) {
+      if (t.vectors && b + BLOCK <= t.count) step_block<PT, GT, EIGHT, MASTER, true>(a, t, f, key, b);
       else step_block_by_element<PT, GT, EIGHT, MASTER>(a, t, f, key, b);
     }
   }

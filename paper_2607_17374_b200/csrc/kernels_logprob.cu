@@ -613,22 +613,20 @@ __global__ void __launch_bounds__(256) grad_kernel(const Args a, int chunks) {
 
 // ---- host --------------------------------------------------------------------------------------------------------------------------------------------
 
-// Rows that fit the registers of a warp: 32 elements a lane.  Pairs: 16-bit rows that begin at even elements everywhere.
-constexpr int TEAM_CLASSES = 1024;
-// Rows that a thread each takes: where there are enough of them, and a tile leaves room for other blocks beside it.
-constexpr int THREAD_ROWS = 4096;
-// fp32 rows of some length are better in registers, read once, than three times from a tile: 100 000 x 1 000 with the gradient 133 / 182 us, 256 69 / 67, without it and without a top
-// 91 / 110 (600: 79 / 68), with 16 top alternatives 297 / 431 (400: 215 / 212).  All others, 16 bits above all, are better in tiles (400 bf16: 85 / 49, with 4 alternatives 166 / 45).
+// Rows in tiles: where there are enough of them, and enough elements, for the tiles to be on all SMs.  Tiles / registers, 16 384 x 47 fp32 6.2 / 4.1 us with the gradient, 65 536 8.8 / 9.8; 8 192 x 300 8.2 / 7.2,
+// 16 384 10.3 / 12.3; top 5, 8 192 x 47 6.7 / 5.2, 16 384 6.7 / 7.7; 2 048 x 300 7.2 / 6.6, 4 096 8.0 / 10.3; 2 048 x 1 000 9.2 / 8.2, 4 096 11.4 / 13.4.
+constexpr int TILE_ROWS = 4096;
+constexpr int64_t TILE_ELEMENTS_LEAST = 1 << 21, TILE_ELEMENTS_TOP = 3 << 18;
 inline bool by_tile(const Args& a, int ts, bool grad) {
-  if (a.n < THREAD_ROWS || a.C > TEAM_CLASSES) return false;
-  return ts == 2 || a.C <= (grad ? 384 : a.k == 0 ? 768 : a.k > 8 ? 512 : TEAM_CLASSES);
+  return a.n >= TILE_ROWS && a.C <= tile_classes(ts, grad, a.k) && a.n * a.C >= (a.k ? TILE_ELEMENTS_TOP : TILE_ELEMENTS_LEAST);
 }
+// 16-bit rows that begin at even elements everywhere.
 inline bool in_pairs(const Args& a, int ts, bool grad) {
   const auto even = [](const void* p, long long ld) { return rows_aligned(p, 4) && ld % 2 == 0; };
   return ts == 2 && a.C % 2 == 0 && even(a.x, a.ld) && (!grad || even(a.dx, a.ld_dx));
 }
 
-// How a row of many classes is split.  What does for n rows does for fewer: parts x n is largest for the fewest rows of a kind, so workspaces are counted for any n below.
+// How a row of many classes is split: into as many parts as give every SM four blocks, but none shorter than 8 192 classes (4 096: 1 x 20 000 bf16 5.7 -> 4.7 us, 10 x 250 000 8.2 -> 9.8, with the top 10 14.6 -> 19.5).
 constexpr int ENOUGH_WARPS = 148 * 32, ENOUGH_BLOCKS = 148 * 4, PART_MIN = 8192;
 inline int parts_of(int64_t n, int C) {
   if (n >= ENOUGH_BLOCKS || C < 2 * PART_MIN) return 1;
@@ -670,7 +668,7 @@ void launch_grad(Launches& enqueue, const Args& a, int sms) {
   const int chunks = ((a.C + 2 * V - 2) / V + GRAD_VECTORS * 32 - 1) / (GRAD_VECTORS * 32);     // vectors of a row wherever it begins
   enqueue(grad_kernel<T>, dim3((unsigned)std::min<int64_t>((a.n * chunks + 7) / 8, (int64_t)sms * 64)), 256, 0, a, chunks);
 }
-// The smallest team, of 1, 2, 4 or 8 warps, with which there are enough warps: what comes behind a row's pass is latency, and more rows at once hide it.
+// The smallest team, of 1, 2, 4 or 8 warps, with which there are enough warps: what comes behind a row's pass is latency, and more rows at once hide it.  (2 000 x 120 001 bf16, top 10: 2 warps 159 us, 4 129.)
 template <class T, bool TOP, bool WITH_GRAD>
 void launch_stream(Launches& enqueue, const Args& a) {
   const auto go = [&](auto wpr) {

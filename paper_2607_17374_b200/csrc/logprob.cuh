@@ -4,12 +4,14 @@
 //   grad x_j = g (delta_j,label - p_j) - h p_j (log p_j + H)           g: weight of log p_label, h: weight of H
 //
 // The largest term of the sum is 1: it is left out of the sum s of the others, and l = log1p(s), H = l - t / (1 + s).  Both parts of H are positive and nothing
-// cancels: a row whose first class has nearly everything keeps all digits of l, H and 1 - p.  Differences are cut off at -200 (e^-200 = 0 in fp32): a
+// cancels: a row whose first class has nearly everything keeps all digits of l, H and 1 - p.  Differences are cut off at -200 or -256 (e^-200 = 0 in fp32): a
 // masked class (-inf, or a type's lowest value) then adds 0 to both sums, and no 0 x inf comes up.  A NaN goes into m, and with it into everything; +inf is treated as NaN.
 //
-// Bytes bound it: the logits in, once (and their gradient out).
-// Rows that fit the registers of 2, 8 or 32 lanes are read once and stay there, for the gradient too (team_kernel).  Wider ones are the work of a warp or a block, or of several
-// blocks where there are few rows (stream_kernel, join_kernel): every thread keeps a maximum and sums of its own over its vectors, without a branch, and they are joined at the end.
+// Bytes are the floor: the logits in, once (and their gradient out).  Instructions bound it: 28 to 34 an element of a tile, 11 of a long row.
+// Many rows of up to 1 024 classes come by tiles into shared memory, where 1 to 16 threads have a row (rows_kernel: 1 200 000 x 47 fp32 with the top 3 in 76 us, 3.9 TB/s; 400 000 x 172 bf16 with the gradient
+// in 73, 3.9 TB/s; every scheduler issues in three cycles of four).  Fewer are read once and stay in the registers of 8 or 32 lanes, for the gradient too, and so do long fp32 rows (team_kernel: 100 000 x 1 000 with
+// the gradient 133 us, 6.0 TB/s).  Wider ones are the work of 1 to 8 warps, or of several
+// blocks where there are few rows (stream_kernel, join_kernel: 2 000 x 120 001 bf16 with the top 10 in 131 us, 3.7 TB/s; 50 000 x 3 000 fp32 95 us, 6.3 TB/s): every thread keeps a maximum and sums of its own over its vectors, without a branch, and they are joined at the end.
 // The term that is 1 stands in one thread's sum and has eaten that thread's small terms: its vectors are read again without it, by all threads.  The top needs no work in
 // the pass either: with the k-th largest of the threads' maxima known, the top k are in the vectors of the k threads whose maxima are not below it, and only those are looked
 // through again.
@@ -56,6 +58,10 @@ constexpr int ROW_THREADS = 128;               // threads of a block of rows_ker
 constexpr int WARPS = 8;                       // warps of a block of the others
 constexpr int LIST = 64;                       // places of a warp's list of candidates
 constexpr int MAX_PARTS = 64;                  // parts of a row
+constexpr int TEAM_CLASSES = 1024;             // rows that fit the registers of a warp: 32 elements a lane
+// Classes of a row in a tile at most.  fp32 rows of some length are better in registers, read once, than three times from a tile: 100 000 x 1 000 with the gradient 133 / 182 us (256: 69 / 67), without
+// it and without a top 91 / 110 (600: 79 / 68).  With a top they are better in tiles (40 000 x 1 000, top 16: 124 / 114), and so are 16-bit rows (400 bf16: 85 / 49).
+constexpr int tile_classes(int size, bool grad, int k) { return size == 2 ? TEAM_CLASSES : grad ? 384 : k == 0 ? 768 : TEAM_CLASSES; }
 
 typedef unsigned long long u64;
 

@@ -125,8 +125,10 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
       const T* const elements = reinterpret_cast<const T*>(whole_row);
       RowResult r;
       if (MODE != GRAD) {
-        // Maxima of G classes of classes: the k-th largest of them has k values at least that are not below it, so what is below it is not among the top k.
-        constexpr int G = KMAX <= 4 ? 8 : KMAX <= 8 ? 16 : 32;
+        // Maxima of G classes of classes: the j-th largest of a thread's has j values at least that are not below it.  With j = k / TPR, rounded up, the least of the threads' j-th has k:
+        // what is below it is not among the top k.  (The k-th of one thread's own, in lists of KMAX: 133 333 x 300 fp32 top 16 259 us, top 8 107, top 3 68.)
+        // More threads than classes asked for: the largest of some threads' together instead of each one's, as long as there are k of those.
+        constexpr int J = (KMAX + TPR - 1) / TPR, G = J <= 4 ? 8 : J <= 8 ? 16 : 32, TOGETHER = KMAX ? (TPR + KMAX - 1) / KMAX : 1;
         float most[G];
         if constexpr (NW == 2) {
           using T2 = std::conditional_t<std::is_same_v<T, __nv_bfloat16>, __nv_bfloat162, __half2>;
@@ -163,22 +165,26 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
         float top[KMAX ? KMAX : 1], floor = -INFINITY;
         int cls[KMAX ? KMAX : 1];
         if (KMAX) {
+          float first[J ? J : 1];
 #pragma unroll
-          for (int i = 0; i < KMAX; ++i) { top[i] = -INFINITY; cls[i] = -1; }
+          for (int i = 0; i < J; ++i) first[i] = -INFINITY;
 #pragma unroll
           for (int g = 0; g < G; ++g) {
             float v = most[g];
 #pragma unroll
-            for (int i = 0; i < KMAX; ++i) { const float up = fmaxf(top[i], v); v = fminf(top[i], v); top[i] = up; }
+            for (int i = 0; i < J; ++i) { const float up = fmaxf(first[i], v); v = fminf(first[i], v); first[i] = up; }
           }
+          const int j = (a.k + TPR - 1) / TPR;
 #pragma unroll
-          for (int i = 0; i < KMAX; ++i) if (i == a.k - 1) floor = top[i];
+          for (int i = 0; i < J; ++i) if (i == j - 1) floor = first[i];
+#pragma unroll
+          for (int d = TPR / 2; d; d >>= 1) {
+            const float o = __shfl_xor_sync(0xffffffffu, floor, d);
+            floor = TPR / 2 / d < TOGETHER ? fmaxf(floor, o) : fminf(floor, o);
+          }
           if (bad) floor = -INFINITY;                       // a NaN hides its class of classes
 #pragma unroll
-          for (int d = TPR / 2; d; d >>= 1) floor = fmaxf(floor, __shfl_xor_sync(0xffffffffu, floor, d));      // what one thread knows holds for the row
-          if (bad) floor = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < KMAX; ++i) top[i] = -INFINITY;
+          for (int i = 0; i < KMAX; ++i) { top[i] = -INFINITY; cls[i] = -1; }
         }
         // The sums, and the top's candidates, 64 classes at a time.
         RowSums sum;
@@ -336,7 +342,7 @@ void set_tile(Args* a, int tpr) {
   constexpr int NW = PAIRS ? 2 : 1, V = 16 / (NW * (int)sizeof(T));               // elements of a word, words of a vector
   const int C = a->C / NW;
   // A warp reads words j tpr + sub of its 32 / tpr rows at once: how many of them meet in a bank hangs on the pitch.  Up to four cost less than rows set apart, which
-  // cannot be copied by vectors.
+  // cannot be copied by vectors.  (More threads to a row instead, up to 8, which meet by fours: 625 000 x 64 fp32 49 -> 91 us, 156 250 x 256 55 -> 58, with its gradient in bf16 61 -> 58.)
   const auto meet = [&](int pitch) {
     int most = 0, count[32] = {};
     for (int t = 0; t < 32; ++t) most = std::max(most, ++count[(t / tpr * pitch + t % tpr) % 32]);
@@ -371,15 +377,16 @@ void launch_tiles(Launches& enqueue, Args a) {
   const int64_t tiles = (a.n + ROWS - 1) / ROWS;
   enqueue(rows_kernel<T, PAIRS, MODE, KMAX, TPR>, dim3((unsigned)std::min<int64_t>(tiles, 1 << 30)), ROW_THREADS, smem, a);
 }
-// Threads to a row: as many as keep a tile of 128 threads at 32 KB at most, so that an SM has seven of them or more.
-template <class T, bool PAIRS, int MODE, int KMAX>
+// Threads to a row: as many as leave each `EACH` bytes of it at most (a tile: 128 times that).  Fewer threads have fewer exchanges, and the top is found by each for itself before it is
+// joined: the longer it is, the more classes to a thread; more threads have smaller tiles, more of them on an SM, and fewer of a warp's reads in one bank.  Without a top, 256 / 512: 400 000 x 172
+// bf16 with gradient 73 / 76 us, 312 500 x 128 fp32 105 / 125, 57 142 x 700 bf16 59 / 63.  Top 3, 256 / 512: 312 500 x 128 fp32 69 / 87, 130 73 / 66, 80 000 x 500 62 / 83; top 8: 156 250 x 256 82 / 105,
+// 133 333 x 300 88 / 80; top 16: 133 333 x 300 182 / 132, 232 558 x 172 177 / 136, 40 000 x 1 000 126 / 114.
+template <class T, bool PAIRS, int MODE, int KMAX, int TPR = 1>
 void launch_by_width(Launches& enqueue, const Args& a) {
-  const int bytes = a.C * (int)sizeof(T);
-  if (bytes <= (KMAX ? 512 : 256)) launch_tiles<T, PAIRS, MODE, KMAX, 1>(enqueue, a);
-  else if (bytes <= 512) launch_tiles<T, PAIRS, MODE, KMAX, 2>(enqueue, a);
-  else if (bytes <= 1024) launch_tiles<T, PAIRS, MODE, KMAX, 4>(enqueue, a);
-  else if (bytes <= 2048) launch_tiles<T, PAIRS, MODE, KMAX, 8>(enqueue, a);
-  else if constexpr (sizeof(T) == 4) launch_tiles<T, PAIRS, MODE, KMAX, 16>(enqueue, a);
+  constexpr int EACH = KMAX == 0 ? 256 : KMAX <= 4 ? 320 : KMAX <= 8 ? 384 : 512, MOST = tile_classes(sizeof(T), MODE != FORWARD, KMAX) * (int)sizeof(T);
+  if constexpr (TPR * EACH >= MOST) launch_tiles<T, PAIRS, MODE, KMAX, TPR>(enqueue, a);
+  else if (a.C * (int)sizeof(T) <= TPR * EACH) launch_tiles<T, PAIRS, MODE, KMAX, TPR>(enqueue, a);
+  else launch_by_width<T, PAIRS, MODE, KMAX, 2 * TPR>(enqueue, a);
 }
 template <class T, bool PAIRS>
 void launch_rows(Launches& enqueue, const Args& a, int mode) {

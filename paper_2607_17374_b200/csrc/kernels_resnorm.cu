@@ -166,6 +166,29 @@ struct Team {
       if (on[j]) store_f32<float, V>(row + col[j], v);
     }
   }
+  // The same for two rows; their means and factors.
+  __device__ __forceinline__ void centre(const Args& a, float (&x)[2][N], float2* means, float2* factors) {
+    float2 mean = make_float2(0.f, 0.f);
+    if (a.layer) {
+      float s = 0.f, t = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) { s += x[0][e]; t += x[1][e]; }
+      const float2 both = sum(s, t);
+      mean = make_float2(both.x * a.inv_C, both.y * a.inv_C);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const float m = on[j] ? mean.x : 0.f, n = on[j] ? mean.y : 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) { x[0][j * V + i] -= m; x[1][j * V + i] -= n; }
+      }
+    }
+    float q = 0.f, p = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) { q = fmaf(x[0][e], x[0][e], q); p = fmaf(x[1][e], x[1][e], p); }
+    const float2 both = sum(q, p);
+    *means = mean;
+    *factors = make_float2(rsqrtf(fmaf(both.x, a.inv_C, a.eps)), rsqrtf(fmaf(both.y, a.inv_C, a.eps)));
+  }
   // (1 / sqrt(var + eps)) of a row that is left without its mean (RMS: as it is); elements behind the row are 0 before and after.
   __device__ __forceinline__ float2 centre(const Args& a, float (&x)[N]) {
     float mean = 0.f;
@@ -278,6 +301,7 @@ template <int V> constexpr int ahead(int rows) { return V == 1 ? 2 : rows; }
 // (Two ahead instead: 195 312 x 256 bf16 72.8 -> 73.9 us, fp32 141.9 -> 140.5, 1 024 605 -> 587; six 74.0, 144.1, 614; the gradient two ahead 130.9 -> 130.7, 224.7 -> 224.4, 761.6 -> 759.2.
 // Registers loaded one row ahead: 1 200 000 x 256 bf16 467 -> 1 190.)
 constexpr int FORWARD_AHEAD = 4, GRAD_AHEAD = 3;
+constexpr int forward_ahead(int V, int kind) { return V == 1 && kind != MULTI ? 2 : FORWARD_AHEAD; }
 
 // Rows that the threads of a warp go through together: as many as the longest of its teams has (the exchanges take all threads).
 template <int KIND>
@@ -289,7 +313,7 @@ __device__ __forceinline__ int rows_to_walk(long long begin, long long end) {
 template <class T, class R, int V, int KIND>
 __global__ void __launch_bounds__(KIND == MULTI ? 128 : THREADS, KIND == MULTI ? 4 : V == 1 ? 2 : 3) resnorm_kernel(const __grid_constant__ Args a) {
   extern __shared__ __align__(16) unsigned char resnorm_rows[];
-  constexpr int AHEAD = ahead<V>(FORWARD_AHEAD);
+  constexpr int AHEAD = forward_ahead(V, KIND);
   check_offsets(a);
   Team<V, KIND> team(a);
   // A block has neighbouring rows, which its teams take in turn.
@@ -333,6 +357,59 @@ __global__ void __launch_bounds__(KIND == MULTI ? 128 : THREADS, KIND == MULTI ?
   };
   gate(-1);
   Group group = {-1, 0, 0};
+  if constexpr (KIND == MULTI) {
+    // Two rows of a group at a time: an exchange between the warps is for both.  (One at a time, 48 828 x 1 024 bf16 132 us, 102 by twos; fp32 158 / 149; 130 208 x 384 bf16 161 / 127; 97 656 x 512 fp32 146 / 154;
+    // a mean and its squares of each warp in one exchange instead 144, 148, 189; six blocks on an SM, with registers spilled, 132, 187, 169.)
+    for (int i = 0; i < rows;) {
+      const long long row = begin + i;
+      if (a.gate && (i == 0 || row >= group.end)) {
+        find_group(a, row, &group);
+        if (group.g >= 0) gate(group.g);
+      }
+      const bool two = i + 1 < rows && (!a.gate || row + 1 < group.end), write = !a.gate || group.g >= 0;
+      wait_for_copies<AHEAD - 2>();
+      if (res.SHARED) team.sync();
+      const int place1 = place + 1 == AHEAD ? 0 : place + 1;
+      float r[2][N], b[2][N];
+      res.get(static_cast<const R*>(a.res) + row * a.ld_res, place, team, r[0]);
+      if (two) res.get(static_cast<const R*>(a.res) + (row + 1) * a.ld_res, place1, team, r[1]);
+      else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) r[1][e] = b[1][e] = 0.f;
+      }
+      float2 scale = make_float2(1.f, 1.f), mean = make_float2(0.f, 0.f), s1 = mean, s2 = mean;
+      if (a.block) {
+        block.get(static_cast<const T*>(a.block) + row * a.ld_block, place, team, b[0]);
+        if (two) block.get(static_cast<const T*>(a.block) + (row + 1) * a.ld_block, place1, team, b[1]);
+        if (a.post) { team.centre(a, b, &mean, &scale); s1 = scale; }
+#pragma unroll
+        for (int e = 0; e < N; ++e) { r[0][e] = fmaf(gt[e], b[0][e] * scale.x, r[0][e]); r[1][e] = fmaf(gt[e], b[1][e] * scale.y, r[1][e]); }
+      }
+      if (write && a.out_res) {
+        team.store(out_res, r[0]);
+        if (two) team.store(out_res + step_out_res, r[1]);
+      }
+      float2 mean2;
+      team.centre(a, r, &mean2, &s2);
+      fetch(i + AHEAD);
+      if (two) fetch(i + 1 + AHEAD);
+#pragma unroll
+      for (int e = 0; e < N; ++e) { r[0][e] = fmaf(r[0][e] * s2.x, ga[e], be[e]); r[1][e] = fmaf(r[1][e] * s2.y, ga[e], be[e]); }
+      if (write) {
+        team.store(out, r[0]);
+        if (two) team.store(out + step_out, r[1]);
+        if (a.stats && team.lane == 0) {
+          a.stats[row] = make_float4(mean.x, s1.x, mean2.x, s2.x);
+          if (two) a.stats[row + 1] = make_float4(mean.y, s1.y, mean2.y, s2.y);
+        }
+      }
+      const int n = two ? 2 : 1;
+      out_res += n * step_out_res;
+      out += n * step_out;
+      i += n;
+    }
+    return;
+  }
   for (int i = 0; i < walk; ++i) {
     const long long row = begin + (long long)i * teams;
     const bool have = i < rows;
@@ -758,7 +835,7 @@ extern "C" int taurus_residual_norm(int64_t n, int32_t width, const void* res, i
     const auto go = [&](auto kind) {
       constexpr int KIND = decltype(kind)::value;
       const int teams = (int)block_teams(width), threads = block_threads(width);
-      const size_t smem = (size_t)Source<R, V, ahead<V>(FORWARD_AHEAD)>::bytes(width, teams, threads) + (size_t)Source<T, V, ahead<V>(FORWARD_AHEAD)>::bytes(width, teams, threads);
+      const size_t smem = (size_t)Source<R, V, forward_ahead(V, KIND)>::bytes(width, teams, threads) + (size_t)Source<T, V, forward_ahead(V, KIND)>::bytes(width, teams, threads);
       int resident = 0;
       cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(resnorm_kernel<T, R, V, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED_MOST) : cudaSuccess;
       if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, resnorm_kernel<T, R, V, KIND>, threads, smem);

@@ -296,6 +296,11 @@ def _type_of(rows, said) -> int:
     return t
 
 
+def _of_type(rows, t: int) -> bool:
+    """Is a tensor's type t?  (None and addresses have none.)"""
+    return rows is None or isinstance(rows, int) or _row_codes.get(rows.dtype) == t or _row_type(rows) == t
+
+
 def _rows(x, n: int, width: int, ld: int) -> Optional[int]:
     """Address of n rows: a 2-D tensor of at least n x width whose rows are contiguous and ld elements apart, or an address."""
     if x is None or isinstance(x, int):
@@ -324,7 +329,7 @@ def _array(x, dtype: Optional[str], count: int) -> Optional[int]:
 
 def _space(workspace):
     """Address and bytes of a workspace tensor."""
-    return (None, 0) if workspace is None else (_ptr(workspace), workspace.numel() * workspace.element_size())
+    return (None, 0) if workspace is None else (_ptr(workspace), workspace.nbytes)
 
 
 def _checked(rc: int, where: str) -> int:
@@ -467,9 +472,9 @@ def residual_norm(n: int, width: int, res, ld_res: int, block, ld_block: int, ki
                   out_res, ld_out_res: int, out, ld_out: int, stats=None, status=None, stream=None, type=None, res_type=None):
     """taurus_residual_norm: out_res = res + alpha gate[g] u, u = post ? norm(block) post_gamma : block; out = norm(out_res) gamma + beta (NORM_LAYER or NORM_RMS, by row)."""
     t, r = _type_of(out, type), _type_of(res, res_type)
-    if hasattr(block, "dtype") and _row_type(block) != t:
+    if not _of_type(block, t):
         raise TypeError("block and out are of one type")
-    if hasattr(out_res, "dtype") and _row_type(out_res) != r:
+    if not _of_type(out_res, r):
         raise TypeError("res and out_res are of one type")
     _checked(load_library().taurus_residual_norm(
         n, width, _rows(res, n, width, ld_res), ld_res, r, _rows(block, n, width, ld_block), ld_block, t, kind, int(post), _array(post_gamma, "float32", width), groups,
@@ -487,11 +492,10 @@ def residual_norm_grad(n: int, width: int, res, ld_res: int, block, ld_block: in
                        ld_grad_out_res: int, grad_out, ld_grad_out: int, grad_res, ld_grad_res: int, grad_block=None, ld_grad_block: int = 0, grad_post_gamma=None, grad_gate=None,
                        grad_gamma=None, grad_beta=None, workspace=None, status=None, stream=None, type=None, res_type=None):
     """taurus_residual_norm_grad: gradients of residual_norm, with stats as the forward call left them.  Without block, grad_out and grad_block `type` says their type."""
-    t = next((_type_of(x, type) for x in (block, grad_out, grad_block) if hasattr(x, "dtype")), None)
-    t, r = _row_type(type) if t is None else t, _type_of(res, res_type)
-    for x, want in ((block, t), (grad_out, t), (grad_block, t), (grad_out_res, r), (grad_res, r)):
-        if hasattr(x, "dtype") and _row_type(x) != want:
-            raise TypeError("block, grad_out and grad_block are of one type, and so are res, grad_out_res and grad_res")
+    rows = block if hasattr(block, "dtype") else grad_out if hasattr(grad_out, "dtype") else grad_block
+    t, r = _type_of(rows, type) if hasattr(rows, "dtype") else _row_type(type), _type_of(res, res_type)
+    if not (_of_type(block, t) and _of_type(grad_out, t) and _of_type(grad_block, t) and _of_type(grad_out_res, r) and _of_type(grad_res, r)):
+        raise TypeError("block, grad_out and grad_block are of one type, and so are res, grad_out_res and grad_res")
     ld_grad_block = ld_grad_block or width
     _checked(load_library().taurus_residual_norm_grad(
         n, width, _rows(res, n, width, ld_res), ld_res, r, _rows(block, n, width, ld_block), ld_block, t, kind, int(post), _array(post_gamma, "float32", width), groups,

@@ -658,7 +658,7 @@ __global__ void __launch_bounds__(JOIN * JOIN) resnorm_join_kernel(const Args a,
   }
   if (!a.d_gate) return;
   // Groups over several teams: up to SHORT parts by one warp, a column a thread; more by the block.
-  constexpr int SHORT = 4 * JOIN;
+  constexpr int SHORT = 4 * JOIN;                                     // (32: gradient of 3 000 x 1 024 in 10 groups 31.0 -> 34.9 us, of 300 000 in 300 1 174 -> 1 300)
   __shared__ int longer[JOIN];
   for (long long t0 = unit0 * JOIN; t0 < a.teams; t0 += units * JOIN) {
     const long long t = t0 + ty;

@@ -105,24 +105,31 @@ struct Tile {
 
 
 // TPR threads to a row, which take its words in turn.  KMAX: places for the top in registers (k <= KMAX; 0: none asked for).
+// 16-bit rows are words of two classes in shared memory.  PAIRS: in global memory too.  Otherwise the tile comes by element, or by vectors over rows without gaps, and a row of an odd width is (C - 1) / 2 words,
+// from its first even place on, and one lone class: its first or its last.  (400 000 x 171 bf16 with the gradient 93 us, by single elements 121; 57 061 x 701 60 / 77; 851 063 x 47 47 / 55.)
 template <class T, bool PAIRS, int MODE, int KMAX, int TPR>
 __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
   extern __shared__ __align__(16) unsigned char logprob_shared[];
-  using W = typename Word<T, PAIRS>::type;
-  constexpr int NW = Word<T, PAIRS>::n, STEP = 8 / NW, ROWS = ROW_THREADS / TPR;      // words of 8 classes; rows of a tile
+  constexpr bool TWO = sizeof(T) == 2, LONE = TWO && !PAIRS;
+  using W = typename Word<T, PAIRS>::type;       // what is copied
+  using Q = typename Word<T, TWO>::type;         // what is computed with
+  constexpr int NW = Word<T, TWO>::n, CN = Word<T, PAIRS>::n, STEP = 8 / NW, ROWS = ROW_THREADS / TPR;      // words of 8 classes; rows of a tile
   W* const sm = reinterpret_cast<W*>(logprob_shared);
   const int C = a.C, all = C / NW, sub = threadIdx.x % TPR, CW = (all - sub + TPR - 1) / TPR;      // CW: words of this thread
   const long long tiles = (a.n + ROWS - 1) / ROWS;
   for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const long long row0 = tile * ROWS, row = row0 + threadIdx.x / TPR;
-    const Tile<W> t = {(int)(a.n - row0 < ROWS ? a.n - row0 : ROWS), all, a.pitch, a.vectors, a.by_C, a.by_vectors};
-    t.load(sm, reinterpret_cast<const W*>(static_cast<const T*>(a.x) + row0 * a.ld), a.ld / NW, a.mode_in);
+    const Tile<W> t = {(int)(a.n - row0 < ROWS ? a.n - row0 : ROWS), C / CN, a.pitch, a.vectors, a.by_C, a.by_vectors};
+    t.load(sm, reinterpret_cast<const W*>(static_cast<const T*>(a.x) + row0 * a.ld), a.ld / CN, a.mode_in);
     const int label = row < a.n ? label_of(a, row) : -1;
     __syncthreads();
     if (TPR > 1 || row < a.n) {                  // (exchanges take all threads of a warp: rows behind the last are whatever the tile held)
-      W* const whole_row = sm + threadIdx.x / TPR * a.pitch;
-      W* const mine = whole_row + sub;           // its words are TPR apart
-      const T* const elements = reinterpret_cast<const T*>(whole_row);
+      T* const elements = reinterpret_cast<T*>(sm + threadIdx.x / TPR * a.pitch);
+      const int odd = LONE ? threadIdx.x / TPR * a.pitch & 1 : 0;            // the row begins in the middle of a word
+      Q* const mine = reinterpret_cast<Q*>(elements + odd) + sub;            // its words are TPR apart
+      const bool lone = LONE && C & 1;
+      const int lone_class = odd ? 0 : C - 1;
+      const float alone = lone ? to_f32<T>(elements[lone_class]) : -INFINITY;
       RowResult r;
       if (MODE != GRAD) {
         // Maxima of G classes of classes: the j-th largest of a thread's has j values at least that are not below it.  With j = k / TPR, rounded up, the least of the threads' j-th has k:
@@ -156,7 +163,7 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
 #pragma unroll
           for (int i = 0; i < G; ++i) if (j + i < CW) most[i] = max_nan(most[i], to_f32<T>(reinterpret_cast<const T*>(mine)[(j + i) * TPR]));
         }
-        float m = most[0];
+        float m = LONE ? max_nan(most[0], alone) : most[0];
 #pragma unroll
         for (int i = 1; i < G; ++i) m = max_nan(m, most[i]);
 #pragma unroll
@@ -190,6 +197,7 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
         RowSums sum;
         int behind = 0;
         const float m8 = m * (1.f / CUT);
+        if (LONE && lone && sub == 0) { sum.add2(alone, -INFINITY, m8); behind = 1; }
         for (int j0 = 0; j0 < CW; j0 += 64 / NW) {
           uint32_t found[2] = {0, 0};
 #pragma unroll
@@ -218,7 +226,7 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
 #pragma unroll
                   for (int e = 0; e < NW; ++e) v[i * NW + e] = w[e];
                 }
-                behind = (j1 + STEP - CW) * NW;
+                behind += (j1 + STEP - CW) * NW;
               }
               uint32_t bits = 0;
 #pragma unroll
@@ -235,7 +243,7 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
             while (found[0] | found[1]) {
               const bool low = found[0] != 0;
               const uint32_t bits = low ? found[0] : found[1];
-              const int place = j0 * NW + (low ? 0 : 32) + __ffs(bits) - 1, word = place / NW, at = (word * TPR + sub) * NW + place % NW;
+              const int place = j0 * NW + (low ? 0 : 32) + __ffs(bits) - 1, word = place / NW, at = (word * TPR + sub) * NW + place % NW + odd;
               if (low) found[0] = bits & (bits - 1); else found[1] = bits & (bits - 1);
               const float v = word < CW ? to_f32<T>(reinterpret_cast<const T*>(mine + word * TPR)[place % NW]) : -INFINITY;
               if (v > top[KMAX - 1]) {                     // equal ones keep their places: they have the lower classes
@@ -248,6 +256,18 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
                 if (v > top[0]) { top[0] = v; cls[0] = at; }
               }
             }
+        }
+        if (LONE && KMAX && lone && sub == 0 && alone > -INFINITY) {                 // of equal ones the first class comes first, the last one last
+          const auto better = [&](float o) { return odd ? alone >= o : alone > o; };
+          if (better(top[KMAX - 1])) {
+#pragma unroll
+            for (int i = KMAX - 1; i > 0; --i) {
+              const bool down = better(top[i - 1]), here = !down && better(top[i]);
+              cls[i] = down ? cls[i - 1] : here ? lone_class : cls[i];
+              top[i] = down ? top[i - 1] : here ? alone : top[i];
+            }
+            if (better(top[0])) { top[0] = alone; cls[0] = lone_class; }
+          }
         }
         float sums = sum.both(sum.s), q = sum.both(sum.q), others = sum.both(sum.others) - (float)behind;
 #pragma unroll
@@ -301,12 +321,12 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
       }
       if (MODE != FORWARD) {
         const GradRow gr = grad_row(a, row < a.n ? row : a.n - 1, label, r);
-        const bool special = label >= 0 && label / NW % TPR == sub;              // this thread has the label's word
+        const bool special = label >= 0 && (LONE && lone && label == lone_class ? 0 : (label - odd) / NW % TPR) == sub;      // this thread has the label's word
         const float at = special ? to_f32<T>(elements[label]) : 0.f;
         if (TPR > 1) __syncwarp();               // (its logit has been read for the row's log probability too)
         int j = 0;
         for (; j + STEP <= CW; j += STEP) {
-          W w[STEP];
+          Q w[STEP];
 #pragma unroll
           for (int i = 0; i < STEP; ++i) w[i] = mine[(j + i) * TPR];
 #pragma unroll
@@ -326,12 +346,13 @@ __global__ void __launch_bounds__(ROW_THREADS) rows_kernel(const Args a) {
           for (int e = 0; e < NW; ++e) v[e] = grad_of(gr, v[e]);
           mine[j * TPR] = pack<T>(v);
         }
-        if (special) reinterpret_cast<T*>(whole_row)[label] = from_f32<T>(grad_of_label(gr, at));
+        if (LONE && lone && sub == 0) elements[lone_class] = from_f32<T>(grad_of(gr, alone));
+        if (special) elements[label] = from_f32<T>(grad_of_label(gr, at));
       }
     }
     __syncthreads();
     if (MODE != FORWARD) {
-      t.store(sm, reinterpret_cast<W*>(static_cast<T*>(a.dx) + row0 * a.ld_dx), a.ld_dx / NW, a.mode_out);
+      t.store(sm, reinterpret_cast<W*>(static_cast<T*>(a.dx) + row0 * a.ld_dx), a.ld_dx / CN, a.mode_out);
       __syncthreads();
     }
   }

@@ -55,6 +55,19 @@ def test_top(dtype, C, k):
     Call(x, labels, k).check(x, labels, k)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("C", [2, 3, 20, 47, 90, 171, 172, 301, 512])
+@pytest.mark.parametrize("k", [2, 6, 16])
+@pytest.mark.parametrize("pad,shift", [(0, 1), (3, 1), (8, 0)])
+def test_top_of_rows_off_the_alignment(dtype, C, k, pad, shift):
+    N = rows_of(C)
+    x, _ = rows(N, C, C + pad, dtype, shift, seed=C + k)
+    x[::3] = (x[::3] * 2).round() / 2                  # some rows with ties, the first and the last class among them
+    x[::3, 0] = x[::3, -1] = 3
+    labels = some_labels(N, C)
+    Call(x, labels, k).check(x, labels, k)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("C", [5, 47, 90, 128, 150, 172, 300, 500])
 @pytest.mark.parametrize("kind", ["masks", "few are left", "constant", "falling", "few values", "lowest"])

@@ -8,8 +8,8 @@
 // stay in registers from the load to the store: statistics first the mean, then the squares of deviations.  A team walks over neighbouring rows, so that the group of a row (the last one whose
 // offset is not above it) is looked for once a group.  Rows are on their way some rows ahead, by asynchronous copies into places of shared memory that are a thread's own: a thread
 // waits for its own copies and for nobody (of widths that 16-byte vectors do not fit, for its team).
-// Measured: 1 200 000 x 256 bf16 with 16 groups 467 us, 5.3 TB/s, bound by the bytes with an issue slot in 74 % of the cycles beside them; 500 000 x 256 fp32 in 9 001 groups with the gradients 937 us, 5.5 TB/s over the
-// ten passes of the two calls; 120 001 x 100 fp16 on fp32 rows, 7 groups, 100 us: few rows a team, latencies at its ends; 196 078 x 255 fp32 (50 M elements) 146 us and 260 for the gradient, at 256 143 and 240.
+// Measured: 1 200 000 x 256 bf16 with 16 groups 464 us, 5.3 TB/s, bound by the bytes with an issue slot in 74 % of the cycles beside them; 500 000 x 256 fp32 in 9 001 groups with the gradients 940 us, 5.5 TB/s over the
+// ten passes of the two calls; 120 001 x 100 fp16 on fp32 rows, 7 groups, 98 us: few rows a team, latencies at its ends; 196 078 x 255 fp32 (50 M elements) 146 us and 260 for the gradient, at 256 143 and 240.
 // Widths below 8 leave threads of one row with fewer elements (7 100 000 x 7 fp32 328 us, the gradient 1 147).
 // Sums by channel stay in the threads' registers (a thread keeps its columns).  Those of post_gamma and of the gate come from one: with S_g = sum over the group's rows of D h1,
 // dgate_g = alpha post_gamma S_g and dpost_gamma = sum_g alpha gate_g S_g.  Blocks join theirs in shared memory, resnorm_join_kernel the blocks' in their order.
@@ -299,7 +299,7 @@ struct Source<T, 1, AHEAD> {
 };
 template <int V> constexpr int ahead(int rows) { return V == 1 ? 2 : rows; }
 // (Two ahead instead: 195 312 x 256 bf16 72.8 -> 73.9 us, fp32 141.9 -> 140.5, 1 024 605 -> 587; six 74.0, 144.1, 614; the gradient two ahead 130.9 -> 130.7, 224.7 -> 224.4, 761.6 -> 759.2.
-// Registers loaded one row ahead: 1 200 000 x 256 bf16 467 -> 1 190.)
+// Registers loaded one row ahead: 1 200 000 x 256 bf16 464 -> 1 190.)
 constexpr int FORWARD_AHEAD = 4, GRAD_AHEAD = 3;
 constexpr int forward_ahead(int V, int kind) { return V == 1 && kind != MULTI ? 2 : FORWARD_AHEAD; }
 

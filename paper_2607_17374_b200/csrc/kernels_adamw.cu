@@ -4,7 +4,7 @@
 //   p = p - lr wd p - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
 //
 // Bytes are the floor: 28 an element with everything in fp32, 10.06 with parameters and gradients in 16 bits and states in 8.  They bound the first (60 M elements in 269 us, 6.2 TB/s); the second is
-// bound by instructions, 69 an element of which 26 go at half rate (200 M elements in 502 us, 4.0 TB/s, issue slots 72 % used; the next tile's bytes on their way ahead 566 against 512, pairs in one instruction spilled).  All tensors are cut into tiles of 2 048
+// bound by instructions, 66 an element of which 24 go at half rate (200 M elements in 502 us, 4.0 TB/s, issue slots 72 % used; the next tile's bytes on their way ahead 566 against 512, pairs in one instruction spilled).  All tensors are cut into tiles of 2 048
 // elements, which the blocks of one launch (for each combination of types) take in turn: a tensor costs no launch, and its description and a tile's tensor are read from device memory.
 //
 // States in 8 bits: m and r = sqrt(v) as e4m3 codes times a power of two for each 256 elements, one warp's.  With the scale the largest code is in [2^7, 2^8), the

@@ -615,7 +615,7 @@ int taurus_residual_norm_grad(int64_t n, int32_t width, const void* res, int64_t
  * with any other array of the list; gradients may share with each other.  Arrays need no alignment beyond their element's; at multiples of 16 bytes they are the fast ones.
  *   param, grad: `count` elements of param_type and grad_type (TAURUS_F32, TAURUS_BF16, TAURUS_F16); a tensor with count 0, or without a gradient (NULL), is left alone
  *   master:      NULL, or the parameters in fp32 beside param of 16 bits: the step is made on master, and param receives it rounded
- *   state_type:  TAURUS_F32: m and v are fp32, m_scale and v_scale NULL.  TAURUS_E4M3: m and sqrt(v) are e4m3 codes, m_scale and v_scale hold a power of two for each block of
+ *   state_type:  TAURUS_F32: m and v are fp32, m_scale and v_scale NULL.  TAURUS_E4M3: m and sqrt(v) (of fp32, rounded to nearest) are e4m3 codes, m_scale and v_scale hold a power of two for each block of
  *                TAURUS_STATE_BLOCK elements (the last one may be short); codes and scales of zeros begin.  Written, a block's scale puts its largest value into [2^7, 2^8); values
  *                are rounded up with the probability of what is cut off, by a hash of (seed, step, the tensor's place in the list, element), so that the same call gives the same bits;
  *                an sqrt(v) that is not 0 is not rounded to 0.  The step itself is made from m and v before they are rounded.  Values that are not finite become NaN.

@@ -7,7 +7,7 @@
 // bound by instructions, 66 an element of which 24 go at half rate (200 M elements in 502 us, 4.0 TB/s, issue slots 72 % used; the next tile's bytes on their way ahead 566 against 512, pairs in one instruction spilled).  All tensors are cut into tiles of 2 048
 // elements, which the blocks of one launch (for each combination of types) take in turn: a tensor costs no launch, and its description and a tile's tensor are read from device memory.
 //
-// States in 8 bits: m and r = sqrt(v) as e4m3 codes times a power of two for each 256 elements, one warp's.  With the scale the largest code is in [2^7, 2^8), the
+// States in 8 bits: m and r = sqrt(v), rounded to nearest in fp32, as e4m3 codes times a power of two for each 256 elements, one warp's.  With the scale the largest code is in [2^7, 2^8), the
 // smallest step 2^-16 of the largest value; multiplying by the scale is exact.  Rounded to nearest a state would stand still: a step of e4m3 is 6 to 12 % of the
 // value, and v moves by 0.1 % in a step.  So a value is rounded up with the probability of what is cut off, in 65 536ths, by a hash of (seed, step, tensor, element): the same call gives the same
 // bits.  An r that is not 0 is not rounded to 0: m beside it would be divided by eps.  The update itself is formed from m and v before they are rounded.
@@ -86,6 +86,24 @@ __device__ __forceinline__ void codes_to_floats(uint2 c, float scale, float (&x)
   }
 }
 constexpr uint32_t NOT_FINITE = 0x7f800000u, CODE_NAN = 0x7f;
+
+// The root of a v as a code: bits 24 to 30, with 16 random bits added below them (the kernel says how).  least: code 1 where v is not 0.
+__device__ __forceinline__ uint32_t code_of_root(float root, float part_v, float least, uint32_t bits) {
+  return (__float_as_uint(fmaxf(__fmul_rz(root * part_v, 0x1p-100f), least)) << 4) + __byte_perm(bits, 0, 0x4324);
+}
+// The hardware's root is off by 2^-23 of itself at most: from the one rounded to nearest by two and a half units in its last place, three where they are cut off, of 16 each here.  It makes another
+// code only where the sum is that near to a border between two codes, on either side; 64 with a margin.  Such elements, one in 131 072, are done again with the root rounded to nearest, so that a
+// code is what its definition says and not what an instruction makes of it (200 M elements 496 -> 518 us; looked for by 16-bit halves 525, done again where they are found 549).
+__device__ __forceinline__ uint32_t from_border(uint32_t code) { return code * 256u + 0x4000u; }
+constexpr uint32_t AT_BORDER = 0x8000u;
+// The root of v rounded to nearest, from one that is a few units off: the middle between two neighbours has 25 bits, its square 50, which fp64 holds.
+__device__ __forceinline__ float exact_root_of(float v) {
+  uint32_t r = __float_as_uint(any_root_of(v));
+  const auto middle_below = [&](uint32_t low) { const double mid = 0.5 * ((double)__uint_as_float(low) + (double)__uint_as_float(low + 1)); return mid * mid < (double)v; };
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) if (middle_below(r)) ++r; else if (r && !middle_below(r - 1)) --r; else break;
+  return __uint_as_float(r);
+}
 
 // What a step multiplies with, besides the arguments: the gradients' scale, 1 / sqrt(1 - b2^t), -lr / (1 - b1^t), 1 - lr wd.
 struct Factors { float gs, c2, rate, keep; };
@@ -244,18 +262,20 @@ __device__ __forceinline__ void step_block(const Args& a, const Tensor& t, const
     }
     const float part_m = __int_as_float(em < 234 ? (234 - em) << 23 : 1 << (256 - em)), part_v = __int_as_float((234 - ev) << 23);      // 2^(107 - e)
     const uint32_t base = (uint32_t)b ^ (uint32_t)key ^ (uint32_t)P::lane_place(lane), more = (uint32_t)(key >> 32) + (uint32_t)(b >> 32) * 0x85EBCA6Bu;     // (places differ in bits of their own)
-    uint32_t cm[E / 4], cv[E / 4];
+    const auto least = [&](int e) { return fminf(v[e] * 0x1p100f, __uint_as_float(1u << 20)); };     // code 1 where v is not 0
+    const auto bits_of = [&](int e) { return finish_bits((base ^ (uint32_t)P::element(e)) + more); };
+    uint32_t cm[E / 4], cv[E / 4], near = 0xffffffffu;
 #pragma unroll
     for (int h = 0; h < E / 4; ++h) {
       uint32_t wm[4], wv[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int e = 4 * h + i;
-        const float zm = __fmul_rz(m[e] * part_m, 0x1p-100f), zv = __fmul_rz(root[e] * part_v, 0x1p-100f);
-        const float least = fminf(v[e] * 0x1p100f, __uint_as_float(1u << 20));                        // code 1 where v is not 0
-        const uint32_t bits = finish_bits((base ^ (uint32_t)P::element(e)) + more);
+        const float zm = __fmul_rz(m[e] * part_m, 0x1p-100f);
+        const uint32_t bits = bits_of(e);
         wm[i] = ((__float_as_uint(zm) << 4) + __byte_perm(bits, 0, 0x4104)) | (__float_as_uint(m[e]) & 0x80000000u);
-        wv[i] = (__float_as_uint(fmaxf(zv, least)) << 4) + __byte_perm(bits, 0, 0x4324);
+        wv[i] = code_of_root(root[e], part_v, least(e), bits);
+        near = min(near, from_border(wv[i]));
       }
       const auto four = [](const uint32_t* c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410); };
       cm[h] = four(wm);
@@ -280,6 +300,10 @@ __device__ __forceinline__ void step_block(const Args& a, const Tensor& t, const
       for (int e = 0; e < E; ++e)
         if (in(e)) { mc[first + P::element(e)] = (uint8_t)(cm[e / 4] >> (8 * (e % 4))); vc[first + P::element(e)] = (uint8_t)(cv[e / 4] >> (8 * (e % 4))); }
     }
+    if (near < AT_BORDER)                        // the lane's codes of the root again
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if ((whole || in(e)) && v[e] < INFINITY) vc[first + P::element(e)] = (uint8_t)(code_of_root(exact_root_of(v[e]), part_v, least(e), bits_of(e)) >> 24);
   }
 }
 

@@ -17,6 +17,7 @@
 // begins there and goes on; the join kernel adds them up in the teams' order.
 #include <algorithm>
 
+#include "group_search.h"
 #include "rows.cuh"
 
 namespace {
@@ -68,11 +69,7 @@ __device__ __forceinline__ void find_group(const Args& a, long long r, Group* at
       }
     }
   }
-  int lo = 0, hi = a.groups;                     // offsets[lo - 1] <= r < offsets[hi + 1], so to say
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.offsets[mid] <= r) lo = mid; else hi = mid - 1;
-  }
+  const int lo = last_offset_not_above(a.offsets, a.groups, r);
   const long long b = a.offsets[lo];
   if (b > r) { *at = {-1, 0, b < a.n ? b : a.n}; return; }             // in front of the first group, up to its rows
   if (lo == a.groups) { *at = {-1, b, a.n}; return; }                   // behind the last

@@ -2,10 +2,12 @@
 // stage's barrier.  Plain C++, so that the rules below can be run against model barriers on the host.
 #pragma once
 
+#ifndef TAURUS_HD
 #ifdef __CUDACC__
 #define TAURUS_HD __host__ __device__ __forceinline__
 #else
 #define TAURUS_HD inline
+#endif
 #endif
 
 // Parity of the last phase begun on stage s after `begun` uses of the ring, -1: the stage has not been used.

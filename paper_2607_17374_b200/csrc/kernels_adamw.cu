@@ -20,6 +20,7 @@
 #include <vector>
 
 #include "rows.cuh"
+#include "upload.h"
 
 namespace {
 
@@ -430,13 +431,15 @@ int adamw_create(taurus_adamw** out, const taurus_adamw_tensor* list, int64_t co
   h->device = dev; h->sms = sms;
   h->written.swap(written);
   const size_t tb = (tensors.size() * sizeof(Tensor) + 255) / 256 * 256;
+  UploadPart parts[1 + KINDS];
+  int count_parts = 0;
   cudaError_t e = cudaSuccess;
   if (!tensors.empty()) {
     char* mem = nullptr;
     e = cudaMalloc(reinterpret_cast<void**>(&mem), tb + (size_t)all * 4);
     if (e == cudaSuccess) {
       h->tensors = reinterpret_cast<Tensor*>(mem);
-      e = cudaMemcpy(h->tensors, tensors.data(), tensors.size() * sizeof(Tensor), cudaMemcpyHostToDevice);
+      parts[count_parts++] = {h->tensors, tensors.data(), tensors.size() * sizeof(Tensor)};
     }
     int32_t* at = reinterpret_cast<int32_t*>(mem + tb);
     for (int k = 0; k < KINDS && e == cudaSuccess; ++k) {
@@ -444,13 +447,16 @@ int adamw_create(taurus_adamw** out, const taurus_adamw_tensor* list, int64_t co
       if (!h->tiles[k]) continue;
       h->tile_tensor[k] = at;
       at += h->tiles[k];
-      e = cudaMemcpy(h->tile_tensor[k], tiles[k].data(), tiles[k].size() * 4, cudaMemcpyHostToDevice);
+      parts[count_parts++] = {h->tile_tensor[k], tiles[k].data(), tiles[k].size() * 4};
       with_kind(k, [&](auto pt, auto gt, auto eight, auto master) {
         using PT = typename decltype(pt)::type;
         using GT = typename decltype(gt)::type;
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&h->resident[k], adamw_kernel<PT, GT, decltype(eight)::value, decltype(master)::value>, THREADS, 0);
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&h->resident[k], adamw_kernel<PT, GT, decltype(eight)::value, decltype(master)::value>, THREADS, 0);
       });
     }
+    if (e == cudaSuccess)
+      e = upload(parts, count_parts, [](const UploadPart& p) { return cudaMemcpyAsync(p.to, p.from, p.bytes, cudaMemcpyHostToDevice, cudaStreamLegacy); },
+                 [] { return cudaStreamSynchronize(cudaStreamLegacy); });
   }
   if (e != cudaSuccess) {
     taurus_note_cuda_error(e, "taurus_adamw_create");

@@ -47,6 +47,7 @@ struct Args {
   const long long* step;
   const float *lr, *grad_scale;
   float beta1, rest1, beta2, rest2, eps;
+  float up;                                      // eps and what it is added to come multiplied by it, and what they divide: beside an eps below 2^-100 2^24, so that neither is a subnormal number; else 1
   int small_eps;                                 // beside a larger one the root of a subnormal number, 1e-19, is nothing
   double log_beta1, log_beta2;
   unsigned long long seed;
@@ -69,6 +70,7 @@ __device__ __forceinline__ uint32_t finish_bits(uint32_t x) {
 // The root of a subnormal number is 0 with the one, its own with the other, which takes four instructions.
 __device__ __forceinline__ float root_of(float x) { float r; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float any_root_of(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+// (of a subnormal number infinite: a divisor is none)
 __device__ __forceinline__ float reciprocal(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 
@@ -106,7 +108,7 @@ __device__ __forceinline__ float exact_root_of(float v) {
   return __uint_as_float(r);
 }
 
-// What a step multiplies with, besides the arguments: the gradients' scale, 1 / sqrt(1 - b2^t), -lr / (1 - b1^t), 1 - lr wd.
+// What a step multiplies with, besides the arguments: the gradients' scale, 1 / sqrt(1 - b2^t) and -lr / (1 - b1^t) (both times `up`), 1 - lr wd.
 struct Factors { float gs, c2, rate, keep; };
 
 // Which elements of a warp's 256 a lane has: 8 in a row where they are 16 bytes at most; else four and four, so that the warp's loads of 16 bytes touch every sector once (8 fp32
@@ -323,7 +325,7 @@ __global__ void __launch_bounds__(THREADS, EIGHT && !MASTER ? 4 : 3) adamw_kerne
   const float lr = *a.lr;
   // 1 - b^t = -(e^(t ln b) - 1)
   const float c1 = -1.f / expm1f((float)((double)step * a.log_beta1)), c2 = rsqrtf(-expm1f((float)((double)step * a.log_beta2)));
-  Factors f = {gs, c2, -lr * c1, 1.f};
+  Factors f = {gs, c2 * a.up, -lr * c1 * a.up, 1.f};
   unsigned long long seed_key = 0, key = 0;
   if (EIGHT) seed_key = absorb(absorb(0x243F6A8885A308D3ull, a.seed), (unsigned long long)step);
   int known = -1;
@@ -497,7 +499,7 @@ extern "C" int taurus_adamw_step(taurus_adamw* h, const int64_t* step, const flo
   Launches enqueue = {static_cast<cudaStream_t>(cuda_stream)};
   Args a = {};
   a.tensors = h->tensors; a.step = reinterpret_cast<const long long*>(step); a.lr = lr; a.grad_scale = grad_scale;
-  a.beta1 = (float)beta1; a.rest1 = (float)(1.0 - beta1); a.beta2 = (float)beta2; a.rest2 = (float)(1.0 - beta2); a.eps = (float)eps; a.small_eps = eps < 1e-11;
+  a.beta1 = (float)beta1; a.rest1 = (float)(1.0 - beta1); a.beta2 = (float)beta2; a.rest2 = (float)(1.0 - beta2); a.up = (float)eps < 0x1p-100f ? 0x1p24f : 1.f; a.eps = (float)eps * a.up; a.small_eps = eps < 1e-11;
   a.log_beta1 = std::log(beta1); a.log_beta2 = std::log(beta2); a.seed = seed; a.status = status;
   for (int k = 0; k < KINDS; ++k) {
     if (!h->tiles[k]) continue;

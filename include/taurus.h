@@ -611,7 +611,7 @@ int taurus_residual_norm_grad(int64_t n, int32_t width, const void* res, int64_t
  *     param = param - lr weight_decay param - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
  * taurus_adamw_create checks a list of tensors once and keeps it in device memory (it allocates and blocks; not while a stream is being captured); taurus_adamw_step does one step for all of
  * them, a launch for each combination of param_type, grad_type, state_type and whether there is a master, asynchronous, capturable.  The arrays stay the caller's and where they are until
- * taurus_adamw_destroy (which waits for the device); a graph that holds a step is not replayed after it.  What is written (param, m, v, scales, master) shares no byte
+ * taurus_adamw_destroy (which waits for the device, and may be called while a stream is being captured); a graph that holds a step is not replayed after it.  What is written (param, m, v, scales, master) shares no byte
  * with any other array of the list; gradients may share with each other.  Arrays need no alignment beyond their element's; at multiples of 16 bytes they are the fast ones.
  *   param, grad: `count` elements of param_type and grad_type (TAURUS_F32, TAURUS_BF16, TAURUS_F16); a tensor with count 0, or without a gradient (NULL), is left alone
  *   master:      NULL, or the parameters in fp32 beside param of 16 bits: the step is made on master, and param receives it rounded

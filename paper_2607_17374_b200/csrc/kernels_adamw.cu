@@ -517,6 +517,13 @@ extern "C" int taurus_adamw_step(taurus_adamw* h, const int64_t* step, const flo
 
 extern "C" void taurus_adamw_destroy(taurus_adamw* h) {
   if (!h) return;
-  if (h->tensors) cudaFree(h->tensors);
+  if (h->tensors) {
+    // A list may go at any time, in a program with a garbage collector also while a stream is being captured, in this thread or another: memory may be freed then by a thread that says so, and
+    // the capture stays valid.
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    if (cudaFree(h->tensors) != cudaSuccess) cudaGetLastError();
+    cudaThreadExchangeStreamCaptureMode(&mode);
+  }
   delete h;
 }

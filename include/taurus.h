@@ -563,7 +563,7 @@ int taurus_norm_rows_grad(int64_t n, int64_t graphs, const int64_t* offsets, con
  *   top_logprob[i * k + r], top_class[i * k + r] = the r-th largest log p and its class, r in [0, k), k in 0 .. TAURUS_MAX_TOP; of equal logits the lowest class comes first
  * Each of the outputs may be NULL (logprob needs labels; with k > 0 one of the two tops at least is there).  A logit of -inf masks its class: its probability is 0, it is not among the top, whose
  * places behind the last class hold -inf and -1.  A row with no other logits has l = 0, entropy 0 and log probabilities of -inf.  A row that holds a NaN or +inf
- * has NaN in every output but the classes, which are in the order of the values that are numbers.
+ * has NaN in every output but the classes, which are in the order of the values that are numbers.  Probabilities below 2^-126 count as 0, in the gradient too.
  * taurus_class_logprob_train also forms the gradient of the logits, for weights of the rows that are known ahead, in one pass where the rows are short:
  *   grad_logits[i][j] = grad_logprob[i] ([j = label] - p_j) - grad_entropy[i] p_j (log p_j + entropy[i])         (logits' type; 0 for masked classes)
  * (either weight may be NULL: zeros; a row without a label takes no part of grad_logprob).  taurus_class_logprob_grad forms it from stats, and entropy where there is a
@@ -618,7 +618,8 @@ int taurus_residual_norm_grad(int64_t n, int32_t width, const void* res, int64_t
  *   state_type:  TAURUS_F32: m and v are fp32, m_scale and v_scale NULL.  TAURUS_E4M3: m and sqrt(v) (of fp32, rounded to nearest) are e4m3 codes, m_scale and v_scale hold a power of two for each block of
  *                TAURUS_STATE_BLOCK elements (the last one may be short); codes and scales of zeros begin.  Written, a block's scale puts its largest value into [2^7, 2^8); values
  *                are rounded up with the probability of what is cut off, by a hash of (seed, step, the tensor's place in the list, element), so that the same call gives the same bits;
- *                an sqrt(v) that is not 0 is not rounded to 0.  The step itself is made from m and v before they are rounded.  Values that are not finite become NaN.
+ *                an sqrt(v) that is not 0 is not rounded to 0.  The step itself is made from m and v before they are rounded.  Values that are not finite become NaN.  sqrt(v) is rounded without
+ *                bias; its square v gains the rounding's variance, some 4 % of v.
  * step: the number of this step, from 1 on; lr: learning rate; grad_scale: NULL for 1 (device memory all three, so that a captured step can be replayed with others).  A *step below 1 changes
  * nothing and gives TAURUS_ERR_INVALID_ARG in *status; a *grad_scale that is not finite (gradients that overflowed) changes nothing.  beta1, beta2 in [0, 1), eps > 0 (as fp32).
  * The step is made on the device that was current at creation, which has to be current.  Steps of one list do not run at the same time.

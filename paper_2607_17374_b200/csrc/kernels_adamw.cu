@@ -4,7 +4,7 @@
 //   p = p - lr wd p - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
 //
 // Bytes are the floor: 28 an element with everything in fp32, 10.06 with parameters and gradients in 16 bits and states in 8.  They bound the first (60 M elements in 269 us, 6.2 TB/s); the second is
-// bound by instructions, 66 an element of which 24 go at half rate (200 M elements in 502 us, 4.0 TB/s, issue slots 72 % used; the next tile's bytes on their way ahead 566 against 512, pairs in one instruction spilled).  All tensors are cut into tiles of 2 048
+// bound by instructions, 68 an element of which 26 go at half rate (200 M elements in 516 us, 3.9 TB/s, issue slots 72 % used; the next tile's bytes on their way ahead 566 against 512, pairs in one instruction spilled).  All tensors are cut into tiles of 2 048
 // elements, which the blocks of one launch (for each combination of types) take in turn: a tensor costs no launch, and its description and a tile's tensor are read from device memory.
 //
 // States in 8 bits: m and r = sqrt(v), rounded to nearest in fp32, as e4m3 codes times a power of two for each 256 elements, one warp's.  With the scale the largest code is in [2^7, 2^8), the
@@ -54,6 +54,7 @@ struct Args {
   int32_t* status;
 };
 
+// The finaliser of the published generator splitmix64 (Steele, Lea, Flood; constants of Stafford's variant 13), with its increment in absorb().
 __device__ __forceinline__ unsigned long long mix64(unsigned long long z) {
   z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
   z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
@@ -96,7 +97,8 @@ __device__ __forceinline__ uint32_t code_of_root(float root, float part_v, float
 }
 // The hardware's root is off by 2^-23 of itself at most: from the one rounded to nearest by two and a half units in its last place, three where they are cut off, of 16 each here.  It makes another
 // code only where the sum is that near to a border between two codes, on either side; 64 with a margin.  Such elements, one in 131 072, are done again with the root rounded to nearest, so that a
-// code is what its definition says and not what an instruction makes of it (200 M elements 496 -> 518 us; looked for by 16-bit halves 525, done again where they are found 549).
+// code is what its definition says and not what an instruction makes of it (without it 20 codes of 200 M are a neighbour's, and they take 496 us instead of 516; borders looked for by 16-bit halves 525,
+// codes done again where they are found 549, from the state read again 536).
 __device__ __forceinline__ uint32_t from_border(uint32_t code) { return code * 256u + 0x4000u; }
 constexpr uint32_t AT_BORDER = 0x8000u;
 // The root of v rounded to nearest, from one that is a few units off: the middle between two neighbours has 25 bits, its square 50, which fp64 holds.

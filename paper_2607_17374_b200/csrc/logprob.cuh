@@ -207,7 +207,7 @@ __device__ __forceinline__ uint32_t pack(const float (&x)[2]) {
 
 }  // namespace
 
-// Short rows of a call, many of them (kernels_logprob_rows.cu).  mode: FORWARD, TRAIN or GRAD; pairs: rows of 16-bit elements by twos.  A launch that fails is kept in `enqueue`.
+// Short rows of a call, many of them (logprob_rows.cuh, a file for each type).  mode: FORWARD, TRAIN or GRAD; pairs: rows of 16-bit elements by twos.  A launch that fails is kept in `enqueue`.
 void logprob_rows_f32(Launches& enqueue, const LogprobArgs& a, int mode);
 void logprob_rows_bf16(Launches& enqueue, const LogprobArgs& a, int mode, bool pairs);
 void logprob_rows_f16(Launches& enqueue, const LogprobArgs& a, int mode, bool pairs);

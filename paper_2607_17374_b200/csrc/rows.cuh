@@ -87,14 +87,14 @@ struct Launches {
   bool early = false;
   template <class... P, class... A>
   void operator()(void (*kernel)(P...), dim3 grid, int threads, size_t smem, A... args) {
+    if (error != cudaSuccess) return;            // a kernel behind one that did not run would take what stands in the workspace for indexes
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid; cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cfg.attrs = &at; cfg.numAttrs = early ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
-    if (e != cudaSuccess && error == cudaSuccess) error = e;
+    error = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
     early = true;
   }
   cudaError_t error = cudaSuccess;

@@ -562,6 +562,13 @@ extern "C" int taurus_embed_rows(int64_t n, const int64_t* ids, const void* tabl
   return TAURUS_OK;
 }
 
+// Has the launch in front gone through?  A kernel behind one that has not would take what stands in the workspace for places of rows.
+static bool launched() {
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) taurus_note_cuda_error(e, "embed_grad");
+  return e == cudaSuccess;
+}
+
 extern "C" int64_t taurus_embed_grad_workspace(int64_t n, int64_t table_rows, int32_t width) {
   if (!table_shape_ok(n, table_rows, width, width, width)) return TAURUS_ERR_INVALID_ARG;
   if (width > TAURUS_MAX_ROW_WIDTH) return TAURUS_ERR_UNSUPPORTED;
@@ -616,12 +623,16 @@ extern "C" int taurus_embed_grad(int64_t n, const int64_t* ids, const void* grad
         while (key < 32 && (table_rows >> key) > 0) ++key;
         // (what fills the block up is all ones and starts behind the items: it stays there)
         embed_sort_small_kernel<<<1, SMALL_THREADS, 0, st>>>(q, (key + 7) / 8);
+        if (!launched()) return TAURUS_ERR_CUDA;
         break;
       }
       q.shift = pass * plan.bits;
       embed_count_kernel<<<plan.blocks, SORT_THREADS, 0, st>>>(q);
+      if (!launched()) return TAURUS_ERR_CUDA;
       embed_scan_kernel<<<((1 << plan.bits) + 31) / 32, SCAN_THREADS, 0, st>>>(q.hist, totals, 1 << plan.bits, plan.blocks);
+      if (!launched()) return TAURUS_ERR_CUDA;
       embed_move_kernel<<<plan.blocks, SORT_THREADS, 0, st>>>(q, totals);
+      if (!launched()) return TAURUS_ERR_CUDA;
       q.ids = nullptr;
       q.key_in = q.key_out; q.pos_in = q.pos_out;
     }
@@ -642,6 +653,7 @@ extern "C" int taurus_embed_grad(int64_t n, const int64_t* ids, const void* grad
             if (nc == 2) embed_sum_kernel<G, T, V, 2><<<grid, GRAD_THREADS, 0, st>>>(a, g, t);
           }
           if (nc == 1) embed_sum_kernel<G, T, V, 1><<<grid, GRAD_THREADS, 0, st>>>(a, g, t);
+          if (!launched()) return (int)TAURUS_ERR_CUDA;
           if (a.pieces > 1) embed_join_kernel<T, V><<<dim3((unsigned)std::min((a.pieces - 1 + JOIN_WARPS - 1) / JOIN_WARPS, sms * 4), (unsigned)((a.vpr + 31) / 32)), JOIN_THREADS, 0, st>>>(a, t);
           return (int)TAURUS_OK;
         }
@@ -649,7 +661,5 @@ extern "C" int taurus_embed_grad(int64_t n, const int64_t* ids, const void* grad
     });
   });
   if (rc) return rc;
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) { taurus_note_cuda_error(e, "embed_grad"); return TAURUS_ERR_CUDA; }
-  return TAURUS_OK;
+  return launched() ? TAURUS_OK : TAURUS_ERR_CUDA;
 }

@@ -25,9 +25,12 @@ cudaError_t cudaPointerGetAttributes(struct cudaPointerAttributes* a, const void
 }
 cudaError_t cudaFuncSetAttribute(const void*, enum cudaFuncAttribute, int) { return attributes_fail ? cudaErrorInvalidValue : cudaSuccess; }
 cudaError_t cudaOccupancyMaxActiveBlocksPerMultiprocessorWithFlags(int* n, const void*, int, size_t, unsigned) { *n = 2; return cudaSuccess; }
-cudaError_t cudaLaunchKernelExC(const cudaLaunchConfig_t*, const void*, void**) { return launches++ == failing ? cudaErrorMemoryAllocation : cudaSuccess; }
+static cudaError_t last = cudaSuccess;
+static cudaError_t launch() { return launches++ == failing ? last = cudaErrorMemoryAllocation : cudaSuccess; }
+cudaError_t cudaLaunchKernelExC(const cudaLaunchConfig_t*, const void*, void**) { return launch(); }
+cudaError_t cudaLaunchKernel(const void*, dim3, dim3, void**, size_t, cudaStream_t) { return launch(); }
 cudaError_t cudaMemsetAsync(void*, int, size_t, cudaStream_t) { return cudaSuccess; }
-cudaError_t cudaGetLastError(void) { return cudaSuccess; }
+cudaError_t cudaGetLastError(void) { const cudaError_t e = last; last = cudaSuccess; return e; }
 }
 
 int main() {
@@ -44,6 +47,8 @@ int main() {
       {"class_logprob_train in parts", 3, 0, [&] { return taurus_class_logprob_train(3, 100000, at(0), 100000, 0, l(1), f(2), f(3), f(4), f(5), f(6), at(8), 100000, at(7), space, nullptr, nullptr); }},
       {"norm_rows", 0, 0, [&] { return taurus_norm_rows(100000, 3, l(0), at(1), 64, 0, 64, 8, f(2), f(3), 1e-5f, 0, at(4), 64, f(5), f(7), at(6), space, nullptr, nullptr); }},
       {"norm_rows_grad", 0, 0, [&] { return taurus_norm_rows_grad(100000, 3, l(0), at(1), 64, 0, 64, 8, f(2), f(3), 0, f(5), f(7), at(8), 64, at(9), 64, f(10), f(11), at(6), space, nullptr, nullptr); }},
+      {"embed_grad, few ids", 0, 0, [&] { return taurus_embed_grad(1000, l(0), at(1), 0, 64, 64, 1.f, at(2), 0, 5000, 64, at(3), space, nullptr, nullptr); }},
+      {"embed_grad", 0, 0, [&] { return taurus_embed_grad(3000000, l(0), at(1), 0, 64, 64, 1.f, at(2), 0, 10000000, 64, at(3), space, nullptr, nullptr); }},
   };
   for (auto& c : calls) {
     attributes_fail = false;
